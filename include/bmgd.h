@@ -285,6 +285,102 @@ int bmgd_debug_null_rounds(bmgd_t* h, int64_t rows, int32_t rounds, int32_t batc
  * path without hanging or faulting a GPU.  Not for softmax handles. */
 int bmgd_debug_wait_timeout(bmgd_t* h, double budget_ms);
 
+/*
+ * ---- Operators on device tensors: one training step of a gated network on a mini-batch ----
+ *
+ * The step kernels above train one linear layer.  The calls below are the parts of a step for a model with a hidden
+ * layer (Sections 4.3 and 4.4 run the same buffering over networks): gather a mini-batch of the shuffled buffer,
+ * the gated block forward, the softmax loss with its gradient, the block backward, the update of all weights.
+ * They need no handle: every pointer is memory of the calling thread's current device, work is ordered on `stream`
+ * (a cudaStream_t; NULL = the legacy default stream), nothing is allocated on the device, and nothing waits for the
+ * device, so each call can be captured into a graph.  Matrices are row-major with a row stride `ld` counted in values.
+ * Any thread may call; calls that share no memory may overlap on different streams.  Outputs must not overlap inputs.
+ */
+
+/* Element types of these operators. */
+enum { BMGD_TYPE_F32 = 0, BMGD_TYPE_BF16 = 1, BMGD_TYPE_F16 = 2 };
+
+/* act(g): g s, g Phi(g), max(g, 0), s, with s = 1 / (1 + exp(-g)) and Phi the normal distribution function. */
+enum { BMGD_ACT_SILU = 0, BMGD_ACT_GELU = 1, BMGD_ACT_RELU = 2, BMGD_ACT_SIGMOID = 3 };
+enum { BMGD_FFN_FORWARD = 0, BMGD_FFN_BACKWARD = 1 };
+
+/* Gated feed-forward block: Y = (act(X Wg) * (X Wu)) Wd, X [rows][inputs], Wg and Wu [inputs][hidden],
+ * Wd [hidden][outputs], all of one type (BF16 or F16; F32 returns BMGD_ERR_UNIMPLEMENTED), sums in fp32.  Any sizes
+ * from 1 (rows from 0) and any row strides; operands whose rows do not start on 16-byte boundaries are copied into
+ * the workspace first. */
+typedef struct bmgd_gated_ffn {
+    int64_t rows;
+    int32_t inputs, hidden, outputs;
+    int32_t type;                        /* BMGD_TYPE_BF16 or BMGD_TYPE_F16 */
+    int32_t activation;                  /* BMGD_ACT_* */
+    int32_t reserved;                    /* must be zero */
+    const void *x, *w_gate, *w_up, *w_down;
+    int64_t ld_x, ld_gate, ld_up, ld_down;
+    void* y;                             /* forward: [rows][outputs], stride ld_y */
+    int64_t ld_y;
+    void *saved_gate, *saved_up;         /* [rows][hidden], 16-byte aligned, stride ld_saved (a multiple of 8): X Wg and X Wu, written by the
+                                            forward pass (both NULL: not wanted) and read by the backward pass */
+    int64_t ld_saved;
+    const void* dy;                      /* backward: gradient of Y, stride ld_dy */
+    int64_t ld_dy;
+    void *dx, *dw_gate, *dw_up, *dw_down; /* backward: gradients, contiguous, shaped like X, Wg, Wu and Wd */
+} bmgd_gated_ffn;
+
+/* Bytes of workspace (device memory, 256-byte aligned, free for reuse once the stream has passed the call) of a pass. */
+int bmgd_gated_ffn_workspace_bytes(const bmgd_gated_ffn* g, int32_t pass, int64_t* bytes);
+int bmgd_gated_ffn_forward(const bmgd_gated_ffn* g, void* workspace, int64_t workspace_bytes, void* stream);
+/* The weights' gradients are sums over the rows in a fixed order: equal calls give equal bits.  rows = 0 gives zeros. */
+int bmgd_gated_ffn_backward(const bmgd_gated_ffn* g, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Softmax loss with its gradient for rows of logits [rows][C] and labels y: residual = scale (softmax - onehot(y)) in
+ * the type of the logits, loss = logsumexp - logit of the label in fp32 (dev_loss may be NULL).  A row whose label is
+ * outside [0, C), or whose logits are all -Inf, counts for nothing: residual zero, loss 0.  NaN and +Inf give NaN rows. */
+int bmgd_softmax_residual(const void* dev_logits, int64_t ld_logits, const int32_t* dev_y, int64_t rows, int32_t C,
+                          int32_t type, double scale, void* dev_residual, int64_t ld_residual, float* dev_loss, void* stream);
+
+/* Rows pi(first), ..., pi(first + count - 1) of a buffer of `rows` contiguous rows of row_bytes bytes, and their int32
+ * labels (dev_y may be NULL), to contiguous memory: pi is the shuffle of round `round` of chain `chain` under `seed`,
+ * the one bmgd_run_rounds draws its mini-batches from. */
+int bmgd_gather_batch(const void* dev_x, int64_t row_bytes, const int32_t* dev_y, int64_t rows, uint64_t seed, uint32_t chain,
+                      uint32_t round, int64_t first, int64_t count, void* dev_out_x, int32_t* dev_out_y, void* stream);
+
+/* One AdamW update (Loshchilov & Hutter 2019; the decay apart from it is BMGD_OPT_ADAM) of many tensors.  With g the
+ * gradient times grad_scale and, if max_norm > 0, times min(1, max_norm / (norm + 1e-6)), norm that of all gradients
+ * together, and t the number of this update:
+ *   m <- a m + (1-a) g;  v <- b v + (1-b) g^2;
+ *   theta <- theta (1 - lr weight_decay) - lr (m / (1-a^t)) / (sqrt(v / (1-b^t)) + eps)
+ * An update whose norm is not finite (max_norm > 0 only) is left out: nothing but its count changes. */
+typedef struct bmgd_adamw_tensor {
+    void* param;             /* theta: F32, BF16 or F16 */
+    const void* grad;        /* any of the three types */
+    void* m;                 /* moments: fp32, or codes of 8 bits */
+    void* v;
+    void* m_scale;           /* state_bits 8: one byte for each 256 values of m and of v (the last block may be partial) */
+    void* v_scale;
+    void* master;            /* fp32 copy of theta that the update runs on, theta being its rounding; F16 needs one, BF16
+                                may do without (theta is then rounded at random, keeping the mean), F32 has none */
+    int64_t count;           /* values; 0 is allowed */
+    double weight_decay;
+    int32_t param_type, grad_type, state_bits, index; /* state_bits 32 or 8; index: part of the key of the random rounding */
+} bmgd_adamw_tensor;
+typedef struct bmgd_adamw_config {
+    double lr, a, b, eps, grad_scale, max_norm;
+    uint64_t seed;           /* of the random rounding (moments in 8 bits, BF16 without a copy) */
+} bmgd_adamw_config;
+/* Four 64-bit words of device memory, zero at first, that belong to one set of tensors: updates taken, updates left
+ * out, a word of the kernel's own, and (max_norm > 0) the bits of the norm as a double. */
+#define BMGD_ADAMW_CONTROL_BYTES 32
+/* Scratch (max_norm > 0 only) for `count` tensors: BMGD_ADAMW_SCRATCH_BYTES(count), 8-byte aligned. */
+#define BMGD_ADAMW_SCRATCH_BYTES(count) ((int64_t)(1 + (count) / 360) * 1184 * 8)
+/* BMGD_ERR_ARG if tensors that are written overlap one another or a gradient.  Hyper-parameters are those of the call:
+ * a captured update repeats them, while t goes on. */
+int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_adamw_config* cfg, void* dev_control,
+                    void* dev_scratch, int64_t scratch_bytes, void* stream);
+
+/* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block kernel on the current
+ * device gave up since the last report: the outputs of that call are void. */
+int bmgd_stream_check(void* stream);
+
 /* Text for a bmgd_status; never NULL. */
 const char* bmgd_strerror(int status);
 /* cudaError_t of the last failed runtime call on this handle (0 if none). */

@@ -33,6 +33,8 @@ EXPORTS = (
     "bmgd_set_theta", "bmgd_get_stats", "bmgd_debug_perm", "bmgd_strerror", "bmgd_last_cuda_error",
     "bmgd_version", "bmgd_run_rounds_noalloc", "bmgd_debug_wait_timeout", "bmgd_partition_index", "bmgd_gather_buffer",
     "bmgd_set_optimizer", "bmgd_set_lr_schedule", "bmgd_set_timeout", "bmgd_debug_null_rounds",
+    "bmgd_gated_ffn_workspace_bytes", "bmgd_gated_ffn_forward", "bmgd_gated_ffn_backward", "bmgd_softmax_residual",
+    "bmgd_gather_batch", "bmgd_adamw_step", "bmgd_stream_check",
 )
 
 OPT_SGD, OPT_NESTEROV, OPT_ADAM = 0, 1, 2
@@ -116,6 +118,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.bmgd_partition_index.argtypes = [u64, u32, i64, i64, P(i64)]
     L.bmgd_gather_buffer.argtypes = [vp, vp, i64, i64, i64, i32, u64, u32, i32, vp, vp, i32, P(i64)]
     L.bmgd_run_rounds_noalloc.argtypes = [vp, vp, i64, i32, i32, i32, i32, vp, i32, i32, dbl, u64, vp]
+    L.bmgd_gated_ffn_workspace_bytes.argtypes = [vp, i32, P(i64)]
+    L.bmgd_gated_ffn_forward.argtypes = [vp, vp, i64, vp]
+    L.bmgd_gated_ffn_backward.argtypes = [vp, vp, i64, vp]
+    L.bmgd_softmax_residual.argtypes = [vp, i64, vp, i64, i32, i32, dbl, vp, i64, vp, vp]
+    L.bmgd_gather_batch.argtypes = [vp, i64, vp, i64, u64, u32, u32, i64, i64, vp, vp, vp]
+    L.bmgd_adamw_step.argtypes = [vp, i32, vp, vp, vp, i64, vp]
+    L.bmgd_stream_check.argtypes = [vp]
     for name in EXPORTS:
         if getattr(L, name).restype is None or name in ("bmgd_strerror",):
             continue

@@ -1,0 +1,60 @@
+// Host side of bmgd_softmax_residual and bmgd_gather_batch.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/bmgd.h"
+#include "residual_kernel.cuh"
+
+namespace {
+
+using namespace bmgdk;
+
+int launched() { return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA; }
+
+template <typename T>
+int residual(const void* z, int64_t ldz, const int32_t* y, void* out, int64_t ldo, float* loss, int64_t rows, int32_t C,
+             float scale, cudaStream_t s) {
+    const int grid = (int)std::min<int64_t>(rows, 148 * 64);
+    residual_rows_kernel<T><<<grid, 256, 0, s>>>(static_cast<const T*>(z), ldz, y, static_cast<T*>(out), ldo, loss, rows, C, scale);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int bmgd_softmax_residual(const void* dev_logits, int64_t ld_logits, const int32_t* dev_y, int64_t rows, int32_t C, int32_t type,
+                          double scale, void* dev_residual, int64_t ld_residual, float* dev_loss, void* stream) {
+    if (rows < 0 || rows > 0x7FFFFFFFll || C < 1 || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16 || !std::isfinite(scale)) return BMGD_ERR_ARG;
+    if (rows == 0) return BMGD_OK;
+    if (!dev_logits || !dev_y || !dev_residual || ld_logits < C || ld_residual < C) return BMGD_ERR_ARG;
+    const int eb = type == BMGD_TYPE_F32 ? 4 : 2;
+    if ((uintptr_t)dev_logits % eb || (uintptr_t)dev_residual % eb || (uintptr_t)dev_y % 4 || (uintptr_t)dev_loss % 4) return BMGD_ERR_ARG;
+    const uintptr_t z = (uintptr_t)dev_logits, o = (uintptr_t)dev_residual;  // the label's logit is read after its row is written
+    if (z < o + (uintptr_t)(((rows - 1) * ld_residual + C) * eb) && o < z + (uintptr_t)(((rows - 1) * ld_logits + C) * eb)) return BMGD_ERR_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const float f = (float)scale;
+    if (type == BMGD_TYPE_F32) return residual<float>(dev_logits, ld_logits, dev_y, dev_residual, ld_residual, dev_loss, rows, C, f, s);
+    if (type == BMGD_TYPE_BF16) return residual<__nv_bfloat16>(dev_logits, ld_logits, dev_y, dev_residual, ld_residual, dev_loss, rows, C, f, s);
+    return residual<__half>(dev_logits, ld_logits, dev_y, dev_residual, ld_residual, dev_loss, rows, C, f, s);
+}
+
+int bmgd_gather_batch(const void* dev_x, int64_t row_bytes, const int32_t* dev_y, int64_t rows, uint64_t seed, uint32_t chain,
+                      uint32_t round, int64_t first, int64_t count, void* dev_out_x, int32_t* dev_out_y, void* stream) {
+    if (rows < 1 || rows > 0x7FFFFFFFll || row_bytes < 1 || first < 0 || count < 0 || first > rows || count > rows - first) return BMGD_ERR_ARG;
+    if (count == 0) return BMGD_OK;
+    if (!dev_x || !dev_out_x || (dev_y && !dev_out_y) || (uintptr_t)dev_y % 4 || (uintptr_t)dev_out_y % 4) return BMGD_ERR_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int grid = (int)std::min<int64_t>((count + 7) / 8, 148 * 8);
+    const unsigned char* x = static_cast<const unsigned char*>(dev_x);
+    unsigned char* o = static_cast<unsigned char*>(dev_out_x);
+    const uintptr_t low = (uintptr_t)dev_x | (uintptr_t)dev_out_x | (uintptr_t)row_bytes;
+    const uint32_t n0 = (uint32_t)rows, a = (uint32_t)first, n = (uint32_t)count;
+    if (low % 16 == 0) gather_batch_kernel<uint4><<<grid, 256, 0, s>>>(x, row_bytes, dev_y, n0, seed, chain, round, a, n, o, dev_out_y);
+    else if (low % 4 == 0) gather_batch_kernel<uint32_t><<<grid, 256, 0, s>>>(x, row_bytes, dev_y, n0, seed, chain, round, a, n, o, dev_out_y);
+    else if (low % 2 == 0) gather_batch_kernel<uint16_t><<<grid, 256, 0, s>>>(x, row_bytes, dev_y, n0, seed, chain, round, a, n, o, dev_out_y);
+    else gather_batch_kernel<unsigned char><<<grid, 256, 0, s>>>(x, row_bytes, dev_y, n0, seed, chain, round, a, n, o, dev_out_y);
+    return launched();
+}
+
+}  // extern "C"

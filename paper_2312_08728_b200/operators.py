@@ -1,0 +1,344 @@
+"""Operators of one training step of a gated network, on device tensors.
+
+    rows, labels = gather_batch(x, y, seed, chain, round, first, count)      the mini-batch of the shuffled buffer
+    logits, saved = gated_ffn(rows, w_gate, w_up, w_down, save=True)         (act(X Wg) * (X Wu)) Wd
+    residual, loss = softmax_residual(logits, labels)                        softmax loss and its gradient
+    dx, dw_gate, dw_up, dw_down = gated_ffn_backward(residual, rows, w_gate, w_up, w_down, saved)
+    adamw_step([w_gate, w_up, w_down], [dw_gate, dw_up, dw_down], m, v, control, lr=1e-3)
+
+Argument checks and marshalling only: the computation runs in the CUDA library (include/bmgd.h), which takes bare
+pointers, so whatever the tensors' own metadata can tell is refused here.  Work is ordered on `stream`, by default the
+current stream of the tensors' device; nothing waits for the device, so every call can be captured into a CUDA graph.
+Outputs and workspaces come from torch's allocator on that stream.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from array import array
+from typing import List, Optional, Sequence, Tuple, Union
+
+import torch
+
+from . import binding as _binding
+from .binding import BMGD_OK, BmgdError
+
+ACT_SILU, ACT_GELU, ACT_RELU, ACT_SIGMOID = 0, 1, 2, 3
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+SCALE_BLOCK = 256       # values that share a scale where moments are held in 8 bits
+CONTROL_WORDS = 4
+
+_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+
+
+def _status(rc: int, where: str) -> None:
+    if rc != BMGD_OK:
+        raise BmgdError(rc, where)
+
+
+@contextlib.contextmanager
+def _other(device: torch.device, stream: Optional[torch.cuda.Stream]):
+    with torch.cuda.device(device):
+        if stream is None:
+            yield
+        else:
+            with torch.cuda.stream(stream):
+                yield
+
+
+def _place(device: torch.device, stream: Optional[torch.cuda.Stream]):
+    """Context in which outputs are allocated and kernels launched: the tensors' device, on the stream that orders them."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors live on {device}")
+    if stream is None and torch.cuda.current_device() == device.index:
+        return contextlib.nullcontext()
+    return _other(device, stream)
+
+
+def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int], dtype: torch.dtype, device: torch.device) -> int:
+    """Refuse a tensor that is not a [rows, cols] matrix with contiguous rows; returns its row stride."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        want = ", ".join("any" if n is None else str(n) for n in (rows, cols))
+        raise ValueError(f"{name} must be [{want}], got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}, got {t.device}")
+    n, c = t.shape
+    s0, s1 = t.stride()
+    if c > 1 and s1 != 1:
+        raise ValueError(f"{name} must have contiguous rows, got strides {(s0, s1)}")
+    if n <= 1:
+        return max(c, 1)
+    if s0 < c:
+        raise ValueError(f"{name} has rows that overlap: stride {s0} for {c} columns")
+    return s0
+
+
+def _device_of(t: torch.Tensor, name: str) -> torch.device:
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a device tensor; there is no CPU path")
+    return t.device
+
+
+# ---------------------------------------------------------------- gated feed-forward block
+
+class _GatedFfn(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(k, ctypes.c_int32) for k in (
+        "inputs", "hidden", "outputs", "type", "activation", "reserved")] + [(k, ctypes.c_void_p) for k in (
+            "x", "w_gate", "w_up", "w_down")] + [(k, ctypes.c_int64) for k in ("ld_x", "ld_gate", "ld_up", "ld_down")] + [
+        ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("saved_gate", ctypes.c_void_p), ("saved_up", ctypes.c_void_p),
+        ("ld_saved", ctypes.c_int64), ("dy", ctypes.c_void_p), ("ld_dy", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in (
+            "dx", "dw_gate", "dw_up", "dw_down")]
+
+
+_FORWARD, _BACKWARD = 0, 1
+
+
+def _ffn_args(x, w_gate, w_up, w_down, activation) -> _GatedFfn:
+    device = _device_of(x, "x")
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"x must be bfloat16 or float16, got {x.dtype}")
+    if activation not in (ACT_SILU, ACT_GELU, ACT_RELU, ACT_SIGMOID):
+        raise ValueError(f"unknown activation code {activation}")
+    g = _GatedFfn()
+    g.ld_x = _matrix(x, "x", None, None, x.dtype, device)
+    n, d = x.shape
+    g.ld_gate = _matrix(w_gate, "w_gate", d, None, x.dtype, device)
+    f = w_gate.shape[1]
+    g.ld_up = _matrix(w_up, "w_up", d, f, x.dtype, device)
+    g.ld_down = _matrix(w_down, "w_down", f, None, x.dtype, device)
+    c = w_down.shape[1]
+    if min(d, f, c) < 1:
+        raise ValueError("the block needs at least one input, one hidden unit and one output")
+    g.rows, g.inputs, g.hidden, g.outputs, g.type, g.activation = n, d, f, c, _TYPES[x.dtype], activation
+    g.x, g.w_gate, g.w_up, g.w_down = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()
+    return g
+
+
+def _workspace(L, g: _GatedFfn, which: int, device: torch.device) -> Tuple[torch.Tensor, int]:
+    need = ctypes.c_int64()
+    _status(L.bmgd_gated_ffn_workspace_bytes(ctypes.byref(g), which, ctypes.byref(need)), "bmgd_gated_ffn_workspace_bytes")
+    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+
+
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: int = ACT_SILU,
+              save: bool = False, stream: Optional[torch.cuda.Stream] = None):
+    """(act(x w_gate) * (x w_up)) w_down for x [rows, inputs], w_gate and w_up [inputs, hidden], w_down [hidden, outputs].
+
+    All four in bfloat16 or all in float16; rows contiguous, any row stride.  With save=True returns (y, saved), saved
+    being what gated_ffn_backward needs beside its other arguments."""
+    g = _ffn_args(x, w_gate, w_up, w_down, activation)
+    L = _binding.load_library()
+    with _place(x.device, stream):
+        y = torch.empty(g.rows, g.outputs, dtype=x.dtype, device=x.device)
+        saved = None
+        if save:
+            saved = torch.empty(2, g.rows, -(-g.hidden // 8) * 8, dtype=x.dtype, device=x.device)
+            g.saved_gate, g.ld_saved = saved.data_ptr(), saved.shape[2]
+            g.saved_up = saved.data_ptr() + saved.shape[1] * saved.shape[2] * 2
+        if g.rows > 0:
+            g.y, g.ld_y = y.data_ptr(), g.outputs
+            w, size = _workspace(L, g, _FORWARD, x.device)
+            _status(L.bmgd_gated_ffn_forward(ctypes.byref(g), w.data_ptr(), size, torch.cuda.current_stream().cuda_stream),
+                    "bmgd_gated_ffn_forward")
+    return (y, saved) if save else y
+
+
+def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                       saved: torch.Tensor, activation: int = ACT_SILU, stream: Optional[torch.cuda.Stream] = None):
+    """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the gradient dy of its output.
+
+    `saved` is what the forward call on the same arguments returned; the gradients have the type of x."""
+    g = _ffn_args(x, w_gate, w_up, w_down, activation)
+    g.ld_dy = _matrix(dy, "dy", g.rows, g.outputs, x.dtype, x.device)
+    width = -(-g.hidden // 8) * 8
+    if saved.shape != (2, g.rows, width) or saved.dtype != x.dtype or saved.device != x.device or not saved.is_contiguous():
+        raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
+    L = _binding.load_library()
+    with _place(x.device, stream):
+        dx, dw_gate, dw_up, dw_down = (torch.empty(s, dtype=x.dtype, device=x.device)
+                                       for s in (x.shape, w_gate.shape, w_up.shape, w_down.shape))
+        g.dx, g.dw_gate, g.dw_up, g.dw_down = dx.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr(), dw_down.data_ptr()
+        g.dy, g.saved_gate, g.ld_saved = dy.data_ptr(), saved.data_ptr(), width
+        g.saved_up = saved.data_ptr() + g.rows * width * 2
+        w, size = _workspace(L, g, _BACKWARD, x.device)
+        _status(L.bmgd_gated_ffn_backward(ctypes.byref(g), w.data_ptr(), size, torch.cuda.current_stream().cuda_stream),
+                "bmgd_gated_ffn_backward")
+    return dx, dw_gate, dw_up, dw_down
+
+
+def stream_check(stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Wait for the stream and raise if a device-side wait of a gated-block kernel on its device gave up."""
+    s = stream if stream is not None else torch.cuda.current_stream()
+    with torch.cuda.device(s.device):
+        _status(_binding.load_library().bmgd_stream_check(s.cuda_stream), "bmgd_stream_check")
+
+
+# ---------------------------------------------------------------- softmax loss, mini-batch
+
+def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[float] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(residual, loss) for logits [rows, C] and int32 labels y [rows]: scale (softmax - onehot), and the loss per row in
+    fp32.  scale defaults to 1 / rows, the mean gradient of the mini-batch.  Rows without a label in [0, C) give zeros."""
+    device = _device_of(logits, "logits")
+    if logits.dtype not in _TYPES:
+        raise ValueError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")
+    ld = _matrix(logits, "logits", None, None, logits.dtype, device)
+    rows, C = logits.shape
+    if C < 1:
+        raise ValueError("logits need at least one class")
+    if y.dim() != 1 or y.shape[0] != rows or y.dtype != torch.int32 or y.device != device or not y.is_contiguous():
+        raise ValueError(f"y must be a contiguous int32 [{rows}] on {device}")
+    L = _binding.load_library()
+    with _place(device, stream):
+        residual = torch.empty(rows, C, dtype=logits.dtype, device=device)
+        loss = torch.empty(rows, dtype=torch.float32, device=device)
+        if rows > 0:
+            _status(L.bmgd_softmax_residual(logits.data_ptr(), ld, y.data_ptr(), rows, C, _TYPES[logits.dtype],
+                                            1.0 / rows if scale is None else float(scale), residual.data_ptr(), C,
+                                            loss.data_ptr(), torch.cuda.current_stream().cuda_stream), "bmgd_softmax_residual")
+    return residual, loss
+
+
+def gather_batch(x: torch.Tensor, y: Optional[torch.Tensor], seed: int, chain: int, round: int, first: int, count: int,
+                 stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Rows first .. first + count - 1 of one round's order of the buffer x [rows, p], with their int32 labels: the
+    mini-batch that run_rounds would take there (round `round` of chain `chain` under `seed`)."""
+    device = _device_of(x, "x")
+    if x.dim() != 2 or not x.is_contiguous() or x.shape[0] < 1 or x.shape[1] < 1:
+        raise ValueError(f"x must be a contiguous [rows, p] with at least one row, got {tuple(x.shape)}")
+    rows = x.shape[0]
+    if y is not None and (y.dim() != 1 or y.shape[0] != rows or y.dtype != torch.int32 or y.device != device or not y.is_contiguous()):
+        raise ValueError(f"y must be a contiguous int32 [{rows}] on {device}")
+    if first < 0 or count < 0 or first + count > rows:
+        raise ValueError(f"rows {first} to {first + count} of a buffer of {rows}")
+    L = _binding.load_library()
+    with _place(device, stream):
+        bx = torch.empty(count, x.shape[1], dtype=x.dtype, device=device)
+        by = torch.empty(count, dtype=torch.int32, device=device) if y is not None else None
+        _status(L.bmgd_gather_batch(x.data_ptr(), x.shape[1] * x.element_size(), y.data_ptr() if y is not None else None, rows,
+                                    int(seed) & 0xFFFFFFFFFFFFFFFF, int(chain) & 0xFFFFFFFF, int(round) & 0xFFFFFFFF, first, count,
+                                    bx.data_ptr(), by.data_ptr() if by is not None else None,
+                                    torch.cuda.current_stream().cuda_stream), "bmgd_gather_batch")
+    return bx, by
+
+
+# ---------------------------------------------------------------- AdamW
+
+class _AdamwConfig(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_double) for k in ("lr", "a", "b", "eps", "grad_scale", "max_norm")] + [("seed", ctypes.c_uint64)]
+
+
+def adamw_state(params: Sequence[torch.Tensor], state_bits: int = 32) -> dict:
+    """Zero moments and counters for adamw_step: keyword arguments m, v, control and, with 8 bits, m_scale and v_scale."""
+    if state_bits not in (8, 32):
+        raise ValueError("state_bits must be 8 or 32")
+    if not params:
+        raise ValueError("no parameters")
+    out = {"control": torch.zeros(CONTROL_WORDS, dtype=torch.int64, device=params[0].device)}
+    if state_bits == 32:
+        out["m"] = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in params]
+        out["v"] = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in params]
+    else:
+        out["m"] = [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for p in params]
+        out["v"] = [torch.zeros(p.shape, dtype=torch.uint8, device=p.device) for p in params]
+        for k in ("m_scale", "v_scale"):
+            out[k] = [torch.zeros(-(-p.numel() // SCALE_BLOCK), dtype=torch.uint8, device=p.device) for p in params]
+    return out
+
+
+def _column(tensors: Sequence[torch.Tensor], name: str, counts: List[int], types: Sequence[torch.dtype], device: int) -> List[int]:
+    """Refuse a list of tensors that does not match the parameters; returns their addresses."""
+    if len(tensors) != len(counts):
+        raise ValueError(f"{name}: {len(tensors)} tensors for {len(counts)} parameters")
+    if [t.numel() for t in tensors] != counts:
+        raise ValueError(f"{name}: a tensor's size does not match its parameter's")
+    if not {t.dtype for t in tensors} <= set(types):
+        raise ValueError(f"{name} must be {' or '.join(str(t) for t in types)}, got {({t.dtype for t in tensors} - set(types)).pop()}")
+    if any([t.get_device() != device for t in tensors]):
+        raise ValueError(f"{name}: all tensors must live on one device")
+    if not all([t.is_contiguous() for t in tensors]):
+        raise ValueError(f"{name}: tensors must be contiguous")
+    return [t.data_ptr() for t in tensors]
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
+               control: torch.Tensor, lr: float, a: float = 0.9, b: float = 0.999, eps: float = 1e-8,
+               weight_decay: Union[float, Sequence[float]] = 0.0, max_norm: float = 0.0, grad_scale: float = 1.0,
+               m_scale: Optional[Sequence[torch.Tensor]] = None, v_scale: Optional[Sequence[torch.Tensor]] = None,
+               masters: Optional[Sequence[Optional[torch.Tensor]]] = None, seed: int = 0,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+    """One AdamW update of all tensors, in place (formula, types and control words: bmgd_adamw_step in include/bmgd.h).
+
+    params: float32, bfloat16 or float16, contiguous, on one device; grads: any of the three types.  m and v: both
+    float32, or float8_e4m3fn and uint8 with the per-256-values scales m_scale and v_scale (adamw_state makes them); a
+    list may mix the two.  masters: float32 copies (None for a parameter without one).  control: int64 [4]."""
+    count = len(params)
+    if count == 0:
+        raise ValueError("no parameters")
+    device = _device_of(params[0], "params")
+    index = device.index
+    counts = [t.numel() for t in params]
+    columns = [_column(params, "params", counts, tuple(_TYPES), index), _column(grads, "grads", counts, tuple(_TYPES), index),
+               _column(m, "m", counts, (torch.float32, torch.float8_e4m3fn), index),
+               _column(v, "v", counts, (torch.float32, torch.uint8), index)]
+    eight = [t.dtype != torch.float32 for t in m]
+    if eight != [t.dtype != torch.float32 for t in v]:
+        raise ValueError("m and v of a parameter must be held in the same number of bits")
+    if any(eight):
+        if m_scale is None or v_scale is None:
+            raise ValueError("moments in 8 bits need m_scale and v_scale")
+        blocks = [-(-n // SCALE_BLOCK) for n in counts]
+        columns += [_column(m_scale, "m_scale", blocks, (torch.uint8,), index), _column(v_scale, "v_scale", blocks, (torch.uint8,), index)]
+    else:
+        columns += [[0] * count, [0] * count]
+    if masters is None:
+        columns.append([0] * count)
+    else:
+        if len(masters) != count:
+            raise ValueError(f"masters: {len(masters)} tensors for {count} parameters")
+        held = [i for i, t in enumerate(masters) if t is not None]
+        at = _column([masters[i] for i in held], "masters", [counts[i] for i in held], (torch.float32,), index)
+        column = [0] * count
+        for i, p in zip(held, at):
+            if params[i].dtype == torch.float32:
+                raise ValueError("a float32 parameter has no master copy")
+            column[i] = p
+        columns.append(column)
+    if control.dtype != torch.int64 or control.numel() != CONTROL_WORDS or control.device != device or not control.is_contiguous():
+        raise ValueError(f"control must be a contiguous int64 [{CONTROL_WORDS}] on {device}")
+    if isinstance(weight_decay, (int, float)):
+        decays = array("d", [weight_decay]) * count
+    else:
+        decays = array("d", weight_decay)
+        if len(decays) != count:
+            raise ValueError(f"weight_decay: {len(decays)} values for {count} parameters")
+    decay_bits = memoryview(decays).cast("B").cast("q")
+    kinds = [_TYPES[p.dtype] | _TYPES[g.dtype] << 32 for p, g in zip(params, grads)]
+    if masters is None and any([k & 0xFFFFFFFF == TYPE_F16 for k in kinds]):
+        raise ValueError("a float16 parameter needs a master copy")
+    bits = [(8 if e else 32) | i << 32 for i, e in enumerate(eight)]
+    table = array("q", [x for row in zip(*columns, counts, decay_bits, kinds, bits) for x in row])  # bmgd_adamw_tensor[count]
+    cfg = _AdamwConfig(float(lr), float(a), float(b), float(eps), float(grad_scale), float(max_norm), int(seed) & 0xFFFFFFFFFFFFFFFF)
+    L = _binding.load_library()
+    with _place(device, stream):
+        scratch, size = None, 0
+        if max_norm > 0:
+            size = (1 + count // 360) * 1184 * 8
+            scratch = torch.empty(size, dtype=torch.uint8, device=device)
+        _status(L.bmgd_adamw_step(table.buffer_info()[0], count, ctypes.byref(cfg), control.data_ptr(),
+                                  scratch.data_ptr() if scratch is not None else None, size,
+                                  torch.cuda.current_stream().cuda_stream), "bmgd_adamw_step")
+
+
+def decode_moments(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The fp32 values that moments in 8 bits stand for (for reading them; adamw_step does this on its own)."""
+    def per_value(scale, n):
+        return scale.to(torch.int32).repeat_interleave(SCALE_BLOCK)[:n]
+    n = m.numel()
+    first = torch.ldexp(m.reshape(-1).float(), per_value(m_scale, n) - 134).reshape(m.shape)
+    codes = v.reshape(-1).to(torch.int32)
+    second = torch.ldexp(1.0 + (codes & 7).float() / 8.0, (codes >> 3) - 157 + per_value(v_scale, n))
+    second = torch.where(codes == 0, 0.0, torch.where(codes == 255, float("nan"), second)).reshape(v.shape)
+    return first, second

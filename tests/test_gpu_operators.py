@@ -1,0 +1,309 @@
+"""The operators of a gated network's training step against their definitions in 64 bits.
+
+Tolerances are bounds, element by element, worked out from the roundings that each operator makes: u is half a step of
+the storage type relative to the value, 2^-24 that of fp32."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2312_08728_b200 import operators as ops
+
+pytestmark = pytest.mark.gpu
+
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+TINY = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float32: 0.0}  # half a step of the subnormals
+E32 = 2.0 ** -24
+ACTS = (ops.ACT_SILU, ops.ACT_GELU, ops.ACT_RELU, ops.ACT_SIGMOID)
+
+
+# ---------------------------------------------------------------- gated block
+
+def activation(act, g):
+    """act, act' and a bound on |act''| in 64 bits."""
+    if act == ops.ACT_RELU:
+        return g.clamp(min=0), (g > 0).double(), 0.0
+    if act == ops.ACT_GELU:
+        return g * torch.special.ndtr(g), torch.special.ndtr(g) + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi), 0.8
+    s = torch.sigmoid(g)
+    if act == ops.ACT_SIGMOID:
+        return s, s * (1 - s), 0.1
+    return g * s, s + g * s * (1 - s), 0.5
+
+
+class Block:
+    """Inputs, 64-bit results and bounds of one block."""
+
+    def __init__(self, rows, d, f, c, dtype, act, seed=0, extra=0, shift=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+
+        def make(n, k, scale):
+            # rows of a wider matrix (extra), starting `shift` values into an allocation
+            flat = torch.randn(shift + n * (k + extra), generator=gen, device="cuda") * scale
+            return flat.to(dtype)[shift:].view(n, k + extra)[:, :k]
+        self.x, self.wg, self.wu = make(rows, d, 1.0), make(d, f, d ** -0.5), make(d, f, d ** -0.5)
+        self.wd, self.dy = make(f, c, f ** -0.5), make(rows, c, 0.5)
+        self.act, self.dtype = act, dtype
+
+    def reference(self):
+        u, tiny = U[self.dtype], TINY[self.dtype]
+        x, wg, wu, wd, dy = (t.double() for t in (self.x, self.wg, self.wu, self.wd, self.dy))
+        n, (d, f), c = x.shape[0], wg.shape, wd.shape[1]
+        g, up = x @ wg, x @ wu
+        a, da, dda = activation(self.act, g)
+        # fp32 sums: at most K roundings of partial sums bounded by the sum of magnitudes; activations in fp32: a few
+        # units of 2^-24 relative, exp(-g) about |g| more, and |g| 2^-22 absolute where 1 + erf cancels
+        eg, eu = d * E32 * (x.abs() @ wg.abs()), d * E32 * (x.abs() @ wu.abs())
+        ea = (8 + 2 * g.abs()) * E32 * a.abs() + g.abs() * 2.0 ** -22 + (da.abs() + dda * eg) * eg
+        eda = (16 + 4 * g.abs()) * E32 * (1 + g.abs()) + dda * eg
+        h = a * up
+        eh = a.abs() * eu + up.abs() * ea + ea * eu
+        eh = eh + u * (h.abs() + eh) + tiny
+        y = h @ wd
+        ey = eh @ wd.abs() + f * E32 * (h.abs() @ wd.abs())
+        out = {"y": (y, ey + u * (y.abs() + ey) + tiny)}
+        # backward: G and U as saved (rounded), products rounded again
+        sg, su = eg + u * (g.abs() + eg) + tiny, eu + u * (up.abs() + eu) + tiny
+        dh = dy @ wd.T
+        edh = c * E32 * (dy.abs() @ wd.abs().T)
+        ea = (da.abs() + dda * sg) * sg + (8 + 2 * g.abs()) * E32 * a.abs() + g.abs() * 2.0 ** -22
+        eda = (0.0 if self.act == ops.ACT_RELU else 1.0) * (dda * sg + eda)
+        if self.act == ops.ACT_RELU:  # within its error of zero the sign of G, and with it act', may be either
+            eda = eda + (g.abs() <= sg).double()
+        du, dg, hh = dh * a, dh * up * da, a * up
+        edu = (dh.abs() + edh) * ea + edh * a.abs()
+        edg = (dh.abs() + edh) * (up.abs() + su) * eda + (dh.abs() + edh) * su * da.abs() + edh * up.abs() * da.abs()
+        ehh = (a.abs() + ea) * su + up.abs() * ea
+        edu, edg, ehh = (e + u * (v.abs() + e) * 1.01 + tiny + 4 * E32 * v.abs() for e, v in ((edu, du), (edg, dg), (ehh, hh)))
+
+        def contraction(*terms):
+            value = sum(p @ q for p, _, q in terms)
+            size = sum((p.abs() + e) @ q.abs() for p, e, q in terms)
+            k = sum(p.shape[1] for p, _, _ in terms)
+            err = sum(e @ q.abs() for _, e, q in terms) + k * E32 * size
+            return value, err + u * (value.abs() + err) + tiny
+        out["dx"] = contraction((dg, edg, wg.T), (du, edu, wu.T))
+        for name, v, e, left in (("dw_gate", dg, edg, x), ("dw_up", du, edu, x)):
+            value, err = contraction((v.T, e.T, left))
+            out[name] = (value.T, err.T)
+        out["dw_down"] = contraction((hh.T, ehh.T, dy))
+        return out
+
+    def run(self, **kw):
+        w = (self.wg, self.wu, self.wd)
+        y, saved = ops.gated_ffn(self.x, *w, self.act, save=True, **kw)
+        dx, dw_gate, dw_up, dw_down = ops.gated_ffn_backward(self.dy, self.x, *w, saved, self.act, **kw)
+        return {"y": y, "dx": dx, "dw_gate": dw_gate, "dw_up": dw_up, "dw_down": dw_down}
+
+    def check(self, got, names=("y", "dx", "dw_gate", "dw_up", "dw_down")):
+        ref = self.reference()
+        for k in names:
+            value, bound = ref[k]
+            assert got[k].dtype == self.dtype and got[k].shape == value.shape, k
+            over = ((got[k].double() - value).abs() - bound * 1.0001 - 1e-30)
+            worst = int(over.argmax())
+            assert float(over.max()) <= 0, (k, worst, got[k].flatten()[worst].item(), value.flatten()[worst].item(),
+                                            bound.flatten()[worst].item())
+
+
+SHAPES = [
+    (1, 8, 8, 8), (1, 64, 128, 64), (3, 1, 1, 1), (2, 17, 33, 5), (128, 64, 64, 64), (129, 65, 129, 257), (127, 200, 63, 10),
+    (256, 512, 1024, 2), (300, 500, 1371, 500), (1000, 136, 264, 72), (1, 1000, 777, 1000), (64, 264, 2056, 24),
+    (513, 1024, 640, 1032), (5, 2048, 4096, 2048), (17, 520, 1000, 8), (33, 4096, 264, 4104),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_gated_block(shape, dtype):
+    b = Block(*shape, dtype, ACTS[sum(shape) % 4], seed=sum(shape))
+    b.check(b.run())
+    y = ops.gated_ffn(b.x, b.wg, b.wu, b.wd, b.act)  # without saving: same result up to its own bound
+    b.check({"y": y}, ("y",))
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gated_block_activations(act):
+    b = Block(70, 96, 200, 40, torch.bfloat16, act, seed=act)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("extra,shift", [(8, 0), (3, 0), (0, 1), (24, 8), (1, 3)])
+@pytest.mark.parametrize("rows", [1, 40, 200])
+def test_gated_block_strides_and_alignment(rows, extra, shift):
+    """Rows of wider matrices, and matrices that start anywhere."""
+    b = Block(rows, 72, 136, 56, torch.float16, ops.ACT_SILU, seed=extra + shift, extra=extra, shift=shift)
+    b.check(b.run())
+
+
+def test_gated_block_large():
+    b = Block(2304, 1024, 2816, 1024, torch.bfloat16, ops.ACT_SILU, seed=5)
+    b.check(b.run())
+
+
+def test_gated_block_is_reproducible_and_leaves_its_inputs():
+    b = Block(777, 264, 520, 136, torch.bfloat16, ops.ACT_GELU, seed=9)
+    before = [t.clone() for t in (b.x, b.wg, b.wu, b.wd, b.dy)]
+    first, second = b.run(), b.run()
+    for k in first:
+        assert torch.equal(first[k], second[k]), k
+    for t, s in zip((b.x, b.wg, b.wu, b.wd, b.dy), before):
+        assert torch.equal(t, s)
+
+
+def test_gated_block_without_rows():
+    b = Block(0, 64, 128, 10, torch.bfloat16, ops.ACT_SILU)
+    out = b.run()
+    assert out["y"].shape == (0, 10) and out["dx"].shape == (0, 64)
+    for k in ("dw_gate", "dw_up", "dw_down"):
+        assert not out[k].any()
+
+
+def test_gated_block_against_differences():
+    """Directional derivatives of sum(dy * Y) in 64 bits, by central differences, against the backward pass."""
+    b = Block(24, 32, 40, 16, torch.float16, ops.ACT_SILU, seed=3)
+    got = b.run()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    tensors = {"dx": b.x, "dw_gate": b.wg, "dw_up": b.wu, "dw_down": b.wd}
+    ref = b.reference()
+
+    def value(**at):
+        x, wg, wu, wd = (at.get(k, t.double()) for k, t in tensors.items())
+        return float(((activation(b.act, x @ wg)[0] * (x @ wu)) @ wd * b.dy.double()).sum())
+    for k, t in tensors.items():
+        direction = torch.randn(t.shape, generator=gen, device="cuda", dtype=torch.float64)
+        step = 1e-4
+        slope = (value(**{k: t.double() + step * direction}) - value(**{k: t.double() - step * direction})) / (2 * step)
+        bound = float((ref[k][1] * direction.abs()).sum())
+        # the error of the central difference: step^2 times a third derivative, below 1e-4 of the sum of magnitudes here
+        assert abs(float((got[k].double() * direction).sum()) - slope) <= bound + 1e-5 * float((ref[k][0] * direction).abs().sum()), k
+
+
+@pytest.mark.parametrize("rows", [2, 130])
+def test_gated_block_nan_stays_in_its_row(rows):
+    b = Block(rows, 64, 128, 32, torch.bfloat16, ops.ACT_SILU, seed=4)
+    clean = ops.gated_ffn(b.x, b.wg, b.wu, b.wd, b.act)
+    b.x[1, 5] = float("nan")
+    y = ops.gated_ffn(b.x, b.wg, b.wu, b.wd, b.act)
+    assert torch.isnan(y[1]).all()
+    assert torch.equal(y[0], clean[0]) and torch.equal(y[2:], clean[2:])
+
+
+@pytest.mark.parametrize("rows", [1, 9, 300])
+def test_gated_block_captured_and_on_another_stream(rows):
+    b = Block(rows, 128, 264, 64, torch.bfloat16, ops.ACT_SILU, seed=6)
+    eager = b.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = b.run(stream=side)
+    side.synchronize()
+    for k in eager:
+        assert torch.equal(eager[k], other[k]), k
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = b.run()
+    b.x.copy_(torch.flip(b.x, (0,)))
+    graph.replay()
+    torch.cuda.synchronize()
+    again = b.run()
+    for k in eager:
+        assert torch.equal(captured[k], again[k]), k
+    ops.stream_check()
+
+
+# ---------------------------------------------------------------- softmax residual
+
+def residual_reference(z, y, scale):
+    z = z.double()
+    C = z.shape[1]
+    fine = (y >= 0) & (y < C) & ~(z == -math.inf).all(dim=1)
+    # relative to the row's largest logit: next to 1e38 the logarithm of a sum is lost even in 64 bits
+    z = z - z.amax(dim=1, keepdim=True).clamp(min=torch.finfo(torch.float64).min)
+    lse = torch.logsumexp(z, dim=1)
+    one = torch.zeros_like(z)
+    at = y.long().clamp(0, C - 1)
+    one[torch.arange(len(y)), at] = 1.0
+    r = (torch.exp(z - lse[:, None]) - one) * scale
+    loss = lse - z[torch.arange(len(y)), at]
+    broken = torch.isnan(lse)  # NaN, or infinity less infinity: the row has no values
+    r, loss = torch.where(broken[:, None], math.nan, r), torch.where(broken, math.nan, loss)
+    return torch.where(fine[:, None], r, 0.0), torch.where(fine, loss, 0.0)
+
+
+def check_residual(z, y, scale=None):
+    residual, loss = ops.softmax_residual(z, y, scale)
+    s = 1.0 / z.shape[0] if scale is None else scale
+    r, l = residual_reference(z, y, s)
+    C, u = z.shape[1], U[z.dtype]
+    span = (z.double().clamp(min=-1e30) - z.double().amax(dim=1, keepdim=True)).abs().clamp(max=200.0)
+    # a probability: exp2 of (z - max) log2 e has an error of a few 2^-24 and |z - max| 2^-23 more; the sum of C such
+    # terms, one partial sum after another in each thread, at most C 2^-24 relative in the worst order
+    p = (r / s + torch.nn.functional.one_hot(y.long().clamp(0, C - 1), C)).abs()
+    err = abs(s) * ((8 + 4 * span + C) * E32 * p + 2 * E32)
+    bound = err + u * (r.abs() + err) + TINY[z.dtype] + 2.0 ** -126
+    ok = ((residual.double() - r).abs() <= bound) | (torch.isnan(r) & torch.isnan(residual))
+    assert bool(ok.all()), (residual.double() - r).abs().max()
+    top = z.double().amax(dim=1).abs().clamp(max=1e30)
+    lb = (C + 16) * E32 + 4 * E32 * (l.abs().clamp(max=1e30) + top)
+    fine = torch.isfinite(l)
+    assert bool(((loss.double() - l).abs() <= lb)[fine].all())
+    assert torch.equal(torch.isnan(l), torch.isnan(loss)) and torch.equal(l == math.inf, loss == math.inf)
+    return residual, loss
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,C", [(1, 1), (1, 2), (256, 10), (1000, 16), (7, 31), (65, 33), (3, 257), (130, 1000), (33, 1025), (5, 4097),
+                                    (40, 10007), (9, 50257), (3, 131071)])
+def test_residual(rows, C, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(rows * C)
+    z = (torch.randn(rows, C, generator=gen, device="cuda") * 4).to(dtype)
+    y = torch.randint(0, C, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    check_residual(z, y)
+    check_residual(z, y, scale=0.75)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("C", [10, 300, 5000, 70001])
+def test_residual_masks_and_labels(C, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(C)
+    z = (torch.randn(12, C, generator=gen, device="cuda") * 4).to(dtype)
+    y = torch.randint(0, C, (12,), generator=gen, device="cuda", dtype=torch.int32)
+    y[0], y[1], y[2] = -1, C, -2 ** 31
+    z[3] = -math.inf                          # nothing left
+    z[4, 1:] = -math.inf; y[4] = 0            # one class left, the label's: probability one
+    z[5, : C // 2] = -math.inf                # a masked half
+    y[5] = C - 1
+    z[6, 0] = -math.inf; y[6] = 0             # the label itself masked: loss infinite
+    z[7, C // 3] = math.nan
+    z[8, C - 1] = math.inf
+    z[9] = torch.finfo(dtype).min             # masked with the type's lowest value throughout
+    z[10, ::2] = torch.finfo(dtype).min; y[10] = 1
+    z[11] = 0.0
+    residual, loss = check_residual(z, y)
+    for i in (0, 1, 2, 3):
+        assert not residual[i].any() and loss[i] == 0
+    assert not residual[4].any() and loss[4] == 0
+    assert loss[6] == math.inf and torch.isnan(residual[7]).all() and torch.isnan(residual[8]).all()
+
+
+@pytest.mark.parametrize("C", [12, 1003])
+def test_residual_rows_of_a_wider_matrix(C):
+    z = torch.randn(37, C + 5, device="cuda", dtype=torch.bfloat16)[:, 2:C + 2]
+    check_residual(z, torch.randint(0, C, (37,), device="cuda", dtype=torch.int32))
+
+
+# ---------------------------------------------------------------- mini-batches
+
+@pytest.mark.parametrize("p,dtype", [(8, torch.bfloat16), (13, torch.bfloat16), (200, torch.float32), (7, torch.uint8)])
+def test_gather_batch_takes_the_rows_of_the_shuffle(p, dtype):
+    rows = 1013
+    x = torch.arange(rows * p, device="cuda").remainder(251).to(dtype).view(rows, p)
+    y = torch.arange(rows, device="cuda", dtype=torch.int32)
+    pi = torch.from_numpy(oracle.perm(77, 2, 5, rows).astype(np.int64)).cuda()
+    bx, by = ops.gather_batch(x, y, 77, 2, 5, 100, 300)
+    assert torch.equal(by.long(), pi[100:400]) and torch.equal(bx, x[pi[100:400]])
+    bx, by = ops.gather_batch(x, None, 77, 2, 5, 1000, 13)
+    assert by is None and torch.equal(bx, x[pi[1000:]])
+    assert ops.gather_batch(x, y, 77, 2, 5, rows, 0)[0].shape == (0, p)
