@@ -318,8 +318,9 @@ typedef struct bmgd_gated_ffn {
     int64_t ld_x, ld_gate, ld_up, ld_down;
     void* y;                             /* forward: [rows][outputs], stride ld_y */
     int64_t ld_y;
-    void *saved_gate, *saved_up;         /* [rows][hidden], 16-byte aligned, stride ld_saved (a multiple of 8): X Wg and X Wu, written by the
-                                            forward pass (both NULL: not wanted) and read by the backward pass */
+    float *saved_value, *saved_slope;    /* [rows][hidden] each, 16-byte aligned, stride ld_saved (a multiple of 8): act(X Wg), */
+    void* saved_hidden;                  /* (X Wu) * act'(X Wg) and, in `type`, act(X Wg) * (X Wu); written by the forward
+                                            pass (all NULL: not wanted), read by the backward pass; the padding may be overwritten */
     int64_t ld_saved;
     const void* dy;                      /* backward: gradient of Y, stride ld_dy */
     int64_t ld_dy;

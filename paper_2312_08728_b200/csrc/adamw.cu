@@ -51,9 +51,9 @@ int check_overlap(const bmgd_adamw_tensor* t, int32_t count) {
 
 bool in_unit(double x) { return x >= 0.0 && x < 1.0; }
 
+// Sum of squares (bits = 0: all tensors), or the update of the tensors whose moments are held in `bits` bits.
 template <int CAP>
-int launch(const bmgd_adamw_tensor* t, int32_t count, const AdamwHead& head, int blocks, bool norm, double* partial,
-           cudaStream_t s) {
+int launch(const bmgd_adamw_tensor* t, int32_t count, const AdamwHead& head, int bits, int blocks, double* partial, cudaStream_t s) {
     AdamwTable<CAP>* T = new (std::nothrow) AdamwTable<CAP>;
     if (!T) return BMGD_ERR_ALLOC;
     T->h = head;
@@ -62,7 +62,7 @@ int launch(const bmgd_adamw_tensor* t, int32_t count, const AdamwHead& head, int
     int k = 0;
     for (int32_t i = 0; i < count; ++i) {
         const bmgd_adamw_tensor& x = t[i];
-        if (x.count == 0) continue;
+        if (x.count == 0 || (bits != 0 && x.state_bits != bits)) continue;
         AdamwEntry& e = T->e[k++];
         e.param = x.param; e.grad = x.grad; e.m = x.m; e.v = x.v;
         e.m_scale = static_cast<uint8_t*>(x.m_scale); e.v_scale = static_cast<uint8_t*>(x.v_scale);
@@ -82,8 +82,9 @@ int launch(const bmgd_adamw_tensor* t, int32_t count, const AdamwHead& head, int
     T->h.chunks = chunks;
     if (k == 0) { T->h.count = 1; std::memset(&T->e[0], 0, sizeof T->e[0]); }  // nothing to update, but the step counts
     const int grid = (int)std::max<long long>(1, std::min<long long>(chunks, blocks));
-    if (norm) adamw_norm_kernel<CAP><<<blocks, kAdamwThreads, 0, s>>>(*T, partial);
-    else adamw_kernel<CAP><<<grid, kAdamwThreads, 0, s>>>(*T);
+    if (bits == 0) adamw_norm_kernel<CAP><<<blocks, kAdamwThreads, 0, s>>>(*T, partial);
+    else if (bits == 8) adamw_kernel<CAP, 8><<<grid, kAdamwThreads, 0, s>>>(*T);
+    else adamw_kernel<CAP, 32><<<grid, kAdamwThreads, 0, s>>>(*T);
     delete T;
     return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA;
 }
@@ -121,7 +122,7 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return BMGD_ERR_CUDA;
-    const int blocks = std::min(kAdamwMaxBlocks, sms * 4);
+    const int blocks = std::min(kAdamwMaxBlocks, sms * 3), sum_blocks = std::min(kAdamwMaxBlocks, sms * 6);  // what fits an SM
     const bool clip = cfg->max_norm > 0.0;
     AdamwHead h{};
     h.control = static_cast<long long*>(dev_control);
@@ -135,24 +136,33 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
     const bool small = count <= kSmallTable;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     double* partial = static_cast<double*>(dev_scratch);
+    auto part = [&](int l, int bits, double* sums) {
+        const int32_t first = l * kLargeTable, some = std::min(count - first, kLargeTable);
+        return small ? launch<kSmallTable>(tensors + first, some, h, bits, bits ? blocks : sum_blocks, sums, s)
+                     : launch<kLargeTable>(tensors + first, some, h, bits, bits ? blocks : sum_blocks, sums, s);
+    };
     if (clip) {
         if (!partial || (uintptr_t)partial % 8 != 0) return BMGD_ERR_ARG;
-        if (scratch_bytes < (int64_t)launches * blocks * 8) return BMGD_ERR_CAPACITY;
+        if (scratch_bytes < (int64_t)launches * sum_blocks * 8) return BMGD_ERR_CAPACITY;
         for (int l = 0; l < launches; ++l) {
-            const int32_t first = l * kLargeTable, some = std::min(count - first, kLargeTable);
-            const int e = small ? launch<kSmallTable>(tensors + first, some, h, blocks, true, partial + (int64_t)l * blocks, s)
-                                : launch<kLargeTable>(tensors + first, some, h, blocks, true, partial + (int64_t)l * blocks, s);
+            const int e = part(l, 0, partial + (int64_t)l * sum_blocks);
             if (e != BMGD_OK) return e;
         }
         h.partial = partial;
-        h.npartial = launches * blocks;
+        h.npartial = launches * sum_blocks;
     }
-    for (int l = 0; l < launches; ++l) {
-        const int32_t first = l * kLargeTable, some = std::min(count - first, kLargeTable);
-        h.final = l == launches - 1;
-        const int e = small ? launch<kSmallTable>(tensors + first, some, h, blocks, false, nullptr, s)
-                            : launch<kLargeTable>(tensors + first, some, h, blocks, false, nullptr, s);
-        if (e != BMGD_OK) return e;
+    int held[2] = {0, 0};  // tensors with moments in 32 and in 8 bits
+    for (int32_t i = 0; i < count; ++i)
+        if (tensors[i].count > 0) ++held[tensors[i].state_bits == 8];
+    const int last = held[1] ? 8 : 32;  // a width without tensors is launched only where there is nothing else to count the update
+    for (int bits = 32; bits >= 8; bits -= 24) {
+        if (bits == 32 && !held[0] && last == 8) continue;
+        if (bits == 8 && !held[1]) continue;
+        for (int l = 0; l < launches; ++l) {
+            h.final = bits == last && l == launches - 1;
+            const int e = part(l, bits, nullptr);
+            if (e != BMGD_OK) return e;
+        }
     }
     return BMGD_OK;
 }

@@ -3,8 +3,8 @@
 // Per value, with t the number of this update, g the gradient times grad_scale and the clipping factor:
 //     m <- a m + (1-a) g;   v <- b v + ((1-b) g) g
 //     theta <- theta (1 - lr wd) - (lr / (1-a^t)) (m / (sqrt(v) / sqrt(1-b^t) + eps))
-// Every product and sum is rounded to fp32 by itself (no contraction), so the result does not depend on how the
-// compiler schedules it: two kernels that process the same value in different places agree bit for bit.
+// Every product and sum is rounded to fp32 by itself (no contraction), so the moments do not depend on how the compiler
+// schedules them, and their codes can be checked bit for bit.
 //
 // What bounds it: memory.  Each value of theta, the gradient and the moments is read once and written once.  A warp
 // takes units of 256 consecutive values of one tensor: lane l holds values 4l..4l+3 and 128+4l..128+4l+3, so that every
@@ -24,6 +24,7 @@
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 namespace bmgdk {
@@ -158,46 +159,39 @@ __device__ __forceinline__ void store_codes(void* base, long long at, long long 
 __device__ __forceinline__ float power_of_two(int biased) { return __uint_as_float((uint32_t)biased << 23); }
 __device__ __forceinline__ bool finite_bits(uint32_t b) { return (b & 0x7F800000u) != 0x7F800000u; }
 
-// value of an e4m3 code before scaling: exact
-__device__ __forceinline__ float decode_m(uint32_t c) {
-    const uint32_t mag = c & 0x7Fu;
-    // exponent field 0 counts in steps of 2^-9
-    float x = mag >= 8u ? __uint_as_float((mag << 20) + (120u << 23)) : (float)mag * 0x1p-9f;
-    if (mag == 0x7Fu) x = __uint_as_float(0x7FC00000u);
-    return __uint_as_float(__float_as_uint(x) | ((c & 0x80u) << 24));
+// ---- codes of 8 bits, four to a word
+// e4m3 values before scaling, by way of fp16, which holds all of them (0x7F and 0xFF give NaN)
+__device__ __forceinline__ void decode_m4(uint32_t w, float (&x)[4]) {
+    const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3);
+    const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    const float2 a = __half22float2(__half2(lo)), b = __half22float2(__half2(hi));
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
-__device__ __forceinline__ uint32_t encode_m(float x, uint32_t r16) {  // x scaled to |x| < 256
-    const uint32_t bits = __float_as_uint(x), mag = bits & 0x7FFFFFFFu;
-    uint32_t c;
-    if (mag >= 0x3C800000u) c = (mag - (120u << 23) + (r16 << 4)) >> 20;  // |x| >= 2^-6
-    else c = min((uint32_t)__fadd_rn(__uint_as_float(mag) * 512.f, (float)r16 * 0x1p-16f), 8u);
-    if (!finite_bits(bits)) c = 0x7Fu;
-    return c | ((bits >> 24) & 0x80u);
+// x scaled to |x| < 256 and finite.  From 2^-6 on the upper bits of x count code steps, 2^20 units of the last place each;
+// below, steps are 2^-9 throughout, which the last places of |x| + 2^-6 count.  Rounding that sum towards zero is exact for the
+// purpose: the draw has 16 bits, so every threshold is a multiple of 16 units.
+__device__ __forceinline__ uint32_t encode_m(float x, uint32_t r16) {
+    const uint32_t mag = __float_as_uint(x) & 0x7FFFFFFFu;
+    const uint32_t low = __float_as_uint(__fadd_rz(__uint_as_float(mag), 0x1p-6f)) - (121u << 23);
+    const uint32_t y = mag >= (121u << 23) ? mag - (120u << 23) : low;
+    return ((y + (r16 << 4)) >> 20) | ((__float_as_uint(x) >> 24) & 0x80u);
 }
-__device__ __forceinline__ float decode_v(uint32_t c, int s) {
-    const uint32_t e = (c >> 3) + (uint32_t)(s - 30);
-    float x = __uint_as_float((e << 23) | ((c & 7u) << 20));
-    if (c == 0u) x = 0.f;
-    if (c == 255u) x = __uint_as_float(0x7FC00000u);
-    return x;
-}
-__device__ __forceinline__ uint32_t encode_v(float v, int s, uint32_t r16) {
-    const int y = (int)(__float_as_uint(v) - ((uint32_t)(s - 30) << 23));
-    uint32_t c = y >= (1 << 20) ? (uint32_t)(y + (int)(r16 << 4)) >> 20 : 1u;
-    if (v == 0.f) c = 0u;
-    if (!finite_bits(__float_as_uint(v))) c = 255u;
-    return c;
-}
-// biased exponent of the largest finite magnitude of the warp's unit
-__device__ __forceinline__ int unit_exponent(const float (&x)[8], int least) {
-    uint32_t top = 0;
+__device__ __forceinline__ void decode_v4(uint32_t w, int s, float (&x)[4]) {
+    const uint32_t base = (uint32_t)(s - 30) << 23;  // exponent and mantissa bits of a code are those of the value, shifted
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t mag = __float_as_uint(x[i]) & 0x7FFFFFFFu;
-        if (mag < 0x7F800000u) top = max(top, mag);
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c = (w >> (8 * i)) & 0xFFu;
+        x[i] = c == 0u ? 0.f : __uint_as_float((c << 20) + base);
     }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
-    return max((int)(top >> 23), least);
+    if (__vcmpeq4(w, 0xFFFFFFFFu)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (((w >> (8 * i)) & 0xFFu) == 0xFFu) x[i] = __uint_as_float(0x7FC00000u);
+    }
+}
+__device__ __forceinline__ uint32_t encode_v(float v, int s, uint32_t r16) {  // v finite
+    const int y = (int)(__float_as_uint(v) - ((uint32_t)(s - 30) << 23) + (r16 << 4));
+    return v == 0.f ? 0u : (uint32_t)max(y >> 20, 1);
 }
 
 // x^n for an integer n >= 0
@@ -243,6 +237,14 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------- the update
+// Square root and quotient of the step within 2^-23 and 2^-22 of their values: they move theta by lr at most, and the exact
+// forms cost as many instructions as the rest of the formula (which bounds the kernel where moments have 8 bits).
+__device__ __forceinline__ float sqrt_near(float x) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 struct AdamwFactors {
     float gscale, step, root, a, a1, b, b1, eps;
     int fine;
@@ -250,10 +252,139 @@ struct AdamwFactors {
     double norm;
 };
 
-template <int CAP>
-__global__ void __launch_bounds__(kAdamwThreads) adamw_kernel(const __grid_constant__ AdamwTable<CAP> T) {
+template <int TYPE> __device__ __forceinline__ void load4_wide(const void* base, long long at, float (&x)[4]) {
+    const float4 v = load4(base, TYPE, at, at + 4, true);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+template <int TYPE, bool WIDE> __device__ __forceinline__ void load4_any(const void* base, long long at, long long n, float (&x)[4]) {
+    if constexpr (WIDE) { load4_wide<TYPE>(base, at, x); return; }
+    const float4 v = load4(base, TYPE, at, n, false);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+
+// One unit of a tensor.  WIDE: it lies within the tensor and every array allows vector accesses.
+template <int PT, bool MASTER, int GT, int BITS, bool WIDE>
+__device__ __forceinline__ void adamw_unit(const AdamwEntry& e, long long unit, int lane, const AdamwFactors& F, float keep, uint32_t key) {
+    const long long n = e.n;
+    const long long at[2] = {unit * kAdamwUnit + lane * 4, unit * kAdamwUnit + lane * 4 + 128};
+    constexpr bool kRandomTheta = PT == kTypeBF16 && !MASTER;
+    float p[2][4], g[2][4], m[2][4], v[2][4];
+    uint32_t cm[2], cv[2];
+    int sm = 0, sv = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        load4_any<GT, WIDE>(e.grad, at[h], n, g[h]);
+        if constexpr (MASTER) load4_any<kTypeF32, WIDE>(e.master, at[h], n, p[h]);
+        else load4_any<PT, WIDE>(e.param, at[h], n, p[h]);
+        if constexpr (BITS == 8) {
+            cm[h] = load_codes(e.m, at[h], n, WIDE);
+            cv[h] = load_codes(e.v, at[h], n, WIDE);
+        } else {
+            load4_any<kTypeF32, WIDE>(e.m, at[h], n, m[h]);
+            load4_any<kTypeF32, WIDE>(e.v, at[h], n, v[h]);
+        }
+    }
+    if constexpr (BITS == 8) {
+        sm = e.m_scale[unit];
+        sv = e.v_scale[unit];
+        const float unscale = power_of_two(sm - 7);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            decode_m4(cm[h], m[h]);
+            decode_v4(cv[h], sv, v[h]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m[h][i] *= unscale;
+        }
+    }
+    uint32_t top_m = 0, top_v = 0;  // largest magnitudes of the new moments, infinities and NaN among them
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float gi = __fmul_rn(g[h][i], F.gscale);
+            m[h][i] = __fadd_rn(__fmul_rn(m[h][i], F.a), __fmul_rn(gi, F.a1));
+            v[h][i] = __fadd_rn(__fmul_rn(v[h][i], F.b), __fmul_rn(__fmul_rn(gi, F.b1), gi));
+            const float denom = __fadd_rn(__fmul_rn(sqrt_near(v[h][i]), F.root), F.eps);
+            p[h][i] = __fsub_rn(__fmul_rn(p[h][i], keep), __fmul_rn(__fdividef(m[h][i], denom), F.step));
+            if constexpr (BITS == 8) {
+                top_m = max(top_m, __float_as_uint(m[h][i]) & 0x7FFFFFFFu);
+                top_v = max(top_v, __float_as_uint(v[h][i]) & 0x7FFFFFFFu);
+            }
+        }
+    }
+    // the unit starts at a multiple of 256, so all its places share the upper 32 bits
+    const uint32_t k = key + (uint32_t)((unsigned long long)at[0] >> 32) * 0x85EBCA6Bu;
+    uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+    if constexpr (BITS == 8) {
+        top_m = __reduce_max_sync(0xFFFFFFFFu, top_m);
+        top_v = __reduce_max_sync(0xFFFFFFFFu, top_v);
+        if (max(top_m, top_v) >= 0x7F800000u) {  // some value is infinite or NaN: the scales go by the others
+            top_m = top_v = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t bm = __float_as_uint(m[h][i]) & 0x7FFFFFFFu, bv = __float_as_uint(v[h][i]) & 0x7FFFFFFFu;
+                    if (bm < 0x7F800000u) top_m = max(top_m, bm);
+                    else { wm[h] |= 0xFFu << (8 * i); m[h][i] = 0.f; }  // the code of NaN
+                    if (bv < 0x7F800000u) top_v = max(top_v, bv);
+                    else { wv[h] |= 0xFFu << (8 * i); v[h][i] = 0.f; }
+                }
+            top_m = __reduce_max_sync(0xFFFFFFFFu, top_m);
+            top_v = __reduce_max_sync(0xFFFFFFFFu, top_v);
+        }
+        sm = max((int)(top_m >> 23), 16);
+        sv = max((int)(top_v >> 23), 40);
+    }
+    const float scale = power_of_two(261 - sm);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if constexpr (BITS == 32) {
+            store4(e.m, kTypeF32, at[h], n, WIDE, m[h]);
+            store4(e.v, kTypeF32, at[h], n, WIDE, v[h]);
+        }
+        if constexpr (MASTER) store4(e.master, kTypeF32, at[h], n, WIDE, p[h]);
+        if constexpr (BITS == 8 || kRandomTheta) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = mix32(((uint32_t)at[h] + i) ^ k);
+                if constexpr (BITS == 8) {
+                    wm[h] |= encode_m(m[h][i] * scale, r & 0xFFFFu) << (8 * i);
+                    wv[h] |= encode_v(v[h][i], sv, r >> 16) << (8 * i);
+                }
+                if constexpr (kRandomTheta) {
+                    const uint32_t b = __float_as_uint(p[h][i]);
+                    const uint32_t up = (b + (mix32(r ^ 0x9E3779B9u) & 0xFFFFu)) & 0xFFFF0000u;
+                    if (finite_bits(b)) p[h][i] = __uint_as_float(up);
+                }
+            }
+        }
+        if constexpr (BITS == 8) {
+            store_codes(e.m, at[h], n, WIDE, wm[h]);
+            store_codes(e.v, at[h], n, WIDE, wv[h]);
+        }
+        store4(e.param, PT, at[h], n, WIDE, p[h]);
+    }
+    if (BITS == 8 && lane == 0) { e.m_scale[unit] = (uint8_t)sm; e.v_scale[unit] = (uint8_t)sv; }
+}
+
+template <int PT, bool MASTER, int GT, int BITS>
+__device__ __forceinline__ void adamw_units(const AdamwEntry& e, long long unit0, int units, int lane, const AdamwFactors& F, uint32_t key) {
+    const float keep = e.keep;
+    for (int u = 0; u < units; ++u) {
+        const long long unit = unit0 + u;
+        if (unit * kAdamwUnit >= e.n) break;
+        if (e.aligned && (unit + 1) * kAdamwUnit <= e.n) adamw_unit<PT, MASTER, GT, BITS, true>(e, unit, lane, F, keep, key);
+        else adamw_unit<PT, MASTER, GT, BITS, false>(e, unit, lane, F, keep, key);
+    }
+}
+
+// BITS: how the moments of all tensors of this launch are held.  Their types differ from tensor to tensor; the code for
+// each combination is chosen once for a warp's units.
+template <int CAP, int BITS>
+__global__ void __launch_bounds__(kAdamwThreads, 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP> T) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    __shared__ AdamwFactors F;
+    __shared__ AdamwFactors shared_factors;
     __shared__ double part[kAdamwThreads / 32];
     if (T.h.npartial > 0) {
         double s = 0.0;
@@ -264,6 +395,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_kernel(const __grid_const
         __syncthreads();
     }
     if (threadIdx.x == 0) {
+        AdamwFactors& F = shared_factors;
         const long long t = T.h.control[0] + 1;
         double scale = T.h.grad_scale;
         F.fine = 1;
@@ -286,102 +418,22 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_kernel(const __grid_const
         F.key = mix32(T.h.seed_lo + (uint32_t)t * 0x9E3779B9u);
     }
     __syncthreads();
+    const AdamwFactors& F = shared_factors;
     if (F.fine) {
-        const float gscale = F.gscale, step = F.step, root = F.root, fa = F.a, fa1 = F.a1, fb = F.b, fb1 = F.b1, eps = F.eps;
         for (long long chunk = blockIdx.x; chunk < T.h.chunks; chunk += gridDim.x) {
             const AdamwEntry& e = T.e[adamw_find(T, chunk)];
-            const long long n = e.n;
-            const bool al = e.aligned, eight = e.bits == 8;
-            const float keep = e.keep;
-            const bool random_theta = e.ptype == kTypeBF16 && e.master == nullptr;
             const uint32_t key = mix32(F.key ^ (T.h.seed_hi + e.index * 0x9E3779B9u));
             const long long unit0 = ((chunk - e.first_chunk) * (kAdamwThreads / 32) + warp) * T.h.units;
-            for (int u = 0; u < T.h.units; ++u) {
-                const long long unit = unit0 + u;
-                if (unit * kAdamwUnit >= n) break;
-                const long long at[2] = {unit * kAdamwUnit + lane * 4, unit * kAdamwUnit + lane * 4 + 128};
-                float p[8], g[8], m[8], v[8];
-                uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
-                int sm = 0, sv = 0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 x = load4(e.grad, e.gtype, at[h], n, al);
-                    const float4 y = e.master ? load4(e.master, kTypeF32, at[h], n, al) : load4(e.param, e.ptype, at[h], n, al);
-                    g[4 * h] = x.x; g[4 * h + 1] = x.y; g[4 * h + 2] = x.z; g[4 * h + 3] = x.w;
-                    p[4 * h] = y.x; p[4 * h + 1] = y.y; p[4 * h + 2] = y.z; p[4 * h + 3] = y.w;
-                    if (eight) {
-                        cm[h] = load_codes(e.m, at[h], n, al);
-                        cv[h] = load_codes(e.v, at[h], n, al);
-                    } else {
-                        const float4 a4 = load4(e.m, kTypeF32, at[h], n, al), b4 = load4(e.v, kTypeF32, at[h], n, al);
-                        m[4 * h] = a4.x; m[4 * h + 1] = a4.y; m[4 * h + 2] = a4.z; m[4 * h + 3] = a4.w;
-                        v[4 * h] = b4.x; v[4 * h + 1] = b4.y; v[4 * h + 2] = b4.z; v[4 * h + 3] = b4.w;
-                    }
-                }
-                if (eight) {
-                    sm = e.m_scale[unit];
-                    sv = e.v_scale[unit];
-                    const float unscale = power_of_two(sm - 7);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        m[i] = decode_m((cm[i >> 2] >> (8 * (i & 3))) & 0xFFu) * unscale;
-                        v[i] = decode_v((cv[i >> 2] >> (8 * (i & 3))) & 0xFFu, sv);
-                    }
-                }
-                float q[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float gi = __fmul_rn(g[i], gscale);
-                    m[i] = __fadd_rn(__fmul_rn(m[i], fa), __fmul_rn(gi, fa1));
-                    v[i] = __fadd_rn(__fmul_rn(v[i], fb), __fmul_rn(__fmul_rn(gi, fb1), gi));
-                    const float denom = __fadd_rn(__fmul_rn(__fsqrt_rn(v[i]), root), eps);
-                    q[i] = __fsub_rn(__fmul_rn(p[i], keep), __fmul_rn(__fdiv_rn(m[i], denom), step));
-                }
-                uint32_t r[8];
-                if (eight || random_theta) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const long long place = at[i >> 2] + (i & 3);
-                        r[i] = mix32((uint32_t)place ^ (key + (uint32_t)(place >> 32) * 0x85EBCA6Bu));
-                    }
-                }
-                if (eight) {
-                    const int tm = unit_exponent(m, 16), tv = unit_exponent(v, 40);
-                    const float scale = power_of_two(261 - tm);
-                    uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        wm[i >> 2] |= encode_m(m[i] * scale, r[i] & 0xFFFFu) << (8 * (i & 3));
-                        wv[i >> 2] |= encode_v(v[i], tv, r[i] >> 16) << (8 * (i & 3));
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        store_codes(e.m, at[h], n, al, wm[h]);
-                        store_codes(e.v, at[h], n, al, wv[h]);
-                    }
-                    if (lane == 0) { e.m_scale[unit] = (uint8_t)tm; e.v_scale[unit] = (uint8_t)tv; }
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[4] = {q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]};
-                    if (!eight) {
-                        const float mm[4] = {m[4 * h], m[4 * h + 1], m[4 * h + 2], m[4 * h + 3]};
-                        const float vv[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-                        store4(e.m, kTypeF32, at[h], n, al, mm);
-                        store4(e.v, kTypeF32, at[h], n, al, vv);
-                    }
-                    if (e.master) store4(e.master, kTypeF32, at[h], n, al, x);
-                    if (random_theta) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t b = __float_as_uint(x[i]);
-                            const uint32_t up = (b + (mix32(r[4 * h + i] ^ 0x9E3779B9u) & 0xFFFFu)) & 0xFFFF0000u;
-                            if (finite_bits(b)) x[i] = __uint_as_float(up);
-                        }
-                    }
-                    store4(e.param, e.ptype, at[h], n, al, x);
-                }
-            }
+            const int units = T.h.units;
+#define BMGD_ADAMW_GRADS(PT, MASTER)                                                                          \
+    if (e.gtype == kTypeF32) adamw_units<PT, MASTER, kTypeF32, BITS>(e, unit0, units, lane, F, key);          \
+    else if (e.gtype == kTypeBF16) adamw_units<PT, MASTER, kTypeBF16, BITS>(e, unit0, units, lane, F, key);   \
+    else adamw_units<PT, MASTER, kTypeF16, BITS>(e, unit0, units, lane, F, key)
+            if (e.ptype == kTypeF32) { BMGD_ADAMW_GRADS(kTypeF32, false); }
+            else if (e.ptype == kTypeF16) { BMGD_ADAMW_GRADS(kTypeF16, true); }
+            else if (e.master) { BMGD_ADAMW_GRADS(kTypeBF16, true); }
+            else { BMGD_ADAMW_GRADS(kTypeBF16, false); }
+#undef BMGD_ADAMW_GRADS
         }
     }
     if (T.h.final) {  // the last block to finish counts the update: every block has read the count by then

@@ -2,14 +2,15 @@
 //
 //   forward    G = X Wg, U = X Wu, H = act(G) * U      one kernel: a tile holds the same columns of G and U side by side,
 //              Y = H Wd                                 so the product is taken where the accumulators are read out
-//   backward   dH = dY Wd^T, dU = dH act(G), dG = dH U act'(G)   one kernel; H is formed again on the way
+//   backward   dH = dY Wd^T, dU = dH act(G), dG = dH (U act'(G))  one kernel; the two factors come from the forward pass
 //              dX = dG Wg^T + dU Wu^T                   one accumulator, the second product continues the first
 //              dWg = X^T dG, dWu = X^T dU               one launch over both
 //              dWd = H^T dY
 // Rows of every matrix are contiguous.  Both ways of reading a tile exist for each operand: "K-major", the contraction
-// index along the rows, or "MN-major", across them; nothing is transposed in memory.  G, U, dG, dU and H are rounded to
-// the type of the rows between the kernels (they are the operands of the next contraction, which takes no other type);
-// sums are fp32 in tensor memory.
+// index along the rows, or "MN-major", across them; nothing is transposed in memory.  H, dG and dU are rounded to the type
+// of the rows between the kernels (they are the operands of the next contraction, which takes no other type); sums are fp32
+// in tensor memory, and act(G) and U act'(G) are kept in fp32 for the backward pass: rounded to 16 bits they would add as much
+// to the gradients' error as both other roundings together, and their traffic hides behind the arithmetic.
 //
 // What bounds it: the tensor cores, from a few hundred rows on.  Warp 0 copies tiles of 64 along the contraction by TMA
 // into a ring of stages with the 128-byte swizzle, warp 1 issues tcgen05.mma, warps 4 to 7 read accumulators out of
@@ -32,23 +33,22 @@ enum { kEpiGated = 0, kEpiPlain = 1, kEpiBackward = 2 };
 
 constexpr int kFfnThreads = 256;
 constexpr int kFfnBK = 64;
+constexpr int kTurnPitch = 36;  // words per row there: 32 and four, so that eight lanes' 16-byte accesses meet no bank twice
 constexpr int kFfnGroup = 8;  // tiles along M that are worked on together: their rows of A stay in L2 while B passes
 
 struct FfnParams {
     CUtensorMap a[2], b[2];  // second pair: the second half of the contraction (segments = 2) or of the launch (problems = 2)
     void* out[2];            // plain: D of problem 0 and 1.  gated: H.  backward: dG, dU
     long long ld_out;
-    void* gate;              // gated: G and U to save (null: not saved).  backward: read
-    void* up;
+    float* value;            // act(G) and U act'(G): written by the gated form (null: not wanted), read by the backward one
+    float* slope;
     long long ld_save;
-    void* h;                 // backward: H
-    long long ld_h;
     long long M;
     int N, K;
     int segments, problems;
     int tiles_m, tiles_n;
     int type, act;
-    int vec;                 // all rows of the outputs (and of G and U) start on 16-byte boundaries
+    int vec;                 // plain: all rows of the outputs start on 16-byte boundaries
     int* status;
     unsigned long long timeout_ns;
 };
@@ -118,16 +118,17 @@ __device__ __forceinline__ void ffn_tmem_free(uint32_t addr, uint32_t cols) {
     if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
     else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
 }
-// 32 consecutive fp32 columns of this thread's lane; the caller waits with tmem_wait before it uses them
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
+// 16 or 32 consecutive fp32 columns of this thread's lane; the caller waits with tmem_wait before it uses them
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* r) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
+    tmem_load16(addr, r);
+    tmem_load16(addr + 16, r + 16);
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -142,7 +143,7 @@ __device__ __forceinline__ float act_value(int act, float g) {
 __device__ __forceinline__ void act_both(int act, float g, float& value, float& slope) {
     if (act == kActRelu) {
         value = g > 0.f ? g : g * 0.f;
-        slope = g > 0.f ? 1.f : 0.f;
+        slope = g > 0.f ? 1.f : g * 0.f;
     } else if (act == kActGelu) {
         const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
         value = g * cdf;
@@ -162,41 +163,6 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ float2 unpack2(int type, uint32_t w) {
-    if (type == BMGD_TYPE_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-    return __half22float2(*reinterpret_cast<__half2*>(&w));
-}
-// 32 columns of one row: columns from N on are left alone
-__device__ __forceinline__ void store32(void* base, long long ld, long long row, int col, int N, int type, bool vec, const float (&x)[32]) {
-    uint16_t* p = static_cast<uint16_t*>(base) + row * ld + col;
-    if (vec && col + 32 <= N) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            reinterpret_cast<uint4*>(p)[i] = make_uint4(pack2(type, x[8 * i], x[8 * i + 1]), pack2(type, x[8 * i + 2], x[8 * i + 3]),
-                                                        pack2(type, x[8 * i + 4], x[8 * i + 5]), pack2(type, x[8 * i + 6], x[8 * i + 7]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (col + i < N) p[i] = (uint16_t)pack2(type, x[i], 0.f);
-    }
-}
-__device__ __forceinline__ void load32(const void* base, long long ld, long long row, int col, int N, bool vec, uint32_t (&w)[16]) {
-    const uint16_t* p = static_cast<const uint16_t*>(base) + row * ld + col;
-    if (vec && col + 32 <= N) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t lo = col + 2 * i < N ? p[2 * i] : 0u, hi = col + 2 * i + 1 < N ? p[2 * i + 1] : 0u;
-            w[i] = lo | (hi << 16);
-        }
-    }
-}
-
 // ---------------------------------------------------------------- shapes
 template <int CG, int BN>
 struct FfnShape {
@@ -205,7 +171,8 @@ struct FfnShape {
     static constexpr int kStage = kA + kB;
     static constexpr int kStages = kStage > 40960 ? 4 : 6;
     static constexpr int kBars = kStages * kStage;         // mbarriers and the tensor-memory address behind the ring
-    static constexpr int kSmem = kBars + 256 + 1024;       // (1024: the ring starts on a 1024-byte boundary)
+    static constexpr int kTurn = kBars + 256;              // where a warp turns rows per lane into pieces of rows per lane
+    static constexpr int kSmem = kTurn + 4 * 32 * kTurnPitch * 4 + 1024;  // (1024: the ring starts on a 1024-byte boundary)
 };
 
 // fetch `ROWS` rows (K-major) or columns (MN-major) of an operand, from `mn` on, 64 along the contraction from `k` on
@@ -323,10 +290,12 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
             }
         }
     } else if (warp >= 4) {
+        // A lane reads a row out of tensor memory; what a warp writes to (or reads from) global memory at a time should be
+        // pieces of rows.  In between the values take turns through shared memory, 32 to a row.
         int acc = 0;
         uint32_t acc_phase = 0;
         const int quarter = warp & 3;
-        const bool vec = P.vec != 0;
+        float* const turn = reinterpret_cast<float*>(ffn_smem + (ring - smem_u32(ffn_smem)) + S::kTurn) + quarter * 32 * kTurnPitch;
         for (long long t = pair; t < tiles; t += pairs) {
             int which, n0;
             long long m0;
@@ -335,64 +304,113 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
             w.aborted = __any_sync(0xFFFFFFFFu, w.aborted);
             if (w.aborted) break;
             tc_fence_after();
-            const long long row = m0 + (long long)rank * 128 + quarter * 32 + lane;
-            const bool in = row < P.M;
+            const long long row0 = m0 + (long long)rank * 128 + quarter * 32;
+            const int rows = (int)min(32ll, P.M - row0);  // (may be negative)
             const uint32_t ta = tmem + (uint32_t)(acc * BN) + ((uint32_t)(quarter * 32) << 16);
+            if constexpr (EPI == kEpiGated) {
+                // 16 columns of G and 16 of U at a time; then a lane has four columns of rows lane / 4, lane / 4 + 8, ...
+                const int sub = (lane & 3) * 4;
 #pragma unroll 1
-            for (int c = 0; c < kCols; c += 32) {
-                const int col = n0 + c;
-                if (col >= P.N) break;
-                if constexpr (EPI == kEpiGated) {
-                    uint32_t rg[32], ru[32];
-                    tmem_load32(ta + (uint32_t)c, rg);
-                    tmem_load32(ta + (uint32_t)(BN / 2 + c), ru);
+                for (int c = 0; c < kCols; c += 16) {
+                    const int col = n0 + c;
+                    if (col >= P.N) break;
+                    uint32_t r[32];
+                    tmem_load16(ta + (uint32_t)c, r);
+                    tmem_load16(ta + (uint32_t)(BN / 2 + c), r + 16);
                     tmem_wait();
-                    if (in) {
-                        float g[32], u[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) { g[i] = __uint_as_float(rg[i]); u[i] = __uint_as_float(ru[i]); }
-                        if (P.gate) {
-                            store32(P.gate, P.ld_save, row, col, P.N, P.type, vec, g);
-                            store32(P.up, P.ld_save, row, col, P.N, P.type, vec, u);
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<uint4*>(turn + lane * kTurnPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) {
+                        const int i = it * 8 + (lane >> 2);
+                        if (i < rows && col + sub < P.N) {  // (rows of H, act(G) and U act'(G) are padded to multiples of 8)
+                            const float4 g = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + sub);
+                            const float4 u = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + 16 + sub);
+                            float4 v, s;
+                            if (P.value) {
+                                act_both(P.act, g.x, v.x, s.x); act_both(P.act, g.y, v.y, s.y);
+                                act_both(P.act, g.z, v.z, s.z); act_both(P.act, g.w, v.w, s.w);
+                                const long long at = (row0 + i) * P.ld_save + col + sub;
+                                *reinterpret_cast<float4*>(P.value + at) = v;
+                                *reinterpret_cast<float4*>(P.slope + at) = make_float4(u.x * s.x, u.y * s.y, u.z * s.z, u.w * s.w);
+                            } else {
+                                v = make_float4(act_value(P.act, g.x), act_value(P.act, g.y), act_value(P.act, g.z), act_value(P.act, g.w));
+                            }
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out[0]) + (row0 + i) * P.ld_out + col + sub) =
+                                make_uint2(pack2(P.type, v.x * u.x, v.y * u.y), pack2(P.type, v.z * u.z, v.w * u.w));
                         }
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) g[i] = act_value(P.act, g[i]) * u[i];
-                        store32(P.out[0], P.ld_out, row, col, P.N, P.type, vec, g);
                     }
-                } else if constexpr (EPI == kEpiPlain) {
+                    __syncwarp();
+                }
+            } else if constexpr (EPI == kEpiBackward) {
+                const int sub = (lane & 7) * 4;
+#pragma unroll 1
+                for (int c = 0; c < kCols; c += 32) {
+                    const int col = n0 + c;
+                    if (col >= P.N) break;
+                    float4 v[8], s[8];
+#pragma unroll
+                    for (int it = 0; it < 8; ++it) {
+                        const int i = it * 4 + (lane >> 3);
+                        const long long at = (row0 + i) * P.ld_save + col + sub;
+                        if (i < rows && col + sub < P.N) {
+                            v[it] = __ldcs(reinterpret_cast<const float4*>(P.value + at));
+                            s[it] = __ldcs(reinterpret_cast<const float4*>(P.slope + at));
+                        }
+                    }
                     uint32_t r[32];
                     tmem_load32(ta + (uint32_t)c, r);
                     tmem_wait();
-                    if (in) {
-                        float x[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
-                        store32(P.out[which], P.ld_out, row, col, P.N, P.type, vec, x);
-                    }
-                } else {
-                    uint32_t r[32], wg[16], wu[16];
-                    tmem_load32(ta + (uint32_t)c, r);
-                    if (in) {
-                        load32(P.gate, P.ld_save, row, col, P.N, vec, wg);
-                        load32(P.up, P.ld_save, row, col, P.N, vec, wu);
-                    }
-                    tmem_wait();
-                    if (in) {
-                        float dg[32], du[32], h[32];
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<uint4*>(turn + lane * kTurnPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float2 g2 = unpack2(P.type, wg[i >> 1]), u2 = unpack2(P.type, wu[i >> 1]);
-                            const float g = i & 1 ? g2.y : g2.x, u = i & 1 ? u2.y : u2.x, d = __uint_as_float(r[i]);
-                            float value, slope;
-                            act_both(P.act, g, value, slope);
-                            h[i] = value * u;
-                            du[i] = d * value;
-                            dg[i] = d * u * slope;
+                    for (int it = 0; it < 8; ++it) {
+                        const int i = it * 4 + (lane >> 3);
+                        if (i < rows && col + sub < P.N) {
+                            const float4 d = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + sub);
+                            const long long at = (row0 + i) * P.ld_out + col + sub;
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out[0]) + at) =
+                                make_uint2(pack2(P.type, d.x * s[it].x, d.y * s[it].y), pack2(P.type, d.z * s[it].z, d.w * s[it].w));
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out[1]) + at) =
+                                make_uint2(pack2(P.type, d.x * v[it].x, d.y * v[it].y), pack2(P.type, d.z * v[it].z, d.w * v[it].w));
                         }
-                        store32(P.out[0], P.ld_out, row, col, P.N, P.type, vec, dg);
-                        store32(P.out[1], P.ld_out, row, col, P.N, P.type, vec, du);
-                        store32(P.h, P.ld_h, row, col, P.N, P.type, vec, h);
                     }
+                    __syncwarp();
+                }
+            } else {
+                uint16_t* const out = static_cast<uint16_t*>(P.out[which]);
+                uint16_t* const half = reinterpret_cast<uint16_t*>(turn);  // 32 16-bit values to a row here, 40 apart
+#pragma unroll 1
+                for (int c = 0; c < kCols; c += 32) {
+                    const int col = n0 + c;
+                    if (col >= P.N) break;
+                    uint32_t r[32];
+                    tmem_load32(ta + (uint32_t)c, r);
+                    tmem_wait();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t q[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) q[j] = pack2(P.type, __uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
+                        *reinterpret_cast<uint4*>(half + lane * 40 + 8 * i) = make_uint4(q[0], q[1], q[2], q[3]);
+                    }
+                    __syncwarp();
+                    if (P.vec && col + 32 <= P.N) {
+#pragma unroll
+                        for (int it = 0; it < 4; ++it) {
+                            const int i = it * 8 + (lane >> 2), sub = (lane & 3) * 8;
+                            if (i < rows)
+                                *reinterpret_cast<uint4*>(out + (row0 + i) * P.ld_out + col + sub) = *reinterpret_cast<const uint4*>(half + i * 40 + sub);
+                        }
+                    } else if (col + lane < P.N) {
+#pragma unroll 8
+                        for (int i = 0; i < rows; ++i) out[(row0 + i) * P.ld_out + col + lane] = half[i * 40 + lane];
+                    }
+                    __syncwarp();
                 }
             }
             tc_fence_before();

@@ -98,8 +98,12 @@ int launch(FfnParams& P, const Matrix (&a)[2], const Matrix (&b)[2], const Devic
     return BMGD_OK;
 }
 
+// Tiles of 256 rows x 256 columns for two CTAs wherever they fill half the GPU; otherwise tiles of 128 x 128 for one.
 template <int EPI, bool A_MN, bool B_MN>
 int contract(FfnParams& P, const Matrix (&a)[2], const Matrix (&b)[2], const Device& dev, cudaStream_t s) {
+    constexpr int kCols = EPI == kEpiGated ? 128 : 256;
+    const int64_t large = ((P.M + 255) / 256) * ((P.N + kCols - 1) / kCols) * P.problems;
+    if (large * 4 >= dev.sms) return launch<2, 256, EPI, A_MN, B_MN>(P, a, b, dev, s);
     return launch<1, 128, EPI, A_MN, B_MN>(P, a, b, dev, s);
 }
 
@@ -145,13 +149,13 @@ int check(const bmgd_gated_ffn* g, int pass, bool pointers) {
     if (g->ld_x < g->inputs || g->ld_gate < g->hidden || g->ld_up < g->hidden || g->ld_down < g->outputs) return BMGD_ERR_ARG;
     if (pass == BMGD_FFN_BACKWARD && g->ld_dy < g->outputs) return BMGD_ERR_ARG;
     if (pass == BMGD_FFN_FORWARD && g->ld_y < g->outputs) return BMGD_ERR_ARG;
-    if ((pass == BMGD_FFN_BACKWARD || g->saved_gate) && (g->ld_saved < g->hidden || g->ld_saved % 8 != 0)) return BMGD_ERR_ARG;
+    if ((pass == BMGD_FFN_BACKWARD || g->saved_value) && (g->ld_saved < g->hidden || g->ld_saved % 8 != 0)) return BMGD_ERR_ARG;
     if (!pointers || g->rows == 0) return BMGD_OK;
     if (bad_pointer(g->x) || bad_pointer(g->w_gate) || bad_pointer(g->w_up) || bad_pointer(g->w_down)) return BMGD_ERR_ARG;
-    if ((g->saved_gate == nullptr) != (g->saved_up == nullptr)) return BMGD_ERR_ARG;
-    if ((uintptr_t)g->saved_gate % 16 || (uintptr_t)g->saved_up % 16) return BMGD_ERR_ARG;
+    if ((g->saved_value == nullptr) != (g->saved_slope == nullptr) || (g->saved_value == nullptr) != (g->saved_hidden == nullptr)) return BMGD_ERR_ARG;
+    if ((uintptr_t)g->saved_value % 16 || (uintptr_t)g->saved_slope % 16 || (uintptr_t)g->saved_hidden % 16) return BMGD_ERR_ARG;
     if (pass == BMGD_FFN_FORWARD) return bad_pointer(g->y) ? BMGD_ERR_ARG : BMGD_OK;
-    if (!g->saved_gate || bad_pointer(g->dy) || bad_pointer(g->dx) || bad_pointer(g->dw_gate) || bad_pointer(g->dw_up) || bad_pointer(g->dw_down))
+    if (!g->saved_value || bad_pointer(g->dy) || bad_pointer(g->dx) || bad_pointer(g->dw_gate) || bad_pointer(g->dw_up) || bad_pointer(g->dw_down))
         return BMGD_ERR_ARG;
     return BMGD_OK;
 }
@@ -166,8 +170,8 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
         const int rc = align_matrix(m, space, run, s);
         if (rc != BMGD_OK) return rc;
     }
-    const int64_t ldh = up8(g->hidden);
-    void* h = space->take(g->rows * ldh * 2);
+    const int64_t ldh = g->saved_hidden ? g->ld_saved : up8(g->hidden);
+    void* h = g->saved_hidden ? g->saved_hidden : space->take(g->rows * ldh * 2);
     if (!run) return BMGD_OK;
     FfnParams P{};
     P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = 2000000000ull;
@@ -175,8 +179,7 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     P.segments = P.problems = 1;
     P.N = g->hidden; P.K = g->inputs;
     P.out[0] = h; P.ld_out = ldh;
-    P.gate = g->saved_gate; P.up = g->saved_up; P.ld_save = g->ld_saved;
-    P.vec = 1;
+    P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     {
         const Matrix a[2] = {x, x}, b[2] = {wg, wu};
         const int rc = contract<kEpiGated, false, true>(P, a, b, dev, s);
@@ -199,19 +202,17 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
         if (rc != BMGD_OK) return rc;
     }
     const int64_t ldh = up8(g->hidden);
-    const Matrix h{space->take(g->rows * ldh * 2), g->rows, g->hidden, ldh}, dg{space->take(g->rows * ldh * 2), g->rows, g->hidden, ldh},
+    const Matrix h{g->saved_hidden, g->rows, g->hidden, g->ld_saved}, dg{space->take(g->rows * ldh * 2), g->rows, g->hidden, ldh},
         du{space->take(g->rows * ldh * 2), g->rows, g->hidden, ldh};
     if (!run) return BMGD_OK;
     FfnParams P{};
     P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = 2000000000ull;
     int rc;
-    {   // dH, and from it dG, dU and H
+    {   // dH, and from it dG and dU
         P.M = g->rows; P.N = g->hidden; P.K = g->outputs;
         P.segments = P.problems = 1;
         P.out[0] = const_cast<void*>(dg.base); P.out[1] = const_cast<void*>(du.base); P.ld_out = ldh;
-        P.gate = g->saved_gate; P.up = g->saved_up; P.ld_save = g->ld_saved;
-        P.h = const_cast<void*>(h.base); P.ld_h = ldh;
-        P.vec = 1;
+        P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
         const Matrix a[2] = {dy, dy}, b[2] = {wd, wd};
         rc = contract<kEpiBackward, false, false>(P, a, b, dev, s);
         if (rc != BMGD_OK) return rc;

@@ -87,7 +87,8 @@ class _GatedFfn(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64)] + [(k, ctypes.c_int32) for k in (
         "inputs", "hidden", "outputs", "type", "activation", "reserved")] + [(k, ctypes.c_void_p) for k in (
             "x", "w_gate", "w_up", "w_down")] + [(k, ctypes.c_int64) for k in ("ld_x", "ld_gate", "ld_up", "ld_down")] + [
-        ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("saved_gate", ctypes.c_void_p), ("saved_up", ctypes.c_void_p),
+        ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("saved_value", ctypes.c_void_p),
+        ("saved_slope", ctypes.c_void_p), ("saved_hidden", ctypes.c_void_p),
         ("ld_saved", ctypes.c_int64), ("dy", ctypes.c_void_p), ("ld_dy", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in (
             "dx", "dw_gate", "dw_up", "dw_down")]
 
@@ -116,6 +117,12 @@ def _ffn_args(x, w_gate, w_up, w_down, activation) -> _GatedFfn:
     return g
 
 
+def _saved_args(g: _GatedFfn, factors: torch.Tensor, hidden: torch.Tensor) -> None:
+    g.ld_saved = hidden.shape[1]
+    g.saved_value, g.saved_hidden = factors.data_ptr(), hidden.data_ptr()
+    g.saved_slope = factors.data_ptr() + g.rows * g.ld_saved * 4
+
+
 def _workspace(L, g: _GatedFfn, which: int, device: torch.device) -> Tuple[torch.Tensor, int]:
     need = ctypes.c_int64()
     _status(L.bmgd_gated_ffn_workspace_bytes(ctypes.byref(g), which, ctypes.byref(need)), "bmgd_gated_ffn_workspace_bytes")
@@ -134,9 +141,10 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
         y = torch.empty(g.rows, g.outputs, dtype=x.dtype, device=x.device)
         saved = None
         if save:
-            saved = torch.empty(2, g.rows, -(-g.hidden // 8) * 8, dtype=x.dtype, device=x.device)
-            g.saved_gate, g.ld_saved = saved.data_ptr(), saved.shape[2]
-            g.saved_up = saved.data_ptr() + saved.shape[1] * saved.shape[2] * 2
+            width = -(-g.hidden // 8) * 8
+            saved = (torch.empty(2, g.rows, width, dtype=torch.float32, device=x.device),
+                     torch.empty(g.rows, width, dtype=x.dtype, device=x.device))
+            _saved_args(g, *saved)
         if g.rows > 0:
             g.y, g.ld_y = y.data_ptr(), g.outputs
             w, size = _workspace(L, g, _FORWARD, x.device)
@@ -146,22 +154,26 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
 
 
 def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
-                       saved: torch.Tensor, activation: int = ACT_SILU, stream: Optional[torch.cuda.Stream] = None):
+                       saved: Tuple[torch.Tensor, torch.Tensor], activation: int = ACT_SILU,
+                       stream: Optional[torch.cuda.Stream] = None):
     """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the gradient dy of its output.
 
     `saved` is what the forward call on the same arguments returned; the gradients have the type of x."""
     g = _ffn_args(x, w_gate, w_up, w_down, activation)
     g.ld_dy = _matrix(dy, "dy", g.rows, g.outputs, x.dtype, x.device)
     width = -(-g.hidden // 8) * 8
-    if saved.shape != (2, g.rows, width) or saved.dtype != x.dtype or saved.device != x.device or not saved.is_contiguous():
+    if not isinstance(saved, tuple) or len(saved) != 2:
         raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
+    for t, shape, dtype in zip(saved, ((2, g.rows, width), (g.rows, width)), (torch.float32, x.dtype)):
+        if t.shape != shape or t.dtype != dtype or t.device != x.device or not t.is_contiguous():
+            raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
     L = _binding.load_library()
     with _place(x.device, stream):
         dx, dw_gate, dw_up, dw_down = (torch.empty(s, dtype=x.dtype, device=x.device)
                                        for s in (x.shape, w_gate.shape, w_up.shape, w_down.shape))
         g.dx, g.dw_gate, g.dw_up, g.dw_down = dx.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr(), dw_down.data_ptr()
-        g.dy, g.saved_gate, g.ld_saved = dy.data_ptr(), saved.data_ptr(), width
-        g.saved_up = saved.data_ptr() + g.rows * width * 2
+        g.dy = dy.data_ptr()
+        _saved_args(g, *saved)
         w, size = _workspace(L, g, _BACKWARD, x.device)
         _status(L.bmgd_gated_ffn_backward(ctypes.byref(g), w.data_ptr(), size, torch.cuda.current_stream().cuda_stream),
                 "bmgd_gated_ffn_backward")

@@ -106,8 +106,9 @@ class Job:
             denom = torch.sqrt(v1 / c2) + eps
             move = lr / c1 * m1 / denom
             q = p * (1 - lr * self.decays[i]) - move
-            # relative errors of the numerator, the root (half of v's) and four more operations
-            eq = 4 * E32 * p.abs() + move.abs() * 12 * E32 + lr / c1 * em / denom + 2 * E32 * q.abs()
+            # in units of 2^-24: v's error halved by the root 3, the root 2, its factor and that factor's rounding 2, the sum
+            # with eps 1, the quotient 4, the product with the step length and that one's rounding 2: 14, and second-order terms
+            eq = 4 * E32 * p.abs() + move.abs() * 15 * E32 + lr / c1 * em / denom + 2 * E32 * q.abs()
             got = (self.masters or self.params)[i]
             if got.dtype == torch.bfloat16:  # rounded at random: less than one step of bf16, at most 2^-7 of the value
                 eq = eq + 2.0 ** -7 * (q.abs() + eq) + 2.0 ** -130

@@ -64,8 +64,8 @@ class Block:
         y = h @ wd
         ey = eh @ wd.abs() + f * E32 * (h.abs() @ wd.abs())
         out = {"y": (y, ey + u * (y.abs() + ey) + tiny)}
-        # backward: G and U as saved (rounded), products rounded again
-        sg, su = eg + u * (g.abs() + eg) + tiny, eu + u * (up.abs() + eu) + tiny
+        # backward: act(G) and U act'(G) are kept in fp32; dG, dU and H are rounded
+        sg, su = eg, eu
         dh = dy @ wd.T
         edh = c * E32 * (dy.abs() @ wd.abs().T)
         ea = (da.abs() + dda * sg) * sg + (8 + 2 * g.abs()) * E32 * a.abs() + g.abs() * 2.0 ** -22
