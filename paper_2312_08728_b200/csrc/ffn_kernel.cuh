@@ -12,11 +12,8 @@
 // in tensor memory, and act(G) and U act'(G) are kept in fp32 for the backward pass: rounded to 16 bits they would add as much
 // to the gradients' error as both other roundings together, and their traffic hides behind the arithmetic.
 //
-// What bounds it: the tensor cores, from a few hundred rows on.  Warp 0 copies tiles of 64 along the contraction by TMA
-// into a ring of stages with the 128-byte swizzle, warp 1 issues tcgen05.mma, warps 4 to 7 read accumulators out of
-// tensor memory; two accumulators take turns, so that reading one out overlaps the next tile's arithmetic.  With
-// CG = 2 two CTAs of a cluster work on one tile of 256 rows: each fetches its 128 rows of A and half of B, and the
-// even one issues for both.
+// What bounds it: the tensor cores, from a few hundred rows on (ffn_kernel); below, reading the weights once
+// (ffn_few_kernel).
 #pragma once
 #include <cstdint>
 #include <cuda.h>
@@ -33,22 +30,32 @@ enum { kEpiGated = 0, kEpiPlain = 1, kEpiBackward = 2 };
 
 constexpr int kFfnThreads = 256;
 constexpr int kFfnBK = 64;
-constexpr int kTurnPitch = 36;  // words per row there: 32 and four, so that eight lanes' 16-byte accesses meet no bank twice
+constexpr int kTurnPitch = 36;  // words per row of the turning buffer: 32 and four, so that eight lanes' 16-byte accesses meet no bank twice
 constexpr int kFfnGroup = 8;  // tiles along M that are worked on together: their rows of A stay in L2 while B passes
+constexpr int kFfnProblems = 3;
+
+// D [M][N] = sum over segments of A_s B_s
+struct FfnProblem {
+    CUtensorMap a[2], b[2];  // one per segment (gated: b[0] is Wg, b[1] is Wu)
+    void* out;               // D, or H
+    long long ld_out;
+    long long first_tile;    // tiles of all problems before this one
+    int M, N, K;
+    int segments;
+    int tiles_m, tiles_n;
+    int a_mn;                // few rows: the weights are read across their rows
+    int vec;                 // rows of D start on 16-byte boundaries
+};
 
 struct FfnParams {
-    CUtensorMap a[2], b[2];  // second pair: the second half of the contraction (segments = 2) or of the launch (problems = 2)
-    void* out[2];            // plain: D of problem 0 and 1.  gated: H.  backward: dG, dU
-    long long ld_out;
+    FfnProblem p[kFfnProblems];
+    int problems;
+    long long tiles;
+    void* out_up;            // backward: dU beside dG
     float* value;            // act(G) and U act'(G): written by the gated form (null: not wanted), read by the backward one
     float* slope;
     long long ld_save;
-    long long M;
-    int N, K;
-    int segments, problems;
-    int tiles_m, tiles_n;
     int type, act;
-    int vec;                 // plain: all rows of the outputs start on 16-byte boundaries
     int* status;
     unsigned long long timeout_ns;
 };
@@ -70,6 +77,11 @@ __device__ __forceinline__ void ffn_wait(uint32_t bar, uint32_t parity, FfnWait&
         }
     }
 }
+
+// A kernel launched as a dependent of the one before it may start while that one still runs; before it touches memory it
+// waits until that one has finished (and with it all before).
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {
     uint32_t r;
@@ -175,20 +187,41 @@ struct FfnShape {
     static constexpr int kSmem = kTurn + 4 * 32 * kTurnPitch * 4 + 1024;  // (1024: the ring starts on a 1024-byte boundary)
 };
 
-// fetch `ROWS` rows (K-major) or columns (MN-major) of an operand, from `mn` on, 64 along the contraction from `k` on
-template <int CG, bool MN_MAJOR, int ROWS>
-__device__ __forceinline__ void ffn_fetch(uint32_t dst, const CUtensorMap* map, int mn, int k, uint32_t bar) {
-    if constexpr (MN_MAJOR) {
+// fetch `rows` rows (K-major) or columns (MN-major) of an operand, from `mn` on, 64 along the contraction from `k` on
+template <int CG>
+__device__ __forceinline__ void ffn_fetch(uint32_t dst, const CUtensorMap* map, bool mn_major, int rows, int mn, int k, uint32_t bar) {
+    if (mn_major) {
 #pragma unroll
-        for (int i = 0; i < ROWS / 64; ++i) ffn_tma<CG>(dst + (uint32_t)(i * 64 * 128), map, mn + i * 64, k, bar);
+        for (int i = 0; i < rows; i += 64) ffn_tma<CG>(dst + (uint32_t)(i * 128), map, mn + i, k, bar);
     } else {
-        ffn_tma<CG>(dst, map, k, mn, bar);  // the map's box has ROWS rows
+        ffn_tma<CG>(dst, map, k, mn, bar);  // the map's box has that many rows
     }
 }
+// Descriptor of such a tile at address 0, and what one instruction's 16 along the contraction add to it.  One thread issues
+// everything: whatever it computes between two instructions the tensor core may have to wait for.
+struct FfnDesc {
+    uint64_t base;
+    uint32_t step;
+    __device__ __forceinline__ explicit FfnDesc(bool mn_major)
+        : base(mn_major ? tc_smem_desc(0, 64 * 128, 1024) : tc_smem_desc(0, 16, 1024)), step(mn_major ? 2048u >> 4 : 32u >> 4) {}
+    // (a shared-memory address carries the CTA's rank in its cluster in the bits above the offset)
+    __device__ __forceinline__ uint64_t at(uint32_t tile) const { return base + ((tile >> 4) & 0x3FFFu); }
+};
+__device__ __forceinline__ uint32_t ffn_idesc(int type, bool a_mn, bool b_mn, int m, int n) {
+    const uint32_t fmt = type == BMGD_TYPE_BF16 ? 1u : 0u;
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(m >> 4) << 24);
+}
 
-// ---------------------------------------------------------------- the kernel
-// EPI: what is done with a tile.  A_MN, B_MN: the operand is read across its rows.  BN: columns of a tile (gated: BN / 2
-// of G and as many of U).
+// ---------------------------------------------------------------- many rows
+// Warp 0 copies tiles of 64 along the contraction by TMA into a ring of stages with the 128-byte swizzle, warp 1 issues
+// tcgen05.mma, warps 4 to 7 read accumulators out of tensor memory; two accumulators take turns, so that reading one out
+// overlaps the next tile's arithmetic.  With CG = 2 two CTAs of a cluster work on one tile of 256 rows: each fetches its 128
+// rows of A and half of B, and the even one issues for both.  The gradients of the three weights are problems of one
+// launch: their tiles fill the GPU together.
+// EPI: what is done with a tile.  BN: columns of a tile (gated: BN / 2 of G and as many of U).  A_MN, B_MN: an operand is
+// read across its rows.  They are known when the kernel is compiled because one thread fetches and one thread issues for the whole
+// tile: choosing at run time cost 5 % of the forward pass at 4096 rows and 13 % of the backward pass.
 template <int CG, int BN, int EPI, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_constant__ FfnParams P) {
     using S = FfnShape<CG, BN>;
@@ -202,6 +235,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;   // columns of the output that a tile covers
     constexpr uint32_t kTmemCols = 2 * BN;
 
+    let_next_kernel_start();
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, 4 * CG); }
@@ -214,17 +248,17 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    wait_for_previous_kernel();
 
-    const long long per_problem = (long long)P.tiles_m * P.tiles_n;
-    const long long tiles = per_problem * P.problems;
-    const int kblocks = (P.K + kFfnBK - 1) / kFfnBK, steps = kblocks * P.segments;
-    auto place = [&](long long t, int& which, long long& m0, int& n0) {
-        which = (int)(t / per_problem);
-        const long long r = t - which * per_problem, g = r / ((long long)kFfnGroup * P.tiles_n);
-        const int first = (int)g * kFfnGroup, gm = min(kFfnGroup, P.tiles_m - first);
-        const int r2 = (int)(r - g * kFfnGroup * P.tiles_n);
-        m0 = (long long)(first + r2 % gm) * (128 * CG);
-        n0 = (r2 / gm) * kCols;
+    const long long tiles = P.tiles;
+    auto place = [&](long long t, int& which, int& m0, int& n0) {
+        which = 0;
+        while (which + 1 < P.problems && P.p[which + 1].first_tile <= t) ++which;
+        const FfnProblem& q = P.p[which];
+        const unsigned r = (unsigned)(t - q.first_tile), per = (unsigned)(kFfnGroup * q.tiles_n), g = r / per;
+        const unsigned first = g * kFfnGroup, gm = min((unsigned)kFfnGroup, (unsigned)q.tiles_m - first), r2 = r - g * per;
+        m0 = (int)(first + r2 % gm) * (128 * CG);
+        n0 = (int)(r2 / gm) * kCols;
     };
     FfnWait w{P.status, P.timeout_ns, false};
 
@@ -233,54 +267,57 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
             int s = 0;
             uint32_t phase = 0;
             for (long long t = pair; t < tiles && !w.aborted; t += pairs) {
-                int which, n0;
-                long long m0;
+                int which, m0, n0;
                 place(t, which, m0, n0);
-                const int am = (int)m0 + (int)rank * 128;
-                for (int k = 0; k < steps; ++k) {
-                    ffn_wait(empty + 8 * s, phase ^ 1u, w);
-                    if (w.aborted) break;
-                    const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
-                    uint32_t bar = full + 8 * s;
-                    if (rank == 0) mbar_arrive_expect_tx(bar, S::kStage * CG);
-                    if constexpr (CG == 2) bar = leader_addr(bar);
-                    const uint32_t sa = ring + s * S::kStage, sb = sa + S::kA;
-                    ffn_fetch<CG, A_MN, 128>(sa, &P.a[seg], am, k0, bar);
-                    if constexpr (EPI == kEpiGated) {
-                        // the first half of the tile's columns is G, the second U; with two CTAs one fetches each
-                        if constexpr (CG == 2) ffn_fetch<CG, B_MN, BN / 2>(sb, &P.b[rank], n0, k0, bar);
-                        else {
-                            ffn_fetch<CG, B_MN, BN / 2>(sb, &P.b[0], n0, k0, bar);
-                            ffn_fetch<CG, B_MN, BN / 2>(sb + S::kB / 2, &P.b[1], n0, k0, bar);
+                const FfnProblem& q = P.p[which];
+                const int am = m0 + (int)rank * 128, K = q.K, segments = q.segments;
+                for (int seg = 0; seg < segments && !w.aborted; ++seg) {
+                    const CUtensorMap* const map_a = &q.a[seg];
+                    const CUtensorMap* const map_b = EPI == kEpiGated ? &q.b[rank] : &q.b[seg];
+                    for (int k0 = 0; k0 < K; k0 += kFfnBK) {
+                        ffn_wait(empty + 8 * s, phase ^ 1u, w);
+                        if (w.aborted) break;
+                        uint32_t bar = full + 8 * s;
+                        if (rank == 0) mbar_arrive_expect_tx(bar, S::kStage * CG);
+                        if constexpr (CG == 2) bar = leader_addr(bar);
+                        const uint32_t sa = ring + s * S::kStage, sb = sa + S::kA;
+                        ffn_fetch<CG>(sa, map_a, A_MN, 128, am, k0, bar);
+                        if constexpr (EPI == kEpiGated) {
+                            // the first half of the tile's columns is G, the second U; with two CTAs one fetches each
+                            if constexpr (CG == 2) ffn_fetch<CG>(sb, map_b, B_MN, BN / 2, n0, k0, bar);
+                            else {
+                                ffn_fetch<CG>(sb, map_b, B_MN, BN / 2, n0, k0, bar);
+                                ffn_fetch<CG>(sb + S::kB / 2, map_b + 1, B_MN, BN / 2, n0, k0, bar);
+                            }
+                        } else {
+                            ffn_fetch<CG>(sb, map_b, B_MN, BN / CG, n0 + (int)rank * (BN / CG), k0, bar);
                         }
-                    } else {
-                        ffn_fetch<CG, B_MN, BN / CG>(sb, &P.b[seg + which], n0 + (int)rank * (BN / CG), k0, bar);
+                        if (++s == S::kStages) { s = 0; phase ^= 1u; }
                     }
-                    if (++s == S::kStages) { s = 0; phase ^= 1u; }
                 }
             }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            const uint32_t fmt = P.type == BMGD_TYPE_BF16 ? 1u : 0u;
-            const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
-                                   ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
+            const uint32_t idesc = ffn_idesc(P.type, A_MN, B_MN, 128 * CG, BN);
+            const FfnDesc ad(A_MN), bd(B_MN);
             int s = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             for (long long t = pair; t < tiles && !w.aborted; t += pairs) {
+                int which, m0, n0;
+                place(t, which, m0, n0);
+                const FfnProblem& q = P.p[which];
+                const int steps = q.segments * ((q.K + kFfnBK - 1) / kFfnBK);
                 ffn_wait(acc_empty + 8 * acc, acc_phase ^ 1u, w);
                 tc_fence_after();
                 for (int k = 0; k < steps && !w.aborted; ++k) {
                     ffn_wait(full + 8 * s, phase, w);
                     if (w.aborted) break;
                     tc_fence_after();
-                    const uint32_t sa = ring + s * S::kStage, sb = sa + S::kA;
+                    uint64_t da = ad.at(ring + s * S::kStage), db = bd.at(ring + s * S::kStage + S::kA);
 #pragma unroll
-                    for (int i = 0; i < kFfnBK / 16; ++i) {
-                        const uint64_t da = A_MN ? tc_smem_desc(sa + i * 2048, 64 * 128, 1024) : tc_smem_desc(sa + i * 32, 16, 1024);
-                        const uint64_t db = B_MN ? tc_smem_desc(sb + i * 2048, 64 * 128, 1024) : tc_smem_desc(sb + i * 32, 16, 1024);
+                    for (int i = 0; i < kFfnBK / 16; ++i, da += ad.step, db += bd.step)
                         ffn_mma<CG>(tmem + (uint32_t)(acc * BN), da, db, idesc, (k | i) != 0 ? 1u : 0u);
-                    }
                     ffn_commit<CG>(empty + 8 * s);
                     if (++s == S::kStages) { s = 0; phase ^= 1u; }
                 }
@@ -297,15 +334,18 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
         const int quarter = warp & 3;
         float* const turn = reinterpret_cast<float*>(ffn_smem + (ring - smem_u32(ffn_smem)) + S::kTurn) + quarter * 32 * kTurnPitch;
         for (long long t = pair; t < tiles; t += pairs) {
-            int which, n0;
-            long long m0;
+            int which, m0, n0;
             place(t, which, m0, n0);
+            const FfnProblem& q = P.p[which];
+            const int N = q.N;
+            const long long ld_out = q.ld_out;
+            uint16_t* const out = static_cast<uint16_t*>(q.out);
             ffn_wait(acc_full + 8 * acc, acc_phase, w);
             w.aborted = __any_sync(0xFFFFFFFFu, w.aborted);
             if (w.aborted) break;
             tc_fence_after();
-            const long long row0 = m0 + (long long)rank * 128 + quarter * 32;
-            const int rows = (int)min(32ll, P.M - row0);  // (may be negative)
+            const long long row0 = (long long)m0 + rank * 128 + quarter * 32;
+            const int rows = (int)min(32ll, q.M - row0);  // (may be negative)
             const uint32_t ta = tmem + (uint32_t)(acc * BN) + ((uint32_t)(quarter * 32) << 16);
             if constexpr (EPI == kEpiGated) {
                 // 16 columns of G and 16 of U at a time; then a lane has four columns of rows lane / 4, lane / 4 + 8, ...
@@ -313,7 +353,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
 #pragma unroll 1
                 for (int c = 0; c < kCols; c += 16) {
                     const int col = n0 + c;
-                    if (col >= P.N) break;
+                    if (col >= N) break;
                     uint32_t r[32];
                     tmem_load16(ta + (uint32_t)c, r);
                     tmem_load16(ta + (uint32_t)(BN / 2 + c), r + 16);
@@ -325,7 +365,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
 #pragma unroll
                     for (int it = 0; it < 4; ++it) {
                         const int i = it * 8 + (lane >> 2);
-                        if (i < rows && col + sub < P.N) {  // (rows of H, act(G) and U act'(G) are padded to multiples of 8)
+                        if (i < rows && col + sub < N) {  // (rows of H, act(G) and U act'(G) are padded to multiples of 8)
                             const float4 g = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + sub);
                             const float4 u = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + 16 + sub);
                             float4 v, s;
@@ -338,7 +378,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
                             } else {
                                 v = make_float4(act_value(P.act, g.x), act_value(P.act, g.y), act_value(P.act, g.z), act_value(P.act, g.w));
                             }
-                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out[0]) + (row0 + i) * P.ld_out + col + sub) =
+                            *reinterpret_cast<uint2*>(out + (row0 + i) * ld_out + col + sub) =
                                 make_uint2(pack2(P.type, v.x * u.x, v.y * u.y), pack2(P.type, v.z * u.z, v.w * u.w));
                         }
                     }
@@ -349,13 +389,13 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
 #pragma unroll 1
                 for (int c = 0; c < kCols; c += 32) {
                     const int col = n0 + c;
-                    if (col >= P.N) break;
+                    if (col >= N) break;
                     float4 v[8], s[8];
 #pragma unroll
                     for (int it = 0; it < 8; ++it) {
                         const int i = it * 4 + (lane >> 3);
                         const long long at = (row0 + i) * P.ld_save + col + sub;
-                        if (i < rows && col + sub < P.N) {
+                        if (i < rows && col + sub < N) {
                             v[it] = __ldcs(reinterpret_cast<const float4*>(P.value + at));
                             s[it] = __ldcs(reinterpret_cast<const float4*>(P.slope + at));
                         }
@@ -370,24 +410,23 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
 #pragma unroll
                     for (int it = 0; it < 8; ++it) {
                         const int i = it * 4 + (lane >> 3);
-                        if (i < rows && col + sub < P.N) {
+                        if (i < rows && col + sub < N) {
                             const float4 d = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + sub);
-                            const long long at = (row0 + i) * P.ld_out + col + sub;
-                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out[0]) + at) =
+                            const long long at = (row0 + i) * ld_out + col + sub;
+                            *reinterpret_cast<uint2*>(out + at) =
                                 make_uint2(pack2(P.type, d.x * s[it].x, d.y * s[it].y), pack2(P.type, d.z * s[it].z, d.w * s[it].w));
-                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out[1]) + at) =
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out_up) + at) =
                                 make_uint2(pack2(P.type, d.x * v[it].x, d.y * v[it].y), pack2(P.type, d.z * v[it].z, d.w * v[it].w));
                         }
                     }
                     __syncwarp();
                 }
             } else {
-                uint16_t* const out = static_cast<uint16_t*>(P.out[which]);
                 uint16_t* const half = reinterpret_cast<uint16_t*>(turn);  // 32 16-bit values to a row here, 40 apart
 #pragma unroll 1
                 for (int c = 0; c < kCols; c += 32) {
                     const int col = n0 + c;
-                    if (col >= P.N) break;
+                    if (col >= N) break;
                     uint32_t r[32];
                     tmem_load32(ta + (uint32_t)c, r);
                     tmem_wait();
@@ -399,16 +438,16 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
                         *reinterpret_cast<uint4*>(half + lane * 40 + 8 * i) = make_uint4(q[0], q[1], q[2], q[3]);
                     }
                     __syncwarp();
-                    if (P.vec && col + 32 <= P.N) {
+                    if (q.vec && col + 32 <= N) {
 #pragma unroll
                         for (int it = 0; it < 4; ++it) {
                             const int i = it * 8 + (lane >> 2), sub = (lane & 3) * 8;
                             if (i < rows)
-                                *reinterpret_cast<uint4*>(out + (row0 + i) * P.ld_out + col + sub) = *reinterpret_cast<const uint4*>(half + i * 40 + sub);
+                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + sub) = *reinterpret_cast<const uint4*>(half + i * 40 + sub);
                         }
-                    } else if (col + lane < P.N) {
+                    } else if (col + lane < N) {
 #pragma unroll 8
-                        for (int i = 0; i < rows; ++i) out[(row0 + i) * P.ld_out + col + lane] = half[i * 40 + lane];
+                        for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + lane] = half[i * 40 + lane];
                     }
                     __syncwarp();
                 }
@@ -435,15 +474,209 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     if (warp == 2) ffn_tmem_free<CG>(tmem, kTmemCols);
 }
 
-// rows of `cols` 16-bit values from stride ld to stride ld_out >= cols, the rest of each row zero: for operands whose
-// rows do not start on 16-byte boundaries, which TMA cannot read
-__global__ void __launch_bounds__(256) ffn_align_kernel(const uint16_t* __restrict__ in, long long ld, uint16_t* __restrict__ out,
-                                                        long long ld_out, long long rows, int cols) {
-    const long long total = rows * ld_out;
+// ---------------------------------------------------------------- few rows
+// The same contractions for up to a few hundred rows, with the roles exchanged: 128 features (columns of the weights) are
+// the rows of a tile, and the NR rows of X its columns, so that the tensor core wastes nothing on missing rows and a stage
+// of the ring is nearly all weights.  The contraction is split over the S CTAs of a cluster, as many as give
+// each SM something to read; their partial sums are added through distributed shared memory in the order of the CTAs.
+constexpr int kFewPart = 128;  // features of a tile
+
+template <int NR, int EPI>
+struct FewShape {
+    static constexpr int kTiles = EPI == kEpiGated ? 2 : 1;       // tiles of weights per stage: Wg and Wu
+    static constexpr int kA = 128 * kFfnBK * 2;
+    static constexpr int kStage = kTiles * kA + NR * kFfnBK * 2;
+    static constexpr int kCtasPerSm = NR <= 64 ? 2 : 1;
+    static constexpr int kRoom = kCtasPerSm == 2 ? 110 * 1024 : 214 * 1024;
+    static constexpr int kStages = kRoom / kStage > 10 ? 10 : kRoom / kStage;
+    static constexpr int kRing = kStages * kStage;
+    static constexpr int kParts = kTiles * NR * kFewPart * 4;      // partial sums, in the ring's place once it is done with
+    static constexpr int kBars = kRing > kParts ? kRing : kParts;
+    static constexpr int kSmem = kBars + 256 + 1024;
+    static constexpr uint32_t kTmemCols = kTiles * NR < 32 ? 32 : kTiles * NR;
+};
+
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr, int cta) {
+    uint32_t a;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(cta));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store4_any(uint16_t* p, int type, bool vec, int left, float4 v) {
+    const uint32_t lo = pack2(type, v.x, v.y), hi = pack2(type, v.z, v.w);
+    if (vec && left >= 4) { *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi); return; }
+    if (left > 0) p[0] = (uint16_t)lo;
+    if (left > 1) p[1] = (uint16_t)(lo >> 16);
+    if (left > 2) p[2] = (uint16_t)hi;
+    if (left > 3) p[3] = (uint16_t)(hi >> 16);
+}
+
+// grid: x = S CTAs (one cluster) per tile of 128 features, y = tiles of NR rows.  p[0].a: the weights, p[0].b: the rows.
+template <int NR, int EPI>
+__global__ void __launch_bounds__(kFfnThreads) ffn_few_kernel(const __grid_constant__ FfnParams P, const int S) {
+    using F = FewShape<NR, EPI>;
+    extern __shared__ unsigned char ffn_smem[];
+    const uint32_t ring = (smem_u32(ffn_smem) + 1023u) & ~1023u;
+    const uint32_t full = ring + F::kBars, empty = full + 8 * F::kStages, done = empty + 8 * F::kStages, slot = done + 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const FfnProblem& q = P.p[0];
+    const int part = (int)blockIdx.x % S, f0 = ((int)blockIdx.x / S) * kFewPart, r0 = (int)blockIdx.y * NR;
+
+    let_next_kernel_start();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < F::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        mbar_init(done, 1);
+        fence_barrier_init();
+    }
+    if (warp == 2) ffn_tmem_alloc<1>(slot, F::kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    wait_for_previous_kernel();
+
+    const int kblocks = (q.K + kFfnBK - 1) / kFfnBK, steps = kblocks * q.segments;
+    const int first = (int)((long long)steps * part / S), last = (int)((long long)steps * (part + 1) / S);
+    FfnWait w{P.status, P.timeout_ns, false};
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t phase = 0;
+            for (int k = first; k < last; ++k) {
+                ffn_wait(empty + 8 * s, phase ^ 1u, w);
+                if (w.aborted) break;
+                const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
+                const uint32_t bar = full + 8 * s, sa = ring + s * F::kStage;
+                mbar_arrive_expect_tx(bar, F::kStage);
+                if constexpr (EPI == kEpiGated) {
+                    ffn_fetch<1>(sa, &q.a[0], q.a_mn, 128, f0, k0, bar);
+                    ffn_fetch<1>(sa + F::kA, &q.a[1], q.a_mn, 128, f0, k0, bar);
+                } else {
+                    ffn_fetch<1>(sa, &q.a[seg], q.a_mn, 128, f0, k0, bar);
+                }
+                ffn_fetch<1>(sa + F::kTiles * F::kA, &q.b[EPI == kEpiGated ? 0 : seg], false, NR, r0, k0, bar);
+                if (++s == F::kStages) { s = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const bool a_mn = q.a_mn;
+            const uint32_t idesc = ffn_idesc(P.type, a_mn, false, 128, NR);
+            const FfnDesc ad(a_mn), bd(false);
+            int s = 0;
+            uint32_t phase = 0;
+            for (int k = first; k < last; ++k) {
+                ffn_wait(full + 8 * s, phase, w);
+                if (w.aborted) break;
+                tc_fence_after();
+                uint64_t da = ad.at(ring + s * F::kStage), db = bd.at(ring + s * F::kStage + F::kTiles * F::kA);
+#pragma unroll
+                for (int i = 0; i < kFfnBK / 16; ++i, da += ad.step, db += bd.step) {
+#pragma unroll
+                    for (int h = 0; h < F::kTiles; ++h)
+                        ffn_mma<1>(tmem + (uint32_t)(h * NR), da + (uint64_t)(h * (F::kA >> 4)), db, idesc, (k != first || i != 0) ? 1u : 0u);
+                }
+                ffn_commit<1>(empty + 8 * s);
+                if (++s == F::kStages) { s = 0; phase ^= 1u; }
+            }
+            if (!w.aborted) ffn_commit<1>(done);
+        }
+    }
+    __syncwarp();
+    // every thread waits for the last product: after it the ring's memory is free for the partial sums [NR][128 features]
+    ffn_wait(done, 0, w);
+    tc_fence_after();
+    if (warp >= 4) {
+        const uint32_t ta = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t to = ring + (uint32_t)(((warp & 3) * 32 + lane) * 4);
+#pragma unroll 1
+        for (int c = 0; c < F::kTiles * NR; c += 16) {
+            uint32_t r[16];
+            tmem_load16(ta + (uint32_t)c, r);
+            tmem_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)((c + i) * kFewPart * 4)), "r"(r[i]) : "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
+    // each CTA finishes its share of the rows: a warp a row at a time, four features per lane
+    const int f = f0 + lane * 4, left = q.N - f;
+    uint16_t* const out = static_cast<uint16_t*>(q.out);
+    const int rows = min(NR, q.M - r0);
+    const bool given_up = __syncthreads_or(w.aborted ? 1 : 0) != 0;
+    for (int i = part * (kFfnThreads / 32) + warp; i < rows && !given_up; i += S * (kFfnThreads / 32)) {
+        const uint32_t at = ring + (uint32_t)((i * kFewPart + lane * 4) * 4);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), u = x;
+        for (int c = 0; c < S; ++c) {
+            const float4 y = ld_cluster4(at, c);
+            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+            if constexpr (EPI == kEpiGated) {
+                const float4 z = ld_cluster4(at + NR * kFewPart * 4, c);
+                u.x += z.x; u.y += z.y; u.z += z.z; u.w += z.w;
+            }
+        }
+        if (left <= 0) continue;
+        const long long row = r0 + i;
+        if constexpr (EPI == kEpiGated) {
+            float4 v, s;
+            act_both(P.act, x.x, v.x, s.x); act_both(P.act, x.y, v.y, s.y);
+            act_both(P.act, x.z, v.z, s.z); act_both(P.act, x.w, v.w, s.w);
+            if (P.value) {
+                *reinterpret_cast<float4*>(P.value + row * P.ld_save + f) = v;
+                *reinterpret_cast<float4*>(P.slope + row * P.ld_save + f) = make_float4(u.x * s.x, u.y * s.y, u.z * s.z, u.w * s.w);
+            }
+            store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(v.x * u.x, v.y * u.y, v.z * u.z, v.w * u.w));
+        } else if constexpr (EPI == kEpiBackward) {
+            const float4 v = *reinterpret_cast<const float4*>(P.value + row * P.ld_save + f);
+            const float4 s = *reinterpret_cast<const float4*>(P.slope + row * P.ld_save + f);
+            store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * s.x, x.y * s.y, x.z * s.z, x.w * s.w));
+            store4_any(static_cast<uint16_t*>(P.out_up) + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * v.x, x.y * v.y, x.z * v.z, x.w * v.w));
+        } else {
+            store4_any(out + row * q.ld_out + f, P.type, q.vec, left, x);
+        }
+    }
+    if (given_up) {  // copies and products may still be in flight
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < kSmxLingerNs) __nanosleep(1000);
+    }
+    __syncthreads();
+    if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }  // peers have read this CTA's sums
+    tc_fence_after();
+    if (warp == 2) ffn_tmem_free<1>(tmem, F::kTmemCols);
+}
+
+// ---------------------------------------------------------------- operands that TMA cannot read
+// Rows of `cols` 16-bit values from stride ld to stride ld_out (a multiple of 8, at least cols), the rest of each row zero.
+struct AlignJob {
+    const uint16_t* in;
+    uint16_t* out;
+    long long ld, rows;
+    int ld_out, cols;
+};
+struct AlignParams {
+    AlignJob job[5];
+};
+__global__ void __launch_bounds__(256) ffn_align_kernel(const __grid_constant__ AlignParams P) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const AlignJob& j = P.job[blockIdx.y];
+    const unsigned per = (unsigned)j.ld_out / 8;
+    const long long total = j.rows * per;
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        const long long r = i / ld_out;
-        const int c = (int)(i - r * ld_out);
-        out[i] = c < cols ? in[r * ld + c] : (uint16_t)0;
+        const long long r = i / per;
+        const int c = (int)(i - r * per) * 8;
+        const uint16_t* in = j.in + r * j.ld + c;
+        uint32_t v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = c + 2 * k < j.cols ? in[2 * k] : 0u, hi = c + 2 * k + 1 < j.cols ? in[2 * k + 1] : 0u;
+            v[k] = lo | (hi << 16);
+        }
+        *reinterpret_cast<uint4*>(j.out + r * j.ld_out + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
 

@@ -68,43 +68,112 @@ int current_device(Device* d) {
     return BMGD_OK;
 }
 
+// One contraction as the host describes it: out [M][N] = sum over segments of a[s] b[s].
+struct Problem {
+    Matrix a[2], b[2];
+    void* out;
+    int64_t ld_out;
+    int64_t M;
+    int N, K, segments;
+    bool vec;
+};
+
+int launch_config(cudaLaunchConfig_t* lc, cudaLaunchAttribute (&at)[2], dim3 grid, int smem, int cluster, cudaStream_t s) {
+    lc->gridDim = grid;
+    lc->blockDim = dim3(kFfnThreads);
+    lc->dynamicSmemBytes = smem;
+    lc->stream = s;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    lc->attrs = at;
+    lc->numAttrs = cluster > 1 ? 2 : 1;
+    return BMGD_OK;
+}
+
 template <int CG, int BN, int EPI, bool A_MN, bool B_MN>
-int launch(FfnParams& P, const Matrix (&a)[2], const Matrix (&b)[2], const Device& dev, cudaStream_t s) {
+int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
     using S = FfnShape<CG, BN>;
     constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;
-    const int pairs_b = EPI == kEpiGated ? 2 : std::max(P.segments, P.problems);
-    for (int i = 0; i < 2; ++i) {
-        const int ka = i < P.segments ? i : 0, kb = i < pairs_b ? i : 0;
-        int rc = make_map(a[ka], P.type, A_MN ? 64 : 128, &P.a[i]);
-        if (rc == BMGD_OK) rc = make_map(b[kb], P.type, B_MN ? 64 : (EPI == kEpiGated ? BN / 2 : BN / CG), &P.b[i]);
-        if (rc != BMGD_OK) return rc;
+    int64_t tiles = 0;
+    for (int k = 0; k < count; ++k) {
+        const Problem& x = problems[k];
+        FfnProblem& q = P.p[k];
+        for (int i = 0; i < 2; ++i) {
+            int rc = BMGD_OK;
+            if (i < x.segments) rc = make_map(x.a[i], P.type, A_MN ? 64 : 128, &q.a[i]);
+            if (rc == BMGD_OK && (i < x.segments || EPI == kEpiGated)) rc = make_map(x.b[i], P.type, B_MN ? 64 : BN / CG, &q.b[i]);
+            if (rc != BMGD_OK) return rc;
+        }
+        q.out = x.out; q.ld_out = x.ld_out;
+        q.M = (int)x.M; q.N = x.N; q.K = x.K; q.segments = x.segments;
+        q.vec = x.vec;
+        q.tiles_m = (int)((x.M + 128 * CG - 1) / (128 * CG));
+        q.tiles_n = (x.N + kCols - 1) / kCols;
+        q.first_tile = tiles;
+        tiles += (int64_t)q.tiles_m * q.tiles_n;
     }
-    P.tiles_m = (int)((P.M + 128 * CG - 1) / (128 * CG));
-    P.tiles_n = (P.N + kCols - 1) / kCols;
-    const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n * P.problems;
+    P.problems = count;
+    P.tiles = tiles;
     if (S::kSmem > dev.smem) return BMGD_ERR_LAUNCH;
     auto* fn = ffn_kernel<CG, BN, EPI, A_MN, B_MN>;
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3((unsigned)std::min<int64_t>(tiles, dev.sms / CG) * CG);
-    lc.blockDim = dim3(kFfnThreads);
-    lc.dynamicSmemBytes = S::kSmem;
-    lc.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    lc.attrs = at; lc.numAttrs = CG > 1 ? 1 : 0;
+    cudaLaunchAttribute at[2];
+    launch_config(&lc, at, dim3((unsigned)std::min<int64_t>(tiles, dev.sms / CG) * CG), S::kSmem, CG, s);
     if (cudaLaunchKernelEx(&lc, fn, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
 
-// Tiles of 256 rows x 256 columns for two CTAs wherever they fill half the GPU; otherwise tiles of 128 x 128 for one.
+// Many rows.  Tiles of 256 rows x 256 columns for two CTAs wherever they fill half the GPU; otherwise tiles of 128 x 128.
 template <int EPI, bool A_MN, bool B_MN>
-int contract(FfnParams& P, const Matrix (&a)[2], const Matrix (&b)[2], const Device& dev, cudaStream_t s) {
+int contract(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
     constexpr int kCols = EPI == kEpiGated ? 128 : 256;
-    const int64_t large = ((P.M + 255) / 256) * ((P.N + kCols - 1) / kCols) * P.problems;
-    if (large * 4 >= dev.sms) return launch<2, 256, EPI, A_MN, B_MN>(P, a, b, dev, s);
-    return launch<1, 128, EPI, A_MN, B_MN>(P, a, b, dev, s);
+    int64_t large = 0;
+    for (int k = 0; k < count; ++k) large += ((problems[k].M + 255) / 256) * ((problems[k].N + kCols - 1) / kCols);
+    if (large * 4 >= dev.sms) return launch<2, 256, EPI, A_MN, B_MN>(P, problems, count, dev, s);
+    return launch<1, 128, EPI, A_MN, B_MN>(P, problems, count, dev, s);
+}
+
+template <int NR, int EPI, bool W_MN>
+int launch_few(FfnParams& P, const Problem& x, const Device& dev, cudaStream_t s) {
+    using F = FewShape<NR, EPI>;
+    FfnProblem& q = P.p[0];
+    // exchanged roles: the weights are the kernel's a, read across the rows where the other form's b is
+    for (int i = 0; i < 2; ++i) {
+        int rc = BMGD_OK;
+        if (i < x.segments || EPI == kEpiGated) rc = make_map(x.b[i], P.type, W_MN ? 64 : 128, &q.a[i]);
+        if (rc == BMGD_OK && i < x.segments) rc = make_map(x.a[i], P.type, NR, &q.b[i]);
+        if (rc != BMGD_OK) return rc;
+    }
+    q.out = x.out; q.ld_out = x.ld_out;
+    q.M = (int)x.M; q.N = x.N; q.K = x.K; q.segments = x.segments;
+    q.a_mn = W_MN; q.vec = x.vec;
+    P.problems = 1;
+    const int tiles = (x.N + kFewPart - 1) / kFewPart, row_tiles = (int)((x.M + NR - 1) / NR);
+    const int steps = x.segments * ((x.K + kFfnBK - 1) / kFfnBK);
+    const int room = dev.sms * F::kCtasPerSm / std::max(1, tiles * row_tiles);
+    const int split = std::max(1, std::min(std::min(8, room), steps / 2));
+    if (F::kSmem > dev.smem) return BMGD_ERR_LAUNCH;
+    auto* fn = ffn_few_kernel<NR, EPI>;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    cudaLaunchConfig_t lc{};
+    cudaLaunchAttribute at[2];
+    launch_config(&lc, at, dim3((unsigned)(tiles * split), (unsigned)row_tiles), F::kSmem, split, s);
+    if (cudaLaunchKernelEx(&lc, fn, P, split) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    return BMGD_OK;
+}
+
+// Rows x weights (W_MN: the weights are read across their rows): up to 256 rows with exchanged roles (two tiles of 128 from 129 on).
+constexpr int64_t kFewRows = 256;
+template <int EPI, bool W_MN>
+int rows_by_weights(FfnParams& P, const Problem& x, const Device& dev, cudaStream_t s) {
+    if (x.M > kFewRows) return contract<EPI, false, W_MN>(P, &x, 1, dev, s);
+    if (x.M <= 16) return launch_few<16, EPI, W_MN>(P, x, dev, s);
+    if (x.M <= 32) return launch_few<32, EPI, W_MN>(P, x, dev, s);
+    if (x.M <= 64) return launch_few<64, EPI, W_MN>(P, x, dev, s);
+    return launch_few<128, EPI, W_MN>(P, x, dev, s);
 }
 
 int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -122,18 +191,26 @@ struct Space {
     }
 };
 
-int align_matrix(Matrix* m, Space* space, bool run, cudaStream_t s) {
-    if (tma_ready(*m)) return BMGD_OK;
-    Matrix to = *m;
-    to.ld = up8(m->cols);
-    to.base = space->take(to.rows * to.ld * 2);
-    if (run) {
-        const int64_t total = to.rows * to.ld;
-        ffn_align_kernel<<<(unsigned)std::min<int64_t>((total + 255) / 256, 148 * 16), 256, 0, s>>>(
-            static_cast<const uint16_t*>(m->base), m->ld, static_cast<uint16_t*>(const_cast<void*>(to.base)), to.ld, to.rows, (int)to.cols);
-        if (cudaGetLastError() != cudaSuccess) return BMGD_ERR_CUDA;
+// Operands that TMA cannot read are copied, all of them in one launch.
+int align_matrices(Matrix* const* list, int count, Space* space, bool run, cudaStream_t s) {
+    AlignParams P{};
+    int jobs = 0;
+    int64_t most = 0;
+    for (int i = 0; i < count; ++i) {
+        Matrix* m = list[i];
+        if (tma_ready(*m)) continue;
+        Matrix to = *m;
+        to.ld = up8(m->cols);
+        to.base = space->take(to.rows * to.ld * 2);
+        P.job[jobs++] = AlignJob{static_cast<const uint16_t*>(m->base), static_cast<uint16_t*>(const_cast<void*>(to.base)), m->ld, m->rows, (int)to.ld, (int)m->cols};
+        most = std::max(most, to.rows * (to.ld / 8));
+        *m = to;
     }
-    *m = to;
+    if (!run || jobs == 0) return BMGD_OK;
+    cudaLaunchConfig_t lc{};
+    cudaLaunchAttribute at[2];
+    launch_config(&lc, at, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 148 * 8), (unsigned)jobs), 0, 1, s);
+    if (cudaLaunchKernelEx(&lc, ffn_align_kernel, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
 
@@ -160,84 +237,53 @@ int check(const bmgd_gated_ffn* g, int pass, bool pointers) {
     return BMGD_OK;
 }
 
+constexpr unsigned long long kTimeoutNs = 2000000000ull;  // bound on any single wait inside a kernel
+
 bool wide(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
 // run = false: only counts the workspace
 int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, int* status, cudaStream_t s) {
     Matrix x{g->x, g->rows, g->inputs, g->ld_x}, wg{g->w_gate, g->inputs, g->hidden, g->ld_gate},
         wu{g->w_up, g->inputs, g->hidden, g->ld_up}, wd{g->w_down, g->hidden, g->outputs, g->ld_down};
-    for (Matrix* m : {&x, &wg, &wu, &wd}) {
-        const int rc = align_matrix(m, space, run, s);
-        if (rc != BMGD_OK) return rc;
-    }
+    Matrix* const operands[4] = {&x, &wg, &wu, &wd};
+    int rc = align_matrices(operands, 4, space, run, s);
+    if (rc != BMGD_OK) return rc;
     const int64_t ldh = g->saved_hidden ? g->ld_saved : up8(g->hidden);
     void* h = g->saved_hidden ? g->saved_hidden : space->take(g->rows * ldh * 2);
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = 2000000000ull;
-    P.M = g->rows;
-    P.segments = P.problems = 1;
-    P.N = g->hidden; P.K = g->inputs;
-    P.out[0] = h; P.ld_out = ldh;
+    P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = kTimeoutNs;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
-    {
-        const Matrix a[2] = {x, x}, b[2] = {wg, wu};
-        const int rc = contract<kEpiGated, false, true>(P, a, b, dev, s);
-        if (rc != BMGD_OK) return rc;
-    }
-    P.N = g->outputs; P.K = g->hidden;
-    P.out[0] = g->y; P.ld_out = g->ld_y;
-    P.vec = wide(g->y, g->ld_y);
+    rc = rows_by_weights<kEpiGated, true>(P, Problem{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true}, dev, s);
+    if (rc != BMGD_OK) return rc;
     const Matrix hm{h, g->rows, g->hidden, ldh};
-    const Matrix a[2] = {hm, hm}, b[2] = {wd, wd};
-    return contract<kEpiPlain, false, true>(P, a, b, dev, s);
+    return rows_by_weights<kEpiPlain, true>(P, Problem{{hm, hm}, {wd, wd}, g->y, g->ld_y, g->rows, g->outputs, g->hidden, 1, wide(g->y, g->ld_y)}, dev, s);
 }
 
 int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, int* status, cudaStream_t s) {
     Matrix x{g->x, g->rows, g->inputs, g->ld_x}, wg{g->w_gate, g->inputs, g->hidden, g->ld_gate},
         wu{g->w_up, g->inputs, g->hidden, g->ld_up}, wd{g->w_down, g->hidden, g->outputs, g->ld_down},
         dy{g->dy, g->rows, g->outputs, g->ld_dy};
-    for (Matrix* m : {&x, &wg, &wu, &wd, &dy}) {
-        const int rc = align_matrix(m, space, run, s);
-        if (rc != BMGD_OK) return rc;
-    }
-    const int64_t ldh = up8(g->hidden);
-    const Matrix h{g->saved_hidden, g->rows, g->hidden, g->ld_saved}, dg{space->take(g->rows * ldh * 2), g->rows, g->hidden, ldh},
-        du{space->take(g->rows * ldh * 2), g->rows, g->hidden, ldh};
+    Matrix* const operands[5] = {&x, &wg, &wu, &wd, &dy};
+    int rc = align_matrices(operands, 5, space, run, s);
+    if (rc != BMGD_OK) return rc;
+    const int64_t ldh = up8(g->hidden), n = g->rows;
+    const Matrix h{g->saved_hidden, n, g->hidden, g->ld_saved}, dg{space->take(n * ldh * 2), n, g->hidden, ldh}, du{space->take(n * ldh * 2), n, g->hidden, ldh};
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = 2000000000ull;
-    int rc;
-    {   // dH, and from it dG and dU
-        P.M = g->rows; P.N = g->hidden; P.K = g->outputs;
-        P.segments = P.problems = 1;
-        P.out[0] = const_cast<void*>(dg.base); P.out[1] = const_cast<void*>(du.base); P.ld_out = ldh;
-        P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
-        const Matrix a[2] = {dy, dy}, b[2] = {wd, wd};
-        rc = contract<kEpiBackward, false, false>(P, a, b, dev, s);
-        if (rc != BMGD_OK) return rc;
-    }
-    {   // dX
-        P.N = g->inputs; P.K = g->hidden; P.segments = 2;
-        P.out[0] = g->dx; P.ld_out = g->inputs;
-        P.vec = wide(g->dx, g->inputs);
-        const Matrix a[2] = {dg, du}, b[2] = {wg, wu};
-        rc = contract<kEpiPlain, false, false>(P, a, b, dev, s);
-        if (rc != BMGD_OK) return rc;
-    }
-    {   // dWg and dWu
-        P.M = g->inputs; P.N = g->hidden; P.K = (int)g->rows; P.segments = 1; P.problems = 2;
-        P.out[0] = g->dw_gate; P.out[1] = g->dw_up; P.ld_out = g->hidden;
-        P.vec = wide(g->dw_gate, g->hidden) && wide(g->dw_up, g->hidden);
-        const Matrix a[2] = {x, x}, b[2] = {dg, du};
-        rc = contract<kEpiPlain, true, true>(P, a, b, dev, s);
-        if (rc != BMGD_OK) return rc;
-    }
-    P.M = g->hidden; P.N = g->outputs; P.problems = 1;
-    P.out[0] = g->dw_down; P.ld_out = g->outputs;
-    P.vec = wide(g->dw_down, g->outputs);
-    const Matrix a[2] = {h, h}, b[2] = {dy, dy};
-    return contract<kEpiPlain, true, true>(P, a, b, dev, s);
+    P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = kTimeoutNs;
+    P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
+    P.out_up = const_cast<void*>(du.base);
+    // dH, and from it dG and dU
+    rc = rows_by_weights<kEpiBackward, false>(P, Problem{{dy, dy}, {wd, wd}, const_cast<void*>(dg.base), ldh, n, g->hidden, g->outputs, 1, true}, dev, s);
+    if (rc != BMGD_OK) return rc;
+    rc = rows_by_weights<kEpiPlain, false>(P, Problem{{dg, du}, {wg, wu}, g->dx, g->inputs, n, g->inputs, g->hidden, 2, wide(g->dx, g->inputs)}, dev, s);
+    if (rc != BMGD_OK) return rc;
+    const Problem weights[3] = {
+        {{x, x}, {dg, dg}, g->dw_gate, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_gate, g->hidden)},
+        {{x, x}, {du, du}, g->dw_up, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_up, g->hidden)},
+        {{h, h}, {dy, dy}, g->dw_down, g->outputs, g->hidden, g->outputs, (int)n, 1, wide(g->dw_down, g->outputs)}};
+    return contract<kEpiPlain, true, true>(P, weights, 3, dev, s);
 }
 
 int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspace_bytes, void* stream) {

@@ -55,6 +55,11 @@ def _place(device: torch.device, stream: Optional[torch.cuda.Stream]):
     return _other(device, stream)
 
 
+def _current(device: torch.device) -> int:
+    """The current stream of the device, as the library takes it (without the object that torch.cuda makes of it)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int], dtype: torch.dtype, device: torch.device) -> int:
     """Refuse a tensor that is not a [rows, cols] matrix with contiguous rows; returns its row stride."""
     if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
@@ -148,7 +153,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
         if g.rows > 0:
             g.y, g.ld_y = y.data_ptr(), g.outputs
             w, size = _workspace(L, g, _FORWARD, x.device)
-            _status(L.bmgd_gated_ffn_forward(ctypes.byref(g), w.data_ptr(), size, torch.cuda.current_stream().cuda_stream),
+            _status(L.bmgd_gated_ffn_forward(ctypes.byref(g), w.data_ptr(), size, _current(x.device)),
                     "bmgd_gated_ffn_forward")
     return (y, saved) if save else y
 
@@ -175,7 +180,7 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
         g.dy = dy.data_ptr()
         _saved_args(g, *saved)
         w, size = _workspace(L, g, _BACKWARD, x.device)
-        _status(L.bmgd_gated_ffn_backward(ctypes.byref(g), w.data_ptr(), size, torch.cuda.current_stream().cuda_stream),
+        _status(L.bmgd_gated_ffn_backward(ctypes.byref(g), w.data_ptr(), size, _current(x.device)),
                 "bmgd_gated_ffn_backward")
     return dx, dw_gate, dw_up, dw_down
 
@@ -209,7 +214,7 @@ def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[floa
         if rows > 0:
             _status(L.bmgd_softmax_residual(logits.data_ptr(), ld, y.data_ptr(), rows, C, _TYPES[logits.dtype],
                                             1.0 / rows if scale is None else float(scale), residual.data_ptr(), C,
-                                            loss.data_ptr(), torch.cuda.current_stream().cuda_stream), "bmgd_softmax_residual")
+                                            loss.data_ptr(), _current(device)), "bmgd_softmax_residual")
     return residual, loss
 
 
@@ -232,7 +237,7 @@ def gather_batch(x: torch.Tensor, y: Optional[torch.Tensor], seed: int, chain: i
         _status(L.bmgd_gather_batch(x.data_ptr(), x.shape[1] * x.element_size(), y.data_ptr() if y is not None else None, rows,
                                     int(seed) & 0xFFFFFFFFFFFFFFFF, int(chain) & 0xFFFFFFFF, int(round) & 0xFFFFFFFF, first, count,
                                     bx.data_ptr(), by.data_ptr() if by is not None else None,
-                                    torch.cuda.current_stream().cuda_stream), "bmgd_gather_batch")
+                                    _current(device)), "bmgd_gather_batch")
     return bx, by
 
 
@@ -341,7 +346,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
             scratch = torch.empty(size, dtype=torch.uint8, device=device)
         _status(L.bmgd_adamw_step(table.buffer_info()[0], count, ctypes.byref(cfg), control.data_ptr(),
                                   scratch.data_ptr() if scratch is not None else None, size,
-                                  torch.cuda.current_stream().cuda_stream), "bmgd_adamw_step")
+                                  _current(device)), "bmgd_adamw_step")
 
 
 def decode_moments(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
