@@ -28,9 +28,7 @@ namespace bmgdk {
 enum { kActSilu = 0, kActGelu = 1, kActRelu = 2, kActSigmoid = 3 };
 enum { kEpiGated = 0, kEpiPlain = 1, kEpiBackward = 2 };
 
-constexpr int kFfnThreads = 256;
 constexpr int kFfnBK = 64;
-constexpr int kTurnPitch = 36;  // words per row of the turning buffer: 32 and four, so that eight lanes' 16-byte accesses meet no bank twice
 constexpr int kFfnGroup = 8;  // tiles along M that are worked on together: their rows of A stay in L2 while B passes
 constexpr int kFfnProblems = 3;
 
@@ -43,7 +41,7 @@ struct FfnProblem {
     int M, N, K;
     int segments;
     int tiles_m, tiles_n;
-    int a_mn;                // few rows: the weights are read across their rows
+    int a_mn, b_mn;          // few rows: an operand is read across its rows
     int vec;                 // rows of D start on 16-byte boundaries
 };
 
@@ -176,7 +174,19 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 // ---------------------------------------------------------------- shapes
-template <int CG, int BN>
+// Read-out: four warps, or eight where a tile's arithmetic can be short (the contraction over few rows of the weights'
+// gradients) or its read-out long (the backward form reads two factors per value).  Each turns its values through a buffer of
+// its own in shared memory: 32 rows of kWords words, kPitch apart so that eight lanes' 16-byte accesses meet no bank twice.
+template <int EPI>
+struct FfnReadOut {
+    static constexpr int kWarps = EPI == kEpiGated ? 4 : 8;
+    static constexpr int kWords = EPI == kEpiGated ? 32 : 16;   // plain: 32 values of 16 bits
+    static constexpr int kPitch = kWords + 4;
+    static constexpr int kCols = EPI == kEpiBackward ? 16 : EPI == kEpiPlain ? 32 : 16;  // columns of the tile taken at a time
+    static constexpr int kBytes = kWarps * 32 * kPitch * 4;
+    static constexpr int kThreads = 128 + kWarps * 32;
+};
+template <int CG, int BN, int EPI>
 struct FfnShape {
     static constexpr int kA = 128 * kFfnBK * 2;            // bytes of A per stage and CTA
     static constexpr int kB = BN / CG * kFfnBK * 2;        // bytes of B per stage and CTA
@@ -184,7 +194,7 @@ struct FfnShape {
     static constexpr int kStages = kStage > 40960 ? 4 : 6;
     static constexpr int kBars = kStages * kStage;         // mbarriers and the tensor-memory address behind the ring
     static constexpr int kTurn = kBars + 256;              // where a warp turns rows per lane into pieces of rows per lane
-    static constexpr int kSmem = kTurn + 4 * 32 * kTurnPitch * 4 + 1024;  // (1024: the ring starts on a 1024-byte boundary)
+    static constexpr int kSmem = kTurn + FfnReadOut<EPI>::kBytes + 1024;  // (1024: the ring starts on a 1024-byte boundary)
 };
 
 // fetch `rows` rows (K-major) or columns (MN-major) of an operand, from `mn` on, 64 along the contraction from `k` on
@@ -223,8 +233,9 @@ __device__ __forceinline__ uint32_t ffn_idesc(int type, bool a_mn, bool b_mn, in
 // read across its rows.  They are known when the kernel is compiled because one thread fetches and one thread issues for the whole
 // tile: choosing at run time cost 5 % of the forward pass at 4096 rows and 13 % of the backward pass.
 template <int CG, int BN, int EPI, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_constant__ FfnParams P) {
-    using S = FfnShape<CG, BN>;
+__global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const __grid_constant__ FfnParams P) {
+    using S = FfnShape<CG, BN, EPI>;
+    using R = FfnReadOut<EPI>;
     extern __shared__ unsigned char ffn_smem[];
     const uint32_t ring = (smem_u32(ffn_smem) + 1023u) & ~1023u;
     const uint32_t full = ring + S::kBars, empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
@@ -235,10 +246,9 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;   // columns of the output that a tile covers
     constexpr uint32_t kTmemCols = 2 * BN;
 
-    let_next_kernel_start();
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, 4 * CG); }
+        for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, R::kWarps * CG); }
         fence_barrier_init();
     }
     if (warp == 2) ffn_tmem_alloc<CG>(slot, kTmemCols);
@@ -249,6 +259,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
     wait_for_previous_kernel();
+    let_next_kernel_start();
 
     const long long tiles = P.tiles;
     auto place = [&](long long t, int& which, int& m0, int& n0) {
@@ -328,11 +339,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
         }
     } else if (warp >= 4) {
         // A lane reads a row out of tensor memory; what a warp writes to (or reads from) global memory at a time should be
-        // pieces of rows.  In between the values take turns through shared memory, 32 to a row.
+        // pieces of rows: in between the values go through shared memory.
         int acc = 0;
         uint32_t acc_phase = 0;
-        const int quarter = warp & 3;
-        float* const turn = reinterpret_cast<float*>(ffn_smem + (ring - smem_u32(ffn_smem)) + S::kTurn) + quarter * 32 * kTurnPitch;
+        const int quarter = warp & 3, part = (warp - 4) >> 2;  // with eight warps two share a quarter of the rows: one takes the even pieces
+        float* const turn = reinterpret_cast<float*>(ffn_smem + (ring - smem_u32(ffn_smem)) + S::kTurn) + (warp - 4) * 32 * R::kPitch;
         for (long long t = pair; t < tiles; t += pairs) {
             int which, m0, n0;
             place(t, which, m0, n0);
@@ -360,14 +371,14 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
                     tmem_wait();
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<uint4*>(turn + lane * kTurnPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                        *reinterpret_cast<uint4*>(turn + lane * R::kPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                     __syncwarp();
 #pragma unroll
                     for (int it = 0; it < 4; ++it) {
                         const int i = it * 8 + (lane >> 2);
                         if (i < rows && col + sub < N) {  // (rows of H, act(G) and U act'(G) are padded to multiples of 8)
-                            const float4 g = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + sub);
-                            const float4 u = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + 16 + sub);
+                            const float4 g = *reinterpret_cast<const float4*>(turn + i * R::kPitch + sub);
+                            const float4 u = *reinterpret_cast<const float4*>(turn + i * R::kPitch + 16 + sub);
                             float4 v, s;
                             if (P.value) {
                                 act_both(P.act, g.x, v.x, s.x); act_both(P.act, g.y, v.y, s.y);
@@ -385,33 +396,33 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
                     __syncwarp();
                 }
             } else if constexpr (EPI == kEpiBackward) {
-                const int sub = (lane & 7) * 4;
+                const int sub = (lane & 3) * 4;
 #pragma unroll 1
-                for (int c = 0; c < kCols; c += 32) {
+                for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols) {
                     const int col = n0 + c;
                     if (col >= N) break;
-                    float4 v[8], s[8];
+                    float4 v[4], s[4];
 #pragma unroll
-                    for (int it = 0; it < 8; ++it) {
-                        const int i = it * 4 + (lane >> 3);
+                    for (int it = 0; it < 4; ++it) {
+                        const int i = it * 8 + (lane >> 2);
                         const long long at = (row0 + i) * P.ld_save + col + sub;
                         if (i < rows && col + sub < N) {
                             v[it] = __ldcs(reinterpret_cast<const float4*>(P.value + at));
                             s[it] = __ldcs(reinterpret_cast<const float4*>(P.slope + at));
                         }
                     }
-                    uint32_t r[32];
-                    tmem_load32(ta + (uint32_t)c, r);
+                    uint32_t r[16];
+                    tmem_load16(ta + (uint32_t)c, r);
                     tmem_wait();
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<uint4*>(turn + lane * kTurnPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint4*>(turn + lane * R::kPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                     __syncwarp();
 #pragma unroll
-                    for (int it = 0; it < 8; ++it) {
-                        const int i = it * 4 + (lane >> 3);
+                    for (int it = 0; it < 4; ++it) {
+                        const int i = it * 8 + (lane >> 2);
                         if (i < rows && col + sub < N) {
-                            const float4 d = *reinterpret_cast<const float4*>(turn + i * kTurnPitch + sub);
+                            const float4 d = *reinterpret_cast<const float4*>(turn + i * R::kPitch + sub);
                             const long long at = (row0 + i) * ld_out + col + sub;
                             *reinterpret_cast<uint2*>(out + at) =
                                 make_uint2(pack2(P.type, d.x * s[it].x, d.y * s[it].y), pack2(P.type, d.z * s[it].z, d.w * s[it].w));
@@ -422,9 +433,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
                     __syncwarp();
                 }
             } else {
-                uint16_t* const half = reinterpret_cast<uint16_t*>(turn);  // 32 16-bit values to a row here, 40 apart
+                uint16_t* const half = reinterpret_cast<uint16_t*>(turn);
+                constexpr int kHalf = R::kPitch * 2;  // 16-bit values from row to row
+                const bool vec = q.vec != 0;
 #pragma unroll 1
-                for (int c = 0; c < kCols; c += 32) {
+                for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols) {
                     const int col = n0 + c;
                     if (col >= N) break;
                     uint32_t r[32];
@@ -432,22 +445,22 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
                     tmem_wait();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        uint32_t q[4];
+                        uint32_t p[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) q[j] = pack2(P.type, __uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
-                        *reinterpret_cast<uint4*>(half + lane * 40 + 8 * i) = make_uint4(q[0], q[1], q[2], q[3]);
+                        for (int j = 0; j < 4; ++j) p[j] = pack2(P.type, __uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
+                        *reinterpret_cast<uint4*>(half + lane * kHalf + 8 * i) = make_uint4(p[0], p[1], p[2], p[3]);
                     }
                     __syncwarp();
-                    if (q.vec && col + 32 <= N) {
+                    if (vec && col + 32 <= N) {
 #pragma unroll
                         for (int it = 0; it < 4; ++it) {
                             const int i = it * 8 + (lane >> 2), sub = (lane & 3) * 8;
                             if (i < rows)
-                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + sub) = *reinterpret_cast<const uint4*>(half + i * 40 + sub);
+                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + sub) = *reinterpret_cast<const uint4*>(half + i * kHalf + sub);
                         }
                     } else if (col + lane < N) {
 #pragma unroll 8
-                        for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + lane] = half[i * 40 + lane];
+                        for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + lane] = half[i * kHalf + lane];
                     }
                     __syncwarp();
                 }
@@ -474,11 +487,13 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     if (warp == 2) ffn_tmem_free<CG>(tmem, kTmemCols);
 }
 
-// ---------------------------------------------------------------- few rows
-// The same contractions for up to a few hundred rows, with the roles exchanged: 128 features (columns of the weights) are
-// the rows of a tile, and the NR rows of X its columns, so that the tensor core wastes nothing on missing rows and a stage
-// of the ring is nearly all weights.  The contraction is split over the S CTAs of a cluster, as many as give
-// each SM something to read; their partial sums are added through distributed shared memory in the order of the CTAs.
+// ---------------------------------------------------------------- few rows, and everything small
+// The same contractions where the tiles of the form above would leave SMs without work, with the roles exchanged: 128
+// features (columns of the weights) are the rows of a tile, and NR rows of X its columns, so that the tensor core wastes nothing
+// on missing rows and a stage of the ring is nearly all weights.  The contraction is split over the S CTAs of a cluster, as many
+// as give each SM something to read; their partial sums are added through distributed shared memory in the order of
+// the CTAs.  What bounds it: reading the weights (4 MB and more), or the latency of one pass through copy, product and sum.
+constexpr int kFewThreads = 256;
 constexpr int kFewPart = 128;  // features of a tile
 
 template <int NR, int EPI>
@@ -486,12 +501,13 @@ struct FewShape {
     static constexpr int kTiles = EPI == kEpiGated ? 2 : 1;       // tiles of weights per stage: Wg and Wu
     static constexpr int kA = 128 * kFfnBK * 2;
     static constexpr int kStage = kTiles * kA + NR * kFfnBK * 2;
-    static constexpr int kCtasPerSm = NR <= 64 ? 2 : 1;
-    static constexpr int kRoom = kCtasPerSm == 2 ? 110 * 1024 : 214 * 1024;
-    static constexpr int kStages = kRoom / kStage > 10 ? 10 : kRoom / kStage;
+    static constexpr int kCtasPerSm = 2;                          // one's arithmetic and read-out overlap the other's copies
+    static constexpr int kStages = 110 * 1024 / kStage > 10 ? 10 : 110 * 1024 / kStage;
     static constexpr int kRing = kStages * kStage;
-    static constexpr int kParts = kTiles * NR * kFewPart * 4;      // partial sums, in the ring's place once it is done with
-    static constexpr int kBars = kRing > kParts ? kRing : kParts;
+    static constexpr int kPassRows = NR < 64 ? NR : 64;            // rows whose partial sums are exchanged at a time
+    static constexpr int kParts = kTiles * kPassRows * kFewPart * 4;  // they take the ring's place once it is done with
+    static_assert(kParts <= kRing, "partial sums");
+    static constexpr int kBars = kRing;
     static constexpr int kSmem = kBars + 256 + 1024;
     static constexpr uint32_t kTmemCols = kTiles * NR < 32 ? 32 : kTiles * NR;
 };
@@ -512,18 +528,23 @@ __device__ __forceinline__ void store4_any(uint16_t* p, int type, bool vec, int 
     if (left > 3) p[3] = (uint16_t)(hi >> 16);
 }
 
-// grid: x = S CTAs (one cluster) per tile of 128 features, y = tiles of NR rows.  p[0].a: the weights, p[0].b: the rows.
+// Grid: S CTAs (one cluster) per tile.  a: the weights, b: the rows; first_tile, tiles_m and tiles_n count tiles of NR rows and
+// 128 features.  early: the kernel before this one is ours and started after everything before it had finished, so the
+// weights, which it does not write, may be fetched while it still runs.
 template <int NR, int EPI>
-__global__ void __launch_bounds__(kFfnThreads) ffn_few_kernel(const __grid_constant__ FfnParams P, const int S) {
+__global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ffn_few_kernel(const __grid_constant__ FfnParams P, const int S, const int early) {
     using F = FewShape<NR, EPI>;
     extern __shared__ unsigned char ffn_smem[];
     const uint32_t ring = (smem_u32(ffn_smem) + 1023u) & ~1023u;
     const uint32_t full = ring + F::kBars, empty = full + 8 * F::kStages, done = empty + 8 * F::kStages, slot = done + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const FfnProblem& q = P.p[0];
-    const int part = (int)blockIdx.x % S, f0 = ((int)blockIdx.x / S) * kFewPart, r0 = (int)blockIdx.y * NR;
+    const int part = (int)blockIdx.x % S, tile = (int)blockIdx.x / S;
+    int which = 0;
+    while (which + 1 < P.problems && P.p[which + 1].first_tile <= tile) ++which;
+    const FfnProblem& q = P.p[which];
+    const int in_problem = tile - (int)q.first_tile;
+    const int f0 = in_problem / q.tiles_m * kFewPart, r0 = in_problem % q.tiles_m * NR;
 
-    let_next_kernel_start();
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done, 1);
@@ -535,36 +556,46 @@ __global__ void __launch_bounds__(kFfnThreads) ffn_few_kernel(const __grid_const
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
-    wait_for_previous_kernel();
+    if (!early) wait_for_previous_kernel();
 
     const int kblocks = (q.K + kFfnBK - 1) / kFfnBK, steps = kblocks * q.segments;
     const int first = (int)((long long)steps * part / S), last = (int)((long long)steps * (part + 1) / S);
     FfnWait w{P.status, P.timeout_ns, false};
     if (warp == 0) {
         if (lane == 0) {
-            int s = 0;
-            uint32_t phase = 0;
-            for (int k = first; k < last; ++k) {
-                ffn_wait(empty + 8 * s, phase ^ 1u, w);
-                if (w.aborted) break;
+            const bool a_mn = q.a_mn, b_mn = q.b_mn;
+            auto weights = [&](int k, int s) {
                 const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
                 const uint32_t bar = full + 8 * s, sa = ring + s * F::kStage;
                 mbar_arrive_expect_tx(bar, F::kStage);
-                if constexpr (EPI == kEpiGated) {
-                    ffn_fetch<1>(sa, &q.a[0], q.a_mn, 128, f0, k0, bar);
-                    ffn_fetch<1>(sa + F::kA, &q.a[1], q.a_mn, 128, f0, k0, bar);
-                } else {
-                    ffn_fetch<1>(sa, &q.a[seg], q.a_mn, 128, f0, k0, bar);
+                ffn_fetch<1>(sa, &q.a[seg], a_mn, 128, f0, k0, bar);
+                if constexpr (EPI == kEpiGated) ffn_fetch<1>(sa + F::kA, &q.a[1], a_mn, 128, f0, k0, bar);
+            };
+            auto rows = [&](int k, int s) {
+                const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
+                ffn_fetch<1>(ring + s * F::kStage + F::kTiles * F::kA, &q.b[seg], b_mn, NR, r0, k0, full + 8 * s);
+            };
+            int ahead = 0;
+            if (early) {
+                for (; ahead < F::kStages && first + ahead < last; ++ahead) weights(first + ahead, ahead);
+                wait_for_previous_kernel();
+            }
+            int s = 0;
+            uint32_t phase = 0;
+            for (int k = first; k < last; ++k) {
+                if (k - first >= ahead) {
+                    ffn_wait(empty + 8 * s, phase ^ 1u, w);
+                    if (w.aborted) break;
+                    weights(k, s);
                 }
-                ffn_fetch<1>(sa + F::kTiles * F::kA, &q.b[EPI == kEpiGated ? 0 : seg], false, NR, r0, k0, bar);
+                rows(k, s);
                 if (++s == F::kStages) { s = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            const bool a_mn = q.a_mn;
-            const uint32_t idesc = ffn_idesc(P.type, a_mn, false, 128, NR);
-            const FfnDesc ad(a_mn), bd(false);
+            const uint32_t idesc = ffn_idesc(P.type, q.a_mn, q.b_mn, 128, NR);
+            const FfnDesc ad(q.a_mn), bd(q.b_mn);
             int s = 0;
             uint32_t phase = 0;
             for (int k = first; k < last; ++k) {
@@ -585,58 +616,70 @@ __global__ void __launch_bounds__(kFfnThreads) ffn_few_kernel(const __grid_const
         }
     }
     __syncwarp();
-    // every thread waits for the last product: after it the ring's memory is free for the partial sums [NR][128 features]
+    // after the last product the ring's memory is free for the partial sums [row][128 features]
     ffn_wait(done, 0, w);
     tc_fence_after();
-    if (warp >= 4) {
-        const uint32_t ta = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    if (early) wait_for_previous_kernel();
+    let_next_kernel_start();
+    const bool given_up = __syncthreads_or(w.aborted ? 1 : 0) != 0;
+
+    const int f = f0 + lane * 4, left = q.N - f;
+    uint16_t* const out = static_cast<uint16_t*>(q.out);
+    const int rows = min(NR, q.M - r0);
+    const uint32_t ta = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+#pragma unroll 1
+    for (int base = 0; base < rows; base += F::kPassRows) {
+        if (base > 0) {  // the sums of the pass before have been read
+            __syncthreads();
+            if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
+        }
+        // two warps share a quarter of the features: they take turns at 16 rows
         const uint32_t to = ring + (uint32_t)(((warp & 3) * 32 + lane) * 4);
 #pragma unroll 1
-        for (int c = 0; c < F::kTiles * NR; c += 16) {
+        for (int c = (warp >> 2) * 16; c < F::kTiles * F::kPassRows; c += 32) {
+            const int h = c / F::kPassRows, col = c - h * F::kPassRows;
+            if (base + col >= rows) continue;
             uint32_t r[16];
-            tmem_load16(ta + (uint32_t)c, r);
+            tmem_load16(ta + (uint32_t)(h * NR + base + col), r);
             tmem_wait();
 #pragma unroll
             for (int i = 0; i < 16; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)((c + i) * kFewPart * 4)), "r"(r[i]) : "memory");
         }
-    }
-    tc_fence_before();
-    __syncthreads();
-    if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
-    // each CTA finishes its share of the rows: a warp a row at a time, four features per lane
-    const int f = f0 + lane * 4, left = q.N - f;
-    uint16_t* const out = static_cast<uint16_t*>(q.out);
-    const int rows = min(NR, q.M - r0);
-    const bool given_up = __syncthreads_or(w.aborted ? 1 : 0) != 0;
-    for (int i = part * (kFfnThreads / 32) + warp; i < rows && !given_up; i += S * (kFfnThreads / 32)) {
-        const uint32_t at = ring + (uint32_t)((i * kFewPart + lane * 4) * 4);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), u = x;
-        for (int c = 0; c < S; ++c) {
-            const float4 y = ld_cluster4(at, c);
-            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        tc_fence_before();
+        __syncthreads();
+        if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
+        // each CTA finishes its share of the rows: a warp a row at a time, four features per lane
+        const int some = min(F::kPassRows, rows - base);
+        for (int i = part * (kFewThreads / 32) + warp; i < some && !given_up; i += S * (kFewThreads / 32)) {
+            const uint32_t at = ring + (uint32_t)((i * kFewPart + lane * 4) * 4);
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f), u = x;
+            for (int c = 0; c < S; ++c) {
+                const float4 y = ld_cluster4(at, c);
+                x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                if constexpr (EPI == kEpiGated) {
+                    const float4 z = ld_cluster4(at + F::kPassRows * kFewPart * 4, c);
+                    u.x += z.x; u.y += z.y; u.z += z.z; u.w += z.w;
+                }
+            }
+            if (left <= 0) continue;
+            const long long row = r0 + base + i;
             if constexpr (EPI == kEpiGated) {
-                const float4 z = ld_cluster4(at + NR * kFewPart * 4, c);
-                u.x += z.x; u.y += z.y; u.z += z.z; u.w += z.w;
+                float4 v, s;
+                act_both(P.act, x.x, v.x, s.x); act_both(P.act, x.y, v.y, s.y);
+                act_both(P.act, x.z, v.z, s.z); act_both(P.act, x.w, v.w, s.w);
+                if (P.value) {
+                    *reinterpret_cast<float4*>(P.value + row * P.ld_save + f) = v;
+                    *reinterpret_cast<float4*>(P.slope + row * P.ld_save + f) = make_float4(u.x * s.x, u.y * s.y, u.z * s.z, u.w * s.w);
+                }
+                store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(v.x * u.x, v.y * u.y, v.z * u.z, v.w * u.w));
+            } else if constexpr (EPI == kEpiBackward) {
+                const float4 v = *reinterpret_cast<const float4*>(P.value + row * P.ld_save + f);
+                const float4 s = *reinterpret_cast<const float4*>(P.slope + row * P.ld_save + f);
+                store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * s.x, x.y * s.y, x.z * s.z, x.w * s.w));
+                store4_any(static_cast<uint16_t*>(P.out_up) + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * v.x, x.y * v.y, x.z * v.z, x.w * v.w));
+            } else {
+                store4_any(out + row * q.ld_out + f, P.type, q.vec, left, x);
             }
-        }
-        if (left <= 0) continue;
-        const long long row = r0 + i;
-        if constexpr (EPI == kEpiGated) {
-            float4 v, s;
-            act_both(P.act, x.x, v.x, s.x); act_both(P.act, x.y, v.y, s.y);
-            act_both(P.act, x.z, v.z, s.z); act_both(P.act, x.w, v.w, s.w);
-            if (P.value) {
-                *reinterpret_cast<float4*>(P.value + row * P.ld_save + f) = v;
-                *reinterpret_cast<float4*>(P.slope + row * P.ld_save + f) = make_float4(u.x * s.x, u.y * s.y, u.z * s.z, u.w * s.w);
-            }
-            store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(v.x * u.x, v.y * u.y, v.z * u.z, v.w * u.w));
-        } else if constexpr (EPI == kEpiBackward) {
-            const float4 v = *reinterpret_cast<const float4*>(P.value + row * P.ld_save + f);
-            const float4 s = *reinterpret_cast<const float4*>(P.slope + row * P.ld_save + f);
-            store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * s.x, x.y * s.y, x.z * s.z, x.w * s.w));
-            store4_any(static_cast<uint16_t*>(P.out_up) + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * v.x, x.y * v.y, x.z * v.z, x.w * v.w));
-        } else {
-            store4_any(out + row * q.ld_out + f, P.type, q.vec, left, x);
         }
     }
     if (given_up) {  // copies and products may still be in flight
@@ -661,8 +704,8 @@ struct AlignParams {
     AlignJob job[5];
 };
 __global__ void __launch_bounds__(256) ffn_align_kernel(const __grid_constant__ AlignParams P) {
-    let_next_kernel_start();
     wait_for_previous_kernel();
+    let_next_kernel_start();
     const AlignJob& j = P.job[blockIdx.y];
     const unsigned per = (unsigned)j.ld_out / 8;
     const long long total = j.rows * per;

@@ -78,9 +78,9 @@ struct Problem {
     bool vec;
 };
 
-int launch_config(cudaLaunchConfig_t* lc, cudaLaunchAttribute (&at)[2], dim3 grid, int smem, int cluster, cudaStream_t s) {
+void launch_config(cudaLaunchConfig_t* lc, cudaLaunchAttribute (&at)[2], dim3 grid, int threads, int smem, int cluster, cudaStream_t s) {
     lc->gridDim = grid;
-    lc->blockDim = dim3(kFfnThreads);
+    lc->blockDim = dim3((unsigned)threads);
     lc->dynamicSmemBytes = smem;
     lc->stream = s;
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -89,12 +89,11 @@ int launch_config(cudaLaunchConfig_t* lc, cudaLaunchAttribute (&at)[2], dim3 gri
     at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     lc->attrs = at;
     lc->numAttrs = cluster > 1 ? 2 : 1;
-    return BMGD_OK;
 }
 
 template <int CG, int BN, int EPI, bool A_MN, bool B_MN>
 int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
-    using S = FfnShape<CG, BN>;
+    using S = FfnShape<CG, BN, EPI>;
     constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;
     int64_t tiles = 0;
     for (int k = 0; k < count; ++k) {
@@ -121,59 +120,76 @@ int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, 
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
-    launch_config(&lc, at, dim3((unsigned)std::min<int64_t>(tiles, dev.sms / CG) * CG), S::kSmem, CG, s);
+    launch_config(&lc, at, dim3((unsigned)std::min<int64_t>(tiles, dev.sms / CG) * CG), FfnReadOut<EPI>::kThreads, S::kSmem, CG, s);
     if (cudaLaunchKernelEx(&lc, fn, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
 
-// Many rows.  Tiles of 256 rows x 256 columns for two CTAs wherever they fill half the GPU; otherwise tiles of 128 x 128.
-template <int EPI, bool A_MN, bool B_MN>
-int contract(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
-    constexpr int kCols = EPI == kEpiGated ? 128 : 256;
-    int64_t large = 0;
-    for (int k = 0; k < count; ++k) large += ((problems[k].M + 255) / 256) * ((problems[k].N + kCols - 1) / kCols);
-    if (large * 4 >= dev.sms) return launch<2, 256, EPI, A_MN, B_MN>(P, problems, count, dev, s);
-    return launch<1, 128, EPI, A_MN, B_MN>(P, problems, count, dev, s);
-}
-
-template <int NR, int EPI, bool W_MN>
-int launch_few(FfnParams& P, const Problem& x, const Device& dev, cudaStream_t s) {
+template <int NR, int EPI, bool ROWS_MN, bool W_MN>
+int launch_few(FfnParams& P, const Problem* problems, int count, bool early, const Device& dev, cudaStream_t s) {
     using F = FewShape<NR, EPI>;
-    FfnProblem& q = P.p[0];
-    // exchanged roles: the weights are the kernel's a, read across the rows where the other form's b is
-    for (int i = 0; i < 2; ++i) {
-        int rc = BMGD_OK;
-        if (i < x.segments || EPI == kEpiGated) rc = make_map(x.b[i], P.type, W_MN ? 64 : 128, &q.a[i]);
-        if (rc == BMGD_OK && i < x.segments) rc = make_map(x.a[i], P.type, NR, &q.b[i]);
-        if (rc != BMGD_OK) return rc;
+    int64_t tiles = 0;
+    int least = 0x7FFFFFFF;
+    for (int k = 0; k < count; ++k) {
+        const Problem& x = problems[k];
+        FfnProblem& q = P.p[k];
+        // exchanged roles: the weights are the kernel's a
+        for (int i = 0; i < 2; ++i) {
+            int rc = BMGD_OK;
+            if (i < x.segments || EPI == kEpiGated) rc = make_map(x.b[i], P.type, W_MN ? 64 : 128, &q.a[i]);
+            if (rc == BMGD_OK && i < x.segments) rc = make_map(x.a[i], P.type, ROWS_MN ? 64 : NR, &q.b[i]);
+            if (rc != BMGD_OK) return rc;
+        }
+        q.out = x.out; q.ld_out = x.ld_out;
+        q.M = (int)x.M; q.N = x.N; q.K = x.K; q.segments = x.segments;
+        q.a_mn = W_MN; q.b_mn = ROWS_MN; q.vec = x.vec;
+        q.tiles_m = (int)((x.M + NR - 1) / NR);
+        q.tiles_n = (x.N + kFewPart - 1) / kFewPart;
+        q.first_tile = tiles;
+        tiles += (int64_t)q.tiles_m * q.tiles_n;
+        least = std::min(least, x.segments * ((x.K + kFfnBK - 1) / kFfnBK));
     }
-    q.out = x.out; q.ld_out = x.ld_out;
-    q.M = (int)x.M; q.N = x.N; q.K = x.K; q.segments = x.segments;
-    q.a_mn = W_MN; q.vec = x.vec;
-    P.problems = 1;
-    const int tiles = (x.N + kFewPart - 1) / kFewPart, row_tiles = (int)((x.M + NR - 1) / NR);
-    const int steps = x.segments * ((x.K + kFfnBK - 1) / kFfnBK);
-    const int room = dev.sms * F::kCtasPerSm / std::max(1, tiles * row_tiles);
-    const int split = std::max(1, std::min(std::min(8, room), steps / 2));
+    P.problems = count;
+    P.tiles = tiles;
+    const int64_t room = (int64_t)dev.sms * F::kCtasPerSm / tiles;
+    const int split = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, room), least / 2));
     if (F::kSmem > dev.smem) return BMGD_ERR_LAUNCH;
     auto* fn = ffn_few_kernel<NR, EPI>;
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
-    launch_config(&lc, at, dim3((unsigned)(tiles * split), (unsigned)row_tiles), F::kSmem, split, s);
-    if (cudaLaunchKernelEx(&lc, fn, P, split) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    launch_config(&lc, at, dim3((unsigned)(tiles * split)), kFewThreads, F::kSmem, split, s);
+    if (cudaLaunchKernelEx(&lc, fn, P, split, early ? 1 : 0) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
 
-// Rows x weights (W_MN: the weights are read across their rows): up to 256 rows with exchanged roles (two tiles of 128 from 129 on).
+// Up to 256 rows, and wherever tiles of 128 x 128 do not fill the GPU once, the form with exchanged roles; otherwise tiles of
+// 256 rows x 256 columns for two CTAs, or of 128 x 128 where those would leave more than half of the GPU idle.  ROWS_MN, W_MN:
+// the first operand, or the second, is read across its rows.
 constexpr int64_t kFewRows = 256;
-template <int EPI, bool W_MN>
-int rows_by_weights(FfnParams& P, const Problem& x, const Device& dev, cudaStream_t s) {
-    if (x.M > kFewRows) return contract<EPI, false, W_MN>(P, &x, 1, dev, s);
-    if (x.M <= 16) return launch_few<16, EPI, W_MN>(P, x, dev, s);
-    if (x.M <= 32) return launch_few<32, EPI, W_MN>(P, x, dev, s);
-    if (x.M <= 64) return launch_few<64, EPI, W_MN>(P, x, dev, s);
-    return launch_few<128, EPI, W_MN>(P, x, dev, s);
+template <int EPI, bool ROWS_MN, bool W_MN>
+int contract(FfnParams& P, const Problem* problems, int count, bool early, const Device& dev, cudaStream_t s) {
+    constexpr int kCols = EPI == kEpiGated ? 128 : 256;
+    int64_t large = 0, small = 0, few = 0, rows = 0;
+    for (int k = 0; k < count; ++k) {
+        const Problem& x = problems[k];
+        large += ((x.M + 255) / 256) * ((x.N + kCols - 1) / kCols);
+        small += ((x.M + 127) / 128) * ((x.N + kCols / 2 - 1) / (kCols / 2));
+        few += ((x.M + 127) / 128) * ((x.N + kFewPart - 1) / kFewPart);
+        rows = std::max(rows, x.M);
+    }
+    if ((!ROWS_MN && rows <= kFewRows) || small <= dev.sms) {
+        if constexpr (!ROWS_MN) {
+            if (rows <= 16) return launch_few<16, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
+            if (rows <= 32) return launch_few<32, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
+        }
+        // (tiles of 64 rows where even those of a contraction too short to split leave room)
+        const int steps = problems[0].segments * ((problems[0].K + kFfnBK - 1) / kFfnBK);
+        if (rows <= 64 || (few * 2 <= dev.sms && steps < 8)) return launch_few<64, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
+        return launch_few<128, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
+    }
+    if (large * 4 >= dev.sms) return launch<2, 256, EPI, ROWS_MN, W_MN>(P, problems, count, dev, s);
+    return launch<1, 128, EPI, ROWS_MN, W_MN>(P, problems, count, dev, s);
 }
 
 int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -209,7 +225,7 @@ int align_matrices(Matrix* const* list, int count, Space* space, bool run, cudaS
     if (!run || jobs == 0) return BMGD_OK;
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
-    launch_config(&lc, at, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 148 * 8), (unsigned)jobs), 0, 1, s);
+    launch_config(&lc, at, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 148 * 8), (unsigned)jobs), 256, 0, 1, s);
     if (cudaLaunchKernelEx(&lc, ffn_align_kernel, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
@@ -254,10 +270,12 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     FfnParams P{};
     P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = kTimeoutNs;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
-    rc = rows_by_weights<kEpiGated, true>(P, Problem{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true}, dev, s);
+    const Problem gated{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true};
+    rc = contract<kEpiGated, false, true>(P, &gated, 1, false, dev, s);
     if (rc != BMGD_OK) return rc;
     const Matrix hm{h, g->rows, g->hidden, ldh};
-    return rows_by_weights<kEpiPlain, true>(P, Problem{{hm, hm}, {wd, wd}, g->y, g->ld_y, g->rows, g->outputs, g->hidden, 1, wide(g->y, g->ld_y)}, dev, s);
+    const Problem down{{hm, hm}, {wd, wd}, g->y, g->ld_y, g->rows, g->outputs, g->hidden, 1, wide(g->y, g->ld_y)};
+    return contract<kEpiPlain, false, true>(P, &down, 1, true, dev, s);
 }
 
 int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, int* status, cudaStream_t s) {
@@ -275,15 +293,17 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     P.out_up = const_cast<void*>(du.base);
     // dH, and from it dG and dU
-    rc = rows_by_weights<kEpiBackward, false>(P, Problem{{dy, dy}, {wd, wd}, const_cast<void*>(dg.base), ldh, n, g->hidden, g->outputs, 1, true}, dev, s);
+    const Problem factors{{dy, dy}, {wd, wd}, const_cast<void*>(dg.base), ldh, n, g->hidden, g->outputs, 1, true};
+    rc = contract<kEpiBackward, false, false>(P, &factors, 1, false, dev, s);
     if (rc != BMGD_OK) return rc;
-    rc = rows_by_weights<kEpiPlain, false>(P, Problem{{dg, du}, {wg, wu}, g->dx, g->inputs, n, g->inputs, g->hidden, 2, wide(g->dx, g->inputs)}, dev, s);
+    const Problem dx{{dg, du}, {wg, wu}, g->dx, g->inputs, n, g->inputs, g->hidden, 2, wide(g->dx, g->inputs)};
+    rc = contract<kEpiPlain, false, false>(P, &dx, 1, true, dev, s);
     if (rc != BMGD_OK) return rc;
     const Problem weights[3] = {
         {{x, x}, {dg, dg}, g->dw_gate, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_gate, g->hidden)},
         {{x, x}, {du, du}, g->dw_up, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_up, g->hidden)},
         {{h, h}, {dy, dy}, g->dw_down, g->outputs, g->hidden, g->outputs, (int)n, 1, wide(g->dw_down, g->outputs)}};
-    return contract<kEpiPlain, true, true>(P, weights, 3, dev, s);
+    return contract<kEpiPlain, true, true>(P, weights, 3, false, dev, s);
 }
 
 int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspace_bytes, void* stream) {
