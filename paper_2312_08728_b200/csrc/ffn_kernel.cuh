@@ -41,7 +41,7 @@ struct FfnProblem {
     int M, N, K;
     int segments;
     int tiles_m, tiles_n;
-    int a_mn, b_mn;          // few rows: an operand is read across its rows
+    int a_mn;                // few rows: the weights are read across their rows
     int vec;                 // rows of D start on 16-byte boundaries
 };
 
@@ -76,6 +76,7 @@ __device__ __forceinline__ void ffn_wait(uint32_t bar, uint32_t parity, FfnWait&
     }
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // A kernel launched as a dependent of the one before it may start while that one still runs; before it touches memory it
 // waits until that one has finished (and with it all before).
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -250,6 +251,10 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, R::kWarps * CG); }
         fence_barrier_init();
+    }
+    if (threadIdx.x == 32) {
+        prefetch_map(&P.p[0].a[0]);
+        prefetch_map(&P.p[0].b[EPI == kEpiGated ? rank : 0]);
     }
     if (warp == 2) ffn_tmem_alloc<CG>(slot, kTmemCols);
     tc_fence_before();
@@ -528,8 +533,62 @@ __device__ __forceinline__ void store4_any(uint16_t* p, int type, bool vec, int 
     if (left > 3) p[3] = (uint16_t)(hi >> 16);
 }
 
-// Grid: S CTAs (one cluster) per tile.  a: the weights, b: the rows; first_tile, tiles_m and tiles_n count tiles of NR rows and
-// 128 features.  early: the kernel before this one is ours and started after everything before it had finished, so the
+// A CTA's share of `some` rows whose partial sums stand in the shared memory of S <= SP CTAs: a warp takes rows S * 8 apart, four
+// features per lane, and as many rows at once as make eight loads: each takes the time of a trip to another SM.
+template <int SP, int PASS_ROWS, int EPI>
+__device__ __forceinline__ void few_finish(const FfnParams& P, const FfnProblem& q, uint32_t sums, int S, int part, int warp, int lane,
+                                           int f, int first_row, int some) {
+    constexpr int kRows = EPI == kEpiGated ? (SP < 4 ? 4 / SP : 1) : 8 / SP;
+    const int left = q.N - f, step = S * (kFewThreads / 32);
+    uint16_t* const out = static_cast<uint16_t*>(q.out);
+    for (int i0 = part * (kFewThreads / 32) + warp; i0 < some; i0 += step * kRows) {
+        float4 y[kRows][SP], z[kRows][SP];
+#pragma unroll
+        for (int b = 0; b < kRows; ++b) {
+            const uint32_t at = sums + (uint32_t)(((i0 + b * step) * kFewPart + lane * 4) * 4);
+            if (b > 0 && i0 + b * step >= some) continue;
+#pragma unroll
+            for (int c = 0; c < SP; ++c) {
+                if (c >= S) continue;
+                y[b][c] = ld_cluster4(at, c);
+                if constexpr (EPI == kEpiGated) z[b][c] = ld_cluster4(at + PASS_ROWS * kFewPart * 4, c);
+            }
+        }
+        if (left <= 0) continue;
+#pragma unroll
+        for (int b = 0; b < kRows; ++b) {
+            if (b > 0 && i0 + b * step >= some) continue;
+            float4 x = y[b][0], u = z[b][0];
+#pragma unroll
+            for (int c = 1; c < SP; ++c) {
+                if (c >= S) continue;
+                x.x += y[b][c].x; x.y += y[b][c].y; x.z += y[b][c].z; x.w += y[b][c].w;
+                if constexpr (EPI == kEpiGated) { u.x += z[b][c].x; u.y += z[b][c].y; u.z += z[b][c].z; u.w += z[b][c].w; }
+            }
+            const long long row = first_row + i0 + b * step;
+            if constexpr (EPI == kEpiGated) {
+                float4 v, s;
+                act_both(P.act, x.x, v.x, s.x); act_both(P.act, x.y, v.y, s.y);
+                act_both(P.act, x.z, v.z, s.z); act_both(P.act, x.w, v.w, s.w);
+                if (P.value) {
+                    *reinterpret_cast<float4*>(P.value + row * P.ld_save + f) = v;
+                    *reinterpret_cast<float4*>(P.slope + row * P.ld_save + f) = make_float4(u.x * s.x, u.y * s.y, u.z * s.z, u.w * s.w);
+                }
+                store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(v.x * u.x, v.y * u.y, v.z * u.z, v.w * u.w));
+            } else if constexpr (EPI == kEpiBackward) {
+                const float4 v = *reinterpret_cast<const float4*>(P.value + row * P.ld_save + f);
+                const float4 s = *reinterpret_cast<const float4*>(P.slope + row * P.ld_save + f);
+                store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * s.x, x.y * s.y, x.z * s.z, x.w * s.w));
+                store4_any(static_cast<uint16_t*>(P.out_up) + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * v.x, x.y * v.y, x.z * v.z, x.w * v.w));
+            } else {
+                store4_any(out + row * q.ld_out + f, P.type, q.vec, left, x);
+            }
+        }
+    }
+}
+
+// Grid: S CTAs (one cluster) per tile.  a: the weights, b: the rows; tiles_m and tiles_n count tiles of NR rows and of 128
+// features.  early: the kernel before this one is ours and started after everything before it had finished, so the
 // weights, which it does not write, may be fetched while it still runs.
 template <int NR, int EPI>
 __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ffn_few_kernel(const __grid_constant__ FfnParams P, const int S, const int early) {
@@ -538,17 +597,19 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
     const uint32_t ring = (smem_u32(ffn_smem) + 1023u) & ~1023u;
     const uint32_t full = ring + F::kBars, empty = full + 8 * F::kStages, done = empty + 8 * F::kStages, slot = done + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const FfnProblem& q = P.p[0];
     const int part = (int)blockIdx.x % S, tile = (int)blockIdx.x / S;
-    int which = 0;
-    while (which + 1 < P.problems && P.p[which + 1].first_tile <= tile) ++which;
-    const FfnProblem& q = P.p[which];
-    const int in_problem = tile - (int)q.first_tile;
-    const int f0 = in_problem / q.tiles_m * kFewPart, r0 = in_problem % q.tiles_m * NR;
+    const int f0 = tile / q.tiles_m * kFewPart, r0 = tile % q.tiles_m * NR;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done, 1);
         fence_barrier_init();
+    }
+    if (threadIdx.x == 32) {
+        prefetch_map(&q.a[0]);
+        prefetch_map(&q.b[0]);
+        if (EPI == kEpiGated || q.segments > 1) prefetch_map(&q.a[1]);
     }
     if (warp == 2) ffn_tmem_alloc<1>(slot, F::kTmemCols);
     tc_fence_before();
@@ -563,7 +624,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
     FfnWait w{P.status, P.timeout_ns, false};
     if (warp == 0) {
         if (lane == 0) {
-            const bool a_mn = q.a_mn, b_mn = q.b_mn;
+            const bool a_mn = q.a_mn;
             auto weights = [&](int k, int s) {
                 const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
                 const uint32_t bar = full + 8 * s, sa = ring + s * F::kStage;
@@ -573,7 +634,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
             };
             auto rows = [&](int k, int s) {
                 const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
-                ffn_fetch<1>(ring + s * F::kStage + F::kTiles * F::kA, &q.b[seg], b_mn, NR, r0, k0, full + 8 * s);
+                ffn_fetch<1>(ring + s * F::kStage + F::kTiles * F::kA, &q.b[seg], false, NR, r0, k0, full + 8 * s);
             };
             int ahead = 0;
             if (early) {
@@ -594,8 +655,8 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            const uint32_t idesc = ffn_idesc(P.type, q.a_mn, q.b_mn, 128, NR);
-            const FfnDesc ad(q.a_mn), bd(q.b_mn);
+            const uint32_t idesc = ffn_idesc(P.type, q.a_mn, false, 128, NR);
+            const FfnDesc ad(q.a_mn), bd(false);
             int s = 0;
             uint32_t phase = 0;
             for (int k = first; k < last; ++k) {
@@ -623,8 +684,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
     let_next_kernel_start();
     const bool given_up = __syncthreads_or(w.aborted ? 1 : 0) != 0;
 
-    const int f = f0 + lane * 4, left = q.N - f;
-    uint16_t* const out = static_cast<uint16_t*>(q.out);
+    const int f = f0 + lane * 4;
     const int rows = min(NR, q.M - r0);
     const uint32_t ta = tmem + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll 1
@@ -648,39 +708,12 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
         tc_fence_before();
         __syncthreads();
         if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
-        // each CTA finishes its share of the rows: a warp a row at a time, four features per lane
-        const int some = min(F::kPassRows, rows - base);
-        for (int i = part * (kFewThreads / 32) + warp; i < some && !given_up; i += S * (kFewThreads / 32)) {
-            const uint32_t at = ring + (uint32_t)((i * kFewPart + lane * 4) * 4);
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f), u = x;
-            for (int c = 0; c < S; ++c) {
-                const float4 y = ld_cluster4(at, c);
-                x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                if constexpr (EPI == kEpiGated) {
-                    const float4 z = ld_cluster4(at + F::kPassRows * kFewPart * 4, c);
-                    u.x += z.x; u.y += z.y; u.z += z.z; u.w += z.w;
-                }
-            }
-            if (left <= 0) continue;
-            const long long row = r0 + base + i;
-            if constexpr (EPI == kEpiGated) {
-                float4 v, s;
-                act_both(P.act, x.x, v.x, s.x); act_both(P.act, x.y, v.y, s.y);
-                act_both(P.act, x.z, v.z, s.z); act_both(P.act, x.w, v.w, s.w);
-                if (P.value) {
-                    *reinterpret_cast<float4*>(P.value + row * P.ld_save + f) = v;
-                    *reinterpret_cast<float4*>(P.slope + row * P.ld_save + f) = make_float4(u.x * s.x, u.y * s.y, u.z * s.z, u.w * s.w);
-                }
-                store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(v.x * u.x, v.y * u.y, v.z * u.z, v.w * u.w));
-            } else if constexpr (EPI == kEpiBackward) {
-                const float4 v = *reinterpret_cast<const float4*>(P.value + row * P.ld_save + f);
-                const float4 s = *reinterpret_cast<const float4*>(P.slope + row * P.ld_save + f);
-                store4_any(out + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * s.x, x.y * s.y, x.z * s.z, x.w * s.w));
-                store4_any(static_cast<uint16_t*>(P.out_up) + row * q.ld_out + f, P.type, true, 4, make_float4(x.x * v.x, x.y * v.y, x.z * v.z, x.w * v.w));
-            } else {
-                store4_any(out + row * q.ld_out + f, P.type, q.vec, left, x);
-            }
-        }
+        // each CTA finishes its share of the rows
+        const int some = given_up ? 0 : min(F::kPassRows, rows - base);
+        if (S == 1) few_finish<1, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
+        else if (S == 2) few_finish<2, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
+        else if (S <= 4) few_finish<4, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
+        else few_finish<8, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
     }
     if (given_up) {  // copies and products may still be in flight
         const unsigned long long t0 = global_ns();

@@ -125,71 +125,88 @@ int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, 
     return BMGD_OK;
 }
 
-template <int NR, int EPI, bool ROWS_MN, bool W_MN>
-int launch_few(FfnParams& P, const Problem* problems, int count, bool early, const Device& dev, cudaStream_t s) {
+template <int NR, int EPI, bool W_MN>
+int launch_few(FfnParams& P, const Problem& x, int split, bool early, const Device& dev, cudaStream_t s) {
     using F = FewShape<NR, EPI>;
-    int64_t tiles = 0;
-    int least = 0x7FFFFFFF;
-    for (int k = 0; k < count; ++k) {
-        const Problem& x = problems[k];
-        FfnProblem& q = P.p[k];
-        // exchanged roles: the weights are the kernel's a
-        for (int i = 0; i < 2; ++i) {
-            int rc = BMGD_OK;
-            if (i < x.segments || EPI == kEpiGated) rc = make_map(x.b[i], P.type, W_MN ? 64 : 128, &q.a[i]);
-            if (rc == BMGD_OK && i < x.segments) rc = make_map(x.a[i], P.type, ROWS_MN ? 64 : NR, &q.b[i]);
-            if (rc != BMGD_OK) return rc;
-        }
-        q.out = x.out; q.ld_out = x.ld_out;
-        q.M = (int)x.M; q.N = x.N; q.K = x.K; q.segments = x.segments;
-        q.a_mn = W_MN; q.b_mn = ROWS_MN; q.vec = x.vec;
-        q.tiles_m = (int)((x.M + NR - 1) / NR);
-        q.tiles_n = (x.N + kFewPart - 1) / kFewPart;
-        q.first_tile = tiles;
-        tiles += (int64_t)q.tiles_m * q.tiles_n;
-        least = std::min(least, x.segments * ((x.K + kFfnBK - 1) / kFfnBK));
+    FfnProblem& q = P.p[0];
+    // exchanged roles: the weights are the kernel's a
+    for (int i = 0; i < 2; ++i) {
+        int rc = BMGD_OK;
+        if (i < x.segments || EPI == kEpiGated) rc = make_map(x.b[i], P.type, W_MN ? 64 : 128, &q.a[i]);
+        if (rc == BMGD_OK && i < x.segments) rc = make_map(x.a[i], P.type, NR, &q.b[i]);
+        if (rc != BMGD_OK) return rc;
     }
-    P.problems = count;
-    P.tiles = tiles;
-    const int64_t room = (int64_t)dev.sms * F::kCtasPerSm / tiles;
-    const int split = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, room), least / 2));
+    q.out = x.out; q.ld_out = x.ld_out;
+    q.M = (int)x.M; q.N = x.N; q.K = x.K; q.segments = x.segments;
+    q.a_mn = W_MN; q.vec = x.vec;
+    q.tiles_m = (int)((x.M + NR - 1) / NR);
+    q.tiles_n = (x.N + kFewPart - 1) / kFewPart;
     if (F::kSmem > dev.smem) return BMGD_ERR_LAUNCH;
     auto* fn = ffn_few_kernel<NR, EPI>;
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
-    launch_config(&lc, at, dim3((unsigned)(tiles * split)), kFewThreads, F::kSmem, split, s);
+    launch_config(&lc, at, dim3((unsigned)(q.tiles_m * q.tiles_n * split)), kFewThreads, F::kSmem, split, s);
     if (cudaLaunchKernelEx(&lc, fn, P, split, early ? 1 : 0) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
 
-// Up to 256 rows, and wherever tiles of 128 x 128 do not fill the GPU once, the form with exchanged roles; otherwise tiles of
-// 256 rows x 256 columns for two CTAs, or of 128 x 128 where those would leave more than half of the GPU idle.  ROWS_MN, W_MN:
-// the first operand, or the second, is read across its rows.
-constexpr int64_t kFewRows = 256;
-template <int EPI, bool ROWS_MN, bool W_MN>
-int contract(FfnParams& P, const Problem* problems, int count, bool early, const Device& dev, cudaStream_t s) {
-    constexpr int kCols = EPI == kEpiGated ? 128 : 256;
-    int64_t large = 0, small = 0, few = 0, rows = 0;
-    for (int k = 0; k < count; ++k) {
-        const Problem& x = problems[k];
-        large += ((x.M + 255) / 256) * ((x.N + kCols - 1) / kCols);
-        small += ((x.M + 127) / 128) * ((x.N + kCols / 2 - 1) / (kCols / 2));
-        few += ((x.M + 127) / 128) * ((x.N + kFewPart - 1) / kFewPart);
-        rows = std::max(rows, x.M);
-    }
-    if ((!ROWS_MN && rows <= kFewRows) || small <= dev.sms) {
-        if constexpr (!ROWS_MN) {
-            if (rows <= 16) return launch_few<16, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
-            if (rows <= 32) return launch_few<32, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
+// Rows per tile and split of the contraction for the form with exchanged roles, by an estimate in microseconds fitted to a
+// sweep on B200 over rows 1 to 2000, widths 256 to 11008: a CTA takes in 80 KB a microsecond (its stages in flight over the
+// latency of a copy), all of them together no more than 8 MB; reading out a row's sums takes 0.015 and exchanging them 0.006
+// more per CTA of the cluster, a cluster about 1.  Within 2 us of the best of the sweep throughout; always taking 128 rows
+// and the largest split that fits cost up to 9 us of 30 there.
+struct FewChoice {
+    int rows, split;
+};
+template <int EPI>
+FewChoice choose_few(const Problem& x, const Device& dev) {
+    const int kinds = EPI == kEpiGated ? 2 : 1, steps = x.segments * ((x.K + kFfnBK - 1) / kFfnBK);
+    FewChoice best{16, 1};
+    double least = 1e30;
+    for (int nr = 16; nr <= 128; nr *= 2) {
+        if (nr > 16 && nr / 2 >= x.M) break;
+        const int64_t tiles = ((x.M + nr - 1) / nr) * ((x.N + kFewPart - 1) / kFewPart), slots = 2 * (int64_t)dev.sms;
+        const double stage = kinds * 16384 + nr * 128, rows = (double)std::min<int64_t>(nr, x.M) * kinds;
+        for (int split : {1, 2, 3, 4, 8}) {
+            if (split > 1 && (tiles * split > slots || split * 2 > steps)) break;
+            const double turns = (double)((tiles * split + slots - 1) / slots);
+            const double copies = std::max(turns * ((steps + split - 1) / split) * stage / 80e3, (double)tiles * steps * stage / 8e6);
+            const double t = copies + turns * rows * (0.015 + 0.006 * (split - 1)) + (split > 1 ? 1.0 : 0.0);
+            if (t < least) { least = t; best = FewChoice{nr, split}; }
         }
-        // (tiles of 64 rows where even those of a contraction too short to split leave room)
-        const int steps = problems[0].segments * ((problems[0].K + kFfnBK - 1) / kFfnBK);
-        if (rows <= 64 || (few * 2 <= dev.sms && steps < 8)) return launch_few<64, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
-        return launch_few<128, EPI, ROWS_MN, W_MN>(P, problems, count, early, dev, s);
     }
-    if (large * 4 >= dev.sms) return launch<2, 256, EPI, ROWS_MN, W_MN>(P, problems, count, dev, s);
+    return best;
+}
+template <int EPI, bool W_MN>
+int contract_few(FfnParams& P, const Problem& x, bool early, const Device& dev, cudaStream_t s) {
+    const FewChoice c = choose_few<EPI>(x, dev);
+    if (c.rows == 16) return launch_few<16, EPI, W_MN>(P, x, c.split, early, dev, s);
+    if (c.rows == 32) return launch_few<32, EPI, W_MN>(P, x, c.split, early, dev, s);
+    if (c.rows == 64) return launch_few<64, EPI, W_MN>(P, x, c.split, early, dev, s);
+    return launch_few<128, EPI, W_MN>(P, x, c.split, early, dev, s);
+}
+
+// Rows by weights.  The form with exchanged roles for few rows, and wherever tiles of 128 x 128 do not fill the GPU once (not
+// for the gated kind, whose exchange is twice as long: 250 rows 1024 -> 4096 took 7 us more of 30 that way).  Otherwise tiles
+// of 256 rows x 256 columns for two CTAs from 0.4 of them per SM on, or of 128 x 128: measured on the gated kind, 777 rows
+// 504 -> 1376 (44 large tiles) 3 us more with the large ones, 300 rows 2048 -> 4096 (64) 4 us more with the small ones.
+template <int EPI, bool ROWS_MN, bool W_MN>
+int contract_many(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
+    constexpr int kCols = EPI == kEpiGated ? 128 : 256;
+    int64_t large = 0;
+    for (int k = 0; k < count; ++k) large += ((problems[k].M + 255) / 256) * ((problems[k].N + kCols - 1) / kCols);
+    // a contraction of a few steps (the weights' gradients of few rows) is all read-out, which pairs of CTAs do not speed up:
+    // one row 4096 -> 11008 -> 4096 took 11 us more of 84 with them
+    const bool short_sum = problems[0].segments * (int64_t)problems[0].K <= 256;
+    if (large * 5 >= dev.sms * 2 && !short_sum) return launch<2, 256, EPI, ROWS_MN, W_MN>(P, problems, count, dev, s);
     return launch<1, 128, EPI, ROWS_MN, W_MN>(P, problems, count, dev, s);
+}
+template <int EPI, bool W_MN>
+int contract(FfnParams& P, const Problem& x, bool early, const Device& dev, cudaStream_t s) {
+    const int64_t tiles = ((x.M + 127) / 128) * ((x.N + 127) / 128);
+    const bool few = EPI == kEpiGated ? x.M <= 128 : x.M <= 256 || tiles <= dev.sms;
+    return few ? contract_few<EPI, W_MN>(P, x, early, dev, s) : contract_many<EPI, false, W_MN>(P, &x, 1, dev, s);
 }
 
 int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -271,11 +288,11 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = kTimeoutNs;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     const Problem gated{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true};
-    rc = contract<kEpiGated, false, true>(P, &gated, 1, false, dev, s);
+    rc = contract<kEpiGated, true>(P, gated, false, dev, s);
     if (rc != BMGD_OK) return rc;
     const Matrix hm{h, g->rows, g->hidden, ldh};
     const Problem down{{hm, hm}, {wd, wd}, g->y, g->ld_y, g->rows, g->outputs, g->hidden, 1, wide(g->y, g->ld_y)};
-    return contract<kEpiPlain, false, true>(P, &down, 1, true, dev, s);
+    return contract<kEpiPlain, true>(P, down, true, dev, s);
 }
 
 int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, int* status, cudaStream_t s) {
@@ -294,16 +311,16 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     P.out_up = const_cast<void*>(du.base);
     // dH, and from it dG and dU
     const Problem factors{{dy, dy}, {wd, wd}, const_cast<void*>(dg.base), ldh, n, g->hidden, g->outputs, 1, true};
-    rc = contract<kEpiBackward, false, false>(P, &factors, 1, false, dev, s);
+    rc = contract<kEpiBackward, false>(P, factors, false, dev, s);
     if (rc != BMGD_OK) return rc;
     const Problem dx{{dg, du}, {wg, wu}, g->dx, g->inputs, n, g->inputs, g->hidden, 2, wide(g->dx, g->inputs)};
-    rc = contract<kEpiPlain, false, false>(P, &dx, 1, true, dev, s);
+    rc = contract<kEpiPlain, false>(P, dx, true, dev, s);
     if (rc != BMGD_OK) return rc;
     const Problem weights[3] = {
         {{x, x}, {dg, dg}, g->dw_gate, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_gate, g->hidden)},
         {{x, x}, {du, du}, g->dw_up, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_up, g->hidden)},
         {{h, h}, {dy, dy}, g->dw_down, g->outputs, g->hidden, g->outputs, (int)n, 1, wide(g->dw_down, g->outputs)}};
-    return contract<kEpiPlain, true, true>(P, weights, 3, false, dev, s);
+    return contract_many<kEpiPlain, true, true>(P, weights, 3, dev, s);
 }
 
 int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspace_bytes, void* stream) {
