@@ -11,11 +11,48 @@ using namespace bmgdk;
 
 int launched() { return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA; }
 
+template <typename T, int TH, int NV>
+int residual_rows(const T* z, int64_t ldz, const int32_t* y, T* out, int64_t ldo, float* loss, int64_t rows, int32_t C, float scale, int R, cudaStream_t s) {
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)(TH == 32 ? (rows + 7) / 8 : rows * R));
+    lc.blockDim = dim3(TH == 32 ? 256 : TH);
+    lc.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = R; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = R > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&lc, residual_row_kernel<T, TH, NV>, z, (long long)ldz, y, out, (long long)ldo, loss, (long long)rows, C, scale, R) != cudaSuccess) {
+        cudaGetLastError();
+        return BMGD_ERR_CUDA;
+    }
+    return BMGD_OK;
+}
+
+// By the row's length in pieces of 16 bytes: a warp to a row up to 256 pieces, then blocks of 128 to 512 threads with eight
+// pieces each, then clusters of blocks of 512; beyond eight of those the row is read twice.
 template <typename T>
-int residual(const void* z, int64_t ldz, const int32_t* y, void* out, int64_t ldo, float* loss, int64_t rows, int32_t C,
-             float scale, cudaStream_t s) {
-    const int grid = (int)std::min<int64_t>(rows, 148 * 64);
-    residual_rows_kernel<T><<<grid, 256, 0, s>>>(static_cast<const T*>(z), ldz, y, static_cast<T*>(out), ldo, loss, rows, C, scale);
+int residual(const void* logits, int64_t ldz, const int32_t* y, void* residual, int64_t ldo, float* loss, int64_t rows, int32_t C, float scale, cudaStream_t s) {
+    const T* z = static_cast<const T*>(logits);
+    T* out = static_cast<T*>(residual);
+    if (C <= 256) {
+        const int lanes = C <= 32 ? 4 : C <= 64 ? 8 : 32;
+        const unsigned grid = (unsigned)std::min<int64_t>((rows * lanes + 255) / 256, 148 * 32);
+        if (lanes == 4) residual_short_kernel<T, 4><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+        else if (lanes == 8) residual_short_kernel<T, 8><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+        else residual_short_kernel<T, 32><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+        return launched();
+    }
+    const int64_t pieces = ((int64_t)C * (int64_t)sizeof(T) + 15) / 16;
+    if (pieces <= 64) return residual_rows<T, 32, 2>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    if (pieces <= 128) return residual_rows<T, 32, 4>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    if (pieces <= 256) return residual_rows<T, 32, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    if (pieces <= 512) return residual_rows<T, 128, 4>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    if (pieces <= 1024) return residual_rows<T, 128, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    if (pieces <= 2048) return residual_rows<T, 256, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    for (int R = 1; R <= 8; R *= 2)
+        if (pieces <= 4096 * R && rows * R <= 0x7FFFFFFFll) return residual_rows<T, 512, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, R, s);
+    residual_long_kernel<T><<<(unsigned)std::min<int64_t>(rows, 148 * 2), 1024, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
     return launched();
 }
 

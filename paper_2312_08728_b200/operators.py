@@ -15,6 +15,8 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import operator
+import struct
 from array import array
 from typing import List, Optional, Sequence, Tuple, Union
 
@@ -36,6 +38,9 @@ def _status(rc: int, where: str) -> None:
         raise BmgdError(rc, where)
 
 
+_HERE = contextlib.nullcontext()
+
+
 @contextlib.contextmanager
 def _other(device: torch.device, stream: Optional[torch.cuda.Stream]):
     with torch.cuda.device(device):
@@ -50,8 +55,8 @@ def _place(device: torch.device, stream: Optional[torch.cuda.Stream]):
     """Context in which outputs are allocated and kernels launched: the tensors' device, on the stream that orders them."""
     if stream is not None and stream.device != device:
         raise ValueError(f"the stream belongs to {stream.device}, the tensors live on {device}")
-    if stream is None and torch.cuda.current_device() == device.index:
-        return contextlib.nullcontext()
+    if stream is None and torch._C._cuda_getDevice() == device.index:
+        return _HERE
     return _other(device, stream)
 
 
@@ -60,24 +65,25 @@ def _current(device: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
-def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int], dtype: torch.dtype, device: torch.device) -> int:
-    """Refuse a tensor that is not a [rows, cols] matrix with contiguous rows; returns its row stride."""
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int], dtype: torch.dtype, device: torch.device):
+    """Refuse a tensor that is not a [rows, cols] matrix with contiguous rows; returns its size and row stride."""
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         want = ", ".join("any" if n is None else str(n) for n in (rows, cols))
-        raise ValueError(f"{name} must be [{want}], got {tuple(t.shape)}")
-    if t.dtype != dtype:
+        raise ValueError(f"{name} must be [{want}], got {tuple(shape)}")
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} must live on {device}, got {t.device}")
-    n, c = t.shape
+    n, c = shape
     s0, s1 = t.stride()
     if c > 1 and s1 != 1:
         raise ValueError(f"{name} must have contiguous rows, got strides {(s0, s1)}")
     if n <= 1:
-        return max(c, 1)
+        return n, c, c if c > 1 else 1
     if s0 < c:
         raise ValueError(f"{name} has rows that overlap: stride {s0} for {c} columns")
-    return s0
+    return n, c, s0
 
 
 def _device_of(t: torch.Tensor, name: str) -> torch.device:
@@ -88,50 +94,45 @@ def _device_of(t: torch.Tensor, name: str) -> torch.device:
 
 # ---------------------------------------------------------------- gated feed-forward block
 
-class _GatedFfn(ctypes.Structure):
-    _fields_ = [("rows", ctypes.c_int64)] + [(k, ctypes.c_int32) for k in (
-        "inputs", "hidden", "outputs", "type", "activation", "reserved")] + [(k, ctypes.c_void_p) for k in (
-            "x", "w_gate", "w_up", "w_down")] + [(k, ctypes.c_int64) for k in ("ld_x", "ld_gate", "ld_up", "ld_down")] + [
-        ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("saved_value", ctypes.c_void_p),
-        ("saved_slope", ctypes.c_void_p), ("saved_hidden", ctypes.c_void_p),
-        ("ld_saved", ctypes.c_int64), ("dy", ctypes.c_void_p), ("ld_dy", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in (
-            "dx", "dw_gate", "dw_up", "dw_down")]
-
-
+# bmgd_gated_ffn of include/bmgd.h: rows; inputs, hidden, outputs, type, activation, reserved; x, w_gate, w_up, w_down and their
+# strides; y and its stride; saved_value, saved_slope, saved_hidden, ld_saved; dy and its stride; dx, dw_gate, dw_up, dw_down
+_GATED_FFN = struct.Struct("=q6i4Q4qQq3QqQq4Q")
 _FORWARD, _BACKWARD = 0, 1
 
 
-def _ffn_args(x, w_gate, w_up, w_down, activation) -> _GatedFfn:
+def _ffn_args(x, w_gate, w_up, w_down, activation):
+    """The members that both passes share, and (rows, inputs, hidden, outputs)."""
     device = _device_of(x, "x")
-    if x.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError(f"x must be bfloat16 or float16, got {x.dtype}")
+    dtype = x.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        raise ValueError(f"x must be bfloat16 or float16, got {dtype}")
     if activation not in (ACT_SILU, ACT_GELU, ACT_RELU, ACT_SIGMOID):
         raise ValueError(f"unknown activation code {activation}")
-    g = _GatedFfn()
-    g.ld_x = _matrix(x, "x", None, None, x.dtype, device)
-    n, d = x.shape
-    g.ld_gate = _matrix(w_gate, "w_gate", d, None, x.dtype, device)
-    f = w_gate.shape[1]
-    g.ld_up = _matrix(w_up, "w_up", d, f, x.dtype, device)
-    g.ld_down = _matrix(w_down, "w_down", f, None, x.dtype, device)
-    c = w_down.shape[1]
-    if min(d, f, c) < 1:
+    n, d, ld_x = _matrix(x, "x", None, None, dtype, device)
+    _, f, ld_gate = _matrix(w_gate, "w_gate", d, None, dtype, device)
+    _, _, ld_up = _matrix(w_up, "w_up", d, f, dtype, device)
+    _, c, ld_down = _matrix(w_down, "w_down", f, None, dtype, device)
+    if d < 1 or f < 1 or c < 1:
         raise ValueError("the block needs at least one input, one hidden unit and one output")
-    g.rows, g.inputs, g.hidden, g.outputs, g.type, g.activation = n, d, f, c, _TYPES[x.dtype], activation
-    g.x, g.w_gate, g.w_up, g.w_down = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()
-    return g
+    return (n, d, f, c, _TYPES[dtype], activation, 0, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
+            ld_x, ld_gate, ld_up, ld_down), (n, d, f, c), device
 
 
-def _saved_args(g: _GatedFfn, factors: torch.Tensor, hidden: torch.Tensor) -> None:
-    g.ld_saved = hidden.shape[1]
-    g.saved_value, g.saved_hidden = factors.data_ptr(), hidden.data_ptr()
-    g.saved_slope = factors.data_ptr() + g.rows * g.ld_saved * 4
+def _saved_args(factors: torch.Tensor, hidden: torch.Tensor):
+    p, ld = factors.data_ptr(), hidden.shape[1]
+    return p, p + hidden.shape[0] * ld * 4, hidden.data_ptr(), ld
 
 
-def _workspace(L, g: _GatedFfn, which: int, device: torch.device) -> Tuple[torch.Tensor, int]:
+def _run_ffn(which: int, args: bytes, device: torch.device) -> None:
+    L = _binding.load_library()
     need = ctypes.c_int64()
-    _status(L.bmgd_gated_ffn_workspace_bytes(ctypes.byref(g), which, ctypes.byref(need)), "bmgd_gated_ffn_workspace_bytes")
-    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+    rc = L.bmgd_gated_ffn_workspace_bytes(args, which, ctypes.byref(need))
+    if rc == BMGD_OK:
+        w = torch.empty(need.value, dtype=torch.uint8, device=device)
+        call = L.bmgd_gated_ffn_forward if which == _FORWARD else L.bmgd_gated_ffn_backward
+        rc = call(args, w.data_ptr(), need.value, _current(device))
+    if rc != BMGD_OK:
+        raise BmgdError(rc, "bmgd_gated_ffn_forward" if which == _FORWARD else "bmgd_gated_ffn_backward")
 
 
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: int = ACT_SILU,
@@ -140,21 +141,16 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
 
     All four in bfloat16 or all in float16; rows contiguous, any row stride.  With save=True returns (y, saved), saved
     being what gated_ffn_backward needs beside its other arguments."""
-    g = _ffn_args(x, w_gate, w_up, w_down, activation)
-    L = _binding.load_library()
-    with _place(x.device, stream):
-        y = torch.empty(g.rows, g.outputs, dtype=x.dtype, device=x.device)
-        saved = None
+    shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
+    with _place(device, stream):
+        y = torch.empty(n, c, dtype=x.dtype, device=device)
+        saved, kept = None, (0, 0, 0, 0)
         if save:
-            width = -(-g.hidden // 8) * 8
-            saved = (torch.empty(2, g.rows, width, dtype=torch.float32, device=x.device),
-                     torch.empty(g.rows, width, dtype=x.dtype, device=x.device))
-            _saved_args(g, *saved)
-        if g.rows > 0:
-            g.y, g.ld_y = y.data_ptr(), g.outputs
-            w, size = _workspace(L, g, _FORWARD, x.device)
-            _status(L.bmgd_gated_ffn_forward(ctypes.byref(g), w.data_ptr(), size, _current(x.device)),
-                    "bmgd_gated_ffn_forward")
+            width = (f + 7) // 8 * 8
+            saved = (torch.empty(2, n, width, dtype=torch.float32, device=device), torch.empty(n, width, dtype=x.dtype, device=device))
+            kept = _saved_args(*saved)
+        if n > 0:
+            _run_ffn(_FORWARD, _GATED_FFN.pack(*shared, y.data_ptr(), c, *kept, 0, 0, 0, 0, 0, 0), device)
     return (y, saved) if save else y
 
 
@@ -164,24 +160,18 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
     """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the gradient dy of its output.
 
     `saved` is what the forward call on the same arguments returned; the gradients have the type of x."""
-    g = _ffn_args(x, w_gate, w_up, w_down, activation)
-    g.ld_dy = _matrix(dy, "dy", g.rows, g.outputs, x.dtype, x.device)
-    width = -(-g.hidden // 8) * 8
+    shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
+    _, _, ld_dy = _matrix(dy, "dy", n, c, x.dtype, device)
+    width = (f + 7) // 8 * 8
     if not isinstance(saved, tuple) or len(saved) != 2:
         raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
-    for t, shape, dtype in zip(saved, ((2, g.rows, width), (g.rows, width)), (torch.float32, x.dtype)):
-        if t.shape != shape or t.dtype != dtype or t.device != x.device or not t.is_contiguous():
+    for t, shape, dtype in zip(saved, ((2, n, width), (n, width)), (torch.float32, x.dtype)):
+        if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
             raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
-    L = _binding.load_library()
-    with _place(x.device, stream):
-        dx, dw_gate, dw_up, dw_down = (torch.empty(s, dtype=x.dtype, device=x.device)
-                                       for s in (x.shape, w_gate.shape, w_up.shape, w_down.shape))
-        g.dx, g.dw_gate, g.dw_up, g.dw_down = dx.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr(), dw_down.data_ptr()
-        g.dy = dy.data_ptr()
-        _saved_args(g, *saved)
-        w, size = _workspace(L, g, _BACKWARD, x.device)
-        _status(L.bmgd_gated_ffn_backward(ctypes.byref(g), w.data_ptr(), size, _current(x.device)),
-                "bmgd_gated_ffn_backward")
+    with _place(device, stream):
+        dx, dw_gate, dw_up, dw_down = [torch.empty(s, dtype=x.dtype, device=device) for s in ((n, d), (d, f), (d, f), (f, c))]
+        _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(*saved), dy.data_ptr(), ld_dy, dx.data_ptr(), dw_gate.data_ptr(),
+                                            dw_up.data_ptr(), dw_down.data_ptr()), device)
     return dx, dw_gate, dw_up, dw_down
 
 
@@ -201,8 +191,7 @@ def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[floa
     device = _device_of(logits, "logits")
     if logits.dtype not in _TYPES:
         raise ValueError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")
-    ld = _matrix(logits, "logits", None, None, logits.dtype, device)
-    rows, C = logits.shape
+    rows, C, ld = _matrix(logits, "logits", None, None, logits.dtype, device)
     if C < 1:
         raise ValueError("logits need at least one class")
     if y.dim() != 1 or y.shape[0] != rows or y.dtype != torch.int32 or y.device != device or not y.is_contiguous():
@@ -265,19 +254,28 @@ def adamw_state(params: Sequence[torch.Tensor], state_bits: int = 32) -> dict:
     return out
 
 
-def _column(tensors: Sequence[torch.Tensor], name: str, counts: List[int], types: Sequence[torch.dtype], device: int) -> List[int]:
-    """Refuse a list of tensors that does not match the parameters; returns their addresses."""
+_dtype = operator.attrgetter("dtype")
+_numel, _get_device, _is_contiguous, _data_ptr = (getattr(torch.Tensor, k) for k in ("numel", "get_device", "is_contiguous", "data_ptr"))
+
+
+def _column(tensors: Sequence[torch.Tensor], name: str, counts: List[int], types: frozenset, device: int):
+    """Refuse a list of tensors that does not match the parameters; returns their addresses and the types among them."""
     if len(tensors) != len(counts):
         raise ValueError(f"{name}: {len(tensors)} tensors for {len(counts)} parameters")
-    if [t.numel() for t in tensors] != counts:
+    if list(map(_numel, tensors)) != counts:
         raise ValueError(f"{name}: a tensor's size does not match its parameter's")
-    if not {t.dtype for t in tensors} <= set(types):
-        raise ValueError(f"{name} must be {' or '.join(str(t) for t in types)}, got {({t.dtype for t in tensors} - set(types)).pop()}")
-    if any([t.get_device() != device for t in tensors]):
+    found = set(map(_dtype, tensors))
+    if not found <= types:
+        raise ValueError(f"{name} must be {' or '.join(sorted(map(str, types)))}, got {(found - types).pop()}")
+    if set(map(_get_device, tensors)) - {device}:
         raise ValueError(f"{name}: all tensors must live on one device")
-    if not all([t.is_contiguous() for t in tensors]):
+    if not all(map(_is_contiguous, tensors)):
         raise ValueError(f"{name}: tensors must be contiguous")
-    return [t.data_ptr() for t in tensors]
+    return list(map(_data_ptr, tensors)), found
+
+
+_ANY, _FLOAT = frozenset(_TYPES), frozenset((torch.float32,))
+_M, _V, _BYTES = frozenset((torch.float32, torch.float8_e4m3fn)), frozenset((torch.float32, torch.uint8)), frozenset((torch.uint8,))
 
 
 def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
@@ -296,47 +294,50 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
         raise ValueError("no parameters")
     device = _device_of(params[0], "params")
     index = device.index
-    counts = [t.numel() for t in params]
-    columns = [_column(params, "params", counts, tuple(_TYPES), index), _column(grads, "grads", counts, tuple(_TYPES), index),
-               _column(m, "m", counts, (torch.float32, torch.float8_e4m3fn), index),
-               _column(v, "v", counts, (torch.float32, torch.uint8), index)]
-    eight = [t.dtype != torch.float32 for t in m]
-    if eight != [t.dtype != torch.float32 for t in v]:
-        raise ValueError("m and v of a parameter must be held in the same number of bits")
-    if any(eight):
+    counts = list(map(_numel, params))
+    at_params, p_types = _column(params, "params", counts, _ANY, index)
+    at_grads, g_types = _column(grads, "grads", counts, _ANY, index)
+    at_m, m_types = _column(m, "m", counts, _M, index)
+    at_v, v_types = _column(v, "v", counts, _V, index)
+    table = array("q", bytes(88 * count))  # bmgd_adamw_tensor[count], filled column by column
+    for k, column in enumerate((at_params, at_grads, at_m, at_v)):
+        table[k::11] = array("q", column)
+    if m_types == _FLOAT and v_types == _FLOAT:
+        table[10::11] = array("q", range(32, 32 + (count << 32), 1 << 32))  # state_bits and index
+    else:
+        eight = [t.dtype is not torch.float32 for t in m]
+        if eight != [t.dtype is not torch.float32 for t in v]:
+            raise ValueError("m and v of a parameter must be held in the same number of bits")
         if m_scale is None or v_scale is None:
             raise ValueError("moments in 8 bits need m_scale and v_scale")
         blocks = [-(-n // SCALE_BLOCK) for n in counts]
-        columns += [_column(m_scale, "m_scale", blocks, (torch.uint8,), index), _column(v_scale, "v_scale", blocks, (torch.uint8,), index)]
-    else:
-        columns += [[0] * count, [0] * count]
-    if masters is None:
-        columns.append([0] * count)
-    else:
+        table[4::11] = array("q", _column(m_scale, "m_scale", blocks, _BYTES, index)[0])
+        table[5::11] = array("q", _column(v_scale, "v_scale", blocks, _BYTES, index)[0])
+        table[10::11] = array("q", [(8 if e else 32) | i << 32 for i, e in enumerate(eight)])
+    if masters is not None:
         if len(masters) != count:
             raise ValueError(f"masters: {len(masters)} tensors for {count} parameters")
         held = [i for i, t in enumerate(masters) if t is not None]
-        at = _column([masters[i] for i in held], "masters", [counts[i] for i in held], (torch.float32,), index)
-        column = [0] * count
-        for i, p in zip(held, at):
-            if params[i].dtype == torch.float32:
+        for i, at in zip(held, _column([masters[i] for i in held], "masters", [counts[i] for i in held], _FLOAT, index)[0]):
+            if params[i].dtype is torch.float32:
                 raise ValueError("a float32 parameter has no master copy")
-            column[i] = p
-        columns.append(column)
+            table[11 * i + 6] = at
+    if torch.float16 in p_types and (masters is None or any(t is None and p.dtype is torch.float16 for p, t in zip(params, masters))):
+        raise ValueError("a float16 parameter needs a master copy")
     if control.dtype != torch.int64 or control.numel() != CONTROL_WORDS or control.device != device or not control.is_contiguous():
         raise ValueError(f"control must be a contiguous int64 [{CONTROL_WORDS}] on {device}")
+    table[7::11] = array("q", counts)
     if isinstance(weight_decay, (int, float)):
         decays = array("d", [weight_decay]) * count
     else:
         decays = array("d", weight_decay)
         if len(decays) != count:
             raise ValueError(f"weight_decay: {len(decays)} values for {count} parameters")
-    decay_bits = memoryview(decays).cast("B").cast("q")
-    kinds = [_TYPES[p.dtype] | _TYPES[g.dtype] << 32 for p, g in zip(params, grads)]
-    if masters is None and any([k & 0xFFFFFFFF == TYPE_F16 for k in kinds]):
-        raise ValueError("a float16 parameter needs a master copy")
-    bits = [(8 if e else 32) | i << 32 for i, e in enumerate(eight)]
-    table = array("q", [x for row in zip(*columns, counts, decay_bits, kinds, bits) for x in row])  # bmgd_adamw_tensor[count]
+    table[8::11] = array("q", decays.tobytes())
+    if len(p_types) == 1 and len(g_types) == 1:
+        table[9::11] = array("q", [_TYPES[params[0].dtype] | _TYPES[grads[0].dtype] << 32]) * count
+    else:
+        table[9::11] = array("q", [_TYPES[p.dtype] | _TYPES[g.dtype] << 32 for p, g in zip(params, grads)])
     cfg = _AdamwConfig(float(lr), float(a), float(b), float(eps), float(grad_scale), float(max_norm), int(seed) & 0xFFFFFFFFFFFFFFFF)
     L = _binding.load_library()
     with _place(device, stream):
