@@ -30,29 +30,31 @@ int residual_rows(const T* z, int64_t ldz, const int32_t* y, T* out, int64_t ldo
 }
 
 // By the row's length in pieces of 16 bytes: a warp to a row up to 256 pieces, then blocks of 128 to 512 threads with eight
-// pieces each, then clusters of blocks of 512; beyond eight of those the row is read twice.
+// pieces each, then the form that reads a row twice, or for a few rows clusters of blocks of 512.
 template <typename T>
 int residual(const void* logits, int64_t ldz, const int32_t* y, void* residual, int64_t ldo, float* loss, int64_t rows, int32_t C, float scale, cudaStream_t s) {
     const T* z = static_cast<const T*>(logits);
     T* out = static_cast<T*>(residual);
-    if (C <= 256) {
-        const int lanes = C <= 32 ? 4 : C <= 64 ? 8 : 32;
-        const unsigned grid = (unsigned)std::min<int64_t>((rows * lanes + 255) / 256, 148 * 32);
-        if (lanes == 4) residual_short_kernel<T, 4><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
-        else if (lanes == 8) residual_short_kernel<T, 8><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
-        else residual_short_kernel<T, 32><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+    if (C <= 64) {
+        const unsigned grid = (unsigned)std::min<int64_t>((rows * (C <= 16 ? 2 : C <= 32 ? 4 : 8) + 255) / 256, 148 * 32);
+        if (C <= 16) residual_short_kernel<T, 2><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+        else if (C <= 32) residual_short_kernel<T, 4><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+        else residual_short_kernel<T, 8><<<grid, 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
         return launched();
     }
     const int64_t pieces = ((int64_t)C * (int64_t)sizeof(T) + 15) / 16;
+    if (pieces <= 32) return residual_rows<T, 32, 1>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
     if (pieces <= 64) return residual_rows<T, 32, 2>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
     if (pieces <= 128) return residual_rows<T, 32, 4>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
     if (pieces <= 256) return residual_rows<T, 32, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
     if (pieces <= 512) return residual_rows<T, 128, 4>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
     if (pieces <= 1024) return residual_rows<T, 128, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
     if (pieces <= 2048) return residual_rows<T, 256, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
-    for (int R = 1; R <= 8; R *= 2)
-        if (pieces <= 4096 * R && rows * R <= 0x7FFFFFFFll) return residual_rows<T, 512, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, R, s);
-    residual_long_kernel<T><<<(unsigned)std::min<int64_t>(rows, 148 * 2), 1024, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+    if (pieces <= 4096) return residual_rows<T, 512, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 1, s);
+    if (rows * 8 <= 148 * 2 && pieces <= 4096 * 8) return residual_rows<T, 512, 8>(z, ldz, y, out, ldo, loss, rows, C, scale, 8, s);
+    if (pieces <= 8192) residual_long_kernel<T, 256><<<(unsigned)std::min<int64_t>(rows, 148 * 4), 256, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+    else if (pieces <= 20480) residual_long_kernel<T, 512><<<(unsigned)std::min<int64_t>(rows, 148 * 2), 512, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
+    else residual_long_kernel<T, 1024><<<(unsigned)std::min<int64_t>(rows, 148), 1024, 0, s>>>(z, ldz, y, out, ldo, loss, rows, C, scale);
     return launched();
 }
 

@@ -52,9 +52,9 @@ __device__ __forceinline__ bool row_counts(const MaxSum& a, int label, int C) {
 }
 __device__ __forceinline__ float row_loss(const MaxSum& a, float z_label) { return (against(a.m) - z_label) + logf(a.s); }
 
-// ---- up to 256 classes: LANES lanes of a warp hold a row, up to eight logits each
+// ---- up to 64 classes: LANES lanes of a warp hold a row, up to eight logits each
 template <typename T, int LANES>
-__global__ void __launch_bounds__(256) residual_short_kernel(const T* __restrict__ z, long long ldz, const int* __restrict__ y,
+__global__ void __launch_bounds__(256, 6) residual_short_kernel(const T* __restrict__ z, long long ldz, const int* __restrict__ y,
                                                              T* __restrict__ out, long long ldo, float* __restrict__ loss,
                                                              long long rows, int C, float scale) {
     const int lane = threadIdx.x & (LANES - 1);
@@ -114,13 +114,100 @@ __device__ __forceinline__ uint32_t residual_rank() {
     return r;
 }
 
-template <typename T, int TH, int NV>
-__global__ void __launch_bounds__(TH == 32 ? 256 : TH) residual_row_kernel(const T* __restrict__ z, long long ldz, const int* __restrict__ y,
-                                                                           T* __restrict__ out, long long ldo, float* __restrict__ loss,
-                                                                           long long rows, int C, float scale, int R) {
+// Two fp32 operations in one instruction: the exponentials' arithmetic is what competes with memory in the 16-bit types.
+struct Pair {
+    unsigned long long v;
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ float2 both() const {
+        float2 r;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+        return r;
+    }
+};
+__device__ __forceinline__ Pair operator+(Pair a, const Pair& b) { asm("add.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v)); return a; }
+__device__ __forceinline__ Pair operator*(Pair a, const Pair& b) { asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v)); return a; }
+// the exponentials of a piece against a maximum, two at a time: exp_fast(x - m)
+template <typename T, typename F>
+__device__ __forceinline__ void piece_powers(const uint4& w, const Pair& minus_m, const Pair& log2e, F&& take) {
     constexpr int VE = Piece<T>::kValues;
-    __shared__ MaxSum part[TH / 32];
-    __shared__ MaxSum total;
+    float x[VE];
+    unpack_piece<T>(w, x);
+#pragma unroll
+    for (int e = 0; e < VE; e += 2) {
+        float2 p = ((Pair(x[e], x[e + 1]) + minus_m) * log2e).both();
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p.x));
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p.y));
+        take(e, Pair(p.x, p.y));
+    }
+}
+template <typename T> __device__ __forceinline__ void put_pair(T* t, const Pair& p);
+template <> __device__ __forceinline__ void put_pair<float>(float* t, const Pair& p) { const float2 x = p.both(); t[0] = x.x; t[1] = x.y; }
+template <> __device__ __forceinline__ void put_pair<__nv_bfloat16>(__nv_bfloat16* t, const Pair& p) {
+    *reinterpret_cast<__nv_bfloat162*>(t) = __float22bfloat162_rn(p.both());
+}
+template <> __device__ __forceinline__ void put_pair<__half>(__half* t, const Pair& p) { *reinterpret_cast<__half2*>(t) = __float22half2_rn(p.both()); }
+
+// largest of a piece's values and `top`, NaN left aside
+__device__ __forceinline__ float piece_max(float top, const uint4& w, float) {
+    float x[4];
+    unpack_piece<float>(w, x);
+    return fmaxf(fmaxf(top, fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
+}
+__device__ __forceinline__ float piece_max(float top, const uint4& w, __nv_bfloat16) {
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&w);
+    const float2 m = __bfloat1622float2(__hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+    return fmaxf(top, fmaxf(m.x, m.y));
+}
+__device__ __forceinline__ float piece_max(float top, const uint4& w, __half) {
+    const __half2* p = reinterpret_cast<const __half2*>(&w);
+    const float2 m = __half22float2(__hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+    return fmaxf(top, fmaxf(m.x, m.y));
+}
+// A value joined over the threads of a block and the R blocks of its cluster, in a fixed order; `cells` is this use's own.
+template <int TH, bool MAX>
+__device__ __forceinline__ float row_join(float v, float* cells, int tid, int R) {
+    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    if constexpr (TH > 32) {
+        if ((tid & 31) == 0) cells[tid >> 5] = v;
+        __syncthreads();
+        v = cells[0];
+#pragma unroll
+        for (int k = 1; k < TH / 32; ++k) v = op(v, cells[k]);
+        if (R > 1) {
+            float* mine = cells + TH / 32;
+            if (tid == 0) *mine = v;
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(mine);
+            float b[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                if (c >= R) break;
+                uint32_t p;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(at), "r"(c));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(b[c]) : "r"(p) : "memory");
+            }
+            v = b[0];
+#pragma unroll
+            for (int c = 1; c < 8; ++c) {
+                if (c >= R) break;
+                v = op(v, b[c]);
+            }
+        }
+    }
+    return v;
+}
+
+// Two of these blocks' worth of registers fit an SM at least; the pieces are unpacked anew in each of the three passes over
+// them (the compiler would rather keep twice as many registers of unpacked values, and one block to an SM: 706 us
+// instead of 443 at 8191 x 50257 in bf16).
+template <typename T, int TH, int NV>
+__global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? (NV <= 2 ? 6 : 4) : 1024 / TH) residual_row_kernel(
+    const T* __restrict__ z, long long ldz, const int* __restrict__ y, T* __restrict__ out, long long ldo, float* __restrict__ loss,
+    long long rows, int C, float scale, int R) {
+    constexpr int VE = Piece<T>::kValues;
+    __shared__ float cells[2][TH / 32 + 1];
     const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
     const int rank = R > 1 ? (int)residual_rank() : 0;
     const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x / R;
@@ -141,129 +228,142 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) residual_row_kernel(const
     const int at = tid < head ? tid : tid + pieces * VE;
     const float edge = odd ? to_f32(zi[at]) : -INFINITY;
 
-    MaxSum a{edge, 0.f};
+    float top = fmaxf(edge, -INFINITY);  // (NaN left aside)
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-        if (tid + k * TH < count) {
-            float x[VE];
-            unpack_piece<T>(w[k], x);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) a.m = fmaxf(a.m, x[e]);
-        }
-    if (isnan(a.m)) a.m = -INFINITY;  // (the odd logit is NaN and there is no other)
-    a.s = exp_fast(edge - against(a.m));
+        if (tid + k * TH < count) top = piece_max(top, w[k], T());
+    top = row_join<TH, true>(top, cells[0], tid, R);
+    // (the difference by itself, not folded into a multiply-add: it is exact next to the largest logit, so that a row with one
+    // class left has probability one and no gradient, and it cannot overflow)
+    const float m = against(top);
+    auto power = [&](float x) { return exp_fast(x - m); };
+    const Pair minus_m(-m, -m), log2e(kLog2e, kLog2e);
+    Pair sums(power(edge), 0.f);  // (-inf gives zero)
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-        if (tid + k * TH < count) {
-            float x[VE];
-            unpack_piece<T>(w[k], x);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) a.s += exp_fast(x[e] - against(a.m));
-        }
-    a = join_lanes(a, 32);
-    if constexpr (TH > 32) {
-        if ((tid & 31) == 0) part[tid >> 5] = a;
-        __syncthreads();
-        a = part[0];
-        for (int k = 1; k < TH / 32; ++k) a = join(a, part[k]);
-        if (R > 1) {  // the row's other blocks, in their order
-            if (tid == 0) total = a;
-            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-            const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&total);
-            MaxSum b[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                if (c >= R) break;
-                uint32_t p;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(mine), "r"(c));
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(b[c].m), "=f"(b[c].s) : "r"(p) : "memory");
-            }
-            a = b[0];
-#pragma unroll
-            for (int c = 1; c < 8; ++c) {
-                if (c >= R) break;
-                a = join(a, b[c]);
-            }
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (waited for at the end)
-        }
-    }
-    const bool counts = row_counts(a, label, C);
-    const float m = against(a.m), factor = counts ? scale / a.s : 0.f, minus = counts ? scale : 0.f;
-    const int in_pieces = label - head;  // the label's place among the pieces
+        if (tid + k * TH < count) piece_powers<T>(w[k], minus_m, log2e, [&](int, const Pair& p) { sums = sums + p; });
+    const float sum = row_join<TH, false>(sums.both().x + sums.both().y, cells[1], tid, R);
+    if (TH > 32 && R > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this block has read the others' cells
+    const bool counts = row_counts(MaxSum{top, sum}, label, C);
+    const float factor = scale / sum;
     const bool same = (((uintptr_t)zi ^ (uintptr_t)oi) & 15u) == 0;
     T* dst = oi + head + (long long)begin * VE;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (tid + k * TH < count) {
-            float x[VE];
-            unpack_piece<T>(w[k], x);
-            const int v = tid + k * TH, first = (begin + v) * VE;
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                float r = exp_fast(x[e] - m) * factor;
-                if (!counts) r = 0.f;
-                x[e] = first + e == in_pieces ? r - minus : r;
-            }
+            const int v = tid + k * TH;
+            uint4 q = make_uint4(0, 0, 0, 0);
+            T* t = reinterpret_cast<T*>(&q);
+            if (counts) piece_powers<T>(w[k], minus_m, log2e, [&](int e, const Pair& p) { put_pair<T>(t + e, p * Pair(factor, factor)); });
             if (same) {
-                uint4 q;
-                T* t = reinterpret_cast<T*>(&q);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) t[e] = from_f32<T>(x[e]);
                 __stcs(reinterpret_cast<uint4*>(dst) + v, q);
             } else {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) dst[(long long)v * VE + e] = from_f32<T>(x[e]);
+                for (int e = 0; e < VE; ++e) dst[(long long)v * VE + e] = t[e];
             }
         }
-    if (odd) {
-        float r = counts ? exp_fast(edge - m) * factor : 0.f;
-        if (at == label) r -= minus;
-        oi[at] = from_f32<T>(r);
+    if (odd) oi[at] = from_f32<T>(counts ? power(edge) * factor : 0.f);
+    // the label's own value is put right by the thread that has just written it
+    const int piece = (label - head) / VE - begin;
+    const bool mine = label >= head && label < head + pieces * VE ? piece >= 0 && piece < count && piece % TH == tid : odd && at == label;
+    if (counts && mine) {
+        const float x = to_f32(zi[label]);
+        oi[label] = from_f32<T>(power(x) * factor - scale);
+        if (loss) loss[i] = logf(sum) + (m - x);
     }
-    if (rank == 0 && tid == 0 && loss) loss[i] = counts ? row_loss(a, to_f32(zi[label])) : 0.f;
+    if (!counts && rank == 0 && tid == 0 && loss) loss[i] = 0.f;
     if (TH > 32 && R > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// ---- rows too long for that: a block per row, the row read twice (the second time mostly from L2)
-template <typename T>
-__global__ void __launch_bounds__(1024) residual_long_kernel(const T* __restrict__ z, long long ldz, const int* __restrict__ y,
-                                                             T* __restrict__ out, long long ldo, float* __restrict__ loss,
-                                                             long long rows, int C, float scale) {
-    __shared__ MaxSum part[32];
+// ---- longer rows than a block's registers hold: a block per row, the row read twice.  The second time it comes from L2, so that
+// memory sees one read and one write, as long as the rows under way fit there: 1024 / TH blocks to an SM, TH growing
+// with the row.  Measured: 8191 x 50257 in bf16 (100 KB a row) with 256 threads 326 us (5.05 TB/s), with 512 threads 370,
+// held in the registers of clusters of two blocks 443; 4096 x 50257 in fp32 (200 KB) 356 with 256 threads, 295 with 512.
+template <typename T, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) residual_long_kernel(const T* __restrict__ z, long long ldz, const int* __restrict__ y,
+                                                                        T* __restrict__ out, long long ldo, float* __restrict__ loss,
+                                                                        long long rows, int C, float scale) {
+    constexpr int VE = Piece<T>::kValues, kAhead = 4;  // pieces a thread has under way
+    __shared__ MaxSum part[TH / 32];
+    const Pair log2e(kLog2e, kLog2e);
+    const int tid = threadIdx.x;
     for (long long i = blockIdx.x; i < rows; i += gridDim.x) {
         const T* zi = z + i * ldz;
         T* oi = out + i * ldo;
-        MaxSum a{-INFINITY, 0.f};
-        for (int c0 = threadIdx.x; c0 < C; c0 += 8 * 1024) {
-            float x[8], top = -INFINITY;
+        const int head = min(C, (int)(((16u - ((uintptr_t)zi & 15u)) & 15u) / sizeof(T)));
+        const int pieces = (C - head) / VE, edges = C - pieces * VE;
+        const uint4* src = reinterpret_cast<const uint4*>(zi + head);
+        const bool odd = tid < edges;
+        const int at = tid < head ? tid : tid + pieces * VE;
+        const float edge = odd ? to_f32(zi[at]) : -INFINITY;
+        MaxSum a{fmaxf(edge, -INFINITY), 0.f};
+        a.s = exp_fast(edge - against(a.m));
+        uint4 w[kAhead], next[kAhead];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[k] = c0 + k * 1024 < C ? to_f32(zi[c0 + k * 1024]) : -INFINITY;
-                top = fmaxf(top, x[k]);
+        for (int k = 0; k < kAhead; ++k)
+            if (tid + k * TH < pieces) next[k] = src[tid + k * TH];
+        for (int k0 = tid; k0 < pieces; k0 += kAhead * TH) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                w[k] = next[k];
+                if (k0 + (kAhead + k) * TH < pieces) next[k] = src[k0 + (kAhead + k) * TH];
             }
-            MaxSum b{top, 0.f};
+            float top = a.m;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) b.s += exp_fast(x[k] - against(top));
-            a = join(a, b);
+            for (int k = 0; k < kAhead; ++k)
+                if (k0 + k * TH < pieces) top = piece_max(top, w[k], T());
+            const float m = against(top);
+            Pair sums(a.s * exp_fast(against(a.m) - m), 0.f);
+            a.m = top;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (k0 + k * TH < pieces) piece_powers<T>(w[k], Pair(-m, -m), log2e, [&](int, const Pair& p) { sums = sums + p; });
+            a.s = sums.both().x + sums.both().y;
         }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)  // the second reading begins while the sums are joined
+            if (tid + k * TH < pieces) next[k] = __ldcs(src + tid + k * TH);
         a = join_lanes(a, 32);
         __syncthreads();  // the row before this one has read its sums
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
+        if ((tid & 31) == 0) part[tid >> 5] = a;
         __syncthreads();
         a = part[0];
-        for (int w = 1; w < 32; ++w) a = join(a, part[w]);
+#pragma unroll
+        for (int k = 1; k < TH / 32; ++k) a = join(a, part[k]);
         const int label = y[i];
-        const bool counts = row_counts(a, label, C);
+        const bool counts = row_counts(a, label, C), same = (((uintptr_t)zi ^ (uintptr_t)oi) & 15u) == 0;
         const float m = against(a.m), factor = scale / a.s;
-        for (int c = threadIdx.x; c < C; c += 1024) {
-            float r = 0.f;
-            if (counts) {
-                r = exp_fast(to_f32(zi[c]) - m) * factor;
-                if (c == label) r -= scale;
+        T* dst = oi + head;
+        for (int k0 = tid; k0 < pieces; k0 += kAhead * TH) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                w[k] = next[k];
+                if (k0 + (kAhead + k) * TH < pieces) next[k] = __ldcs(src + k0 + (kAhead + k) * TH);
             }
-            oi[c] = from_f32<T>(r);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (k0 + k * TH < pieces) {
+                    const int v = k0 + k * TH;
+                    uint4 q = make_uint4(0, 0, 0, 0);
+                    T* t = reinterpret_cast<T*>(&q);
+                    if (counts) piece_powers<T>(w[k], Pair(-m, -m), log2e, [&](int e, const Pair& p) { put_pair<T>(t + e, p * Pair(factor, factor)); });
+                    if (same) {
+                        __stcs(reinterpret_cast<uint4*>(dst) + v, q);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) dst[(long long)v * VE + e] = t[e];
+                    }
+                }
         }
-        if (threadIdx.x == 0 && loss) loss[i] = counts ? row_loss(a, to_f32(zi[label])) : 0.f;
+        if (odd) oi[at] = from_f32<T>(counts ? exp_fast(edge - m) * factor : 0.f);
+        // the label's own value is put right by the thread that has just written it
+        const int piece = (label - head) / VE;
+        if (counts && (label >= head && label < head + pieces * VE ? piece % TH == tid : odd && at == label)) {
+            const float x = to_f32(zi[label]);
+            oi[label] = from_f32<T>(exp_fast(x - m) * factor - scale);
+            if (loss) loss[i] = row_loss(a, x);
+        }
+        if (!counts && tid == 0 && loss) loss[i] = 0.f;
     }
 }
 

@@ -256,7 +256,7 @@ def check_residual(z, y, scale=None):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("rows,C", [(1, 1), (1, 2), (256, 10), (1000, 16), (7, 31), (65, 33), (3, 257), (130, 1000), (33, 1025), (5, 4097),
                                     (40, 10007), (2, 16391), (1, 40001), (9, 50257), (3, 131071),
-                                    (2, 270001)])
+                                    (2, 270001), (70, 35001), (3, 600011)])
 def test_residual(rows, C, dtype):
     gen = torch.Generator(device="cuda").manual_seed(rows * C)
     z = (torch.randn(rows, C, generator=gen, device="cuda") * 4).to(dtype)
