@@ -278,3 +278,31 @@ def test_another_stream():
     side.synchronize()
     for x, y in zip(job.params, twin.params):
         assert torch.equal(x, y)
+
+
+def test_refusals():
+    p, g = [torch.zeros(300, device="cuda")], [torch.zeros(300, device="cuda")]
+    s = ops.adamw_state(p)
+    s8 = ops.adamw_state(p, 8)
+    h = [p[0].half()]
+    calls = [
+        lambda: ops.adamw_step(p, [], lr=1.0, **s), lambda: ops.adamw_step(p, [g[0][:299]], lr=1.0, **s), lambda: ops.adamw_step(p, [g[0].double()], lr=1.0, **s),
+        lambda: ops.adamw_step(p, [g[0].cpu()], lr=1.0, **s), lambda: ops.adamw_step([torch.zeros(600, device="cuda")[::2]], g, lr=1.0, **s),
+        lambda: ops.adamw_step(p, g, s["m"], s8["v"], s["control"], 1.0), lambda: ops.adamw_step(p, g, s8["m"], s8["v"], s["control"], 1.0),
+        lambda: ops.adamw_step(p, g, s8["m"], s8["v"], s["control"], 1.0, m_scale=s8["m_scale"], v_scale=[s8["v_scale"][0][:1]]),
+        lambda: ops.adamw_step(p, g, s["m"], s["v"], s["control"][:3], 1.0), lambda: ops.adamw_step(p, g, s["m"], s["v"], s["control"].float(), 1.0),
+        lambda: ops.adamw_step(h, g, s["m"], s["v"], s["control"], 1.0), lambda: ops.adamw_step(h, g, s["m"], s["v"], s["control"], 1.0, masters=[None]),
+        lambda: ops.adamw_step(p, g, s["m"], s["v"], s["control"], 1.0, masters=[torch.zeros(300, device="cuda")]),
+        lambda: ops.adamw_step(p, g, s["m"], s["v"], s["control"], 1.0, weight_decay=[0.1, 0.1]),
+        lambda: ops.adamw_step(p, g, s["m"], s["v"], s["control"], 1.0, masters=[]),
+    ]
+    for k, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            raise AssertionError(f"call {k} was not refused")
+    from paper_2312_08728_b200.binding import BmgdError
+    for call in (lambda: ops.adamw_step(p, p, lr=1.0, **s), lambda: ops.adamw_step(p * 2, g * 2, s["m"] * 2, s["v"] * 2, s["control"], 1.0),
+                 lambda: ops.adamw_step(p, g, lr=math.nan, **s), lambda: ops.adamw_step(p, g, lr=1.0, a=1.0, **s), lambda: ops.adamw_step(p, g, lr=1.0, max_norm=-1.0, **s)):
+        with pytest.raises(BmgdError):
+            call()
+    assert s["control"].tolist() == [0, 0, 0, 0]

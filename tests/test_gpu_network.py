@@ -1,0 +1,108 @@
+"""The operators run together, as a training step uses them, and the model that does so."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2312_08728_b200 import operators as ops
+from paper_2312_08728_b200.network import GatedSoftmax
+from test_gpu_adamw import Job
+from test_gpu_operators import Block, check_residual
+
+pytestmark = pytest.mark.gpu
+
+
+def sample(N, p, C, dtype, seed=0):
+    """Classes around C centres: something to learn."""
+    gen = torch.Generator().manual_seed(seed)
+    centres = torch.randn(C, p, generator=gen)
+    y = torch.randint(0, C, (N,), generator=gen, dtype=torch.int32)
+    return (centres[y.long()] + 0.7 * torch.randn(N, p, generator=gen)).to(dtype), y
+
+
+@pytest.mark.parametrize("p,hidden,C,n,dtype,bits", [(24, 40, 5, 32, torch.bfloat16, 32), (33, 70, 10, 100, torch.float16, 32),
+                                                     (64, 128, 16, 256, torch.bfloat16, 8), (200, 301, 10, 300, torch.bfloat16, 32)])
+def test_steps_of_a_round_operator_by_operator(p, hidden, C, n, dtype, bits):
+    """Three mini-batches: the rows are those of the shuffle, and every operator's result is within its bound of the definition
+    on the inputs that it was given."""
+    x, y = sample(3 * n - 7, p, C, dtype)
+    x, y = x.cuda(), y.cuda()
+    net = GatedSoftmax(x.shape[0], p, 1, hidden, C, dtype=dtype, state_bits=bits, weight_decay=0.05, max_norm=0.7, seed=3)
+    pi = torch.from_numpy(oracle.perm(9, 0, 0, x.shape[0]).astype(np.int64)).cuda()
+    for k in range(3):
+        count = min(n, x.shape[0] - k * n)
+        bx, by = ops.gather_batch(x, y, 9, 0, 0, k * n, count)
+        rows = pi[k * n:k * n + count]
+        assert torch.equal(bx, x[rows]) and torch.equal(by, y[rows])
+        b = Block.__new__(Block)
+        b.x, (b.wg, b.wu, b.wd), b.act, b.dtype = bx, net.weights, net.activation, dtype
+        logits, saved = ops.gated_ffn(bx, *net.weights, net.activation, save=True)
+        residual, loss = check_residual(logits, by)
+        b.dy = residual
+        dx, *grads = ops.gated_ffn_backward(residual, bx, *net.weights, saved, net.activation)
+        b.check({"y": logits, "dx": dx, "dw_gate": grads[0], "dw_up": grads[1], "dw_down": grads[2]})
+        job = Job.__new__(Job)
+        job.params, job.masters, job.grads, job.state, job.bits, job.seed, job.t = net.weights, net.masters, grads, net.state, bits, 3, k
+        job.decays = [0.05] * 3
+        before = job.before()
+        norm = float(torch.sqrt(sum(g.double().square().sum() for g in grads)))
+        net_loss = net.step(bx, by, 1e-2)
+        assert torch.equal(net_loss, loss)
+        job.check(before, gscale=min(1.0, 0.7 / (norm + 1e-6)))
+    net.sync()
+
+
+def test_rounds_over_buffers_are_the_steps_in_a_row():
+    """run_rounds over two slots, a resident buffer and step by step: the same bits."""
+    p, hidden, C, n = 40, 64, 7, 48
+    x, y = sample(400, p, C, torch.bfloat16)
+    parts = [(x[:200].pin_memory(), y[:200].pin_memory()), (x[200:].pin_memory(), y[200:].pin_memory())]
+    nets = [GatedSoftmax(400, p, 2, hidden, C, seed=1) for _ in range(3)]
+    copy = torch.cuda.Stream()
+    slot = nets[0].load_buffer(*parts[0], stream=copy)
+    for k in range(4):  # two passes over two buffers
+        following = nets[0].load_buffer(*parts[(k + 1) % 2], stream=copy) if k < 3 else None
+        nets[0].run_rounds(slot, 2, n, 1e-2, seed=70 + k)
+        slot = following
+        dx, dy = (t.cuda() for t in parts[k % 2])
+        nets[1].run_rounds_resident(dx, dy, 2, n, 1e-2, seed=70 + k)
+        for t in range(2):
+            pi = torch.from_numpy(oracle.perm(70 + k, 0, t, 200).astype(np.int64)).cuda()
+            for first in range(0, 200, n):
+                nets[2].step(dx[pi[first:first + n]], dy[pi[first:first + n]], 1e-2)
+    nets[0].sync()
+    for a, b, c in zip(*(net.get_theta() for net in nets)):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_captured_into_a_graph(bits):
+    x, y = sample(128, 48, 6, torch.bfloat16)
+    x, y = x.cuda(), y.cuda()
+    nets = [GatedSoftmax(128, 48, 1, 96, 6, state_bits=bits, seed=2, max_norm=1.0) for _ in range(2)]
+    nets[0].step(x, y, 1e-2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss = nets[0].step(x, y, 1e-2)
+    for _ in range(4):
+        graph.replay()
+    for _ in range(5):
+        want = nets[1].step(x, y, 1e-2)
+    torch.cuda.synchronize()
+    assert torch.equal(loss, want)
+    for a, b in zip(nets[0].get_theta(), nets[1].get_theta()):
+        assert torch.equal(a, b)
+
+
+def test_refusals():
+    net = GatedSoftmax(100, 16, 2, 32, 4)
+    x, y = sample(50, 16, 4, torch.bfloat16)
+    with pytest.raises(Exception):
+        net.run_rounds(0, 1, 10, 1e-3, 0)               # nothing loaded
+    with pytest.raises(Exception):
+        net.load_buffer(torch.cat([x, x]), torch.cat([y, y]))  # more rows than a slot holds
+    for bad_x, bad_y in ((x.float(), y), (x[:, :8], y), (x, y.long()), (x, y[:10])):
+        with pytest.raises(ValueError):
+            net.load_buffer(bad_x, bad_y)
+    with pytest.raises(ValueError):
+        net.set_theta([torch.zeros(1)] * 3)

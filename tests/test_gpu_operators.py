@@ -308,3 +308,29 @@ def test_gather_batch_takes_the_rows_of_the_shuffle(p, dtype):
     bx, by = ops.gather_batch(x, None, 77, 2, 5, 1000, 13)
     assert by is None and torch.equal(bx, x[pi[1000:]])
     assert ops.gather_batch(x, y, 77, 2, 5, rows, 0)[0].shape == (0, p)
+
+
+# ---------------------------------------------------------------- refusals that need device tensors
+
+def test_refusals():
+    b = Block(6, 16, 24, 8, torch.bfloat16, ops.ACT_SILU)
+    w = [b.wg, b.wu, b.wd]
+    y, saved = ops.gated_ffn(b.x, *w, save=True)
+
+    def backward(dy=b.dy, saved=saved):
+        return ops.gated_ffn_backward(dy, b.x, *w, saved)
+    calls = [
+        lambda: ops.gated_ffn(b.x.float(), *w), lambda: ops.gated_ffn(b.x.half(), *w), lambda: ops.gated_ffn(b.x.cpu(), *w),
+        lambda: ops.gated_ffn(b.x[:, :8], *w), lambda: ops.gated_ffn(b.x, b.wg, b.wu[:, :16], b.wd), lambda: ops.gated_ffn(b.x, b.wg, b.wu, b.wd[:16]),
+        lambda: ops.gated_ffn(b.x.t().contiguous().t(), *w), lambda: ops.gated_ffn(b.x, *w, activation=9),
+        lambda: ops.gated_ffn(b.x, b.wg.cpu(), b.wu, b.wd), lambda: ops.gated_ffn(b.x[0], *w), lambda: ops.gated_ffn(b.x, b.wg[:, :0], b.wu[:, :0], b.wd[:0]),
+        lambda: backward(dy=b.dy[:, :4]), lambda: backward(dy=b.dy[:3]), lambda: backward(dy=b.dy.float()), lambda: backward(saved=y),
+        lambda: backward(saved=saved[:1]), lambda: backward(saved=(saved[0][:, :3], saved[1])), lambda: backward(saved=(saved[0], saved[1].half())),
+        lambda: ops.softmax_residual(y, torch.zeros(6, dtype=torch.int64, device="cuda")), lambda: ops.softmax_residual(y, torch.zeros(5, dtype=torch.int32, device="cuda")),
+        lambda: ops.softmax_residual(y, torch.zeros(6, dtype=torch.int32)), lambda: ops.softmax_residual(y.double(), torch.zeros(6, dtype=torch.int32, device="cuda")),
+        lambda: ops.gather_batch(b.x, None, 0, 0, 0, 3, 4), lambda: ops.gather_batch(b.x[:, :8], None, 0, 0, 0, 0, 1), lambda: ops.gather_batch(b.x, None, 0, 0, 0, -1, 1),
+    ]
+    for k, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            raise AssertionError(f"call {k} was not refused")
