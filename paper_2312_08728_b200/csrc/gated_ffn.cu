@@ -1,5 +1,6 @@
 // Host side of the gated feed-forward block: checks, tensor maps, choice of tile, launches.
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 #include <mutex>
 
@@ -12,12 +13,6 @@ using namespace bmgdk;
 
 // Set by a kernel whose wait ran out of time; read and cleared by bmgd_stream_check.
 __device__ int g_ffn_status[2];
-
-int* status_address() {
-    void* p = nullptr;
-    if (cudaGetSymbolAddress(&p, g_ffn_status) != cudaSuccess) { cudaGetLastError(); return nullptr; }
-    return static_cast<int*>(p);
-}
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -55,16 +50,44 @@ int make_map(const Matrix& m, int type, int box_rows, CUtensorMap* out) {
     return r == CUDA_SUCCESS ? BMGD_OK : BMGD_ERR_CUDA;
 }
 
+// What a launch needs to know of the current device.  Looked up once per device: a call of a small block takes less time on
+// the GPU than these queries take on the host.
+constexpr int kMaxDevices = 64;
 struct Device {
-    int sms, smem;
+    int index, sms, smem;
+    int* status;
 };
 int current_device(Device* d) {
+    static Device known[kMaxDevices];
+    static std::atomic<bool> ready[kMaxDevices];
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&d->smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess) {
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    if (dev >= 0 && dev < kMaxDevices && ready[dev].load(std::memory_order_acquire)) { *d = known[dev]; return BMGD_OK; }
+    void* p = nullptr;
+    d->index = dev;
+    if (cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&d->smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess ||
+        cudaGetSymbolAddress(&p, g_ffn_status) != cudaSuccess) {
         cudaGetLastError();
         return BMGD_ERR_CUDA;
     }
+    d->status = static_cast<int*>(p);
+    static std::mutex one;
+    std::lock_guard<std::mutex> hold(one);
+    if (dev >= 0 && dev < kMaxDevices && !ready[dev].load(std::memory_order_relaxed)) {
+        known[dev] = *d;
+        ready[dev].store(true, std::memory_order_release);
+    }
+    return BMGD_OK;
+}
+// A kernel's dynamic shared memory, allowed once per device; `done` holds a bit per device and belongs to the kernel.
+template <typename K>
+int allow_smem(K* fn, int bytes, const Device& dev, std::atomic<unsigned long long>& done) {
+    const unsigned long long bit = 1ull << (dev.index & 63);
+    if (done.load(std::memory_order_relaxed) & bit) return BMGD_OK;
+    if (bytes > dev.smem) return BMGD_ERR_LAUNCH;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    if (dev.index < kMaxDevices) done.fetch_or(bit, std::memory_order_relaxed);
     return BMGD_OK;
 }
 
@@ -115,9 +138,10 @@ int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, 
     }
     P.problems = count;
     P.tiles = tiles;
-    if (S::kSmem > dev.smem) return BMGD_ERR_LAUNCH;
     auto* fn = ffn_kernel<CG, BN, EPI, A_MN, B_MN>;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    static std::atomic<unsigned long long> allowed{0};
+    const int rc = allow_smem(fn, S::kSmem, dev, allowed);
+    if (rc != BMGD_OK) return rc;
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
     launch_config(&lc, at, dim3((unsigned)std::min<int64_t>(tiles, dev.sms / CG) * CG), FfnReadOut<EPI>::kThreads, S::kSmem, CG, s);
@@ -141,9 +165,10 @@ int launch_few(FfnParams& P, const Problem& x, int split, bool early, const Devi
     q.a_mn = W_MN; q.vec = x.vec;
     q.tiles_m = (int)((x.M + NR - 1) / NR);
     q.tiles_n = (x.N + kFewPart - 1) / kFewPart;
-    if (F::kSmem > dev.smem) return BMGD_ERR_LAUNCH;
     auto* fn = ffn_few_kernel<NR, EPI>;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    static std::atomic<unsigned long long> allowed{0};
+    const int rc = allow_smem(fn, F::kSmem, dev, allowed);
+    if (rc != BMGD_OK) return rc;
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
     launch_config(&lc, at, dim3((unsigned)(q.tiles_m * q.tiles_n * split)), kFewThreads, F::kSmem, split, s);
@@ -275,7 +300,7 @@ constexpr unsigned long long kTimeoutNs = 2000000000ull;  // bound on any single
 bool wide(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
 // run = false: only counts the workspace
-int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, int* status, cudaStream_t s) {
+int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, cudaStream_t s) {
     Matrix x{g->x, g->rows, g->inputs, g->ld_x}, wg{g->w_gate, g->inputs, g->hidden, g->ld_gate},
         wu{g->w_up, g->inputs, g->hidden, g->ld_up}, wd{g->w_down, g->hidden, g->outputs, g->ld_down};
     Matrix* const operands[4] = {&x, &wg, &wu, &wd};
@@ -285,7 +310,7 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     void* h = g->saved_hidden ? g->saved_hidden : space->take(g->rows * ldh * 2);
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = kTimeoutNs;
+    P.type = g->type; P.act = g->activation; P.status = dev.status; P.timeout_ns = kTimeoutNs;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     const Problem gated{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true};
     rc = contract<kEpiGated, true>(P, gated, false, dev, s);
@@ -295,7 +320,7 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     return contract<kEpiPlain, true>(P, down, true, dev, s);
 }
 
-int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, int* status, cudaStream_t s) {
+int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, cudaStream_t s) {
     Matrix x{g->x, g->rows, g->inputs, g->ld_x}, wg{g->w_gate, g->inputs, g->hidden, g->ld_gate},
         wu{g->w_up, g->inputs, g->hidden, g->ld_up}, wd{g->w_down, g->hidden, g->outputs, g->ld_down},
         dy{g->dy, g->rows, g->outputs, g->ld_dy};
@@ -306,7 +331,7 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     const Matrix h{g->saved_hidden, n, g->hidden, g->ld_saved}, dg{space->take(n * ldh * 2), n, g->hidden, ldh}, du{space->take(n * ldh * 2), n, g->hidden, ldh};
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = status; P.timeout_ns = kTimeoutNs;
+    P.type = g->type; P.act = g->activation; P.status = dev.status; P.timeout_ns = kTimeoutNs;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     P.out_up = const_cast<void*>(du.base);
     // dH, and from it dG and dU
@@ -337,16 +362,14 @@ int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspa
     }
     Device dev{};
     Space need{nullptr, 0};
-    rc = pass == BMGD_FFN_FORWARD ? forward(g, &need, false, dev, nullptr, s) : backward(g, &need, false, dev, nullptr, s);
+    rc = pass == BMGD_FFN_FORWARD ? forward(g, &need, false, dev, s) : backward(g, &need, false, dev, s);
     if (rc != BMGD_OK) return rc;
     if (!workspace || (uintptr_t)workspace % 256 != 0) return BMGD_ERR_ARG;
     if (workspace_bytes < need.used) return BMGD_ERR_CAPACITY;
     rc = current_device(&dev);
     if (rc != BMGD_OK) return rc;
-    int* status = status_address();
-    if (!status) return BMGD_ERR_CUDA;
     Space space{static_cast<unsigned char*>(workspace), 0};
-    return pass == BMGD_FFN_FORWARD ? forward(g, &space, true, dev, status, s) : backward(g, &space, true, dev, status, s);
+    return pass == BMGD_FFN_FORWARD ? forward(g, &space, true, dev, s) : backward(g, &space, true, dev, s);
 }
 
 }  // namespace
@@ -359,7 +382,7 @@ int bmgd_gated_ffn_workspace_bytes(const bmgd_gated_ffn* g, int32_t pass, int64_
     if (rc != BMGD_OK) return rc;
     Device dev{};
     Space need{nullptr, 0};
-    const int r = pass == BMGD_FFN_FORWARD ? forward(g, &need, false, dev, nullptr, nullptr) : backward(g, &need, false, dev, nullptr, nullptr);
+    const int r = pass == BMGD_FFN_FORWARD ? forward(g, &need, false, dev, nullptr) : backward(g, &need, false, dev, nullptr);
     *bytes = std::max<int64_t>(need.used, 256);
     return r;
 }

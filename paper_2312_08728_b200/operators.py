@@ -118,9 +118,10 @@ def _ffn_args(x, w_gate, w_up, w_down, activation):
             ld_x, ld_gate, ld_up, ld_down), (n, d, f, c), device
 
 
-def _saved_args(factors: torch.Tensor, hidden: torch.Tensor):
-    p, ld = factors.data_ptr(), hidden.shape[1]
-    return p, p + hidden.shape[0] * ld * 4, hidden.data_ptr(), ld
+def _saved_args(saved: torch.Tensor, n: int, width: int):
+    """Where the three parts of `saved` stand: act(X Wg) and (X Wu) * act'(X Wg) in fp32, their rows' product in 16 bits."""
+    p = saved.data_ptr()
+    return p, p + n * width * 4, p + n * width * 8, width
 
 
 def _run_ffn(which: int, args: bytes, device: torch.device) -> None:
@@ -143,19 +144,19 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     being what gated_ffn_backward needs beside its other arguments."""
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
     with _place(device, stream):
-        y = torch.empty(n, c, dtype=x.dtype, device=device)
+        y = x.new_empty((n, c))
         saved, kept = None, (0, 0, 0, 0)
         if save:
             width = (f + 7) // 8 * 8
-            saved = (torch.empty(2, n, width, dtype=torch.float32, device=device), torch.empty(n, width, dtype=x.dtype, device=device))
-            kept = _saved_args(*saved)
+            saved = x.new_empty((n, 5 * width))
+            kept = _saved_args(saved, n, width)
         if n > 0:
             _run_ffn(_FORWARD, _GATED_FFN.pack(*shared, y.data_ptr(), c, *kept, 0, 0, 0, 0, 0, 0), device)
     return (y, saved) if save else y
 
 
 def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
-                       saved: Tuple[torch.Tensor, torch.Tensor], activation: int = ACT_SILU,
+                       saved: torch.Tensor, activation: int = ACT_SILU,
                        stream: Optional[torch.cuda.Stream] = None):
     """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the gradient dy of its output.
 
@@ -163,14 +164,11 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
     _, _, ld_dy = _matrix(dy, "dy", n, c, x.dtype, device)
     width = (f + 7) // 8 * 8
-    if not isinstance(saved, tuple) or len(saved) != 2:
+    if saved.shape != (n, 5 * width) or saved.dtype is not x.dtype or saved.device != device or not saved.is_contiguous():
         raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
-    for t, shape, dtype in zip(saved, ((2, n, width), (n, width)), (torch.float32, x.dtype)):
-        if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-            raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
     with _place(device, stream):
-        dx, dw_gate, dw_up, dw_down = [torch.empty(s, dtype=x.dtype, device=device) for s in ((n, d), (d, f), (d, f), (f, c))]
-        _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(*saved), dy.data_ptr(), ld_dy, dx.data_ptr(), dw_gate.data_ptr(),
+        dx, dw_gate, dw_up, dw_down = x.new_empty((n, d)), x.new_empty((d, f)), x.new_empty((d, f)), x.new_empty((f, c))
+        _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(saved, n, width), dy.data_ptr(), ld_dy, dx.data_ptr(), dw_gate.data_ptr(),
                                             dw_up.data_ptr(), dw_down.data_ptr()), device)
     return dx, dw_gate, dw_up, dw_down
 
@@ -198,7 +196,7 @@ def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[floa
         raise ValueError(f"y must be a contiguous int32 [{rows}] on {device}")
     L = _binding.load_library()
     with _place(device, stream):
-        residual = torch.empty(rows, C, dtype=logits.dtype, device=device)
+        residual = logits.new_empty((rows, C))
         loss = torch.empty(rows, dtype=torch.float32, device=device)
         if rows > 0:
             _status(L.bmgd_softmax_residual(logits.data_ptr(), ld, y.data_ptr(), rows, C, _TYPES[logits.dtype],

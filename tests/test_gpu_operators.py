@@ -325,7 +325,7 @@ def test_refusals():
         lambda: ops.gated_ffn(b.x.t().contiguous().t(), *w), lambda: ops.gated_ffn(b.x, *w, activation=9),
         lambda: ops.gated_ffn(b.x, b.wg.cpu(), b.wu, b.wd), lambda: ops.gated_ffn(b.x[0], *w), lambda: ops.gated_ffn(b.x, b.wg[:, :0], b.wu[:, :0], b.wd[:0]),
         lambda: backward(dy=b.dy[:, :4]), lambda: backward(dy=b.dy[:3]), lambda: backward(dy=b.dy.float()), lambda: backward(saved=y),
-        lambda: backward(saved=saved[:1]), lambda: backward(saved=(saved[0][:, :3], saved[1])), lambda: backward(saved=(saved[0], saved[1].half())),
+        lambda: backward(saved=saved[:5]), lambda: backward(saved=saved[:, :24]), lambda: backward(saved=saved.half()), lambda: backward(saved=saved.cpu()),
         lambda: ops.softmax_residual(y, torch.zeros(6, dtype=torch.int64, device="cuda")), lambda: ops.softmax_residual(y, torch.zeros(5, dtype=torch.int32, device="cuda")),
         lambda: ops.softmax_residual(y, torch.zeros(6, dtype=torch.int32)), lambda: ops.softmax_residual(y.double(), torch.zeros(6, dtype=torch.int32, device="cuda")),
         lambda: ops.gather_batch(b.x, None, 0, 0, 0, 3, 4), lambda: ops.gather_batch(b.x[:, :8], None, 0, 0, 0, 0, 1), lambda: ops.gather_batch(b.x, None, 0, 0, 0, -1, 1),
