@@ -91,6 +91,9 @@ int allow_smem(K* fn, int bytes, const Device& dev, std::atomic<unsigned long lo
     return BMGD_OK;
 }
 
+// Bound on any single wait inside a kernel: two seconds, and more than a step of the contraction ever takes for each step.
+unsigned long long wait_bound(int64_t steps) { return 2000000000ull + 10000ull * (unsigned long long)steps; }
+
 // One contraction as the host describes it: out [M][N] = sum over segments of a[s] b[s].
 struct Problem {
     Matrix a[2], b[2];
@@ -118,10 +121,11 @@ template <int CG, int BN, int EPI, bool A_MN, bool B_MN>
 int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
     using S = FfnShape<CG, BN, EPI>;
     constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;
-    int64_t tiles = 0;
+    int64_t tiles = 0, steps = 0;
     for (int k = 0; k < count; ++k) {
         const Problem& x = problems[k];
         FfnProblem& q = P.p[k];
+        steps = std::max(steps, (int64_t)x.segments * x.K / kFfnBK);
         for (int i = 0; i < 2; ++i) {
             int rc = BMGD_OK;
             if (i < x.segments) rc = make_map(x.a[i], P.type, A_MN ? 64 : 128, &q.a[i]);
@@ -138,6 +142,7 @@ int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, 
     }
     P.problems = count;
     P.tiles = tiles;
+    P.timeout_ns = wait_bound(steps);
     auto* fn = ffn_kernel<CG, BN, EPI, A_MN, B_MN>;
     static std::atomic<unsigned long long> allowed{0};
     const int rc = allow_smem(fn, S::kSmem, dev, allowed);
@@ -165,6 +170,7 @@ int launch_few(FfnParams& P, const Problem& x, int split, bool early, const Devi
     q.a_mn = W_MN; q.vec = x.vec;
     q.tiles_m = (int)((x.M + NR - 1) / NR);
     q.tiles_n = (x.N + kFewPart - 1) / kFewPart;
+    P.timeout_ns = wait_bound((int64_t)x.segments * x.K / kFfnBK);
     auto* fn = ffn_few_kernel<NR, EPI>;
     static std::atomic<unsigned long long> allowed{0};
     const int rc = allow_smem(fn, F::kSmem, dev, allowed);
@@ -295,8 +301,6 @@ int check(const bmgd_gated_ffn* g, int pass, bool pointers) {
     return BMGD_OK;
 }
 
-constexpr unsigned long long kTimeoutNs = 2000000000ull;  // bound on any single wait inside a kernel
-
 bool wide(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
 // run = false: only counts the workspace
@@ -310,7 +314,7 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     void* h = g->saved_hidden ? g->saved_hidden : space->take(g->rows * ldh * 2);
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = dev.status; P.timeout_ns = kTimeoutNs;
+    P.type = g->type; P.act = g->activation; P.status = dev.status;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     const Problem gated{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true};
     rc = contract<kEpiGated, true>(P, gated, false, dev, s);
@@ -331,7 +335,7 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     const Matrix h{g->saved_hidden, n, g->hidden, g->ld_saved}, dg{space->take(n * ldh * 2), n, g->hidden, ldh}, du{space->take(n * ldh * 2), n, g->hidden, ldh};
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = dev.status; P.timeout_ns = kTimeoutNs;
+    P.type = g->type; P.act = g->activation; P.status = dev.status;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     P.out_up = const_cast<void*>(du.base);
     // dH, and from it dG and dU

@@ -213,6 +213,24 @@ def test_gated_block_captured_and_on_another_stream(rows):
     ops.stream_check()
 
 
+def test_gated_block_calls_at_once():
+    """Calls of different forms under way on three streams at the same time give what they give alone."""
+    jobs = [Block(*shape, torch.bfloat16, ops.ACT_SILU, seed=i) for i, shape in
+            enumerate([(3, 512, 1376, 512), (700, 256, 1024, 256), (100, 1024, 2048, 40)])]
+    alone = [b.run() for b in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        together = []
+        for b, s in zip(jobs, streams):
+            together.append(b.run(stream=s))
+    torch.cuda.synchronize()
+    for one, other in zip(alone, together):
+        for k in one:
+            assert torch.equal(one[k], other[k]), k
+    ops.stream_check()
+
+
 # ---------------------------------------------------------------- softmax residual
 
 def residual_reference(z, y, scale):
@@ -256,7 +274,8 @@ def check_residual(z, y, scale=None):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("rows,C", [(1, 1), (1, 2), (256, 10), (1000, 16), (7, 31), (65, 33), (3, 257), (130, 1000), (33, 1025), (5, 4097),
                                     (40, 10007), (2, 16391), (1, 40001), (9, 50257), (3, 131071),
-                                    (2, 270001), (70, 35001), (3, 600011)])
+                                    (2, 270001), (70, 35001), (3, 600011),
+                                    (700, 32771), (400, 36865), (333, 53249)])
 def test_residual(rows, C, dtype):
     gen = torch.Generator(device="cuda").manual_seed(rows * C)
     z = (torch.randn(rows, C, generator=gen, device="cuda") * 4).to(dtype)
