@@ -115,7 +115,7 @@ def peak_hbm():
 
 
 # sources of the operators on device tensors: none of the measured step kernels is made from them
-OPERATOR_SOURCES = {"adamw.cu", "adamw_kernel.cuh", "ffn_kernel.cuh", "gated_ffn.cu", "residual.cu", "residual_kernel.cuh"}
+OPERATOR_SOURCES = {"adamw.cu", "adamw_kernel.cuh", "ffn_kernel.cuh", "gated_ffn.cu", "pair.cuh", "residual.cu", "residual_kernel.cuh"}
 
 
 def kernel_source_hash():

@@ -365,7 +365,7 @@ typedef struct bmgd_adamw_tensor {
     int32_t param_type, grad_type, state_bits, index; /* state_bits 32 or 8; index: part of the key of the random rounding */
 } bmgd_adamw_tensor;
 typedef struct bmgd_adamw_config {
-    double lr, a, b, eps, grad_scale, max_norm;
+    double lr, a, b, eps, grad_scale, max_norm;  /* eps below 2^-63 counts as 2^-63 */
     uint64_t seed;           /* of the random rounding (moments in 8 bits, BF16 without a copy) */
 } bmgd_adamw_config;
 /* Four 64-bit words of device memory, zero at first, that belong to one set of tensors: updates taken, updates left

@@ -122,12 +122,13 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return BMGD_ERR_CUDA;
-    const int blocks = std::min(kAdamwMaxBlocks, sms * 3), sum_blocks = std::min(kAdamwMaxBlocks, sms * 6);  // what fits an SM
+    // as many blocks as fit an SM: of the sum of squares, and of the update of moments in 32 and in 8 bits
+    const int sum_blocks = std::min(kAdamwMaxBlocks, sms * 6), blocks = std::min(kAdamwMaxBlocks, sms * 3), blocks8 = std::min(kAdamwMaxBlocks, sms * 4);
     const bool clip = cfg->max_norm > 0.0;
     AdamwHead h{};
     h.control = static_cast<long long*>(dev_control);
     h.lr = cfg->lr; h.a = cfg->a; h.b = cfg->b; h.grad_scale = cfg->grad_scale; h.max_norm = cfg->max_norm;
-    h.eps = (float)cfg->eps;
+    h.eps = std::max((float)cfg->eps, 0x1p-63f);
     h.seed_lo = (uint32_t)cfg->seed; h.seed_hi = (uint32_t)(cfg->seed >> 32);
     // a warp takes up to four units of a tensor in a row, fewer where that would leave SMs without work
     const int64_t per_unit = (int64_t)blocks * (kAdamwThreads / 32) * kAdamwUnit;
@@ -138,8 +139,8 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
     double* partial = static_cast<double*>(dev_scratch);
     auto part = [&](int l, int bits, double* sums) {
         const int32_t first = l * kLargeTable, some = std::min(count - first, kLargeTable);
-        return small ? launch<kSmallTable>(tensors + first, some, h, bits, bits ? blocks : sum_blocks, sums, s)
-                     : launch<kLargeTable>(tensors + first, some, h, bits, bits ? blocks : sum_blocks, sums, s);
+        return small ? launch<kSmallTable>(tensors + first, some, h, bits, bits == 0 ? sum_blocks : bits == 8 ? blocks8 : blocks, sums, s)
+                     : launch<kLargeTable>(tensors + first, some, h, bits, bits == 0 ? sum_blocks : bits == 8 ? blocks8 : blocks, sums, s);
     };
     if (clip) {
         if (!partial || (uintptr_t)partial % 8 != 0) return BMGD_ERR_ARG;

@@ -6,7 +6,8 @@
 // Every product and sum is rounded to fp32 by itself (no contraction), so the moments do not depend on how the compiler
 // schedules them, and their codes can be checked bit for bit.
 //
-// What bounds it: memory.  Each value of theta, the gradient and the moments is read once and written once.  A warp
+// What bounds it: memory (200 million fp32 values: 893 us, 6.3 TB/s; bf16 with fp32 copies 903 us, 6.6 TB/s), and where moments
+// have 8 bits the arithmetic of their codes.  Each value of theta, the gradient and the moments is read once and written once.  A warp
 // takes units of 256 consecutive values of one tensor: lane l holds values 4l..4l+3 and 128+4l..128+4l+3, so that every
 // access of the warp is one contiguous piece, and the 256 values that share a scale in the 8-bit form sit in one warp.
 //
@@ -26,6 +27,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
+
+#include "pair.cuh"
 
 namespace bmgdk {
 
@@ -237,11 +240,17 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------- the update
-// Square root and quotient of the step within 2^-23 and 2^-22 of their values: they move theta by lr at most, and the exact
-// forms cost as many instructions as the rest of the formula (which bounds the kernel where moments have 8 bits).
+// m / (sqrt(v) root + eps) with the root and the reciprocal each within 2^-23 of their values: they move theta by lr at most, and
+// the exact forms cost as many instructions as the rest of the formula.  (eps is at least 2^-63: nothing here is subnormal
+// but a v that counts for nothing beside it.)
 __device__ __forceinline__ float sqrt_near(float x) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_near(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
@@ -262,9 +271,10 @@ template <int TYPE, bool WIDE> __device__ __forceinline__ void load4_any(const v
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
 
-// One unit of a tensor.  WIDE: it lies within the tensor and every array allows vector accesses.
+// One unit of a tensor.  WIDE: it lies within the tensor and every array allows vector accesses.  (Other units, and those with
+// infinities or NaN where moments have 8 bits, are few: their code is kept out of the way.)
 template <int PT, bool MASTER, int GT, int BITS, bool WIDE>
-__device__ __forceinline__ void adamw_unit(const AdamwEntry& e, long long unit, int lane, const AdamwFactors& F, float keep, uint32_t key) {
+__device__ __forceinline__ void adamw_unit_body(const AdamwEntry& e, long long unit, int lane, const AdamwFactors& F, float keep, uint32_t key) {
     const long long n = e.n;
     const long long at[2] = {unit * kAdamwUnit + lane * 4, unit * kAdamwUnit + lane * 4 + 128};
     constexpr bool kRandomTheta = PT == kTypeBF16 && !MASTER;
@@ -305,7 +315,7 @@ __device__ __forceinline__ void adamw_unit(const AdamwEntry& e, long long unit, 
             m[h][i] = __fadd_rn(__fmul_rn(m[h][i], F.a), __fmul_rn(gi, F.a1));
             v[h][i] = __fadd_rn(__fmul_rn(v[h][i], F.b), __fmul_rn(__fmul_rn(gi, F.b1), gi));
             const float denom = __fadd_rn(__fmul_rn(sqrt_near(v[h][i]), F.root), F.eps);
-            p[h][i] = __fsub_rn(__fmul_rn(p[h][i], keep), __fmul_rn(__fdividef(m[h][i], denom), F.step));
+            p[h][i] = __fsub_rn(__fmul_rn(p[h][i], keep), __fmul_rn(__fmul_rn(m[h][i], reciprocal_near(denom)), F.step));
             if constexpr (BITS == 8) {
                 top_m = max(top_m, __float_as_uint(m[h][i]) & 0x7FFFFFFFu);
                 top_v = max(top_v, __float_as_uint(v[h][i]) & 0x7FFFFFFFu);
@@ -369,20 +379,146 @@ __device__ __forceinline__ void adamw_unit(const AdamwEntry& e, long long unit, 
 }
 
 template <int PT, bool MASTER, int GT, int BITS>
+__device__ __noinline__ void adamw_unit_any(const AdamwEntry& e, long long unit, int lane, const AdamwFactors& F, float keep, uint32_t key) {
+    adamw_unit_body<PT, MASTER, GT, BITS, false>(e, unit, lane, F, keep, key);
+}
+
+// largest magnitude and smallest value of three; NaN wins the first
+__device__ __forceinline__ float top3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float low3(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// the uppermost bytes of four words, in order
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
+    return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410);
+}
+
+// A full unit with moments in 8 bits.  Instructions and the latency of a unit's loads bound this form, not memory (200 million
+// values in bf16: 1079 us value by value, 741 in this way with three blocks to an SM, 653 with four; their traffic needs 310),
+// hence: two values to an instruction wherever the formula allows; the largest and
+// smallest of several values in one; four codes at a time through bytes.
+// A code is the upper bits of y, the value's exponent and mantissa counted from the format's smallest, plus the draw: for m
+// y is the larger of the magnitude's bits and those of (magnitude + 2^-6) less 2^23, which count in constant steps below
+// 2^-6 (there the second is the larger, above it the first); for v it is at least one code.  y * 16 + draw * 256 then has the code
+// in its uppermost byte, for m plus 0xC0 (120 << 23, times 16), which (b ^ 0xC0) & 0x7F takes off.
+template <int PT, bool MASTER, int GT>
+__device__ __forceinline__ void adamw_unit8(const AdamwEntry& e, long long unit, int lane, const AdamwFactors& F, float keep, uint32_t key) {
+    const long long at = unit * kAdamwUnit + lane * 4;
+    constexpr bool kRandomTheta = PT == kTypeBF16 && !MASTER;
+    float p[8], g[8], m[8], v[8];
+    uint32_t cm[2], cv[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        load4_wide<GT>(e.grad, at + 128 * h, *reinterpret_cast<float(*)[4]>(g + 4 * h));
+        if constexpr (MASTER) load4_wide<kTypeF32>(e.master, at + 128 * h, *reinterpret_cast<float(*)[4]>(p + 4 * h));
+        else load4_wide<PT>(e.param, at + 128 * h, *reinterpret_cast<float(*)[4]>(p + 4 * h));
+        cm[h] = load_codes(e.m, at + 128 * h, e.n, true);
+        cv[h] = load_codes(e.v, at + 128 * h, e.n, true);
+    }
+    const int old_m = e.m_scale[unit], old_v = e.v_scale[unit];
+    const uint32_t base = (uint32_t)(old_v - 30) << 23;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        decode_m4(cm[h], *reinterpret_cast<float(*)[4]>(m + 4 * h));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * h + i] = __uint_as_float(__byte_perm(cv[h], 0, 0x4440 + i) * (1u << 20) + base);
+        // a byte of zeros (no moment yet) or of ones (NaN) among the four
+        if (((cv[h] - 0x01010101u) & ~cv[h] & 0x80808080u) | ((~cv[h] - 0x01010101u) & cv[h] & 0x80808080u)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t c = (cv[h] >> (8 * i)) & 0xFFu;
+                if (c == 0u) v[4 * h + i] = 0.f;
+                if (c == 0xFFu) v[4 * h + i] = __uint_as_float(0x7FC00000u);
+            }
+        }
+    }
+    const Pair unscale(power_of_two(old_m - 7)), gscale(F.gscale), a(F.a), a1(F.a1), b(F.b), b1(F.b1), root(F.root), eps(F.eps), kept(keep), step(-F.step);
+    float top_m = 0.f, top_v = 0.f, top_p = 0.f, low_v = __uint_as_float(0x7F7FFFFFu);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const Pair gi = Pair(g[i], g[i + 1]) * gscale;
+        const Pair mi = (Pair(m[i], m[i + 1]) * unscale) * a + gi * a1;
+        const float2 vi = (Pair(v[i], v[i + 1]) * b + (gi * b1) * gi).both();
+        const float2 denom = (Pair(sqrt_near(vi.x), sqrt_near(vi.y)) * root + eps).both();
+        const Pair quotient = mi * Pair(reciprocal_near(denom.x), reciprocal_near(denom.y));
+        const float2 pi = (Pair(p[i], p[i + 1]) * kept + quotient * step).both(), mm = mi.both();
+        m[i] = mm.x; m[i + 1] = mm.y;
+        v[i] = vi.x; v[i + 1] = vi.y;
+        p[i] = pi.x; p[i + 1] = pi.y;
+        top_m = top3(top_m, mm.x, mm.y);
+        top_v = top3(top_v, vi.x, vi.y);
+        top_p = top3(top_p, pi.x, pi.y);
+        low_v = low3(low_v, vi.x, vi.y);
+    }
+    if (__any_sync(0xFFFFFFFFu, !(top3(top_m, top_v, top_p) < INFINITY))) {  // nothing has been written yet
+        adamw_unit_any<PT, MASTER, GT, 8>(e, unit, lane, F, keep, key);
+        return;
+    }
+    const int new_m = max((int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_m)) >> 23), 16);
+    const int new_v = max((int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_v)) >> 23), 40);
+    const Pair scale(power_of_two(261 - new_m));
+    const uint32_t from = (uint32_t)(new_v - 30) << 23;
+    const uint32_t k = key + (uint32_t)((unsigned long long)at >> 32) * 0x85EBCA6Bu;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t place = (uint32_t)(at + 128 * h) ^ k;  // (a multiple of four before the key: i sets its lowest bits)
+        uint32_t xm[4], um[4], uv[4], theta[4];
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const float2 x = (Pair(m[4 * h + i], m[4 * h + i + 1]) * scale).both();
+            xm[i] = __float_as_uint(x.x);
+            xm[i + 1] = __float_as_uint(x.y);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = mix32(place ^ (uint32_t)i), mag = xm[i] & 0x7FFFFFFFu;
+            const uint32_t small = __float_as_uint(__fadd_rz(__uint_as_float(mag), 0x1p-6f)) - (1u << 23);
+            um[i] = max(mag, small) * 16u + __byte_perm(r, 0, 0x4104);
+            uv[i] = (uint32_t)max((int)(__float_as_uint(v[4 * h + i]) - from), 1 << 20) * 16u + __byte_perm(r, 0, 0x4324);
+            if constexpr (kRandomTheta) theta[i] = __float_as_uint(p[4 * h + i]) + (mix32(r ^ 0x9E3779B9u) & 0xFFFFu);
+        }
+        uint32_t wv = top_bytes(uv);
+        if (low_v == 0.f) {  // (v is never negative)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[4 * h + i] == 0.f) wv &= ~(0xFFu << (8 * i));
+        }
+        store_codes(e.m, at + 128 * h, e.n, true, ((top_bytes(um) ^ 0xC0C0C0C0u) & 0x7F7F7F7Fu) | (top_bytes(xm) & 0x80808080u));
+        store_codes(e.v, at + 128 * h, e.n, true, wv);
+        if constexpr (MASTER) store4(e.master, kTypeF32, at + 128 * h, e.n, true, *reinterpret_cast<float(*)[4]>(p + 4 * h));
+        if constexpr (kRandomTheta)
+            __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(e.param) + at + 128 * h),
+                   make_uint2(__byte_perm(theta[0], theta[1], 0x7632), __byte_perm(theta[2], theta[3], 0x7632)));
+        else store4(e.param, PT, at + 128 * h, e.n, true, *reinterpret_cast<float(*)[4]>(p + 4 * h));
+    }
+    if (lane == 0) { e.m_scale[unit] = (uint8_t)new_m; e.v_scale[unit] = (uint8_t)new_v; }
+}
+
+template <int PT, bool MASTER, int GT, int BITS>
 __device__ __forceinline__ void adamw_units(const AdamwEntry& e, long long unit0, int units, int lane, const AdamwFactors& F, uint32_t key) {
     const float keep = e.keep;
     for (int u = 0; u < units; ++u) {
         const long long unit = unit0 + u;
         if (unit * kAdamwUnit >= e.n) break;
-        if (e.aligned && (unit + 1) * kAdamwUnit <= e.n) adamw_unit<PT, MASTER, GT, BITS, true>(e, unit, lane, F, keep, key);
-        else adamw_unit<PT, MASTER, GT, BITS, false>(e, unit, lane, F, keep, key);
+        if (e.aligned && (unit + 1) * kAdamwUnit <= e.n) {
+            if constexpr (BITS == 8) adamw_unit8<PT, MASTER, GT>(e, unit, lane, F, keep, key);
+            else adamw_unit_body<PT, MASTER, GT, BITS, true>(e, unit, lane, F, keep, key);
+        } else {
+            adamw_unit_any<PT, MASTER, GT, BITS>(e, unit, lane, F, keep, key);
+        }
     }
 }
 
 // BITS: how the moments of all tensors of this launch are held.  Their types differ from tensor to tensor; the code for
 // each combination is chosen once for a warp's units.
 template <int CAP, int BITS>
-__global__ void __launch_bounds__(kAdamwThreads, 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP> T) {
+__global__ void __launch_bounds__(kAdamwThreads, BITS == 8 ? 4 : 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP> T) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     __shared__ AdamwFactors shared_factors;
     __shared__ double part[kAdamwThreads / 32];

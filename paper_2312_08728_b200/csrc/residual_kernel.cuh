@@ -11,6 +11,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include "pair.cuh"
 #include "shuffle.cuh"
 
 namespace bmgdk {
@@ -114,18 +115,7 @@ __device__ __forceinline__ uint32_t residual_rank() {
     return r;
 }
 
-// Two fp32 operations in one instruction: the exponentials' arithmetic is what competes with memory in the 16-bit types.
-struct Pair {
-    unsigned long long v;
-    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ float2 both() const {
-        float2 r;
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-        return r;
-    }
-};
-__device__ __forceinline__ Pair operator+(Pair a, const Pair& b) { asm("add.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v)); return a; }
-__device__ __forceinline__ Pair operator*(Pair a, const Pair& b) { asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v)); return a; }
+// (in pairs, because the exponentials' arithmetic competes with memory in the 16-bit types)
 // the exponentials of a piece against a maximum, two at a time: exp_fast(x - m)
 template <typename T, typename F>
 __device__ __forceinline__ void piece_powers(const uint4& w, const Pair& minus_m, const Pair& log2e, F&& take) {
