@@ -400,7 +400,7 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
 }
 
 // A full unit with moments in 8 bits.  Instructions and the latency of a unit's loads bound this form, not memory (200 million
-// values in bf16: 1079 us value by value, 741 in this way with three blocks to an SM, 653 with four; their traffic needs 310),
+// values in bf16: 1079 us value by value, 741 in this way with three blocks to an SM, 662 with four; their traffic needs 310),
 // hence: two values to an instruction wherever the formula allows; the largest and
 // smallest of several values in one; four codes at a time through bytes.
 // A code is the upper bits of y, the value's exponent and mantissa counted from the format's smallest, plus the draw: for m
@@ -442,9 +442,12 @@ __device__ __forceinline__ void adamw_unit8(const AdamwEntry& e, long long unit,
     float top_m = 0.f, top_v = 0.f, top_p = 0.f, low_v = __uint_as_float(0x7F7FFFFFu);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
+        // (the sums one by one: a sum of products in pairs comes out as one rounding, and the moments' codes are defined by two)
         const Pair gi = Pair(g[i], g[i + 1]) * gscale;
-        const Pair mi = (Pair(m[i], m[i + 1]) * unscale) * a + gi * a1;
-        const float2 vi = (Pair(v[i], v[i + 1]) * b + (gi * b1) * gi).both();
+        const float2 ma = ((Pair(m[i], m[i + 1]) * unscale) * a).both(), mb = (gi * a1).both();
+        const float2 va = (Pair(v[i], v[i + 1]) * b).both(), vb = ((gi * b1) * gi).both();
+        const Pair mi(__fadd_rn(ma.x, mb.x), __fadd_rn(ma.y, mb.y));
+        const float2 vi = make_float2(__fadd_rn(va.x, vb.x), __fadd_rn(va.y, vb.y));
         const float2 denom = (Pair(sqrt_near(vi.x), sqrt_near(vi.y)) * root + eps).both();
         const Pair quotient = mi * Pair(reciprocal_near(denom.x), reciprocal_near(denom.y));
         const float2 pi = (Pair(p[i], p[i + 1]) * kept + quotient * step).both(), mm = mi.both();

@@ -169,6 +169,29 @@ def test_moments_in_8_bits_bit_for_bit():
             assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("param,grad", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32)])
+def test_moments_in_8_bits_do_not_depend_on_alignment(param, grad):
+    """A sum of products rounded once instead of twice would show in a code of some millions: the forms for aligned and for
+    other tensors agree in all of 2^24."""
+    n = 1 << 24
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    p = (torch.randn(n, generator=gen, device="cuda") * 0.1).to(param)
+    grads = [(torch.randn(n, generator=gen, device="cuda") * torch.exp2(torch.randint(-6, 6, (n,), generator=gen, device="cuda").float())).to(grad) for _ in range(3)]
+
+    def moved(t):
+        out = torch.zeros(n + 1, dtype=t.dtype, device="cuda")[1:]
+        out.copy_(t)
+        return out
+    states = [ops.adamw_state([p], 8) for _ in range(2)]
+    params = [p.clone(), moved(p)]
+    for g in grads:
+        ops.adamw_step([params[0]], [g], lr=1e-3, seed=4, **states[0])
+        ops.adamw_step([params[1]], [moved(g)], lr=1e-3, seed=4, **states[1])
+        for k in ("m", "v", "m_scale", "v_scale"):
+            a, b = (s[k][0].view(torch.uint8) for s in states)
+            assert torch.equal(a, b), (k, int((a != b).sum()))
+
+
 def test_moments_in_8_bits_keep_their_mean():
     """A constant gradient: v must approach its square and m the gradient, although every change is below half a step."""
     n, steps = 1 << 16, 1500
