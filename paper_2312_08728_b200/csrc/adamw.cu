@@ -123,7 +123,7 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return BMGD_ERR_CUDA;
     // as many blocks as fit an SM: of the sum of squares, and of the update of moments in 32 and in 8 bits
-    const int sum_blocks = std::min(kAdamwMaxBlocks, sms * 6), blocks = std::min(kAdamwMaxBlocks, sms * 3), blocks8 = std::min(kAdamwMaxBlocks, sms * 4);
+    const int sum_blocks = std::min(kAdamwMaxBlocks, sms * 8), blocks = std::min(kAdamwMaxBlocks, sms * 3), blocks8 = std::min(kAdamwMaxBlocks, sms * 4);
     const bool clip = cfg->max_norm > 0.0;
     AdamwHead h{};
     h.control = static_cast<long long*>(dev_control);

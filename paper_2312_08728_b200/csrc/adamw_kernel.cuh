@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kAdamwThreads, BITS == 8 ? 4 : 3) adamw_kernel
         if (T.h.npartial > 0) {
             double s = 0.0;
             for (int w = 0; w < kAdamwThreads / 32; ++w) s += part[w];
-            const double norm = sqrt(s) * T.h.grad_scale;
+            const double norm = sqrt(s) * fabs(T.h.grad_scale);
             F.norm = norm;
             F.fine = isfinite(norm) ? 1 : 0;
             scale *= fmin(T.h.max_norm / (norm + 1e-6), 1.0);

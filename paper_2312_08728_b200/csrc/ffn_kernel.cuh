@@ -175,24 +175,28 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 // ---------------------------------------------------------------- shapes
-// Read-out: four warps, or eight where a tile's arithmetic can be short (the contraction over few rows of the weights'
-// gradients) or its read-out long (the backward form reads two factors per value).  Each turns its values through a buffer of
-// its own in shared memory: 32 rows of kWords words, kPitch apart so that eight lanes' 16-byte accesses meet no bank twice.
+// Read-out: eight warps (with four the gated form that saves its factors kept the tensor cores waiting at 2048 inputs: 64 %
+// active, and one stage of the ring less costs nothing there).  Each turns its values through a buffer of its own in shared
+// memory, rows of kWords words.  The 16-byte piece c of row r stands at c ^ turn_key(r), so that eight lanes meet no bank twice,
+// neither those of eight rows that write the same piece nor those of two rows that read four pieces each.
 template <int EPI>
 struct FfnReadOut {
-    static constexpr int kWarps = EPI == kEpiGated ? 4 : 8;
-    static constexpr int kWords = EPI == kEpiGated ? 32 : 16;   // plain: 32 values of 16 bits
-    static constexpr int kPitch = kWords + 4;
-    static constexpr int kCols = EPI == kEpiBackward ? 16 : EPI == kEpiPlain ? 32 : 16;  // columns of the tile taken at a time
-    static constexpr int kBytes = kWarps * 32 * kPitch * 4;
+    static constexpr int kWarps = 8;
+    static constexpr int kRows = EPI == kEpiBackward ? 16 : 32;
+    static constexpr int kWords = EPI == kEpiPlain ? 16 : 32;   // plain: 32 values of 16 bits
+    static constexpr int kCols = EPI == kEpiGated ? 16 : 32;    // columns of the tile taken at a time
+    static constexpr int kBytes = kWarps * kRows * kWords * 4;
     static constexpr int kThreads = 128 + kWarps * 32;
 };
+// word of piece `c` (16 bytes) of row `r` in a buffer of 32-word rows, or of 16-word rows
+__device__ __forceinline__ int turn32(int r, int c) { return r * 32 + ((c ^ (((r & 1) << 2) | ((r >> 1) & 3))) << 2); }
+__device__ __forceinline__ int turn16(int r, int c) { return r * 16 + ((c ^ ((r >> 1) & 3)) << 2); }
 template <int CG, int BN, int EPI>
 struct FfnShape {
     static constexpr int kA = 128 * kFfnBK * 2;            // bytes of A per stage and CTA
     static constexpr int kB = BN / CG * kFfnBK * 2;        // bytes of B per stage and CTA
     static constexpr int kStage = kA + kB;
-    static constexpr int kStages = kStage > 40960 ? 4 : 6;
+    static constexpr int kStages = EPI == kEpiGated ? 5 : 6;
     static constexpr int kBars = kStages * kStage;         // mbarriers and the tensor-memory address behind the ring
     static constexpr int kTurn = kBars + 256;              // where a warp turns rows per lane into pieces of rows per lane
     static constexpr int kSmem = kTurn + FfnReadOut<EPI>::kBytes + 1024;  // (1024: the ring starts on a 1024-byte boundary)
@@ -347,8 +351,8 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
         // pieces of rows: in between the values go through shared memory.
         int acc = 0;
         uint32_t acc_phase = 0;
-        const int quarter = warp & 3, part = (warp - 4) >> 2;  // with eight warps two share a quarter of the rows: one takes the even pieces
-        float* const turn = reinterpret_cast<float*>(ffn_smem + (ring - smem_u32(ffn_smem)) + S::kTurn) + (warp - 4) * 32 * R::kPitch;
+        const int quarter = warp & 3, part = (warp - 4) >> 2;  // two warps share a quarter of the rows: one takes the even pieces
+        float* const turn = reinterpret_cast<float*>(ffn_smem + (ring - smem_u32(ffn_smem)) + S::kTurn) + (warp - 4) * R::kRows * R::kWords;
         for (long long t = pair; t < tiles; t += pairs) {
             int which, m0, n0;
             place(t, which, m0, n0);
@@ -367,7 +371,7 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                 // 16 columns of G and 16 of U at a time; then a lane has four columns of rows lane / 4, lane / 4 + 8, ...
                 const int sub = (lane & 3) * 4;
 #pragma unroll 1
-                for (int c = 0; c < kCols; c += 16) {
+                for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols) {
                     const int col = n0 + c;
                     if (col >= N) break;
                     uint32_t r[32];
@@ -376,14 +380,14 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                     tmem_wait();
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<uint4*>(turn + lane * R::kPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                        *reinterpret_cast<uint4*>(turn + turn32(lane, i)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                     __syncwarp();
 #pragma unroll
                     for (int it = 0; it < 4; ++it) {
                         const int i = it * 8 + (lane >> 2);
                         if (i < rows && col + sub < N) {  // (rows of H, act(G) and U act'(G) are padded to multiples of 8)
-                            const float4 g = *reinterpret_cast<const float4*>(turn + i * R::kPitch + sub);
-                            const float4 u = *reinterpret_cast<const float4*>(turn + i * R::kPitch + 16 + sub);
+                            const float4 g = *reinterpret_cast<const float4*>(turn + turn32(i, lane & 3));
+                            const float4 u = *reinterpret_cast<const float4*>(turn + turn32(i, 4 + (lane & 3)));
                             float4 v, s;
                             if (P.value) {
                                 act_both(P.act, g.x, v.x, s.x); act_both(P.act, g.y, v.y, s.y);
@@ -401,45 +405,52 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                     __syncwarp();
                 }
             } else if constexpr (EPI == kEpiBackward) {
-                const int sub = (lane & 3) * 4;
+                // 32 columns of the factors at a time, a lane four columns of rows lane / 8, lane / 8 + 4, ...: pieces of 128 bytes
+                // (4096 x 5632 values from 2048 outputs: 92 us, with pieces of 64 bytes 112); the sums come through shared memory 16
+                // rows at a time.
+                const int sub = (lane & 7) * 4;
 #pragma unroll 1
                 for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols) {
                     const int col = n0 + c;
                     if (col >= N) break;
-                    float4 v[4], s[4];
+                    float4 v[8], s[8];
 #pragma unroll
-                    for (int it = 0; it < 4; ++it) {
-                        const int i = it * 8 + (lane >> 2);
+                    for (int it = 0; it < 8; ++it) {
+                        const int i = it * 4 + (lane >> 3);
                         const long long at = (row0 + i) * P.ld_save + col + sub;
                         if (i < rows && col + sub < N) {
                             v[it] = __ldcs(reinterpret_cast<const float4*>(P.value + at));
                             s[it] = __ldcs(reinterpret_cast<const float4*>(P.slope + at));
                         }
                     }
-                    uint32_t r[16];
-                    tmem_load16(ta + (uint32_t)c, r);
+                    uint32_t r[32];
+                    tmem_load32(ta + (uint32_t)c, r);
                     tmem_wait();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<uint4*>(turn + lane * R::kPitch + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
-                    __syncwarp();
+                    for (int half = 0; half < 2; ++half) {
+                        if ((lane >> 4) == half) {
 #pragma unroll
-                    for (int it = 0; it < 4; ++it) {
-                        const int i = it * 8 + (lane >> 2);
-                        if (i < rows && col + sub < N) {
-                            const float4 d = *reinterpret_cast<const float4*>(turn + i * R::kPitch + sub);
-                            const long long at = (row0 + i) * ld_out + col + sub;
-                            *reinterpret_cast<uint2*>(out + at) =
-                                make_uint2(pack2(P.type, d.x * s[it].x, d.y * s[it].y), pack2(P.type, d.z * s[it].z, d.w * s[it].w));
-                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out_up) + at) =
-                                make_uint2(pack2(P.type, d.x * v[it].x, d.y * v[it].y), pack2(P.type, d.z * v[it].z, d.w * v[it].w));
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<uint4*>(turn + turn32(lane & 15, i)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
                         }
+                        __syncwarp();
+#pragma unroll
+                        for (int it = 4 * half; it < 4 * half + 4; ++it) {
+                            const int i = it * 4 + (lane >> 3);
+                            if (i < rows && col + sub < N) {
+                                const float4 d = *reinterpret_cast<const float4*>(turn + turn32(i & 15, lane & 7));
+                                const long long at = (row0 + i) * ld_out + col + sub;
+                                *reinterpret_cast<uint2*>(out + at) =
+                                    make_uint2(pack2(P.type, d.x * s[it].x, d.y * s[it].y), pack2(P.type, d.z * s[it].z, d.w * s[it].w));
+                                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out_up) + at) =
+                                    make_uint2(pack2(P.type, d.x * v[it].x, d.y * v[it].y), pack2(P.type, d.z * v[it].z, d.w * v[it].w));
+                            }
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             } else {
                 uint16_t* const half = reinterpret_cast<uint16_t*>(turn);
-                constexpr int kHalf = R::kPitch * 2;  // 16-bit values from row to row
                 const bool vec = q.vec != 0;
 #pragma unroll 1
                 for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols) {
@@ -453,7 +464,7 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                         uint32_t p[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) p[j] = pack2(P.type, __uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
-                        *reinterpret_cast<uint4*>(half + lane * kHalf + 8 * i) = make_uint4(p[0], p[1], p[2], p[3]);
+                        *reinterpret_cast<uint4*>(turn + turn16(lane, i)) = make_uint4(p[0], p[1], p[2], p[3]);
                     }
                     __syncwarp();
                     if (vec && col + 32 <= N) {
@@ -461,11 +472,11 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                         for (int it = 0; it < 4; ++it) {
                             const int i = it * 8 + (lane >> 2), sub = (lane & 3) * 8;
                             if (i < rows)
-                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + sub) = *reinterpret_cast<const uint4*>(half + i * kHalf + sub);
+                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + sub) = *reinterpret_cast<const uint4*>(turn + turn16(i, lane & 3));
                         }
                     } else if (col + lane < N) {
 #pragma unroll 8
-                        for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + lane] = half[i * kHalf + lane];
+                        for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + lane] = half[2 * turn16(i, lane >> 3) + (lane & 7)];
                     }
                     __syncwarp();
                 }
