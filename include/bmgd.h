@@ -324,10 +324,11 @@ typedef struct bmgd_gated_ffn {
     int64_t ld_saved;
     const void* dy;                      /* backward: gradient of Y, stride ld_dy */
     int64_t ld_dy;
-    void *dx, *dw_gate, *dw_up, *dw_down; /* backward: gradients, contiguous, shaped like X, Wg, Wu and Wd */
+    void *dx, *dw_gate, *dw_up, *dw_down; /* backward: gradients, contiguous, shaped like X, Wg, Wu and Wd (dx NULL: not wanted) */
 } bmgd_gated_ffn;
 
-/* Bytes of workspace (device memory, 256-byte aligned, free for reuse once the stream has passed the call) of a pass. */
+/* Bytes of workspace (device memory, 256-byte aligned, free for reuse once the stream has passed the call) of a pass; 0: it
+ * needs none. */
 int bmgd_gated_ffn_workspace_bytes(const bmgd_gated_ffn* g, int32_t pass, int64_t* bytes);
 int bmgd_gated_ffn_forward(const bmgd_gated_ffn* g, void* workspace, int64_t workspace_bytes, void* stream);
 /* The weights' gradients are sums over the rows in a fixed order: equal calls give equal bits.  rows = 0 gives zeros. */

@@ -296,7 +296,7 @@ int check(const bmgd_gated_ffn* g, int pass, bool pointers) {
     if ((g->saved_value == nullptr) != (g->saved_slope == nullptr) || (g->saved_value == nullptr) != (g->saved_hidden == nullptr)) return BMGD_ERR_ARG;
     if ((uintptr_t)g->saved_value % 16 || (uintptr_t)g->saved_slope % 16 || (uintptr_t)g->saved_hidden % 16) return BMGD_ERR_ARG;
     if (pass == BMGD_FFN_FORWARD) return bad_pointer(g->y) ? BMGD_ERR_ARG : BMGD_OK;
-    if (!g->saved_value || bad_pointer(g->dy) || bad_pointer(g->dx) || bad_pointer(g->dw_gate) || bad_pointer(g->dw_up) || bad_pointer(g->dw_down))
+    if (!g->saved_value || bad_pointer(g->dy) || (uintptr_t)g->dx % 2 != 0 || bad_pointer(g->dw_gate) || bad_pointer(g->dw_up) || bad_pointer(g->dw_down))
         return BMGD_ERR_ARG;
     return BMGD_OK;
 }
@@ -342,9 +342,11 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     const Problem factors{{dy, dy}, {wd, wd}, const_cast<void*>(dg.base), ldh, n, g->hidden, g->outputs, 1, true};
     rc = contract<kEpiBackward, false>(P, factors, false, dev, s);
     if (rc != BMGD_OK) return rc;
-    const Problem dx{{dg, du}, {wg, wu}, g->dx, g->inputs, n, g->inputs, g->hidden, 2, wide(g->dx, g->inputs)};
-    rc = contract<kEpiPlain, false>(P, dx, true, dev, s);
-    if (rc != BMGD_OK) return rc;
+    if (g->dx) {
+        const Problem dx{{dg, du}, {wg, wu}, g->dx, g->inputs, n, g->inputs, g->hidden, 2, wide(g->dx, g->inputs)};
+        rc = contract<kEpiPlain, false>(P, dx, true, dev, s);
+        if (rc != BMGD_OK) return rc;
+    }
     const Problem weights[3] = {
         {{x, x}, {dg, dg}, g->dw_gate, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_gate, g->hidden)},
         {{x, x}, {du, du}, g->dw_up, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_up, g->hidden)},
@@ -368,7 +370,7 @@ int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspa
     Space need{nullptr, 0};
     rc = pass == BMGD_FFN_FORWARD ? forward(g, &need, false, dev, s) : backward(g, &need, false, dev, s);
     if (rc != BMGD_OK) return rc;
-    if (!workspace || (uintptr_t)workspace % 256 != 0) return BMGD_ERR_ARG;
+    if (need.used > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)) return BMGD_ERR_ARG;
     if (workspace_bytes < need.used) return BMGD_ERR_CAPACITY;
     rc = current_device(&dev);
     if (rc != BMGD_OK) return rc;
@@ -387,7 +389,7 @@ int bmgd_gated_ffn_workspace_bytes(const bmgd_gated_ffn* g, int32_t pass, int64_
     Device dev{};
     Space need{nullptr, 0};
     const int r = pass == BMGD_FFN_FORWARD ? forward(g, &need, false, dev, nullptr) : backward(g, &need, false, dev, nullptr);
-    *bytes = std::max<int64_t>(need.used, 256);
+    *bytes = need.used;
     return r;
 }
 

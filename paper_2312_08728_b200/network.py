@@ -115,7 +115,7 @@ class GatedSoftmax:
         """One update from the rows of one mini-batch; returns the loss of each."""
         logits, saved = ops.gated_ffn(x, *self.weights, self.activation, save=True)
         residual, loss = ops.softmax_residual(logits, y)
-        _, *grads = ops.gated_ffn_backward(residual, x, *self.weights, saved, self.activation)
+        _, *grads = ops.gated_ffn_backward(residual, x, *self.weights, saved, self.activation, need_dx=False)
         ops.adamw_step(self.weights, grads, lr=lr, masters=self.masters, **self.state, **self._rule)
         return loss
 

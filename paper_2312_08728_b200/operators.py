@@ -129,9 +129,9 @@ def _run_ffn(which: int, args: bytes, device: torch.device) -> None:
     need = ctypes.c_int64()
     rc = L.bmgd_gated_ffn_workspace_bytes(args, which, ctypes.byref(need))
     if rc == BMGD_OK:
-        w = torch.empty(need.value, dtype=torch.uint8, device=device)
+        w = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
         call = L.bmgd_gated_ffn_forward if which == _FORWARD else L.bmgd_gated_ffn_backward
-        rc = call(args, w.data_ptr(), need.value, _current(device))
+        rc = call(args, w.data_ptr() if w is not None else None, need.value, _current(device))
     if rc != BMGD_OK:
         raise BmgdError(rc, "bmgd_gated_ffn_forward" if which == _FORWARD else "bmgd_gated_ffn_backward")
 
@@ -157,8 +157,9 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
 
 def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
                        saved: torch.Tensor, activation: int = ACT_SILU,
-                       stream: Optional[torch.cuda.Stream] = None):
-    """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the gradient dy of its output.
+                       need_dx: bool = True, stream: Optional[torch.cuda.Stream] = None):
+    """Gradients (dx, dw_gate, dw_up, dw_down) of gated_ffn for the gradient dy of its output; dx is None with need_dx=False
+    (the first layer of a model has no use for it).
 
     `saved` is what the forward call on the same arguments returned; the gradients have the type of x."""
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
@@ -167,8 +168,10 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
     if saved.shape != (n, 5 * width) or saved.dtype is not x.dtype or saved.device != device or not saved.is_contiguous():
         raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
     with _place(device, stream):
-        dx, dw_gate, dw_up, dw_down = x.new_empty((n, d)), x.new_empty((d, f)), x.new_empty((d, f)), x.new_empty((f, c))
-        _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(saved, n, width), dy.data_ptr(), ld_dy, dx.data_ptr(), dw_gate.data_ptr(),
+        dx = x.new_empty((n, d)) if need_dx else None
+        dw_gate, dw_up, dw_down = x.new_empty((d, f)), x.new_empty((d, f)), x.new_empty((f, c))
+        _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(saved, n, width), dy.data_ptr(), ld_dy,
+                                            dx.data_ptr() if need_dx else 0, dw_gate.data_ptr(),
                                             dw_up.data_ptr(), dw_down.data_ptr()), device)
     return dx, dw_gate, dw_up, dw_down
 

@@ -39,7 +39,7 @@ def test_workspace_counts_intermediates_and_copies():
     assert rc == 0 and moved > plain
     saved = dict(value=PTR, slope=PTR, hidden_saved=PTR, ld_saved=16)
     rc, kept = workspace(**saved)                  # the hidden rows go to the caller
-    assert rc == 0 and kept <= plain
+    assert rc == 0 and kept == 0
     rc, back = workspace(1, **saved)
     assert rc == 0 and back >= 2 * 4 * 16 * 2
 
@@ -71,7 +71,8 @@ def test_gated_ffn_workspace_and_pass():
     assert L.bmgd_gated_ffn_forward(ffn(), PTR, 8, None) == binding.ERR_CAPACITY
     assert L.bmgd_gated_ffn_backward(ffn(), PTR, 1 << 40, None) == binding.ERR_ARG       # nothing saved
     saved = dict(value=PTR, slope=PTR, hidden_saved=PTR, ld_saved=16)
-    for k in ("dy", "dx", "dw_gate", "dw_up", "dw_down"):
+    assert L.bmgd_gated_ffn_backward(ffn(**saved, dx=PTR + 1), PTR, 1 << 40, None) == binding.ERR_ARG
+    for k in ("dy", "dw_gate", "dw_up", "dw_down"):
         assert L.bmgd_gated_ffn_backward(ffn(**saved, **{k: 0}), PTR, 1 << 40, None) == binding.ERR_ARG
     assert L.bmgd_gated_ffn_backward(ffn(**saved, ld_dy=7), PTR, 1 << 40, None) == binding.ERR_ARG
     need = ctypes.c_int64()
