@@ -71,11 +71,10 @@ int launch(const bmgd_adamw_tensor* t, int32_t count, const AdamwHead& head, int
         e.first_chunk = chunks;
         e.keep = (float)(1.0 - head.lr * x.weight_decay);
         e.index = (uint32_t)x.index;
-        e.ptype = (uint8_t)x.param_type; e.gtype = (uint8_t)x.grad_type; e.bits = (uint8_t)x.state_bits;
+        e.ptype = (uint8_t)x.param_type; e.gtype = (uint8_t)x.grad_type;
         const int sb = x.state_bits == 8 ? 1 : 4;
         e.aligned = (uintptr_t)x.param % (4 * type_bytes(x.param_type)) == 0 && (uintptr_t)x.grad % (4 * type_bytes(x.grad_type)) == 0 &&
                     (uintptr_t)x.m % (4 * sb) == 0 && (uintptr_t)x.v % (4 * sb) == 0 && (uintptr_t)x.master % 16 == 0;
-        e.reserved = 0;
         chunks += (x.count + per_chunk - 1) / per_chunk;
     }
     T->h.count = k;

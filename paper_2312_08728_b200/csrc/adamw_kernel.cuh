@@ -50,8 +50,7 @@ struct AdamwEntry {
     long long first_chunk;  // chunks of all entries before this one
     float keep;             // 1 - lr wd
     uint32_t index;         // place of the tensor in the caller's list: part of the random key
-    uint8_t ptype, gtype, bits, aligned;
-    uint32_t reserved;
+    uint8_t ptype, gtype, aligned;
 };
 
 struct AdamwHead {

@@ -4,8 +4,7 @@
 //              Y = H Wd                                 so the product is taken where the accumulators are read out
 //   backward   dH = dY Wd^T, dU = dH act(G), dG = dH (U act'(G))  one kernel; the two factors come from the forward pass
 //              dX = dG Wg^T + dU Wu^T                   one accumulator, the second product continues the first
-//              dWg = X^T dG, dWu = X^T dU               one launch over both
-//              dWd = H^T dY
+//              dWg = X^T dG, dWu = X^T dU, dWd = H^T dY  one launch over the three
 // Rows of every matrix are contiguous.  Both ways of reading a tile exist for each operand: "K-major", the contraction
 // index along the rows, or "MN-major", across them; nothing is transposed in memory.  H, dG and dU are rounded to the type
 // of the rows between the kernels (they are the operands of the next contraction, which takes no other type); sums are fp32
@@ -177,7 +176,7 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
 // ---------------------------------------------------------------- shapes
 // Read-out: eight warps (with four the gated form that saves its factors kept the tensor cores waiting at 2048 inputs: 64 %
 // active, and one stage of the ring less costs nothing there).  Each turns its values through a buffer of its own in shared
-// memory, rows of kWords words.  The 16-byte piece c of row r stands at c ^ turn_key(r), so that eight lanes meet no bank twice,
+// memory, rows of kWords words.  The 16-byte pieces of a row stand in an order of the row's own (turn32, turn16), so that eight lanes meet no bank twice,
 // neither those of eight rows that write the same piece nor those of two rows that read four pieces each.
 template <int EPI>
 struct FfnReadOut {

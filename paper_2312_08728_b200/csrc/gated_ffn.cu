@@ -184,14 +184,15 @@ int launch_few(FfnParams& P, const Problem& x, int split, bool early, const Devi
 
 // Rows per tile and split of the contraction for the form with exchanged roles, by an estimate in microseconds fitted to a
 // sweep on B200 over rows 1 to 2000, widths 256 to 11008: a CTA takes in 80 KB a microsecond (its stages in flight over the
-// latency of a copy), all of them together no more than 8 MB; reading out a row's sums takes 0.015 and exchanging them 0.006
-// more per CTA of the cluster, a cluster about 1.  Within 2 us of the best of the sweep throughout; always taking 128 rows
-// and the largest split that fits cost up to 9 us of 30 there.
+// latency of a copy), all of them together no more than 24 MB; reading out a row's sums takes 0.015 (backward 0.02) and
+// exchanging them 0.006 (0.01) more per CTA of the cluster, a cluster about 1.  Its choice is within 3 us of the best of the sweep throughout; always taking 128 rows and the
+// largest split that fits cost up to 9 us of 30 there.
 struct FewChoice {
     int rows, split;
 };
 template <int EPI>
 FewChoice choose_few(const Problem& x, const Device& dev) {
+    const double read_out = EPI == kEpiBackward ? 0.02 : 0.015, exchange = EPI == kEpiBackward ? 0.01 : 0.006;
     const int kinds = EPI == kEpiGated ? 2 : 1, steps = x.segments * ((x.K + kFfnBK - 1) / kFfnBK);
     FewChoice best{16, 1};
     double least = 1e30;
@@ -202,8 +203,8 @@ FewChoice choose_few(const Problem& x, const Device& dev) {
         for (int split : {1, 2, 3, 4, 8}) {
             if (split > 1 && (tiles * split > slots || split * 2 > steps)) break;
             const double turns = (double)((tiles * split + slots - 1) / slots);
-            const double copies = std::max(turns * ((steps + split - 1) / split) * stage / 80e3, (double)tiles * steps * stage / 8e6);
-            const double t = copies + turns * rows * (0.015 + 0.006 * (split - 1)) + (split > 1 ? 1.0 : 0.0);
+            const double copies = std::max(turns * ((steps + split - 1) / split) * stage / 80e3, (double)tiles * steps * stage / 24e6);
+            const double t = copies + turns * rows * (read_out + exchange * (split - 1)) + (split > 1 ? 1.0 : 0.0);
             if (t < least) { least = t; best = FewChoice{nr, split}; }
         }
     }
