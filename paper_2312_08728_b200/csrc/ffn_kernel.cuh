@@ -176,20 +176,19 @@ __device__ __forceinline__ uint32_t pack2(int type, float a, float b) {
 // ---------------------------------------------------------------- shapes
 // Read-out: eight warps (with four the gated form that saves its factors kept the tensor cores waiting at 2048 inputs: 64 %
 // active, and one stage of the ring less costs nothing there).  Each turns its values through a buffer of its own in shared
-// memory, rows of kWords words.  The 16-byte pieces of a row stand in an order of the row's own (turn32, turn16), so that eight lanes meet no bank twice,
+// memory, rows of kWords words.  The 16-byte pieces of a row stand in an order of the row's own (turn32), so that eight lanes meet no bank twice,
 // neither those of eight rows that write the same piece nor those of two rows that read four pieces each.
 template <int EPI>
 struct FfnReadOut {
     static constexpr int kWarps = 8;
     static constexpr int kRows = EPI == kEpiBackward ? 16 : 32;
-    static constexpr int kWords = EPI == kEpiPlain ? 16 : 32;   // plain: 32 values of 16 bits
-    static constexpr int kCols = EPI == kEpiGated ? 16 : 32;    // columns of the tile taken at a time
+    static constexpr int kWords = 32;                           // plain: 64 values of 16 bits
+    static constexpr int kCols = EPI == kEpiGated ? 16 : EPI == kEpiPlain ? 64 : 32;  // columns of the tile taken at a time
     static constexpr int kBytes = kWarps * kRows * kWords * 4;
     static constexpr int kThreads = 128 + kWarps * 32;
 };
-// word of piece `c` (16 bytes) of row `r` in a buffer of 32-word rows, or of 16-word rows
+// word of piece `c` (16 bytes) of row `r`
 __device__ __forceinline__ int turn32(int r, int c) { return r * 32 + ((c ^ (((r & 1) << 2) | ((r >> 1) & 3))) << 2); }
-__device__ __forceinline__ int turn16(int r, int c) { return r * 16 + ((c ^ ((r >> 1) & 3)) << 2); }
 template <int CG, int BN, int EPI>
 struct FfnShape {
     static constexpr int kA = 128 * kFfnBK * 2;            // bytes of A per stage and CTA
@@ -449,33 +448,40 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                     }
                 }
             } else {
-                uint16_t* const half = reinterpret_cast<uint16_t*>(turn);
+                // 64 columns at a time: rows of 128 bytes
+                const uint16_t* const half = reinterpret_cast<const uint16_t*>(turn);
                 const bool vec = q.vec != 0;
 #pragma unroll 1
                 for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols) {
                     const int col = n0 + c;
                     if (col >= N) break;
-                    uint32_t r[32];
+                    uint32_t r[64];
                     tmem_load32(ta + (uint32_t)c, r);
+                    tmem_load32(ta + (uint32_t)(c + 32), r + 32);
                     tmem_wait();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 8; ++i) {
                         uint32_t p[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) p[j] = pack2(P.type, __uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
-                        *reinterpret_cast<uint4*>(turn + turn16(lane, i)) = make_uint4(p[0], p[1], p[2], p[3]);
+                        *reinterpret_cast<uint4*>(turn + turn32(lane, i)) = make_uint4(p[0], p[1], p[2], p[3]);
                     }
                     __syncwarp();
-                    if (vec && col + 32 <= N) {
+                    if (vec && col + 64 <= N) {
 #pragma unroll
-                        for (int it = 0; it < 4; ++it) {
-                            const int i = it * 8 + (lane >> 2), sub = (lane & 3) * 8;
+                        for (int it = 0; it < 8; ++it) {
+                            const int i = it * 4 + (lane >> 3);
                             if (i < rows)
-                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + sub) = *reinterpret_cast<const uint4*>(turn + turn16(i, lane & 3));
+                                *reinterpret_cast<uint4*>(out + (row0 + i) * ld_out + col + (lane & 7) * 8) = *reinterpret_cast<const uint4*>(turn + turn32(i, lane & 7));
                         }
-                    } else if (col + lane < N) {
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 64; h += 32) {
+                            if (col + h + lane < N) {
 #pragma unroll 8
-                        for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + lane] = half[2 * turn16(i, lane >> 3) + (lane & 7)];
+                                for (int i = 0; i < rows; ++i) out[(row0 + i) * ld_out + col + h + lane] = half[2 * turn32(i, (h + lane) >> 3) + (lane & 7)];
+                            }
+                        }
                     }
                     __syncwarp();
                 }
