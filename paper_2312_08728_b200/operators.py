@@ -86,6 +86,11 @@ def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int]
     return n, c, s0
 
 
+def _like(t: torch.Tensor, ld: int) -> torch.Tensor:
+    """An uninitialised contiguous tensor of the size and type of the matrix t, whose row stride is ld."""
+    return torch.empty_like(t) if ld == t.shape[1] else t.new_empty(t.shape)
+
+
 def _device_of(t: torch.Tensor, name: str) -> torch.device:
     if t.device.type != "cuda":
         raise ValueError(f"{name} must be a device tensor; there is no CPU path")
@@ -168,8 +173,9 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
     if saved.shape != (n, 5 * width) or saved.dtype is not x.dtype or saved.device != device or not saved.is_contiguous():
         raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
     with _place(device, stream):
-        dx = x.new_empty((n, d)) if need_dx else None
-        dw_gate, dw_up, dw_down = x.new_empty((d, f)), x.new_empty((d, f)), x.new_empty((f, c))
+        ld_x, ld_gate, ld_up, ld_down = shared[11:]
+        dx = _like(x, ld_x) if need_dx else None
+        dw_gate, dw_up, dw_down = _like(w_gate, ld_gate), _like(w_up, ld_up), _like(w_down, ld_down)
         _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(saved, n, width), dy.data_ptr(), ld_dy,
                                             dx.data_ptr() if need_dx else 0, dw_gate.data_ptr(),
                                             dw_up.data_ptr(), dw_down.data_ptr()), device)
@@ -199,7 +205,7 @@ def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[floa
         raise ValueError(f"y must be a contiguous int32 [{rows}] on {device}")
     L = _binding.load_library()
     with _place(device, stream):
-        residual = logits.new_empty((rows, C))
+        residual = _like(logits, ld)
         loss = torch.empty(rows, dtype=torch.float32, device=device)
         if rows > 0:
             _status(L.bmgd_softmax_residual(logits.data_ptr(), ld, y.data_ptr(), rows, C, _TYPES[logits.dtype],
@@ -259,8 +265,8 @@ _dtype = operator.attrgetter("dtype")
 _numel, _get_device, _is_contiguous, _data_ptr = (getattr(torch.Tensor, k) for k in ("numel", "get_device", "is_contiguous", "data_ptr"))
 
 
-def _column(tensors: Sequence[torch.Tensor], name: str, counts: List[int], types: frozenset, device: int):
-    """Refuse a list of tensors that does not match the parameters; returns their addresses and the types among them."""
+def _column(tensors: Sequence[torch.Tensor], name: str, counts: List[int], types: frozenset, device: int) -> List[int]:
+    """Refuse a list of tensors that does not match the parameters; returns their addresses."""
     if len(tensors) != len(counts):
         raise ValueError(f"{name}: {len(tensors)} tensors for {len(counts)} parameters")
     if list(map(_numel, tensors)) != counts:
@@ -272,7 +278,7 @@ def _column(tensors: Sequence[torch.Tensor], name: str, counts: List[int], types
         raise ValueError(f"{name}: all tensors must live on one device")
     if not all(map(_is_contiguous, tensors)):
         raise ValueError(f"{name}: tensors must be contiguous")
-    return list(map(_data_ptr, tensors)), found
+    return list(map(_data_ptr, tensors))
 
 
 _ANY, _FLOAT = frozenset(_TYPES), frozenset((torch.float32,))
@@ -296,13 +302,17 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     device = _device_of(params[0], "params")
     index = device.index
     counts = list(map(_numel, params))
-    at_params, p_types = _column(params, "params", counts, _ANY, index)
-    at_grads, g_types = _column(grads, "grads", counts, _ANY, index)
-    at_m, m_types = _column(m, "m", counts, _M, index)
-    at_v, v_types = _column(v, "v", counts, _V, index)
+    p_types, g_types, m_types, v_types = (set(map(_dtype, t)) for t in (params, grads, m, v))
+    every = [*params, *grads, *m, *v]
+    if not (len(grads) == len(m) == len(v) == count and p_types <= _ANY and g_types <= _ANY and m_types <= _M and v_types <= _V and
+            list(map(_numel, every)) == counts * 4 and set(map(_get_device, every)) == {index} and all(map(_is_contiguous, every))):
+        for t, name, types in ((params, "params", _ANY), (grads, "grads", _ANY), (m, "m", _M), (v, "v", _V)):
+            _column(t, name, counts, types, index)  # (says which)
+        raise ValueError("params, grads, m and v do not match")
+    addresses = array("q", map(_data_ptr, every))
     table = array("q", bytes(88 * count))  # bmgd_adamw_tensor[count], filled column by column
-    for k, column in enumerate((at_params, at_grads, at_m, at_v)):
-        table[k::11] = array("q", column)
+    for k in range(4):
+        table[k::11] = addresses[k * count:(k + 1) * count]
     if m_types == _FLOAT and v_types == _FLOAT:
         table[10::11] = array("q", range(32, 32 + (count << 32), 1 << 32))  # state_bits and index
     else:
@@ -312,14 +322,14 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
         if m_scale is None or v_scale is None:
             raise ValueError("moments in 8 bits need m_scale and v_scale")
         blocks = [-(-n // SCALE_BLOCK) for n in counts]
-        table[4::11] = array("q", _column(m_scale, "m_scale", blocks, _BYTES, index)[0])
-        table[5::11] = array("q", _column(v_scale, "v_scale", blocks, _BYTES, index)[0])
+        table[4::11] = array("q", _column(m_scale, "m_scale", blocks, _BYTES, index))
+        table[5::11] = array("q", _column(v_scale, "v_scale", blocks, _BYTES, index))
         table[10::11] = array("q", [(8 if e else 32) | i << 32 for i, e in enumerate(eight)])
     if masters is not None:
         if len(masters) != count:
             raise ValueError(f"masters: {len(masters)} tensors for {count} parameters")
         held = [i for i, t in enumerate(masters) if t is not None]
-        for i, at in zip(held, _column([masters[i] for i in held], "masters", [counts[i] for i in held], _FLOAT, index)[0]):
+        for i, at in zip(held, _column([masters[i] for i in held], "masters", [counts[i] for i in held], _FLOAT, index)):
             if params[i].dtype is torch.float32:
                 raise ValueError("a float32 parameter has no master copy")
             table[11 * i + 6] = at
