@@ -53,6 +53,7 @@ struct FfnParams {
     float* slope;
     long long ld_save;
     int type, act;
+    int early;               // many rows: this launch needs nothing of the one before it, only of those before that
     int* status;
     unsigned long long timeout_ns;
 };
@@ -265,7 +266,9 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
-    wait_for_previous_kernel();
+    // early: the kernel before this one is ours, and let this one start only when everything before it had finished.  The two
+    // share no memory that either writes, so they may run side by side; this one still ends after that one.
+    if (!P.early) wait_for_previous_kernel();
     let_next_kernel_start();
 
     const long long tiles = P.tiles;
@@ -506,6 +509,7 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
     if constexpr (CG == 2) { cluster_arrive_release(); cluster_wait_acquire(); }
     tc_fence_after();
     if (warp == 2) ffn_tmem_free<CG>(tmem, kTmemCols);
+    if (P.early) wait_for_previous_kernel();
 }
 
 // ---------------------------------------------------------------- few rows, and everything small

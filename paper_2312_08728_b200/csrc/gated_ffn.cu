@@ -352,6 +352,7 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
         {{x, x}, {dg, dg}, g->dw_gate, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_gate, g->hidden)},
         {{x, x}, {du, du}, g->dw_up, g->hidden, g->inputs, g->hidden, (int)n, 1, wide(g->dw_up, g->hidden)},
         {{h, h}, {dy, dy}, g->dw_down, g->outputs, g->hidden, g->outputs, (int)n, 1, wide(g->dw_down, g->outputs)}};
+    P.early = g->dx != nullptr;  // dX and the weights' gradients need nothing of one another
     return contract_many<kEpiPlain, true, true>(P, weights, 3, dev, s);
 }
 
