@@ -306,7 +306,7 @@ enum { BMGD_FFN_FORWARD = 0, BMGD_FFN_BACKWARD = 1 };
 
 /* Gated feed-forward block: Y = (act(X Wg) * (X Wu)) Wd, X [rows][inputs], Wg and Wu [inputs][hidden],
  * Wd [hidden][outputs], all of one type (BF16 or F16; F32 returns BMGD_ERR_UNIMPLEMENTED), sums in fp32.  Any sizes
- * from 1 (rows from 0) and any row strides; operands whose rows do not start on 16-byte boundaries are copied into
+ * from 1 (rows from 0) up to 2^24 (rows 2^31 - 256) and any row strides; operands whose rows do not start on 16-byte boundaries are copied into
  * the workspace first. */
 typedef struct bmgd_gated_ffn {
     int64_t rows;
@@ -361,7 +361,7 @@ typedef struct bmgd_adamw_tensor {
     void* v_scale;
     void* master;            /* fp32 copy of theta that the update runs on, theta being its rounding; F16 needs one, BF16
                                 may do without (theta is then rounded at random, keeping the mean), F32 has none */
-    int64_t count;           /* values; 0 is allowed */
+    int64_t count;           /* values, up to 2^40; 0 is allowed */
     double weight_decay;
     int32_t param_type, grad_type, state_bits, index; /* state_bits 32 or 8; index: part of the key of the random rounding */
 } bmgd_adamw_tensor;

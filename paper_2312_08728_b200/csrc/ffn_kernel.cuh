@@ -637,7 +637,8 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
-    if (!early) wait_for_previous_kernel();
+    // (all but the warp that fetches: the bounded waits below must not count the time of the kernel before)
+    if (!early || warp != 0) wait_for_previous_kernel();
 
     const int kblocks = (q.K + kFfnBK - 1) / kFfnBK, steps = kblocks * q.segments;
     const int first = (int)((long long)steps * part / S), last = (int)((long long)steps * (part + 1) / S);
@@ -697,10 +698,10 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
         }
     }
     __syncwarp();
+    if (early && warp == 0) wait_for_previous_kernel();
     // after the last product the ring's memory is free for the partial sums [row][128 features]
     ffn_wait(done, 0, w);
     tc_fence_after();
-    if (early) wait_for_previous_kernel();
     let_next_kernel_start();
     const bool given_up = __syncthreads_or(w.aborted ? 1 : 0) != 0;
 

@@ -72,6 +72,8 @@ class GatedSoftmax:
         with torch.cuda.stream(copy):
             x[:rows].copy_(host_x, non_blocking=True)
             y[:rows].copy_(host_y, non_blocking=True)
+        x.record_stream(copy)  # (the model may be dropped while a copy is under way)
+        y.record_stream(copy)
         self._loaded[s].record(copy)
         self._count[s] = rows
         self._next ^= 1

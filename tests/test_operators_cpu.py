@@ -188,3 +188,11 @@ def test_columns_are_checked():
             ops._column(bad, "m", [3, 8], ops._FLOAT, -1)
     with pytest.raises(ValueError):
         ops._column(good, "m", [3, 8], ops._FLOAT, 0)
+
+
+def test_no_cpu_path():
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    from paper_2312_08728_b200.network import GatedSoftmax
+    with pytest.raises(RuntimeError):
+        GatedSoftmax(100, 8, 2, 16, 4)
