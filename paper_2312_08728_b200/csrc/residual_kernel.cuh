@@ -39,9 +39,12 @@ __device__ __forceinline__ float exp_fast(float x) {  // exp for x <= 0 within 2
 }
 // (the difference is taken first: next to the type's lowest value a product with log2 e would overflow)
 __device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.f : m; }
+// factor that takes a sum to a larger maximum; a sum without one is 0 or NaN and stays so (0 times the exponential of what
+// lies between 0 and a row of very negative logits would be NaN)
+__device__ __forceinline__ float carry(float from, float to) { return from == -INFINITY ? 1.f : exp_fast(from - against(to)); }
 __device__ __forceinline__ MaxSum join(const MaxSum& a, const MaxSum& b) {
-    const float m = fmaxf(a.m, b.m), to = against(m);
-    return MaxSum{m, a.s * exp_fast(against(a.m) - to) + b.s * exp_fast(against(b.m) - to)};
+    const float m = fmaxf(a.m, b.m);
+    return MaxSum{m, a.s * carry(a.m, m) + b.s * carry(b.m, m)};
 }
 __device__ __forceinline__ MaxSum join_lanes(MaxSum a, int lanes) {
     for (int o = lanes / 2; o > 0; o >>= 1) a = join(a, MaxSum{__shfl_xor_sync(0xFFFFFFFFu, a.m, o), __shfl_xor_sync(0xFFFFFFFFu, a.s, o)});
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) residual_long_kernel(const T* _
             for (int k = 0; k < kAhead; ++k)
                 if (k0 + k * TH < pieces) top = piece_max(top, w[k], T());
             const float m = against(top);
-            Pair sums(a.s * exp_fast(against(a.m) - m), 0.f);
+            Pair sums(a.s * carry(a.m, top), 0.f);
             a.m = top;
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)

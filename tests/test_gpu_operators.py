@@ -319,6 +319,22 @@ def test_residual_masks_and_labels(C, dtype):
     assert loss[6] == math.inf and torch.isnan(residual[7]).all() and torch.isnan(residual[8]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,C", [(9, 1), (9, 2), (9, 3), (9, 17), (9, 64), (9, 65), (9, 1025), (9, 40001), (64, 35001), (64, 70001), (9, 300007)])
+def test_residual_rows_far_below_zero(rows, C, dtype):
+    """exp(-max) overflows: threads that hold only masked logits, or none, must still count for nothing."""
+    gen = torch.Generator(device="cuda").manual_seed(C)
+    z = torch.randn(rows, C, generator=gen, device="cuda") * 4
+    y = torch.randint(0, C, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    z[0::3] -= 100.0
+    z[1::3] -= 60000.0
+    z[2::3] = torch.finfo(dtype).min
+    if C > 2:
+        z[3:, 1::2] = -math.inf
+        z[6:, : C - 1] = -math.inf            # one class left, at the end of the row
+    check_residual(z.to(dtype), y)
+
+
 @pytest.mark.parametrize("C", [12, 1003])
 def test_residual_rows_of_a_wider_matrix(C):
     z = torch.randn(37, C + 5, device="cuda", dtype=torch.bfloat16)[:, 2:C + 2]
