@@ -60,6 +60,8 @@ class GatedSoftmax:
         rows = host_x.shape[0]
         if rows > self.rows:
             raise BmgdError(ERR_CAPACITY, "load_buffer")
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"the stream belongs to {stream.device}, the model lives on {self.device}")
         s, current = self._next, torch.cuda.current_stream(self.device)
         copy = stream if stream is not None else current
         if self._slots[s] is None:
@@ -69,6 +71,7 @@ class GatedSoftmax:
             self._freed[s].record(current)  # (new memory may still be in use by work issued before)
         x, y = self._slots[s]
         copy.wait_event(self._freed[s])
+        self._count[s] = 0  # (nothing to train on, should a copy fail)
         with torch.cuda.stream(copy):
             x[:rows].copy_(host_x, non_blocking=True)
             y[:rows].copy_(host_y, non_blocking=True)
@@ -87,9 +90,10 @@ class GatedSoftmax:
         current.wait_event(self._loaded[slot])
         x, y = self._slots[slot]
         n = self._count[slot]
-        loss = self._rounds(x[:n], y[:n], rounds, batch_size, lr, seed)
-        self._freed[slot].record(current)
-        return loss
+        try:
+            return self._rounds(x[:n], y[:n], rounds, batch_size, lr, seed)
+        finally:
+            self._freed[slot].record(current)  # (a step that fails leaves the steps before it under way)
 
     def run_rounds_resident(self, dev_x: torch.Tensor, dev_y: torch.Tensor, rounds: int, batch_size: int, lr: float,
                             seed: int) -> torch.Tensor:

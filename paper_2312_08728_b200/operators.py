@@ -9,7 +9,8 @@
 Argument checks and marshalling only: the computation runs in the CUDA library (include/bmgd.h), which takes bare
 pointers, so whatever the tensors' own metadata can tell is refused here.  Work is ordered on `stream`, by default the
 current stream of the tensors' device; nothing waits for the device, so every call can be captured into a CUDA graph.
-Outputs and workspaces come from torch's allocator on that stream.
+Outputs and workspaces come from torch's allocator on that stream.  Where `stream` is not the current one, the order between
+the two is the caller's (wait_stream or events); the memory of inputs and outputs is kept until both are done with it.
 """
 from __future__ import annotations
 
@@ -58,6 +59,24 @@ def _place(device: torch.device, stream: Optional[torch.cuda.Stream]):
     if stream is None and torch._C._cuda_getDevice() == device.index:
         return _HERE
     return _other(device, stream)
+
+
+def _lend(stream: Optional[torch.cuda.Stream], device: torch.device, inputs) -> None:
+    """Tell the allocator that a call on another stream reads or writes these tensors: a caller may drop them at once."""
+    if stream is not None and stream != torch.cuda.current_stream(device):
+        for t in inputs:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _hand(stream: Optional[torch.cuda.Stream], device: torch.device, outputs) -> None:
+    """The same for tensors allocated on that stream, which the caller goes on to use on the current one."""
+    if stream is not None:
+        here = torch.cuda.current_stream(device)
+        if stream != here:
+            for t in outputs:
+                if t is not None:
+                    t.record_stream(here)
 
 
 def _current(device: torch.device) -> int:
@@ -148,7 +167,9 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     All four in bfloat16 or all in float16; rows contiguous, any row stride.  With save=True returns (y, saved), saved
     being what gated_ffn_backward needs beside its other arguments."""
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
-    with _place(device, stream):
+    place = _place(device, stream)
+    _lend(stream, device, (x, w_gate, w_up, w_down))
+    with place:
         y = x.new_empty((n, c))
         saved, kept = None, (0, 0, 0, 0)
         if save:
@@ -157,6 +178,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
             kept = _saved_args(saved, n, width)
         if n > 0:
             _run_ffn(_FORWARD, _GATED_FFN.pack(*shared, y.data_ptr(), c, *kept, 0, 0, 0, 0, 0, 0), device)
+    _hand(stream, device, (y, saved))
     return (y, saved) if save else y
 
 
@@ -172,13 +194,16 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
     width = (f + 7) // 8 * 8
     if saved.shape != (n, 5 * width) or saved.dtype is not x.dtype or saved.device != device or not saved.is_contiguous():
         raise ValueError("saved must be what gated_ffn returned for the same rows and weights")
-    with _place(device, stream):
+    place = _place(device, stream)
+    _lend(stream, device, (dy, x, w_gate, w_up, w_down, saved))
+    with place:
         ld_x, ld_gate, ld_up, ld_down = shared[11:]
         dx = _like(x, ld_x) if need_dx else None
         dw_gate, dw_up, dw_down = _like(w_gate, ld_gate), _like(w_up, ld_up), _like(w_down, ld_down)
         _run_ffn(_BACKWARD, _GATED_FFN.pack(*shared, 0, 0, *_saved_args(saved, n, width), dy.data_ptr(), ld_dy,
                                             dx.data_ptr() if need_dx else 0, dw_gate.data_ptr(),
                                             dw_up.data_ptr(), dw_down.data_ptr()), device)
+    _hand(stream, device, (dx, dw_gate, dw_up, dw_down))
     return dx, dw_gate, dw_up, dw_down
 
 
@@ -204,13 +229,16 @@ def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[floa
     if y.dim() != 1 or y.shape[0] != rows or y.dtype != torch.int32 or y.device != device or not y.is_contiguous():
         raise ValueError(f"y must be a contiguous int32 [{rows}] on {device}")
     L = _binding.load_library()
-    with _place(device, stream):
+    place = _place(device, stream)
+    _lend(stream, device, (logits, y))
+    with place:
         residual = _like(logits, ld)
         loss = torch.empty(rows, dtype=torch.float32, device=device)
         if rows > 0:
             _status(L.bmgd_softmax_residual(logits.data_ptr(), ld, y.data_ptr(), rows, C, _TYPES[logits.dtype],
                                             1.0 / rows if scale is None else float(scale), residual.data_ptr(), C,
                                             loss.data_ptr(), _current(device)), "bmgd_softmax_residual")
+    _hand(stream, device, (residual, loss))
     return residual, loss
 
 
@@ -227,13 +255,16 @@ def gather_batch(x: torch.Tensor, y: Optional[torch.Tensor], seed: int, chain: i
     if first < 0 or count < 0 or first + count > rows:
         raise ValueError(f"rows {first} to {first + count} of a buffer of {rows}")
     L = _binding.load_library()
-    with _place(device, stream):
+    place = _place(device, stream)
+    _lend(stream, device, (x, y))
+    with place:
         bx = torch.empty(count, x.shape[1], dtype=x.dtype, device=device)
         by = torch.empty(count, dtype=torch.int32, device=device) if y is not None else None
         _status(L.bmgd_gather_batch(x.data_ptr(), x.shape[1] * x.element_size(), y.data_ptr() if y is not None else None, rows,
                                     int(seed) & 0xFFFFFFFFFFFFFFFF, int(chain) & 0xFFFFFFFF, int(round) & 0xFFFFFFFF, first, count,
                                     bx.data_ptr(), by.data_ptr() if by is not None else None,
                                     _current(device)), "bmgd_gather_batch")
+    _hand(stream, device, (bx, by))
     return bx, by
 
 
@@ -351,7 +382,10 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
         table[9::11] = array("q", [_TYPES[p.dtype] | _TYPES[g.dtype] << 32 for p, g in zip(params, grads)])
     cfg = _AdamwConfig(float(lr), float(a), float(b), float(eps), float(grad_scale), float(max_norm), int(seed) & 0xFFFFFFFFFFFFFFFF)
     L = _binding.load_library()
-    with _place(device, stream):
+    place = _place(device, stream)
+    if stream is not None:
+        _lend(stream, device, [*every, control, *(m_scale or ()), *(v_scale or ()), *(masters or ())])
+    with place:
         scratch, size = None, 0
         if max_norm > 0:
             size = (1 + count // 360) * 1184 * 8

@@ -1,4 +1,6 @@
 """The operators run together, as a training step uses them, and the model that does so."""
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -106,3 +108,71 @@ def test_refusals():
             net.load_buffer(bad_x, bad_y)
     with pytest.raises(ValueError):
         net.set_theta([torch.zeros(1)] * 3)
+
+
+def test_memory_of_a_call_on_another_stream_is_kept():
+    """Tensors that the caller drops while a call on another stream is still to run (or outputs of it, while the caller's stream
+    still reads them) do not go to the next allocation."""
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    weights = [torch.zeros(s, **bf) for s in ((640, 64), (640, 64), (64, 640))]
+    labels = torch.zeros(512, dtype=torch.int32, device="cuda")
+    calls = [lambda t: ops.gated_ffn(t, *weights, stream=side), lambda t: ops.softmax_residual(t, labels, stream=side)[0],
+             lambda t: ops.gather_batch(t, labels, 1, 0, 0, 0, 512, stream=side)[0],
+             lambda t: ops.gated_ffn_backward(t, t.clone(), *weights, torch.zeros(512, 5 * 64, **bf), stream=side)[0]]
+    for call in calls:
+        call(torch.zeros(512, 640, **bf))     # (loads what the call needs, before a kernel holds the stream)
+        torch.cuda.synchronize()
+        t = torch.zeros(512, 640, **bf)
+        at = t.data_ptr()
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        out = call(t)
+        del t
+        assert torch.empty(512, 640, **bf).data_ptr() != at
+        here.wait_stream(side)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(100_000_000)
+        at = out.data_ptr()
+        del out
+        with torch.cuda.stream(side):
+            assert torch.empty(512, 640, **bf).data_ptr() != at
+        torch.cuda.synchronize()
+    params = [torch.zeros(1 << 20, device="cuda")]
+    state = ops.adamw_state(params)
+    ops.adamw_step(params, [torch.zeros_like(params[0])], lr=0.1, stream=side, **state)
+    torch.cuda.synchronize()
+    g = torch.ones_like(params[0])
+    at = g.data_ptr()
+    side.wait_stream(here)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    ops.adamw_step(params, [g], lr=0.1, stream=side, **state)
+    del g
+    assert torch.empty(1 << 20, device="cuda").data_ptr() != at
+    torch.cuda.synchronize()
+
+
+def test_rounds_that_fail_leave_their_slot_in_use(monkeypatch):
+    """The steps before the failure still read the buffer: the slot is free behind them, not before."""
+    x, y = sample(64, 16, 4, torch.bfloat16)
+    net = GatedSoftmax(64, 16, 1, 32, 4)
+    slot = net.load_buffer(x.pin_memory(), y.pin_memory())
+    torch.cuda.synchronize()
+
+    def step(*_):
+        torch.cuda._sleep(100_000_000)
+        raise RuntimeError("no memory")
+    monkeypatch.setattr(net, "step", step)
+    with pytest.raises(RuntimeError, match="no memory"):
+        net.run_rounds(slot, 1, 16, 0.1, 0)
+    assert not net._freed[slot].query()
+    torch.cuda.synchronize()
+
+
+def test_buffers_are_not_loaded_on_another_device():
+    x, y = sample(8, 16, 4, torch.bfloat16)
+    net = GatedSoftmax(8, 16, 1, 32, 4)
+    with pytest.raises(ValueError, match="stream"):
+        net.load_buffer(x.pin_memory(), y.pin_memory(), stream=types.SimpleNamespace(device=torch.device("cuda", 1)))
