@@ -202,6 +202,28 @@ def test_gated_block_nan_stays_in_its_row(rows):
     assert torch.equal(y[0], clean[0]) and torch.equal(y[2:], clean[2:])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("rows,f", [(1, 40), (9, 264), (300, 136), (700, 2048)])
+def test_gated_block_relu_of_minus_infinity(rows, f, dtype):
+    """max(-Inf, 0) is 0: units switched off by a weight of -Inf give what they give when a finite weight does it."""
+    d, c = 64, 48
+    b = Block(rows, d, f, c, dtype, ops.ACT_RELU, seed=rows)
+    b.x[:, 5] = 1.0
+    off = torch.arange(0, f, 3, device="cuda")
+    b.wg[5, off] = -1000.0
+    want, y = b.run(), ops.gated_ffn(b.x, b.wg, b.wu, b.wd, b.act)
+    b.wg[5, off] = -math.inf
+    got = b.run()
+    assert torch.equal(ops.gated_ffn(b.x, b.wg, b.wu, b.wd, b.act), y)
+    others = torch.arange(d, device="cuda") != 5
+    for k in ("y", "dw_gate", "dw_up", "dw_down"):
+        assert torch.equal(got[k], want[k]), k
+    assert torch.equal(got["dx"][:, others], want["dx"][:, others])
+    assert torch.isnan(got["dx"][:, 5]).all()  # 0 times -Inf
+    b.x[0, 7] = math.nan
+    assert torch.isnan(ops.gated_ffn(b.x, b.wg, b.wu, b.wd, b.act)[0]).all()
+
+
 @pytest.mark.parametrize("rows", [1, 9, 300])
 def test_gated_block_captured_and_on_another_stream(rows):
     b = Block(rows, 128, 264, 64, torch.bfloat16, ops.ACT_SILU, seed=6)
