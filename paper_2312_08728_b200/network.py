@@ -10,9 +10,17 @@ of freshly shuffled mini-batches, the shuffle being the one of `Bmgd` (round t u
 Rows are bf16 or fp16; the weights are held in fp32 and in the rows' type, the update is AdamW with moments in 32 or 8
 bits.  Every step is the operators of `operators.py` in a row: gather_batch, gated_ffn, softmax_residual,
 gated_ffn_backward, adamw_step.
+
+fp16 has no exponents for gradients of a mean over many rows: a probability of 1e-4 over 1,000 rows lies below its normal
+values, and the gradients that follow from it lower still (1,000 rows that a net 512 -> 1024 -> 10 knows with e^9 to 1: the relative error of
+dWg is 0.08, of 8,192 rows 0.43; with the loss scaled 0.0005).  So with fp16 rows the residual, and with it every gradient, is
+multiplied by a power of two S, which the update divides out again in fp32; S / rows is between 1/2 and 1, S at most 2^13 and,
+up to 128 rows, 1, unless the caller gives `loss_scale`.  An update whose gradients are not finite is left out
+(state["control"] counts them), and S falls to a quarter eight steps after one.
 """
 from __future__ import annotations
 
+import sys
 from typing import Dict, List, Optional
 
 import torch
@@ -20,6 +28,9 @@ import torch
 from . import operators as ops
 from .binding import ERR_CAPACITY, ERR_STATE, BmgdError, check_buffer
 from .inputs import DTYPE_BF16, LOSS_SOFTMAX
+
+_LAG = 8               # steps between an update and the look at whether it was left out: the host runs ahead that far
+_LEAST = 2.0 ** -20    # of the factor by which S has fallen (rows with NaN are not to blame on the scale for ever)
 
 
 class GatedSoftmax:
@@ -29,16 +40,21 @@ class GatedSoftmax:
 
     def __init__(self, N: int, p: int, K: int, hidden: int, C: int, dtype: torch.dtype = torch.bfloat16,
                  activation: int = ops.ACT_SILU, device: int = 0, state_bits: int = 32, a: float = 0.9, b: float = 0.999,
-                 eps: float = 1e-8, weight_decay: float = 0.0, max_norm: float = 0.0, seed: int = 0):
+                 eps: float = 1e-8, weight_decay: float = 0.0, max_norm: float = 0.0, seed: int = 0,
+                 loss_scale: Optional[float] = None):
         if not torch.cuda.is_available():
             raise RuntimeError("GatedSoftmax needs a CUDA device; there is no CPU path")
         if N < 1 or p < 1 or K < 1 or K > N or hidden < 1 or C < 2:
             raise ValueError("N, p, K, hidden and C must be positive, K at most N, C at least 2")
         if dtype not in (torch.bfloat16, torch.float16):
             raise ValueError(f"dtype must be bfloat16 or float16, got {dtype}")
+        if loss_scale is not None and (dtype is not torch.float16 or not 0.0 < loss_scale < float("inf")):
+            raise ValueError("loss_scale must be positive and finite, and is for float16 only")
         self.N, self.p, self.K, self.hidden, self.C, self.dtype, self.activation = N, p, K, hidden, C, dtype, activation
         self.device = torch.device("cuda", device)
         self.rows = -(-N // K)
+        if dtype is torch.float16 and max_norm == 0.0:
+            max_norm = sys.float_info.max   # clips nothing, and leaves an update out whose norm is not finite
         self._rule = dict(a=a, b=b, eps=eps, weight_decay=weight_decay, max_norm=max_norm, seed=seed)
         gen = torch.Generator(device=self.device).manual_seed(seed)
         shapes = ((p, hidden), (p, hidden), (hidden, C))
@@ -50,6 +66,11 @@ class GatedSoftmax:
         self._loaded = [torch.cuda.Event() for _ in range(2)]
         self._freed = [torch.cuda.Event() for _ in range(2)]
         self._next = 0
+        self.loss_scale = loss_scale
+        if dtype is torch.float16:
+            self._lowered, self._steps, self._lowered_at, self._left_out = 1.0, 0, 0, 0
+            self._counts = torch.zeros(_LAG, ops.CONTROL_WORDS, dtype=torch.int64).pin_memory()
+            self._counted = [torch.cuda.Event() for _ in range(_LAG)]
 
     def load_buffer(self, host_x: torch.Tensor, host_y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Start copying one buffer (pinned host tensors, labels int32) into the next slot on `stream`, behind the last
@@ -117,12 +138,36 @@ class GatedSoftmax:
                 loss = self.step(*ops.gather_batch(x, y, seed, 0, t, first, min(batch_size, n - first)), lr)
         return loss
 
+    def _scale(self, rows: int) -> float:
+        """S for a mini-batch of that many rows.  What is looked at is always the update _LAG steps back, whether the device is
+        ahead or behind: equal runs give equal bits."""
+        if self.dtype is not torch.float16:
+            return 1.0
+        if self._steps >= _LAG and not torch.cuda.is_current_stream_capturing():
+            k = self._steps % _LAG
+            self._counted[k].synchronize()
+            left_out = int(self._counts[k, 1])
+            if left_out > self._left_out and self._steps - _LAG >= self._lowered_at:  # (taken with the present S)
+                self._lowered, self._lowered_at = max(self._lowered / 4, _LEAST), self._steps
+            self._left_out = left_out
+        if self.loss_scale is not None:
+            return self.loss_scale * self._lowered
+        return (1.0 if rows <= 128 else 2.0 ** min(rows.bit_length() - 1, 13)) * self._lowered
+
     def step(self, x: torch.Tensor, y: torch.Tensor, lr: float) -> torch.Tensor:
-        """One update from the rows of one mini-batch; returns the loss of each."""
+        """One update from the rows of one mini-batch; returns the loss of each.  (A step captured into a graph keeps the S of its
+        capture.)"""
+        scale = self._scale(x.shape[0])
         logits, saved = ops.gated_ffn(x, *self.weights, self.activation, save=True)
-        residual, loss = ops.softmax_residual(logits, y)
+        residual, loss = ops.softmax_residual(logits, y, None if scale == 1.0 else scale / max(x.shape[0], 1))
         _, *grads = ops.gated_ffn_backward(residual, x, *self.weights, saved, self.activation, need_dx=False)
-        ops.adamw_step(self.weights, grads, lr=lr, masters=self.masters, **self.state, **self._rule)
+        ops.adamw_step(self.weights, grads, lr=lr, masters=self.masters, grad_scale=1.0 / scale, **self.state, **self._rule)
+        if self.dtype is torch.float16 and not torch.cuda.is_current_stream_capturing():
+            k = self._steps % _LAG
+            with torch.cuda.device(self.device):
+                self._counts[k].copy_(self.state["control"], non_blocking=True)
+                self._counted[k].record()
+            self._steps += 1
         return loss
 
     def logits(self, x: torch.Tensor) -> torch.Tensor:

@@ -219,7 +219,11 @@ def stream_check(stream: Optional[torch.cuda.Stream] = None) -> None:
 def softmax_residual(logits: torch.Tensor, y: torch.Tensor, scale: Optional[float] = None,
                      stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(residual, loss) for logits [rows, C] and int32 labels y [rows]: scale (softmax - onehot), and the loss per row in
-    fp32.  scale defaults to 1 / rows, the mean gradient of the mini-batch.  Rows without a label in [0, C) give zeros."""
+    fp32.  scale defaults to 1 / rows, the mean gradient of the mini-batch.  Rows without a label in [0, C) give zeros.
+
+    float16 has too few exponents for the default over many rows: values below 6e-5 lose bits, those below 3e-8 are zero, and what
+    gated_ffn_backward makes of them is smaller still.  Give it S / rows with a power of two S near the number of rows, and
+    adamw_step grad_scale=1 / S."""
     device = _device_of(logits, "logits")
     if logits.dtype not in _TYPES:
         raise ValueError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")

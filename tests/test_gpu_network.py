@@ -176,3 +176,73 @@ def test_buffers_are_not_loaded_on_another_device():
     net = GatedSoftmax(8, 16, 1, 32, 4)
     with pytest.raises(ValueError, match="stream"):
         net.load_buffer(x.pin_memory(), y.pin_memory(), stream=types.SimpleNamespace(device=torch.device("cuda", 1)))
+
+
+def known_classes(net, rows, seed=0):
+    """Rows close to their class's centre, and output weights that give every row's label odds of about e^9: all residuals are small."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    centres = torch.randn(net.C, net.p, generator=gen, device="cuda")
+    y = torch.randint(0, net.C, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    x = (centres[y.long()] + 0.02 * torch.randn(rows, net.p, generator=gen, device="cuda")).half()
+    h = hidden(net, centres.double())
+    net.set_theta([net.masters[0], net.masters[1], 9.0 * torch.linalg.pinv(h)])
+    return x, y
+
+
+def hidden(net, x):
+    g = x @ net.weights[0].double()
+    return g * torch.sigmoid(g) * (x @ net.weights[1].double())
+
+
+@pytest.mark.parametrize("rows,loss_scale", [(100, 64.0), (256, None), (1000, None), (8192, None), (20000, None)])
+def test_gradients_in_fp16_of_rows_that_are_known_well(rows, loss_scale):
+    """The first moments after one step are (1 - a) times the gradient of the mean loss: each of the three as a whole against 64 bits.
+
+    Logits of up to 16 are rounded to fp16 by at most 2^-8, which moves a probability, odds of two of them, by 2^-7 of itself.  The
+    residual, H or dG and dU, and the weights' gradients are rounded by 2^-11 of each value; sums over rows and classes of
+    either sign may make the first two count for more: 2^-8 allows seven besides the last.  Values below fp16's
+    normal ones are not allowed for.  (Without a scale a restatement has errors of 0.03 at 256 rows to 0.8 at 20,000.)"""
+    net = GatedSoftmax(rows, 128, 1, 256, 10, dtype=torch.float16, seed=1, loss_scale=loss_scale)
+    x, y = known_classes(net, rows)
+    leaves = [w.double().requires_grad_() for w in net.weights]
+    xd = x.double()
+    g = xd @ leaves[0]
+    loss = torch.nn.functional.cross_entropy((g * torch.sigmoid(g) * (xd @ leaves[1])) @ leaves[2], y.long())
+    loss.backward()
+    assert float(loss.detach()) < 1e-2  # known well, as this test means it
+    net.step(x, y, 1e-4)
+    assert net.state["control"].tolist()[:2] == [1, 0]
+    for m, leaf in zip(net.state["m"], leaves):
+        err = float((m.double() / 0.1 - leaf.grad).norm() / leaf.grad.norm())
+        assert err < 2.0 ** -7 + 2.0 ** -8, err
+
+
+def test_scale_in_fp16_falls_where_gradients_overflow():
+    """Hidden values of about 2,600 and one label: dWd is -0.75 times their mean at first and S times that, 499,000 with S = 256,
+    overflows; so does 125,000 with S = 64, not 31,000 with S = 16.  The first two times eight updates are left out, the others
+    taken; the same twice over, whether or not the host waits in between."""
+    nets = [GatedSoftmax(256, 32, 1, 64, 4, dtype=torch.float16, activation=ops.ACT_RELU, seed=2) for _ in range(2)]
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = (torch.randn(256, 32, generator=gen, device="cuda").abs() * 40).half()
+    y = torch.zeros(256, device="cuda", dtype=torch.int32)
+    for net in nets:
+        net.set_theta([torch.full_like(net.masters[0], 0.05), torch.full_like(net.masters[1], 0.05), torch.zeros_like(net.masters[2])])
+    start = nets[0].get_theta()
+    for t in range(60):
+        nets[0].step(x, y, 1e-6)
+        nets[1].step(x, y, 1e-6)
+        torch.cuda.synchronize()
+        if t < 8:  # nothing has been looked at yet
+            assert nets[1].state["control"].tolist()[:2] == [0, t + 1]
+    taken, left_out = nets[0].state["control"].tolist()[:2]
+    assert (taken, left_out) == (44, 16)
+    assert torch.equal(nets[0].state["control"], nets[1].state["control"])
+    for a, b, s in zip(nets[0].get_theta(), nets[1].get_theta(), start):
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+    assert not torch.equal(nets[0].get_theta()[2], start[2])
+
+
+def test_loss_scale_is_for_fp16():
+    for kw in (dict(loss_scale=2.0), dict(dtype=torch.float16, loss_scale=0.0), dict(dtype=torch.float16, loss_scale=float("inf"))):
+        with pytest.raises(ValueError, match="loss_scale"):
+            GatedSoftmax(8, 16, 1, 32, 4, **kw)
