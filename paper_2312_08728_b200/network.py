@@ -74,7 +74,7 @@ class GatedSoftmax:
 
     def load_buffer(self, host_x: torch.Tensor, host_y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Start copying one buffer (pinned host tensors, labels int32) into the next slot on `stream`, behind the last
-        computation that read that slot; returns the slot."""
+        computation that read that slot and the last copy into it; returns the slot."""
         if host_x.device.type != "cpu" or host_y.device.type != "cpu":
             raise ValueError("load_buffer takes host tensors")
         self._check(host_x, host_y)
@@ -92,13 +92,16 @@ class GatedSoftmax:
             self._freed[s].record(current)  # (new memory may still be in use by work issued before)
         x, y = self._slots[s]
         copy.wait_event(self._freed[s])
+        copy.wait_event(self._loaded[s])  # (a slot may be loaded again without having been trained on, on another stream)
         self._count[s] = 0  # (nothing to train on, should a copy fail)
-        with torch.cuda.stream(copy):
-            x[:rows].copy_(host_x, non_blocking=True)
-            y[:rows].copy_(host_y, non_blocking=True)
-        x.record_stream(copy)  # (the model may be dropped while a copy is under way)
-        y.record_stream(copy)
-        self._loaded[s].record(copy)
+        try:
+            with torch.cuda.stream(copy):
+                x[:rows].copy_(host_x, non_blocking=True)
+                y[:rows].copy_(host_y, non_blocking=True)
+        finally:  # (if the second copy fails the first is under way all the same)
+            x.record_stream(copy)  # (the model may be dropped while a copy is under way)
+            y.record_stream(copy)
+            self._loaded[s].record(copy)
         self._count[s] = rows
         self._next ^= 1
         return s

@@ -246,3 +246,45 @@ def test_loss_scale_is_for_fp16():
     for kw in (dict(loss_scale=2.0), dict(dtype=torch.float16, loss_scale=0.0), dict(dtype=torch.float16, loss_scale=float("inf"))):
         with pytest.raises(ValueError, match="loss_scale"):
             GatedSoftmax(8, 16, 1, 32, 4, **kw)
+
+
+def test_a_slot_loaded_again_on_another_stream():
+    """Three loads without a round in between, on three streams, the first of them held up: the third, into the same slot, is
+    behind it, and the slot holds what was loaded last."""
+    net = GatedSoftmax(128, 32, 2, 64, 4)
+    held, other, last = (torch.cuda.Stream() for _ in range(3))
+    parts = [(torch.full((64, 32), k, dtype=torch.bfloat16).pin_memory(), torch.full((64,), k, dtype=torch.int32).pin_memory()) for k in range(3)]
+    net.load_buffer(*parts[0]); net.load_buffer(*parts[0])    # (memory for the slots, before a kernel holds a stream)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(held):
+        torch.cuda._sleep(100_000_000)
+    slots = [net.load_buffer(*part, stream=s) for part, s in zip(parts, (held, other, last))]
+    assert slots == [0, 1, 0]
+    assert not net._loaded[0].query()                         # the last copy waits for the one that is held up
+    torch.cuda.synchronize()
+    x, y = net._slots[0]
+    assert bool((x == 2).all()) and bool((y == 2).all())
+
+
+def test_a_copy_that_fails_is_waited_for(monkeypatch):
+    """The labels' copy fails behind the rows': the next load of the slot, on another stream, is behind the rows' copy."""
+    net = GatedSoftmax(64, 32, 1, 64, 4)
+    x, y = torch.ones(64, 32, dtype=torch.bfloat16).pin_memory(), torch.ones(64, dtype=torch.int32).pin_memory()
+    slot = net.load_buffer(x, y)
+    net.load_buffer(x, y)
+    torch.cuda.synchronize()
+    held = torch.cuda.Stream()
+    with torch.cuda.stream(held):
+        torch.cuda._sleep(100_000_000)
+    real = net._slots[slot]
+    net._slots[slot] = (real[0], types.SimpleNamespace(__getitem__=None, record_stream=lambda s: None))  # no labels can be copied here
+    with pytest.raises(TypeError):
+        net.load_buffer(x, y, stream=held)
+    assert not net._loaded[slot].query()
+    net._slots[slot] = real
+    with pytest.raises(Exception):
+        net.run_rounds(slot, 1, 16, 0.1, 0)                   # nothing whole to train on
+    again = torch.cuda.Stream()
+    assert net.load_buffer(x + 1, y, stream=again) == slot
+    torch.cuda.synchronize()
+    assert bool((net._slots[slot][0] == 2).all())
