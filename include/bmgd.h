@@ -141,6 +141,7 @@ int bmgd_destroy(bmgd_t* h);
  * can be issued while an earlier buffer is still being computed on.  *slot receives the slot
  * id.  The host arrays must stay valid until the copy has run (bmgd_sync, or a
  * synchronisation of `stream`); they must be pinned for the copy to overlap with compute.
+ * The copy is ordered behind the last computation that read the slot and the last copy into it.
  * Errors: BMGD_ERR_CAPACITY if rows exceeds ceil(N/K); BMGD_ERR_STATE without slots.
  */
 int bmgd_load_buffer(bmgd_t* h, const void* host_x, const void* host_y, int64_t rows,

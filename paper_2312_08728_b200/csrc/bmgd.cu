@@ -716,8 +716,10 @@ int bmgd_load_buffer(bmgd_t* h, const void* host_x, const void* host_y, int64_t 
     if (!guard.ok) return cuda_fail(h, cudaErrorInvalidDevice);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const int s = h->next_slot;
-    // the kernel that last read this slot must be done before the slot is overwritten
-    if (h->slot_has_data[s]) BMGD_CUDA(h, cudaStreamWaitEvent(cs, h->freed[s], 0));
+    // the kernel that last read this slot must be done before the slot is overwritten, and so must the last copy into it: a
+    // slot may be loaded again, on another stream, without having been trained on.  (An event not yet recorded holds nothing up.)
+    BMGD_CUDA(h, cudaStreamWaitEvent(cs, h->freed[s], 0));
+    BMGD_CUDA(h, cudaStreamWaitEvent(cs, h->loaded[s], 0));
     EventPair ep{};
     const bool timing = (h->cfg.flags & BMGD_FLAG_TIMING) != 0;
     if (timing) {
@@ -726,8 +728,14 @@ int bmgd_load_buffer(bmgd_t* h, const void* host_x, const void* host_y, int64_t 
         BMGD_CUDA(h, cudaEventRecord(ep.a, cs));
     }
     const size_t xbytes = (size_t)rows * h->cfg.p * h->xb, ybytes = (size_t)rows * h->yb;
-    BMGD_CUDA(h, cudaMemcpyAsync(h->base + h->lay.slot_x[s], host_x, xbytes, cudaMemcpyHostToDevice, cs));
-    BMGD_CUDA(h, cudaMemcpyAsync(h->base + h->lay.slot_y[s], host_y, ybytes, cudaMemcpyHostToDevice, cs));
+    h->slot_has_data[s] = false;  // nothing whole to train on, should a copy fail
+    cudaError_t e = cudaMemcpyAsync(h->base + h->lay.slot_x[s], host_x, xbytes, cudaMemcpyHostToDevice, cs);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(h->base + h->lay.slot_y[s], host_y, ybytes, cudaMemcpyHostToDevice, cs);
+    if (e != cudaSuccess) {
+        cudaEventRecord(h->loaded[s], cs);  // the first copy may be under way
+        if (timing) h->event_pool.push_back(ep);
+        return cuda_fail(h, e);
+    }
     if (timing) {
         BMGD_CUDA(h, cudaEventRecord(ep.b, cs));
         h->copy_events.push_back(ep);
