@@ -380,9 +380,16 @@ typedef struct bmgd_adamw_config {
 int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_adamw_config* cfg, void* dev_control,
                     void* dev_scratch, int64_t scratch_bytes, void* stream);
 
-/* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block kernel on the current
- * device gave up since the last report: the outputs of that call are void. */
+/* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block kernel on the current device
+ * gave up since the last report (to whichever stream's caller asks first; none is lost): the outputs of that call are
+ * void.  Calls before and after it, and on other streams, are not touched by it. */
 int bmgd_stream_check(void* stream);
+
+/* A pass whose kernels fetch no more than `fills` pieces of their operands per CTA and give up any single wait after budget_ms
+ * (at most 1000): they run out of time as they would waiting for copies that never land, and return.  For testing the
+ * error path without hanging or faulting a GPU. */
+int bmgd_debug_gated_ffn_timeout(const bmgd_gated_ffn* g, int32_t pass, void* workspace, int64_t workspace_bytes, int32_t fills,
+                                 double budget_ms, void* stream);
 
 /* Text for a bmgd_status; never NULL. */
 const char* bmgd_strerror(int status);

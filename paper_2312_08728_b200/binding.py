@@ -34,7 +34,7 @@ EXPORTS = (
     "bmgd_version", "bmgd_run_rounds_noalloc", "bmgd_debug_wait_timeout", "bmgd_partition_index", "bmgd_gather_buffer",
     "bmgd_set_optimizer", "bmgd_set_lr_schedule", "bmgd_set_timeout", "bmgd_debug_null_rounds",
     "bmgd_gated_ffn_workspace_bytes", "bmgd_gated_ffn_forward", "bmgd_gated_ffn_backward", "bmgd_softmax_residual",
-    "bmgd_gather_batch", "bmgd_adamw_step", "bmgd_stream_check",
+    "bmgd_gather_batch", "bmgd_adamw_step", "bmgd_stream_check", "bmgd_debug_gated_ffn_timeout",
 )
 
 OPT_SGD, OPT_NESTEROV, OPT_ADAM = 0, 1, 2
@@ -125,6 +125,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.bmgd_gather_batch.argtypes = [vp, i64, vp, i64, u64, u32, u32, i64, i64, vp, vp, vp]
     L.bmgd_adamw_step.argtypes = [vp, i32, vp, vp, vp, i64, vp]
     L.bmgd_stream_check.argtypes = [vp]
+    L.bmgd_debug_gated_ffn_timeout.argtypes = [vp, i32, vp, i64, i32, dbl, vp]
     for name in EXPORTS:
         if getattr(L, name).restype is None or name in ("bmgd_strerror",):
             continue

@@ -54,12 +54,14 @@ struct FfnParams {
     long long ld_save;
     int type, act;
     int early;               // many rows: this launch needs nothing of the one before it, only of those before that
-    int* status;
+    unsigned fills;          // stages of its ring that a CTA fills: as many as there are, fewer only to test how waits run out
+    unsigned* gave_up;       // counts waits that ran out of time
     unsigned long long timeout_ns;
 };
 
+// A wait with a limit of its own: that one kernel gave up says nothing about the others, on this stream or another.
 struct FfnWait {
-    int* status;
+    unsigned* gave_up;
     unsigned long long timeout_ns;
     bool aborted;
 };
@@ -68,8 +70,8 @@ __device__ __forceinline__ void ffn_wait(uint32_t bar, uint32_t parity, FfnWait&
     const unsigned long long t0 = global_ns();
     uint32_t spins = 0;
     while (!mbar_try_wait(bar, parity)) {
-        if ((++spins & 0xFFu) == 0u && (global_ns() - t0 >= w.timeout_ns || ((volatile int*)w.status)[0] != 0)) {
-            atomicCAS(w.status, 0, kStatusTimeout);
+        if ((++spins & 0xFFu) == 0u && global_ns() - t0 >= w.timeout_ns) {
+            atomicAdd(w.gave_up, 1u);
             w.aborted = true;
             return;
         }
@@ -282,21 +284,22 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
         m0 = (int)(first + r2 % gm) * (128 * CG);
         n0 = (int)(r2 / gm) * kCols;
     };
-    FfnWait w{P.status, P.timeout_ns, false};
+    FfnWait w{P.gave_up, P.timeout_ns, false};
 
     if (warp == 0) {
         if (lane == 0) {
             int s = 0;
             uint32_t phase = 0;
-            for (long long t = pair; t < tiles && !w.aborted; t += pairs) {
+            unsigned left = P.fills;
+            for (long long t = pair; t < tiles && !w.aborted && left != 0; t += pairs) {
                 int which, m0, n0;
                 place(t, which, m0, n0);
                 const FfnProblem& q = P.p[which];
                 const int am = m0 + (int)rank * 128, K = q.K, segments = q.segments;
-                for (int seg = 0; seg < segments && !w.aborted; ++seg) {
+                for (int seg = 0; seg < segments && !w.aborted && left != 0; ++seg) {
                     const CUtensorMap* const map_a = &q.a[seg];
                     const CUtensorMap* const map_b = EPI == kEpiGated ? &q.b[rank] : &q.b[seg];
-                    for (int k0 = 0; k0 < K; k0 += kFfnBK) {
+                    for (int k0 = 0; k0 < K && left != 0; k0 += kFfnBK, --left) {
                         ffn_wait(empty + 8 * s, phase ^ 1u, w);
                         if (w.aborted) break;
                         uint32_t bar = full + 8 * s;
@@ -643,10 +646,11 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
 
     const int kblocks = (q.K + kFfnBK - 1) / kFfnBK, steps = kblocks * q.segments;
     const int first = (int)((long long)steps * part / S), last = (int)((long long)steps * (part + 1) / S);
-    FfnWait w{P.status, P.timeout_ns, false};
+    FfnWait w{P.gave_up, P.timeout_ns, false};
     if (warp == 0) {
         if (lane == 0) {
             const bool a_mn = q.a_mn;
+            const int fill_to = (int)min((long long)last, (long long)first + P.fills);
             auto weights = [&](int k, int s) {
                 const int seg = k >= kblocks ? 1 : 0, k0 = (k - seg * kblocks) * kFfnBK;
                 const uint32_t bar = full + 8 * s, sa = ring + s * F::kStage;
@@ -660,12 +664,12 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
             };
             int ahead = 0;
             if (early) {
-                for (; ahead < F::kStages && first + ahead < last; ++ahead) weights(first + ahead, ahead);
+                for (; ahead < F::kStages && first + ahead < fill_to; ++ahead) weights(first + ahead, ahead);
                 wait_for_previous_kernel();
             }
             int s = 0;
             uint32_t phase = 0;
-            for (int k = first; k < last; ++k) {
+            for (int k = first; k < fill_to; ++k) {
                 if (k - first >= ahead) {
                     ffn_wait(empty + 8 * s, phase ^ 1u, w);
                     if (w.aborted) break;

@@ -11,8 +11,9 @@ namespace {
 
 using namespace bmgdk;
 
-// Set by a kernel whose wait ran out of time; read and cleared by bmgd_stream_check.
-__device__ int g_ffn_status[2];
+// Waits that ran out of time on this device, ever.  Only counted up: what bmgd_stream_check has reported is kept on the host,
+// so that no report can wipe out another.
+__device__ unsigned g_ffn_gave_up;
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -55,7 +56,9 @@ int make_map(const Matrix& m, int type, int box_rows, CUtensorMap* out) {
 constexpr int kMaxDevices = 64;
 struct Device {
     int index, sms, smem;
-    int* status;
+    unsigned* gave_up;
+    unsigned fills;                // see FfnParams
+    unsigned long long budget_ns;  // of any single wait inside a kernel; 0: wait_bound
 };
 int current_device(Device* d) {
     static Device known[kMaxDevices];
@@ -67,11 +70,13 @@ int current_device(Device* d) {
     d->index = dev;
     if (cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&d->smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess ||
-        cudaGetSymbolAddress(&p, g_ffn_status) != cudaSuccess) {
+        cudaGetSymbolAddress(&p, g_ffn_gave_up) != cudaSuccess) {
         cudaGetLastError();
         return BMGD_ERR_CUDA;
     }
-    d->status = static_cast<int*>(p);
+    d->gave_up = static_cast<unsigned*>(p);
+    d->fills = ~0u;
+    d->budget_ns = 0;
     static std::mutex one;
     std::lock_guard<std::mutex> hold(one);
     if (dev >= 0 && dev < kMaxDevices && !ready[dev].load(std::memory_order_relaxed)) {
@@ -92,7 +97,7 @@ int allow_smem(K* fn, int bytes, const Device& dev, std::atomic<unsigned long lo
 }
 
 // Bound on any single wait inside a kernel: two seconds, and more than a step of the contraction ever takes for each step.
-unsigned long long wait_bound(int64_t steps) { return 2000000000ull + 10000ull * (unsigned long long)steps; }
+unsigned long long wait_bound(const Device& dev, int64_t steps) { return dev.budget_ns ? dev.budget_ns : 2000000000ull + 10000ull * (unsigned long long)steps; }
 
 // One contraction as the host describes it: out [M][N] = sum over segments of a[s] b[s].
 struct Problem {
@@ -142,7 +147,7 @@ int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, 
     }
     P.problems = count;
     P.tiles = tiles;
-    P.timeout_ns = wait_bound(steps);
+    P.timeout_ns = wait_bound(dev, steps);
     auto* fn = ffn_kernel<CG, BN, EPI, A_MN, B_MN>;
     static std::atomic<unsigned long long> allowed{0};
     const int rc = allow_smem(fn, S::kSmem, dev, allowed);
@@ -170,7 +175,7 @@ int launch_few(FfnParams& P, const Problem& x, int split, bool early, const Devi
     q.a_mn = W_MN; q.vec = x.vec;
     q.tiles_m = (int)((x.M + NR - 1) / NR);
     q.tiles_n = (x.N + kFewPart - 1) / kFewPart;
-    P.timeout_ns = wait_bound((int64_t)x.segments * x.K / kFfnBK);
+    P.timeout_ns = wait_bound(dev, (int64_t)x.segments * x.K / kFfnBK);
     auto* fn = ffn_few_kernel<NR, EPI>;
     static std::atomic<unsigned long long> allowed{0};
     const int rc = allow_smem(fn, F::kSmem, dev, allowed);
@@ -315,7 +320,7 @@ int forward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev, 
     void* h = g->saved_hidden ? g->saved_hidden : space->take(g->rows * ldh * 2);
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = dev.status;
+    P.type = g->type; P.act = g->activation; P.gave_up = dev.gave_up; P.fills = dev.fills;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     const Problem gated{{x, x}, {wg, wu}, h, ldh, g->rows, g->hidden, g->inputs, 1, true};
     rc = contract<kEpiGated, true>(P, gated, false, dev, s);
@@ -336,7 +341,7 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     const Matrix h{g->saved_hidden, n, g->hidden, g->ld_saved}, dg{space->take(n * ldh * 2), n, g->hidden, ldh}, du{space->take(n * ldh * 2), n, g->hidden, ldh};
     if (!run) return BMGD_OK;
     FfnParams P{};
-    P.type = g->type; P.act = g->activation; P.status = dev.status;
+    P.type = g->type; P.act = g->activation; P.gave_up = dev.gave_up; P.fills = dev.fills;
     P.value = g->saved_value; P.slope = g->saved_slope; P.ld_save = g->ld_saved;
     P.out_up = const_cast<void*>(du.base);
     // dH, and from it dG and dU
@@ -356,7 +361,8 @@ int backward(const bmgd_gated_ffn* g, Space* space, bool run, const Device& dev,
     return contract_many<kEpiPlain, true, true>(P, weights, 3, dev, s);
 }
 
-int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspace_bytes, void* stream) {
+int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspace_bytes, void* stream, unsigned fills = ~0u,
+             unsigned long long budget_ns = 0) {
     int rc = check(g, pass, true);
     if (rc != BMGD_OK) return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -376,6 +382,8 @@ int run_pass(const bmgd_gated_ffn* g, int pass, void* workspace, int64_t workspa
     if (workspace_bytes < need.used) return BMGD_ERR_CAPACITY;
     rc = current_device(&dev);
     if (rc != BMGD_OK) return rc;
+    dev.fills = fills;
+    dev.budget_ns = budget_ns;
     Space space{static_cast<unsigned char*>(workspace), 0};
     return pass == BMGD_FFN_FORWARD ? forward(g, &space, true, dev, s) : backward(g, &space, true, dev, s);
 }
@@ -403,14 +411,29 @@ int bmgd_gated_ffn_backward(const bmgd_gated_ffn* g, void* workspace, int64_t wo
     return run_pass(g, BMGD_FFN_BACKWARD, workspace, workspace_bytes, stream);
 }
 
+int bmgd_debug_gated_ffn_timeout(const bmgd_gated_ffn* g, int32_t pass, void* workspace, int64_t workspace_bytes, int32_t fills,
+                                 double budget_ms, void* stream) {
+    if (fills < 0 || !(budget_ms > 0.0) || budget_ms > 1000.0) return BMGD_ERR_ARG;
+    return run_pass(g, pass, workspace, workspace_bytes, stream, (unsigned)fills, (unsigned long long)(budget_ms * 1e6));
+}
+
 int bmgd_stream_check(void* stream) {
-    if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
-    int st[2] = {0, 0};
-    if (cudaMemcpyFromSymbol(st, g_ffn_status, sizeof st) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
-    if (st[0] == 0) return BMGD_OK;
-    const int zero[2] = {0, 0};
-    cudaMemcpyToSymbol(g_ffn_status, zero, sizeof zero);
-    return st[0];
+    static std::mutex one;
+    static unsigned reported[kMaxDevices];
+    Device dev{};
+    const int rc = current_device(&dev);
+    if (rc != BMGD_OK) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    unsigned count = 0;
+    if (cudaMemcpyAsync(&count, dev.gave_up, sizeof count, cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+        cudaGetLastError();
+        return BMGD_ERR_CUDA;
+    }
+    std::lock_guard<std::mutex> hold(one);
+    unsigned& known = reported[dev.index & (kMaxDevices - 1)];
+    if ((int)(count - known) <= 0) return BMGD_OK;  // (another thread may have read, and reported, a later count)
+    known = count;
+    return BMGD_ERR_TIMEOUT;
 }
 
 }  // extern "C"

@@ -208,7 +208,7 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
 
 
 def stream_check(stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Wait for the stream and raise if a device-side wait of a gated-block kernel on its device gave up."""
+    """Wait for the stream and raise, once, if a device-side wait of a gated-block kernel on its device gave up."""
     s = stream if stream is not None else torch.cuda.current_stream()
     with torch.cuda.device(s.device):
         _status(_binding.load_library().bmgd_stream_check(s.cuda_stream), "bmgd_stream_check")
