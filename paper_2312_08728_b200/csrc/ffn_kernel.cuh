@@ -78,6 +78,39 @@ __device__ __forceinline__ void ffn_wait(uint32_t bar, uint32_t parity, FfnWait&
     }
 }
 
+// Parity of the last round of stage `i` of a ring, `s` and `phase` being the stage and the round's parity that come next; 1
+// for a stage without a round, which a barrier takes for completed.
+constexpr __host__ __device__ uint32_t ffn_last_round(int i, int s, uint32_t phase) { return i < s ? phase : phase ^ 1u; }
+constexpr bool ffn_last_round_holds() {
+    for (int stages = 1; stages <= 10; ++stages)
+        for (int fills = 0; fills <= 35; ++fills) {
+            int s = 0;
+            uint32_t phase = 0;
+            for (int k = 0; k < fills; ++k)
+                if (++s == stages) { s = 0; phase ^= 1u; }
+            for (int i = 0; i < stages; ++i) {
+                const int rounds = fills / stages + (i < fills % stages ? 1 : 0);
+                if (ffn_last_round(i, s, phase) != (rounds == 0 ? 1u : (uint32_t)(rounds - 1) & 1u)) return false;
+            }
+        }
+    return true;
+}
+static_assert(ffn_last_round_holds(), "a drained ring waits for the last round of every stage");
+// A block leaves only when its copies have landed and its products are done, whoever of its warps gave up: the thread that
+// issued them waits for the last round of every stage (in a launch that went well they are complete), with a limit again.
+constexpr unsigned long long kFfnDrainNs = 1000000000ull;
+__device__ __forceinline__ void ffn_drain(uint32_t bars, int stages, int s, uint32_t phase, const FfnWait& w) {
+    FfnWait d{w.gave_up, kFfnDrainNs, false};
+    for (int i = 0; i < stages; ++i) ffn_wait(bars + 8 * i, ffn_last_round(i, s, phase), d);
+}
+// What ffn_drain does not see after a wait was given up, it leaves time for: copies of a pair's second CTA that the first
+// one, stopped earlier, had not announced, and arrivals on their way to the other CTA's barriers.
+constexpr unsigned long long kFfnLingerNs = 1000000ull;
+__device__ __forceinline__ void ffn_linger() {
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < kFfnLingerNs) __nanosleep(1000);
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // A kernel launched as a dependent of the one before it may start while that one still runs; before it touches memory it
 // waits until that one has finished (and with it all before).
@@ -321,6 +354,7 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                     }
                 }
             }
+            if (rank == 0) ffn_drain(full, S::kStages, s, phase, w);  // (copies of both CTAs: the other one waits for this one below)
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -350,6 +384,7 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
                 ffn_commit<CG>(acc_full + 8 * acc);
                 if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
+            ffn_drain(empty, S::kStages, s, phase, w);
         }
     } else if (warp >= 4) {
         // A lane reads a row out of tensor memory; what a warp writes to (or reads from) global memory at a time should be
@@ -504,10 +539,7 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
         }
     }
     __syncwarp();
-    if (__any_sync(0xFFFFFFFFu, w.aborted)) {  // given up: copies and products may still be in flight
-        const unsigned long long t0 = global_ns();
-        while (global_ns() - t0 < kSmxLingerNs) __nanosleep(1000);
-    }
+    if (__any_sync(0xFFFFFFFFu, w.aborted)) ffn_linger();
     tc_fence_before();
     __syncthreads();
     if constexpr (CG == 2) { cluster_arrive_release(); cluster_wait_acquire(); }
@@ -678,6 +710,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
                 rows(k, s);
                 if (++s == F::kStages) { s = 0; phase ^= 1u; }
             }
+            ffn_drain(full, F::kStages, s, phase, w);
         }
     } else if (warp == 1) {
         if (lane == 0) {
@@ -699,7 +732,8 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
                 ffn_commit<1>(empty + 8 * s);
                 if (++s == F::kStages) { s = 0; phase ^= 1u; }
             }
-            if (!w.aborted) ffn_commit<1>(done);
+            if (!w.aborted) ffn_commit<1>(done);  // (waited for below)
+            else ffn_drain(empty, F::kStages, s, phase, w);
         }
     }
     __syncwarp();
@@ -741,10 +775,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
         else if (S <= 4) few_finish<4, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
         else few_finish<8, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
     }
-    if (given_up) {  // copies and products may still be in flight
-        const unsigned long long t0 = global_ns();
-        while (global_ns() - t0 < kSmxLingerNs) __nanosleep(1000);
-    }
+    if (given_up) ffn_linger();
     __syncthreads();
     if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }  // peers have read this CTA's sums
     tc_fence_after();

@@ -39,7 +39,7 @@ def starve(b, fills, budget_ms=5.0):
     return out
 
 
-@pytest.mark.parametrize("fills", [0, 2])
+@pytest.mark.parametrize("fills", [0, 1, 2])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
 def test_a_wait_that_runs_out_touches_no_other_call(shape, fills):
     b = Block(*shape, torch.bfloat16, ops.ACT_SILU, seed=1)
