@@ -381,8 +381,8 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
                     void* dev_scratch, int64_t scratch_bytes, void* stream);
 
 /* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block kernel on the current device
- * gave up since the last report (to whichever stream's caller asks first; none is lost): the outputs of that call are
- * void.  Calls before and after it, and on other streams, are not touched by it. */
+ * gave up since the last report (to whichever stream's caller asks first; none is lost).  What that call had not
+ * computed by then is NaN in its outputs.  Calls before and after it, and on other streams, are not touched by it. */
 int bmgd_stream_check(void* stream);
 
 /* A pass whose kernels fetch no more than `fills` pieces of their operands per CTA and give up any single wait after budget_ms

@@ -177,6 +177,10 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
     tmem_load16(addr + 16, r + 16);
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void fill_nan(uint32_t (&r)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = 0x7FC00000u;
+}
 
 // ---------------------------------------------------------------- activation
 // act(g) and act'(g) in fp32 (silu g s, gelu g Phi(g), relu, sigmoid s; s = 1 / (1 + exp(-g)))
@@ -402,10 +406,22 @@ __global__ void __launch_bounds__(FfnReadOut<EPI>::kThreads, 1) ffn_kernel(const
             uint16_t* const out = static_cast<uint16_t*>(q.out);
             ffn_wait(acc_full + 8 * acc, acc_phase, w);
             w.aborted = __any_sync(0xFFFFFFFFu, w.aborted);
-            if (w.aborted) break;
-            tc_fence_after();
             const long long row0 = (long long)m0 + rank * 128 + quarter * 32;
             const int rows = (int)min(32ll, q.M - row0);  // (may be negative)
+            if (w.aborted) {  // this warp's part of this tile, and of those that follow, has not been computed: NaN
+                for (int c = part * R::kCols; c < kCols; c += 2 * R::kCols)
+#pragma unroll 1
+                    for (int k = lane; k < rows * R::kCols; k += 32) {
+                        const int col = n0 + c + k % R::kCols;
+                        const long long row = row0 + k / R::kCols;
+                        if (col >= N) continue;
+                        out[row * ld_out + col] = 0x7FFFu;  // (in either 16-bit type)
+                        if constexpr (EPI == kEpiBackward) static_cast<uint16_t*>(P.out_up)[row * ld_out + col] = 0x7FFFu;
+                        if (EPI == kEpiGated && P.value) P.value[row * P.ld_save + col] = P.slope[row * P.ld_save + col] = __uint_as_float(0x7FC00000u);
+                    }
+                continue;
+            }
+            tc_fence_after();
             const uint32_t ta = tmem + (uint32_t)(acc * BN) + ((uint32_t)(quarter * 32) << 16);
             if constexpr (EPI == kEpiGated) {
                 // 16 columns of G and 16 of U at a time; then a lane has four columns of rows lane / 4, lane / 4 + 8, ...
@@ -762,6 +778,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
             uint32_t r[16];
             tmem_load16(ta + (uint32_t)(h * NR + base + col), r);
             tmem_wait();
+            if (given_up) fill_nan(r);  // (every CTA of the cluster adds them, so all of the tile's outputs are NaN)
 #pragma unroll
             for (int i = 0; i < 16; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)((c + i) * kFewPart * 4)), "r"(r[i]) : "memory");
         }
@@ -769,7 +786,7 @@ __global__ void __launch_bounds__(kFewThreads, FewShape<NR, EPI>::kCtasPerSm) ff
         __syncthreads();
         if (S > 1) { cluster_arrive_release(); cluster_wait_acquire(); }
         // each CTA finishes its share of the rows
-        const int some = given_up ? 0 : min(F::kPassRows, rows - base);
+        const int some = min(F::kPassRows, rows - base);
         if (S == 1) few_finish<1, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
         else if (S == 2) few_finish<2, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);
         else if (S <= 4) few_finish<4, F::kPassRows, EPI>(P, q, ring, S, part, warp, lane, f, r0 + base, some);

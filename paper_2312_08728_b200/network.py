@@ -190,5 +190,6 @@ class GatedSoftmax:
             w.copy_(m)
 
     def sync(self) -> None:
-        """Wait for everything issued on the current stream and report a device-side error if one was raised."""
+        """Wait for everything issued on the current stream and report a device-side error if one was raised (the step concerned
+        has NaN for gradients then, and so have the weights after it unless max_norm is given, which leaves such an update out)."""
         ops.stream_check(torch.cuda.current_stream(self.device))

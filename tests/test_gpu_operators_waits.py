@@ -39,6 +39,26 @@ def starve(b, fills, budget_ms=5.0):
     return out
 
 
+@pytest.mark.parametrize("dtype,act", [(torch.bfloat16, ops.ACT_SILU), (torch.float16, ops.ACT_RELU)], ids=["bf16-silu", "fp16-relu"])
+@pytest.mark.parametrize("fills", [0, 1, 8])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_what_was_not_computed_is_nan(shape, fills, dtype, act):
+    """No output keeps what its memory held, or holds a part of a sum: each is right or NaN."""
+    b = Block(*shape, dtype, act, seed=2)
+    want = b.run()
+    got = starve(b, fills)
+    for k in want:
+        lost = torch.isnan(got[k])
+        assert bool((lost | (got[k] == want[k])).all()), k
+        assert fills > 0 or bool(lost.all()), k
+    if not any(bool(torch.isnan(got[k]).any()) for k in want):
+        assert fills == 8                      # everything could be fetched
+        ops.stream_check()
+    else:
+        with pytest.raises(binding.BmgdError):
+            ops.stream_check()
+
+
 @pytest.mark.parametrize("fills", [0, 1, 2])
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
 def test_a_wait_that_runs_out_touches_no_other_call(shape, fills):
