@@ -240,9 +240,16 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const __grid_
 
 // ---------------------------------------------------------------- the update
 // m / (sqrt(v) root + eps) with the root and the reciprocal each within 2^-23 of their values: they move theta by lr at most, and
-// the exact forms cost as many instructions as the rest of the formula.  (eps is at least 2^-63: nothing here is subnormal
-// but a v that counts for nothing beside it.)
+// the exact forms cost as many instructions as the rest of the formula.  The square root takes subnormal v for what they are: in
+// the first updates root = 1 / sqrt(1-b^t) is 30 or more, and sqrt(v) root counts beside the smallest eps (2^-63) although v is below
+// 2^-126.  The sum is at least 2^-63, so the reciprocal needs no subnormals.
 __device__ __forceinline__ float sqrt_near(float x) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// the same for x = 0 or x >= 2^-126, with fewer instructions (about 3 % of the update with moments in 8 bits)
+__device__ __forceinline__ float sqrt_normal(float x) {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
@@ -447,7 +454,7 @@ __device__ __forceinline__ void adamw_unit8(const AdamwEntry& e, long long unit,
         const float2 va = (Pair(v[i], v[i + 1]) * b).both(), vb = ((gi * b1) * gi).both();
         const Pair mi(__fadd_rn(ma.x, mb.x), __fadd_rn(ma.y, mb.y));
         const float2 vi = make_float2(__fadd_rn(va.x, vb.x), __fadd_rn(va.y, vb.y));
-        const float2 denom = (Pair(sqrt_near(vi.x), sqrt_near(vi.y)) * root + eps).both();
+        const float2 denom = (Pair(sqrt_normal(vi.x), sqrt_normal(vi.y)) * root + eps).both();
         const Pair quotient = mi * Pair(reciprocal_near(denom.x), reciprocal_near(denom.y));
         const float2 pi = (Pair(p[i], p[i + 1]) * kept + quotient * step).both(), mm = mi.both();
         m[i] = mm.x; m[i + 1] = mm.y;
@@ -458,9 +465,15 @@ __device__ __forceinline__ void adamw_unit8(const AdamwEntry& e, long long unit,
         top_p = top3(top_p, pi.x, pi.y);
         low_v = low3(low_v, vi.x, vi.y);
     }
-    if (__any_sync(0xFFFFFFFFu, !(top3(top_m, top_v, top_p) < INFINITY))) {  // nothing has been written yet
-        adamw_unit_any<PT, MASTER, GT, 8>(e, unit, lane, F, keep, key);
-        return;
+    // infinities, NaN and subnormal v are the other form's; nothing has been written yet
+    if (__any_sync(0xFFFFFFFFu, !(top3(top_m, top_v, top_p) < INFINITY) || low_v < 0x1p-126f)) {
+        bool other = !(top3(top_m, top_v, top_p) < INFINITY);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) other = other || (v[i] > 0.f && v[i] < 0x1p-126f);
+        if (__any_sync(0xFFFFFFFFu, other)) {
+            adamw_unit_any<PT, MASTER, GT, 8>(e, unit, lane, F, keep, key);
+            return;
+        }
     }
     const int new_m = max((int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_m)) >> 23), 16);
     const int new_v = max((int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top_v)) >> 23), 40);

@@ -329,3 +329,30 @@ def test_refusals():
         with pytest.raises(BmgdError):
             call()
     assert s["control"].tolist() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("b", [0.999, 0.9999999])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,master,shift", [(torch.float32, False, 0), (torch.float32, False, 1), (torch.bfloat16, True, 0)])
+def test_first_updates_from_tiny_gradients_with_the_least_eps(param, master, shift, bits, b):
+    """eps = 0 counts as 2^-63, and the second moments of gradients of 1e-22 to 1e-15 are subnormal: sqrt(v) / sqrt(1 - b) is not
+    small beside eps, so the first update moves theta by up to lr, not by a multiple of it."""
+    n, lr, a = 4096 + 37, 0.01, 0.9
+    gen = torch.Generator(device="cuda").manual_seed(bits)
+    size = 10.0 ** (torch.rand(n, generator=gen, device="cuda", dtype=torch.float64) * 7 - 22)
+    g = torch.zeros(n + shift, device="cuda")[shift:]
+    g.copy_(torch.where(torch.rand(n, generator=gen, device="cuda") < 0.5, -size, size))
+    p = [torch.zeros(n + shift, device="cuda", dtype=param)[shift:]]
+    masters = [torch.zeros(n, device="cuda")] if master else None
+    ops.adamw_step(p, [g], lr=lr, a=a, b=b, eps=0.0, masters=masters, **ops.adamw_state(p, bits))
+    gd = g.double()
+    v, eps, root = (1 - b) * gd * gd, 2.0 ** -63, (1 - b) ** -0.5
+    denom = v.sqrt() * root + eps
+    move = lr / (1 - a) * (1 - a) * gd / denom
+    # v has a relative error of 4 units of 2^-24 where it is normal and one subnormal step, 2^-149, at most; the rest in units of 2^-24:
+    # the root 2 and its factor 2, the sum 1, the quotient 4, m 2, the step length 2, theta 1
+    dv = 4 * E32 * v + 2.0 ** -149
+    spread = ((v + dv).sqrt() - (v - dv).clamp(min=0).sqrt()) * root / ((v - dv).clamp(min=0).sqrt() * root + eps)
+    err = ((masters or p)[0].double() + move).abs()
+    assert bool((err <= move.abs() * (spread + 16 * E32) + 2.0 ** -149).all()), float((err / move.abs()).max())
+    assert float(move.abs().max()) <= lr
