@@ -96,8 +96,9 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
                     void* dev_scratch, int64_t scratch_bytes, void* stream) {
     if (!cfg || !dev_control || count < 0 || (count > 0 && !tensors)) return BMGD_ERR_ARG;
     if ((uintptr_t)dev_control % 8 != 0) return BMGD_ERR_ARG;
-    if (!std::isfinite(cfg->lr) || !in_unit(cfg->a) || !in_unit(cfg->b) || !(cfg->eps >= 0.0) || !std::isfinite(cfg->eps) ||
-        !std::isfinite(cfg->grad_scale) || !(cfg->max_norm >= 0.0) || !std::isfinite(cfg->max_norm))
+    // (lr, the decay and the gradients' factor are fp32 in the kernel: what overflows there would be Inf)
+    if (!std::isfinite((float)cfg->lr) || !in_unit(cfg->a) || !in_unit(cfg->b) || !(cfg->eps >= 0.0) || !std::isfinite(cfg->eps) ||
+        !std::isfinite((float)cfg->grad_scale) || !(cfg->max_norm >= 0.0) || !std::isfinite(cfg->max_norm))
         return BMGD_ERR_ARG;
     int64_t total = 0;
     for (int32_t i = 0; i < count; ++i) {
@@ -105,7 +106,7 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
         if (e.count < 0 || e.count > ((int64_t)1 << 40)) return BMGD_ERR_ARG;
         if (e.param_type < BMGD_TYPE_F32 || e.param_type > BMGD_TYPE_F16 || e.grad_type < BMGD_TYPE_F32 || e.grad_type > BMGD_TYPE_F16)
             return BMGD_ERR_ARG;
-        if ((e.state_bits != 8 && e.state_bits != 32) || !std::isfinite(e.weight_decay)) return BMGD_ERR_ARG;
+        if ((e.state_bits != 8 && e.state_bits != 32) || !std::isfinite((float)(cfg->lr * e.weight_decay))) return BMGD_ERR_ARG;
         if (e.count == 0) continue;
         if (!e.param || !e.grad || !e.m || !e.v || (e.state_bits == 8 && (!e.m_scale || !e.v_scale))) return BMGD_ERR_ARG;
         if ((uintptr_t)e.param % type_bytes(e.param_type) || (uintptr_t)e.grad % type_bytes(e.grad_type) || (uintptr_t)e.master % 4 ||

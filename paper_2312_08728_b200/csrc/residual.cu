@@ -64,7 +64,7 @@ extern "C" {
 
 int bmgd_softmax_residual(const void* dev_logits, int64_t ld_logits, const int32_t* dev_y, int64_t rows, int32_t C, int32_t type,
                           double scale, void* dev_residual, int64_t ld_residual, float* dev_loss, void* stream) {
-    if (rows < 0 || rows > 0x7FFFFFFFll || C < 1 || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16 || !std::isfinite(scale)) return BMGD_ERR_ARG;
+    if (rows < 0 || rows > 0x7FFFFFFFll || C < 1 || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16 || !std::isfinite((float)scale)) return BMGD_ERR_ARG;
     if (rows == 0) return BMGD_OK;
     if (!dev_logits || !dev_y || !dev_residual || ld_logits < C || ld_residual < C) return BMGD_ERR_ARG;
     const int eb = type == BMGD_TYPE_F32 ? 4 : 2;

@@ -196,3 +196,13 @@ def test_no_cpu_path():
     from paper_2312_08728_b200.network import GatedSoftmax
     with pytest.raises(RuntimeError):
         GatedSoftmax(100, 8, 2, 16, 4)
+
+
+@pytest.mark.parametrize("value", [3.5e38, -3.5e38, 1e300])
+def test_factors_that_overflow_in_fp32_are_refused(value):
+    """They are doubles at the call and fp32 in the kernels: as Inf they would turn every result into NaN."""
+    assert residual(scale=value) == binding.ERR_ARG
+    assert adamw([{}], lr=value) == binding.ERR_ARG
+    assert adamw([{}], grad_scale=value) == binding.ERR_ARG
+    assert adamw([dict(weight_decay=value)], lr=1.0) == binding.ERR_ARG
+    assert adamw([dict(weight_decay=float("inf"))], lr=0.0) == binding.ERR_ARG
