@@ -11,6 +11,9 @@ pointers, so whatever the tensors' own metadata can tell is refused here.  Work 
 current stream of the tensors' device; nothing waits for the device, so every call can be captured into a CUDA graph.
 Outputs and workspaces come from torch's allocator on that stream.  Where `stream` is not the current one, the order between
 the two is the caller's (wait_stream or events); the memory of inputs and outputs is kept until both are done with it.
+
+None of them is part of an autograd graph: gradients are outputs like others.  gated_ffn refuses tensors that require gradients
+where a graph would be recorded (call it under torch.no_grad(), with gated_ffn_backward beside it).
 """
 from __future__ import annotations
 
@@ -167,6 +170,8 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     All four in bfloat16 or all in float16; rows contiguous, any row stride.  With save=True returns (y, saved), saved
     being what gated_ffn_backward needs beside its other arguments."""
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
+    if torch.is_grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or w_down.requires_grad):
+        raise ValueError("gated_ffn records no autograd graph: call it under torch.no_grad(), or with detached tensors")
     place = _place(device, stream)
     _lend(stream, device, (x, w_gate, w_up, w_down))
     with place:
