@@ -13,7 +13,8 @@ Outputs and workspaces come from torch's allocator on that stream.  Where `strea
 the two is the caller's (wait_stream or events); the memory of inputs and outputs is kept until both are done with it.
 
 None of them is part of an autograd graph: gradients are outputs like others.  gated_ffn refuses tensors that require gradients
-where a graph would be recorded (call it under torch.no_grad(), with gated_ffn_backward beside it).
+where a graph would be recorded (call it under torch.no_grad(), with gated_ffn_backward beside it).  adamw_step writes parameters and
+copies in place and tells autograd so: a graph that has saved one of them refuses its backward pass.
 """
 from __future__ import annotations
 
@@ -402,6 +403,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
         _status(L.bmgd_adamw_step(table.buffer_info()[0], count, ctypes.byref(cfg), control.data_ptr(),
                                   scratch.data_ptr() if scratch is not None else None, size,
                                   _current(device)), "bmgd_adamw_step")
+    torch._C._increment_version(params if masters is None else [*params, *(t for t in masters if t is not None)])
 
 
 def decode_moments(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:

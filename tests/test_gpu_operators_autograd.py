@@ -21,3 +21,27 @@ def test_the_block_refuses_to_drop_a_graph(which):
     assert torch.equal(y, want)
     grads = ops.gated_ffn_backward(torch.ones_like(y), *tensors, saved)  # explicit gradients, in either mode
     assert not any(g.requires_grad for g in grads)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("master", [False, True])
+def test_a_graph_that_saved_a_weight_sees_its_update(bits, master):
+    w = torch.randn(16, 16, **BF, requires_grad=True)
+    copies = [w.detach().float().requires_grad_()] if master else None
+    x = torch.randn(4, 16, **BF, requires_grad=True)
+    loss = (x @ w).sum() + ((x.float() @ copies[0]).sum() if master else 0)
+    grad, state = torch.randn(16, 16, **BF), ops.adamw_state([w], bits)
+    versions = w._version, copies[0]._version if master else None
+    ops.adamw_step([w], [grad], lr=1e-2, masters=copies, **state)
+    assert w._version > versions[0] and (not master or copies[0]._version > versions[1])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    (x @ w).sum().backward()                   # a graph of the new weight
+
+
+def test_weights_made_in_inference_mode_are_updated():
+    with torch.inference_mode():
+        w = torch.zeros(300, device="cuda")
+        state = ops.adamw_state([w])
+    ops.adamw_step([w], [torch.ones(300, device="cuda")], lr=1e-2, **state)
+    assert torch.allclose(w, torch.full_like(w, -1e-2), atol=1e-6)
