@@ -20,7 +20,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
-#include "softmax_kernel.cuh"
+#include "glm_kernel.cuh"  // barriers, clusters, the clock: its kernels are made in the tables that ask for them
+#include "tensor_core.cuh"
 
 namespace bmgdk {
 

@@ -34,6 +34,7 @@
 
 #include "glm_kernel.cuh"
 #include "shuffle.cuh"
+#include "tensor_core.cuh"
 
 namespace bmgdk {
 
@@ -148,8 +149,6 @@ __device__ __forceinline__ void tc_alloc(uint32_t dst_smem, uint32_t ncols) {
 __device__ __forceinline__ void tc_dealloc(uint32_t taddr, uint32_t ncols) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // D[tmem] (+)= A[smem] * B[smem], bf16 inputs, fp32 accumulate; issued by one thread
 __device__ __forceinline__ void tc_mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -183,16 +182,6 @@ __device__ __forceinline__ void tc_load_sum(uint32_t tmem_lane_base, uint32_t co
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] += t[i];
     }
-}
-// shared-memory matrix descriptor, 128-byte swizzle: start address, leading and stride byte offsets in 16-byte units
-__device__ __forceinline__ uint64_t tc_smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr >> 4) & 0x3FFFu);
-    d |= (uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16;
-    d |= (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32;
-    d |= (uint64_t)1 << 46;   // descriptor version of this architecture
-    d |= (uint64_t)2 << 61;   // 128-byte swizzle
-    return d;
 }
 // instruction descriptor: fp32 accumulator, bf16 A and B, M x N tile, A read K-major or MN-major, B K-major
 __device__ __forceinline__ uint32_t tc_idesc(int M, int N, bool a_mn_major) {

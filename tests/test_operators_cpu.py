@@ -1,6 +1,7 @@
 """What the operators refuse, before any pointer reaches a kernel.  No GPU needed: the Python checks run on tensors' metadata
 (the meta device stands in for another one), the C checks on sizes and null pointers."""
 import ctypes
+import os
 import struct
 
 import pytest
@@ -206,3 +207,10 @@ def test_factors_that_overflow_in_fp32_are_refused(value):
     assert adamw([{}], grad_scale=value) == binding.ERR_ARG
     assert adamw([dict(weight_decay=value)], lr=1.0) == binding.ERR_ARG
     assert adamw([dict(weight_decay=float("inf"))], lr=0.0) == binding.ERR_ARG
+
+
+def test_operators_do_not_carry_the_softmax_step_kernel():
+    """Its launcher makes the kernel's instances wherever it is included: only where they are launched."""
+    csrc = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    with_it = [f for f in sorted(os.listdir(csrc)) if '#include "softmax_kernel.cuh"' in open(os.path.join(csrc, f)).read()]
+    assert with_it == ["bmgd.cu"]
