@@ -16,10 +16,12 @@ values, and the gradients that follow from it lower still (1,000 rows that a net
 dWg is 0.08, of 8,192 rows 0.43; with the loss scaled 0.0005).  So with fp16 rows the residual, and with it every gradient, is
 multiplied by a power of two S, which the update divides out again in fp32; S / rows is between 1/2 and 1, S at most 2^13 and,
 up to 128 rows, 1, unless the caller gives `loss_scale`.  An update whose gradients are not finite is left out
-(state["control"] counts them), and S falls to a quarter eight steps after one.
+(state["control"] counts them).  Eight steps after one whose loss was a number, S falls to a quarter; it rises again by as much
+after 2,000 updates without one.  (A loss that is NaN comes from the rows, or from hidden values above 65,504: no S mends that.)
 """
 from __future__ import annotations
 
+import math
 import sys
 from typing import Dict, List, Optional
 
@@ -30,7 +32,8 @@ from .binding import ERR_CAPACITY, ERR_STATE, BmgdError, check_buffer
 from .inputs import DTYPE_BF16, LOSS_SOFTMAX
 
 _LAG = 8               # steps between an update and the look at whether it was left out: the host runs ahead that far
-_LEAST = 2.0 ** -20    # of the factor by which S has fallen (rows with NaN are not to blame on the scale for ever)
+_RAISE = 2000          # updates in a row that were taken, before S rises again
+_LEAST = 2.0 ** -20    # of the factor by which S has fallen
 
 
 class GatedSoftmax:
@@ -68,8 +71,9 @@ class GatedSoftmax:
         self._next = 0
         self.loss_scale = loss_scale
         if dtype is torch.float16:
-            self._lowered, self._steps, self._lowered_at, self._left_out = 1.0, 0, 0, 0
+            self._lowered, self._steps, self._lowered_at, self._left_out, self._taken = 1.0, 0, 0, 0, 0
             self._counts = torch.zeros(_LAG, ops.CONTROL_WORDS, dtype=torch.int64).pin_memory()
+            self._losses = torch.zeros(_LAG).pin_memory()
             self._counted = [torch.cuda.Event() for _ in range(_LAG)]
 
     def load_buffer(self, host_x: torch.Tensor, host_y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
@@ -150,8 +154,11 @@ class GatedSoftmax:
             k = self._steps % _LAG
             self._counted[k].synchronize()
             left_out = int(self._counts[k, 1])
-            if left_out > self._left_out and self._steps - _LAG >= self._lowered_at:  # (taken with the present S)
-                self._lowered, self._lowered_at = max(self._lowered / 4, _LEAST), self._steps
+            self._taken = self._taken + 1 if left_out == self._left_out else 0
+            if left_out > self._left_out and not math.isnan(float(self._losses[k])) and self._steps - _LAG >= self._lowered_at:
+                self._lowered, self._lowered_at = max(self._lowered / 4, _LEAST), self._steps  # (it was taken with the present S)
+            elif self._taken >= _RAISE and self._lowered < 1.0:
+                self._lowered, self._taken = self._lowered * 4, 0
             self._left_out = left_out
         if self.loss_scale is not None:
             return self.loss_scale * self._lowered
@@ -169,6 +176,7 @@ class GatedSoftmax:
             k = self._steps % _LAG
             with torch.cuda.device(self.device):
                 self._counts[k].copy_(self.state["control"], non_blocking=True)
+                self._losses[k].copy_(loss.sum(), non_blocking=True)
                 self._counted[k].record()
             self._steps += 1
         return loss

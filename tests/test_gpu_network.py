@@ -288,3 +288,51 @@ def test_a_copy_that_fails_is_waited_for(monkeypatch):
     assert net.load_buffer(x + 1, y, stream=again) == slot
     torch.cuda.synchronize()
     assert bool((net._slots[slot][0] == 2).all())
+
+
+def test_scale_in_fp16_is_not_lowered_for_rows_with_nan():
+    net = GatedSoftmax(256, 32, 1, 64, 4, dtype=torch.float16, seed=2)
+    x, y = (t.cuda() for t in sample(256, 32, 4, torch.float16))
+    bad = x.clone()
+    bad[7, 3] = float("nan")
+    for k in range(40):
+        net.step(bad if k % 3 == 0 else x, y, 1e-3)
+    assert net.state["control"].tolist()[:2] == [26, 14]
+    assert net._lowered == 1.0 and all(torch.isfinite(t).all() for t in net.get_theta())
+
+
+def test_scale_in_fp16_rises_again(monkeypatch):
+    """After one mini-batch whose gradients overflow, S is back where it was after as many good updates as are asked for."""
+    from paper_2312_08728_b200 import network
+    monkeypatch.setattr(network, "_RAISE", 16)
+    net = GatedSoftmax(256, 32, 1, 64, 4, dtype=torch.float16, activation=ops.ACT_RELU, seed=2)
+    net.set_theta([torch.full_like(net.masters[0], 0.05), torch.full_like(net.masters[1], 0.05), torch.zeros_like(net.masters[2])])
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn(256, 32, generator=gen, device="cuda").abs().half()
+    y = torch.zeros(256, device="cuda", dtype=torch.int32)
+    seen = []
+    for k in range(40):
+        net.step(x * 40 if k == 3 else x, y, 1e-6)   # (40 x: see the test above)
+        seen.append(net._lowered)
+    # step 3 is looked at before step 11, the good ones from step 4 on before steps 12 to 27
+    assert seen == [1.0] * 11 + [0.25] * 16 + [1.0] * 13
+    assert net.state["control"].tolist()[:2] == [39, 1]
+
+
+def test_a_step_in_fp16_captured_into_a_graph():
+    """It keeps the S of its capture and looks at nothing on the host."""
+    x, y = (t.cuda() for t in sample(256, 48, 6, torch.float16))
+    nets = [GatedSoftmax(256, 48, 1, 96, 6, dtype=torch.float16, seed=2) for _ in range(2)]
+    for net in nets:
+        net.step(x, y, 1e-2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nets[0].step(x, y, 1e-2)
+    for _ in range(12):
+        graph.replay()
+        nets[1].step(x, y, 1e-2)
+    nets[0].step(x, y, 1e-2)
+    nets[1].step(x, y, 1e-2)
+    for a, b in zip(nets[0].get_theta(), nets[1].get_theta()):
+        assert torch.equal(a, b)
+    assert nets[0].state["control"].tolist()[:2] == [14, 0]
