@@ -306,7 +306,8 @@ enum { BMGD_ACT_SILU = 0, BMGD_ACT_GELU = 1, BMGD_ACT_RELU = 2, BMGD_ACT_SIGMOID
 enum { BMGD_FFN_FORWARD = 0, BMGD_FFN_BACKWARD = 1 };
 
 /* Gated feed-forward block: Y = (act(X Wg) * (X Wu)) Wd, X [rows][inputs], Wg and Wu [inputs][hidden],
- * Wd [hidden][outputs], all of one type (BF16 or F16; F32 returns BMGD_ERR_UNIMPLEMENTED), sums in fp32.  Any sizes
+ * Wd [hidden][outputs], all of one type (BF16 or F16; F32 returns BMGD_ERR_UNIMPLEMENTED), sums in fp32, the
+ * product in brackets rounded to that type, as dG and dU are in the backward pass (F16: Inf from 65,520 on).  Any sizes
  * from 1 (rows from 0) up to 2^24 (rows 2^31 - 256) and any row strides; operands whose rows do not start on 16-byte boundaries are copied into
  * the workspace first. */
 typedef struct bmgd_gated_ffn {

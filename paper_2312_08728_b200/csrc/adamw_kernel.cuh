@@ -6,10 +6,11 @@
 // Every product and sum is rounded to fp32 by itself (no contraction), so the moments do not depend on how the compiler
 // schedules them, and their codes can be checked bit for bit.
 //
-// What bounds it: memory (200 million fp32 values: 893 us, 6.3 TB/s; bf16 with fp32 copies 903 us, 6.6 TB/s), and where moments
-// have 8 bits the arithmetic of their codes.  Each value of theta, the gradient and the moments is read once and written once.  A warp
-// takes units of 256 consecutive values of one tensor: lane l holds values 4l..4l+3 and 128+4l..128+4l+3, so that every
-// access of the warp is one contiguous piece, and the 256 values that share a scale in the 8-bit form sit in one warp.
+// What bounds it: memory (200 million fp32 values: 898 us, 6.2 TB/s; bf16 with fp32 copies 929 us, 6.5 TB/s), and where moments
+// have 8 bits the 77 instructions a value and the wait for a unit's loads (see adamw_unit8).  Each value of theta, the gradient and
+// the moments is read once and written once.  A warp takes units of 256 consecutive values of one tensor: lane l holds values
+// 4l..4l+3 and 128+4l..128+4l+3, so that every access of the warp is one contiguous piece, and the 256 values that share a scale
+// in the 8-bit form sit in one warp.
 //
 // Moments in 8 bits.  256 consecutive values share one byte s, the biased fp32 exponent of their largest magnitude:
 //   m: code in e4m3, value code * 2^(s-134): the largest magnitude lies in [128, 256) before scaling;
@@ -406,7 +407,8 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
 }
 
 // A full unit with moments in 8 bits.  Instructions and the latency of a unit's loads bound this form, not memory (200 million
-// values in bf16: 1079 us value by value, 741 in this way with three blocks to an SM, 662 with four; their traffic needs 310),
+// values in bf16: 1079 us value by value, 741 in this way with three blocks to an SM, 664 with four, whose 64 registers
+// spill 132 bytes over all combinations of types; their traffic needs 310; issue slots 56 % and memory 28 % busy),
 // hence: two values to an instruction wherever the formula allows; the largest and
 // smallest of several values in one; four codes at a time through bytes.
 // A code is the upper bits of y, the value's exponent and mantissa counted from the format's smallest, plus the draw: for m

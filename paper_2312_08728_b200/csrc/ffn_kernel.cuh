@@ -7,7 +7,8 @@
 //              dWg = X^T dG, dWu = X^T dU, dWd = H^T dY  one launch over the three
 // Rows of every matrix are contiguous.  Both ways of reading a tile exist for each operand: "K-major", the contraction
 // index along the rows, or "MN-major", across them; nothing is transposed in memory.  H, dG and dU are rounded to the type
-// of the rows between the kernels (they are the operands of the next contraction, which takes no other type); sums are fp32
+// of the rows between the kernels (they are the operands of the next contraction, which takes no other type; in fp16 values
+// above 65,504 become Inf there); sums are fp32
 // in tensor memory, and act(G) and U act'(G) are kept in fp32 for the backward pass: rounded to 16 bits they would add as much
 // to the gradients' error as both other roundings together, and their traffic hides behind the arithmetic.
 //
@@ -270,7 +271,7 @@ __device__ __forceinline__ uint32_t ffn_idesc(int type, bool a_mn, bool b_mn, in
 
 // ---------------------------------------------------------------- many rows
 // Warp 0 copies tiles of 64 along the contraction by TMA into a ring of stages with the 128-byte swizzle, warp 1 issues
-// tcgen05.mma, warps 4 to 7 read accumulators out of tensor memory; two accumulators take turns, so that reading one out
+// tcgen05.mma, warps 4 to 11 read accumulators out of tensor memory; two accumulators take turns, so that reading one out
 // overlaps the next tile's arithmetic.  With CG = 2 two CTAs of a cluster work on one tile of 256 rows: each fetches its 128
 // rows of A and half of B, and the even one issues for both.  The gradients of the three weights are problems of one
 // launch: their tiles fill the GPU together.

@@ -191,7 +191,8 @@ int launch_few(FfnParams& P, const Problem& x, int split, bool early, const Devi
 // sweep on B200 over rows 1 to 2000, widths 256 to 11008: a CTA takes in 80 KB a microsecond (its stages in flight over the
 // latency of a copy), all of them together no more than 24 MB; reading out a row's sums takes 0.015 (backward 0.02) and
 // exchanging them 0.006 (0.01) more per CTA of the cluster, a cluster about 1.  Its choice is within 3 us of the best of the
-// sweep throughout; always taking 128 rows and the largest split that fits cost up to 9 us of 30 there.
+// sweep throughout; always taking 128 rows and the largest split that fits cost up to 9 us of 30 there.  (Splits of 5 to 7 were
+// not part of the sweep.)
 struct FewChoice {
     int rows, split;
 };

@@ -168,7 +168,8 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
               save: bool = False, stream: Optional[torch.cuda.Stream] = None):
     """(act(x w_gate) * (x w_up)) w_down for x [rows, inputs], w_gate and w_up [inputs, hidden], w_down [hidden, outputs].
 
-    All four in bfloat16 or all in float16; rows contiguous, any row stride.  With save=True returns (y, saved), saved
+    All four in bfloat16 or all in float16; rows contiguous, any row stride.  Sums are fp32, the product in brackets is rounded to
+    that type in between (float16: it must stay below 65,504).  With save=True returns (y, saved), saved
     being what gated_ffn_backward needs beside its other arguments."""
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
     if torch.is_grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or w_down.requires_grad):
