@@ -14,7 +14,8 @@ the two is the caller's (wait_stream or events); the memory of inputs and output
 
 None of them is part of an autograd graph: gradients are outputs like others.  gated_ffn refuses tensors that require gradients
 where a graph would be recorded (call it under torch.no_grad(), with gated_ffn_backward beside it).  adamw_step writes parameters and
-copies in place and tells autograd so: a graph that has saved one of them refuses its backward pass.
+copies in place and tells autograd so: a graph that has saved one of them refuses its backward pass (an update that is replayed from a
+CUDA graph tells it only at its capture).
 """
 from __future__ import annotations
 
@@ -215,7 +216,8 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
 
 
 def stream_check(stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Wait for the stream and raise, once, if a device-side wait of a gated-block kernel on its device gave up."""
+    """Wait for the stream and raise, once, if a device-side wait of a gated-block kernel on its device gave up.  What that kernel had
+    not computed by then is NaN in its outputs."""
     s = stream if stream is not None else torch.cuda.current_stream()
     with torch.cuda.device(s.device):
         _status(_binding.load_library().bmgd_stream_check(s.cuda_stream), "bmgd_stream_check")
