@@ -381,7 +381,97 @@ typedef struct bmgd_adamw_config {
 int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_adamw_config* cfg, void* dev_control,
                     void* dev_scratch, int64_t scratch_bytes, void* stream);
 
-/* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block kernel on the current device
+/* Root-mean-square norm of rows with the residual's addition, of one type (all three): with t = x + residual, rounded to the type
+ * (t = x without a residual), and s = 1 / sqrt(mean of t^2 + eps),   y = t s weight.  Sums are fp32: values beyond 1.8e19 make s zero.
+ * y in the type, or (codes and scale instead) in 8 bits: codes = y * 127 / a to the nearest whole number, scale = a / 127 with a the
+ * row's largest magnitude; rows below 2^-120 throughout have codes and scale 0, rows with NaN or Inf codes 0 and scale NaN.
+ * Nothing that is written may overlap what is read, or anything else that is written.  Any row strides from `width` on. */
+typedef struct bmgd_rms_norm {
+    int64_t rows;                        /* 0 to 2^31 - 1 */
+    int32_t width;                       /* 1 to 2^24 */
+    int32_t type, weight_type;           /* weight_type: `type` or BMGD_TYPE_F32 */
+    int32_t reserved;                    /* must be zero */
+    double eps;                          /* 0 gives NaN for rows of zeros */
+    const void* x;
+    const void* residual;                /* NULL: none */
+    const void* weight;                  /* [width]; NULL: ones */
+    void* total;                         /* t: written by the forward pass (NULL without a residual), read by the backward pass (x then) */
+    void* y;
+    int8_t* codes;
+    float* scale;                        /* [rows] */
+    float* rstd;                         /* s [rows]: written by the forward pass if it is not NULL, read by the backward pass */
+    int64_t ld_x, ld_residual, ld_total, ld_y, ld_codes;
+    const void* dy;                      /* backward: gradient of y, */
+    const void* dtotal;                  /* and of t as the later parts of a model use it (NULL: none) */
+    void* dx;                            /* gradient of x, and of the residual */
+    void* dweight;                       /* [width], of weight_type; with a weight only */
+    int64_t ld_dy, ld_dtotal, ld_dx;
+} bmgd_rms_norm;
+int bmgd_rms_norm_forward(const bmgd_rms_norm* a, void* stream);
+/* Workspace of the backward pass (256-byte aligned); the forward pass needs none. */
+int bmgd_rms_norm_workspace_bytes(const bmgd_rms_norm* a, int64_t* bytes);
+/* The weight's gradient is a sum over the rows in a fixed order: equal calls give equal bits.  rows = 0 gives zeros. */
+int bmgd_rms_norm_backward(const bmgd_rms_norm* a, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Rows of x, or with a gate of act(gate) * x in fp32, in 8 bits: codes and scale [rows] as above. */
+int bmgd_quantize_rows(const void* dev_x, int64_t ld_x, const void* dev_gate, int64_t ld_gate, int64_t rows, int32_t width, int32_t type,
+                       int32_t activation, int8_t* dev_codes, int64_t ld_codes, float* dev_scale, void* stream);
+/* Weights [inputs][outputs] as codes [outputs][inputs] with a scale for each output, as bmgd_quantized_linear reads them. */
+int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_t outputs, int32_t type, int8_t* dev_codes,
+                         int64_t ld_codes, float* dev_scale, void* stream);
+
+/* Product in 8-bit integers: y = (codes weight^T) scale_i weight_scale_j + bias_j, codes [rows][inputs], weight
+ * [outputs][inputs]; the sums are exact, the rest is fp32, rounded once to `type`.  Operands whose rows do not start on 16-byte
+ * boundaries are copied into the workspace first.  y overlaps no operand. */
+typedef struct bmgd_quantized_linear_args {
+    int64_t rows;                        /* 0 to 2^31 - 256 */
+    int32_t inputs, outputs;             /* 1 to 131,071 (sums of 32 bits) and 2^24 */
+    int32_t type;                        /* of y */
+    int32_t reserved;                    /* must be zero */
+    const int8_t* codes;
+    const float* scale;                  /* [rows] */
+    const int8_t* weight;
+    const float* weight_scale;           /* [outputs] */
+    const float* bias;                   /* [outputs]; NULL: none */
+    void* y;
+    int64_t ld_codes, ld_weight, ld_y;
+} bmgd_quantized_linear_args;
+int bmgd_quantized_linear_workspace_bytes(const bmgd_quantized_linear_args* a, int64_t* bytes);
+int bmgd_quantized_linear(const bmgd_quantized_linear_args* a, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Of each row of logits [rows][C]: the log probability of class y, the entropy, and the `top` most probable classes, in falling
+ * order, equal logits by rising class, with their log probabilities.  A row whose y is outside [0, C) has log probability 0; one whose
+ * logits are all -Inf has log probability and entropy 0 and alternatives -Inf; NaN and +Inf give NaN (NaN comes first among the alternatives). */
+typedef struct bmgd_log_probs_args {
+    int64_t rows;                        /* 0 to 2^31 - 1 */
+    int32_t C;                           /* 1 to 2^30 */
+    int32_t type;
+    int32_t top;                         /* 0 to 32, at most C */
+    int32_t reserved;                    /* must be zero */
+    const void* logits;
+    const int32_t* y;                    /* NULL: no row has a class */
+    float *logprob, *entropy;            /* [rows] each; NULL: not wanted */
+    float* saved;                        /* [rows][3] for the backward pass; NULL: not wanted */
+    int32_t* top_class;                  /* [rows][top] */
+    float* top_logprob;
+    int64_t ld_logits;
+    const float *dlogprob, *dentropy;    /* backward: gradients of the two, NULL: zero */
+    void* dlogits;                       /* in the type of the logits; may be the logits themselves (value for value), overlaps nothing else */
+    int64_t ld_dlogits;
+} bmgd_log_probs_args;
+int bmgd_log_probs(const bmgd_log_probs_args* a, void* stream);
+/* dlogits = dlogprob ([c = y] - p_c) - dentropy p_c (log p_c + H).  Rows without a class, or without a distribution, as above. */
+int bmgd_log_probs_backward(const bmgd_log_probs_args* a, void* stream);
+
+/* Dropout: y = residual (NULL: 0) + x * 65536 / (65536 - k) where value j (counted row by row) is kept, k = rate * 65536 to the
+ * nearest.  Value 8 b + e is kept where number e of block b is at least k: the eight numbers of 16 bits are the words, low half
+ * first, of Philox4x32-10 with counter (b, b >> 32, *dev_step, 0x44524F50 + layer) and key seed.  dev_step (low 32 bits of an int64 in device
+ * memory; NULL: 0) lets a captured call draw anew each time, as the count in an update's control words does.  The gradient of x is the same
+ * call on the gradient of y without a residual.  y may be x or the residual itself.  rate from 0 to below 1 - 2^-17, layer from 0 to 65,535. */
+int bmgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int64_t ld_residual, int64_t rows, int64_t width, int32_t type,
+                 double rate, uint64_t seed, const int64_t* dev_step, int32_t layer, void* dev_y, int64_t ld_y, void* stream);
+
+/* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block or 8-bit product kernel on the current device
  * gave up since the last report (to whichever stream's caller asks first; none is lost).  What that call had not
  * computed by then is NaN in its outputs.  Calls before and after it, and on other streams, are not touched by it. */
 int bmgd_stream_check(void* stream);
@@ -391,6 +481,10 @@ int bmgd_stream_check(void* stream);
  * error path without hanging or faulting a GPU. */
 int bmgd_debug_gated_ffn_timeout(const bmgd_gated_ffn* g, int32_t pass, void* workspace, int64_t workspace_bytes, int32_t fills,
                                  double budget_ms, void* stream);
+
+/* The same for the product in 8-bit integers. */
+int bmgd_debug_quantized_linear_timeout(const bmgd_quantized_linear_args* a, void* workspace, int64_t workspace_bytes, int32_t fills,
+                                        double budget_ms, void* stream);
 
 /* Text for a bmgd_status; never NULL. */
 const char* bmgd_strerror(int status);

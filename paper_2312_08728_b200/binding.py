@@ -35,6 +35,9 @@ EXPORTS = (
     "bmgd_set_optimizer", "bmgd_set_lr_schedule", "bmgd_set_timeout", "bmgd_debug_null_rounds",
     "bmgd_gated_ffn_workspace_bytes", "bmgd_gated_ffn_forward", "bmgd_gated_ffn_backward", "bmgd_softmax_residual",
     "bmgd_gather_batch", "bmgd_adamw_step", "bmgd_stream_check", "bmgd_debug_gated_ffn_timeout",
+    "bmgd_rms_norm_forward", "bmgd_rms_norm_workspace_bytes", "bmgd_rms_norm_backward", "bmgd_quantize_rows", "bmgd_quantize_weight",
+    "bmgd_quantized_linear_workspace_bytes", "bmgd_quantized_linear", "bmgd_log_probs", "bmgd_log_probs_backward", "bmgd_dropout",
+    "bmgd_debug_quantized_linear_timeout",
 )
 
 OPT_SGD, OPT_NESTEROV, OPT_ADAM = 0, 1, 2
@@ -126,6 +129,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.bmgd_adamw_step.argtypes = [vp, i32, vp, vp, vp, i64, vp]
     L.bmgd_stream_check.argtypes = [vp]
     L.bmgd_debug_gated_ffn_timeout.argtypes = [vp, i32, vp, i64, i32, dbl, vp]
+    L.bmgd_rms_norm_forward.argtypes = [vp, vp]
+    L.bmgd_rms_norm_workspace_bytes.argtypes = [vp, P(i64)]
+    L.bmgd_rms_norm_backward.argtypes = [vp, vp, i64, vp]
+    L.bmgd_quantize_rows.argtypes = [vp, i64, vp, i64, i64, i32, i32, i32, vp, i64, vp, vp]
+    L.bmgd_quantize_weight.argtypes = [vp, i64, i32, i32, i32, vp, i64, vp, vp]
+    L.bmgd_quantized_linear_workspace_bytes.argtypes = [vp, P(i64)]
+    L.bmgd_quantized_linear.argtypes = [vp, vp, i64, vp]
+    L.bmgd_log_probs.argtypes = [vp, vp]
+    L.bmgd_log_probs_backward.argtypes = [vp, vp]
+    L.bmgd_dropout.argtypes = [vp, i64, vp, i64, i64, i64, i32, dbl, u64, vp, i32, vp, i64, vp]
+    L.bmgd_debug_quantized_linear_timeout.argtypes = [vp, vp, i64, i32, dbl, vp]
     for name in EXPORTS:
         if getattr(L, name).restype is None or name in ("bmgd_strerror",):
             continue

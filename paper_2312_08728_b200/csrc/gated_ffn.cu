@@ -1,65 +1,22 @@
 // Host side of the gated feed-forward block: checks, tensor maps, choice of tile, launches.
 #include <algorithm>
 #include <atomic>
-#include <cstring>
 #include <mutex>
 
 #include "../../include/bmgd.h"
 #include "ffn_kernel.cuh"
+#include "operator_host.cuh"
 
 namespace {
-
-using namespace bmgdk;
 
 // Waits that ran out of time on this device, ever.  Only counted up: what bmgd_stream_check has reported is kept on the host,
 // so that no report can wipe out another.
 __device__ unsigned g_ffn_gave_up;
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled() {
-    static std::once_flag once;
-    static EncodeTiledFn fn = nullptr;
-    std::call_once(once, [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-        else
-            cudaGetLastError();
-    });
-    return fn;
-}
+}  // namespace
 
-// A matrix of 16-bit values as the kernels read it.
-struct Matrix {
-    const void* base;
-    int64_t rows, cols, ld;
-};
+namespace bmgdk {
 
-int make_map(const Matrix& m, int type, int box_rows, CUtensorMap* out) {
-    EncodeTiledFn enc = encode_tiled();
-    if (!enc) return BMGD_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)m.ld * 2u};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
-    const cuuint32_t step[2] = {1u, 1u};
-    const CUresult r = enc(out, type == BMGD_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                           const_cast<void*>(m.base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? BMGD_OK : BMGD_ERR_CUDA;
-}
-
-// What a launch needs to know of the current device.  Looked up once per device: a call of a small block takes less time on
-// the GPU than these queries take on the host.
-constexpr int kMaxDevices = 64;
-struct Device {
-    int index, sms, smem;
-    unsigned* gave_up;
-    unsigned fills;                // see FfnParams
-    unsigned long long budget_ns;  // of any single wait inside a kernel; 0: wait_bound
-};
 int current_device(Device* d) {
     static Device known[kMaxDevices];
     static std::atomic<bool> ready[kMaxDevices];
@@ -85,19 +42,30 @@ int current_device(Device* d) {
     }
     return BMGD_OK;
 }
-// A kernel's dynamic shared memory, allowed once per device; `done` holds a bit per device and belongs to the kernel.
-template <typename K>
-int allow_smem(K* fn, int bytes, const Device& dev, std::atomic<unsigned long long>& done) {
-    const unsigned long long bit = 1ull << (dev.index & 63);
-    if (done.load(std::memory_order_relaxed) & bit) return BMGD_OK;
-    if (bytes > dev.smem) return BMGD_ERR_LAUNCH;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
-    if (dev.index < kMaxDevices) done.fetch_or(bit, std::memory_order_relaxed);
-    return BMGD_OK;
-}
+}  // namespace bmgdk
 
-// Bound on any single wait inside a kernel: two seconds, and more than a step of the contraction ever takes for each step.
-unsigned long long wait_bound(const Device& dev, int64_t steps) { return dev.budget_ns ? dev.budget_ns : 2000000000ull + 10000ull * (unsigned long long)steps; }
+namespace {
+
+using namespace bmgdk;
+
+// A matrix of 16-bit values as the kernels read it.
+struct Matrix {
+    const void* base;
+    int64_t rows, cols, ld;
+};
+
+int make_map(const Matrix& m, int type, int box_rows, CUtensorMap* out) {
+    EncodeTiledFn enc = encode_tiled();
+    if (!enc) return BMGD_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)m.ld * 2u};
+    const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
+    const cuuint32_t step[2] = {1u, 1u};
+    const CUresult r = enc(out, type == BMGD_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                           const_cast<void*>(m.base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? BMGD_OK : BMGD_ERR_CUDA;
+}
 
 // One contraction as the host describes it: out [M][N] = sum over segments of a[s] b[s].
 struct Problem {
@@ -108,19 +76,6 @@ struct Problem {
     int N, K, segments;
     bool vec;
 };
-
-void launch_config(cudaLaunchConfig_t* lc, cudaLaunchAttribute (&at)[2], dim3 grid, int threads, int smem, int cluster, cudaStream_t s) {
-    lc->gridDim = grid;
-    lc->blockDim = dim3((unsigned)threads);
-    lc->dynamicSmemBytes = smem;
-    lc->stream = s;
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-    lc->attrs = at;
-    lc->numAttrs = cluster > 1 ? 2 : 1;
-}
 
 template <int CG, int BN, int EPI, bool A_MN, bool B_MN>
 int launch(FfnParams& P, const Problem* problems, int count, const Device& dev, cudaStream_t s) {
@@ -248,19 +203,7 @@ int contract(FfnParams& P, const Problem& x, bool early, const Device& dev, cuda
 }
 
 int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
-int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 bool tma_ready(const Matrix& m) { return (uintptr_t)m.base % 16 == 0 && m.ld % 8 == 0; }
-
-// Workspace in the order it is used: copies of operands whose rows TMA cannot read, then the intermediates.
-struct Space {
-    unsigned char* base;
-    int64_t used;
-    void* take(int64_t bytes) {
-        void* p = base ? base + used : nullptr;
-        used += up256(bytes);
-        return p;
-    }
-};
 
 // Operands that TMA cannot read are copied, all of them in one launch.
 int align_matrices(Matrix* const* list, int count, Space* space, bool run, cudaStream_t s) {

@@ -1,0 +1,237 @@
+// Host side of bmgd_rms_norm_forward, bmgd_rms_norm_backward, bmgd_quantize_rows and bmgd_quantize_weight.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/bmgd.h"
+#include "norm_kernel.cuh"
+#include "operator_host.cuh"
+
+namespace {
+
+using namespace bmgdk;
+
+int launched() { return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA; }
+int value_bytes(int type) { return type == BMGD_TYPE_F32 ? 4 : 2; }
+bool off(const void* p, int bytes) { return (uintptr_t)p % (unsigned)bytes != 0; }
+// whether [rows][width] of stride ld at p and the same of stride lq at q share memory
+bool overlap(const void* p, int64_t ld, int64_t pw, const void* q, int64_t lq, int64_t qw, int64_t rows) {
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return a < b + (uintptr_t)((rows - 1) * lq + qw) && b < a + (uintptr_t)((rows - 1) * ld + pw);
+}
+
+// By the row's length in pieces of 16 bytes: a warp to a row up to 128, then blocks of 128 to 1024 threads with four pieces each, then the
+// form that reads rows more than once.
+template <typename T, bool CODES>
+int forward(const NormParams& P, cudaStream_t s) {
+    const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
+    const unsigned rows = (unsigned)P.rows, eights = (unsigned)((P.rows + 7) / 8);
+    if (pieces <= 32) norm_row_kernel<T, 32, 1, CODES><<<eights, 256, 0, s>>>(P);
+    else if (pieces <= 128) norm_row_kernel<T, 32, 4, CODES><<<eights, 256, 0, s>>>(P);
+    else if (pieces <= 256) norm_row_kernel<T, 128, 2, CODES><<<rows, 128, 0, s>>>(P);
+    else if (pieces <= 512) norm_row_kernel<T, 128, 4, CODES><<<rows, 128, 0, s>>>(P);
+    else if (pieces <= 1024) norm_row_kernel<T, 256, 4, CODES><<<rows, 256, 0, s>>>(P);
+    else if (pieces <= 2048) norm_row_kernel<T, 512, 4, CODES><<<rows, 512, 0, s>>>(P);
+    else if (pieces <= 4096) norm_row_kernel<T, 1024, 4, CODES><<<rows, 1024, 0, s>>>(P);
+    else norm_long_kernel<T, CODES><<<rows, 1024, 0, s>>>(P);
+    return launched();
+}
+
+// Blocks of the backward pass, and how they divide a row: pieces of 16 bytes where every row of every tensor starts on such a boundary,
+// else single values.
+struct BackShape {
+    int values, threads, blocks;  // threads 0: the form for long rows
+};
+BackShape back_shape(const bmgd_rms_norm* a, int sms) {
+    const int ve = 16 / value_bytes(a->type);
+    const uintptr_t low = (uintptr_t)a->total | (uintptr_t)a->dy | (uintptr_t)a->dtotal | (uintptr_t)a->dx |
+                          (uintptr_t)((a->ld_total | a->ld_dy | (a->dtotal ? a->ld_dtotal : 0) | a->ld_dx) * value_bytes(a->type));
+    BackShape b{};
+    b.values = low % 16 == 0 && a->width % ve == 0 ? ve : 1;
+    const int count = a->width / b.values;
+    if (count <= 128) b.threads = 32;
+    else if (count <= 512) b.threads = 128;
+    else if (count <= 1024) b.threads = 256;
+    else if (count <= 2048) b.threads = 512;
+    else if (count <= 4096) b.threads = 1024;
+    const int per = b.threads == 32 ? 2 : b.threads == 0 ? 1 : std::max(1, 512 / b.threads);
+    b.blocks = (int)std::min<int64_t>(b.threads == 32 ? (a->rows + 7) / 8 : a->rows, (int64_t)sms * per);
+    return b;
+}
+template <typename T, int VE>
+int backward(const NormParams& P, const BackShape& b, cudaStream_t s) {
+    const unsigned grid = (unsigned)b.blocks;
+    if (b.threads == 0) norm_back_long_kernel<T><<<grid, 1024, 0, s>>>(P);
+    else if (b.threads == 32 && P.width <= 32 * VE) norm_back_kernel<T, VE, 32, 1><<<grid, 256, 0, s>>>(P);
+    else if (b.threads == 32) norm_back_kernel<T, VE, 32, 4><<<grid, 256, 0, s>>>(P);
+    else if (b.threads == 128) norm_back_kernel<T, VE, 128, 4><<<grid, 128, 0, s>>>(P);
+    else if (b.threads == 256) norm_back_kernel<T, VE, 256, 4><<<grid, 256, 0, s>>>(P);
+    else if (b.threads == 512) norm_back_kernel<T, VE, 512, 4><<<grid, 512, 0, s>>>(P);
+    else norm_back_kernel<T, VE, 1024, 4><<<grid, 1024, 0, s>>>(P);
+    return launched();
+}
+template <typename T>
+int backward_all(const NormParams& P, const BackShape& b, cudaStream_t s) {
+    const int rc = b.values == 1 ? backward<T, 1>(P, b, s) : backward<T, Piece<T>::kValues>(P, b, s);
+    if (rc != BMGD_OK || !P.dweight) return rc;
+    cudaLaunchConfig_t lc{};
+    cudaLaunchAttribute at[2];
+    launch_config(&lc, at, dim3((unsigned)((P.width + 31) / 32)), 1024, 0, 1, s);
+    if (cudaLaunchKernelEx(&lc, norm_weight_kernel<T>, (const float*)P.part, b.blocks, P.width, P.dweight, P.weight_f32) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    return BMGD_OK;
+}
+
+int check(const bmgd_rms_norm* a) {
+    if (!a || a->rows < 0 || a->rows > 0x7FFFFFFFll || a->width < 1 || a->width > (1 << 24) || a->reserved != 0) return BMGD_ERR_ARG;
+    if (a->type < BMGD_TYPE_F32 || a->type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
+    if (a->weight && a->weight_type != a->type && a->weight_type != BMGD_TYPE_F32) return BMGD_ERR_ARG;
+    if (!(a->eps >= 0.0) || !std::isfinite((float)a->eps)) return BMGD_ERR_ARG;
+    return off(a->weight, a->weight_type == BMGD_TYPE_F32 ? 4 : value_bytes(a->type)) ? BMGD_ERR_ARG : BMGD_OK;
+}
+NormParams shared_params(const bmgd_rms_norm* a) {
+    NormParams P{};
+    P.weight = a->weight;
+    P.weight_f32 = a->weight_type == BMGD_TYPE_F32;
+    P.rows = a->rows; P.width = a->width; P.eps = (float)a->eps;
+    P.rstd = a->rstd;
+    return P;
+}
+
+int check_backward(const bmgd_rms_norm* a) {
+    const int rc = check(a);
+    if (rc != BMGD_OK) return rc;
+    const int eb = value_bytes(a->type);
+    if (a->ld_total < a->width || a->ld_dy < a->width || a->ld_dx < a->width || (a->dtotal && a->ld_dtotal < a->width)) return BMGD_ERR_ARG;
+    if ((a->dweight != nullptr) != (a->weight != nullptr) || off(a->dweight, a->weight_type == BMGD_TYPE_F32 ? 4 : eb)) return BMGD_ERR_ARG;
+    if (a->rows == 0) return BMGD_OK;
+    if (!a->total || !a->dy || !a->dx || !a->rstd) return BMGD_ERR_ARG;
+    if (off(a->total, eb) || off(a->dy, eb) || off(a->dx, eb) || off(a->dtotal, eb) || off(a->rstd, 4)) return BMGD_ERR_ARG;
+    const int64_t w = (int64_t)a->width * eb;  // a row of dx may be written before another thread has read the same row
+    if (overlap(a->dx, a->ld_dx * eb, w, a->total, a->ld_total * eb, w, a->rows) || overlap(a->dx, a->ld_dx * eb, w, a->dy, a->ld_dy * eb, w, a->rows) ||
+        (a->dtotal && overlap(a->dx, a->ld_dx * eb, w, a->dtotal, a->ld_dtotal * eb, w, a->rows))) return BMGD_ERR_ARG;
+    return BMGD_OK;
+}
+
+template <typename T>
+int codes(const CodesParams& P, cudaStream_t s) {
+    const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
+    const unsigned rows = (unsigned)P.rows, eights = (unsigned)((P.rows + 7) / 8);
+    if (pieces <= 32) codes_row_kernel<T, 32, 1><<<eights, 256, 0, s>>>(P);
+    else if (pieces <= 128) codes_row_kernel<T, 32, 4><<<eights, 256, 0, s>>>(P);
+    else if (pieces <= 256) codes_row_kernel<T, 128, 2><<<rows, 128, 0, s>>>(P);
+    else if (pieces <= 512) codes_row_kernel<T, 128, 4><<<rows, 128, 0, s>>>(P);
+    else if (pieces <= 1024) codes_row_kernel<T, 256, 4><<<rows, 256, 0, s>>>(P);
+    else if (pieces <= 2048) codes_row_kernel<T, 512, 4><<<rows, 512, 0, s>>>(P);
+    else if (pieces <= 4096) codes_row_kernel<T, 1024, 4><<<rows, 1024, 0, s>>>(P);
+    else codes_long_kernel<T><<<rows, 1024, 0, s>>>(P);
+    return launched();
+}
+
+template <typename T>
+int weight_codes(const void* w, int64_t ld_w, int inputs, int outputs, signed char* codes, int64_t ld_codes, float* scale, cudaStream_t s) {
+    codes_weight_kernel<T><<<(unsigned)((outputs + 31) / 32), 1024, 0, s>>>(static_cast<const T*>(w), ld_w, inputs, outputs, codes, ld_codes, scale);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int bmgd_rms_norm_forward(const bmgd_rms_norm* a, void* stream) {
+    const int rc = check(a);
+    if (rc != BMGD_OK) return rc;
+    if (a->rows == 0) return BMGD_OK;
+    const int eb = value_bytes(a->type);
+    const int64_t w = (int64_t)a->width * eb;
+    if (!a->x || a->ld_x < a->width || off(a->x, eb) || off(a->residual, eb) || off(a->total, eb) || off(a->y, eb) || off(a->rstd, 4) || off(a->scale, 4)) return BMGD_ERR_ARG;
+    if ((a->y == nullptr) == (a->codes == nullptr) || (a->codes != nullptr) != (a->scale != nullptr)) return BMGD_ERR_ARG;
+    if (a->y ? a->ld_y < a->width : a->ld_codes < a->width) return BMGD_ERR_ARG;
+    if ((a->residual != nullptr) != (a->total != nullptr) || (a->residual && (a->ld_residual < a->width || a->ld_total < a->width))) return BMGD_ERR_ARG;
+    // What is written overlaps nothing that is read: rows are read more than once where they are long.
+    const void* const out[2] = {a->total, a->y ? a->y : (const void*)a->codes};
+    const int64_t ld_out[2] = {a->ld_total * eb, a->y ? a->ld_y * eb : a->ld_codes}, w_out[2] = {w, a->y ? w : (int64_t)a->width};
+    for (int k = 0; k < 2; ++k) {
+        if (!out[k]) continue;
+        if (overlap(out[k], ld_out[k], w_out[k], a->x, a->ld_x * eb, w, a->rows)) return BMGD_ERR_ARG;
+        if (a->residual && overlap(out[k], ld_out[k], w_out[k], a->residual, a->ld_residual * eb, w, a->rows)) return BMGD_ERR_ARG;
+    }
+    if (out[0] && overlap(out[0], ld_out[0], w, out[1], ld_out[1], w_out[1], a->rows)) return BMGD_ERR_ARG;
+    NormParams P = shared_params(a);
+    P.x = a->x; P.ld_x = a->ld_x;
+    P.residual = a->residual; P.ld_residual = a->ld_residual;
+    P.total = a->total; P.ld_total = a->ld_total;
+    P.y = a->y; P.ld_y = a->ld_y;
+    P.codes = reinterpret_cast<signed char*>(a->codes); P.ld_codes = a->ld_codes; P.scale = a->scale;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (a->type == BMGD_TYPE_F32) return a->y ? forward<float, false>(P, s) : forward<float, true>(P, s);
+    if (a->type == BMGD_TYPE_BF16) return a->y ? forward<__nv_bfloat16, false>(P, s) : forward<__nv_bfloat16, true>(P, s);
+    return a->y ? forward<__half, false>(P, s) : forward<__half, true>(P, s);
+}
+
+int bmgd_rms_norm_workspace_bytes(const bmgd_rms_norm* a, int64_t* bytes) {
+    if (!bytes) return BMGD_ERR_ARG;
+    const int rc = check(a);
+    if (rc != BMGD_OK) return rc;
+    // (for the most blocks that a GPU of this kind is given, so that no device has to be asked)
+    *bytes = a->weight && a->rows > 0 ? up256(back_shape(a, 148).blocks * (int64_t)a->width * 4) : 0;
+    return BMGD_OK;
+}
+
+int bmgd_rms_norm_backward(const bmgd_rms_norm* a, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_backward(a);
+    if (rc != BMGD_OK) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (a->rows == 0) {
+        if (a->dweight && cudaMemsetAsync(a->dweight, 0, (size_t)a->width * (a->weight_type == BMGD_TYPE_F32 ? 4 : 2), s) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+        return BMGD_OK;
+    }
+    int64_t need = 0;
+    rc = bmgd_rms_norm_workspace_bytes(a, &need);
+    if (rc != BMGD_OK) return rc;
+    if (need > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)) return BMGD_ERR_ARG;
+    if (workspace_bytes < need) return BMGD_ERR_CAPACITY;
+    const BackShape b = back_shape(a, 148);
+    NormParams P = shared_params(a);
+    P.x = a->total; P.ld_x = a->ld_total;
+    P.dy = a->dy; P.ld_dy = a->ld_dy;
+    P.dtotal = a->dtotal; P.ld_dtotal = a->ld_dtotal;
+    P.dx = a->dx; P.ld_dx = a->ld_dx;
+    P.dweight = a->dweight;
+    P.part = a->weight ? static_cast<float*>(workspace) : nullptr;
+    if (a->type == BMGD_TYPE_F32) return backward_all<float>(P, b, s);
+    if (a->type == BMGD_TYPE_BF16) return backward_all<__nv_bfloat16>(P, b, s);
+    return backward_all<__half>(P, b, s);
+}
+
+int bmgd_quantize_rows(const void* dev_x, int64_t ld_x, const void* dev_gate, int64_t ld_gate, int64_t rows, int32_t width, int32_t type,
+                       int32_t activation, int8_t* dev_codes, int64_t ld_codes, float* dev_scale, void* stream) {
+    if (rows < 0 || rows > 0x7FFFFFFFll || width < 1 || width > (1 << 24) || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
+    if (activation < BMGD_ACT_SILU || activation > BMGD_ACT_SIGMOID) return BMGD_ERR_ARG;
+    if (rows == 0) return BMGD_OK;
+    const int eb = value_bytes(type);
+    if (!dev_x || !dev_codes || !dev_scale || ld_x < width || ld_codes < width || (dev_gate && ld_gate < width)) return BMGD_ERR_ARG;
+    if (off(dev_x, eb) || off(dev_gate, eb) || off(dev_scale, 4)) return BMGD_ERR_ARG;
+    const int64_t w = (int64_t)width * eb;
+    if (overlap(dev_codes, ld_codes, width, dev_x, ld_x * eb, w, rows) ||
+        (dev_gate && overlap(dev_codes, ld_codes, width, dev_gate, ld_gate * eb, w, rows))) return BMGD_ERR_ARG;
+    CodesParams P{dev_x, dev_gate, reinterpret_cast<signed char*>(dev_codes), dev_scale, ld_x, ld_gate, ld_codes, rows, width, activation};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == BMGD_TYPE_F32) return codes<float>(P, s);
+    if (type == BMGD_TYPE_BF16) return codes<__nv_bfloat16>(P, s);
+    return codes<__half>(P, s);
+}
+
+int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_t outputs, int32_t type, int8_t* dev_codes,
+                         int64_t ld_codes, float* dev_scale, void* stream) {
+    if (inputs < 1 || outputs < 1 || inputs > (1 << 24) || outputs > (1 << 24) || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
+    if (!dev_w || !dev_codes || !dev_scale || ld_w < outputs || ld_codes < inputs || off(dev_w, value_bytes(type)) || off(dev_scale, 4)) return BMGD_ERR_ARG;
+    const int eb = value_bytes(type);
+    const uintptr_t a = (uintptr_t)dev_w, b = (uintptr_t)dev_codes;
+    if (a < b + (uintptr_t)((outputs - 1) * ld_codes + inputs) && b < a + (uintptr_t)(((inputs - 1) * ld_w + outputs) * eb)) return BMGD_ERR_ARG;
+    signed char* q = reinterpret_cast<signed char*>(dev_codes);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == BMGD_TYPE_F32) return weight_codes<float>(dev_w, ld_w, inputs, outputs, q, ld_codes, dev_scale, s);
+    if (type == BMGD_TYPE_BF16) return weight_codes<__nv_bfloat16>(dev_w, ld_w, inputs, outputs, q, ld_codes, dev_scale, s);
+    return weight_codes<__half>(dev_w, ld_w, inputs, outputs, q, ld_codes, dev_scale, s);
+}
+
+}  // extern "C"

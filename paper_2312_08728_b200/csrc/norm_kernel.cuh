@@ -1,0 +1,551 @@
+// Root-mean-square norm of rows with the residual's addition (bmgd_rms_norm_forward, bmgd_rms_norm_backward), and rows in 8 bits
+// (its output there, bmgd_quantize_rows, bmgd_quantize_weight).
+//
+//     t = x + r rounded to the rows' type,  s = 1 / sqrt(mean_c t_c^2 + eps),  y_c = t_c s w_c
+//     backward, g = dy w:  dt_c = dtotal_c + s (g_c - t_c s^2 mean(g t)),   dw_c = sum over rows of dy_c t_c s
+//     8 bits:  a = max_c |y_c|,  scale = a / 127,  code_c = y_c (127 / a) rounded to the nearest whole number
+//
+// The norm is that of the rounded sum: it is what the next block reads as its residual, what is kept for the backward pass, and so
+// the gradients are those of the values that were computed.  All sums are fp32.  What bounds it: memory, each value read and
+// written once; rows are held in registers between the sum and its use.
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "activation.cuh"
+#include "launch.cuh"
+#include "values.cuh"
+
+namespace bmgdk {
+
+// Rows whose largest magnitude is below 2^-120 are zeros in 8 bits: 127 divided by it would leave the range of fp32.
+constexpr float kCodesLeast = 7.52316384526264e-37f;  // 2^-120
+
+struct NormParams {
+    const void *x, *residual, *weight;  // residual, weight: null for none
+    void *total, *y;                    // total: null without a residual
+    signed char* codes;                 // instead of y
+    float *scale, *rstd;                // rstd: null if it is not wanted
+    const void *dy, *dtotal;
+    void *dx, *dweight;
+    float* part;                        // backward: [gridDim.x][width], sums of each block's rows
+    long long ld_x, ld_residual, ld_total, ld_y, ld_codes, ld_dy, ld_dtotal, ld_dx;
+    long long rows;
+    int width;
+    int weight_f32;
+    float eps;
+};
+
+template <typename T>
+__device__ __forceinline__ void load_weights(const void* weight, int f32, int c, float (&w)[Piece<T>::kValues]) {
+    constexpr int VE = Piece<T>::kValues;
+    if (!weight) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) w[e] = 1.f;
+    } else if (f32 || sizeof(T) == 4) {
+        const float* p = static_cast<const float*>(weight) + c;
+        if (((uintptr_t)p & 15u) == 0) {
+#pragma unroll
+            for (int e = 0; e < VE; e += 4) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(p + e));
+                w[e] = v.x; w[e + 1] = v.y; w[e + 2] = v.z; w[e + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) w[e] = __ldg(p + e);
+        }
+    } else {
+        const T* p = static_cast<const T*>(weight) + c;
+        if (((uintptr_t)p & 15u) == 0) {
+            unpack_piece<T>(__ldg(reinterpret_cast<const uint4*>(p)), w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) w[e] = to_f32(p[e]);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ float load_weight(const void* weight, int f32, int c) {
+    if (!weight) return 1.f;
+    return f32 ? static_cast<const float*>(weight)[c] : to_f32(static_cast<const T*>(weight)[c]);
+}
+
+// The factor that takes a row's values to whole numbers, and its scale.  A row with NaN or Inf (top is one of them) has scale
+// NaN and codes 0; so has what is computed from it.
+struct RowCodes {
+    float factor, scale;
+    __device__ __forceinline__ explicit RowCodes(float top) {
+        const bool fine = top < INFINITY, some = top >= kCodesLeast;
+        factor = fine && some ? __fdiv_rn(127.f, top) : 0.f;
+        scale = !fine ? __uint_as_float(0x7FC00000u) : some ? __fdiv_rn(top, 127.f) : 0.f;
+    }
+    // (factor 0: also 0 times NaN or Inf is 0)
+    __device__ __forceinline__ int code(float y) const { return factor == 0.f ? 0 : __float2int_rn(y * factor); }
+};
+__device__ __forceinline__ float nan_max(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+// (|y factor| <= 127 (1 + 2^-23): no code leaves the range)
+template <int VE>
+__device__ __forceinline__ void store_codes(signed char* p, const RowCodes& rc, const float (&y)[VE]) {
+    uint32_t w[VE / 4];
+#pragma unroll
+    for (int e = 0; e < VE; e += 4)
+        w[e / 4] = (uint32_t)(rc.code(y[e]) & 255) | (uint32_t)(rc.code(y[e + 1]) & 255) << 8 | (uint32_t)(rc.code(y[e + 2]) & 255) << 16 |
+                   (uint32_t)rc.code(y[e + 3]) << 24;
+    if (((uintptr_t)p & (VE - 1)) == 0) {
+        if constexpr (VE == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(p) = w[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) p[e] = (signed char)(w[e / 4] >> (8 * (e & 3)));
+    }
+}
+
+// ---- forward, rows held in registers: TH threads share a row (TH = 32: a warp, eight rows to a block), NV pieces each
+template <typename T, int TH, int NV, bool CODES>
+__global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __grid_constant__ NormParams P) {
+    constexpr int VE = Piece<T>::kValues;
+    __shared__ float cells[2][TH / 32];
+    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i >= P.rows) return;  // (a whole warp; otherwise the grid has exactly the rows)
+    const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
+    const T* r = P.residual ? static_cast<const T*>(P.residual) + i * P.ld_residual : nullptr;
+    T* total = static_cast<T*>(P.total) + i * P.ld_total;
+    const RowPieces<T> row(x, P.width);
+    uint4 w[NV];
+    float t[VE], sum = 0.f, edge = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (tid + k * TH < row.pieces) w[k] = load_piece(x + row.column(tid + k * TH));
+    const bool odd = tid < row.edges;
+    const int at = row.edge(tid);
+    if (odd) edge = to_f32(x[at]);
+    if (r) {
+        uint4 v[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * TH < row.pieces) v[k] = load_piece(r + row.column(tid + k * TH));
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * TH >= row.pieces) continue;
+            float u[VE];
+            unpack_piece<T>(w[k], t);
+            unpack_piece<T>(v[k], u);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) t[e] += u[e];
+            w[k] = pack_piece<T>(t);
+            store_piece(total + row.column(tid + k * TH), w[k]);
+        }
+        if (odd) {
+            const T v1 = from_f32<T>(edge + to_f32(r[at]));
+            total[at] = v1;
+            edge = to_f32(v1);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (tid + k * TH >= row.pieces) continue;
+        unpack_piece<T>(w[k], t);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) sum += t[e] * t[e];
+    }
+    sum = join_row<TH, kJoinSum>(sum + edge * edge, cells[0]);
+    const float s = rsqrtf(sum / (float)P.width + P.eps);
+    if (P.rstd && tid == 0) P.rstd[i] = s;
+    if (odd) edge *= s * load_weight<T>(P.weight, P.weight_f32, at);
+    if constexpr (!CODES) {
+        T* y = static_cast<T*>(P.y) + i * P.ld_y;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * TH >= row.pieces) continue;
+            const int c = row.column(tid + k * TH);
+            float u[VE];
+            load_weights<T>(P.weight, P.weight_f32, c, u);
+            unpack_piece<T>(w[k], t);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) t[e] = t[e] * s * u[e];
+            store_piece(y + c, pack_piece<T>(t));
+        }
+        if (odd) y[at] = from_f32<T>(edge);
+    } else {
+        float v[NV][VE], top = odd ? fabsf(edge) : 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * TH >= row.pieces) continue;
+            float u[VE];
+            load_weights<T>(P.weight, P.weight_f32, row.column(tid + k * TH), u);
+            unpack_piece<T>(w[k], v[k]);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                v[k][e] = v[k][e] * s * u[e];
+                top = nan_max(top, fabsf(v[k][e]));
+            }
+        }
+        const RowCodes rc(join_row<TH, kJoinMax>(top, cells[1]));
+        signed char* q = P.codes + i * P.ld_codes;
+        if (tid == 0) P.scale[i] = rc.scale;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * TH < row.pieces) store_codes<VE>(q + row.column(tid + k * TH), rc, v[k]);
+        if (odd) q[at] = (signed char)rc.code(edge);
+    }
+}
+
+// ---- forward, rows of any length: a block of 1024 to a row, which is read again for each of the steps (from L2, mostly)
+template <typename T, bool CODES>
+__global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__ NormParams P) {
+    constexpr int VE = Piece<T>::kValues, TH = 1024;
+    __shared__ float cells[2][TH / 32];
+    const int tid = threadIdx.x;
+    const long long i = blockIdx.x;
+    const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
+    const T* r = P.residual ? static_cast<const T*>(P.residual) + i * P.ld_residual : nullptr;
+    T* total = static_cast<T*>(P.total) + i * P.ld_total;
+    const RowPieces<T> row(x, P.width);
+    const T* src = r ? total : x;  // where the sum is read from later (each thread reads what it has written)
+    const bool odd = tid < row.edges;
+    const int at = row.edge(tid);
+    float t[VE], u[VE], sum = 0.f, edge = odd ? to_f32(x[at]) : 0.f;
+    if (odd && r) {
+        const T v1 = from_f32<T>(edge + to_f32(r[at]));
+        total[at] = v1;
+        edge = to_f32(v1);
+    }
+    for (int k = tid; k < row.pieces; k += TH) {
+        const int c = row.column(k);
+        uint4 w = load_piece(x + c);
+        unpack_piece<T>(w, t);
+        if (r) {
+            unpack_piece<T>(load_piece(r + c), u);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) t[e] += u[e];
+            w = pack_piece<T>(t);
+            store_piece(total + c, w);
+            unpack_piece<T>(w, t);
+        }
+#pragma unroll
+        for (int e = 0; e < VE; ++e) sum += t[e] * t[e];
+    }
+    sum = join_row<TH, kJoinSum>(sum + edge * edge, cells[0]);
+    const float s = rsqrtf(sum / (float)P.width + P.eps);
+    if (P.rstd && tid == 0) P.rstd[i] = s;
+    if (odd) edge *= s * load_weight<T>(P.weight, P.weight_f32, at);
+    auto normed = [&](int c) {
+        unpack_piece<T>(load_piece(src + c), t);
+        load_weights<T>(P.weight, P.weight_f32, c, u);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) t[e] = t[e] * s * u[e];
+    };
+    if constexpr (!CODES) {
+        T* y = static_cast<T*>(P.y) + i * P.ld_y;
+        for (int k = tid; k < row.pieces; k += TH) {
+            normed(row.column(k));
+            store_piece(y + row.column(k), pack_piece<T>(t));
+        }
+        if (odd) y[at] = from_f32<T>(edge);
+    } else {
+        float top = odd ? fabsf(edge) : 0.f;
+        for (int k = tid; k < row.pieces; k += TH) {
+            normed(row.column(k));
+#pragma unroll
+            for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(t[e]));
+        }
+        const RowCodes rc(join_row<TH, kJoinMax>(top, cells[1]));
+        signed char* q = P.codes + i * P.ld_codes;
+        if (tid == 0) P.scale[i] = rc.scale;
+        for (int k = tid; k < row.pieces; k += TH) {
+            normed(row.column(k));
+            store_codes<VE>(q + row.column(k), rc, t);
+        }
+        if (odd) q[at] = (signed char)rc.code(edge);
+    }
+}
+
+// ---- backward: blocks (TH = 32: of eight warps, a row each) go through the rows with the grid's stride, each thread adding up its
+// columns' share of dw in registers; norm_weight_kernel adds the blocks' sums in their order, so equal calls give equal bits.  The columns of a thread are the
+// same in every row, so they are pieces (VE values of 16 bytes) where all rows start on 16-byte boundaries, single values elsewhere.
+template <typename T, int VE>
+struct Columns;  // VE neighbouring values as they are held and moved
+template <typename T>
+struct Columns<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void unpack(float (&x)[1]) const { x[0] = to_f32(v); }
+    static __device__ __forceinline__ void store(T* p, const float (&x)[1]) { *p = from_f32<T>(x[0]); }
+    static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[1]) { x[0] = load_weight<T>(w, f32, c); }
+};
+template <typename T, int VE>
+struct Columns {
+    static_assert(VE == Piece<T>::kValues, "a piece, or one value");
+    uint4 v;
+    __device__ __forceinline__ void load(const T* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void unpack(float (&x)[VE]) const { unpack_piece<T>(v, x); }
+    static __device__ __forceinline__ void store(T* p, const float (&x)[VE]) { *reinterpret_cast<uint4*>(p) = pack_piece<T>(x); }
+    static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[VE]) { load_weights<T>(w, f32, c, x); }
+};
+
+template <typename T, int VE, int TH, int NV>
+__global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 2 : 512 / TH ? 512 / TH : 1) norm_back_kernel(const __grid_constant__ NormParams P) {
+    constexpr int kGroups = TH == 32 ? 8 : 1;
+    using Col = Columns<T, VE>;
+    __shared__ float cells[2][TH / 32];
+    __shared__ float joined[TH == 32 ? 8 : 1][TH == 32 ? 32 * NV * VE : 1];
+    let_next_kernel_start();
+    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    const long long group = blockIdx.x * (long long)kGroups + (TH == 32 ? threadIdx.x >> 5 : 0u);
+    const int count = P.width / VE;  // (VE divides it)
+    float dw[NV][VE] = {};
+    int turn = 0;
+    for (long long i = group; i < P.rows; i += (long long)gridDim.x * kGroups, turn ^= 1) {
+        const T* t = static_cast<const T*>(P.x) + i * P.ld_x;
+        const T* dy = static_cast<const T*>(P.dy) + i * P.ld_dy;
+        const T* dt = static_cast<const T*>(P.dtotal) + i * P.ld_dtotal;
+        T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
+        Col a[NV], b[NV], d[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (tid + k * TH) * VE;
+            if (tid + k * TH >= count) continue;
+            a[k].load(t + c);
+            b[k].load(dy + c);
+            if (P.dtotal) d[k].load(dt + c);
+        }
+        const float s = __ldg(P.rstd + i);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * TH >= count) continue;
+            float u[VE], v[VE], w[VE];
+            a[k].unpack(u);
+            b[k].unpack(v);
+            Col::weights(P.weight, P.weight_f32, (tid + k * TH) * VE, w);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float unit = u[e] * s;
+                sum += v[e] * w[e] * unit;
+                dw[k][e] += v[e] * unit;
+            }
+        }
+        // (cells of the row before last: whoever writes them has passed the last row's barrier, behind the last use of them)
+        const float mean = join_row<TH, kJoinSum>(sum, cells[turn]) / (float)P.width;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (tid + k * TH) * VE;
+            if (tid + k * TH >= count) continue;
+            float u[VE], v[VE], w[VE];
+            a[k].unpack(u);
+            b[k].unpack(v);
+            Col::weights(P.weight, P.weight_f32, c, w);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) v[e] = s * (v[e] * w[e] - u[e] * s * mean);
+            if (P.dtotal) {
+                d[k].unpack(u);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) v[e] += u[e];
+            }
+            Col::store(dx + c, v);
+        }
+    }
+    if (!P.part) return;
+    float* part = P.part + (long long)blockIdx.x * P.width;
+    if constexpr (TH == 32) {  // the eight warps' sums, in their order
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) joined[threadIdx.x >> 5][(tid + k * 32) * VE + e] = dw[k][e];
+        __syncthreads();
+        for (int c = threadIdx.x; c < P.width; c += 256) {
+            float v = joined[0][c];
+#pragma unroll
+            for (int g = 1; g < 8; ++g) v += joined[g][c];
+            part[c] = v;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * TH >= count) continue;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) part[(tid + k * TH) * VE + e] = dw[k][e];
+        }
+    }
+}
+
+// rows of any length: read twice, the columns' sums kept in memory (each by the thread that adds to it)
+template <typename T>
+__global__ void __launch_bounds__(1024) norm_back_long_kernel(const __grid_constant__ NormParams P) {
+    constexpr int TH = 1024;
+    __shared__ float cells[2][TH / 32];
+    let_next_kernel_start();
+    const int tid = threadIdx.x;
+    float* part = P.part ? P.part + (long long)blockIdx.x * P.width : nullptr;
+    int turn = 0;
+    for (long long i = blockIdx.x; i < P.rows; i += gridDim.x, turn ^= 1) {
+        const T* t = static_cast<const T*>(P.x) + i * P.ld_x;
+        const T* dy = static_cast<const T*>(P.dy) + i * P.ld_dy;
+        const T* dt = static_cast<const T*>(P.dtotal) + i * P.ld_dtotal;
+        T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
+        const float s = __ldg(P.rstd + i);
+        float sum = 0.f;
+#pragma unroll 4
+        for (int c = tid; c < P.width; c += TH) {
+            const float unit = to_f32(t[c]) * s, v = to_f32(dy[c]);
+            sum += v * load_weight<T>(P.weight, P.weight_f32, c) * unit;
+            if (part) part[c] = i == blockIdx.x ? v * unit : part[c] + v * unit;
+        }
+        const float mean = join_row<TH, kJoinSum>(sum, cells[turn]) / (float)P.width;
+#pragma unroll 4
+        for (int c = tid; c < P.width; c += TH) {
+            float v = s * (to_f32(dy[c]) * load_weight<T>(P.weight, P.weight_f32, c) - to_f32(t[c]) * s * mean);
+            if (P.dtotal) v += to_f32(dt[c]);
+            dx[c] = from_f32<T>(v);
+        }
+    }
+}
+
+// dw from the blocks' sums: 32 columns to a block, 32 threads to a column
+template <typename T>
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* __restrict__ part, int blocks, int width, void* __restrict__ dweight, int f32) {
+    __shared__ float cells[32][33];
+    wait_for_previous_kernel();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float v = 0.f;
+    if (c < width) {
+#pragma unroll 4
+        for (int b = warp; b < blocks; b += 32) v += __ldcg(part + (long long)b * width + c);
+    }
+    cells[warp][lane] = v;
+    __syncthreads();
+    if (warp != 0 || c >= width) return;
+    v = cells[0][lane];
+#pragma unroll
+    for (int k = 1; k < 32; ++k) v += cells[k][lane];
+    if (f32) static_cast<float*>(dweight)[c] = v;
+    else static_cast<T*>(dweight)[c] = from_f32<T>(v);
+}
+
+// ---------------------------------------------------------------- rows in 8 bits
+// h = x, or act(gate) x; codes and scale as above.  A row is held as fp32 values between its maximum and its codes.
+struct CodesParams {
+    const void *x, *gate;  // gate: null for none
+    signed char* codes;
+    float* scale;
+    long long ld_x, ld_gate, ld_codes, rows;
+    int width, act;
+};
+template <typename T>
+__device__ __forceinline__ void gated_piece(const CodesParams& P, const uint4& x, const uint4& g, float (&h)[Piece<T>::kValues]) {
+    unpack_piece<T>(x, h);
+    if (P.gate) {
+        float u[Piece<T>::kValues];
+        unpack_piece<T>(g, u);
+#pragma unroll
+        for (int e = 0; e < Piece<T>::kValues; ++e) h[e] *= act_value(P.act, u[e]);
+    }
+}
+template <typename T, int TH, int NV>
+__global__ void __launch_bounds__(TH == 32 ? 256 : TH) codes_row_kernel(const __grid_constant__ CodesParams P) {
+    constexpr int VE = Piece<T>::kValues;
+    __shared__ float cells[TH / 32];
+    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i >= P.rows) return;
+    const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
+    const T* g = static_cast<const T*>(P.gate) + i * P.ld_gate;
+    const RowPieces<T> row(x, P.width);
+    uint4 w[NV], v[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (tid + k * TH >= row.pieces) continue;
+        w[k] = load_piece(x + row.column(tid + k * TH));
+        if (P.gate) v[k] = load_piece(g + row.column(tid + k * TH));
+    }
+    const bool odd = tid < row.edges;
+    const int at = row.edge(tid);
+    float edge = 0.f;
+    if (odd) edge = to_f32(x[at]) * (P.gate ? act_value(P.act, to_f32(g[at])) : 1.f);
+    float h[NV][VE], top = fabsf(edge);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (tid + k * TH >= row.pieces) continue;
+        gated_piece<T>(P, w[k], v[k], h[k]);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(h[k][e]));
+    }
+    const RowCodes rc(join_row<TH, kJoinMax>(top, cells));
+    signed char* q = P.codes + i * P.ld_codes;
+    if (tid == 0) P.scale[i] = rc.scale;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (tid + k * TH < row.pieces) store_codes<VE>(q + row.column(tid + k * TH), rc, h[k]);
+    if (odd) q[at] = (signed char)rc.code(edge);
+}
+template <typename T>
+__global__ void __launch_bounds__(1024) codes_long_kernel(const __grid_constant__ CodesParams P) {
+    constexpr int VE = Piece<T>::kValues, TH = 1024;
+    __shared__ float cells[TH / 32];
+    const int tid = threadIdx.x;
+    const long long i = blockIdx.x;
+    const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
+    const T* g = static_cast<const T*>(P.gate) + i * P.ld_gate;
+    const RowPieces<T> row(x, P.width);
+    const bool odd = tid < row.edges;
+    const int at = row.edge(tid);
+    float edge = 0.f, h[VE];
+    if (odd) edge = to_f32(x[at]) * (P.gate ? act_value(P.act, to_f32(g[at])) : 1.f);
+    float top = fabsf(edge);
+    auto read = [&](int c) { gated_piece<T>(P, load_piece(x + c), P.gate ? load_piece(g + c) : make_uint4(0, 0, 0, 0), h); };
+    for (int k = tid; k < row.pieces; k += TH) {
+        read(row.column(k));
+#pragma unroll
+        for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(h[e]));
+    }
+    const RowCodes rc(join_row<TH, kJoinMax>(top, cells));
+    signed char* q = P.codes + i * P.ld_codes;
+    if (tid == 0) P.scale[i] = rc.scale;
+    for (int k = tid; k < row.pieces; k += TH) {
+        read(row.column(k));
+        store_codes<VE>(q + row.column(k), rc, h);
+    }
+    if (odd) q[at] = (signed char)rc.code(edge);
+}
+
+// Weights [inputs][outputs] as codes [outputs][inputs] with a scale for each output: 32 outputs to a block, read once for their
+// maxima and once more for the codes, which go through shared memory to stand along the inputs.
+template <typename T>
+__global__ void __launch_bounds__(1024) codes_weight_kernel(const T* __restrict__ w, long long ld_w, int inputs, int outputs,
+                                                            signed char* __restrict__ codes, long long ld_codes, float* __restrict__ scale) {
+    __shared__ float cells[32][33];
+    __shared__ signed char tile[32][132];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float top = 0.f;
+    if (c < outputs) {
+#pragma unroll 4
+        for (int k = warp; k < inputs; k += 32) top = nan_max(top, fabsf(to_f32(w[(long long)k * ld_w + c])));
+    }
+    cells[warp][lane] = top;
+    __syncthreads();
+    top = cells[0][lane];
+#pragma unroll
+    for (int k = 1; k < 32; ++k) top = nan_max(top, cells[k][lane]);
+    const RowCodes rc(top);
+    if (warp == 0 && c < outputs) scale[c] = rc.scale;
+    for (int k0 = 0; k0 < inputs; k0 += 128) {
+#pragma unroll
+        for (int k = warp; k < 128; k += 32)
+            tile[lane][k] = c < outputs && k0 + k < inputs ? (signed char)rc.code(to_f32(w[(long long)(k0 + k) * ld_w + c])) : 0;
+        __syncthreads();
+        const int out = blockIdx.x * 32 + warp;
+        if (out < outputs) {
+#pragma unroll
+            for (int k = lane; k < 128; k += 32)
+                if (k0 + k < inputs) codes[(long long)out * ld_codes + k0 + k] = tile[warp][k];
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace bmgdk

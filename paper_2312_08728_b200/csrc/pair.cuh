@@ -16,5 +16,9 @@ struct Pair {
 };
 __device__ __forceinline__ Pair operator+(Pair a, const Pair& b) { asm("add.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v)); return a; }
 __device__ __forceinline__ Pair operator*(Pair a, const Pair& b) { asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(a.v) : "l"(b.v)); return a; }
+__device__ __forceinline__ Pair multiply_add(const Pair& a, const Pair& b, Pair c) {  // one rounding
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(c.v) : "l"(a.v), "l"(b.v));
+    return c;
+}
 
 }  // namespace bmgdk

@@ -7,36 +7,18 @@
 // [0, C), or whose logits are all -inf (a mask that leaves nothing), has no gradient: zeros, loss 0.
 #pragma once
 #include <cstdint>
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
-#include "pair.cuh"
 #include "shuffle.cuh"
+#include "values.cuh"
 
 namespace bmgdk {
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-template <typename T> __device__ __forceinline__ float to_f32(T x);
-template <> __device__ __forceinline__ float to_f32<float>(float x) { return x; }
-template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <> __device__ __forceinline__ float to_f32<__half>(__half x) { return __half2float(x); }
-template <typename T> __device__ __forceinline__ T from_f32(float x);
-template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
 // Maximum and sum of exp(z - maximum) of some of a row's logits.  NaN enters the sum, not the maximum; while the maximum is
 // -inf the sum is taken relative to 0, so that -inf counts for nothing and NaN still shows.
 struct MaxSum {
     float m, s;
 };
-__device__ __forceinline__ float exp_fast(float x) {  // exp for x <= 0 within 2^-22 + |x| 2^-23 of itself; below 2^-126 zero
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * kLog2e));
-    return r;
-}
 // (the difference is taken first: next to the type's lowest value a product with log2 e would overflow)
 __device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.f : m; }
 // factor that takes a sum to a larger maximum; a sum without one is 0 or NaN and stays so (0 times the exponential of what
@@ -103,15 +85,6 @@ __global__ void __launch_bounds__(256, 6) residual_short_kernel(const T* __restr
 // R blocks (a cluster) of TH threads share a row (TH = 32: a warp has one, eight to a block).  A thread holds up to NV pieces
 // of 16 bytes; the logits before the first 16-byte boundary and behind the last go one each to the first threads.  All
 // of a thread's loads are in flight together, which is what keeps memory busy: bound by the one pass over the data.
-template <typename T> struct Piece {
-    static constexpr int kValues = 16 / (int)sizeof(T);
-};
-template <typename T>
-__device__ __forceinline__ void unpack_piece(const uint4& w, float (&x)[Piece<T>::kValues]) {
-    const T* p = reinterpret_cast<const T*>(&w);
-#pragma unroll
-    for (int i = 0; i < Piece<T>::kValues; ++i) x[i] = to_f32(p[i]);
-}
 __device__ __forceinline__ uint32_t residual_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -133,13 +106,6 @@ __device__ __forceinline__ void piece_powers(const uint4& w, const Pair& minus_m
         take(e, Pair(p.x, p.y));
     }
 }
-template <typename T> __device__ __forceinline__ void put_pair(T* t, const Pair& p);
-template <> __device__ __forceinline__ void put_pair<float>(float* t, const Pair& p) { const float2 x = p.both(); t[0] = x.x; t[1] = x.y; }
-template <> __device__ __forceinline__ void put_pair<__nv_bfloat16>(__nv_bfloat16* t, const Pair& p) {
-    *reinterpret_cast<__nv_bfloat162*>(t) = __float22bfloat162_rn(p.both());
-}
-template <> __device__ __forceinline__ void put_pair<__half>(__half* t, const Pair& p) { *reinterpret_cast<__half2*>(t) = __float22half2_rn(p.both()); }
-
 // largest of a piece's values and `top`, NaN left aside
 __device__ __forceinline__ float piece_max(float top, const uint4& w, float) {
     float x[4];

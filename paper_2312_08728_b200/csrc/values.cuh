@@ -1,0 +1,110 @@
+// Values of the three element types in fp32 and back, and rows of them in pieces of 16 bytes.
+#pragma once
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "pair.cuh"
+
+namespace bmgdk {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <typename T> __device__ __forceinline__ float to_f32(T x);
+template <> __device__ __forceinline__ float to_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float to_f32<__half>(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+__device__ __forceinline__ float exp_fast(float x) {  // exp for x <= 0 within 2^-22 + |x| 2^-23 of itself; below 2^-126 zero
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * kLog2e));
+    return r;
+}
+template <typename T> struct Piece {
+    static constexpr int kValues = 16 / (int)sizeof(T);
+};
+template <typename T>
+__device__ __forceinline__ void unpack_piece(const uint4& w, float (&x)[Piece<T>::kValues]) {
+    const T* p = reinterpret_cast<const T*>(&w);
+#pragma unroll
+    for (int i = 0; i < Piece<T>::kValues; ++i) x[i] = to_f32(p[i]);
+}
+template <typename T> __device__ __forceinline__ void put_pair(T* t, const Pair& p);
+template <> __device__ __forceinline__ void put_pair<float>(float* t, const Pair& p) { const float2 x = p.both(); t[0] = x.x; t[1] = x.y; }
+template <> __device__ __forceinline__ void put_pair<__nv_bfloat16>(__nv_bfloat16* t, const Pair& p) {
+    *reinterpret_cast<__nv_bfloat162*>(t) = __float22bfloat162_rn(p.both());
+}
+template <> __device__ __forceinline__ void put_pair<__half>(__half* t, const Pair& p) { *reinterpret_cast<__half2*>(t) = __float22half2_rn(p.both()); }
+
+// A piece at p, at once where it stands on a 16-byte boundary, value by value elsewhere.  What is read once and what is
+// written for a later kernel passes the caches as data that is not wanted again.
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T* p) {
+    if (((uintptr_t)p & 15u) == 0) return __ldcs(reinterpret_cast<const uint4*>(p));
+    uint4 w;
+    T* t = reinterpret_cast<T*>(&w);
+#pragma unroll
+    for (int i = 0; i < Piece<T>::kValues; ++i) t[i] = p[i];
+    return w;
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, const uint4& w) {
+    if (((uintptr_t)p & 15u) == 0) {
+        *reinterpret_cast<uint4*>(p) = w;
+        return;
+    }
+    const T* t = reinterpret_cast<const T*>(&w);
+#pragma unroll
+    for (int i = 0; i < Piece<T>::kValues; ++i) p[i] = t[i];
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_piece(const float (&x)[Piece<T>::kValues]) {
+    uint4 w;
+    T* t = reinterpret_cast<T*>(&w);
+#pragma unroll
+    for (int i = 0; i < Piece<T>::kValues; i += 2) put_pair<T>(t + i, Pair(x[i], x[i + 1]));
+    return w;
+}
+// How a row of `width` values at p falls into pieces: `head` values before the first 16-byte boundary, `pieces`, the rest.
+// (head + rest < 2 * 16 / sizeof(T) <= 16 values, one each for the first threads.)
+template <typename T>
+struct RowPieces {
+    int head, pieces, edges;
+    __device__ __forceinline__ RowPieces(const T* p, int width) {
+        head = min(width, (int)(((16u - ((uintptr_t)p & 15u)) & 15u) / sizeof(T)));
+        pieces = (width - head) / Piece<T>::kValues;
+        edges = width - pieces * Piece<T>::kValues;
+    }
+    __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + pieces * Piece<T>::kValues; }  // column of edge i
+    __device__ __forceinline__ int column(int piece) const { return head + piece * Piece<T>::kValues; }
+};
+
+// A value joined over the threads of a row, in a fixed order: a warp (TH = 32) or a block of TH threads.  `cells` (TH / 32
+// values) is this use's own until the next barrier of the block.
+enum { kJoinSum, kJoinMax };
+template <int TH, int OP>
+__device__ __forceinline__ float join_row(float v, float* cells) {
+    auto op = [](float a, float b) {
+        if (OP == kJoinSum) return a + b;
+        float m;  // (NaN wins)
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+        return m;
+    };
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    if constexpr (TH > 32) {
+        if ((threadIdx.x & 31) == 0) cells[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = cells[0];
+#pragma unroll
+        for (int k = 1; k < TH / 32; ++k) v = op(v, cells[k]);
+    }
+    return v;
+}
+
+}  // namespace bmgdk

@@ -1,4 +1,4 @@
-"""Operators of one training step of a gated network, on device tensors.
+"""Operators of a gated network's training step, and of its scoring, on device tensors.
 
     rows, labels = gather_batch(x, y, seed, chain, round, first, count)      the mini-batch of the shuffled buffer
     logits, saved = gated_ffn(rows, w_gate, w_up, w_down, save=True)         (act(X Wg) * (X Wu)) Wd
@@ -6,14 +6,28 @@
     dx, dw_gate, dw_up, dw_down = gated_ffn_backward(residual, rows, w_gate, w_up, w_down, saved)
     adamw_step([w_gate, w_up, w_down], [dw_gate, dw_up, dw_down], m, v, control, lr=1e-3)
 
+Between blocks:
+
+    y, total, rstd = rms_norm(x, weight, residual=total, save=True)          norm of x + residual
+    dx, dweight = rms_norm_backward(dy, total, weight, rstd, dtotal)         dx is the gradient of the residual too
+    total = dropout(y, rate, seed, layer, step, residual=total)              its gradient: dropout(dtotal, rate, seed, layer, step)
+
+Scored with weights in 8 bits, and the answer:
+
+    codes, scale = quantize_weight(w)                                        laid out once
+    q, q_scale, total = rms_norm_int8(x, weight, residual=total)             or quantize_rows(up, gate=gate)
+    y = int8_linear(q, q_scale, codes, scale)
+    logprob, entropy, classes, logprobs = log_probs(logits, labels, top=5)   log_probs_backward for its gradient
+
 Argument checks and marshalling only: the computation runs in the CUDA library (include/bmgd.h), which takes bare
 pointers, so whatever the tensors' own metadata can tell is refused here.  Work is ordered on `stream`, by default the
 current stream of the tensors' device; nothing waits for the device, so every call can be captured into a CUDA graph.
 Outputs and workspaces come from torch's allocator on that stream.  Where `stream` is not the current one, the order between
 the two is the caller's (wait_stream or events); the memory of inputs and outputs is kept until both are done with it.
 
-None of them is part of an autograd graph: gradients are outputs like others.  gated_ffn refuses tensors that require gradients
-where a graph would be recorded (call it under torch.no_grad(), with gated_ffn_backward beside it).  adamw_step writes parameters and
+None of them is part of an autograd graph: gradients are outputs like others.  gated_ffn, rms_norm, rms_norm_int8, quantize_rows, int8_linear,
+log_probs and dropout refuse tensors that require gradients where a graph would be recorded (call them under torch.no_grad(), with the
+backward calls beside them).  adamw_step writes parameters and
 copies in place and tells autograd so: a graph that has saved one of them refuses its backward pass (an update that is replayed from a
 CUDA graph tells it only at its capture).
 """
@@ -121,6 +135,26 @@ def _device_of(t: torch.Tensor, name: str) -> torch.device:
     return t.device
 
 
+def _no_graph(name: str, *tensors: Optional[torch.Tensor]) -> None:
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{name} records no autograd graph: call it under torch.no_grad(), or with detached tensors")
+
+
+def _vector(t: Optional[torch.Tensor], name: str, size: int, dtype: torch.dtype, device: torch.device) -> int:
+    """Refuse a tensor that is not a contiguous vector of that size and type; returns its address (0 for None)."""
+    if t is None:
+        return 0
+    if t.dim() != 1 or t.shape[0] != size or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} [{size}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _floating(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
 # ---------------------------------------------------------------- gated feed-forward block
 
 # bmgd_gated_ffn of include/bmgd.h: rows; inputs, hidden, outputs, type, activation, reserved; x, w_gate, w_up, w_down and their
@@ -173,8 +207,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     that type in between (float16: it must stay below 65,504).  With save=True returns (y, saved), saved
     being what gated_ffn_backward needs beside its other arguments."""
     shared, (n, d, f, c), device = _ffn_args(x, w_gate, w_up, w_down, activation)
-    if torch.is_grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or w_down.requires_grad):
-        raise ValueError("gated_ffn records no autograd graph: call it under torch.no_grad(), or with detached tensors")
+    _no_graph("gated_ffn", x, w_gate, w_up, w_down)
     place = _place(device, stream)
     _lend(stream, device, (x, w_gate, w_up, w_down))
     with place:
@@ -216,7 +249,7 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, 
 
 
 def stream_check(stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Wait for the stream and raise, once, if a device-side wait of a gated-block kernel on its device gave up.  What that kernel had
+    """Wait for the stream and raise, once, if a device-side wait of a gated-block or 8-bit product kernel on its device gave up.  What that kernel had
     not computed by then is NaN in its outputs."""
     s = stream if stream is not None else torch.cuda.current_stream()
     with torch.cuda.device(s.device):
@@ -279,6 +312,292 @@ def gather_batch(x: torch.Tensor, y: Optional[torch.Tensor], seed: int, chain: i
                                     _current(device)), "bmgd_gather_batch")
     _hand(stream, device, (bx, by))
     return bx, by
+
+
+# ---------------------------------------------------------------- norm with the residual's addition, rows in 8 bits
+
+# bmgd_rms_norm of include/bmgd.h: rows; width, type, weight_type, reserved; eps; x, residual, weight, total, y, codes, scale, rstd; strides of
+# x, residual, total, y, codes; dy, dtotal, dx, dweight; strides of dy, dtotal, dx
+_RMS_NORM = struct.Struct("=q4id8Q5q4Q3q")
+
+
+def _norm_args(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, name: str):
+    """What all the norm's calls check, and (device, rows, width, stride of x, the struct's first members, address of weight)."""
+    device = _device_of(x, name)
+    code = _floating(x, name)
+    n, d, ld = _matrix(x, name, None, None, x.dtype, device)
+    if d < 1:
+        raise ValueError(f"{name} needs at least one column")
+    if not 0.0 <= eps < float("inf"):
+        raise ValueError(f"eps must be non-negative and finite, got {eps}")
+    kind = code
+    if weight is not None:
+        if weight.dtype is not x.dtype and weight.dtype is not torch.float32:
+            raise ValueError(f"weight must be {x.dtype} or float32, got {weight.dtype}")
+        kind = _TYPES[weight.dtype]
+    at = _vector(weight, "weight", d, weight.dtype if weight is not None else x.dtype, device)
+    return device, n, d, ld, (n, d, code, kind, 0, float(eps)), at
+
+
+def _codes_like(n: int, width: int, device: torch.device) -> torch.Tensor:
+    """Uninitialised codes [n, width] whose rows start on 16-byte boundaries."""
+    wide = -(-width // 16) * 16
+    codes = torch.empty((n, wide), dtype=torch.int8, device=device)
+    return codes if wide == width else codes[:, :width]
+
+
+def _run_norm(name, x, weight, residual, eps, save, quantized, stream):
+    device, n, d, ld_x, head, _ = _norm_args(x, weight, eps, "x")
+    ld_r = 0
+    if residual is not None:
+        _, _, ld_r = _matrix(residual, "residual", n, d, x.dtype, device)
+    _no_graph(name, x, weight, residual)
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (x, weight, residual))
+    with place:
+        total = x if residual is None else x.new_empty((n, d))
+        y, codes, scale, rstd = None, None, None, None
+        if quantized:
+            codes, scale = _codes_like(n, d, device), torch.empty(n, dtype=torch.float32, device=device)
+        else:
+            y = x.new_empty((n, d))
+        if save:
+            rstd = torch.empty(n, dtype=torch.float32, device=device)
+        if n > 0:
+            pointers = [0 if t is None else t.data_ptr() for t in (x, residual, weight, total if residual is not None else None, y, codes, scale, rstd)]
+            _status(L.bmgd_rms_norm_forward(_RMS_NORM.pack(*head, *pointers, ld_x, ld_r, d, d, codes.stride(0) if quantized else 0, 0, 0, 0, 0, 0, 0, 0),
+                                            _current(device)), "bmgd_rms_norm_forward")
+    _hand(stream, device, (total if residual is not None else None, y, codes, scale, rstd))
+    return y, codes, scale, total, rstd
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             save: bool = False, stream: Optional[torch.cuda.Stream] = None):
+    """(y, total) for x [rows, width] and, of the same size and type, residual: total = x + residual in that type (x itself without a
+    residual), y = total / sqrt(mean(total^2) + eps) * weight.  With save=True (y, total, rstd), what rms_norm_backward needs.
+
+    float32, bfloat16 or float16, rows contiguous, any row stride; weight [width] of that type or float32.  Sums are fp32."""
+    y, _, _, total, rstd = _run_norm("rms_norm", x, weight, residual, eps, save, False, stream)
+    return (y, total, rstd) if save else (y, total)
+
+
+def rms_norm_int8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(codes, scale, total): as rms_norm, with y in 8 bits as int8_linear reads it (y is about codes * scale[:, None])."""
+    _, codes, scale, total, _ = _run_norm("rms_norm_int8", x, weight, residual, eps, False, True, stream)
+    return codes, scale, total
+
+
+def rms_norm_backward(dy: torch.Tensor, total: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor,
+                      dtotal: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(dx, dweight) of rms_norm for the gradient dy of y and, where total is used further on, dtotal of total.  dx is the gradient
+    of x and of the residual; dweight has the weight's type (None without a weight)."""
+    device, n, d, ld_t, head, at_weight = _norm_args(total, weight, 0.0, "total")
+    _, _, ld_dy = _matrix(dy, "dy", n, d, total.dtype, device)
+    ld_dt = 0
+    if dtotal is not None:
+        _, _, ld_dt = _matrix(dtotal, "dtotal", n, d, total.dtype, device)
+    at_rstd = _vector(rstd, "rstd", n, torch.float32, device)
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (dy, total, weight, rstd, dtotal))
+    with place:
+        dx = total.new_empty((n, d))
+        dweight = torch.empty_like(weight) if weight is not None else None
+        args = _RMS_NORM.pack(*head, 0, 0, at_weight, total.data_ptr(), 0, 0, 0, at_rstd, 0, 0, ld_t, 0, 0, dy.data_ptr(),
+                              dtotal.data_ptr() if dtotal is not None else 0, dx.data_ptr(), dweight.data_ptr() if weight is not None else 0, ld_dy, ld_dt, d)
+        need = ctypes.c_int64()
+        _status(L.bmgd_rms_norm_workspace_bytes(args, ctypes.byref(need)), "bmgd_rms_norm_workspace_bytes")
+        w = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+        _status(L.bmgd_rms_norm_backward(args, w.data_ptr() if w is not None else None, need.value, _current(device)), "bmgd_rms_norm_backward")
+    _hand(stream, device, (dx, dweight))
+    return dx, dweight
+
+
+def quantize_rows(x: torch.Tensor, gate: Optional[torch.Tensor] = None, activation: int = ACT_SILU,
+                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(codes, scale) of the rows of x [rows, width], or with a gate of the same size and type those of act(gate) * x: int8 with
+    the row's largest magnitude at 127, and that magnitude / 127 in float32."""
+    device = _device_of(x, "x")
+    code = _floating(x, "x")
+    n, d, ld_x = _matrix(x, "x", None, None, x.dtype, device)
+    if d < 1:
+        raise ValueError("x needs at least one column")
+    ld_g = 0
+    if gate is not None:
+        _, _, ld_g = _matrix(gate, "gate", n, d, x.dtype, device)
+    if activation not in (ACT_SILU, ACT_GELU, ACT_RELU, ACT_SIGMOID):
+        raise ValueError(f"unknown activation code {activation}")
+    _no_graph("quantize_rows", x, gate)
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (x, gate))
+    with place:
+        codes, scale = _codes_like(n, d, device), torch.empty(n, dtype=torch.float32, device=device)
+        if n > 0:
+            _status(L.bmgd_quantize_rows(x.data_ptr(), ld_x, gate.data_ptr() if gate is not None else None, ld_g, n, d, code, activation,
+                                         codes.data_ptr(), codes.stride(0), scale.data_ptr(), _current(device)), "bmgd_quantize_rows")
+    _hand(stream, device, (codes, scale))
+    return codes, scale
+
+
+# ---------------------------------------------------------------- product in 8-bit integers
+
+def quantize_weight(w: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(codes, scale) of a weight [inputs, outputs] as int8_linear reads it: int8 [outputs, inputs] with each output's largest
+    magnitude at 127, and that magnitude / 127 in float32 [outputs].  Done once for a weight."""
+    device = _device_of(w, "w")
+    code = _floating(w, "w")
+    d, c, ld = _matrix(w, "w", None, None, w.dtype, device)
+    if d < 1 or c < 1:
+        raise ValueError("w needs at least one input and one output")
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (w,))
+    with place:
+        codes, scale = _codes_like(c, d, device), torch.empty(c, dtype=torch.float32, device=device)
+        _status(L.bmgd_quantize_weight(w.data_ptr(), ld, d, c, code, codes.data_ptr(), codes.stride(0), scale.data_ptr(), _current(device)),
+                "bmgd_quantize_weight")
+    _hand(stream, device, (codes, scale))
+    return codes, scale
+
+
+# bmgd_quantized_linear_args: rows; inputs, outputs, type, reserved; codes, scale, weight, weight_scale, bias, y; ld_codes, ld_weight, ld_y
+_QUANTIZED_LINEAR = struct.Struct("=q4i6Q3q")
+_MOST_INPUTS = 131071
+
+
+def int8_linear(q: torch.Tensor, q_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """(q w^T) * q_scale[:, None] * w_scale + bias for q [rows, inputs] and w [outputs, inputs] in int8, scales and bias in float32; the sums
+    are exact, the result is rounded once to dtype (float32, bfloat16 or float16).  Up to 131,071 inputs."""
+    device = _device_of(q, "q")
+    n, d, ld_q = _matrix(q, "q", None, None, torch.int8, device)
+    c, _, ld_w = _matrix(w, "w", None, d, torch.int8, device)
+    if c < 1 or not 1 <= d <= _MOST_INPUTS:
+        raise ValueError(f"the product needs 1 to {_MOST_INPUTS} inputs and at least one output, got {d} and {c}")
+    if dtype not in _TYPES:
+        raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+    at_q, at_w, at_b = (_vector(t, name, k, torch.float32, device) for t, name, k in ((q_scale, "q_scale", n), (w_scale, "w_scale", c), (bias, "bias", c)))
+    if q_scale is None or w_scale is None:
+        raise ValueError("q_scale and w_scale are needed")
+    _no_graph("int8_linear", q_scale, w_scale, bias)
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (q, q_scale, w, w_scale, bias))
+    with place:
+        y = torch.empty((n, c), dtype=dtype, device=device)
+        if n > 0:
+            args = _QUANTIZED_LINEAR.pack(n, d, c, _TYPES[dtype], 0, q.data_ptr(), at_q, w.data_ptr(), at_w, at_b, y.data_ptr(), ld_q, ld_w, c)
+            need = ctypes.c_int64()
+            _status(L.bmgd_quantized_linear_workspace_bytes(args, ctypes.byref(need)), "bmgd_quantized_linear_workspace_bytes")
+            work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+            _status(L.bmgd_quantized_linear(args, work.data_ptr() if work is not None else None, need.value, _current(device)), "bmgd_quantized_linear")
+    _hand(stream, device, (y,))
+    return y
+
+
+# ---------------------------------------------------------------- log probabilities
+
+# bmgd_log_probs_args: rows; C, type, top, reserved; logits, y, logprob, entropy, saved, top_class, top_logprob; ld_logits; dlogprob, dentropy,
+# dlogits; ld_dlogits
+_LOG_PROBS = struct.Struct("=q4i7Qq3Qq")
+MOST_ALTERNATIVES = 32
+
+
+def _score_args(logits: torch.Tensor, y: Optional[torch.Tensor]):
+    device = _device_of(logits, "logits")
+    code = _floating(logits, "logits")
+    rows, C, ld = _matrix(logits, "logits", None, None, logits.dtype, device)
+    if C < 1:
+        raise ValueError("logits need at least one class")
+    return device, code, rows, C, ld, _vector(y, "y", rows, torch.int32, device)
+
+
+def log_probs(logits: torch.Tensor, y: Optional[torch.Tensor] = None, top: int = 0, save: bool = False,
+              stream: Optional[torch.cuda.Stream] = None):
+    """(logprob, entropy, classes, logprobs) of logits [rows, C]: the log probability of the int32 label y of each row (0 for a row whose
+    label is outside [0, C), or without y), the entropy of its distribution, and its `top` (0 to 32) most probable classes with their log
+    probabilities [rows, top], in falling order, equal ones by rising class.  All in float32 and int32.  With save=True a fifth,
+    what log_probs_backward needs.
+
+    Rows whose logits are all -Inf have log probability and entropy 0 and alternatives of -Inf; NaN and +Inf in a row give NaN."""
+    device, code, rows, C, ld, at_y = _score_args(logits, y)
+    if not 0 <= top <= min(C, MOST_ALTERNATIVES):
+        raise ValueError(f"top must be 0 to {min(C, MOST_ALTERNATIVES)}, got {top}")
+    _no_graph("log_probs", logits)
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (logits, y))
+    with place:
+        logprob, entropy = (torch.empty(rows, dtype=torch.float32, device=device) for _ in range(2))
+        classes = torch.empty((rows, top), dtype=torch.int32, device=device)
+        values = torch.empty((rows, top), dtype=torch.float32, device=device)
+        saved = torch.empty((rows, 3), dtype=torch.float32, device=device) if save else None
+        if rows > 0:
+            _status(L.bmgd_log_probs(_LOG_PROBS.pack(rows, C, code, top, 0, logits.data_ptr(), at_y, logprob.data_ptr(), entropy.data_ptr(),
+                                                     saved.data_ptr() if save else 0, classes.data_ptr() if top else 0, values.data_ptr() if top else 0,
+                                                     ld, 0, 0, 0, 0), _current(device)), "bmgd_log_probs")
+    _hand(stream, device, (logprob, entropy, classes, values, saved))
+    return (logprob, entropy, classes, values, saved) if save else (logprob, entropy, classes, values)
+
+
+def log_probs_backward(dlogprob: Optional[torch.Tensor], dentropy: Optional[torch.Tensor], logits: torch.Tensor, y: Optional[torch.Tensor],
+                       saved: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of the logits, in their type, for the gradients of log_probs' first two results (float32 [rows], None for zero).
+
+    float16 holds no gradients of a mean over many rows: scale the two up (as softmax_residual says)."""
+    device, code, rows, C, ld, at_y = _score_args(logits, y)
+    at_l, at_e = _vector(dlogprob, "dlogprob", rows, torch.float32, device), _vector(dentropy, "dentropy", rows, torch.float32, device)
+    if saved.shape != (rows, 3) or saved.dtype is not torch.float32 or saved.device != device or not saved.is_contiguous():
+        raise ValueError("saved must be what log_probs returned for the same logits")
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (dlogprob, dentropy, logits, y, saved))
+    with place:
+        dlogits = _like(logits, ld)
+        if rows > 0:
+            _status(L.bmgd_log_probs_backward(_LOG_PROBS.pack(rows, C, code, 0, 0, logits.data_ptr(), at_y, 0, 0, saved.data_ptr(), 0, 0, ld,
+                                                              at_l, at_e, dlogits.data_ptr(), C), _current(device)), "bmgd_log_probs_backward")
+    _hand(stream, device, (dlogits,))
+    return dlogits
+
+
+# ---------------------------------------------------------------- dropout
+
+def dropout(x: torch.Tensor, rate: float, seed: int, layer: int = 0, step: Optional[torch.Tensor] = None,
+            residual: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """x [rows, width] with a share `rate` of its values dropped and the others divided by what is kept, plus the residual.
+
+    Which values stay follows from (seed, layer, step) and a value's place alone (bmgd_dropout in include/bmgd.h): the gradient is the same call
+    on the output's gradient, without the residual.  step: an int64 [1] on the device, read when the call runs, for instance
+    state["control"][:1] of adamw_state, so that a captured call draws anew with each update; None counts as 0."""
+    device = _device_of(x, "x")
+    code = _floating(x, "x")
+    n, d, ld_x = _matrix(x, "x", None, None, x.dtype, device)
+    if d < 1:
+        raise ValueError("x needs at least one column")
+    ld_r = 0
+    if residual is not None:
+        _, _, ld_r = _matrix(residual, "residual", n, d, x.dtype, device)
+    if not 0.0 <= rate < 1.0 - 2.0 ** -17:
+        raise ValueError(f"rate must be 0 to below 1 - 2^-17, got {rate}")
+    if not 0 <= layer <= 0xFFFF:
+        raise ValueError(f"layer must be 0 to 65535, got {layer}")
+    at_step = _vector(step, "step", 1, torch.int64, device)
+    _no_graph("dropout", x, residual)
+    L = _binding.load_library()
+    place = _place(device, stream)
+    _lend(stream, device, (x, residual, step))
+    with place:
+        y = x.new_empty((n, d))
+        if n > 0:
+            _status(L.bmgd_dropout(x.data_ptr(), ld_x, residual.data_ptr() if residual is not None else None, ld_r, n, d, code, float(rate),
+                                   int(seed) & 0xFFFFFFFFFFFFFFFF, at_step or None, layer, y.data_ptr(), d, _current(device)), "bmgd_dropout")
+    _hand(stream, device, (y,))
+    return y
 
 
 # ---------------------------------------------------------------- AdamW
