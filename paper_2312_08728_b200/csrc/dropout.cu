@@ -8,15 +8,19 @@ namespace {
 
 using namespace bmgdk;
 
+template <typename T, bool ONE_ROW, bool RES>
+int dropout_as(const DropoutParams& P, cudaStream_t s) {
+    constexpr int kAhead = 2;
+    const int64_t units = ONE_ROW ? (P.width + 7) / 8 : P.rows * ((P.width + 7) / 8 + 1);
+    const int64_t blocks = (units + 256 * kAhead - 1) / (256 * kAhead);
+    if (blocks > 0x7FFFFFFFll) return BMGD_ERR_ARG;
+    dropout_kernel<T, ONE_ROW, RES, kAhead><<<(unsigned)blocks, 256, 0, s>>>(P);
+    return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA;
+}
 template <typename T>
 int dropout(const DropoutParams& P, cudaStream_t s) {
-    const bool one = P.rows == 1;
-    const int64_t units = one ? (P.width + 7) / 8 : P.rows * ((P.width + 7) / 8 + 1);
-    const int64_t blocks = (units + 256 * kDropAhead - 1) / (256 * kDropAhead);
-    if (blocks > 0x7FFFFFFFll) return BMGD_ERR_ARG;
-    if (one) dropout_kernel<T, true><<<(unsigned)blocks, 256, 0, s>>>(P);
-    else dropout_kernel<T, false><<<(unsigned)blocks, 256, 0, s>>>(P);
-    return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA;
+    if (P.rows == 1) return P.residual ? dropout_as<T, true, true>(P, s) : dropout_as<T, true, false>(P, s);
+    return P.residual ? dropout_as<T, false, true>(P, s) : dropout_as<T, false, false>(P, s);
 }
 
 // [rows][width] of strides lp and lq (in bytes w a row): the same memory value for value, or none of it

@@ -28,58 +28,69 @@ struct DropoutParams {
     float factor;
 };
 
-constexpr int kDropAhead = 4;  // blocks of eight values that a thread has under way
-
-// rows of `width` values; contiguous tensors come as one row.  A row's values lie in blocks (i width) / 8 to ((i + 1) width - 1) / 8,
-// the first and the last of which it may share with its neighbours.
-template <typename T, bool ONE_ROW>
+// Rows of `width` values; contiguous tensors come as one row.  A row's values lie in blocks (i width) / 8 to ((i + 1) width - 1) / 8,
+// the first and the last of which it may share with its neighbours.  AHEAD: blocks of eight values that a thread has under way.
+template <typename T, bool ONE_ROW, bool RES, int AHEAD>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropoutParams P) {
     constexpr int VE = Piece<T>::kValues, kParts = 8 / VE;
     const uint32_t step = P.step ? (uint32_t)__ldg(P.step) : 0u;
     const uint32_t k0 = (uint32_t)P.seed, k1 = (uint32_t)(P.seed >> 32);
+    const uint32_t limits = P.threshold | P.threshold << 16;
     const long long per = ONE_ROW ? (P.width + 7) / 8 : (P.width + 7) / 8 + 1, units = ONE_ROW ? per : per * P.rows;
-    const long long first = (long long)blockIdx.x * (256 * kDropAhead) + threadIdx.x;
-    uint4 v[kDropAhead][kParts], r[kDropAhead][kParts];
-    long long at[kDropAhead], row[kDropAhead];  // first value of the block in its row (may be negative), row
+    const long long chunk = (long long)blockIdx.x * (256 * AHEAD);
+    uint4 v[AHEAD][kParts], r[AHEAD][kParts];
+    const T *x[AHEAD], *z[AHEAD];
+    T* y[AHEAD];
+    long long block[AHEAD];
+    int first[AHEAD], last[AHEAD];  // values of the block that belong to the row
 #pragma unroll
-    for (int a = 0; a < kDropAhead; ++a) {
-        const long long u = first + a * 256;
-        row[a] = ONE_ROW ? 0 : u / per;
-        const long long start = ONE_ROW ? 0 : row[a] * P.width;
-        at[a] = u < units ? (start / 8 + (ONE_ROW ? u : u - row[a] * per)) * 8 - start : P.width;
-        if (at[a] < 0 || at[a] + 8 > P.width) continue;
-        const T* x = static_cast<const T*>(P.x) + row[a] * P.ld_x + at[a];
-        const T* z = static_cast<const T*>(P.residual) + row[a] * P.ld_residual + at[a];
+    for (int a = 0; a < AHEAD; ++a) {
+        const long long u = chunk + (int)threadIdx.x + a * 256;
+        long long row = 0, at = u * 8;
+        block[a] = u;
+        if constexpr (!ONE_ROW) {
+            row = u < 0xFFFFFFFFll && per < 0xFFFFFFFFll ? (long long)((uint32_t)u / (uint32_t)per) : u / per;
+            const long long start = row * P.width;
+            block[a] = start / 8 + (u - row * per);
+            at = block[a] * 8 - start;
+        }
+        first[a] = at < 0 ? (int)-at : 0;
+        last[a] = u >= units ? 0 : (int)min(8ll, P.width - at);  // (may be negative)
+        x[a] = static_cast<const T*>(P.x) + row * P.ld_x + at;
+        z[a] = static_cast<const T*>(P.residual) + row * P.ld_residual + at;
+        y[a] = static_cast<T*>(P.y) + row * P.ld_y + at;
+        if (first[a] > 0 || last[a] < 8) continue;
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
-            v[a][p] = load_piece(x + p * VE);
-            if (P.residual) r[a][p] = load_piece(z + p * VE);
+            v[a][p] = load_piece(x[a] + p * VE);
+            if constexpr (RES) r[a][p] = load_piece(z[a] + p * VE);
         }
     }
 #pragma unroll
-    for (int a = 0; a < kDropAhead; ++a) {
-        if (at[a] >= P.width) continue;
-        const long long block = ((ONE_ROW ? 0 : row[a] * P.width) + at[a]) / 8;
+    for (int a = 0; a < AHEAD; ++a) {
+        if (last[a] <= first[a]) continue;
         uint32_t w[4];
-        philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), step, P.tag, k0, k1, w);
-        auto kept = [&](int e, float x) { return ((w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu) >= P.threshold ? x * P.factor : 0.f; };
-        T* y = static_cast<T*>(P.y) + row[a] * P.ld_y + at[a];
-        if (at[a] >= 0 && at[a] + 8 <= P.width) {
+        philox4x32_10((uint32_t)block[a], (uint32_t)(block[a] >> 32), step, P.tag, k0, k1, w);
+        bool keep[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) __vibmax_u16x2(w[e >> 1], limits, &keep[e + 1], &keep[e]);  // (both halves at once: whether a half is at least its limit)
+        if (first[a] == 0 && last[a] == 8) {
 #pragma unroll
             for (int p = 0; p < kParts; ++p) {
-                float x[VE], z[VE];
-                unpack_piece<T>(v[a][p], x);
-                if (P.residual) unpack_piece<T>(r[a][p], z);
+                float f[VE], g[VE];
+                unpack_piece<T>(v[a][p], f);
+                if constexpr (RES) unpack_piece<T>(r[a][p], g);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) x[e] = kept(p * VE + e, x[e]) + (P.residual ? z[e] : 0.f);
-                store_piece(y + p * VE, pack_piece<T>(x));
+                for (int e = 0; e < VE; ++e) {
+                    f[e] = keep[p * VE + e] ? f[e] * P.factor : 0.f;
+                    if constexpr (RES) f[e] += g[e];
+                }
+                store_piece(y[a] + p * VE, pack_piece<T>(f));
             }
         } else {
-            const T* x = static_cast<const T*>(P.x) + row[a] * P.ld_x + at[a];
-            const T* z = static_cast<const T*>(P.residual) + row[a] * P.ld_residual + at[a];
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (at[a] + e >= 0 && at[a] + e < P.width) y[e] = from_f32<T>(kept(e, to_f32(x[e])) + (P.residual ? to_f32(z[e]) : 0.f));
+                if (e >= first[a] && e < last[a]) y[a][e] = from_f32<T>((keep[e] ? to_f32(x[a][e]) * P.factor : 0.f) + (RES ? to_f32(z[a][e]) : 0.f));
         }
     }
 }

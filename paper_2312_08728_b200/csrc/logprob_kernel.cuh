@@ -7,11 +7,13 @@
 //     alternatives: the K largest logits in falling order, equal ones by rising class
 //
 // One pass over the row keeps a running maximum with both sums in every thread; t needs no second pass because both sums are
-// carried to a larger maximum together: s' = s f, t' = (t + s (M - M')) f with f = e^(M - M').
+// carried to a larger maximum together: s' = s f, t' = (t + s (M - M')) f with f = e^(M - M').  The sums are taken in powers of two,
+// 2^(z L - m) with L = log2 e in fp32 and m = M L rounded: one multiply-add a logit.  What m is rounded by is the same in every
+// term; it is put right once, in log s (Score).
 //
 // Alternatives.  Each thread's maximum is known after that pass.  The maxima of 32 parts of the row (the threads of equal lane) bound the K-th
-// largest logit from below: at least K of the parts hold a logit at or above the K-th largest of them.  Only threads whose own
-// maximum reaches that bound look at their logits again (a few dozen of a row of independent logits, from L2), what reaches the
+// largest logit from below: at least K of the parts hold a logit at or above the K-th largest of them.  Only the logits of threads whose own
+// maximum reaches that bound are looked at again (a few dozen threads of a row of independent logits, from L2), what reaches the
 // bound is put aside, and its K largest are ranked by counting.  Rows with more candidates than there is room (thousands of equal logits, a mask that
 // leaves fewer than K) are taken value by value: largest below the last one, with all that equal it.
 //
@@ -29,7 +31,7 @@
 namespace bmgdk {
 
 constexpr int kMostAlternatives = 32;
-constexpr float kFarBelow = -200.f;  // e^-200 is 0 in fp32: a logit that far below (-Inf too) counts for nothing, and 0 times it is 0
+constexpr float kFarBelow = -200.f;  // e^-200 is 0 in fp32, as kFar2
 
 struct LogProbParams {
     const void* z;
@@ -44,40 +46,47 @@ struct LogProbParams {
     int C, top;
 };
 
-// Maximum (NaN wins), sum of exponentials and of exponentials times their distance from it.
+// Maximum M (NaN wins), its stand-in m = M L, and sums of 2^(z L - m) and (z L - m) 2^(z L - m).  |M| is at most kWide where the sums
+// are used (a row beyond is done anew by score_careful); m is held within it, which leaves the sums of what is smaller zero.
 struct Score {
     float m, s, t;
 };
-__device__ __forceinline__ float score_base(float m) { return m == -INFINITY ? 0.f : m; }
+constexpr float kWide = 8.507059e37f;   // 2^126: z L stays finite
+constexpr float kFar2 = -300.f;         // 2^-300 is 0 in fp32: a logit that far below (-Inf too) counts for nothing, and 0 times it is 0
 __device__ __forceinline__ float score_max(float a, float b) {
     float m;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
     return m;
 }
+__device__ __forceinline__ float score_base(float m) { return fminf(fmaxf(m, -kWide), kWide) * kLog2e; }
+__device__ __forceinline__ float power_of_two(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ void score_raise(Score& a, float m) {  // to a maximum not below its own
-    const float d = fmaxf(a.m - score_base(m), kFarBelow), f = exp_fast(d);  // (a.m = -Inf: both sums are 0)
-    a.t = (a.t + a.s * d) * f;
+    const float d = fmaxf(score_base(a.m) - score_base(m), kFar2), f = power_of_two(d);  // (a.m = -Inf: both sums are 0)
+    a.t = fmaf(a.s, d, a.t) * f;
     a.s *= f;
     a.m = m;
 }
-__device__ __forceinline__ Score score_join(Score a, Score b) {
-    const float m = score_max(a.m, b.m);
+__device__ __forceinline__ Score score_warp(Score a) {
+    float m;
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(a.m));
     score_raise(a, m);
-    score_raise(b, m);
-    return Score{m, a.s + b.s, a.t + b.t};
-}
-__device__ __forceinline__ Score score_lanes(Score a) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        a = score_join(a, Score{__shfl_xor_sync(0xFFFFFFFFu, a.m, o), __shfl_xor_sync(0xFFFFFFFFu, a.s, o), __shfl_xor_sync(0xFFFFFFFFu, a.t, o)});
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o);
+        a.t += __shfl_xor_sync(0xFFFFFFFFu, a.t, o);
+    }
     return a;
 }
 __device__ __forceinline__ void score_one(Score& a, float x) {
     const float m = score_max(a.m, x);
     if (!(m <= a.m)) score_raise(a, m);
-    const float d = fmaxf(x - score_base(a.m), kFarBelow), p = exp_fast(d);
+    const float d = fmaxf(fmaf(x, kLog2e, -score_base(a.m)), kFar2), p = power_of_two(d);
     a.s += p;
-    a.t += d * p;
+    a.t = fmaf(d, p, a.t);
 }
 template <typename T>
 __device__ __forceinline__ float score_piece_max(const uint4& w) {
@@ -95,26 +104,34 @@ __device__ __forceinline__ float score_piece_max(const uint4& w) {
         return score_max(m.x, m.y);
     }
 }
-// adds a piece to sums relative to the present maximum
+// adds a piece to sums against the base of the present maximum
 template <typename T>
-__device__ __forceinline__ void score_piece(const uint4& w, const Pair& minus_m, Pair& s, Pair& t) {
+__device__ __forceinline__ void score_piece(const uint4& w, float base, float& s, float& t) {
     constexpr int VE = Piece<T>::kValues;
-    const Pair log2e(kLog2e);
     float x[VE];
     unpack_piece<T>(w, x);
 #pragma unroll
-    for (int e = 0; e < VE; e += 2) {
-        float2 d = (Pair(x[e], x[e + 1]) + minus_m).both();
-        d.x = fmaxf(d.x, kFarBelow);
-        d.y = fmaxf(d.y, kFarBelow);
-        const Pair dd(d.x, d.y);
-        float2 p = (dd * log2e).both();
-        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p.x));
-        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p.y));
-        const Pair pp(p.x, p.y);
-        s = s + pp;
-        t = multiply_add(dd, pp, t);
+    for (int e = 0; e < VE; ++e) {
+        const float d = fmaxf(fmaf(x[e], kLog2e, -base), kFar2), p = power_of_two(d);
+        s += p;
+        t = fmaf(d, p, t);
     }
+}
+// What a row's sums say.
+struct RowScore {
+    float m, log_s, entropy;  // log p = (z - m) - log_s
+    bool nothing, broken;     // no distribution; NaN or +Inf
+};
+__device__ __forceinline__ RowScore row_score(const Score& a) {
+    RowScore r;
+    r.m = a.m;
+    r.nothing = a.m == -INFINITY;
+    r.broken = !(a.m < INFINITY);
+    const float nan = __uint_as_float(0x7FC00000u), ln2 = 0.69314718056f;
+    const float log_s = logf(a.s);
+    r.entropy = r.broken ? nan : r.nothing ? 0.f : log_s - ln2 * (a.t / a.s);
+    r.log_s = r.broken ? nan : r.nothing ? 0.f : log_s - ln2 * fmaf(a.m, kLog2e, -score_base(a.m));
+    return r;
 }
 
 // ---- order of the alternatives: 32 bits that rise with the value (-0 as 0, NaN above all), and back
@@ -133,6 +150,7 @@ __device__ __forceinline__ unsigned long long candidate(uint32_t rank, int c) { 
 template <int TH, int ROOM>
 struct LogProbShared {
     Score part[TH / 32];
+    RowScore row;
     float lanes[TH / 32][32];
     int owners[TH];
     unsigned long long found[ROOM];
@@ -209,146 +227,230 @@ __device__ __noinline__ void take_by_value(const T* z, int C, int top, LogProbSh
     row_sync<TH>();
 }
 
-// TH threads to a row (TH = 32: a warp, eight rows to a block).
+// A row whose maximum is beyond +-2^126 (all logits at a type's lowest value, say), against differences that are taken first: all
+// threads of the row call it, with its maximum; each returns the whole row's sums, as row_score gives them.
+template <typename T, int TH, int ROOM>
+__device__ __noinline__ RowScore score_careful(const T* z, int C, float m, LogProbShared<TH, ROOM>& S) {
+    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    float s = 0.f, t = 0.f;
+    for (int c = tid; c < C; c += TH) {
+        const float d = fmaxf(to_f32(z[c]) - m, kFarBelow), p = exp_fast(d);
+        s += p;
+        t = fmaf(d, p, t);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+    }
+    if constexpr (TH > 32) {
+        __syncthreads();  // (the sums before these have been read)
+        if (lane == 0) S.part[warp] = Score{m, s, t};
+        __syncthreads();
+        s = t = 0.f;
+        for (int k = 0; k < TH / 32; ++k) {
+            s += S.part[k].s;
+            t += S.part[k].t;
+        }
+    }
+    const float log_s = logf(s);
+    return RowScore{m, log_s, log_s - t / s, false, false};
+}
+
+// TH threads to a row (TH = 32: a warp, eight rows to a block), rows taken with the grid's stride: the first pieces of the next row are
+// fetched before this one's sums are joined.
 template <typename T, int TH, bool TOP>
 __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 ? 2 : 1024 / TH) logprob_kernel(const __grid_constant__ LogProbParams P) {
     constexpr int VE = Piece<T>::kValues, kAhead = 4, kWarps = TH / 32;
-    constexpr int kRoom = TH == 32 ? 96 : 512;
-    __shared__ LogProbShared<TH, TOP ? kRoom : 1> shared[TH == 32 ? 8 : 1];
-    auto& S = shared[TH == 32 ? threadIdx.x >> 5 : 0];
+    constexpr int kRoom = TH == 32 ? 160 : 512;
+    // (two sets that take turns: a thread that begins a row may meet others that still read what they share of the row before)
+    __shared__ LogProbShared<TH, TOP ? kRoom : 1> shared[TH == 32 ? 8 : 1][2];
     const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (i >= P.rows) return;  // (a whole warp; otherwise the grid has exactly the rows)
-    const T* z = static_cast<const T*>(P.z) + i * P.ld;
-    const RowPieces<T> row(z, P.C);
-    const uint4* src = reinterpret_cast<const uint4*>(z + row.head);
-    const int pieces = row.pieces;
-    const int label = P.y ? P.y[i] : -1;
-    float at_label = 0.f;
-    if (label >= 0 && label < P.C) at_label = to_f32(z[label]);
-
-    // ---- one pass: the sums of each thread, and its maximum
-    Score a{-INFINITY, 0.f, 0.f};
-    uint4 w[kAhead], next[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-        if (tid + k * TH < pieces) next[k] = src[tid + k * TH];
-    if (tid < row.edges) score_one(a, to_f32(z[row.edge(tid)]));
-    for (int k0 = tid; k0 < pieces; k0 += kAhead * TH) {
-        float m = a.m;
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            w[k] = next[k];
-            if (k0 + (kAhead + k) * TH < pieces) next[k] = src[k0 + (kAhead + k) * TH];
-        }
+    const long long step = TH == 32 ? gridDim.x * 8ll : (long long)gridDim.x;
+    uint4 next[kAhead];
+    float edge = -INFINITY;
+    auto begin = [&](long long i) {  // the first pieces of a row
+        const T* z = static_cast<const T*>(P.z) + i * P.ld;
+        const RowPieces<T> row(z, P.C);
+        const uint4* src = reinterpret_cast<const uint4*>(z + row.head);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (k0 + k * TH < pieces) m = score_max(m, score_piece_max<T>(w[k]));
-        if (!(m <= a.m)) score_raise(a, m);
-        const float base = score_base(a.m);
-        Pair s(a.s, 0.f), t(a.t, 0.f);
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (k0 + k * TH < pieces) score_piece<T>(w[k], Pair(-base), s, t);
-        const float2 s2 = s.both(), t2 = t.both();
-        a.s = s2.x + s2.y;
-        a.t = t2.x + t2.y;
-    }
-    const float own = a.m;  // this thread's maximum
-    if constexpr (TOP && TH > 32) S.lanes[warp][lane] = own;
-    a = score_lanes(a);
-    if constexpr (TH > 32) {
-        if (lane == 0) S.part[warp] = a;
-    }
-    if constexpr (TOP) {
-        if (tid == 0) S.owner_count = S.found_count = 0;
-    }
-    row_sync<TH>();
-    if constexpr (TH > 32) {
-        a = S.part[0];
-#pragma unroll
-        for (int k = 1; k < kWarps; ++k) a = score_join(a, S.part[k]);
-    }
-    const bool nothing = a.m == -INFINITY, broken = !(a.m < INFINITY);  // (no distribution; NaN or +Inf)
-    const float nan = __uint_as_float(0x7FC00000u);
-    const float log_s = broken ? nan : nothing ? 0.f : logf(a.s);
-    if (tid == 0) {
-        const float entropy = broken ? nan : nothing ? 0.f : log_s - a.t / a.s;
-        if (P.logprob) P.logprob[i] = label < 0 || label >= P.C || nothing ? 0.f : (at_label - a.m) - log_s;
-        if (P.entropy) P.entropy[i] = entropy;
-        if (P.saved) {
-            P.saved[3 * i] = a.m;
-            P.saved[3 * i + 1] = log_s;
-            P.saved[3 * i + 2] = entropy;
-        }
-    }
-    if constexpr (!TOP) return;
-
-    // ---- the alternatives
-    const int top = P.top;
-    uint32_t bound = 0;
-    if (TH == 32 || warp == 0) {
-        uint32_t g = rank_bits(own);
-        if constexpr (TH > 32) {
-            g = 0;
-#pragma unroll
-            for (int k = 0; k < kWarps; ++k) g = max(g, rank_bits(S.lanes[k][lane]));
-        }
-        int rank = 0;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const uint32_t o = __shfl_sync(0xFFFFFFFFu, g, j);
-            rank += o > g || (o == g && j < lane) ? 1 : 0;
-        }
-        bound = __shfl_sync(0xFFFFFFFFu, g, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1);
-        if (TH > 32 && lane == 0) S.bound = bound;
-    }
-    if constexpr (TH > 32) {
-        __syncthreads();
-        bound = S.bound;
-    }
-    if (rank_bits(own) >= bound) S.owners[atomicAdd(&S.owner_count, 1)] = tid;
-    row_sync<TH>();
-    // (a warp takes an owner at a time, each lane some of its pieces; lane 0 its edge, if it has one)
-    auto consider = [&](float x, int c) {
-        const uint32_t r = rank_bits(x);
-        if (r >= bound) {
-            const int n = atomicAdd(&S.found_count, 1);
-            if (n < kRoom) S.found[n] = candidate(r, c);
-        }
+            if (tid + k * TH < row.pieces) next[k] = src[tid + k * TH];
+        if (tid < row.edges) edge = to_f32(z[row.edge(tid)]);
     };
-    const int owners = S.owner_count;
-    for (int k = warp; k < owners; k += kWarps) {
-        const int u = S.owners[k];
-        if (lane == 0 && u < row.edges) consider(to_f32(z[row.edge(u)]), row.edge(u));
-        for (int p = u + lane * TH; p < pieces; p += 32 * TH) {
-            const uint4 v = src[p];
-            if (rank_bits(score_piece_max<T>(v)) < bound) continue;
-            float x[VE];
-            unpack_piece<T>(v, x);
+    long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i < P.rows) begin(i);
+    for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
+        auto& S = shared[TH == 32 ? threadIdx.x >> 5 : 0][turn];
+        const T* z = static_cast<const T*>(P.z) + i * P.ld;
+        const RowPieces<T> row(z, P.C);
+        const uint4* src = reinterpret_cast<const uint4*>(z + row.head);
+        const int pieces = row.pieces;
+        const int label = P.y ? __ldg(P.y + i) : -1;
+        float at_label = 0.f;
+        if (tid == 0 && label >= 0 && label < P.C) at_label = to_f32(z[label]);
+
+        // ---- one pass: the sums of each thread, and its maximum
+        Score a{-INFINITY, 0.f, 0.f};
+        const bool odd = tid < row.edges;
+        const float edge_value = edge;
+        if (odd) score_one(a, edge_value);
+        uint4 w[kAhead];
+        int k0 = tid;
+        const int rounds = pieces / (kAhead * TH);  // in which every thread has kAhead pieces
+        for (int round = 0; round < rounds; ++round, k0 += kAhead * TH) {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) consider(x[e], row.column(p) + e);
+            for (int k = 0; k < kAhead; ++k) {
+                w[k] = next[k];
+                if (k0 + (kAhead + k) * TH < pieces) next[k] = src[k0 + (kAhead + k) * TH];
+            }
+            const float m = score_max(a.m, score_max(score_max(score_piece_max<T>(w[0]), score_piece_max<T>(w[1])),
+                                                     score_max(score_piece_max<T>(w[2]), score_piece_max<T>(w[3]))));
+            if (!(m <= a.m)) score_raise(a, m);
+            const float base = score_base(a.m);
+            float s2 = 0.f, t2 = 0.f;  // (two sums each: the additions follow one another)
+#pragma unroll
+            for (int k = 0; k < kAhead; k += 2) {
+                score_piece<T>(w[k], base, a.s, a.t);
+                score_piece<T>(w[k + 1], base, s2, t2);
+            }
+            a.s += s2;
+            a.t += t2;
         }
-    }
-    row_sync<TH>();
-    int found = S.found_count;
-    if (found > kRoom) {
+        {  // what is left of the row: up to kAhead pieces a thread
+            float m = a.m;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                w[k] = next[k];
+                if (k0 + k * TH < pieces) m = score_max(m, score_piece_max<T>(w[k]));
+            }
+            if (!(m <= a.m)) score_raise(a, m);
+            const float base = score_base(a.m);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (k0 + k * TH < pieces) score_piece<T>(w[k], base, a.s, a.t);
+        }
+        if (i + step < P.rows) begin(i + step);
+        const float own = a.m;  // this thread's maximum
+        if constexpr (TOP && TH > 32) S.lanes[warp][lane] = own;
+        a = score_warp(a);
+        if constexpr (TH > 32) {
+            if (lane == 0) S.part[warp] = a;
+        }
+        if constexpr (TOP) {
+            if (tid == 0) S.owner_count = S.found_count = 0;
+        }
         row_sync<TH>();
-        take_by_value<T>(z, P.C, top, S);
-        found = top;
-    }
-    for (int k = tid; k < found; k += TH) {
-        const unsigned long long mine = S.found[k];
-        int rank = 0;
-        for (int j = 0; j < found; ++j) rank += S.found[j] > mine ? 1 : 0;
-        if (rank >= top) continue;
-        const float x = rank_value((uint32_t)(mine >> 32));
-        P.index[i * top + rank] = (int)(0xFFFFFFFFu - (uint32_t)mine);
-        P.value[i * top + rank] = broken ? nan : nothing ? -INFINITY : (x - a.m) - log_s;
+        // the row's sums and, for the alternatives, the bound: by one warp
+        RowScore r{};
+        uint32_t g = 0;
+        if (TH == 32 || warp == 0) {
+            if constexpr (TH > 32) a = score_warp(lane < kWarps ? S.part[lane] : Score{-INFINITY, 0.f, 0.f});
+            r = row_score(a);
+        }
+        if constexpr (TH > 32) {
+            if (warp == 0 && lane == 0) S.row = r;
+        }
+        if constexpr (TOP) {
+            if (TH == 32 || warp == 0) {
+                g = rank_bits(own);
+                if constexpr (TH > 32) {
+                    float m = S.lanes[0][lane];
+#pragma unroll
+                    for (int k = 1; k < kWarps; ++k) m = score_max(m, S.lanes[k][lane]);
+                    g = rank_bits(m);
+                }
+                int rank = 0;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const uint32_t o = __shfl_sync(0xFFFFFFFFu, g, j);
+                    rank += o > g || (o == g && j < lane) ? 1 : 0;
+                }
+                g = __shfl_sync(0xFFFFFFFFu, g, __ffs(__ballot_sync(0xFFFFFFFFu, rank == P.top - 1)) - 1);
+                if (TH > 32 && lane == 0) S.bound = g;
+            }
+        }
+        bool wide = TH == 32 && fabsf(r.m) > kWide && fabsf(r.m) < INFINITY;
+        if constexpr (TH > 32 && TOP) {
+            __syncthreads();
+            r = S.row;
+            g = S.bound;
+            wide = fabsf(r.m) > kWide && fabsf(r.m) < INFINITY;
+        }
+        if constexpr (TH > 32 && !TOP) {  // (no other barrier is needed: whether the row is one of the rare ones, each thread sees for itself)
+            float m = S.part[0].m;
+#pragma unroll
+            for (int k = 1; k < kWarps; ++k) m = score_max(m, S.part[k].m);
+            wide = fabsf(m) > kWide && fabsf(m) < INFINITY;
+            if (wide) r.m = m;
+        }
+        if (wide) r = score_careful<T>(z, P.C, r.m, S);
+        const float nan = __uint_as_float(0x7FC00000u);
+        if (tid == 0) {
+            if (P.logprob) P.logprob[i] = label < 0 || label >= P.C || r.nothing ? 0.f : (at_label - r.m) - r.log_s;
+            if (P.entropy) P.entropy[i] = r.entropy;
+            if (P.saved) {
+                P.saved[3 * i] = r.m;
+                P.saved[3 * i + 1] = r.log_s;
+                P.saved[3 * i + 2] = r.entropy;
+            }
+        }
+        if constexpr (TOP) {
+            // ---- the alternatives
+            const int top = P.top;
+            const float bound = rank_value(g);
+            auto consider = [&](float x, int c) {
+                if (x < bound) return;  // (NaN is no less)
+                const int n = atomicAdd(&S.found_count, 1);
+                if (n < kRoom) S.found[n] = candidate(rank_bits(x), c);
+            };
+            auto consider_piece = [&](const uint4& v, int p) {
+                if (score_piece_max<T>(v) < bound) return;
+                float x[VE];
+                unpack_piece<T>(v, x);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) consider(x[e], row.column(p) + e);
+            };
+            if (odd) consider(edge_value, row.edge(tid));
+            if (rounds == 0) {  // the whole row is still in registers
+                if (!(own < bound)) {
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k)
+                        if (tid + k * TH < pieces) consider_piece(w[k], tid + k * TH);
+                }
+            } else {  // all threads look at the pieces of those whose maximum reaches the bound
+                if (!(own < bound)) S.owners[atomicAdd(&S.owner_count, 1)] = tid;
+                row_sync<TH>();
+                const unsigned per = (unsigned)(pieces + TH - 1) / TH, items = (unsigned)S.owner_count * per;
+#pragma unroll 2
+                for (unsigned k = tid; k < items; k += TH) {
+                    const unsigned o = k / per;
+                    const int p = S.owners[o] + (int)(k - o * per) * TH;
+                    if (p < pieces) consider_piece(src[p], p);
+                }
+            }
+            row_sync<TH>();
+            int found = S.found_count;
+            if (found > kRoom) {
+                row_sync<TH>();
+                take_by_value<T>(z, P.C, top, S);
+                found = top;
+            }
+            for (int k = tid; k < found; k += TH) {
+                const unsigned long long mine = S.found[k];
+                int rank = 0;
+#pragma unroll 4
+                for (int j = 0; j < found; ++j) rank += S.found[j] > mine ? 1 : 0;
+                if (rank >= top) continue;
+                const float x = rank_value((uint32_t)(mine >> 32));
+                P.index[i * top + rank] = (int)(0xFFFFFFFFu - (uint32_t)mine);
+                P.value[i * top + rank] = r.broken ? nan : r.nothing ? -INFINITY : (x - r.m) - r.log_s;
+            }
+        }
     }
 }
 
-// ---- gradient: each logit read once, its gradient written once
+// ---- gradient: each logit read once, its gradient written once.  gridDim.y blocks share a row.
 template <typename T, int TH>
 __global__ void __launch_bounds__(TH == 32 ? 256 : TH) logprob_back_kernel(const __grid_constant__ LogProbParams P) {
     constexpr int VE = Piece<T>::kValues, kAhead = 2;
@@ -369,9 +471,9 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) logprob_back_kernel(const
         const float lp = fmaxf((x - base) - (nothing ? 0.f : log_s), kFarBelow), v = exp_fast(lp) * (k0 + k1 * lp);
         return c == label ? v + a : v;
     };
-    if (tid < row.edges) dz[row.edge(tid)] = from_f32<T>(one(to_f32(z[row.edge(tid)]), row.edge(tid)));
+    if (blockIdx.y == 0 && tid < row.edges) dz[row.edge(tid)] = from_f32<T>(one(to_f32(z[row.edge(tid)]), row.edge(tid)));
     const Pair minus_m(-base), minus_s(nothing ? 0.f : -log_s), log2e(kLog2e), p0(k0), p1(k1);
-    for (int q0 = tid; q0 < row.pieces; q0 += kAhead * TH) {
+    for (int q0 = (int)blockIdx.y * kAhead * TH + tid; q0 < row.pieces; q0 += (int)gridDim.y * kAhead * TH) {
         uint4 w[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)

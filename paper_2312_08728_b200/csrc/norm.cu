@@ -13,60 +13,93 @@ using namespace bmgdk;
 int launched() { return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA; }
 int value_bytes(int type) { return type == BMGD_TYPE_F32 ? 4 : 2; }
 bool off(const void* p, int bytes) { return (uintptr_t)p % (unsigned)bytes != 0; }
+// whether rows of that stride in bytes all start on 16-byte boundaries
+bool on16(const void* p, int64_t stride) { return ((uintptr_t)p | (uintptr_t)stride) % 16 == 0; }
 // whether [rows][width] of stride ld at p and the same of stride lq at q share memory
 bool overlap(const void* p, int64_t ld, int64_t pw, const void* q, int64_t lq, int64_t qw, int64_t rows) {
     const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
     return a < b + (uintptr_t)((rows - 1) * lq + qw) && b < a + (uintptr_t)((rows - 1) * ld + pw);
 }
 
-// By the row's length in pieces of 16 bytes: a warp to a row up to 128, then blocks of 128 to 1024 threads with four pieces each, then the
-// form that reads rows more than once.
+// Threads of a row of `count` pieces: a warp up to 64 (two each), then two pieces a thread up to 1024, four beyond.
+struct Threads {
+    int pieces, threads;  // of a thread; 32: a warp, eight rows to a block
+};
+Threads threads_for(int64_t count) {
+    if (count <= 32) return {1, 32};
+    if (count <= 64) return {2, 32};
+    const int nv = count <= 1024 ? 2 : 4;
+    return {nv, (int)((count + nv * 32 - 1) / (nv * 32)) * 32};
+}
+// Blocks that go through the rows: as many as the registers of an SM hold (64 a thread, with four pieces 128)
+unsigned flow_grid(const Threads& t, int64_t rows, int per_sm_threads) {
+    if (t.threads == 32) return (unsigned)std::min<int64_t>((rows + 7) / 8, 148 * (per_sm_threads / 256));
+    return (unsigned)std::min<int64_t>(rows, 148 * std::max(1, per_sm_threads / t.threads));
+}
+
+template <typename T, bool RES, bool CODES>
+int forward_flow(const NormParams& P, cudaStream_t s) {
+    const Threads t = threads_for(P.width / Piece<T>::kValues);
+    const unsigned grid = flow_grid(t, P.rows, t.pieces == 4 ? 512 : 1024);
+    if (t.threads == 32 && t.pieces == 1) norm_flow_kernel<T, 1, true, RES, CODES><<<grid, 256, 0, s>>>(P);
+    else if (t.threads == 32) norm_flow_kernel<T, 2, true, RES, CODES><<<grid, 256, 0, s>>>(P);
+    else if (t.pieces == 2) norm_flow_kernel<T, 2, false, RES, CODES><<<grid, t.threads, 0, s>>>(P);
+    else norm_flow_kernel<T, 4, false, RES, CODES><<<grid, t.threads, 0, s>>>(P);
+    return launched();
+}
+// Rows on 16-byte boundaries of up to 2048 pieces; rows on others, held in registers too: a warp to a row up to 128 pieces, then blocks of 256 and
+// 1024 threads; longer rows are read more than once.
 template <typename T, bool CODES>
-int forward(const NormParams& P, cudaStream_t s) {
+int forward(const NormParams& P, bool aligned, cudaStream_t s) {
     const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
-    const unsigned rows = (unsigned)P.rows, eights = (unsigned)((P.rows + 7) / 8);
-    if (pieces <= 32) norm_row_kernel<T, 32, 1, CODES><<<eights, 256, 0, s>>>(P);
-    else if (pieces <= 128) norm_row_kernel<T, 32, 4, CODES><<<eights, 256, 0, s>>>(P);
-    else if (pieces <= 256) norm_row_kernel<T, 128, 2, CODES><<<rows, 128, 0, s>>>(P);
+    const unsigned rows = (unsigned)P.rows;
+    if (aligned && pieces <= 2048) return P.residual ? forward_flow<T, true, CODES>(P, s) : forward_flow<T, false, CODES>(P, s);
+    if (pieces <= 128) norm_row_kernel<T, 32, 4, CODES><<<(rows + 7) / 8, 256, 0, s>>>(P);
     else if (pieces <= 512) norm_row_kernel<T, 128, 4, CODES><<<rows, 128, 0, s>>>(P);
     else if (pieces <= 1024) norm_row_kernel<T, 256, 4, CODES><<<rows, 256, 0, s>>>(P);
-    else if (pieces <= 2048) norm_row_kernel<T, 512, 4, CODES><<<rows, 512, 0, s>>>(P);
     else if (pieces <= 4096) norm_row_kernel<T, 1024, 4, CODES><<<rows, 1024, 0, s>>>(P);
     else norm_long_kernel<T, CODES><<<rows, 1024, 0, s>>>(P);
     return launched();
 }
 
-// Blocks of the backward pass, and how they divide a row: pieces of 16 bytes where every row of every tensor starts on such a boundary,
-// else single values.
+// How the backward pass divides a row: pieces of 16 bytes where every row of every tensor starts on such a boundary, else single values.
 struct BackShape {
-    int values, threads, blocks;  // threads 0: the form for long rows
+    int values;           // of a thread's piece
+    Threads of;           // threads 0: the form for long rows
+    int blocks;
 };
-BackShape back_shape(const bmgd_rms_norm* a, int sms) {
+BackShape back_shape(const bmgd_rms_norm* a) {
     const int ve = 16 / value_bytes(a->type);
     const uintptr_t low = (uintptr_t)a->total | (uintptr_t)a->dy | (uintptr_t)a->dtotal | (uintptr_t)a->dx |
                           (uintptr_t)((a->ld_total | a->ld_dy | (a->dtotal ? a->ld_dtotal : 0) | a->ld_dx) * value_bytes(a->type));
     BackShape b{};
     b.values = low % 16 == 0 && a->width % ve == 0 ? ve : 1;
     const int count = a->width / b.values;
-    if (count <= 128) b.threads = 32;
-    else if (count <= 512) b.threads = 128;
-    else if (count <= 1024) b.threads = 256;
-    else if (count <= 2048) b.threads = 512;
-    else if (count <= 4096) b.threads = 1024;
-    const int per = b.threads == 32 ? 2 : b.threads == 0 ? 1 : std::max(1, 512 / b.threads);
-    b.blocks = (int)std::min<int64_t>(b.threads == 32 ? (a->rows + 7) / 8 : a->rows, (int64_t)sms * per);
+    b.of = threads_for(count);
+    if (count > (b.values == 1 ? 4096 : 2048)) b.of.threads = 0;
+    b.blocks = b.of.threads == 0 ? (int)std::min<int64_t>(a->rows, 148) : (int)flow_grid(b.of, a->rows, 512);
     return b;
 }
+constexpr int kMostSums = 50 * 1024;  // columns whose sums fit shared memory
 template <typename T, int VE>
 int backward(const NormParams& P, const BackShape& b, cudaStream_t s) {
     const unsigned grid = (unsigned)b.blocks;
-    if (b.threads == 0) norm_back_long_kernel<T><<<grid, 1024, 0, s>>>(P);
-    else if (b.threads == 32 && P.width <= 32 * VE) norm_back_kernel<T, VE, 32, 1><<<grid, 256, 0, s>>>(P);
-    else if (b.threads == 32) norm_back_kernel<T, VE, 32, 4><<<grid, 256, 0, s>>>(P);
-    else if (b.threads == 128) norm_back_kernel<T, VE, 128, 4><<<grid, 128, 0, s>>>(P);
-    else if (b.threads == 256) norm_back_kernel<T, VE, 256, 4><<<grid, 256, 0, s>>>(P);
-    else if (b.threads == 512) norm_back_kernel<T, VE, 512, 4><<<grid, 512, 0, s>>>(P);
-    else norm_back_kernel<T, VE, 1024, 4><<<grid, 1024, 0, s>>>(P);
+    if (b.of.threads == 0) {
+        const int bytes = P.width * 4;
+        if (!P.part || P.width > kMostSums) {
+            norm_back_long_kernel<T, VE, false><<<grid, 1024, 0, s>>>(P);
+            return launched();
+        }
+        Device dev{};
+        int rc = current_device(&dev);
+        static std::atomic<unsigned long long> allowed{0};
+        if (rc == BMGD_OK) rc = allow_smem(norm_back_long_kernel<T, VE, true>, kMostSums * 4, dev, allowed);
+        if (rc != BMGD_OK) return rc;
+        norm_back_long_kernel<T, VE, true><<<grid, 1024, (size_t)bytes, s>>>(P);
+    } else if (b.of.threads == 32 && b.of.pieces == 1) norm_back_kernel<T, VE, 1, true><<<grid, 256, 0, s>>>(P);
+    else if (b.of.threads == 32) norm_back_kernel<T, VE, 2, true><<<grid, 256, 0, s>>>(P);
+    else if (b.of.pieces == 2) norm_back_kernel<T, VE, 2, false><<<grid, b.of.threads, 0, s>>>(P);
+    else norm_back_kernel<T, VE, 4, false><<<grid, b.of.threads, 0, s>>>(P);
     return launched();
 }
 template <typename T>
@@ -111,16 +144,24 @@ int check_backward(const bmgd_rms_norm* a) {
     return BMGD_OK;
 }
 
+template <typename T, bool GATE>
+int codes_flow(const CodesParams& P, cudaStream_t s) {
+    const Threads t = threads_for(P.width / Piece<T>::kValues);
+    const unsigned grid = flow_grid(t, P.rows, t.pieces == 4 ? 704 : 1024);
+    if (t.threads == 32 && t.pieces == 1) codes_flow_kernel<T, 1, true, GATE><<<grid, 256, 0, s>>>(P);
+    else if (t.threads == 32) codes_flow_kernel<T, 2, true, GATE><<<grid, 256, 0, s>>>(P);
+    else if (t.pieces == 2) codes_flow_kernel<T, 2, false, GATE><<<grid, t.threads, 0, s>>>(P);
+    else codes_flow_kernel<T, 4, false, GATE><<<grid, t.threads, 0, s>>>(P);
+    return launched();
+}
 template <typename T>
-int codes(const CodesParams& P, cudaStream_t s) {
+int codes(const CodesParams& P, bool aligned, cudaStream_t s) {
     const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
-    const unsigned rows = (unsigned)P.rows, eights = (unsigned)((P.rows + 7) / 8);
-    if (pieces <= 32) codes_row_kernel<T, 32, 1><<<eights, 256, 0, s>>>(P);
-    else if (pieces <= 128) codes_row_kernel<T, 32, 4><<<eights, 256, 0, s>>>(P);
-    else if (pieces <= 256) codes_row_kernel<T, 128, 2><<<rows, 128, 0, s>>>(P);
+    const unsigned rows = (unsigned)P.rows;
+    if (aligned && pieces <= 2048) return P.gate ? codes_flow<T, true>(P, s) : codes_flow<T, false>(P, s);
+    if (pieces <= 128) codes_row_kernel<T, 32, 4><<<(rows + 7) / 8, 256, 0, s>>>(P);
     else if (pieces <= 512) codes_row_kernel<T, 128, 4><<<rows, 128, 0, s>>>(P);
     else if (pieces <= 1024) codes_row_kernel<T, 256, 4><<<rows, 256, 0, s>>>(P);
-    else if (pieces <= 2048) codes_row_kernel<T, 512, 4><<<rows, 512, 0, s>>>(P);
     else if (pieces <= 4096) codes_row_kernel<T, 1024, 4><<<rows, 1024, 0, s>>>(P);
     else codes_long_kernel<T><<<rows, 1024, 0, s>>>(P);
     return launched();
@@ -162,17 +203,18 @@ int bmgd_rms_norm_forward(const bmgd_rms_norm* a, void* stream) {
     P.y = a->y; P.ld_y = a->ld_y;
     P.codes = reinterpret_cast<signed char*>(a->codes); P.ld_codes = a->ld_codes; P.scale = a->scale;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a->type == BMGD_TYPE_F32) return a->y ? forward<float, false>(P, s) : forward<float, true>(P, s);
-    if (a->type == BMGD_TYPE_BF16) return a->y ? forward<__nv_bfloat16, false>(P, s) : forward<__nv_bfloat16, true>(P, s);
-    return a->y ? forward<__half, false>(P, s) : forward<__half, true>(P, s);
+    const bool aligned = w % 16 == 0 && on16(a->x, a->ld_x * eb) && on16(a->residual, a->residual ? a->ld_residual * eb : 0) &&
+                         on16(a->total, a->total ? a->ld_total * eb : 0) && (a->y ? on16(a->y, a->ld_y * eb) : on16(a->codes, a->ld_codes));
+    if (a->type == BMGD_TYPE_F32) return a->y ? forward<float, false>(P, aligned, s) : forward<float, true>(P, aligned, s);
+    if (a->type == BMGD_TYPE_BF16) return a->y ? forward<__nv_bfloat16, false>(P, aligned, s) : forward<__nv_bfloat16, true>(P, aligned, s);
+    return a->y ? forward<__half, false>(P, aligned, s) : forward<__half, true>(P, aligned, s);
 }
 
 int bmgd_rms_norm_workspace_bytes(const bmgd_rms_norm* a, int64_t* bytes) {
     if (!bytes) return BMGD_ERR_ARG;
     const int rc = check(a);
     if (rc != BMGD_OK) return rc;
-    // (for the most blocks that a GPU of this kind is given, so that no device has to be asked)
-    *bytes = a->weight && a->rows > 0 ? up256(back_shape(a, 148).blocks * (int64_t)a->width * 4) : 0;
+    *bytes = a->weight && a->rows > 0 ? up256(back_shape(a).blocks * (int64_t)a->width * 4) : 0;
     return BMGD_OK;
 }
 
@@ -189,7 +231,7 @@ int bmgd_rms_norm_backward(const bmgd_rms_norm* a, void* workspace, int64_t work
     if (rc != BMGD_OK) return rc;
     if (need > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)) return BMGD_ERR_ARG;
     if (workspace_bytes < need) return BMGD_ERR_CAPACITY;
-    const BackShape b = back_shape(a, 148);
+    const BackShape b = back_shape(a);
     NormParams P = shared_params(a);
     P.x = a->total; P.ld_x = a->ld_total;
     P.dy = a->dy; P.ld_dy = a->ld_dy;
@@ -215,9 +257,10 @@ int bmgd_quantize_rows(const void* dev_x, int64_t ld_x, const void* dev_gate, in
         (dev_gate && overlap(dev_codes, ld_codes, width, dev_gate, ld_gate * eb, w, rows))) return BMGD_ERR_ARG;
     CodesParams P{dev_x, dev_gate, reinterpret_cast<signed char*>(dev_codes), dev_scale, ld_x, ld_gate, ld_codes, rows, width, activation};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (type == BMGD_TYPE_F32) return codes<float>(P, s);
-    if (type == BMGD_TYPE_BF16) return codes<__nv_bfloat16>(P, s);
-    return codes<__half>(P, s);
+    const bool aligned = w % 16 == 0 && on16(dev_x, ld_x * eb) && on16(dev_gate, dev_gate ? ld_gate * eb : 0) && on16(dev_codes, ld_codes);
+    if (type == BMGD_TYPE_F32) return codes<float>(P, aligned, s);
+    if (type == BMGD_TYPE_BF16) return codes<__nv_bfloat16>(P, aligned, s);
+    return codes<__half>(P, aligned, s);
 }
 
 int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_t outputs, int32_t type, int8_t* dev_codes,

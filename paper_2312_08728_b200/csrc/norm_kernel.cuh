@@ -36,6 +36,14 @@ struct NormParams {
     float eps;
 };
 
+// Sums of squares.  fp32 rows: in 64 bits, since their results are held to fp32 themselves (codes next to a border follow every bit).
+template <typename T> struct SquareSum { typedef float type; };
+template <> struct SquareSum<float> { typedef double type; };
+__device__ __forceinline__ void add_square(float& sum, float t) { sum = fmaf(t, t, sum); }
+__device__ __forceinline__ void add_square(double& sum, float t) { sum = fma((double)t, (double)t, sum); }
+template <typename V>
+__device__ __forceinline__ float root_factor(V sum, const NormParams& P) { return rsqrtf((float)(sum / (V)P.width) + P.eps); }
+
 template <typename T>
 __device__ __forceinline__ void load_weights(const void* weight, int f32, int c, float (&w)[Piece<T>::kValues]) {
     constexpr int VE = Piece<T>::kValues;
@@ -79,22 +87,19 @@ struct RowCodes {
         factor = fine && some ? __fdiv_rn(127.f, top) : 0.f;
         scale = !fine ? __uint_as_float(0x7FC00000u) : some ? __fdiv_rn(top, 127.f) : 0.f;
     }
-    // (factor 0: also 0 times NaN or Inf is 0)
-    __device__ __forceinline__ int code(float y) const { return factor == 0.f ? 0 : __float2int_rn(y * factor); }
+    // The code stands in the low byte: next to 1.5 2^23 the step of fp32 is one, so the sum is the whole number, rounded to nearest
+    // (conversions take the exponentials' unit: 4096 x 11008 values 43 us with them).  |y factor| <= 127 (1 + 2^-23): no code leaves the range.
+    __device__ __forceinline__ uint32_t bits(float y) const { return __float_as_uint(__fadd_rn(__fmul_rn(y, factor), 12582912.f)); }
+    __device__ __forceinline__ signed char code(float y) const { return factor == 0.f ? (signed char)0 : (signed char)bits(y); }
 };
-__device__ __forceinline__ float nan_max(float a, float b) {
-    float m;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-    return m;
-}
-// (|y factor| <= 127 (1 + 2^-23): no code leaves the range)
 template <int VE>
 __device__ __forceinline__ void store_codes(signed char* p, const RowCodes& rc, const float (&y)[VE]) {
     uint32_t w[VE / 4];
 #pragma unroll
-    for (int e = 0; e < VE; e += 4)
-        w[e / 4] = (uint32_t)(rc.code(y[e]) & 255) | (uint32_t)(rc.code(y[e + 1]) & 255) << 8 | (uint32_t)(rc.code(y[e + 2]) & 255) << 16 |
-                   (uint32_t)rc.code(y[e + 3]) << 24;
+    for (int e = 0; e < VE; e += 4) {
+        w[e / 4] = __byte_perm(__byte_perm(rc.bits(y[e]), rc.bits(y[e + 1]), 0x0040), __byte_perm(rc.bits(y[e + 2]), rc.bits(y[e + 3]), 0x0040), 0x5410);
+        if (rc.factor == 0.f) w[e / 4] = 0;  // (also for NaN and Inf)
+    }
     if (((uintptr_t)p & (VE - 1)) == 0) {
         if constexpr (VE == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t*>(p) = w[0];
@@ -104,11 +109,125 @@ __device__ __forceinline__ void store_codes(signed char* p, const RowCodes& rc, 
     }
 }
 
-// ---- forward, rows held in registers: TH threads share a row (TH = 32: a warp, eight rows to a block), NV pieces each
+// A value joined over the threads of a row, in a fixed order: a warp, or a whole block of any number of warps, whose spare cells are zero.
+template <bool WARP, int OP, typename V>
+__device__ __forceinline__ V join_threads(V v, V (&cells)[32]) {
+    auto op = [](V a, V b) { if constexpr (OP == kJoinSum) return a + b; else return nan_max(a, b); };
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    if constexpr (!WARP) {
+        if ((threadIdx.x & 31) == 0) cells[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0;  // (maxima here are of magnitudes)
+        for (int k = 0; k < (int)(blockDim.x >> 5); k += 4) v = op(op(v, cells[k]), op(cells[k + 1], op(cells[k + 2], cells[k + 3])));
+    }
+    return v;
+}
+
+// ---- forward, rows on 16-byte boundaries throughout: every thread has the same columns in every row, so that its weights stay in registers
+// (read anew for each row they took four times the shared-memory cycles of the row itself: 8192 x 4096 31.5 us), and blocks go through the
+// rows with the grid's stride, the next row under way while this one is summed up and written.  WARP: a warp to a row, eight rows to a block; otherwise
+// as many threads as NV pieces each need.
+template <typename T, int NV, bool WARP, bool RES, bool CODES>
+__global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_kernel(const __grid_constant__ NormParams P) {
+    constexpr int VE = Piece<T>::kValues;
+    typedef typename SquareSum<T>::type Sum;
+    __shared__ Sum sums[2][32];
+    __shared__ float tops[2][32];
+    const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
+    const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
+    const int count = P.width / VE;  // (VE divides it)
+    if constexpr (!WARP) {
+        for (int k = threadIdx.x; k < 64; k += blockDim.x) {
+            (&sums[0][0])[k] = 0;
+            (&tops[0][0])[k] = 0.f;
+        }
+        __syncthreads();
+    }
+    float w[NV][VE];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (tid + k * threads < count) load_weights<T>(P.weight, P.weight_f32, (tid + k * threads) * VE, w[k]);
+    uint4 nx[NV], nr[NV];
+    auto fetch = [&](long long i) {
+        const uint4* x = reinterpret_cast<const uint4*>(static_cast<const T*>(P.x) + i * P.ld_x);
+        const uint4* r = reinterpret_cast<const uint4*>(static_cast<const T*>(P.residual) + i * P.ld_residual);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * threads < count) {
+                nx[k] = __ldcs(x + tid + k * threads);
+                if constexpr (RES) nr[k] = __ldcs(r + tid + k * threads);
+            }
+    };
+    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i < P.rows) fetch(i);
+    for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
+        Sum sum = 0;
+        uint4 v[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * threads >= count) continue;
+            float t[VE];
+            v[k] = nx[k];
+            unpack_piece<T>(v[k], t);
+            if constexpr (RES) {
+                float u[VE];
+                unpack_piece<T>(nr[k], u);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) t[e] += u[e];
+                v[k] = pack_piece<T>(t);
+                reinterpret_cast<uint4*>(static_cast<T*>(P.total) + i * P.ld_total)[tid + k * threads] = v[k];
+                unpack_piece<T>(v[k], t);
+            }
+#pragma unroll
+            for (int e = 0; e < VE; ++e) add_square(sum, t[e]);
+        }
+        if (i + step < P.rows) fetch(i + step);
+        const float s = root_factor(join_threads<WARP, kJoinSum>(sum, sums[turn]), P);
+        if (P.rstd && tid == 0) P.rstd[i] = s;
+        if constexpr (!CODES) {
+            uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(P.y) + i * P.ld_y);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (tid + k * threads >= count) continue;
+                float t[VE];
+                unpack_piece<T>(v[k], t);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[k][e];
+                y[tid + k * threads] = pack_piece<T>(t);
+            }
+        } else {
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (tid + k * threads >= count) continue;
+                float t[VE];
+                unpack_piece<T>(v[k], t);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(t[e] * s * w[k][e]));
+            }
+            const RowCodes rc(join_threads<WARP, kJoinMax>(top, tops[turn]));
+            signed char* q = P.codes + i * P.ld_codes;
+            if (tid == 0) P.scale[i] = rc.scale;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (tid + k * threads >= count) continue;
+                float t[VE];
+                unpack_piece<T>(v[k], t);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[k][e];
+                store_codes<VE>(q + (tid + k * threads) * VE, rc, t);
+            }
+        }
+    }
+}
+
+// ---- forward, rows on any boundary, held in registers: TH threads share a row (TH = 32: a warp, eight rows to a block), NV pieces each
 template <typename T, int TH, int NV, bool CODES>
 __global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __grid_constant__ NormParams P) {
     constexpr int VE = Piece<T>::kValues;
-    __shared__ float cells[2][TH / 32];
+    __shared__ typename SquareSum<T>::type sums[TH / 32];
+    __shared__ float tops[TH / 32];
     const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
     const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
     if (i >= P.rows) return;  // (a whole warp; otherwise the grid has exactly the rows)
@@ -117,7 +236,8 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __g
     T* total = static_cast<T*>(P.total) + i * P.ld_total;
     const RowPieces<T> row(x, P.width);
     uint4 w[NV];
-    float t[VE], sum = 0.f, edge = 0.f;
+    typename SquareSum<T>::type sum = 0;
+    float t[VE], edge = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (tid + k * TH < row.pieces) w[k] = load_piece(x + row.column(tid + k * TH));
@@ -151,10 +271,10 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __g
         if (tid + k * TH >= row.pieces) continue;
         unpack_piece<T>(w[k], t);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) sum += t[e] * t[e];
+        for (int e = 0; e < VE; ++e) add_square(sum, t[e]);
     }
-    sum = join_row<TH, kJoinSum>(sum + edge * edge, cells[0]);
-    const float s = rsqrtf(sum / (float)P.width + P.eps);
+    add_square(sum, edge);
+    const float s = root_factor(join_row<TH, kJoinSum>(sum, sums), P);
     if (P.rstd && tid == 0) P.rstd[i] = s;
     if (odd) edge *= s * load_weight<T>(P.weight, P.weight_f32, at);
     if constexpr (!CODES) {
@@ -185,13 +305,13 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __g
                 top = nan_max(top, fabsf(v[k][e]));
             }
         }
-        const RowCodes rc(join_row<TH, kJoinMax>(top, cells[1]));
+        const RowCodes rc(join_row<TH, kJoinMax>(top, tops));
         signed char* q = P.codes + i * P.ld_codes;
         if (tid == 0) P.scale[i] = rc.scale;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (tid + k * TH < row.pieces) store_codes<VE>(q + row.column(tid + k * TH), rc, v[k]);
-        if (odd) q[at] = (signed char)rc.code(edge);
+        if (odd) q[at] = rc.code(edge);
     }
 }
 
@@ -199,7 +319,8 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __g
 template <typename T, bool CODES>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__ NormParams P) {
     constexpr int VE = Piece<T>::kValues, TH = 1024;
-    __shared__ float cells[2][TH / 32];
+    __shared__ typename SquareSum<T>::type sums[TH / 32];
+    __shared__ float tops[TH / 32];
     const int tid = threadIdx.x;
     const long long i = blockIdx.x;
     const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
@@ -209,7 +330,8 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__
     const T* src = r ? total : x;  // where the sum is read from later (each thread reads what it has written)
     const bool odd = tid < row.edges;
     const int at = row.edge(tid);
-    float t[VE], u[VE], sum = 0.f, edge = odd ? to_f32(x[at]) : 0.f;
+    typename SquareSum<T>::type sum = 0;
+    float t[VE], u[VE], edge = odd ? to_f32(x[at]) : 0.f;
     if (odd && r) {
         const T v1 = from_f32<T>(edge + to_f32(r[at]));
         total[at] = v1;
@@ -228,10 +350,10 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__
             unpack_piece<T>(w, t);
         }
 #pragma unroll
-        for (int e = 0; e < VE; ++e) sum += t[e] * t[e];
+        for (int e = 0; e < VE; ++e) add_square(sum, t[e]);
     }
-    sum = join_row<TH, kJoinSum>(sum + edge * edge, cells[0]);
-    const float s = rsqrtf(sum / (float)P.width + P.eps);
+    add_square(sum, edge);
+    const float s = root_factor(join_row<TH, kJoinSum>(sum, sums), P);
     if (P.rstd && tid == 0) P.rstd[i] = s;
     if (odd) edge *= s * load_weight<T>(P.weight, P.weight_f32, at);
     auto normed = [&](int c) {
@@ -254,14 +376,14 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__
 #pragma unroll
             for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(t[e]));
         }
-        const RowCodes rc(join_row<TH, kJoinMax>(top, cells[1]));
+        const RowCodes rc(join_row<TH, kJoinMax>(top, tops));
         signed char* q = P.codes + i * P.ld_codes;
         if (tid == 0) P.scale[i] = rc.scale;
         for (int k = tid; k < row.pieces; k += TH) {
             normed(row.column(k));
             store_codes<VE>(q + row.column(k), rc, t);
         }
-        if (odd) q[at] = (signed char)rc.code(edge);
+        if (odd) q[at] = rc.code(edge);
     }
 }
 
@@ -273,7 +395,8 @@ struct Columns;  // VE neighbouring values as they are held and moved
 template <typename T>
 struct Columns<T, 1> {
     T v;
-    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void load(const T* p) { v = __ldcs(p); }
+    __device__ __forceinline__ void load_again(const T* p) { v = *p; }  // (what will be read again)
     __device__ __forceinline__ void unpack(float (&x)[1]) const { x[0] = to_f32(v); }
     static __device__ __forceinline__ void store(T* p, const float (&x)[1]) { *p = from_f32<T>(x[0]); }
     static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[1]) { x[0] = load_weight<T>(w, f32, c); }
@@ -283,76 +406,98 @@ struct Columns {
     static_assert(VE == Piece<T>::kValues, "a piece, or one value");
     uint4 v;
     __device__ __forceinline__ void load(const T* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void load_again(const T* p) { v = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void unpack(float (&x)[VE]) const { unpack_piece<T>(v, x); }
     static __device__ __forceinline__ void store(T* p, const float (&x)[VE]) { *reinterpret_cast<uint4*>(p) = pack_piece<T>(x); }
     static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[VE]) { load_weights<T>(w, f32, c, x); }
 };
 
-template <typename T, int VE, int TH, int NV>
-__global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 2 : 512 / TH ? 512 / TH : 1) norm_back_kernel(const __grid_constant__ NormParams P) {
-    constexpr int kGroups = TH == 32 ? 8 : 1;
+template <typename T, int VE, int NV, bool WARP>
+__global__ void __launch_bounds__(WARP ? 256 : VE == 1 ? 1024 : 512, WARP ? 2 : 1) norm_back_kernel(const __grid_constant__ NormParams P) {
+    constexpr bool kAhead = NV <= 4 && NV * VE <= 16;  // the next row is under way while this one is summed up (not where registers do not suffice)
     using Col = Columns<T, VE>;
-    __shared__ float cells[2][TH / 32];
-    __shared__ float joined[TH == 32 ? 8 : 1][TH == 32 ? 32 * NV * VE : 1];
+    __shared__ __align__(16) float cells[2][32];
+    __shared__ float joined[WARP ? 8 : 1][WARP ? 32 * NV * VE : 1];
     let_next_kernel_start();
-    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const long long group = blockIdx.x * (long long)kGroups + (TH == 32 ? threadIdx.x >> 5 : 0u);
+    const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
+    const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
     const int count = P.width / VE;  // (VE divides it)
-    float dw[NV][VE] = {};
-    int turn = 0;
-    for (long long i = group; i < P.rows; i += (long long)gridDim.x * kGroups, turn ^= 1) {
+    if constexpr (!WARP) {
+        for (int k = threadIdx.x; k < 64; k += blockDim.x) (&cells[0][0])[k] = 0.f;
+        __syncthreads();
+    }
+    float w[kAhead ? NV : 1][VE], dw[NV][VE] = {};
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * threads < count) Col::weights(P.weight, P.weight_f32, (tid + k * threads) * VE, w[k]);
+    }
+    auto weights = [&](int k) -> float (&)[VE] {
+        if constexpr (kAhead) return w[k];
+        Col::weights(P.weight, P.weight_f32, (tid + k * threads) * VE, w[0]);
+        return w[0];
+    };
+    Col a[NV], b[NV], d[NV], na[NV], nb[NV], nd[NV];
+    float s = 0.f;
+    auto fetch = [&](long long i) {
         const T* t = static_cast<const T*>(P.x) + i * P.ld_x;
         const T* dy = static_cast<const T*>(P.dy) + i * P.ld_dy;
         const T* dt = static_cast<const T*>(P.dtotal) + i * P.ld_dtotal;
-        T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
-        Col a[NV], b[NV], d[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (tid + k * TH) * VE;
-            if (tid + k * TH >= count) continue;
-            a[k].load(t + c);
-            b[k].load(dy + c);
-            if (P.dtotal) d[k].load(dt + c);
+            const int c = (tid + k * threads) * VE;
+            if (tid + k * threads >= count) continue;
+            na[k].load(t + c);
+            nb[k].load(dy + c);
+            if (P.dtotal) nd[k].load(dt + c);
         }
-        const float s = __ldg(P.rstd + i);
+        s = __ldg(P.rstd + i);
+    };
+    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (kAhead && i < P.rows) fetch(i);
+    for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
+        if (!kAhead) fetch(i);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) { a[k] = na[k]; b[k] = nb[k]; d[k] = nd[k]; }
+        const float si = s;
+        if (kAhead && i + step < P.rows) fetch(i + step);
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (tid + k * TH >= count) continue;
-            float u[VE], v[VE], w[VE];
+            if (tid + k * threads >= count) continue;
+            float u[VE], v[VE];
             a[k].unpack(u);
             b[k].unpack(v);
-            Col::weights(P.weight, P.weight_f32, (tid + k * TH) * VE, w);
+            float (&wk)[VE] = weights(k);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float unit = u[e] * s;
-                sum += v[e] * w[e] * unit;
-                dw[k][e] += v[e] * unit;
+                const float p = v[e] * (u[e] * si);
+                sum = fmaf(p, wk[e], sum);
+                dw[k][e] += p;
             }
         }
-        // (cells of the row before last: whoever writes them has passed the last row's barrier, behind the last use of them)
-        const float mean = join_row<TH, kJoinSum>(sum, cells[turn]) / (float)P.width;
+        const float mean = join_threads<WARP, kJoinSum>(sum, cells[turn]) / (float)P.width;
+        T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = (tid + k * TH) * VE;
-            if (tid + k * TH >= count) continue;
-            float u[VE], v[VE], w[VE];
+            if (tid + k * threads >= count) continue;
+            float u[VE], v[VE];
             a[k].unpack(u);
             b[k].unpack(v);
-            Col::weights(P.weight, P.weight_f32, c, w);
+            float (&wk)[VE] = weights(k);
 #pragma unroll
-            for (int e = 0; e < VE; ++e) v[e] = s * (v[e] * w[e] - u[e] * s * mean);
+            for (int e = 0; e < VE; ++e) v[e] = si * (v[e] * wk[e] - u[e] * si * mean);
             if (P.dtotal) {
                 d[k].unpack(u);
 #pragma unroll
                 for (int e = 0; e < VE; ++e) v[e] += u[e];
             }
-            Col::store(dx + c, v);
+            Col::store(dx + (tid + k * threads) * VE, v);
         }
     }
     if (!P.part) return;
     float* part = P.part + (long long)blockIdx.x * P.width;
-    if constexpr (TH == 32) {  // the eight warps' sums, in their order
+    if constexpr (WARP) {  // the eight warps' sums, in their order
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -367,21 +512,25 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 2 : 512 / TH ?
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (tid + k * TH >= count) continue;
+            if (tid + k * threads >= count) continue;
 #pragma unroll
-            for (int e = 0; e < VE; ++e) part[(tid + k * TH) * VE + e] = dw[k][e];
+            for (int e = 0; e < VE; ++e) part[(tid + k * threads) * VE + e] = dw[k][e];
         }
     }
 }
 
-// rows of any length: read twice, the columns' sums kept in memory (each by the thread that adds to it)
-template <typename T>
+// longer rows: read twice (the second time from L2), the columns' sums kept in shared memory where they fit (SUMS), else in the block's part of the workspace; each is
+// only touched by the thread that adds to it
+template <typename T, int VE, bool SUMS>
 __global__ void __launch_bounds__(1024) norm_back_long_kernel(const __grid_constant__ NormParams P) {
     constexpr int TH = 1024;
+    using Col = Columns<T, VE>;
+    extern __shared__ __align__(16) float norm_sums[];
     __shared__ float cells[2][TH / 32];
     let_next_kernel_start();
-    const int tid = threadIdx.x;
-    float* part = P.part ? P.part + (long long)blockIdx.x * P.width : nullptr;
+    const int tid = threadIdx.x, count = P.width / VE;  // (VE divides it)
+    float* const part = P.part ? P.part + (long long)blockIdx.x * P.width : nullptr;
+    float* const dw = SUMS ? norm_sums : part;
     int turn = 0;
     for (long long i = blockIdx.x; i < P.rows; i += gridDim.x, turn ^= 1) {
         const T* t = static_cast<const T*>(P.x) + i * P.ld_x;
@@ -389,21 +538,51 @@ __global__ void __launch_bounds__(1024) norm_back_long_kernel(const __grid_const
         const T* dt = static_cast<const T*>(P.dtotal) + i * P.ld_dtotal;
         T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
         const float s = __ldg(P.rstd + i);
+        const bool first = i == blockIdx.x;
         float sum = 0.f;
-#pragma unroll 4
-        for (int c = tid; c < P.width; c += TH) {
-            const float unit = to_f32(t[c]) * s, v = to_f32(dy[c]);
-            sum += v * load_weight<T>(P.weight, P.weight_f32, c) * unit;
-            if (part) part[c] = i == blockIdx.x ? v * unit : part[c] + v * unit;
+#pragma unroll 2
+        for (int k = tid; k < count; k += TH) {
+            const int c = k * VE;
+            Col a, b;
+            float u[VE], v[VE], w[VE];
+            a.load_again(t + c);
+            b.load_again(dy + c);
+            a.unpack(u);
+            b.unpack(v);
+            Col::weights(P.weight, P.weight_f32, c, w);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float p = v[e] * (u[e] * s);
+                sum = fmaf(p, w[e], sum);
+                if (part) dw[c + e] = first ? p : dw[c + e] + p;
+            }
         }
         const float mean = join_row<TH, kJoinSum>(sum, cells[turn]) / (float)P.width;
-#pragma unroll 4
-        for (int c = tid; c < P.width; c += TH) {
-            float v = s * (to_f32(dy[c]) * load_weight<T>(P.weight, P.weight_f32, c) - to_f32(t[c]) * s * mean);
-            if (P.dtotal) v += to_f32(dt[c]);
-            dx[c] = from_f32<T>(v);
+#pragma unroll 2
+        for (int k = tid; k < count; k += TH) {
+            const int c = k * VE;
+            Col a, b;
+            float u[VE], v[VE], w[VE];
+            a.load(t + c);
+            b.load(dy + c);
+            a.unpack(u);
+            b.unpack(v);
+            Col::weights(P.weight, P.weight_f32, c, w);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) v[e] = s * (v[e] * w[e] - u[e] * s * mean);
+            if (P.dtotal) {
+                a.load(dt + c);
+                a.unpack(u);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) v[e] += u[e];
+            }
+            Col::store(dx + c, v);
         }
     }
+    if (SUMS && part)
+        for (int k = tid; k < count; k += TH)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) part[k * VE + e] = dw[k * VE + e];
 }
 
 // dw from the blocks' sums: 32 columns to a block, 32 threads to a column
@@ -436,16 +615,110 @@ struct CodesParams {
     long long ld_x, ld_gate, ld_codes, rows;
     int width, act;
 };
+// act(gate) as it is wanted here.  16-bit rows: exponential and reciprocal from the special unit, within a few 2^-23 of the value.  fp32 rows: the exact functions, because
+// their codes are read against values of the same type, and next to a border a code follows every bit.
+template <typename T, int ACT>
+__device__ __forceinline__ float gate_value(float g) {
+    if constexpr (ACT == kActRelu) return g <= 0.f ? 0.f : g;
+    if constexpr (ACT == kActGelu) return g * (0.5f * (1.f + erff(g * 0.70710678118654752f)));
+    float s;
+    if constexpr (sizeof(T) == 4) {
+        s = __fdiv_rn(1.f, 1.f + expf(-g));
+    } else {
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(g * -kLog2e));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + s));
+    }
+    return ACT == kActSigmoid ? s : g * s;
+}
+// h *= act(u), the activation chosen outside the loops
+template <typename T, int N>
+__device__ __forceinline__ void gate_values(int act, float (&h)[N], const float (&u)[N]) {
+    switch (act) {
+    case kActRelu:
+#pragma unroll
+        for (int e = 0; e < N; ++e) h[e] *= gate_value<T, kActRelu>(u[e]);
+        break;
+    case kActGelu:
+#pragma unroll
+        for (int e = 0; e < N; ++e) h[e] *= gate_value<T, kActGelu>(u[e]);
+        break;
+    case kActSigmoid:
+#pragma unroll
+        for (int e = 0; e < N; ++e) h[e] *= gate_value<T, kActSigmoid>(u[e]);
+        break;
+    default:
+#pragma unroll
+        for (int e = 0; e < N; ++e) h[e] *= gate_value<T, kActSilu>(u[e]);
+    }
+}
 template <typename T>
 __device__ __forceinline__ void gated_piece(const CodesParams& P, const uint4& x, const uint4& g, float (&h)[Piece<T>::kValues]) {
     unpack_piece<T>(x, h);
     if (P.gate) {
         float u[Piece<T>::kValues];
         unpack_piece<T>(g, u);
-#pragma unroll
-        for (int e = 0; e < Piece<T>::kValues; ++e) h[e] *= act_value(P.act, u[e]);
+        gate_values<T>(P.act, h, u);
     }
 }
+template <typename T>
+__device__ __forceinline__ float gated_one(const CodesParams& P, T x, const T* g) {
+    float h[1] = {to_f32(x)};
+    if (P.gate) {
+        const float u[1] = {to_f32(*g)};
+        gate_values<T>(P.act, h, u);
+    }
+    return h[0];
+}
+// rows on 16-byte boundaries throughout: as norm_flow_kernel
+template <typename T, int NV, bool WARP, bool GATE>
+__global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) codes_flow_kernel(const __grid_constant__ CodesParams P) {
+    constexpr int VE = Piece<T>::kValues;
+    __shared__ __align__(16) float cells[2][32];
+    const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
+    const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
+    const int count = P.width / VE;  // (VE divides it)
+    if constexpr (!WARP) {
+        for (int k = threadIdx.x; k < 64; k += blockDim.x) (&cells[0][0])[k] = 0.f;
+        __syncthreads();
+    }
+    uint4 nx[NV], ng[NV];
+    auto fetch = [&](long long i) {
+        const uint4* x = reinterpret_cast<const uint4*>(static_cast<const T*>(P.x) + i * P.ld_x);
+        const uint4* g = reinterpret_cast<const uint4*>(static_cast<const T*>(P.gate) + i * P.ld_gate);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * threads < count) {
+                nx[k] = __ldcs(x + tid + k * threads);
+                if constexpr (GATE) ng[k] = __ldcs(g + tid + k * threads);
+            }
+    };
+    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i < P.rows) fetch(i);
+    for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
+        float h[NV][VE], top = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * threads >= count) continue;
+            unpack_piece<T>(nx[k], h[k]);
+            if constexpr (GATE) {
+                float u[VE];
+                unpack_piece<T>(ng[k], u);
+                gate_values<T>(P.act, h[k], u);
+            }
+#pragma unroll
+            for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(h[k][e]));
+        }
+        if (i + step < P.rows) fetch(i + step);
+        const RowCodes rc(join_threads<WARP, kJoinMax>(top, cells[turn]));
+        signed char* q = P.codes + i * P.ld_codes;
+        if (tid == 0) P.scale[i] = rc.scale;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * threads < count) store_codes<VE>(q + (tid + k * threads) * VE, rc, h[k]);
+    }
+}
+
+// rows on any boundary
 template <typename T, int TH, int NV>
 __global__ void __launch_bounds__(TH == 32 ? 256 : TH) codes_row_kernel(const __grid_constant__ CodesParams P) {
     constexpr int VE = Piece<T>::kValues;
@@ -466,7 +739,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) codes_row_kernel(const __
     const bool odd = tid < row.edges;
     const int at = row.edge(tid);
     float edge = 0.f;
-    if (odd) edge = to_f32(x[at]) * (P.gate ? act_value(P.act, to_f32(g[at])) : 1.f);
+    if (odd) edge = gated_one(P, x[at], g + at);
     float h[NV][VE], top = fabsf(edge);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -481,7 +754,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) codes_row_kernel(const __
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (tid + k * TH < row.pieces) store_codes<VE>(q + row.column(tid + k * TH), rc, h[k]);
-    if (odd) q[at] = (signed char)rc.code(edge);
+    if (odd) q[at] = rc.code(edge);
 }
 template <typename T>
 __global__ void __launch_bounds__(1024) codes_long_kernel(const __grid_constant__ CodesParams P) {
@@ -495,7 +768,7 @@ __global__ void __launch_bounds__(1024) codes_long_kernel(const __grid_constant_
     const bool odd = tid < row.edges;
     const int at = row.edge(tid);
     float edge = 0.f, h[VE];
-    if (odd) edge = to_f32(x[at]) * (P.gate ? act_value(P.act, to_f32(g[at])) : 1.f);
+    if (odd) edge = gated_one(P, x[at], g + at);
     float top = fabsf(edge);
     auto read = [&](int c) { gated_piece<T>(P, load_piece(x + c), P.gate ? load_piece(g + c) : make_uint4(0, 0, 0, 0), h); };
     for (int k = tid; k < row.pieces; k += TH) {
@@ -510,7 +783,7 @@ __global__ void __launch_bounds__(1024) codes_long_kernel(const __grid_constant_
         read(row.column(k));
         store_codes<VE>(q + row.column(k), rc, h);
     }
-    if (odd) q[at] = (signed char)rc.code(edge);
+    if (odd) q[at] = rc.code(edge);
 }
 
 // Weights [inputs][outputs] as codes [outputs][inputs] with a scale for each output: 32 outputs to a block, read once for their
@@ -536,7 +809,7 @@ __global__ void __launch_bounds__(1024) codes_weight_kernel(const T* __restrict_
     for (int k0 = 0; k0 < inputs; k0 += 128) {
 #pragma unroll
         for (int k = warp; k < 128; k += 32)
-            tile[lane][k] = c < outputs && k0 + k < inputs ? (signed char)rc.code(to_f32(w[(long long)(k0 + k) * ld_w + c])) : 0;
+            tile[lane][k] = c < outputs && k0 + k < inputs ? rc.code(to_f32(w[(long long)(k0 + k) * ld_w + c])) : (signed char)0;
         __syncthreads();
         const int out = blockIdx.x * 32 + warp;
         if (out < outputs) {

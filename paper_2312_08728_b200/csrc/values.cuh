@@ -87,14 +87,14 @@ struct RowPieces {
 // A value joined over the threads of a row, in a fixed order: a warp (TH = 32) or a block of TH threads.  `cells` (TH / 32
 // values) is this use's own until the next barrier of the block.
 enum { kJoinSum, kJoinMax };
-template <int TH, int OP>
-__device__ __forceinline__ float join_row(float v, float* cells) {
-    auto op = [](float a, float b) {
-        if (OP == kJoinSum) return a + b;
-        float m;  // (NaN wins)
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-        return m;
-    };
+__device__ __forceinline__ float nan_max(float a, float b) {  // NaN wins
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+template <int TH, int OP, typename V>
+__device__ __forceinline__ V join_row(V v, V* cells) {
+    auto op = [](V a, V b) { if constexpr (OP == kJoinSum) return a + b; else return nan_max(a, b); };
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
     if constexpr (TH > 32) {
