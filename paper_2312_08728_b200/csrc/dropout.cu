@@ -8,19 +8,15 @@ namespace {
 
 using namespace bmgdk;
 
-template <typename T, bool ONE_ROW, bool RES>
-int dropout_as(const DropoutParams& P, cudaStream_t s) {
-    constexpr int kAhead = 2;
-    const int64_t units = ONE_ROW ? (P.width + 7) / 8 : P.rows * ((P.width + 7) / 8 + 1);
-    const int64_t blocks = (units + 256 * kAhead - 1) / (256 * kAhead);
-    if (blocks > 0x7FFFFFFFll) return BMGD_ERR_ARG;
-    dropout_kernel<T, ONE_ROW, RES, kAhead><<<(unsigned)blocks, 256, 0, s>>>(P);
-    return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA;
-}
-template <typename T>
+template <typename T, bool RES>
 int dropout(const DropoutParams& P, cudaStream_t s) {
-    if (P.rows == 1) return P.residual ? dropout_as<T, true, true>(P, s) : dropout_as<T, true, false>(P, s);
-    return P.residual ? dropout_as<T, false, true>(P, s) : dropout_as<T, false, false>(P, s);
+    constexpr int kAhead = 2;
+    const bool flat = P.rows == 1 && ((uintptr_t)P.x | (uintptr_t)P.y | (uintptr_t)P.residual) % 16 == 0;
+    const int64_t blocks = flat ? (P.width / 8 + 1 + 256 * kAhead - 1) / (256 * kAhead) : (P.rows * ((P.width + 7) / 8 + 1) + 255) / 256;
+    if (blocks > 0x7FFFFFFFll) return BMGD_ERR_ARG;
+    if (flat) dropout_flat_kernel<T, RES, kAhead><<<(unsigned)blocks, 256, 0, s>>>(P);
+    else dropout_rows_kernel<T, RES><<<(unsigned)blocks, 256, 0, s>>>(P);
+    return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA;
 }
 
 // [rows][width] of strides lp and lq (in bytes w a row): the same memory value for value, or none of it
@@ -51,9 +47,9 @@ int bmgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int6
                     kDropTag + (uint32_t)layer, (float)(65536.0 / (65536.0 - threshold))};
     if (ld_x == width && ld_y == width && (!dev_residual || ld_residual == width)) { P.width *= rows; P.rows = 1; }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (type == BMGD_TYPE_F32) return dropout<float>(P, s);
-    if (type == BMGD_TYPE_BF16) return dropout<__nv_bfloat16>(P, s);
-    return dropout<__half>(P, s);
+    if (type == BMGD_TYPE_F32) return dev_residual ? dropout<float, true>(P, s) : dropout<float, false>(P, s);
+    if (type == BMGD_TYPE_BF16) return dev_residual ? dropout<__nv_bfloat16, true>(P, s) : dropout<__nv_bfloat16, false>(P, s);
+    return dev_residual ? dropout<__half, true>(P, s) : dropout<__half, false>(P, s);
 }
 
 }  // extern "C"

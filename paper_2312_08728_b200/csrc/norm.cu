@@ -144,14 +144,21 @@ int check_backward(const bmgd_rms_norm* a) {
     return BMGD_OK;
 }
 
+// Up to 384 threads with two, four or six pieces: a row's values are held in fp32, and two blocks of four pieces a thread (85 registers) fit an SM.
 template <typename T, bool GATE>
 int codes_flow(const CodesParams& P, cudaStream_t s) {
-    const Threads t = threads_for(P.width / Piece<T>::kValues);
-    const unsigned grid = flow_grid(t, P.rows, t.pieces == 4 ? 704 : 1024);
+    const int64_t count = P.width / Piece<T>::kValues;
+    Threads t = threads_for(count);
+    if (t.threads > 32) {
+        t.pieces = count <= 768 ? 2 : count <= 1536 ? 4 : 6;
+        t.threads = (int)((count + t.pieces * 32 - 1) / (t.pieces * 32)) * 32;
+    }
+    const unsigned grid = flow_grid(t, P.rows, t.pieces == 6 ? 384 : t.pieces == 4 ? 768 : 1024);
     if (t.threads == 32 && t.pieces == 1) codes_flow_kernel<T, 1, true, GATE><<<grid, 256, 0, s>>>(P);
     else if (t.threads == 32) codes_flow_kernel<T, 2, true, GATE><<<grid, 256, 0, s>>>(P);
     else if (t.pieces == 2) codes_flow_kernel<T, 2, false, GATE><<<grid, t.threads, 0, s>>>(P);
-    else codes_flow_kernel<T, 4, false, GATE><<<grid, t.threads, 0, s>>>(P);
+    else if (t.pieces == 4) codes_flow_kernel<T, 4, false, GATE><<<grid, t.threads, 0, s>>>(P);
+    else codes_flow_kernel<T, 6, false, GATE><<<grid, t.threads, 0, s>>>(P);
     return launched();
 }
 template <typename T>

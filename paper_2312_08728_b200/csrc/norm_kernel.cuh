@@ -671,7 +671,7 @@ __device__ __forceinline__ float gated_one(const CodesParams& P, T x, const T* g
 }
 // rows on 16-byte boundaries throughout: as norm_flow_kernel
 template <typename T, int NV, bool WARP, bool GATE>
-__global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) codes_flow_kernel(const __grid_constant__ CodesParams P) {
+__global__ void __launch_bounds__(WARP ? 256 : 384, NV == 6 ? 1 : 2) codes_flow_kernel(const __grid_constant__ CodesParams P) {
     constexpr int VE = Piece<T>::kValues;
     __shared__ __align__(16) float cells[2][32];
     const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;

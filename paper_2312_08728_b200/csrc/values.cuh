@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "pair.cuh"
 
@@ -29,10 +30,29 @@ template <typename T> struct Piece {
     static constexpr int kValues = 16 / (int)sizeof(T);
 };
 template <typename T>
-__device__ __forceinline__ void unpack_piece(const uint4& w, float (&x)[Piece<T>::kValues]) {
-    const T* p = reinterpret_cast<const T*>(&w);
+__device__ __forceinline__ void unpack_piece(const uint4& w, float (&x)[Piece<T>::kValues]);
+template <>
+__device__ __forceinline__ void unpack_piece<float>(const uint4& w, float (&x)[4]) {
+    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+}
+template <>
+__device__ __forceinline__ void unpack_piece<__nv_bfloat16>(const uint4& w, float (&x)[8]) {  // (bf16 is the upper half of fp32)
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < Piece<T>::kValues; ++i) x[i] = to_f32(p[i]);
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+    }
+}
+template <>
+__device__ __forceinline__ void unpack_piece<__half>(const uint4& w, float (&x)[8]) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
 }
 template <typename T> __device__ __forceinline__ void put_pair(T* t, const Pair& p);
 template <> __device__ __forceinline__ void put_pair<float>(float* t, const Pair& p) { const float2 x = p.both(); t[0] = x.x; t[1] = x.y; }
@@ -63,12 +83,19 @@ __device__ __forceinline__ void store_piece(T* p, const uint4& w) {
     for (int i = 0; i < Piece<T>::kValues; ++i) p[i] = t[i];
 }
 template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {  // two 16-bit values
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+template <typename T>
 __device__ __forceinline__ uint4 pack_piece(const float (&x)[Piece<T>::kValues]) {
-    uint4 w;
-    T* t = reinterpret_cast<T*>(&w);
-#pragma unroll
-    for (int i = 0; i < Piece<T>::kValues; i += 2) put_pair<T>(t + i, Pair(x[i], x[i + 1]));
-    return w;
+    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    else return make_uint4(pack_pair<T>(x[0], x[1]), pack_pair<T>(x[2], x[3]), pack_pair<T>(x[4], x[5]), pack_pair<T>(x[6], x[7]));
 }
 // How a row of `width` values at p falls into pieces: `head` values before the first 16-byte boundary, `pieces`, the rest.
 // (head + rest < 2 * 16 / sizeof(T) <= 16 values, one each for the first threads.)
