@@ -43,8 +43,15 @@ int bmgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int6
     if ((uintptr_t)dev_x % eb || (uintptr_t)dev_y % eb || (uintptr_t)dev_residual % eb || (uintptr_t)dev_step % 8) return BMGD_ERR_ARG;
     if (!apart_or_same(dev_y, ld_y * eb, dev_x, ld_x * eb, width * eb, rows)) return BMGD_ERR_ARG;
     if (dev_residual && !apart_or_same(dev_y, ld_y * eb, dev_residual, ld_residual * eb, width * eb, rows)) return BMGD_ERR_ARG;
-    DropoutParams P{dev_x, dev_residual, dev_y, reinterpret_cast<const long long*>(dev_step), ld_x, ld_residual, ld_y, rows, width, seed, threshold,
-                    kDropTag + (uint32_t)layer, (float)(65536.0 / (65536.0 - threshold))};
+    DropoutParams P{};
+    P.x = dev_x; P.residual = dev_residual; P.y = dev_y; P.step = reinterpret_cast<const long long*>(dev_step);
+    P.ld_x = ld_x; P.ld_residual = ld_residual; P.ld_y = ld_y; P.rows = rows; P.width = width;
+    for (uint32_t r = 0; r < 10; ++r) {
+        P.key[r][0] = (uint32_t)seed + r * 0x9E3779B9u;
+        P.key[r][1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u;
+    }
+    P.threshold = threshold; P.tag = kDropTag + (uint32_t)layer;
+    P.factor = (float)(65536.0 / (65536.0 - threshold));
     if (ld_x == width && ld_y == width && (!dev_residual || ld_residual == width)) { P.width *= rows; P.rows = 1; }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == BMGD_TYPE_F32) return dev_residual ? dropout<float, true>(P, s) : dropout<float, false>(P, s);

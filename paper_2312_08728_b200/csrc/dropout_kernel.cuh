@@ -22,20 +22,21 @@ struct DropoutParams {
     void* y;
     const long long* step;     // null: 0
     long long ld_x, ld_residual, ld_y, rows, width;
-    unsigned long long seed;
+    uint32_t key[10][2];       // of the ten rounds
     uint32_t threshold, tag;
     float factor;
 };
 
 // Which of the eight values of a block are kept.  A 32 x 32 multiplication gives both halves of its product in one instruction.
-__device__ __forceinline__ void drop_block(long long block, uint32_t step, uint32_t tag, uint32_t k0, uint32_t k1, uint32_t limit, bool (&keep)[8]) {
-    uint32_t c0 = (uint32_t)block, c1 = (uint32_t)((unsigned long long)block >> 32), c2 = step, c3 = tag;
+__device__ __forceinline__ void drop_block(const DropoutParams& P, long long block, uint32_t step, bool (&keep)[8]) {
+    uint32_t c0 = (uint32_t)block, c1 = (uint32_t)((unsigned long long)block >> 32), c2 = step, c3 = P.tag;
+    const uint32_t limit = P.threshold << 16;
 #pragma unroll
-    for (int r = 0; r < 10; ++r, k0 += 0x9E3779B9u, k1 += 0xBB67AE85u) {
+    for (int r = 0; r < 10; ++r) {
         const unsigned long long a = 0xD2511F53ull * c0, b = 0xCD9E8D57ull * c2;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ P.key[r][0];
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ P.key[r][1];
         c3 = (uint32_t)a;
     }
     const uint32_t w[4] = {c0, c1, c2, c3};
@@ -83,11 +84,11 @@ __global__ void __launch_bounds__(256) dropout_flat_kernel(const __grid_constant
         const int u = (int)threadIdx.x + a * 256;
         bool keep[8];
         if (u < left) {
-            drop_block(begin + u, step, P.tag, (uint32_t)P.seed, (uint32_t)(P.seed >> 32), P.threshold << 16, keep);
+            drop_block(P, begin + u, step, keep);
 #pragma unroll
             for (int p = 0; p < kParts; ++p) y[u * kParts + p] = drop_piece<T, RES, VE>(v[a][p], r[a][p], keep + p * VE, P.factor);
         } else if (begin + u == full && full * 8 < P.width) {  // the last values, fewer than eight
-            drop_block(full, step, P.tag, (uint32_t)P.seed, (uint32_t)(P.seed >> 32), P.threshold << 16, keep);
+            drop_block(P, full, step, keep);
             const T *xs = static_cast<const T*>(P.x) + full * 8, *zs = static_cast<const T*>(P.residual) + full * 8;
             T* ys = static_cast<T*>(P.y) + full * 8;
 #pragma unroll
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(256) dropout_rows_kernel(const __grid_constant
         }
     }
     bool keep[8];
-    drop_block(block, step, P.tag, (uint32_t)P.seed, (uint32_t)(P.seed >> 32), P.threshold << 16, keep);
+    drop_block(P, block, step, keep);
     if (whole) {
 #pragma unroll
         for (int p = 0; p < kParts; ++p) store_piece(y + p * VE, drop_piece<T, RES, VE>(v[p], r[p], keep + p * VE, P.factor));

@@ -7,9 +7,10 @@
 //     alternatives: the K largest logits in falling order, equal ones by rising class
 //
 // One pass over the row keeps a running maximum with both sums in every thread; t needs no second pass because both sums are
-// carried to a larger maximum together: s' = s f, t' = (t + s (M - M')) f with f = e^(M - M').  The sums are taken in powers of two,
-// 2^(z L - m) with L = log2 e in fp32 and m = M L rounded: one multiply-add a logit.  What m is rounded by is the same in every
-// term; it is put right once, in log s (Score).
+// carried to a larger maximum together: s' = s f, t' = (t + s (M - M')) f with f = e^(M - M').  While a thread reads, its sums may stay with
+// an earlier maximum as long as the present one is no more than 40 above it (no term overflows): among 32 lanes some maximum rises in nearly every round.
+// The sums are taken in powers of two, 2^(z L - m) with L = log2 e in fp32 and m = M L rounded: one multiply-add a logit.  What m is
+// rounded by is the same in every term; it is put right once, in log s (row_score).
 //
 // Alternatives.  Each thread's maximum is known after that pass.  The maxima of 32 parts of the row (the threads of equal lane) bound the K-th
 // largest logit from below: at least K of the parts hold a logit at or above the K-th largest of them.  Only the logits of threads whose own
@@ -81,13 +82,6 @@ __device__ __forceinline__ Score score_warp(Score a) {
     }
     return a;
 }
-__device__ __forceinline__ void score_one(Score& a, float x) {
-    const float m = score_max(a.m, x);
-    if (!(m <= a.m)) score_raise(a, m);
-    const float d = fmaxf(fmaf(x, kLog2e, -score_base(a.m)), kFar2), p = power_of_two(d);
-    a.s += p;
-    a.t = fmaf(d, p, a.t);
-}
 template <typename T>
 __device__ __forceinline__ float score_piece_max(const uint4& w) {
     if constexpr (sizeof(T) == 4) {
@@ -104,19 +98,112 @@ __device__ __forceinline__ float score_piece_max(const uint4& w) {
         return score_max(m.x, m.y);
     }
 }
+// What the terms of a maximum are taken against: its stand-in, and a floor so far below that e^(floor - M) is 0 and (floor L - m) finite.
+// Logits below it, -Inf among them, are raised to it: two at a time in 16-bit types (a minimum in fp32 after the multiply-add would be
+// an instruction for each), in fp32 after the multiply-add.
+template <typename T>
+struct Against {
+    float base;
+    uint32_t floor2;
+    __device__ __forceinline__ explicit Against(float m) : base(score_base(m)), floor2(0) {
+        if constexpr (sizeof(T) == 2) {
+            const float least = std::is_same<T, __half>::value ? -65504.f : -2.f * kWide;
+            if (std::is_same<T, __half>::value) base = fmaxf(base, least * kLog2e);  // (m = -Inf: no term above one)
+            const float f = fmaxf(fmaf(fabsf(m), -1.f / 64, m) - 130.f, least);  // (NaN: least)
+            floor2 = pack_pair<T>(f, f);
+        }
+    }
+};
+// Whether a row's maximum asks for the careful form: beyond +-2^126, or in fp16 too near the lowest value for a floor.
+template <typename T>
+__device__ __forceinline__ bool score_wide(float m) {
+    return fabsf(m) < INFINITY && (fabsf(m) > kWide || (std::is_same<T, __half>::value && m < -65000.f));
+}
 // adds a piece to sums against the base of the present maximum
 template <typename T>
-__device__ __forceinline__ void score_piece(const uint4& w, float base, float& s, float& t) {
+__device__ __forceinline__ void score_piece(const uint4& w, const Against<T>& g, float& s, float& t) {
     constexpr int VE = Piece<T>::kValues;
     float x[VE];
-    unpack_piece<T>(w, x);
+    if constexpr (sizeof(T) == 2) {
+        uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 h = __hmax2(*reinterpret_cast<const __half2*>(&v[i]), *reinterpret_cast<const __half2*>(&g.floor2));
+                v[i] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&v[i]), *reinterpret_cast<const __nv_bfloat162*>(&g.floor2));
+                v[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
+        unpack_piece<T>(make_uint4(v[0], v[1], v[2], v[3]), x);
+    } else {
+        unpack_piece<T>(w, x);
+    }
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-        const float d = fmaxf(fmaf(x[e], kLog2e, -base), kFar2), p = power_of_two(d);
+        float d = fmaf(x[e], kLog2e, -g.base);
+        if constexpr (sizeof(T) == 4) d = fmaxf(d, kFar2);
+        const float p = power_of_two(d);
         s += p;
         t = fmaf(d, p, t);
     }
 }
+// largest value of four pieces
+template <typename T>
+__device__ __forceinline__ float score_pieces_max(const uint4 (&w)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        return score_max(score_max(score_piece_max<T>(w[0]), score_piece_max<T>(w[1])), score_max(score_piece_max<T>(w[2]), score_piece_max<T>(w[3])));
+    } else {
+        typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type Two;
+        const Two *a = reinterpret_cast<const Two*>(&w[0]), *b = reinterpret_cast<const Two*>(&w[1]), *c = reinterpret_cast<const Two*>(&w[2]), *d = reinterpret_cast<const Two*>(&w[3]);
+        uint4 m;
+        Two* t = reinterpret_cast<Two*>(&m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = __hmax2_nan(__hmax2_nan(a[i], b[i]), __hmax2_nan(c[i], d[i]));
+        return score_piece_max<T>(m);
+    }
+}
+// A thread's sums while it reads: against `from`, the largest value at the time they were last carried on.
+template <typename T>
+struct Reading {
+    Score a;      // (a.m: the largest value so far)
+    float from;
+    Against<T> g;
+    __device__ __forceinline__ Reading() : a{-INFINITY, 0.f, 0.f}, from(-INFINITY), g(-INFINITY) {}
+    __device__ __forceinline__ void reach(float m) {
+        a.m = score_max(a.m, m);
+        if (!(a.m - from <= 40.f)) {  // (also the first time, and while all is -Inf)
+            Score b{from, a.s, a.t};
+            score_raise(b, a.m);
+            a = b;
+            from = a.m;
+            g = Against<T>(from);
+        }
+    }
+    __device__ __forceinline__ void add_four(const uint4 (&w)[4]) {
+        reach(score_pieces_max<T>(w));
+        float s = 0.f, t = 0.f;  // (two sums each: the additions follow one another)
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+            score_piece<T>(w[k], g, a.s, a.t);
+            score_piece<T>(w[k + 1], g, s, t);
+        }
+        a.s += s;
+        a.t += t;
+    }
+    __device__ __forceinline__ void add_one(float x) {
+        reach(x);
+        const float d = fmaxf(fmaf(x, kLog2e, -g.base), kFar2), p = power_of_two(d);
+        a.s += p;
+        a.t = fmaf(d, p, a.t);
+    }
+    __device__ __forceinline__ Score done() const {
+        Score b{from, a.s, a.t};
+        score_raise(b, a.m);
+        return b;
+    }
+};
 // What a row's sums say.
 struct RowScore {
     float m, log_s, entropy;  // log p = (z - m) - log_s
@@ -153,8 +240,9 @@ struct LogProbShared {
     RowScore row;
     float lanes[TH / 32][32];
     int owners[TH];
+    int spots[ROOM];
     unsigned long long found[ROOM];
-    int owner_count, found_count;
+    int owner_count, spot_count, found_count;
     uint32_t bound;
     uint32_t best[TH / 32], place[TH / 32], equal[TH / 32];
 };
@@ -227,7 +315,7 @@ __device__ __noinline__ void take_by_value(const T* z, int C, int top, LogProbSh
     row_sync<TH>();
 }
 
-// A row whose maximum is beyond +-2^126 (all logits at a type's lowest value, say), against differences that are taken first: all
+// A row whose maximum score_wide names (all logits at a type's lowest value, say), against differences that are taken first: all
 // threads of the row call it, with its maximum; each returns the whole row's sums, as row_score gives them.
 template <typename T, int TH, int ROOM>
 __device__ __noinline__ RowScore score_careful(const T* z, int C, float m, LogProbShared<TH, ROOM>& S) {
@@ -291,45 +379,48 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
         if (tid == 0 && label >= 0 && label < P.C) at_label = to_f32(z[label]);
 
         // ---- one pass: the sums of each thread, and its maximum
-        Score a{-INFINITY, 0.f, 0.f};
+        Reading<T> read;
         const bool odd = tid < row.edges;
         const float edge_value = edge;
-        if (odd) score_one(a, edge_value);
+        if (odd) read.add_one(edge_value);
         uint4 w[kAhead];
-        int k0 = tid;
-        const int rounds = pieces / (kAhead * TH);  // in which every thread has kAhead pieces
-        for (int round = 0; round < rounds; ++round, k0 += kAhead * TH) {
+        // rounds in which every thread has kAhead pieces, two to a turn: one set of registers is filled while the other is worked on
+        const int rounds = pieces / (kAhead * TH);
+        const uint4* at = src + tid;
+        int left = rounds;
+        auto fill = [&](uint4 (&v)[kAhead], const uint4* from) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                w[k] = next[k];
-                if (k0 + (kAhead + k) * TH < pieces) next[k] = src[k0 + (kAhead + k) * TH];
-            }
-            const float m = score_max(a.m, score_max(score_max(score_piece_max<T>(w[0]), score_piece_max<T>(w[1])),
-                                                     score_max(score_piece_max<T>(w[2]), score_piece_max<T>(w[3]))));
-            if (!(m <= a.m)) score_raise(a, m);
-            const float base = score_base(a.m);
-            float s2 = 0.f, t2 = 0.f;  // (two sums each: the additions follow one another)
+            for (int k = 0; k < kAhead; ++k) v[k] = from[k * TH];
+        };
+        for (; left > 2; left -= 2, at += 2 * kAhead * TH) {
+            fill(w, at + kAhead * TH);
+            read.add_four(next);
+            fill(next, at + 2 * kAhead * TH);
+            read.add_four(w);
+        }
+        int k0 = tid + (rounds - left) * kAhead * TH;
+        for (; left > 0; --left) {
 #pragma unroll
-            for (int k = 0; k < kAhead; k += 2) {
-                score_piece<T>(w[k], base, a.s, a.t);
-                score_piece<T>(w[k + 1], base, s2, t2);
-            }
-            a.s += s2;
-            a.t += t2;
+            for (int k = 0; k < kAhead; ++k)
+                if (k0 + (kAhead + k) * TH < pieces) w[k] = src[k0 + (kAhead + k) * TH];
+            read.add_four(next);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) next[k] = w[k];
+            k0 += kAhead * TH;
         }
         {  // what is left of the row: up to kAhead pieces a thread
-            float m = a.m;
+            float m = read.a.m;
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 w[k] = next[k];
                 if (k0 + k * TH < pieces) m = score_max(m, score_piece_max<T>(w[k]));
             }
-            if (!(m <= a.m)) score_raise(a, m);
-            const float base = score_base(a.m);
+            read.reach(m);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
-                if (k0 + k * TH < pieces) score_piece<T>(w[k], base, a.s, a.t);
+                if (k0 + k * TH < pieces) score_piece<T>(w[k], read.g, read.a.s, read.a.t);
         }
+        Score a = read.done();
         if (i + step < P.rows) begin(i + step);
         const float own = a.m;  // this thread's maximum
         if constexpr (TOP && TH > 32) S.lanes[warp][lane] = own;
@@ -338,7 +429,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
             if (lane == 0) S.part[warp] = a;
         }
         if constexpr (TOP) {
-            if (tid == 0) S.owner_count = S.found_count = 0;
+            if (tid == 0) S.owner_count = S.spot_count = S.found_count = 0;
         }
         row_sync<TH>();
         // the row's sums and, for the alternatives, the bound: by one warp
@@ -370,18 +461,18 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
                 if (TH > 32 && lane == 0) S.bound = g;
             }
         }
-        bool wide = TH == 32 && fabsf(r.m) > kWide && fabsf(r.m) < INFINITY;
+        bool wide = TH == 32 && score_wide<T>(r.m);
         if constexpr (TH > 32 && TOP) {
             __syncthreads();
             r = S.row;
             g = S.bound;
-            wide = fabsf(r.m) > kWide && fabsf(r.m) < INFINITY;
+            wide = score_wide<T>(r.m);
         }
         if constexpr (TH > 32 && !TOP) {  // (no other barrier is needed: whether the row is one of the rare ones, each thread sees for itself)
             float m = S.part[0].m;
 #pragma unroll
             for (int k = 1; k < kWarps; ++k) m = score_max(m, S.part[k].m);
-            wide = fabsf(m) > kWide && fabsf(m) < INFINITY;
+            wide = score_wide<T>(m);
             if (wide) r.m = m;
         }
         if (wide) r = score_careful<T>(z, P.C, r.m, S);
@@ -426,15 +517,25 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
                 for (unsigned k = tid; k < items; k += TH) {
                     const unsigned o = k / per;
                     const int p = S.owners[o] + (int)(k - o * per) * TH;
-                    if (p < pieces) consider_piece(src[p], p);
+                    if (p >= pieces || score_piece_max<T>(src[p]) < bound) continue;
+                    const int n = atomicAdd(&S.spot_count, 1);
+                    if (n < kRoom) S.spots[n] = row.column(p);
+                }
+                row_sync<TH>();
+                const int spots = min(S.spot_count, kRoom) * VE;  // (a logit to a thread)
+                for (int k = tid; k < spots; k += TH) {
+                    const int c = S.spots[k / VE] + k % VE;
+                    consider(to_f32(z[c]), c);
                 }
             }
             row_sync<TH>();
-            int found = S.found_count;
+            int found = max(S.found_count, S.spot_count);
             if (found > kRoom) {
                 row_sync<TH>();
                 take_by_value<T>(z, P.C, top, S);
                 found = top;
+            } else {
+                found = S.found_count;
             }
             for (int k = tid; k < found; k += TH) {
                 const unsigned long long mine = S.found[k];

@@ -124,7 +124,7 @@ NormParams shared_params(const bmgd_rms_norm* a) {
     NormParams P{};
     P.weight = a->weight;
     P.weight_f32 = a->weight_type == BMGD_TYPE_F32;
-    P.rows = a->rows; P.width = a->width; P.eps = (float)a->eps;
+    P.rows = a->rows; P.width = a->width; P.eps = (float)a->eps; P.per_width = 1.f / (float)a->width;
     P.rstd = a->rstd;
     return P;
 }

@@ -11,6 +11,7 @@
 #pragma once
 #include <cstdint>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "activation.cuh"
 #include "launch.cuh"
@@ -33,7 +34,7 @@ struct NormParams {
     long long rows;
     int width;
     int weight_f32;
-    float eps;
+    float eps, per_width;               // per_width: 1 / width
 };
 
 // Sums of squares.  fp32 rows: in 64 bits, since their results are held to fp32 themselves (codes next to a border follow every bit).
@@ -42,7 +43,10 @@ template <> struct SquareSum<float> { typedef double type; };
 __device__ __forceinline__ void add_square(float& sum, float t) { sum = fmaf(t, t, sum); }
 __device__ __forceinline__ void add_square(double& sum, float t) { sum = fma((double)t, (double)t, sum); }
 template <typename V>
-__device__ __forceinline__ float root_factor(V sum, const NormParams& P) { return rsqrtf((float)(sum / (V)P.width) + P.eps); }
+__device__ __forceinline__ float root_factor(V sum, const NormParams& P) {
+    if constexpr (std::is_same<V, double>::value) return rsqrtf((float)(sum / (double)P.width) + P.eps);
+    else return rsqrtf(fmaf(sum, P.per_width, P.eps));
+}
 
 template <typename T>
 __device__ __forceinline__ void load_weights(const void* weight, int f32, int c, float (&w)[Piece<T>::kValues]) {
@@ -92,7 +96,7 @@ struct RowCodes {
     __device__ __forceinline__ uint32_t bits(float y) const { return __float_as_uint(__fadd_rn(__fmul_rn(y, factor), 12582912.f)); }
     __device__ __forceinline__ signed char code(float y) const { return factor == 0.f ? (signed char)0 : (signed char)bits(y); }
 };
-template <int VE>
+template <int VE, bool ALIGNED = false>
 __device__ __forceinline__ void store_codes(signed char* p, const RowCodes& rc, const float (&y)[VE]) {
     uint32_t w[VE / 4];
 #pragma unroll
@@ -100,7 +104,7 @@ __device__ __forceinline__ void store_codes(signed char* p, const RowCodes& rc, 
         w[e / 4] = __byte_perm(__byte_perm(rc.bits(y[e]), rc.bits(y[e + 1]), 0x0040), __byte_perm(rc.bits(y[e + 2]), rc.bits(y[e + 3]), 0x0040), 0x5410);
         if (rc.factor == 0.f) w[e / 4] = 0;  // (also for NaN and Inf)
     }
-    if (((uintptr_t)p & (VE - 1)) == 0) {
+    if (ALIGNED || ((uintptr_t)p & (VE - 1)) == 0) {
         if constexpr (VE == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t*>(p) = w[0];
     } else {
@@ -119,7 +123,12 @@ __device__ __forceinline__ V join_threads(V v, V (&cells)[32]) {
         if ((threadIdx.x & 31) == 0) cells[threadIdx.x >> 5] = v;
         __syncthreads();
         v = 0;  // (maxima here are of magnitudes)
-        for (int k = 0; k < (int)(blockDim.x >> 5); k += 4) v = op(op(v, cells[k]), op(cells[k + 1], op(cells[k + 2], cells[k + 3])));
+        for (int k = 0; k < (int)(blockDim.x >> 5); k += 4) {
+            V c[4];
+            if constexpr (sizeof(V) == 4) *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(cells + k);
+            else for (int e = 0; e < 4; ++e) c[e] = cells[k + e];
+            v = op(op(v, c[0]), op(c[1], op(c[2], c[3])));
+        }
     }
     return v;
 }
@@ -132,8 +141,8 @@ template <typename T, int NV, bool WARP, bool RES, bool CODES>
 __global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_kernel(const __grid_constant__ NormParams P) {
     constexpr int VE = Piece<T>::kValues;
     typedef typename SquareSum<T>::type Sum;
-    __shared__ Sum sums[2][32];
-    __shared__ float tops[2][32];
+    __shared__ __align__(16) Sum sums[2][32];
+    __shared__ __align__(16) float tops[2][32];
     const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
     const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
     const int count = P.width / VE;  // (VE divides it)
@@ -216,7 +225,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_k
                 unpack_piece<T>(v[k], t);
 #pragma unroll
                 for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[k][e];
-                store_codes<VE>(q + (tid + k * threads) * VE, rc, t);
+                store_codes<VE, true>(q + (tid + k * threads) * VE, rc, t);
             }
         }
     }
@@ -476,7 +485,7 @@ __global__ void __launch_bounds__(WARP ? 256 : VE == 1 ? 1024 : 512, WARP ? 2 : 
                 dw[k][e] += p;
             }
         }
-        const float mean = join_threads<WARP, kJoinSum>(sum, cells[turn]) / (float)P.width;
+        const float mean = join_threads<WARP, kJoinSum>(sum, cells[turn]) * P.per_width;
         T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -557,7 +566,7 @@ __global__ void __launch_bounds__(1024) norm_back_long_kernel(const __grid_const
                 if (part) dw[c + e] = first ? p : dw[c + e] + p;
             }
         }
-        const float mean = join_row<TH, kJoinSum>(sum, cells[turn]) / (float)P.width;
+        const float mean = join_row<TH, kJoinSum>(sum, cells[turn]) * P.per_width;
 #pragma unroll 2
         for (int k = tid; k < count; k += TH) {
             const int c = k * VE;
@@ -714,7 +723,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 384, NV == 6 ? 1 : 2) codes_flow_
         if (tid == 0) P.scale[i] = rc.scale;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (tid + k * threads < count) store_codes<VE>(q + (tid + k * threads) * VE, rc, h[k]);
+            if (tid + k * threads < count) store_codes<VE, true>(q + (tid + k * threads) * VE, rc, h[k]);
     }
 }
 
