@@ -10,15 +10,14 @@ using namespace bmgdk;
 
 int launched() { return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA; }
 
-// By the row's length in pieces of 16 bytes: a warp to a row up to 128, then blocks of 128 to 512 threads; as many blocks as an SM holds.
+// By the row's length in pieces of 16 bytes: a warp to a row up to 128, then blocks of 64 threads, or of 512 where the rows are too few to give
+// every SM some.  As many blocks as an SM holds.
 template <typename T, bool TOP>
 int forward(const LogProbParams& P, cudaStream_t s) {
     const int64_t pieces = ((int64_t)P.C * (int64_t)sizeof(T) + 15) / 16;
-    auto grid = [&](int threads) { return (unsigned)std::min<int64_t>(threads == 32 ? (P.rows + 7) / 8 : P.rows, 148 * (threads == 32 ? 4 : 1024 / threads)); };
-    if (pieces <= 128) logprob_kernel<T, 32, TOP><<<grid(32), 256, 0, s>>>(P);
-    else if (pieces <= 1024) logprob_kernel<T, 128, TOP><<<grid(128), 128, 0, s>>>(P);
-    else if (pieces <= 8192 && P.rows > 148) logprob_kernel<T, 256, TOP><<<grid(256), 256, 0, s>>>(P);
-    else logprob_kernel<T, 512, TOP><<<grid(512), 512, 0, s>>>(P);
+    if (pieces <= 128) logprob_kernel<T, 32, TOP><<<(unsigned)std::min<int64_t>((P.rows + 7) / 8, 148 * 3), 256, 0, s>>>(P);
+    else if (pieces <= 512 || P.rows > 148 * 4) logprob_kernel<T, 64, TOP><<<(unsigned)std::min<int64_t>(P.rows, 148 * 12), 64, 0, s>>>(P);
+    else logprob_kernel<T, 512, TOP><<<(unsigned)std::min<int64_t>(P.rows, 148), 512, 0, s>>>(P);
     return launched();
 }
 // A warp to a row up to 128 pieces, else blocks of 256 threads, several to a row where the rows alone do not fill the GPU.

@@ -12,9 +12,9 @@
 // The sums are taken in powers of two, 2^(z L - m) with L = log2 e in fp32 and m = M L rounded: one multiply-add a logit.  What m is
 // rounded by is the same in every term; it is put right once, in log s (row_score).
 //
-// Alternatives.  Each thread's maximum is known after that pass.  The maxima of 32 parts of the row (the threads of equal lane) bound the K-th
-// largest logit from below: at least K of the parts hold a logit at or above the K-th largest of them.  Only the logits of threads whose own
-// maximum reaches that bound are looked at again (a few dozen threads of a row of independent logits, from L2), what reaches the
+// Alternatives.  The maxima of 32 parts of the row (the threads of equal lane) bound the K-th
+// largest logit from below: at least K of the parts hold a logit at or above the K-th largest of them.  While it reads, a thread leaves the
+// maximum of each of its stretches in shared memory; only stretches that reach the bound are looked at again (a few dozen of a row of independent logits, from L2), what reaches the
 // bound is put aside, and its K largest are ranked by counting.  Rows with more candidates than there is room (thousands of equal logits, a mask that
 // leaves fewer than K) are taken value by value: largest below the last one, with all that equal it.
 //
@@ -98,53 +98,18 @@ __device__ __forceinline__ float score_piece_max(const uint4& w) {
         return score_max(m.x, m.y);
     }
 }
-// What the terms of a maximum are taken against: its stand-in, and a floor so far below that e^(floor - M) is 0 and (floor L - m) finite.
-// Logits below it, -Inf among them, are raised to it: two at a time in 16-bit types (a minimum in fp32 after the multiply-add would be
-// an instruction for each), in fp32 after the multiply-add.
+// Whether a row's maximum asks for the careful form
+__device__ __forceinline__ bool score_wide(float m) { return fabsf(m) < INFINITY && fabsf(m) > kWide; }
+// adds a piece to sums against a base.  (Raising what is far below in its 16-bit form, two at a time, took longer: 8191 x 50257 155 us
+// instead of 151.)
 template <typename T>
-struct Against {
-    float base;
-    uint32_t floor2;
-    __device__ __forceinline__ explicit Against(float m) : base(score_base(m)), floor2(0) {
-        if constexpr (sizeof(T) == 2) {
-            const float least = std::is_same<T, __half>::value ? -65504.f : -2.f * kWide;
-            if (std::is_same<T, __half>::value) base = fmaxf(base, least * kLog2e);  // (m = -Inf: no term above one)
-            const float f = fmaxf(fmaf(fabsf(m), -1.f / 64, m) - 130.f, least);  // (NaN: least)
-            floor2 = pack_pair<T>(f, f);
-        }
-    }
-};
-// Whether a row's maximum asks for the careful form: beyond +-2^126, or in fp16 too near the lowest value for a floor.
-template <typename T>
-__device__ __forceinline__ bool score_wide(float m) {
-    return fabsf(m) < INFINITY && (fabsf(m) > kWide || (std::is_same<T, __half>::value && m < -65000.f));
-}
-// adds a piece to sums against the base of the present maximum
-template <typename T>
-__device__ __forceinline__ void score_piece(const uint4& w, const Against<T>& g, float& s, float& t) {
+__device__ __forceinline__ void score_piece(const uint4& w, float base, float& s, float& t) {
     constexpr int VE = Piece<T>::kValues;
     float x[VE];
-    if constexpr (sizeof(T) == 2) {
-        uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (std::is_same<T, __half>::value) {
-                const __half2 h = __hmax2(*reinterpret_cast<const __half2*>(&v[i]), *reinterpret_cast<const __half2*>(&g.floor2));
-                v[i] = *reinterpret_cast<const uint32_t*>(&h);
-            } else {
-                const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&v[i]), *reinterpret_cast<const __nv_bfloat162*>(&g.floor2));
-                v[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-        }
-        unpack_piece<T>(make_uint4(v[0], v[1], v[2], v[3]), x);
-    } else {
-        unpack_piece<T>(w, x);
-    }
+    unpack_piece<T>(w, x);
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-        float d = fmaf(x[e], kLog2e, -g.base);
-        if constexpr (sizeof(T) == 4) d = fmaxf(d, kFar2);
-        const float p = power_of_two(d);
+        const float d = fmaxf(fmaf(x[e], kLog2e, -base), kFar2), p = power_of_two(d);
         s += p;
         t = fmaf(d, p, t);
     }
@@ -167,10 +132,8 @@ __device__ __forceinline__ float score_pieces_max(const uint4 (&w)[4]) {
 // A thread's sums while it reads: against `from`, the largest value at the time they were last carried on.
 template <typename T>
 struct Reading {
-    Score a;      // (a.m: the largest value so far)
-    float from;
-    Against<T> g;
-    __device__ __forceinline__ Reading() : a{-INFINITY, 0.f, 0.f}, from(-INFINITY), g(-INFINITY) {}
+    Score a{-INFINITY, 0.f, 0.f};  // (a.m: the largest value so far)
+    float from = -INFINITY, base = 0.f;
     __device__ __forceinline__ void reach(float m) {
         a.m = score_max(a.m, m);
         if (!(a.m - from <= 40.f)) {  // (also the first time, and while all is -Inf)
@@ -178,23 +141,25 @@ struct Reading {
             score_raise(b, a.m);
             a = b;
             from = a.m;
-            g = Against<T>(from);
+            base = score_base(from);
         }
     }
-    __device__ __forceinline__ void add_four(const uint4 (&w)[4]) {
-        reach(score_pieces_max<T>(w));
+    __device__ __forceinline__ float add_four(const uint4 (&w)[4]) {  // returns the largest of them
+        const float m = score_pieces_max<T>(w);
+        reach(m);
         float s = 0.f, t = 0.f;  // (two sums each: the additions follow one another)
 #pragma unroll
         for (int k = 0; k < 4; k += 2) {
-            score_piece<T>(w[k], g, a.s, a.t);
-            score_piece<T>(w[k + 1], g, s, t);
+            score_piece<T>(w[k], base, a.s, a.t);
+            score_piece<T>(w[k + 1], base, s, t);
         }
         a.s += s;
         a.t += t;
+        return m;
     }
     __device__ __forceinline__ void add_one(float x) {
         reach(x);
-        const float d = fmaxf(fmaf(x, kLog2e, -g.base), kFar2), p = power_of_two(d);
+        const float d = fmaxf(fmaf(x, kLog2e, -base), kFar2), p = power_of_two(d);
         a.s += p;
         a.t = fmaf(d, p, a.t);
     }
@@ -239,10 +204,9 @@ struct LogProbShared {
     Score part[TH / 32];
     RowScore row;
     float lanes[TH / 32][32];
-    int owners[TH];
-    int spots[ROOM];
     unsigned long long found[ROOM];
-    int owner_count, spot_count, found_count;
+    int spots[ROOM], classes[ROOM];
+    int spot_count, found_count;
     uint32_t bound;
     uint32_t best[TH / 32], place[TH / 32], equal[TH / 32];
 };
@@ -346,13 +310,18 @@ __device__ __noinline__ RowScore score_careful(const T* z, int C, float m, LogPr
 }
 
 // TH threads to a row (TH = 32: a warp, eight rows to a block), rows taken with the grid's stride: the first pieces of the next row are
-// fetched before this one's sums are joined.
+// fetched before this one's sums are joined.  Small blocks with many registers: 8191 x 50257 bf16 took 135 us with 64 threads and 85 registers, 142
+// with 128, 157 with 256; 142 with 64 threads and 64 registers.
 template <typename T, int TH, bool TOP>
-__global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 ? 2 : 1024 / TH) logprob_kernel(const __grid_constant__ LogProbParams P) {
-    constexpr int VE = Piece<T>::kValues, kAhead = 4, kWarps = TH / 32;
-    constexpr int kRoom = TH == 32 ? 160 : 512;
+__global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 3 : TH >= 512 ? 1 : 768 / TH) logprob_kernel(const __grid_constant__ LogProbParams P) {
+    constexpr int VE = Piece<T>::kValues, kAhead = 4, kWarps = TH / 32, kRound = kAhead * TH;
+    constexpr int kRoom = 160;
+    // maxima kept of a row's stretches, each thread its own; as few bytes as will do, because the loads under way need the rest for L1 (12 blocks to an
+    // SM of 17 KB each: 8191 x 50257 with 20 alternatives 209 us, of 8 KB 173)
+    constexpr int kStretches = 4096 / (int)sizeof(T);
     // (two sets that take turns: a thread that begins a row may meet others that still read what they share of the row before)
-    __shared__ LogProbShared<TH, TOP ? kRoom : 1> shared[TH == 32 ? 8 : 1][2];
+    __shared__ LogProbShared<TH, TOP ? kRoom : 1> shared[TH == 32 ? 8 : 1][TH == 32 ? 1 : 2];
+    __shared__ T stretch[TOP && TH > 32 ? kStretches : 1];
     const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long step = TH == 32 ? gridDim.x * 8ll : (long long)gridDim.x;
     uint4 next[kAhead];
@@ -369,7 +338,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
     long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
     if (i < P.rows) begin(i);
     for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
-        auto& S = shared[TH == 32 ? threadIdx.x >> 5 : 0][turn];
+        auto& S = shared[TH == 32 ? threadIdx.x >> 5 : 0][TH == 32 ? 0 : turn];
         const T* z = static_cast<const T*>(P.z) + i * P.ld;
         const RowPieces<T> row(z, P.C);
         const uint4* src = reinterpret_cast<const uint4*>(z + row.head);
@@ -385,41 +354,53 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
         if (odd) read.add_one(edge_value);
         uint4 w[kAhead];
         // rounds in which every thread has kAhead pieces, two to a turn: one set of registers is filled while the other is worked on
-        const int rounds = pieces / (kAhead * TH);
+        const int rounds = pieces / kRound;
+        const int span = (rounds + kStretches / TH - 1) / (kStretches / TH);  // rounds of a stretch
+        int stretches = 0, in_stretch = 0;
+        float highest = -INFINITY;
+        auto add = [&](const uint4 (&v)[kAhead]) {
+            const float m = read.add_four(v);
+            if constexpr (TOP && TH > 32) {
+                highest = score_max(highest, m);
+                if (++in_stretch == span) {
+                    stretch[stretches++ * TH + tid] = from_f32<T>(highest);  // (exact: it is one of them)
+                    highest = -INFINITY;
+                    in_stretch = 0;
+                }
+            }
+        };
         const uint4* at = src + tid;
         int left = rounds;
-        auto fill = [&](uint4 (&v)[kAhead], const uint4* from) {
+        for (; left > 2; left -= 2, at += 2 * kRound) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) v[k] = from[k * TH];
-        };
-        for (; left > 2; left -= 2, at += 2 * kAhead * TH) {
-            fill(w, at + kAhead * TH);
-            read.add_four(next);
-            fill(next, at + 2 * kAhead * TH);
-            read.add_four(w);
+            for (int k = 0; k < kAhead; ++k) w[k] = at[kRound + k * TH];
+            add(next);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) next[k] = at[2 * kRound + k * TH];
+            add(w);
         }
-        int k0 = tid + (rounds - left) * kAhead * TH;
+        int k0 = tid + (rounds - left) * kRound;
         for (; left > 0; --left) {
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
                 if (k0 + (kAhead + k) * TH < pieces) w[k] = src[k0 + (kAhead + k) * TH];
-            read.add_four(next);
+            add(next);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) next[k] = w[k];
-            k0 += kAhead * TH;
+            k0 += kRound;
         }
-        {  // what is left of the row: up to kAhead pieces a thread
-            float m = read.a.m;
+        if (TOP && TH > 32 && in_stretch > 0) stretch[stretches++ * TH + tid] = from_f32<T>(highest);  // (exact: it is one of them)
+        // what is left of the row, up to kAhead pieces a thread: they stay in registers
+        highest = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                w[k] = next[k];
-                if (k0 + k * TH < pieces) m = score_max(m, score_piece_max<T>(w[k]));
-            }
-            read.reach(m);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (k0 + k * TH < pieces) score_piece<T>(w[k], read.g, read.a.s, read.a.t);
+        for (int k = 0; k < kAhead; ++k) {
+            w[k] = next[k];
+            if (k0 + k * TH < pieces) highest = score_max(highest, score_piece_max<T>(w[k]));
         }
+        read.reach(highest);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (k0 + k * TH < pieces) score_piece<T>(w[k], read.base, read.a.s, read.a.t);
         Score a = read.done();
         if (i + step < P.rows) begin(i + step);
         const float own = a.m;  // this thread's maximum
@@ -429,7 +410,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
             if (lane == 0) S.part[warp] = a;
         }
         if constexpr (TOP) {
-            if (tid == 0) S.owner_count = S.spot_count = S.found_count = 0;
+            if (tid == 0) S.spot_count = S.found_count = 0;
         }
         row_sync<TH>();
         // the row's sums and, for the alternatives, the bound: by one warp
@@ -451,28 +432,30 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
                     for (int k = 1; k < kWarps; ++k) m = score_max(m, S.lanes[k][lane]);
                     g = rank_bits(m);
                 }
-                int rank = 0;
+                // the 32 parts' maxima in falling order, lane by lane
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const uint32_t o = __shfl_sync(0xFFFFFFFFu, g, j);
-                    rank += o > g || (o == g && j < lane) ? 1 : 0;
-                }
-                g = __shfl_sync(0xFFFFFFFFu, g, __ffs(__ballot_sync(0xFFFFFFFFu, rank == P.top - 1)) - 1);
+                for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+                    for (int j = k >> 1; j > 0; j >>= 1) {
+                        const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, g, j);
+                        g = ((lane & k) == 0) == ((lane & j) == 0) ? max(g, o) : min(g, o);
+                    }
+                g = __shfl_sync(0xFFFFFFFFu, g, P.top - 1);
                 if (TH > 32 && lane == 0) S.bound = g;
             }
         }
-        bool wide = TH == 32 && score_wide<T>(r.m);
+        bool wide = TH == 32 && score_wide(r.m);
         if constexpr (TH > 32 && TOP) {
             __syncthreads();
             r = S.row;
             g = S.bound;
-            wide = score_wide<T>(r.m);
+            wide = score_wide(r.m);
         }
         if constexpr (TH > 32 && !TOP) {  // (no other barrier is needed: whether the row is one of the rare ones, each thread sees for itself)
             float m = S.part[0].m;
 #pragma unroll
             for (int k = 1; k < kWarps; ++k) m = score_max(m, S.part[k].m);
-            wide = score_wide<T>(m);
+            wide = score_wide(m);
             if (wide) r.m = m;
         }
         if (wide) r = score_careful<T>(z, P.C, r.m, S);
@@ -490,42 +473,44 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
             // ---- the alternatives
             const int top = P.top;
             const float bound = rank_value(g);
-            auto consider = [&](float x, int c) {
-                if (x < bound) return;  // (NaN is no less)
+            auto found_one = [&](int c) {
                 const int n = atomicAdd(&S.found_count, 1);
-                if (n < kRoom) S.found[n] = candidate(rank_bits(x), c);
+                if (n < kRoom) S.classes[n] = c;
             };
             auto consider_piece = [&](const uint4& v, int p) {
-                if (score_piece_max<T>(v) < bound) return;
+                if (score_piece_max<T>(v) < bound) return;  // (NaN is no less)
                 float x[VE];
                 unpack_piece<T>(v, x);
+                uint32_t hits = 0;
 #pragma unroll
-                for (int e = 0; e < VE; ++e) consider(x[e], row.column(p) + e);
+                for (int e = 0; e < VE; ++e) hits |= x[e] < bound ? 0u : 1u << e;
+                for (; hits; hits &= hits - 1) found_one(row.column(p) + __ffs(hits) - 1);
             };
-            if (odd) consider(edge_value, row.edge(tid));
-            if (rounds == 0) {  // the whole row is still in registers
-                if (!(own < bound)) {
+            if (odd && !(edge_value < bound)) found_one(row.edge(tid));
+            if (!(highest < bound)) {
 #pragma unroll
-                    for (int k = 0; k < kAhead; ++k)
-                        if (tid + k * TH < pieces) consider_piece(w[k], tid + k * TH);
-                }
-            } else {  // all threads look at the pieces of those whose maximum reaches the bound
-                if (!(own < bound)) S.owners[atomicAdd(&S.owner_count, 1)] = tid;
-                row_sync<TH>();
-                const unsigned per = (unsigned)(pieces + TH - 1) / TH, items = (unsigned)S.owner_count * per;
+                for (int k = 0; k < kAhead; ++k)
+                    if (k0 + k * TH < pieces) consider_piece(w[k], k0 + k * TH);
+            }
+            if (rounds > 0) {
+                if constexpr (TH > 32) {
+#pragma unroll 4
+                    for (int k = 0; k < stretches; ++k)
+                        if (!(to_f32(stretch[k * TH + tid]) < bound)) {
+                            const int n = atomicAdd(&S.spot_count, 1);
+                            if (n < kRoom) S.spots[n] = k * TH + tid;
+                        }
+                    __syncthreads();
+                    // all threads look at the pieces of the stretches found: `reach` pieces each, TH apart
+                    const unsigned reach = (unsigned)span * kAhead, items = (unsigned)min(S.spot_count, kRoom) * reach;
 #pragma unroll 2
-                for (unsigned k = tid; k < items; k += TH) {
-                    const unsigned o = k / per;
-                    const int p = S.owners[o] + (int)(k - o * per) * TH;
-                    if (p >= pieces || score_piece_max<T>(src[p]) < bound) continue;
-                    const int n = atomicAdd(&S.spot_count, 1);
-                    if (n < kRoom) S.spots[n] = row.column(p);
-                }
-                row_sync<TH>();
-                const int spots = min(S.spot_count, kRoom) * VE;  // (a logit to a thread)
-                for (int k = tid; k < spots; k += TH) {
-                    const int c = S.spots[k / VE] + k % VE;
-                    consider(to_f32(z[c]), c);
+                    for (unsigned k = tid; k < items; k += TH) {
+                        const unsigned o = k / reach, spot = (unsigned)S.spots[o], first = spot / TH * reach;
+                        const unsigned p = (first + (k - o * reach)) * TH + spot % TH;
+                        if (p < (unsigned)(rounds * kRound)) consider_piece(src[p], (int)p);
+                    }
+                } else {  // (a warp's row of one round: its pieces are read again)
+                    for (int p = tid; p < rounds * kRound; p += TH) consider_piece(src[p], p);
                 }
             }
             row_sync<TH>();
@@ -536,6 +521,8 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
                 found = top;
             } else {
                 found = S.found_count;
+                for (int k = tid; k < found; k += TH) S.found[k] = candidate(rank_bits(to_f32(z[S.classes[k]])), S.classes[k]);
+                row_sync<TH>();
             }
             for (int k = tid; k < found; k += TH) {
                 const unsigned long long mine = S.found[k];
@@ -547,6 +534,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 4 : TH >= 512 
                 P.index[i * top + rank] = (int)(0xFFFFFFFFu - (uint32_t)mine);
                 P.value[i * top + rank] = r.broken ? nan : r.nothing ? -INFINITY : (x - r.m) - r.log_s;
             }
+            if constexpr (TH == 32) __syncwarp();  // (a warp has one set)
         }
     }
 }
