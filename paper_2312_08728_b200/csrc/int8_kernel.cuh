@@ -476,6 +476,85 @@ __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __gr
     if (warp == 2) ffn_tmem_free<1>(tmem, F::kTmemCols);
 }
 
+// ---------------------------------------------------------------- one to four tokens
+// A warp to a channel, its row of weights read in batches of 32 x 8 pieces of 16 bytes, the next batch (or channel) under way while this
+// one is multiplied on the integer dot-product units; the tokens stand in shared memory.  Bound by reading the weights once.  No tensor maps, barriers or
+// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 in place of int8_few_kernel 11.8 -> see the launch's comment.
+constexpr int kInt8Vec = 8;
+struct Int8VecParams {
+    const signed char *q, *w;               // rows of w on 16-byte boundaries
+    const float *q_scale, *w_scale, *bias;
+    void* out;
+    long long ld_q, ld_w, ld_out;
+    int N, K, type;
+};
+template <int M>
+__global__ void __launch_bounds__(768) int8_vec_kernel(const __grid_constant__ Int8VecParams P) {
+    extern __shared__ uint4 int8_tokens[];  // [M][pieces], zeros behind the last value
+    wait_for_previous_kernel();
+    let_next_kernel_start();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int pieces = (P.K + 15) / 16, full = P.K / 16, batches = (full + 32 * kInt8Vec - 1) / (32 * kInt8Vec), step = (int)gridDim.x * warps;
+    int n = (int)blockIdx.x * warps + warp;
+    uint4 v[kInt8Vec];
+    auto fetch = [&](int channel, int batch) {
+        const uint4* row = reinterpret_cast<const uint4*>(P.w + channel * P.ld_w);
+#pragma unroll
+        for (int u = 0; u < kInt8Vec; ++u) {
+            const int p = (batch * kInt8Vec + u) * 32 + lane;
+            v[u] = p < full ? __ldcs(row + p) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    if (n < P.N) fetch(n, 0);
+    for (int m = 0; m < M; ++m) {
+        signed char* to = reinterpret_cast<signed char*>(int8_tokens + m * pieces);
+        const signed char* from = P.q + m * P.ld_q;
+        if (((uintptr_t)from & 15u) == 0) {
+            for (int p = threadIdx.x; p < full; p += blockDim.x) int8_tokens[m * pieces + p] = *reinterpret_cast<const uint4*>(from + 16 * p);
+            if (threadIdx.x < 16 && full < pieces) to[full * 16 + threadIdx.x] = full * 16 + (int)threadIdx.x < P.K ? from[full * 16 + threadIdx.x] : (signed char)0;
+        } else {
+            for (int c = threadIdx.x; c < pieces * 16; c += blockDim.x) to[c] = c < P.K ? from[c] : (signed char)0;
+        }
+    }
+    __syncthreads();
+    for (; n < P.N; n += step) {
+        int sum[M] = {};
+        for (int b = 0; b < batches; ++b) {
+            uint4 now[kInt8Vec];
+#pragma unroll
+            for (int u = 0; u < kInt8Vec; ++u) now[u] = v[u];
+            if (b + 1 < batches) fetch(n, b + 1);
+            else if (n + step < P.N) fetch(n + step, 0);
+#pragma unroll
+            for (int u = 0; u < kInt8Vec; ++u) {
+                const int p = (b * kInt8Vec + u) * 32 + lane;
+                if (p >= full) continue;
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    const uint4 t = int8_tokens[m * pieces + p];
+                    sum[m] = __dp4a((int)now[u].x, (int)t.x, sum[m]);
+                    sum[m] = __dp4a((int)now[u].y, (int)t.y, sum[m]);
+                    sum[m] = __dp4a((int)now[u].z, (int)t.z, sum[m]);
+                    sum[m] = __dp4a((int)now[u].w, (int)t.w, sum[m]);
+                }
+            }
+        }
+        if (batches == 0 && n + step < P.N) fetch(n + step, 0);
+        // what is left of the row, fewer than 16 values
+        if (full * 16 + lane < P.K) {
+            const int c = full * 16 + lane, x = P.w[n * P.ld_w + c];
+#pragma unroll
+            for (int m = 0; m < M; ++m) sum[m] += x * reinterpret_cast<const signed char*>(int8_tokens + m * pieces)[c];
+        }
+        const float ws = __ldg(P.w_scale + n), bias = P.bias ? __ldg(P.bias + n) : 0.f;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int total = __reduce_add_sync(0xFFFFFFFFu, sum[m]);
+            if (lane == m) int8_store1(P.out, P.type, m * P.ld_out + n, (float)total * __ldg(P.q_scale + m) * ws + bias);
+        }
+    }
+}
+
 // ---------------------------------------------------------------- operands that TMA cannot read
 // Rows of `cols` bytes from stride ld to stride ld_out (a multiple of 16, at least cols), the rest of each row zero.
 struct Int8AlignJob {
@@ -495,17 +574,30 @@ __device__ __forceinline__ void int8_align_one(const Int8AlignJob& j) {
         const int c = (int)(i - r * per) * 16;
         const signed char* in = j.in + r * j.ld + c;
         uint32_t v[4];
+        const unsigned shift = (unsigned)((uintptr_t)in & 3u);
+        // inside the row: words, shifted; next to its ends byte by byte
+        if (c >= 4 && c + 20 <= j.cols) {
+            const uint32_t* word = reinterpret_cast<const uint32_t*>(in - shift);
+            uint32_t lo = word[0];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[k] = 0;
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t hi = word[k + 1];
+                v[k] = __funnelshift_r(lo, hi, 8 * shift);
+                lo = hi;
+            }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + 4 * k + e < j.cols) v[k] |= (uint32_t)(unsigned char)in[4 * k + e] << (8 * e);
+            for (int k = 0; k < 4; ++k) {
+                v[k] = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + 4 * k + e < j.cols) v[k] |= (uint32_t)(unsigned char)in[4 * k + e] << (8 * e);
+            }
         }
         *reinterpret_cast<uint4*>(j.out + r * j.ld_out + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
-template <int JOBS>
+template <int JOBS>  // (a template, so that every file may hold it)
 __global__ void __launch_bounds__(256) int8_align_kernel(const __grid_constant__ Int8AlignParams P) {
     wait_for_previous_kernel();
     let_next_kernel_start();

@@ -91,6 +91,8 @@ FewChoice choose_few(const Int8Params& P, const Device& dev) {
     return best;
 }
 
+constexpr int kVecBytes = 200 * 1024;  // of tokens in shared memory
+
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
 bool tma_ready(const Bytes& m) { return (uintptr_t)m.base % 16 == 0 && m.ld % 16 == 0; }
 
@@ -126,9 +128,49 @@ int check(const bmgd_quantized_linear_args* a, bool pointers) {
     return BMGD_OK;
 }
 
+// Up to four tokens: warps per SM so that the channels come out even, at least eight: 148 x W channels at a time.  (11008 channels: 15 warps, five each.)
+template <int M>
+int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
+    int best = 8;
+    if (P.N <= dev.sms * 8) {
+        best = std::max(1, (P.N + dev.sms - 1) / dev.sms);
+    } else {
+        int64_t least = INT64_MAX;
+        for (int w = 8; w <= 24; ++w) {
+            const int64_t span = (int64_t)dev.sms * w, reached = (P.N + span - 1) / span * span;
+            if (reached <= least) { least = reached; best = w; }
+        }
+    }
+    const int bytes = M * ((P.K + 15) / 16) * 16;
+    auto* fn = int8_vec_kernel<M>;
+    if (bytes > 48 * 1024) {
+        static std::atomic<unsigned long long> allowed{0};
+        const int rc = allow_smem(fn, kVecBytes, dev, allowed);
+        if (rc != BMGD_OK) return rc;
+    }
+    cudaLaunchConfig_t lc{};
+    cudaLaunchAttribute at[2];
+    launch_config(&lc, at, dim3((unsigned)std::min((P.N + best - 1) / best, dev.sms)), best * 32, bytes, 1, s);
+    if (cudaLaunchKernelEx(&lc, fn, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    return BMGD_OK;
+}
+// whether the form for one to four tokens takes it
+bool few_enough(const bmgd_quantized_linear_args* a) {
+    return a->rows <= 4 && (uintptr_t)a->weight % 16 == 0 && (a->ld_weight % 16 == 0 || a->outputs == 1) && a->rows * ((a->inputs + 15) / 16 * 16) <= kVecBytes;
+}
+
 // run = false: only counts the workspace
 int product(const bmgd_quantized_linear_args* a, Space* space, bool run, const Device& dev, cudaStream_t s) {
     Bytes q{a->codes, a->rows, a->inputs, a->ld_codes}, w{a->weight, a->outputs, a->inputs, a->ld_weight};
+    if (few_enough(a) && dev.budget_ns == 0) {  // (the others' waits are what a budget is given to test)
+        if (!run) return BMGD_OK;
+        const Int8VecParams V{reinterpret_cast<const signed char*>(a->codes), reinterpret_cast<const signed char*>(a->weight), a->scale, a->weight_scale, a->bias, a->y,
+                              a->ld_codes, a->ld_weight, a->ld_y, a->outputs, a->inputs, a->type};
+        if (a->rows == 1) return launch_vec<1>(V, dev, s);
+        if (a->rows == 2) return launch_vec<2>(V, dev, s);
+        if (a->rows == 3) return launch_vec<3>(V, dev, s);
+        return launch_vec<4>(V, dev, s);
+    }
     Bytes* const operands[2] = {&q, &w};
     const int rc = align_operands(operands, space, run, s);
     if (rc != BMGD_OK || !run) return rc;
@@ -159,6 +201,7 @@ int run_product(const bmgd_quantized_linear_args* a, void* workspace, int64_t wo
     int rc = check(a, true);
     if (rc != BMGD_OK || a->rows == 0) return rc;
     Device dev{};
+    dev.budget_ns = budget_ns;
     Space need{nullptr, 0};
     rc = product(a, &need, false, dev, nullptr);
     if (rc != BMGD_OK) return rc;
