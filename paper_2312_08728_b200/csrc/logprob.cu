@@ -20,14 +20,16 @@ int forward(const LogProbParams& P, cudaStream_t s) {
     else logprob_kernel<T, 512, TOP><<<(unsigned)std::min<int64_t>(P.rows, 148), 512, 0, s>>>(P);
     return launched();
 }
-// A warp to a row up to 128 pieces, else blocks of 256 threads, several to a row where the rows alone do not fill the GPU.
+// A warp to a row up to 128 pieces, else blocks of 256 threads, from 2048 pieces on 512 (8191 x 50257: 265 and 255 us), several to a row where the
+// rows alone do not fill the GPU.
 template <typename T>
 int backward(const LogProbParams& P, cudaStream_t s) {
     const int64_t pieces = ((int64_t)P.C * (int64_t)sizeof(T) + 15) / 16;
     const unsigned rows = (unsigned)P.rows;
-    const unsigned share = (unsigned)std::max<int64_t>(1, std::min<int64_t>((pieces + 511) / 512, 148 * 4 / P.rows));
+    const unsigned share = (unsigned)std::max<int64_t>(1, std::min<int64_t>((pieces + 1023) / 1024, 148 * 4 / P.rows));
     if (pieces <= 128) logprob_back_kernel<T, 32><<<(rows + 7) / 8, 256, 0, s>>>(P);
-    else logprob_back_kernel<T, 256><<<dim3(rows, share), 256, 0, s>>>(P);
+    else if (pieces < 2048 || share > 1) logprob_back_kernel<T, 256><<<dim3(rows, share), 256, 0, s>>>(P);
+    else logprob_back_kernel<T, 512><<<rows, 512, 0, s>>>(P);
     return launched();
 }
 
@@ -50,6 +52,7 @@ LogProbParams params(const bmgd_log_probs_args* a) {
     P.dlogprob = a->dlogprob; P.dentropy = a->dentropy;
     P.dz = a->dlogits; P.ld_dz = a->ld_dlogits;
     P.rows = a->rows; P.C = a->C; P.top = a->top;
+    P.far = a->rows * a->C * (a->type == BMGD_TYPE_F32 ? 4 : 2) > kFarBytes;
     return P;
 }
 

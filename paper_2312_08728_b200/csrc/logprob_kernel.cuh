@@ -44,7 +44,7 @@ struct LogProbParams {
     const float *dlogprob, *dentropy;  // backward; null: zeros
     void* dz;
     long long ld, ld_dz, rows;
-    int C, top;
+    int C, top, far;            // far: dz is not to stay in L2
 };
 
 // Maximum M (NaN wins), its stand-in m = M L, and sums of 2^(z L - m) and (z L - m) 2^(z L - m).  |M| is at most kWide where the sums
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 3 : TH >= 512 
 // ---- gradient: each logit read once, its gradient written once.  gridDim.y blocks share a row.
 template <typename T, int TH>
 __global__ void __launch_bounds__(TH == 32 ? 256 : TH) logprob_back_kernel(const __grid_constant__ LogProbParams P) {
-    constexpr int VE = Piece<T>::kValues, kAhead = 2;
+    constexpr int VE = Piece<T>::kValues, kAhead = 4;
     const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
     const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
     if (i >= P.rows) return;
@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) logprob_back_kernel(const
                 }
                 put_pair<T>(t + e, Pair(v.x, v.y));
             }
-            store_piece(dz + c, out);
+            store_piece(dz + c, out, P.far != 0);
         }
     }
 }

@@ -126,6 +126,7 @@ NormParams shared_params(const bmgd_rms_norm* a) {
     P.weight_f32 = a->weight_type == BMGD_TYPE_F32;
     P.rows = a->rows; P.width = a->width; P.eps = (float)a->eps; P.per_width = 1.f / (float)a->width;
     P.rstd = a->rstd;
+    P.far = a->rows * a->width * value_bytes(a->type) > kFarBytes;
     return P;
 }
 

@@ -35,6 +35,7 @@ struct NormParams {
     int width;
     int weight_f32;
     float eps, per_width;               // per_width: 1 / width
+    int far;                            // results are not to stay in L2
 };
 
 // Sums of squares.  fp32 rows: in 64 bits, since their results are held to fp32 themselves (codes next to a border follow every bit).
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_k
 #pragma unroll
                 for (int e = 0; e < VE; ++e) t[e] += u[e];
                 v[k] = pack_piece<T>(t);
-                reinterpret_cast<uint4*>(static_cast<T*>(P.total) + i * P.ld_total)[tid + k * threads] = v[k];
+                store16(reinterpret_cast<uint4*>(static_cast<T*>(P.total) + i * P.ld_total) + tid + k * threads, v[k], P.far != 0);
                 unpack_piece<T>(v[k], t);
             }
 #pragma unroll
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_k
                 unpack_piece<T>(v[k], t);
 #pragma unroll
                 for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[k][e];
-                y[tid + k * threads] = pack_piece<T>(t);
+                store16(y + tid + k * threads, pack_piece<T>(t), P.far != 0);
             }
         } else {
             float top = 0.f;
@@ -407,7 +408,7 @@ struct Columns<T, 1> {
     __device__ __forceinline__ void load(const T* p) { v = __ldcs(p); }
     __device__ __forceinline__ void load_again(const T* p) { v = *p; }  // (what will be read again)
     __device__ __forceinline__ void unpack(float (&x)[1]) const { x[0] = to_f32(v); }
-    static __device__ __forceinline__ void store(T* p, const float (&x)[1]) { *p = from_f32<T>(x[0]); }
+    static __device__ __forceinline__ void store(T* p, const float (&x)[1], bool) { *p = from_f32<T>(x[0]); }
     static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[1]) { x[0] = load_weight<T>(w, f32, c); }
 };
 template <typename T, int VE>
@@ -417,7 +418,7 @@ struct Columns {
     __device__ __forceinline__ void load(const T* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void load_again(const T* p) { v = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void unpack(float (&x)[VE]) const { unpack_piece<T>(v, x); }
-    static __device__ __forceinline__ void store(T* p, const float (&x)[VE]) { *reinterpret_cast<uint4*>(p) = pack_piece<T>(x); }
+    static __device__ __forceinline__ void store(T* p, const float (&x)[VE], bool far) { store16(reinterpret_cast<uint4*>(p), pack_piece<T>(x), far); }
     static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[VE]) { load_weights<T>(w, f32, c, x); }
 };
 
@@ -501,7 +502,7 @@ __global__ void __launch_bounds__(WARP ? 256 : VE == 1 ? 1024 : 512, WARP ? 2 : 
 #pragma unroll
                 for (int e = 0; e < VE; ++e) v[e] += u[e];
             }
-            Col::store(dx + (tid + k * threads) * VE, v);
+            Col::store(dx + (tid + k * threads) * VE, v, P.far != 0);
         }
     }
     if (!P.part) return;
@@ -585,7 +586,7 @@ __global__ void __launch_bounds__(1024) norm_back_long_kernel(const __grid_const
 #pragma unroll
                 for (int e = 0; e < VE; ++e) v[e] += u[e];
             }
-            Col::store(dx + c, v);
+            Col::store(dx + c, v, P.far != 0);
         }
     }
     if (SUMS && part)
