@@ -52,14 +52,15 @@ struct LogProbParams {
 struct Score {
     float m, s, t;
 };
-constexpr float kWide = 8.507059e37f;   // 2^126: z L stays finite
+constexpr float kWide = 16777216.f;     // 2^24: m is M L within one
 constexpr float kFar2 = -300.f;         // 2^-300 is 0 in fp32: a logit that far below (-Inf too) counts for nothing, and 0 times it is 0
 __device__ __forceinline__ float score_max(float a, float b) {
     float m;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
     return m;
 }
-__device__ __forceinline__ float score_base(float m) { return fminf(fmaxf(m, -kWide), kWide) * kLog2e; }
+// (rounded by itself: within a multiply-add the product would be another number, and carrying sums on to the same maximum no longer one)
+__device__ __forceinline__ float score_base(float m) { return __fmul_rn(fminf(fmaxf(m, -kWide), kWide), kLog2e); }
 __device__ __forceinline__ float power_of_two(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -279,7 +280,7 @@ __device__ __noinline__ void take_by_value(const T* z, int C, int top, LogProbSh
     row_sync<TH>();
 }
 
-// A row whose maximum score_wide names (all logits at a type's lowest value, say), against differences that are taken first: all
+// A row whose maximum is beyond +-2^24 (all logits at a type's lowest value, say), against differences that are taken first: all
 // threads of the row call it, with its maximum; each returns the whole row's sums, as row_score gives them.
 template <typename T, int TH, int ROOM>
 __device__ __noinline__ RowScore score_careful(const T* z, int C, float m, LogProbShared<TH, ROOM>& S) {
@@ -555,13 +556,17 @@ __global__ void __launch_bounds__(TH == 32 ? 256 : TH) logprob_back_kernel(const
     const bool nothing = m == -INFINITY || !(labelled_row || P.dentropy);  // no distribution, or nothing asked of it
     const float a = labelled_row && !nothing ? P.dlogprob[i] : 0.f, b = P.dentropy && !nothing ? P.dentropy[i] : 0.f;
     // dz = p (k0 + k1 log p), and a for the label
-    const float k0 = nothing ? 0.f : -(a + b * entropy), k1 = nothing ? 0.f : -b, base = nothing ? 0.f : m;
+    const float k0 = -(a + b * entropy), k1 = -b, base = m;
     auto one = [&](float x, int c) {
-        const float lp = fmaxf((x - base) - (nothing ? 0.f : log_s), kFarBelow), v = exp_fast(lp) * (k0 + k1 * lp);
+        const float lp = fmaxf((x - base) - log_s, kFarBelow), v = exp_fast(lp) * (k0 + k1 * lp);
         return c == label ? v + a : v;
     };
-    if (blockIdx.y == 0 && tid < row.edges) dz[row.edge(tid)] = from_f32<T>(one(to_f32(z[row.edge(tid)]), row.edge(tid)));
-    const Pair minus_m(-base), minus_s(nothing ? 0.f : -log_s), log2e(kLog2e), p0(k0), p1(k1);
+    if (!nothing && blockIdx.y == 0 && tid < row.edges) dz[row.edge(tid)] = from_f32<T>(one(to_f32(z[row.edge(tid)]), row.edge(tid)));
+    if (nothing) {  // (zeros, whatever the row holds)
+        for (int c = (int)blockIdx.y * TH + tid; c < P.C; c += (int)gridDim.y * TH) dz[c] = from_f32<T>(0.f);
+        return;
+    }
+    const Pair minus_m(-base), minus_s(-log_s), log2e(kLog2e), p0(k0), p1(k1);
     for (int q0 = (int)blockIdx.y * kAhead * TH + tid; q0 < row.pieces; q0 += (int)gridDim.y * kAhead * TH) {
         uint4 w[kAhead];
 #pragma unroll

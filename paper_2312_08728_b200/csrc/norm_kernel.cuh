@@ -3,7 +3,7 @@
 //
 //     t = x + r rounded to the rows' type,  s = 1 / sqrt(mean_c t_c^2 + eps),  y_c = t_c s w_c
 //     backward, g = dy w:  dt_c = dtotal_c + s (g_c - t_c s^2 mean(g t)),   dw_c = sum over rows of dy_c t_c s
-//     8 bits:  a = max_c |y_c|,  scale = a / 127,  code_c = y_c (127 / a) rounded to the nearest whole number
+//     8 bits:  a = max_c |y_c|,  scale = a / 127,  code_c = y_c (1 / a) 127 rounded to the nearest whole number
 //
 // The norm is that of the rounded sum: it is what the next block reads as its residual, what is kept for the backward pass, and so
 // the gradients are those of the values that were computed.  All sums are fp32.  What bounds it: memory, each value read and
@@ -89,7 +89,7 @@ struct RowCodes {
     float factor, scale;
     __device__ __forceinline__ explicit RowCodes(float top) {
         const bool fine = top < INFINITY, some = top >= kCodesLeast;
-        factor = fine && some ? __fdiv_rn(127.f, top) : 0.f;
+        factor = fine && some ? __fmul_rn(__frcp_rn(top), 127.f) : 0.f;
         scale = !fine ? __uint_as_float(0x7FC00000u) : some ? __fdiv_rn(top, 127.f) : 0.f;
     }
     // The code stands in the low byte: next to 1.5 2^23 the step of fp32 is one, so the sum is the whole number, rounded to nearest

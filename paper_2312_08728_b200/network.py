@@ -18,12 +18,16 @@ multiplied by a power of two S, which the update divides out again in fp32; S / 
 up to 128 rows, 1, unless the caller gives `loss_scale`.  An update whose gradients are not finite is left out
 (state["control"] counts them).  Eight steps after one whose loss was a number, S falls to a quarter; it rises again by as much
 after 2,000 updates without one.  (A loss that is NaN comes from the rows, or from hidden values above 65,504: no S mends that.)
+
+ResidualGatedSoftmax puts residual blocks in front of that layer, t <- t + dropout((act(u Wg) * (u Wu)) Wd) with u the norm of t, and one more
+norm before the layer itself.  Both models score rows (score: log probabilities of labels, entropies, best alternatives) and
+hand out a copy of themselves with weights in 8 bits to score with (quantized).
 """
 from __future__ import annotations
 
 import math
 import sys
-from typing import Dict, List, Optional
+from typing import Dict, List, Optional, Tuple
 
 import torch
 
@@ -60,8 +64,8 @@ class GatedSoftmax:
             max_norm = sys.float_info.max   # clips nothing, and leaves an update out whose norm is not finite
         self._rule = dict(a=a, b=b, eps=eps, weight_decay=weight_decay, max_norm=max_norm, seed=seed)
         gen = torch.Generator(device=self.device).manual_seed(seed)
-        shapes = ((p, hidden), (p, hidden), (hidden, C))
-        self.masters: List[torch.Tensor] = [torch.randn(s, generator=gen, device=self.device) * s[0] ** -0.5 for s in shapes]
+        self.masters: List[torch.Tensor] = [torch.randn(s, generator=gen, device=self.device) * s[0] ** -0.5 if len(s) == 2 else
+                                            torch.ones(s, device=self.device) for s in self._shapes()]
         self.weights: List[torch.Tensor] = [m.to(dtype) for m in self.masters]
         self.state: Dict = ops.adamw_state(self.weights, state_bits)
         self._slots: List[Optional[tuple]] = [None, None]    # (x, y) on the device
@@ -75,6 +79,10 @@ class GatedSoftmax:
             self._counts = torch.zeros(_LAG, ops.CONTROL_WORDS, dtype=torch.int64).pin_memory()
             self._losses = torch.zeros(_LAG).pin_memory()
             self._counted = [torch.cuda.Event() for _ in range(_LAG)]
+
+    def _shapes(self) -> List[Tuple[int, ...]]:
+        """Of the weights: matrices [inputs, outputs], and the norms' vectors, which begin as ones."""
+        return [(self.p, self.hidden), (self.p, self.hidden), (self.hidden, self.C)]
 
     def load_buffer(self, host_x: torch.Tensor, host_y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Start copying one buffer (pinned host tensors, labels int32) into the next slot on `stream`, behind the last
@@ -168,9 +176,7 @@ class GatedSoftmax:
         """One update from the rows of one mini-batch; returns the loss of each.  (A step captured into a graph keeps the S of its
         capture.)"""
         scale = self._scale(x.shape[0])
-        logits, saved = ops.gated_ffn(x, *self.weights, self.activation, save=True)
-        residual, loss = ops.softmax_residual(logits, y, None if scale == 1.0 else scale / max(x.shape[0], 1))
-        _, *grads = ops.gated_ffn_backward(residual, x, *self.weights, saved, self.activation, need_dx=False)
+        grads, loss = self._gradients(x, y, None if scale == 1.0 else scale / max(x.shape[0], 1))
         ops.adamw_step(self.weights, grads, lr=lr, masters=self.masters, grad_scale=1.0 / scale, **self.state, **self._rule)
         if self.dtype is torch.float16 and not torch.cuda.is_current_stream_capturing():
             k = self._steps % _LAG
@@ -181,9 +187,25 @@ class GatedSoftmax:
             self._steps += 1
         return loss
 
+    def _gradients(self, x: torch.Tensor, y: torch.Tensor, scale: Optional[float]) -> Tuple[List[torch.Tensor], torch.Tensor]:
+        """Gradients of all weights, and the loss of each row."""
+        logits, saved = ops.gated_ffn(x, *self.weights, self.activation, save=True)
+        residual, loss = ops.softmax_residual(logits, y, scale)
+        _, *grads = ops.gated_ffn_backward(residual, x, *self.weights, saved, self.activation, need_dx=False)
+        return grads, loss
+
     def logits(self, x: torch.Tensor) -> torch.Tensor:
         """The model's answer for device rows x."""
         return ops.gated_ffn(x, *self.weights, self.activation)
+
+    def score(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, top: int = 0):
+        """(logprob, entropy, classes, logprobs) for device rows x, as operators.log_probs gives them: of the labels y, and of the
+        `top` most probable classes."""
+        return ops.log_probs(self.logits(x), y, top)
+
+    def quantized(self) -> "QuantizedScorer":
+        """The model as it is now with its matrices in 8 bits, to score with."""
+        return QuantizedScorer(self)
 
     def get_theta(self) -> List[torch.Tensor]:
         """Copies of the fp32 weights (Wg, Wu, Wd) on the host."""
@@ -191,8 +213,8 @@ class GatedSoftmax:
 
     def set_theta(self, theta) -> None:
         """Overwrite the weights; the optimizer's state stays."""
-        if len(theta) != 3 or any(t.shape != m.shape for t, m in zip(theta, self.masters)):
-            raise ValueError("theta must be [p, hidden], [p, hidden] and [hidden, C]")
+        if len(theta) != len(self.masters) or any(t.shape != m.shape for t, m in zip(theta, self.masters)):
+            raise ValueError("theta must be " + ", ".join(str(list(m.shape)) for m in self.masters))
         for t, m, w in zip(theta, self.masters, self.weights):
             m.copy_(t)
             w.copy_(m)
@@ -201,3 +223,100 @@ class GatedSoftmax:
         """Wait for everything issued on the current stream and report a device-side error if one was raised (the step concerned
         has NaN for gradients then, and so have the weights after it unless max_norm is given, which leaves such an update out)."""
         ops.stream_check(torch.cuda.current_stream(self.device))
+
+
+class ResidualGatedSoftmax(GatedSoftmax):
+    """GatedSoftmax behind `blocks` residual blocks of the same hidden width:
+
+        t_0 = X,   t_(l+1) = t_l + dropout((act(u_l Wg_l) * (u_l Wu_l)) Wd_l),   u_l = t_l / sqrt(mean(t_l^2) + norm_eps) * w_l
+        logits = (act(u Wg) * (u Wu)) Wd  of the norm u of the last t
+
+    The weights' order: Wg, Wu, Wd of each block and of the last layer, then the norms' vectors, which are not decayed.  Dropout takes place in
+    training only; its masks follow from the seed, the block and the count of updates taken."""
+
+    def __init__(self, N: int, p: int, K: int, hidden: int, C: int, blocks: int = 1, dropout: float = 0.0, norm_eps: float = 1e-6, **options):
+        if blocks < 0 or blocks > 0xFFFF:
+            raise ValueError("blocks must be 0 to 65535")
+        if not 0.0 <= dropout < 1.0 - 2.0 ** -17:
+            raise ValueError("dropout must be 0 to below 1 - 2^-17")
+        self.blocks, self.dropout, self.norm_eps = blocks, dropout, norm_eps
+        super().__init__(N, p, K, hidden, C, **options)
+        decay = self._rule["weight_decay"]
+        self._rule["weight_decay"] = [decay if m.dim() == 2 else 0.0 for m in self.masters]
+
+    def _shapes(self) -> List[Tuple[int, ...]]:
+        one = [(self.p, self.hidden), (self.p, self.hidden), (self.hidden, self.p)]
+        return one * self.blocks + super()._shapes() + [(self.p,)] * (self.blocks + 1)
+
+    def _block(self, l: int) -> List[torch.Tensor]:
+        return self.weights[3 * l:3 * l + 3]
+
+    def _norm(self, l: int) -> torch.Tensor:
+        return self.weights[3 * (self.blocks + 1) + l]
+
+    def _drop(self, v: torch.Tensor, l: int, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return ops.dropout(v, self.dropout, self._rule["seed"], layer=l, step=self.state["control"][:1], residual=residual)
+
+    def _gradients(self, x, y, scale):
+        kept, v, total = [], x, None
+        for l in range(self.blocks + 1):
+            u, total, rstd = ops.rms_norm(v, self._norm(l), residual=total, eps=self.norm_eps, save=True)
+            v, saved = ops.gated_ffn(u, *self._block(l), self.activation, save=True)
+            kept.append((u, total, rstd, saved))
+            if self.dropout > 0 and l < self.blocks:
+                v, total = self._drop(v, l, total), None
+        residual, loss = ops.softmax_residual(v, y, scale)
+        matrices: List[torch.Tensor] = []
+        vectors: List[torch.Tensor] = []
+        dv, dtotal = residual, None
+        for l in reversed(range(self.blocks + 1)):
+            u, total, rstd, saved = kept[l]
+            du, *grads = ops.gated_ffn_backward(dv, u, *self._block(l), saved, self.activation)
+            dtotal, dw = ops.rms_norm_backward(du, total, self._norm(l), rstd, dtotal)
+            matrices[:0] = grads
+            vectors.insert(0, dw)
+            if l > 0:
+                dv = self._drop(dtotal, l - 1) if self.dropout > 0 else dtotal
+        return matrices + vectors, loss
+
+    def logits(self, x):
+        v, total = x, None
+        for l in range(self.blocks + 1):
+            u, total = ops.rms_norm(v, self._norm(l), residual=total, eps=self.norm_eps)
+            v = ops.gated_ffn(u, *self._block(l), self.activation)
+        return v
+
+
+class QuantizedScorer:
+    """A model's copy with its matrices in 8 bits, a scale for each output: rows are brought to 8 bits in front of each product, a scale
+    for each row, and the sums are exact.  Between the products values have the rows' type."""
+
+    def __init__(self, net: GatedSoftmax):
+        self.dtype, self.p, self.hidden, self.activation = net.dtype, net.p, net.hidden, net.activation
+        self.norms: List[torch.Tensor] = []
+        self.norm_eps = 0.0
+        layers = 1
+        if isinstance(net, ResidualGatedSoftmax):
+            layers, self.norm_eps = net.blocks + 1, net.norm_eps
+            self.norms = [net._norm(l).clone() for l in range(layers)]
+        self.layers = []
+        for l in range(layers):
+            w_gate, w_up, w_down = net.masters[3 * l:3 * l + 3]
+            self.layers.append((*ops.quantize_weight(torch.cat((w_gate, w_up), dim=1)), *ops.quantize_weight(w_down)))
+
+    def logits(self, x: torch.Tensor) -> torch.Tensor:
+        """The model's answer for device rows x."""
+        v, total = x, None
+        for l, (both, both_scale, down, down_scale) in enumerate(self.layers):
+            if self.norms:
+                q, scale, total = ops.rms_norm_int8(v, self.norms[l], residual=total, eps=self.norm_eps)
+            else:
+                q, scale = ops.quantize_rows(v)
+            v = ops.int8_linear(q, scale, both, both_scale, dtype=self.dtype)
+            q, scale = ops.quantize_rows(v[:, self.hidden:], gate=v[:, :self.hidden], activation=self.activation)
+            v = ops.int8_linear(q, scale, down, down_scale, dtype=self.dtype)
+        return v
+
+    def score(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, top: int = 0):
+        """As GatedSoftmax.score."""
+        return ops.log_probs(self.logits(x), y, top)
