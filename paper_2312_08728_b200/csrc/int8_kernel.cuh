@@ -52,7 +52,7 @@ __device__ __forceinline__ void int8_store1(void* out, int type, long long at, f
 
 // ---------------------------------------------------------------- many tokens
 // As ffn_kernel: warp 0 copies tiles into the ring, warp 1 issues the products, warps 4 to 11 read accumulators out, which take
-// turns.  CG = 2: pairs of CTAs, 256 tokens by 256 channels.  The tokens are the tile's rows; a channel's scale and bias come from shared memory,
+// turns.  CG = 2: pairs of CTAs, 256 tokens by 192 or 256 channels (128 channels took as long a tile as 256).  The tokens are the tile's rows; a channel's scale and bias come from shared memory,
 // where the read-out warps put those of the next tile before they wait for its products.
 constexpr int kInt8Threads = 128 + 8 * 32;
 template <int CG, int BN>
@@ -60,7 +60,7 @@ struct Int8Shape {
     static constexpr int kA = 128 * kInt8BK;
     static constexpr int kB = BN / CG * kInt8BK;
     static constexpr int kStage = kA + kB;
-    static constexpr int kStages = 5;
+    static constexpr int kStages = kStage <= 28672 ? 6 : 5;
     static constexpr int kBars = kStages * kStage;
     static constexpr int kScale = kBars + 256;                   // [2][2][BN] fp32: scale and bias of a tile's channels
     static constexpr int kTurn = kScale + 2 * 2 * BN * 4;
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_kernel(const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_ctarank() : 0u;
     const int pair = (int)blockIdx.x / CG, pairs = (int)gridDim.x / CG;
-    constexpr uint32_t kTmemCols = 2 * BN;
+    constexpr uint32_t kTmemCols = BN <= 128 ? 256 : 512;  // (two accumulators, in a power of two)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
@@ -476,10 +476,11 @@ __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __gr
     if (warp == 2) ffn_tmem_free<1>(tmem, F::kTmemCols);
 }
 
-// ---------------------------------------------------------------- one to four tokens
+// ---------------------------------------------------------------- one or two tokens
 // A warp to a channel, its row of weights read in batches of 32 x 8 pieces of 16 bytes, the next batch (or channel) under way while this
 // one is multiplied on the integer dot-product units; the tokens stand in shared memory.  Bound by reading the weights once.  No tensor maps, barriers or
-// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 in place of int8_few_kernel 11.8 -> see the launch's comment.
+// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 10.9 us where int8_few_kernel took 11.8 (a launch by itself 2.3,
+// reading the weights at the copy rate 6.9).  Four tokens took 16.0 this way, 12.0 that way: each is read from shared memory as often as the weights from memory.
 constexpr int kInt8Vec = 8;
 struct Int8VecParams {
     const signed char *q, *w;               // rows of w on 16-byte boundaries

@@ -125,10 +125,14 @@ int check(const bmgd_quantized_linear_args* a, bool pointers) {
     if (!pointers || a->rows == 0) return BMGD_OK;
     if (!a->codes || !a->scale || !a->weight || !a->weight_scale || !a->y) return BMGD_ERR_ARG;
     if ((uintptr_t)a->scale % 4 || (uintptr_t)a->weight_scale % 4 || (uintptr_t)a->bias % 4 || (uintptr_t)a->y % (a->type == BMGD_TYPE_F32 ? 4 : 2)) return BMGD_ERR_ARG;
+    const uintptr_t y = (uintptr_t)a->y, end = y + (uintptr_t)(((a->rows - 1) * a->ld_y + a->outputs) * (a->type == BMGD_TYPE_F32 ? 4 : 2));
+    const uintptr_t q = (uintptr_t)a->codes, w = (uintptr_t)a->weight;
+    if (q < end && y < q + (uintptr_t)((a->rows - 1) * a->ld_codes + a->inputs)) return BMGD_ERR_ARG;
+    if (w < end && y < w + (uintptr_t)((a->outputs - 1) * a->ld_weight + a->inputs)) return BMGD_ERR_ARG;
     return BMGD_OK;
 }
 
-// Up to four tokens: warps per SM so that the channels come out even, at least eight: 148 x W channels at a time.  (11008 channels: 15 warps, five each.)
+// One or two tokens: warps per SM so that the channels come out even, at least eight: 148 x W channels at a time.  (11008 channels: 15 warps, five each.)
 template <int M>
 int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
     int best = 8;
@@ -154,9 +158,9 @@ int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
     if (cudaLaunchKernelEx(&lc, fn, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
-// whether the form for one to four tokens takes it
+// whether the form for one or two tokens takes it
 bool few_enough(const bmgd_quantized_linear_args* a) {
-    return a->rows <= 4 && (uintptr_t)a->weight % 16 == 0 && (a->ld_weight % 16 == 0 || a->outputs == 1) && a->rows * ((a->inputs + 15) / 16 * 16) <= kVecBytes;
+    return a->rows <= 2 && (uintptr_t)a->weight % 16 == 0 && (a->ld_weight % 16 == 0 || a->outputs == 1) && a->rows * ((a->inputs + 15) / 16 * 16) <= kVecBytes;
 }
 
 // run = false: only counts the workspace
@@ -166,10 +170,7 @@ int product(const bmgd_quantized_linear_args* a, Space* space, bool run, const D
         if (!run) return BMGD_OK;
         const Int8VecParams V{reinterpret_cast<const signed char*>(a->codes), reinterpret_cast<const signed char*>(a->weight), a->scale, a->weight_scale, a->bias, a->y,
                               a->ld_codes, a->ld_weight, a->ld_y, a->outputs, a->inputs, a->type};
-        if (a->rows == 1) return launch_vec<1>(V, dev, s);
-        if (a->rows == 2) return launch_vec<2>(V, dev, s);
-        if (a->rows == 3) return launch_vec<3>(V, dev, s);
-        return launch_vec<4>(V, dev, s);
+        return a->rows == 1 ? launch_vec<1>(V, dev, s) : launch_vec<2>(V, dev, s);
     }
     Bytes* const operands[2] = {&q, &w};
     const int rc = align_operands(operands, space, run, s);
@@ -183,18 +184,22 @@ int product(const bmgd_quantized_linear_args* a, Space* space, bool run, const D
     P.vec = (uintptr_t)a->y % 16 == 0 && a->ld_y * eb % 16 == 0;
     P.fills = dev.fills; P.gave_up = dev.gave_up;
     P.timeout_ns = wait_bound(dev, P.K / kInt8BK);
-    // The rules of the 16-bit contractions: exchanged roles for few tokens and wherever tiles of 128 x 128 do not fill the GPU once,
-    // pairs of CTAs from 0.4 of their tiles per SM on.
-    const int64_t tiles = ((a->rows + 127) / 128) * ((a->outputs + 127ll) / 128);
-    if (a->rows <= 256 || tiles <= dev.sms) {
+    // Exchanged roles up to 64 tokens, and where tiles of 128 x 128 do not fill half the GPU; otherwise the tiles that take least turns, a turn of
+    // 128 x 128, of 256 x 192 and of 256 x 256 for a pair being as 0.30 to 0.33 to 0.38 (microseconds for 128 inputs).  Measured on 4096 -> 11008: 128 tokens
+    // 18.0 with exchanged roles, 14.4, 15.6, 17.3 with the three; 256: 23.7, 22.8, 16.0, 17.7; 512: 27.1 with the third, 24.0 with the second; 1024: 44.7, 38.5.
+    const int64_t small = ((a->rows + 127) / 128) * ((a->outputs + 127ll) / 128);
+    if (a->rows <= 64 || small * 2 < dev.sms) {
         const FewChoice c = choose_few(P, dev);
         if (c.rows == 16) return launch_few<16>(P, q, w, c.split, dev, s);
         if (c.rows == 32) return launch_few<32>(P, q, w, c.split, dev, s);
         if (c.rows == 64) return launch_few<64>(P, q, w, c.split, dev, s);
         return launch_few<128>(P, q, w, c.split, dev, s);
     }
-    const int64_t large = ((a->rows + 255) / 256) * ((a->outputs + 255ll) / 256);
-    return large * 5 >= dev.sms * 2 ? launch<2, 256>(P, q, w, dev, s) : launch<1, 128>(P, q, w, dev, s);
+    const int64_t pairs = dev.sms / 2, tall = (a->rows + 255) / 256;
+    auto turns = [](int64_t tiles, int64_t units) { return (double)((tiles + units - 1) / units); };
+    const double t128 = 0.30 * turns(small, dev.sms), t192 = 0.33 * turns(tall * ((a->outputs + 191ll) / 192), pairs), t256 = 0.38 * turns(tall * ((a->outputs + 255ll) / 256), pairs);
+    if (t128 <= t192 && t128 <= t256) return launch<1, 128>(P, q, w, dev, s);
+    return t192 <= t256 ? launch<2, 192>(P, q, w, dev, s) : launch<2, 256>(P, q, w, dev, s);
 }
 
 int run_product(const bmgd_quantized_linear_args* a, void* workspace, int64_t workspace_bytes, void* stream, unsigned fills = ~0u, unsigned long long budget_ns = 0) {

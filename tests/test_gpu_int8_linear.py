@@ -41,7 +41,7 @@ def check(q, qs, w, ws, bias=None, dtype=torch.bfloat16, **kw):
     return y
 
 
-# one to four tokens; a cluster's split and none; tiles of one CTA; tiles of CTA pairs; sizes that end inside pieces and tiles
+# one and two tokens; a cluster's split and none; tiles of one CTA; tiles of CTA pairs; sizes that end inside pieces and tiles
 SHAPES = [(1, 1, 1), (1, 16, 8), (1, 4096, 1371), (2, 777, 300), (3, 128, 1000), (4, 2000, 2501), (5, 40, 40), (16, 128, 128), (17, 1371, 2501),
           (29, 2048, 264), (64, 96, 4104), (100, 4096, 130), (129, 520, 129), (200, 1000, 1000), (257, 264, 5000), (300, 1024, 6000), (777, 500, 3001),
           (2304, 1040, 2824), (1025, 4112, 2050)]

@@ -98,6 +98,7 @@ def linear(**kw):
     dict(rows=-1), dict(rows=2 ** 31), dict(inputs=0), dict(inputs=131072, ld_codes=131072, ld_weight=131072), dict(outputs=0), dict(outputs=2 ** 24 + 1, ld_y=2 ** 25), dict(type=3), dict(reserved=1),
     dict(codes=0), dict(scale=0), dict(weight=0), dict(weight_scale=0), dict(y=0), dict(ld_codes=63), dict(ld_weight=63), dict(ld_y=31), dict(scale=PTR + 2),
     dict(weight_scale=PTR + 1), dict(bias=PTR + 2), dict(y=FAR + 1), dict(type=ops.TYPE_F32, y=FAR + 2),
+    dict(y=PTR), dict(y=PTR + 200), dict(y=2 * PTR + 1024), dict(y=2 * PTR - 100),
 ])
 def test_quantized_linear(kw):
     assert L.bmgd_quantized_linear(linear(**kw), PTR, 1 << 40, None) == binding.ERR_ARG
