@@ -21,90 +21,101 @@ bool overlap(const void* p, int64_t ld, int64_t pw, const void* q, int64_t lq, i
     return a < b + (uintptr_t)((rows - 1) * lq + qw) && b < a + (uintptr_t)((rows - 1) * ld + pw);
 }
 
-// Threads of a row of `count` pieces: a warp up to 64 (two each), then two pieces a thread up to 1024, four beyond.
+// Threads of a row of `count` pieces: a warp up to 64 (two each), then two pieces a thread up to 1024, four up to 2048, eight.
 struct Threads {
     int pieces, threads;  // of a thread; 32: a warp, eight rows to a block
 };
 Threads threads_for(int64_t count) {
     if (count <= 32) return {1, 32};
     if (count <= 64) return {2, 32};
-    const int nv = count <= 1024 ? 2 : 4;
+    const int nv = count <= 1024 ? 2 : count <= 2048 ? 4 : 8;
     return {nv, (int)((count + nv * 32 - 1) / (nv * 32)) * 32};
 }
-// Blocks that go through the rows: as many as the registers of an SM hold (64 a thread, with four pieces 128)
+// Blocks that go through the rows: as many as the registers of an SM hold (64 a thread, with four pieces 128), and a multiple of eight where they come
+// round again: eight rows on, every tensor's rows start at the same place within 16 bytes.
 unsigned flow_grid(const Threads& t, int64_t rows, int per_sm_threads) {
     if (t.threads == 32) return (unsigned)std::min<int64_t>((rows + 7) / 8, 148 * (per_sm_threads / 256));
-    return (unsigned)std::min<int64_t>(rows, 148 * std::max(1, per_sm_threads / t.threads));
+    const int64_t most = 148 * std::max(1, per_sm_threads / t.threads) / 8 * 8;
+    return (unsigned)std::min<int64_t>(rows, most);
 }
 
-template <typename T, bool RES, bool CODES>
+template <typename T, bool RES, bool CODES, bool ANY>
 int forward_flow(const NormParams& P, cudaStream_t s) {
-    const Threads t = threads_for(P.width / Piece<T>::kValues);
-    const unsigned grid = flow_grid(t, P.rows, t.pieces == 4 ? 512 : 1024);
-    if (t.threads == 32 && t.pieces == 1) norm_flow_kernel<T, 1, true, RES, CODES><<<grid, 256, 0, s>>>(P);
-    else if (t.threads == 32) norm_flow_kernel<T, 2, true, RES, CODES><<<grid, 256, 0, s>>>(P);
-    else if (t.pieces == 2) norm_flow_kernel<T, 2, false, RES, CODES><<<grid, t.threads, 0, s>>>(P);
-    else norm_flow_kernel<T, 4, false, RES, CODES><<<grid, t.threads, 0, s>>>(P);
+    const Threads t = threads_for((P.width + Piece<T>::kValues - 1) / Piece<T>::kValues);
+    const unsigned grid = flow_grid(t, P.rows, t.pieces >= 4 ? 512 : 1024);
+    if (t.threads == 32 && t.pieces == 1) norm_flow_kernel<T, 1, true, RES, CODES, ANY><<<grid, 256, 0, s>>>(P);
+    else if (t.threads == 32) norm_flow_kernel<T, 2, true, RES, CODES, ANY><<<grid, 256, 0, s>>>(P);
+    else if (t.pieces == 2) norm_flow_kernel<T, 2, false, RES, CODES, ANY><<<grid, t.threads, 0, s>>>(P);
+    else if (t.pieces == 4) norm_flow_kernel<T, 4, false, RES, CODES, ANY><<<grid, t.threads, 0, s>>>(P);
+    else norm_flow_kernel<T, 8, false, RES, CODES, ANY><<<grid, t.threads, 0, s>>>(P);
     return launched();
 }
-// Rows on 16-byte boundaries of up to 2048 pieces; rows on others, held in registers too: a warp to a row up to 128 pieces, then blocks of 256 and
-// 1024 threads; longer rows are read more than once.
+// Rows of up to 4096 pieces; longer ones are read more than once.
 template <typename T, bool CODES>
 int forward(const NormParams& P, bool aligned, cudaStream_t s) {
     const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
-    const unsigned rows = (unsigned)P.rows;
-    if (aligned && pieces <= 2048) return P.residual ? forward_flow<T, true, CODES>(P, s) : forward_flow<T, false, CODES>(P, s);
-    if (pieces <= 128) norm_row_kernel<T, 32, 4, CODES><<<(rows + 7) / 8, 256, 0, s>>>(P);
-    else if (pieces <= 512) norm_row_kernel<T, 128, 4, CODES><<<rows, 128, 0, s>>>(P);
-    else if (pieces <= 1024) norm_row_kernel<T, 256, 4, CODES><<<rows, 256, 0, s>>>(P);
-    else if (pieces <= 4096) norm_row_kernel<T, 1024, 4, CODES><<<rows, 1024, 0, s>>>(P);
-    else norm_long_kernel<T, CODES><<<rows, 1024, 0, s>>>(P);
-    return launched();
+    if (pieces > 4096) {
+        norm_long_kernel<T, CODES><<<(unsigned)P.rows, 1024, 0, s>>>(P);
+        return launched();
+    }
+    if (aligned) return P.residual ? forward_flow<T, true, CODES, false>(P, s) : forward_flow<T, false, CODES, false>(P, s);
+    return P.residual ? forward_flow<T, true, CODES, true>(P, s) : forward_flow<T, false, CODES, true>(P, s);
 }
 
-// How the backward pass divides a row: pieces of 16 bytes where every row of every tensor starts on such a boundary, else single values.
+// How the backward pass takes a row: in pieces of 16 bytes where every row of every tensor starts on such a boundary; on any boundary; long rows
+// in pieces or single values.
 struct BackShape {
-    int values;           // of a thread's piece
+    bool aligned;
     Threads of;           // threads 0: the form for long rows
     int blocks;
 };
 BackShape back_shape(const bmgd_rms_norm* a) {
-    const int ve = 16 / value_bytes(a->type);
+    const int eb = value_bytes(a->type), ve = 16 / eb;
     const uintptr_t low = (uintptr_t)a->total | (uintptr_t)a->dy | (uintptr_t)a->dtotal | (uintptr_t)a->dx |
-                          (uintptr_t)((a->ld_total | a->ld_dy | (a->dtotal ? a->ld_dtotal : 0) | a->ld_dx) * value_bytes(a->type));
+                          (uintptr_t)((a->ld_total | a->ld_dy | (a->dtotal ? a->ld_dtotal : 0) | a->ld_dx) * eb);
     BackShape b{};
-    b.values = low % 16 == 0 && a->width % ve == 0 ? ve : 1;
-    const int count = a->width / b.values;
-    b.of = threads_for(count);
-    if (count > (b.values == 1 ? 4096 : 2048)) b.of.threads = 0;
-    b.blocks = b.of.threads == 0 ? (int)std::min<int64_t>(a->rows, 148) : (int)flow_grid(b.of, a->rows, 512);
+    b.aligned = low % 16 == 0 && a->width % ve == 0;
+    const int pieces = (a->width + ve - 1) / ve;
+    if (pieces > 2048) {
+        b.blocks = (int)std::min<int64_t>(a->rows, 148);
+    } else {
+        b.of = threads_for(pieces);
+        b.blocks = (int)flow_grid(b.of, a->rows, 512);
+    }
     return b;
 }
 constexpr int kMostSums = 50 * 1024;  // columns whose sums fit shared memory
 template <typename T, int VE>
-int backward(const NormParams& P, const BackShape& b, cudaStream_t s) {
+int backward_long(const NormParams& P, unsigned grid, cudaStream_t s) {
+    if (!P.part || P.width > kMostSums) {
+        norm_back_long_kernel<T, VE, false><<<grid, 1024, 0, s>>>(P);
+        return launched();
+    }
+    Device dev{};
+    int rc = current_device(&dev);
+    static std::atomic<unsigned long long> allowed{0};
+    if (rc == BMGD_OK) rc = allow_smem(norm_back_long_kernel<T, VE, true>, kMostSums * 4, dev, allowed);
+    if (rc != BMGD_OK) return rc;
+    norm_back_long_kernel<T, VE, true><<<grid, 1024, (size_t)P.width * 4, s>>>(P);
+    return launched();
+}
+template <typename T, bool ANY>
+int backward_flow(const NormParams& P, const BackShape& b, cudaStream_t s) {
     const unsigned grid = (unsigned)b.blocks;
-    if (b.of.threads == 0) {
-        const int bytes = P.width * 4;
-        if (!P.part || P.width > kMostSums) {
-            norm_back_long_kernel<T, VE, false><<<grid, 1024, 0, s>>>(P);
-            return launched();
-        }
-        Device dev{};
-        int rc = current_device(&dev);
-        static std::atomic<unsigned long long> allowed{0};
-        if (rc == BMGD_OK) rc = allow_smem(norm_back_long_kernel<T, VE, true>, kMostSums * 4, dev, allowed);
-        if (rc != BMGD_OK) return rc;
-        norm_back_long_kernel<T, VE, true><<<grid, 1024, (size_t)bytes, s>>>(P);
-    } else if (b.of.threads == 32 && b.of.pieces == 1) norm_back_kernel<T, VE, 1, true><<<grid, 256, 0, s>>>(P);
-    else if (b.of.threads == 32) norm_back_kernel<T, VE, 2, true><<<grid, 256, 0, s>>>(P);
-    else if (b.of.pieces == 2) norm_back_kernel<T, VE, 2, false><<<grid, b.of.threads, 0, s>>>(P);
-    else norm_back_kernel<T, VE, 4, false><<<grid, b.of.threads, 0, s>>>(P);
+    if (b.of.threads == 32 && b.of.pieces == 1) norm_back_kernel<T, 1, true, ANY><<<grid, 256, 0, s>>>(P);
+    else if (b.of.threads == 32) norm_back_kernel<T, 2, true, ANY><<<grid, 256, 0, s>>>(P);
+    else if (b.of.pieces == 2) norm_back_kernel<T, 2, false, ANY><<<grid, b.of.threads, 0, s>>>(P);
+    else norm_back_kernel<T, 4, false, ANY><<<grid, b.of.threads, 0, s>>>(P);
     return launched();
 }
 template <typename T>
+int backward(const NormParams& P, const BackShape& b, cudaStream_t s) {
+    if (b.of.threads == 0) return b.aligned ? backward_long<T, Piece<T>::kValues>(P, (unsigned)b.blocks, s) : backward_long<T, 1>(P, (unsigned)b.blocks, s);
+    return b.aligned ? backward_flow<T, false>(P, b, s) : backward_flow<T, true>(P, b, s);
+}
+template <typename T>
 int backward_all(const NormParams& P, const BackShape& b, cudaStream_t s) {
-    const int rc = b.values == 1 ? backward<T, 1>(P, b, s) : backward<T, Piece<T>::kValues>(P, b, s);
+    const int rc = backward<T>(P, b, s);
     if (rc != BMGD_OK || !P.dweight) return rc;
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];

@@ -134,19 +134,44 @@ __device__ __forceinline__ V join_threads(V v, V (&cells)[32]) {
     return v;
 }
 
-// ---- forward, rows on 16-byte boundaries throughout: every thread has the same columns in every row, so that its weights stay in registers
+// ---- forward, rows held in registers: every thread has the same columns in every row that it meets, so that its weights stay in registers
 // (read anew for each row they took four times the shared-memory cycles of the row itself: 8192 x 4096 31.5 us), and blocks go through the
 // rows with the grid's stride, the next row under way while this one is summed up and written.  WARP: a warp to a row, eight rows to a block; otherwise
-// as many threads as NV pieces each need.
-template <typename T, int NV, bool WARP, bool RES, bool CODES>
-__global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_kernel(const __grid_constant__ NormParams P) {
+// as many threads as NV pieces each need.  ANY: rows that do not all start on 16-byte boundaries.  A block's rows are a multiple of eight apart (norm.cu sees to it), so
+// all of them start at the same place within 16 bytes, in each tensor: the values before the first boundary of x (`head`) and behind its last piece go one each to the first
+// threads, and tensors whose rows start elsewhere than x's are read and written value by value.
+template <typename T, bool ANY>
+struct Place {  // of a block's (a warp's) rows
+    int head, pieces, edges;
+    __device__ __forceinline__ Place(const T* x, int width) : head(0), pieces(width / Piece<T>::kValues), edges(0) {
+        if constexpr (ANY) {
+            const RowPieces<T> row(x, width);
+            head = row.head;
+            pieces = row.pieces;
+            edges = row.edges;
+        }
+    }
+    __device__ __forceinline__ int column(int piece) const { return head + piece * Piece<T>::kValues; }
+    __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + pieces * Piece<T>::kValues; }
+    __device__ __forceinline__ static uint4 load(const T* p) {
+        if constexpr (ANY) return load_piece(p);
+        else return __ldcs(reinterpret_cast<const uint4*>(p));
+    }
+    __device__ __forceinline__ static void store(T* p, const uint4& w, bool far) {
+        if constexpr (ANY) store_piece(p, w, far);
+        else store16(reinterpret_cast<uint4*>(p), w, far);
+    }
+};
+
+template <typename T, int NV, bool WARP, bool RES, bool CODES, bool ANY>
+__global__ void __launch_bounds__(WARP ? 256 : 512, NV >= 4 ? 1 : 2) norm_flow_kernel(const __grid_constant__ NormParams P) {
     constexpr int VE = Piece<T>::kValues;
+    constexpr bool kAhead = NV <= 4;  // (registers do not suffice for two rows of eight pieces, nor for their weights)
     typedef typename SquareSum<T>::type Sum;
     __shared__ __align__(16) Sum sums[2][32];
     __shared__ __align__(16) float tops[2][32];
     const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
     const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
-    const int count = P.width / VE;  // (VE divides it)
     if constexpr (!WARP) {
         for (int k = threadIdx.x; k < 64; k += blockDim.x) {
             (&sums[0][0])[k] = 0;
@@ -154,29 +179,42 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_k
         }
         __syncthreads();
     }
-    float w[NV][VE];
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-        if (tid + k * threads < count) load_weights<T>(P.weight, P.weight_f32, (tid + k * threads) * VE, w[k]);
-    uint4 nx[NV], nr[NV];
-    auto fetch = [&](long long i) {
-        const uint4* x = reinterpret_cast<const uint4*>(static_cast<const T*>(P.x) + i * P.ld_x);
-        const uint4* r = reinterpret_cast<const uint4*>(static_cast<const T*>(P.residual) + i * P.ld_residual);
+    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i >= P.rows) return;  // (a whole warp; otherwise there is a row for each block)
+    const Place<T, ANY> place(static_cast<const T*>(P.x) + i * P.ld_x, P.width);
+    const bool odd = ANY && tid < place.edges;
+    const int at = odd ? place.edge(tid) : 0;
+    float w[kAhead ? NV : 1][VE], edge_weight = odd ? load_weight<T>(P.weight, P.weight_f32, at) : 0.f;
+    if constexpr (kAhead) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (tid + k * threads < count) {
-                nx[k] = __ldcs(x + tid + k * threads);
-                if constexpr (RES) nr[k] = __ldcs(r + tid + k * threads);
+            if (tid + k * threads < place.pieces) load_weights<T>(P.weight, P.weight_f32, place.column(tid + k * threads), w[k]);
+    }
+    uint4 nx[NV], nr[RES ? NV : 1];
+    float next_edge = 0.f, next_residual = 0.f;
+    auto fetch = [&](long long row) {
+        const T* x = static_cast<const T*>(P.x) + row * P.ld_x;
+        const T* r = static_cast<const T*>(P.residual) + row * P.ld_residual;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * threads < place.pieces) {
+                nx[k] = place.load(x + place.column(tid + k * threads));
+                if constexpr (RES) nr[k] = place.load(r + place.column(tid + k * threads));
             }
+        if (odd) {
+            next_edge = to_f32(x[at]);
+            if constexpr (RES) next_residual = to_f32(r[at]);
+        }
     };
-    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (i < P.rows) fetch(i);
+    fetch(i);
     for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
         Sum sum = 0;
         uint4 v[NV];
+        float edge = next_edge;
+        T* total = static_cast<T*>(P.total) + i * P.ld_total;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (tid + k * threads >= count) continue;
+            if (tid + k * threads >= place.pieces) continue;
             float t[VE];
             v[k] = nx[k];
             unpack_piece<T>(v[k], t);
@@ -186,142 +224,63 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV == 4 ? 1 : 2) norm_flow_k
 #pragma unroll
                 for (int e = 0; e < VE; ++e) t[e] += u[e];
                 v[k] = pack_piece<T>(t);
-                store16(reinterpret_cast<uint4*>(static_cast<T*>(P.total) + i * P.ld_total) + tid + k * threads, v[k], P.far != 0);
+                place.store(total + place.column(tid + k * threads), v[k], P.far != 0);
                 unpack_piece<T>(v[k], t);
             }
 #pragma unroll
             for (int e = 0; e < VE; ++e) add_square(sum, t[e]);
         }
-        if (i + step < P.rows) fetch(i + step);
+        if (odd) {
+            if constexpr (RES) {
+                const T v1 = from_f32<T>(edge + next_residual);
+                total[at] = v1;
+                edge = to_f32(v1);
+            }
+            add_square(sum, edge);
+        }
+        if (kAhead && i + step < P.rows) fetch(i + step);
         const float s = root_factor(join_threads<WARP, kJoinSum>(sum, sums[turn]), P);
         if (P.rstd && tid == 0) P.rstd[i] = s;
+        edge = edge * s * edge_weight;
+        auto normed = [&](int k, float (&t)[VE]) {
+            if constexpr (!kAhead) load_weights<T>(P.weight, P.weight_f32, place.column(tid + k * threads), w[0]);
+            unpack_piece<T>(v[k], t);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[kAhead ? k : 0][e];
+        };
         if constexpr (!CODES) {
-            uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(P.y) + i * P.ld_y);
+            T* y = static_cast<T*>(P.y) + i * P.ld_y;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (tid + k * threads >= count) continue;
+                if (tid + k * threads >= place.pieces) continue;
                 float t[VE];
-                unpack_piece<T>(v[k], t);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[k][e];
-                store16(y + tid + k * threads, pack_piece<T>(t), P.far != 0);
+                normed(k, t);
+                place.store(y + place.column(tid + k * threads), pack_piece<T>(t), P.far != 0);
             }
+            if (odd) y[at] = from_f32<T>(edge);
         } else {
-            float top = 0.f;
+            float top = odd ? fabsf(edge) : 0.f;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (tid + k * threads >= count) continue;
+                if (tid + k * threads >= place.pieces) continue;
                 float t[VE];
-                unpack_piece<T>(v[k], t);
+                normed(k, t);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(t[e] * s * w[k][e]));
+                for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(t[e]));
             }
             const RowCodes rc(join_threads<WARP, kJoinMax>(top, tops[turn]));
             signed char* q = P.codes + i * P.ld_codes;
             if (tid == 0) P.scale[i] = rc.scale;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (tid + k * threads >= count) continue;
+                if (tid + k * threads >= place.pieces) continue;
                 float t[VE];
-                unpack_piece<T>(v[k], t);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) t[e] = t[e] * s * w[k][e];
-                store_codes<VE, true>(q + (tid + k * threads) * VE, rc, t);
+                normed(k, t);
+                store_codes<VE, !ANY>(q + place.column(tid + k * threads), rc, t);
             }
+            if (odd) q[at] = rc.code(edge);
         }
-    }
-}
-
-// ---- forward, rows on any boundary, held in registers: TH threads share a row (TH = 32: a warp, eight rows to a block), NV pieces each
-template <typename T, int TH, int NV, bool CODES>
-__global__ void __launch_bounds__(TH == 32 ? 256 : TH) norm_row_kernel(const __grid_constant__ NormParams P) {
-    constexpr int VE = Piece<T>::kValues;
-    __shared__ typename SquareSum<T>::type sums[TH / 32];
-    __shared__ float tops[TH / 32];
-    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (i >= P.rows) return;  // (a whole warp; otherwise the grid has exactly the rows)
-    const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
-    const T* r = P.residual ? static_cast<const T*>(P.residual) + i * P.ld_residual : nullptr;
-    T* total = static_cast<T*>(P.total) + i * P.ld_total;
-    const RowPieces<T> row(x, P.width);
-    uint4 w[NV];
-    typename SquareSum<T>::type sum = 0;
-    float t[VE], edge = 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-        if (tid + k * TH < row.pieces) w[k] = load_piece(x + row.column(tid + k * TH));
-    const bool odd = tid < row.edges;
-    const int at = row.edge(tid);
-    if (odd) edge = to_f32(x[at]);
-    if (r) {
-        uint4 v[NV];
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (tid + k * TH < row.pieces) v[k] = load_piece(r + row.column(tid + k * TH));
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tid + k * TH >= row.pieces) continue;
-            float u[VE];
-            unpack_piece<T>(w[k], t);
-            unpack_piece<T>(v[k], u);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) t[e] += u[e];
-            w[k] = pack_piece<T>(t);
-            store_piece(total + row.column(tid + k * TH), w[k]);
-        }
-        if (odd) {
-            const T v1 = from_f32<T>(edge + to_f32(r[at]));
-            total[at] = v1;
-            edge = to_f32(v1);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        if (tid + k * TH >= row.pieces) continue;
-        unpack_piece<T>(w[k], t);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) add_square(sum, t[e]);
-    }
-    add_square(sum, edge);
-    const float s = root_factor(join_row<TH, kJoinSum>(sum, sums), P);
-    if (P.rstd && tid == 0) P.rstd[i] = s;
-    if (odd) edge *= s * load_weight<T>(P.weight, P.weight_f32, at);
-    if constexpr (!CODES) {
-        T* y = static_cast<T*>(P.y) + i * P.ld_y;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tid + k * TH >= row.pieces) continue;
-            const int c = row.column(tid + k * TH);
-            float u[VE];
-            load_weights<T>(P.weight, P.weight_f32, c, u);
-            unpack_piece<T>(w[k], t);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) t[e] = t[e] * s * u[e];
-            store_piece(y + c, pack_piece<T>(t));
-        }
-        if (odd) y[at] = from_f32<T>(edge);
-    } else {
-        float v[NV][VE], top = odd ? fabsf(edge) : 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tid + k * TH >= row.pieces) continue;
-            float u[VE];
-            load_weights<T>(P.weight, P.weight_f32, row.column(tid + k * TH), u);
-            unpack_piece<T>(w[k], v[k]);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                v[k][e] = v[k][e] * s * u[e];
-                top = nan_max(top, fabsf(v[k][e]));
-            }
-        }
-        const RowCodes rc(join_row<TH, kJoinMax>(top, tops));
-        signed char* q = P.codes + i * P.ld_codes;
-        if (tid == 0) P.scale[i] = rc.scale;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (tid + k * TH < row.pieces) store_codes<VE>(q + row.column(tid + k * TH), rc, v[k]);
-        if (odd) q[at] = rc.code(edge);
+        if (!kAhead && i + step < P.rows) fetch(i + step);
     }
 }
 
@@ -397,9 +356,131 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__
     }
 }
 
-// ---- backward: blocks (TH = 32: of eight warps, a row each) go through the rows with the grid's stride, each thread adding up its
-// columns' share of dw in registers; norm_weight_kernel adds the blocks' sums in their order, so equal calls give equal bits.  The columns of a thread are the
-// same in every row, so they are pieces (VE values of 16 bytes) where all rows start on 16-byte boundaries, single values elsewhere.
+// ---- backward: as the forward pass, each thread adding up its columns' share of dw in registers; norm_weight_kernel adds the blocks' sums
+// in their order, so equal calls give equal bits.
+template <typename T, int NV, bool WARP, bool ANY>
+__global__ void __launch_bounds__(WARP ? 256 : 512, WARP ? 2 : 1) norm_back_kernel(const __grid_constant__ NormParams P) {
+    constexpr int VE = Piece<T>::kValues;
+    constexpr bool kAhead = NV <= 2;  // the next row is under way while this one is summed up (not where registers do not suffice)
+    __shared__ __align__(16) float cells[2][32];
+    __shared__ float joined[WARP ? 8 : 1][WARP ? 32 * NV * VE + 2 * VE : 1];
+    let_next_kernel_start();
+    const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
+    const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
+    if constexpr (!WARP) {
+        for (int k = threadIdx.x; k < 64; k += blockDim.x) (&cells[0][0])[k] = 0.f;
+        __syncthreads();
+    }
+    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    // (a warp without a row holds zeros for all columns)
+    const Place<T, ANY> place(static_cast<const T*>(P.x) + (i < P.rows ? i : 0) * P.ld_x, P.width);
+    const bool odd = ANY && tid < place.edges;
+    const int at = odd ? place.edge(tid) : 0;
+    float w[kAhead ? NV : 1][VE], dw[NV][VE] = {}, edge_weight = odd ? load_weight<T>(P.weight, P.weight_f32, at) : 0.f, edge_dw = 0.f;
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (tid + k * threads < place.pieces) load_weights<T>(P.weight, P.weight_f32, place.column(tid + k * threads), w[k]);
+    }
+    auto weights = [&](int k) -> float (&)[VE] {
+        if constexpr (kAhead) return w[k];
+        load_weights<T>(P.weight, P.weight_f32, place.column(tid + k * threads), w[0]);
+        return w[0];
+    };
+    uint4 na[NV], nb[NV], nd[NV];
+    float s = 0.f, ea = 0.f, eb = 0.f, ed = 0.f;
+    auto fetch = [&](long long row) {
+        const T* t = static_cast<const T*>(P.x) + row * P.ld_x;
+        const T* dy = static_cast<const T*>(P.dy) + row * P.ld_dy;
+        const T* dt = static_cast<const T*>(P.dtotal) + row * P.ld_dtotal;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = place.column(tid + k * threads);
+            if (tid + k * threads >= place.pieces) continue;
+            na[k] = place.load(t + c);
+            nb[k] = place.load(dy + c);
+            if (P.dtotal) nd[k] = place.load(dt + c);
+        }
+        if (odd) {
+            ea = to_f32(t[at]);
+            eb = to_f32(dy[at]);
+            if (P.dtotal) ed = to_f32(dt[at]);
+        }
+        s = __ldg(P.rstd + row);
+    };
+    if (kAhead && i < P.rows) fetch(i);
+    for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
+        if (!kAhead) fetch(i);
+        uint4 a[NV], b[NV], d[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) { a[k] = na[k]; b[k] = nb[k]; d[k] = nd[k]; }
+        const float si = s, a1 = ea, b1 = eb, d1 = ed;
+        if (kAhead && i + step < P.rows) fetch(i + step);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * threads >= place.pieces) continue;
+            float u[VE], v[VE];
+            unpack_piece<T>(a[k], u);
+            unpack_piece<T>(b[k], v);
+            float (&wk)[VE] = weights(k);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float p = v[e] * (u[e] * si);
+                sum = fmaf(p, wk[e], sum);
+                dw[k][e] += p;
+            }
+        }
+        if (odd) {
+            const float p = b1 * (a1 * si);
+            sum = fmaf(p, edge_weight, sum);
+            edge_dw += p;
+        }
+        const float mean = join_threads<WARP, kJoinSum>(sum, cells[turn]) * P.per_width;
+        T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (tid + k * threads >= place.pieces) continue;
+            float u[VE], v[VE];
+            unpack_piece<T>(a[k], u);
+            unpack_piece<T>(b[k], v);
+            float (&wk)[VE] = weights(k);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) v[e] = si * (v[e] * wk[e] - u[e] * si * mean);
+            if (P.dtotal) {
+                unpack_piece<T>(d[k], u);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) v[e] += u[e];
+            }
+            place.store(dx + place.column(tid + k * threads), pack_piece<T>(v), P.far != 0);
+        }
+        if (odd) {
+            const float v = si * (b1 * edge_weight - a1 * si * mean);
+            dx[at] = from_f32<T>(P.dtotal ? v + d1 : v);
+        }
+    }
+    if (!P.part) return;
+    float* part = P.part + (long long)blockIdx.x * P.width;
+    float* to = WARP ? joined[threadIdx.x >> 5] : part;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (tid + k * threads >= place.pieces) continue;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) to[place.column(tid + k * threads) + e] = dw[k][e];
+    }
+    if (odd) to[at] = edge_dw;
+    if constexpr (WARP) {  // the eight warps' sums, in their order
+        __syncthreads();
+        for (int c = threadIdx.x; c < P.width; c += 256) {
+            float v = joined[0][c];
+#pragma unroll
+            for (int g = 1; g < 8; ++g) v += joined[g][c];
+            part[c] = v;
+        }
+    }
+}
+
+// VE neighbouring values of a long row as they are held and moved: a piece, or one
 template <typename T, int VE>
 struct Columns;  // VE neighbouring values as they are held and moved
 template <typename T>
@@ -421,113 +502,6 @@ struct Columns {
     static __device__ __forceinline__ void store(T* p, const float (&x)[VE], bool far) { store16(reinterpret_cast<uint4*>(p), pack_piece<T>(x), far); }
     static __device__ __forceinline__ void weights(const void* w, int f32, int c, float (&x)[VE]) { load_weights<T>(w, f32, c, x); }
 };
-
-template <typename T, int VE, int NV, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : VE == 1 ? 1024 : 512, WARP ? 2 : 1) norm_back_kernel(const __grid_constant__ NormParams P) {
-    constexpr bool kAhead = NV <= 4 && NV * VE <= 16;  // the next row is under way while this one is summed up (not where registers do not suffice)
-    using Col = Columns<T, VE>;
-    __shared__ __align__(16) float cells[2][32];
-    __shared__ float joined[WARP ? 8 : 1][WARP ? 32 * NV * VE : 1];
-    let_next_kernel_start();
-    const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
-    const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
-    const int count = P.width / VE;  // (VE divides it)
-    if constexpr (!WARP) {
-        for (int k = threadIdx.x; k < 64; k += blockDim.x) (&cells[0][0])[k] = 0.f;
-        __syncthreads();
-    }
-    float w[kAhead ? NV : 1][VE], dw[NV][VE] = {};
-    if constexpr (kAhead) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (tid + k * threads < count) Col::weights(P.weight, P.weight_f32, (tid + k * threads) * VE, w[k]);
-    }
-    auto weights = [&](int k) -> float (&)[VE] {
-        if constexpr (kAhead) return w[k];
-        Col::weights(P.weight, P.weight_f32, (tid + k * threads) * VE, w[0]);
-        return w[0];
-    };
-    Col a[NV], b[NV], d[NV], na[NV], nb[NV], nd[NV];
-    float s = 0.f;
-    auto fetch = [&](long long i) {
-        const T* t = static_cast<const T*>(P.x) + i * P.ld_x;
-        const T* dy = static_cast<const T*>(P.dy) + i * P.ld_dy;
-        const T* dt = static_cast<const T*>(P.dtotal) + i * P.ld_dtotal;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = (tid + k * threads) * VE;
-            if (tid + k * threads >= count) continue;
-            na[k].load(t + c);
-            nb[k].load(dy + c);
-            if (P.dtotal) nd[k].load(dt + c);
-        }
-        s = __ldg(P.rstd + i);
-    };
-    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (kAhead && i < P.rows) fetch(i);
-    for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
-        if (!kAhead) fetch(i);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) { a[k] = na[k]; b[k] = nb[k]; d[k] = nd[k]; }
-        const float si = s;
-        if (kAhead && i + step < P.rows) fetch(i + step);
-        float sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tid + k * threads >= count) continue;
-            float u[VE], v[VE];
-            a[k].unpack(u);
-            b[k].unpack(v);
-            float (&wk)[VE] = weights(k);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float p = v[e] * (u[e] * si);
-                sum = fmaf(p, wk[e], sum);
-                dw[k][e] += p;
-            }
-        }
-        const float mean = join_threads<WARP, kJoinSum>(sum, cells[turn]) * P.per_width;
-        T* dx = static_cast<T*>(P.dx) + i * P.ld_dx;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tid + k * threads >= count) continue;
-            float u[VE], v[VE];
-            a[k].unpack(u);
-            b[k].unpack(v);
-            float (&wk)[VE] = weights(k);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) v[e] = si * (v[e] * wk[e] - u[e] * si * mean);
-            if (P.dtotal) {
-                d[k].unpack(u);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) v[e] += u[e];
-            }
-            Col::store(dx + (tid + k * threads) * VE, v, P.far != 0);
-        }
-    }
-    if (!P.part) return;
-    float* part = P.part + (long long)blockIdx.x * P.width;
-    if constexpr (WARP) {  // the eight warps' sums, in their order
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) joined[threadIdx.x >> 5][(tid + k * 32) * VE + e] = dw[k][e];
-        __syncthreads();
-        for (int c = threadIdx.x; c < P.width; c += 256) {
-            float v = joined[0][c];
-#pragma unroll
-            for (int g = 1; g < 8; ++g) v += joined[g][c];
-            part[c] = v;
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (tid + k * threads >= count) continue;
-#pragma unroll
-            for (int e = 0; e < VE; ++e) part[(tid + k * threads) * VE + e] = dw[k][e];
-        }
-    }
-}
 
 // longer rows: read twice (the second time from L2), the columns' sums kept in shared memory where they fit (SUMS), else in the block's part of the workspace; each is
 // only touched by the thread that adds to it
