@@ -157,33 +157,30 @@ int check_backward(const bmgd_rms_norm* a) {
 }
 
 // Up to 384 threads with two, four or six pieces: a row's values are held in fp32, and two blocks of four pieces a thread (85 registers) fit an SM.
-template <typename T, bool GATE>
+template <typename T, bool GATE, bool ANY>
 int codes_flow(const CodesParams& P, cudaStream_t s) {
-    const int64_t count = P.width / Piece<T>::kValues;
+    const int64_t count = (P.width + Piece<T>::kValues - 1) / Piece<T>::kValues;
     Threads t = threads_for(count);
     if (t.threads > 32) {
         t.pieces = count <= 768 ? 2 : count <= 1536 ? 4 : 6;
         t.threads = (int)((count + t.pieces * 32 - 1) / (t.pieces * 32)) * 32;
     }
     const unsigned grid = flow_grid(t, P.rows, t.pieces == 6 ? 384 : t.pieces == 4 ? 768 : 1024);
-    if (t.threads == 32 && t.pieces == 1) codes_flow_kernel<T, 1, true, GATE><<<grid, 256, 0, s>>>(P);
-    else if (t.threads == 32) codes_flow_kernel<T, 2, true, GATE><<<grid, 256, 0, s>>>(P);
-    else if (t.pieces == 2) codes_flow_kernel<T, 2, false, GATE><<<grid, t.threads, 0, s>>>(P);
-    else if (t.pieces == 4) codes_flow_kernel<T, 4, false, GATE><<<grid, t.threads, 0, s>>>(P);
-    else codes_flow_kernel<T, 6, false, GATE><<<grid, t.threads, 0, s>>>(P);
+    if (t.threads == 32 && t.pieces == 1) codes_flow_kernel<T, 1, true, GATE, ANY><<<grid, 256, 0, s>>>(P);
+    else if (t.threads == 32) codes_flow_kernel<T, 2, true, GATE, ANY><<<grid, 256, 0, s>>>(P);
+    else if (t.pieces == 2) codes_flow_kernel<T, 2, false, GATE, ANY><<<grid, t.threads, 0, s>>>(P);
+    else if (t.pieces == 4) codes_flow_kernel<T, 4, false, GATE, ANY><<<grid, t.threads, 0, s>>>(P);
+    else codes_flow_kernel<T, 6, false, GATE, ANY><<<grid, t.threads, 0, s>>>(P);
     return launched();
 }
 template <typename T>
 int codes(const CodesParams& P, bool aligned, cudaStream_t s) {
-    const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
-    const unsigned rows = (unsigned)P.rows;
-    if (aligned && pieces <= 2048) return P.gate ? codes_flow<T, true>(P, s) : codes_flow<T, false>(P, s);
-    if (pieces <= 128) codes_row_kernel<T, 32, 4><<<(rows + 7) / 8, 256, 0, s>>>(P);
-    else if (pieces <= 512) codes_row_kernel<T, 128, 4><<<rows, 128, 0, s>>>(P);
-    else if (pieces <= 1024) codes_row_kernel<T, 256, 4><<<rows, 256, 0, s>>>(P);
-    else if (pieces <= 4096) codes_row_kernel<T, 1024, 4><<<rows, 1024, 0, s>>>(P);
-    else codes_long_kernel<T><<<rows, 1024, 0, s>>>(P);
-    return launched();
+    if (((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16 > 6 * 384) {
+        codes_long_kernel<T><<<(unsigned)P.rows, 1024, 0, s>>>(P);
+        return launched();
+    }
+    if (aligned) return P.gate ? codes_flow<T, true, false>(P, s) : codes_flow<T, false, false>(P, s);
+    return P.gate ? codes_flow<T, true, true>(P, s) : codes_flow<T, false, true>(P, s);
 }
 
 template <typename T>

@@ -153,13 +153,14 @@ struct Place {  // of a block's (a warp's) rows
     }
     __device__ __forceinline__ int column(int piece) const { return head + piece * Piece<T>::kValues; }
     __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + pieces * Piece<T>::kValues; }
-    __device__ __forceinline__ static uint4 load(const T* p) {
-        if constexpr (ANY) return load_piece(p);
-        else return __ldcs(reinterpret_cast<const uint4*>(p));
+    // (counted in pieces, not values, where that is possible: 4096 x 11008 values behind the gate took 64 us otherwise, 50 so)
+    __device__ __forceinline__ uint4 load(const T* row, int piece) const {
+        if constexpr (ANY) return load_piece(row + column(piece));
+        else return __ldcs(reinterpret_cast<const uint4*>(row) + piece);
     }
-    __device__ __forceinline__ static void store(T* p, const uint4& w, bool far) {
-        if constexpr (ANY) store_piece(p, w, far);
-        else store16(reinterpret_cast<uint4*>(p), w, far);
+    __device__ __forceinline__ void store(T* row, int piece, const uint4& w, bool far) const {
+        if constexpr (ANY) store_piece(row + column(piece), w, far);
+        else store16(reinterpret_cast<uint4*>(row) + piece, w, far);
     }
 };
 
@@ -198,8 +199,8 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV >= 4 ? 1 : 2) norm_flow_k
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (tid + k * threads < place.pieces) {
-                nx[k] = place.load(x + place.column(tid + k * threads));
-                if constexpr (RES) nr[k] = place.load(r + place.column(tid + k * threads));
+                nx[k] = place.load(x, tid + k * threads);
+                if constexpr (RES) nr[k] = place.load(r, tid + k * threads);
             }
         if (odd) {
             next_edge = to_f32(x[at]);
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV >= 4 ? 1 : 2) norm_flow_k
 #pragma unroll
                 for (int e = 0; e < VE; ++e) t[e] += u[e];
                 v[k] = pack_piece<T>(t);
-                place.store(total + place.column(tid + k * threads), v[k], P.far != 0);
+                place.store(total, tid + k * threads, v[k], P.far != 0);
                 unpack_piece<T>(v[k], t);
             }
 #pragma unroll
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV >= 4 ? 1 : 2) norm_flow_k
                 if (tid + k * threads >= place.pieces) continue;
                 float t[VE];
                 normed(k, t);
-                place.store(y + place.column(tid + k * threads), pack_piece<T>(t), P.far != 0);
+                place.store(y, tid + k * threads, pack_piece<T>(t), P.far != 0);
             }
             if (odd) y[at] = from_f32<T>(edge);
         } else {
@@ -395,11 +396,10 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, WARP ? 2 : 1) norm_back_kern
         const T* dt = static_cast<const T*>(P.dtotal) + row * P.ld_dtotal;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int c = place.column(tid + k * threads);
             if (tid + k * threads >= place.pieces) continue;
-            na[k] = place.load(t + c);
-            nb[k] = place.load(dy + c);
-            if (P.dtotal) nd[k] = place.load(dt + c);
+            na[k] = place.load(t, tid + k * threads);
+            nb[k] = place.load(dy, tid + k * threads);
+            if (P.dtotal) nd[k] = place.load(dt, tid + k * threads);
         }
         if (odd) {
             ea = to_f32(t[at]);
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, WARP ? 2 : 1) norm_back_kern
 #pragma unroll
                 for (int e = 0; e < VE; ++e) v[e] += u[e];
             }
-            place.store(dx + place.column(tid + k * threads), pack_piece<T>(v), P.far != 0);
+            place.store(dx, tid + k * threads, pack_piece<T>(v), P.far != 0);
         }
         if (odd) {
             const float v = si * (b1 * edge_weight - a1 * si * mean);
@@ -653,36 +653,42 @@ __device__ __forceinline__ float gated_one(const CodesParams& P, T x, const T* g
     }
     return h[0];
 }
-// rows on 16-byte boundaries throughout: as norm_flow_kernel
-template <typename T, int NV, bool WARP, bool GATE>
+// as norm_flow_kernel
+template <typename T, int NV, bool WARP, bool GATE, bool ANY>
 __global__ void __launch_bounds__(WARP ? 256 : 384, NV == 6 ? 1 : 2) codes_flow_kernel(const __grid_constant__ CodesParams P) {
     constexpr int VE = Piece<T>::kValues;
     __shared__ __align__(16) float cells[2][32];
     const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
     const long long step = (long long)gridDim.x * (WARP ? 8 : 1);
-    const int count = P.width / VE;  // (VE divides it)
     if constexpr (!WARP) {
         for (int k = threadIdx.x; k < 64; k += blockDim.x) (&cells[0][0])[k] = 0.f;
         __syncthreads();
     }
-    uint4 nx[NV], ng[NV];
-    auto fetch = [&](long long i) {
-        const uint4* x = reinterpret_cast<const uint4*>(static_cast<const T*>(P.x) + i * P.ld_x);
-        const uint4* g = reinterpret_cast<const uint4*>(static_cast<const T*>(P.gate) + i * P.ld_gate);
+    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (i >= P.rows) return;  // (a whole warp; otherwise there is a row for each block)
+    const Place<T, ANY> place(static_cast<const T*>(P.x) + i * P.ld_x, P.width);
+    const bool odd = ANY && tid < place.edges;
+    const int at = odd ? place.edge(tid) : 0;
+    uint4 nx[NV], ng[GATE ? NV : 1];
+    float next_edge = 0.f;
+    auto fetch = [&](long long row) {
+        const T* x = static_cast<const T*>(P.x) + row * P.ld_x;
+        const T* g = static_cast<const T*>(P.gate) + row * P.ld_gate;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (tid + k * threads < count) {
-                nx[k] = __ldcs(x + tid + k * threads);
-                if constexpr (GATE) ng[k] = __ldcs(g + tid + k * threads);
+            if (tid + k * threads < place.pieces) {
+                nx[k] = place.load(x, tid + k * threads);
+                if constexpr (GATE) ng[k] = place.load(g, tid + k * threads);
             }
+        if (odd) next_edge = gated_one(P, x[at], g + at);
     };
-    long long i = WARP ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (i < P.rows) fetch(i);
+    fetch(i);
     for (int turn = 0; i < P.rows; i += step, turn ^= 1) {
-        float h[NV][VE], top = 0.f;
+        const float edge = next_edge;
+        float h[NV][VE], top = fabsf(edge);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (tid + k * threads >= count) continue;
+            if (tid + k * threads >= place.pieces) continue;
             unpack_piece<T>(nx[k], h[k]);
             if constexpr (GATE) {
                 float u[VE];
@@ -698,48 +704,11 @@ __global__ void __launch_bounds__(WARP ? 256 : 384, NV == 6 ? 1 : 2) codes_flow_
         if (tid == 0) P.scale[i] = rc.scale;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (tid + k * threads < count) store_codes<VE, true>(q + (tid + k * threads) * VE, rc, h[k]);
+            if (tid + k * threads < place.pieces) store_codes<VE, !ANY>(q + place.column(tid + k * threads), rc, h[k]);
+        if (odd) q[at] = rc.code(edge);
     }
 }
-
-// rows on any boundary
-template <typename T, int TH, int NV>
-__global__ void __launch_bounds__(TH == 32 ? 256 : TH) codes_row_kernel(const __grid_constant__ CodesParams P) {
-    constexpr int VE = Piece<T>::kValues;
-    __shared__ float cells[TH / 32];
-    const int tid = TH == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const long long i = TH == 32 ? blockIdx.x * 8ll + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (i >= P.rows) return;
-    const T* x = static_cast<const T*>(P.x) + i * P.ld_x;
-    const T* g = static_cast<const T*>(P.gate) + i * P.ld_gate;
-    const RowPieces<T> row(x, P.width);
-    uint4 w[NV], v[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        if (tid + k * TH >= row.pieces) continue;
-        w[k] = load_piece(x + row.column(tid + k * TH));
-        if (P.gate) v[k] = load_piece(g + row.column(tid + k * TH));
-    }
-    const bool odd = tid < row.edges;
-    const int at = row.edge(tid);
-    float edge = 0.f;
-    if (odd) edge = gated_one(P, x[at], g + at);
-    float h[NV][VE], top = fabsf(edge);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        if (tid + k * TH >= row.pieces) continue;
-        gated_piece<T>(P, w[k], v[k], h[k]);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) top = nan_max(top, fabsf(h[k][e]));
-    }
-    const RowCodes rc(join_row<TH, kJoinMax>(top, cells));
-    signed char* q = P.codes + i * P.ld_codes;
-    if (tid == 0) P.scale[i] = rc.scale;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-        if (tid + k * TH < row.pieces) store_codes<VE>(q + row.column(tid + k * TH), rc, h[k]);
-    if (odd) q[at] = rc.code(edge);
-}
+// rows of any length, read twice
 template <typename T>
 __global__ void __launch_bounds__(1024) codes_long_kernel(const __grid_constant__ CodesParams P) {
     constexpr int VE = Piece<T>::kValues, TH = 1024;
