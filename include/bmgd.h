@@ -414,8 +414,18 @@ int bmgd_rms_norm_workspace_bytes(const bmgd_rms_norm* a, int64_t* bytes);
 int bmgd_rms_norm_backward(const bmgd_rms_norm* a, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Rows of x, or with a gate of act(gate) * x in fp32, in 8 bits: codes and scale [rows] as above. */
-int bmgd_quantize_rows(const void* dev_x, int64_t ld_x, const void* dev_gate, int64_t ld_gate, int64_t rows, int32_t width, int32_t type,
-                       int32_t activation, int8_t* dev_codes, int64_t ld_codes, float* dev_scale, void* stream);
+typedef struct bmgd_quantize_rows_args {
+    int64_t rows;                        /* 0 to 2^31 - 1 */
+    int32_t width;                       /* 1 to 2^24 */
+    int32_t type, activation;            /* of x and gate; BMGD_ACT_* */
+    int32_t reserved;                    /* must be zero */
+    const void* x;
+    const void* gate;                    /* NULL: none */
+    int8_t* codes;
+    float* scale;
+    int64_t ld_x, ld_gate, ld_codes;
+} bmgd_quantize_rows_args;
+int bmgd_quantize_rows(const bmgd_quantize_rows_args* a, void* stream);
 /* Weights [inputs][outputs] as codes [outputs][inputs] with a scale for each output, as bmgd_quantized_linear reads them. */
 int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_t outputs, int32_t type, int8_t* dev_codes,
                          int64_t ld_codes, float* dev_scale, void* stream);
@@ -465,11 +475,22 @@ int bmgd_log_probs_backward(const bmgd_log_probs_args* a, void* stream);
 
 /* Dropout: y = residual (NULL: 0) + x * 65536 / (65536 - k) where value j (counted row by row) is kept, k = rate * 65536 to the
  * nearest.  Value 8 b + e is kept where number e of block b is at least k: the eight numbers of 16 bits are the words, low half
- * first, of Philox4x32-10 with counter (b, b >> 32, *dev_step, 0x44524F50 + layer) and key seed.  dev_step (low 32 bits of an int64 in device
- * memory; NULL: 0) lets a captured call draw anew each time, as the count in an update's control words does.  The gradient of x is the same
- * call on the gradient of y without a residual.  y may be x or the residual itself.  rate from 0 to below 1 - 2^-17, layer from 0 to 65,535. */
-int bmgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int64_t ld_residual, int64_t rows, int64_t width, int32_t type,
-                 double rate, uint64_t seed, const int64_t* dev_step, int32_t layer, void* dev_y, int64_t ld_y, void* stream);
+ * first, of Philox4x32-10 with counter (b, b >> 32, *step, 0x44524F50 + layer) and key seed.  The gradient of x is the same call on the gradient
+ * of y without a residual.  y may be x or the residual itself, value for value; it overlaps them in no other way. */
+typedef struct bmgd_dropout_args {
+    int64_t rows, width;                 /* 0 to 2^31 - 1, 1 to 2^40 */
+    int32_t type;
+    int32_t layer;                       /* 0 to 65,535 */
+    double rate;                         /* 0 to below 1 - 2^-17 */
+    uint64_t seed;
+    const int64_t* step;                 /* low 32 bits of a word in device memory, NULL: 0; lets a captured call draw anew each time, as the
+                                            count in an update's control words does */
+    const void* x;
+    const void* residual;
+    void* y;
+    int64_t ld_x, ld_residual, ld_y;
+} bmgd_dropout_args;
+int bmgd_dropout(const bmgd_dropout_args* a, void* stream);
 
 /* Wait for `stream` and report, once, BMGD_ERR_TIMEOUT if a device-side wait of a gated-block or 8-bit product kernel on the current device
  * gave up since the last report (to whichever stream's caller asks first; none is lost).  What that call had not

@@ -132,13 +132,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.bmgd_rms_norm_forward.argtypes = [vp, vp]
     L.bmgd_rms_norm_workspace_bytes.argtypes = [vp, P(i64)]
     L.bmgd_rms_norm_backward.argtypes = [vp, vp, i64, vp]
-    L.bmgd_quantize_rows.argtypes = [vp, i64, vp, i64, i64, i32, i32, i32, vp, i64, vp, vp]
+    L.bmgd_quantize_rows.argtypes = [vp, vp]
     L.bmgd_quantize_weight.argtypes = [vp, i64, i32, i32, i32, vp, i64, vp, vp]
     L.bmgd_quantized_linear_workspace_bytes.argtypes = [vp, P(i64)]
     L.bmgd_quantized_linear.argtypes = [vp, vp, i64, vp]
     L.bmgd_log_probs.argtypes = [vp, vp]
     L.bmgd_log_probs_backward.argtypes = [vp, vp]
-    L.bmgd_dropout.argtypes = [vp, i64, vp, i64, i64, i64, i32, dbl, u64, vp, i32, vp, i64, vp]
+    L.bmgd_dropout.argtypes = [vp, vp]
     L.bmgd_debug_quantized_linear_timeout.argtypes = [vp, vp, i64, i32, dbl, vp]
     for name in EXPORTS:
         if getattr(L, name).restype is None or name in ("bmgd_strerror",):

@@ -260,22 +260,21 @@ int bmgd_rms_norm_backward(const bmgd_rms_norm* a, void* workspace, int64_t work
     return backward_all<__half>(P, b, s);
 }
 
-int bmgd_quantize_rows(const void* dev_x, int64_t ld_x, const void* dev_gate, int64_t ld_gate, int64_t rows, int32_t width, int32_t type,
-                       int32_t activation, int8_t* dev_codes, int64_t ld_codes, float* dev_scale, void* stream) {
-    if (rows < 0 || rows > 0x7FFFFFFFll || width < 1 || width > (1 << 24) || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
-    if (activation < BMGD_ACT_SILU || activation > BMGD_ACT_SIGMOID) return BMGD_ERR_ARG;
-    if (rows == 0) return BMGD_OK;
-    const int eb = value_bytes(type);
-    if (!dev_x || !dev_codes || !dev_scale || ld_x < width || ld_codes < width || (dev_gate && ld_gate < width)) return BMGD_ERR_ARG;
-    if (off(dev_x, eb) || off(dev_gate, eb) || off(dev_scale, 4)) return BMGD_ERR_ARG;
-    const int64_t w = (int64_t)width * eb;
-    if (overlap(dev_codes, ld_codes, width, dev_x, ld_x * eb, w, rows) ||
-        (dev_gate && overlap(dev_codes, ld_codes, width, dev_gate, ld_gate * eb, w, rows))) return BMGD_ERR_ARG;
-    CodesParams P{dev_x, dev_gate, reinterpret_cast<signed char*>(dev_codes), dev_scale, ld_x, ld_gate, ld_codes, rows, width, activation};
+int bmgd_quantize_rows(const bmgd_quantize_rows_args* a, void* stream) {
+    if (!a || a->rows < 0 || a->rows > 0x7FFFFFFFll || a->width < 1 || a->width > (1 << 24) || a->type < BMGD_TYPE_F32 || a->type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
+    if (a->activation < BMGD_ACT_SILU || a->activation > BMGD_ACT_SIGMOID || a->reserved != 0) return BMGD_ERR_ARG;
+    if (a->rows == 0) return BMGD_OK;
+    const int eb = value_bytes(a->type);
+    if (!a->x || !a->codes || !a->scale || a->ld_x < a->width || a->ld_codes < a->width || (a->gate && a->ld_gate < a->width)) return BMGD_ERR_ARG;
+    if (off(a->x, eb) || off(a->gate, eb) || off(a->scale, 4)) return BMGD_ERR_ARG;
+    const int64_t w = (int64_t)a->width * eb;
+    if (overlap(a->codes, a->ld_codes, a->width, a->x, a->ld_x * eb, w, a->rows) ||
+        (a->gate && overlap(a->codes, a->ld_codes, a->width, a->gate, a->ld_gate * eb, w, a->rows))) return BMGD_ERR_ARG;
+    const CodesParams P{a->x, a->gate, reinterpret_cast<signed char*>(a->codes), a->scale, a->ld_x, a->ld_gate, a->ld_codes, a->rows, a->width, a->activation};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool aligned = w % 16 == 0 && on16(dev_x, ld_x * eb) && on16(dev_gate, dev_gate ? ld_gate * eb : 0) && on16(dev_codes, ld_codes);
-    if (type == BMGD_TYPE_F32) return codes<float>(P, aligned, s);
-    if (type == BMGD_TYPE_BF16) return codes<__nv_bfloat16>(P, aligned, s);
+    const bool aligned = w % 16 == 0 && on16(a->x, a->ld_x * eb) && on16(a->gate, a->gate ? a->ld_gate * eb : 0) && on16(a->codes, a->ld_codes);
+    if (a->type == BMGD_TYPE_F32) return codes<float>(P, aligned, s);
+    if (a->type == BMGD_TYPE_BF16) return codes<__nv_bfloat16>(P, aligned, s);
     return codes<__half>(P, aligned, s);
 }
 

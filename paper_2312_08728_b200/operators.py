@@ -130,7 +130,7 @@ def _like(t: torch.Tensor, ld: int) -> torch.Tensor:
 
 
 def _device_of(t: torch.Tensor, name: str) -> torch.device:
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor; there is no CPU path")
     return t.device
 
@@ -442,6 +442,10 @@ def rms_norm_backward(dy: torch.Tensor, total: torch.Tensor, weight: Optional[to
     return dx, dweight
 
 
+# bmgd_quantize_rows_args: rows; width, type, activation, reserved; x, gate, codes, scale; ld_x, ld_gate, ld_codes
+_QUANTIZE_ROWS = struct.Struct("=q4i4Q3q")
+
+
 def quantize_rows(x: torch.Tensor, gate: Optional[torch.Tensor] = None, activation: int = ACT_SILU,
                   stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(codes, scale) of the rows of x [rows, width], or with a gate of the same size and type those of act(gate) * x: int8 with
@@ -463,8 +467,9 @@ def quantize_rows(x: torch.Tensor, gate: Optional[torch.Tensor] = None, activati
     with place:
         codes, scale = _codes_of(n, d), _one_per_row(n)
         if n > 0:
-            _status(L.bmgd_quantize_rows(x.data_ptr(), ld_x, gate.data_ptr() if gate is not None else None, ld_g, n, d, code, activation,
-                                         codes.data_ptr(), (d + 15) // 16 * 16, scale.data_ptr(), _current(device)), "bmgd_quantize_rows")
+            _status(L.bmgd_quantize_rows(_QUANTIZE_ROWS.pack(n, d, code, activation, 0, x.data_ptr(), gate.data_ptr() if gate is not None else 0,
+                                                             codes.data_ptr(), scale.data_ptr(), ld_x, ld_g, (d + 15) // 16 * 16), _current(device)),
+                    "bmgd_quantize_rows")
     _hand(stream, device, (codes, scale))
     return codes, scale
 
@@ -595,6 +600,10 @@ def log_probs_backward(dlogprob: Optional[torch.Tensor], dentropy: Optional[torc
 
 # ---------------------------------------------------------------- dropout
 
+# bmgd_dropout_args: rows, width; type, layer; rate; seed; step; x, residual, y; ld_x, ld_residual, ld_y
+_DROPOUT = struct.Struct("=2q2id5Q3q")
+
+
 def dropout(x: torch.Tensor, rate: float, seed: int, layer: int = 0, step: Optional[torch.Tensor] = None,
             residual: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """x [rows, width] with a share `rate` of its values dropped and the others divided by what is kept, plus the residual.
@@ -622,8 +631,8 @@ def dropout(x: torch.Tensor, rate: float, seed: int, layer: int = 0, step: Optio
     with place:
         y = _rows_of(n, d, x.dtype)
         if n > 0:
-            _status(L.bmgd_dropout(x.data_ptr(), ld_x, residual.data_ptr() if residual is not None else None, ld_r, n, d, code, float(rate),
-                                   int(seed) & 0xFFFFFFFFFFFFFFFF, at_step or None, layer, y.data_ptr(), d, _current(device)), "bmgd_dropout")
+            _status(L.bmgd_dropout(_DROPOUT.pack(n, d, code, layer, rate, int(seed) & 0xFFFFFFFFFFFFFFFF, at_step, x.data_ptr(),
+                                                 residual.data_ptr() if residual is not None else 0, y.data_ptr(), ld_x, ld_r, d), _current(device)), "bmgd_dropout")
     _hand(stream, device, (y,))
     return y
 

@@ -129,10 +129,12 @@ def test_in_place():
         want = ops.dropout(x[:, :d], 0.3, 4, residual=r[:, :d])
         for into in (x.clone(), r.clone()):
             a, b = (into, r) if torch.equal(into, x) else (x, into)
-            assert L.bmgd_dropout(a.data_ptr(), ld, b.data_ptr(), ld, n, d, ops.TYPE_BF16, 0.3, 4, None, 0, into.data_ptr(), ld, s) == 0
+            args = ops._DROPOUT.pack(n, d, ops.TYPE_BF16, 0, 0.3, 4, 0, a.data_ptr(), b.data_ptr(), into.data_ptr(), ld, ld, ld)
+            assert L.bmgd_dropout(args, s) == 0
             torch.cuda.synchronize()
             assert torch.equal(into[:, :d], want)
-        assert L.bmgd_dropout(x.data_ptr(), ld, None, 0, n, d, ops.TYPE_BF16, 0.3, 4, None, 0, x.data_ptr() + 2, ld, s) == binding.ERR_ARG
+        args = ops._DROPOUT.pack(n, d, ops.TYPE_BF16, 0, 0.3, 4, 0, x.data_ptr(), 0, x.data_ptr() + 2, ld, 0, ld)
+        assert L.bmgd_dropout(args, s) == binding.ERR_ARG
 
 
 def test_refusals():

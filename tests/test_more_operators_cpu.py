@@ -23,6 +23,7 @@ BACK = dict(x=0, y=0, total=PTR, rstd=PTR, dy=2 * PTR, dx=FAR, dweight=3 * PTR)
 
 
 def test_structs_match_the_header():
+    assert ops._QUANTIZE_ROWS.size == 80 and ops._DROPOUT.size == 96
     assert ops._RMS_NORM.size == 192 and ops._QUANTIZED_LINEAR.size == 96 and ops._LOG_PROBS.size == 120
 
 
@@ -63,17 +64,19 @@ def test_norm_workspace():
 
 
 @pytest.mark.parametrize("kw", [
-    dict(rows=-1), dict(rows=2 ** 31), dict(width=0), dict(width=2 ** 24 + 1), dict(type=3), dict(activation=4), dict(activation=-1), dict(x=None), dict(codes=None),
-    dict(scale=None), dict(ld_x=63), dict(ld_codes=63), dict(gate=2 * PTR, ld_gate=63), dict(x=PTR + 1), dict(gate=2 * PTR + 1), dict(scale=PTR + 2),
+    dict(rows=-1), dict(rows=2 ** 31), dict(width=0), dict(width=2 ** 24 + 1), dict(type=3), dict(activation=4), dict(activation=-1), dict(reserved=1), dict(x=0), dict(codes=0),
+    dict(scale=0), dict(ld_x=63), dict(ld_codes=63), dict(gate=2 * PTR, ld_gate=63), dict(x=PTR + 1), dict(gate=2 * PTR + 1), dict(scale=PTR + 2),
     dict(codes=PTR + 10), dict(gate=FAR + 5),
 ])
 def test_quantize_rows(kw):
-    v = dict(x=PTR, ld_x=64, gate=None, ld_gate=64, rows=4, width=64, type=ops.TYPE_BF16, activation=0, codes=FAR, ld_codes=64, scale=3 * PTR)
+    v = dict(rows=4, width=64, type=ops.TYPE_BF16, activation=0, reserved=0, x=PTR, gate=0, codes=FAR, scale=3 * PTR, ld_x=64, ld_gate=64, ld_codes=64)
+    assert set(kw) <= set(v)
     v.update(kw)
-    assert L.bmgd_quantize_rows(*v.values(), None) == binding.ERR_ARG
+    assert L.bmgd_quantize_rows(ops._QUANTIZE_ROWS.pack(*v.values()), None) == binding.ERR_ARG
     v.update(rows=0)
-    if not set(kw) & {"rows", "width", "type", "activation"}:
-        assert L.bmgd_quantize_rows(*v.values(), None) == 0
+    if not set(kw) & {"rows", "width", "type", "activation", "reserved"}:
+        assert L.bmgd_quantize_rows(ops._QUANTIZE_ROWS.pack(*v.values()), None) == 0
+    assert L.bmgd_quantize_rows(None, None) == binding.ERR_ARG
 
 
 @pytest.mark.parametrize("kw", [
@@ -154,17 +157,19 @@ def test_log_probs_of_nothing():
 
 @pytest.mark.parametrize("kw", [
     dict(rows=-1), dict(rows=2 ** 31), dict(width=0), dict(width=2 ** 40 + 1), dict(type=3), dict(rate=1.0), dict(rate=-0.1), dict(rate=float("nan")), dict(rate=1 - 2.0 ** -18),
-    dict(layer=-1), dict(layer=65536), dict(x=None), dict(y=None), dict(ld_x=63), dict(ld_y=63), dict(residual=2 * PTR, ld_residual=63), dict(x=PTR + 1), dict(y=FAR + 1),
+    dict(layer=-1), dict(layer=65536), dict(x=0), dict(y=0), dict(ld_x=63), dict(ld_y=63), dict(residual=2 * PTR, ld_residual=63), dict(x=PTR + 1), dict(y=FAR + 1),
     dict(residual=2 * PTR + 1), dict(step=PTR + 4), dict(y=PTR + 2), dict(y=PTR, ld_y=65), dict(residual=FAR + 2), dict(rows=2 ** 30, width=2 ** 31, ld_x=2 ** 31, ld_y=2 ** 31),
 ])
 def test_dropout(kw):
-    v = dict(x=PTR, ld_x=64, residual=None, ld_residual=64, rows=4, width=64, type=ops.TYPE_BF16, rate=0.1, seed=1, step=None, layer=0, y=FAR, ld_y=64)
+    v = dict(rows=4, width=64, type=ops.TYPE_BF16, layer=0, rate=0.1, seed=1, step=0, x=PTR, residual=0, y=FAR, ld_x=64, ld_residual=64, ld_y=64)
+    assert set(kw) <= set(v)
     v.update(kw)
-    assert L.bmgd_dropout(*v.values(), None) == binding.ERR_ARG
+    assert L.bmgd_dropout(ops._DROPOUT.pack(*v.values()), None) == binding.ERR_ARG
 
 
 def test_dropout_of_nothing():
-    assert L.bmgd_dropout(None, 64, None, 64, 0, 64, ops.TYPE_BF16, 0.1, 1, None, 0, None, 64, None) == 0
+    assert L.bmgd_dropout(ops._DROPOUT.pack(0, 64, ops.TYPE_BF16, 0, 0.1, 1, 0, 0, 0, 0, 64, 64, 64), None) == 0
+    assert L.bmgd_dropout(None, None) == binding.ERR_ARG
 
 
 @pytest.mark.parametrize("call", [
