@@ -477,11 +477,12 @@ __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __gr
 }
 
 // ---------------------------------------------------------------- one or two tokens
-// A warp to a channel, its row of weights read in batches of 32 x 8 pieces of 16 bytes, the next batch (or channel) under way while this
+// A warp to a channel, its row of weights read in batches of 32 x 4 pieces of 16 bytes, the next batch (or channel) under way while this
 // one is multiplied on the integer dot-product units; the tokens stand in shared memory.  Bound by reading the weights once.  No tensor maps, barriers or
-// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 10.9 us where int8_few_kernel took 11.8 (a launch by itself 2.3,
-// reading the weights at the copy rate 6.9).  Four tokens took 16.0 this way, 12.0 that way: each is read from shared memory as often as the weights from memory.
-constexpr int kInt8Vec = 8;
+// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 9.9 us where int8_few_kernel took 11.8 (a launch by itself 2.3,
+// reading the weights at the copy rate 6.9); in batches of 8 pieces with half as many warps 10.9.  Four tokens took 16.0 that way where int8_few_kernel
+// takes 12.0: each is read from shared memory as often as the weights from memory.
+constexpr int kInt8Vec = 4;
 struct Int8VecParams {
     const signed char *q, *w;               // rows of w on 16-byte boundaries
     const float *q_scale, *w_scale, *bias;
@@ -490,7 +491,7 @@ struct Int8VecParams {
     int N, K, type;
 };
 template <int M>
-__global__ void __launch_bounds__(768) int8_vec_kernel(const __grid_constant__ Int8VecParams P) {
+__global__ void __launch_bounds__(512, 2) int8_vec_kernel(const __grid_constant__ Int8VecParams P) {
     extern __shared__ uint4 int8_tokens[];  // [M][pieces], zeros behind the last value
     wait_for_previous_kernel();
     let_next_kernel_start();

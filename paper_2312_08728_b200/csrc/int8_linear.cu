@@ -91,7 +91,7 @@ FewChoice choose_few(const Int8Params& P, const Device& dev) {
     return best;
 }
 
-constexpr int kVecBytes = 200 * 1024;  // of tokens in shared memory
+constexpr int kVecBytes = 100 * 1024;  // of tokens in shared memory, for each of two blocks to an SM
 
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
 bool tma_ready(const Bytes& m) { return (uintptr_t)m.base % 16 == 0 && m.ld % 16 == 0; }
@@ -132,16 +132,18 @@ int check(const bmgd_quantized_linear_args* a, bool pointers) {
     return BMGD_OK;
 }
 
-// One or two tokens: warps per SM so that the channels come out even, at least eight: 148 x W channels at a time.  (11008 channels: 15 warps, five each.)
+// One or two tokens: two blocks to an SM, with as many warps each (8 to 16) as let the channels come out most evenly, 2 x 148 x W of them at a
+// time.  (11008 channels: 13 warps, three each; 4096: 14, one each.)
 template <int M>
 int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
+    const int blocks = 2 * dev.sms;
     int best = 8;
-    if (P.N <= dev.sms * 8) {
-        best = std::max(1, (P.N + dev.sms - 1) / dev.sms);
+    if (P.N <= blocks * 8) {
+        best = std::max(1, (P.N + blocks - 1) / blocks);
     } else {
         int64_t least = INT64_MAX;
-        for (int w = 8; w <= 24; ++w) {
-            const int64_t span = (int64_t)dev.sms * w, reached = (P.N + span - 1) / span * span;
+        for (int w = 8; w <= 16; ++w) {
+            const int64_t span = (int64_t)blocks * w, reached = (P.N + span - 1) / span * span;
             if (reached <= least) { least = reached; best = w; }
         }
     }
@@ -154,7 +156,7 @@ int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
     }
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
-    launch_config(&lc, at, dim3((unsigned)std::min((P.N + best - 1) / best, dev.sms)), best * 32, bytes, 1, s);
+    launch_config(&lc, at, dim3((unsigned)std::min((P.N + best - 1) / best, blocks)), best * 32, bytes, 1, s);
     if (cudaLaunchKernelEx(&lc, fn, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }

@@ -6,7 +6,7 @@
 //     8 bits:  a = max_c |y_c|,  scale = a / 127,  code_c = y_c (1 / a) 127 rounded to the nearest whole number
 //
 // The norm is that of the rounded sum: it is what the next block reads as its residual, what is kept for the backward pass, and so
-// the gradients are those of the values that were computed.  All sums are fp32.  What bounds it: memory, each value read and
+// the gradients are those of the values that were computed.  Sums are fp32, squares of fp32 rows 64 bits.  What bounds it: memory, each value read and
 // written once; rows are held in registers between the sum and its use.
 #pragma once
 #include <cstdint>

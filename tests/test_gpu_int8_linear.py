@@ -44,7 +44,7 @@ def check(q, qs, w, ws, bias=None, dtype=torch.bfloat16, **kw):
 # one and two tokens; a cluster's split and none; tiles of one CTA; tiles of CTA pairs; sizes that end inside pieces and tiles
 SHAPES = [(1, 1, 1), (1, 16, 8), (1, 4096, 1371), (2, 777, 300), (3, 128, 1000), (4, 2000, 2501), (5, 40, 40), (16, 128, 128), (17, 1371, 2501),
           (29, 2048, 264), (64, 96, 4104), (100, 4096, 130), (129, 520, 129), (200, 1000, 1000), (257, 264, 5000), (300, 1024, 6000), (777, 500, 3001),
-          (2304, 1040, 2824), (1025, 4112, 2050)]
+          (2304, 1040, 2824), (1025, 4112, 2050), (2048, 264, 2048), (1, 1040, 6000), (2, 4112, 2370)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "fp16", "fp32"])
@@ -152,7 +152,7 @@ def starve(job, fills, dtype=torch.bfloat16, budget_ms=5.0):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("fills", [0, 1, 8])
-@pytest.mark.parametrize("shape", [(3, 2048, 1376), (100, 128, 136), (700, 512, 2700), (2304, 1024, 2816)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("shape", [(3, 2048, 1376), (100, 128, 136), (700, 512, 2700), (2304, 1024, 2816), (2048, 1024, 2048)], ids=lambda s: "x".join(map(str, s)))
 def test_what_was_not_computed_is_nan(shape, fills, dtype):
     job = operands(*shape, seed=2)
     want = ops.int8_linear(*job, dtype=dtype)
