@@ -432,7 +432,7 @@ int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_
 
 /* Product in 8-bit integers: y = (codes weight^T) scale_i weight_scale_j + bias_j, codes [rows][inputs], weight
  * [outputs][inputs]; the sums are exact, the rest is fp32, rounded once to `type`.  Operands whose rows do not start on 16-byte
- * boundaries are copied into the workspace first.  y overlaps no operand. */
+ * boundaries are copied into the workspace first, unless the tokens or the tiles are few.  y overlaps no operand. */
 typedef struct bmgd_quantized_linear_args {
     int64_t rows;                        /* 0 to 2^31 - 256 */
     int32_t inputs, outputs;             /* 1 to 131,071 (sums of 32 bits) and 2^24 */
@@ -451,7 +451,8 @@ int bmgd_quantized_linear(const bmgd_quantized_linear_args* a, void* workspace, 
 
 /* Of each row of logits [rows][C]: the log probability of class y, the entropy, and the `top` most probable classes, in falling
  * order, equal logits by rising class, with their log probabilities.  A row whose y is outside [0, C) has log probability 0; one whose
- * logits are all -Inf has log probability and entropy 0 and alternatives -Inf; NaN and +Inf give NaN (NaN comes first among the alternatives). */
+ * logits are all -Inf has log probability and entropy 0 and alternatives -Inf; NaN and +Inf give NaN (NaN comes first among the alternatives).
+ * What is written overlaps neither the logits nor y nor anything else that is written. */
 typedef struct bmgd_log_probs_args {
     int64_t rows;                        /* 0 to 2^31 - 1 */
     int32_t C;                           /* 1 to 2^30 */

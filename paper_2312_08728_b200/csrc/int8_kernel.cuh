@@ -20,6 +20,8 @@ constexpr int kInt8None = (int)0x80000000u;  // no sum of up to 131,071 products
 
 struct Int8Params {
     CUtensorMap q, w;
+    const signed char *q_rows, *w_rows;     // the same memory, for rows on any boundary (int8_few_kernel)
+    long long ld_q, ld_w;
     const float *q_scale, *w_scale, *bias;  // bias: null for none
     void* out;
     long long ld_out, tiles;
@@ -364,8 +366,101 @@ __device__ __forceinline__ void int8_few_finish(const Int8Params& P, uint32_t su
     }
 }
 
-// Grid: S CTAs (one cluster) per tile; tiles_m and tiles_n count tiles of NR tokens and of 128 channels.
+// Stages filled by the block's own threads where the rows of an operand do not start on 16-byte boundaries.  A thread keeps to its pieces' rows and columns of
+// a stage, reads the two aligned pieces that hold each of its own and shifts them against one another.  They may reach into the neighbouring rows, never beyond the matrix:
+// its ends, and rows of fewer than 48 values, are read byte by byte.  With a copy of both operands in front of the kernel
+// instead: 29 x 1371 -> 2501 8.5 us and 3.5 more on the host, now 8.7; 60 x 4099 -> 4097 17.3, now 15.8; 16 x 11009 -> 4096 26.7, now 22.7 (with strides of 11008 13).
+// Pieces stand where TMA would put them (128-byte swizzle); rows and columns beyond the matrix are zeros.
+constexpr int kInt8Fillers = kInt8FewThreads - 32;
 template <int NR>
+struct Int8FewFill {
+    static constexpr int kPieces = (kInt8Part + NR) * 8, kEach = (kPieces + kInt8Fillers - 1) / kInt8Fillers, kBatch = kEach <= 7 ? kEach : (kEach + 1) / 2;
+    static_assert(kInt8Fillers % 8 == 0, "a thread keeps to its columns");
+    const signed char* row[kEach];  // at this thread's columns
+    unsigned some, first, last;     // a bit for each: not beyond the matrix; the matrix's first row, its last
+    int thread, c;
+
+    __device__ __forceinline__ static const signed char* place(const Int8Params& P, int f0, int r0, int i, int& r, int& rows) {  // of row i of a stage
+        const bool token = i >= kInt8Part;
+        r = token ? r0 + i - kInt8Part : f0 + i;
+        rows = token ? P.M : P.N;
+        return token ? P.q_rows + r * P.ld_q : P.w_rows + r * P.ld_w;
+    }
+    __device__ __forceinline__ void start(const Int8Params& P, int f0, int r0, int thread_) {
+        some = first = last = 0;
+        thread = thread_;
+        c = (thread & 7) * 16;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            int r, rows;
+            row[u] = place(P, f0, r0, (thread + u * kInt8Fillers) >> 3, r, rows) + c;
+            if (thread + u * kInt8Fillers >= kPieces || r >= rows) continue;
+            some |= 1u << u;
+            if (r == 0 || P.K < 48) first |= 1u << u;
+            if (r == rows - 1 || P.K < 48) last |= 1u << u;
+        }
+    }
+    // A stage's rows on their way to L2, two stages ahead (16 x 11009 -> 4096: 28 us to 24).  It reads nothing, so it may come before the wait for the kernel in front.
+    __device__ __forceinline__ void fetch(const Int8Params& P, int k) const {
+        if (c != 0 || k * kInt8BK >= P.K) return;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u)
+            if (some >> u & 1u) asm volatile("prefetch.global.L2 [%0];" ::"l"(row[u] + k * kInt8BK));
+    }
+    __device__ __forceinline__ static void put(uint32_t stage, int i, const uint32_t (&x)[4]) {
+        const int r = i >> 3;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + (uint32_t)(r * kInt8BK + (((i ^ r) & 7) << 4))), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+    }
+    __device__ __forceinline__ void operator()(const Int8Params& P, int f0, int r0, uint32_t stage, int k) const {
+        const int at = k * kInt8BK + c, count = P.K - at;  // values from here to the rows' ends
+        const unsigned here = count > 0 ? some : 0u, ends = here & ((at == 0 ? first : 0u) | (count < 32 ? last : 0u)), pieces = here & ~ends;
+#pragma unroll
+        for (int u0 = 0; u0 < kEach; u0 += kBatch) {
+            uint4 v[kBatch][2];
+#pragma unroll
+            for (int u = u0; u < min(kEach, u0 + kBatch); ++u) {
+                const uint4* two = reinterpret_cast<const uint4*>(row[u] + k * kInt8BK - ((uintptr_t)row[u] & 15u));
+#pragma unroll
+                for (int e = 0; e < 2; ++e) v[u - u0][e] = pieces >> u & 1u ? __ldg(two + e) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int u = u0; u < min(kEach, u0 + kBatch); ++u) {
+                const uint4 &l = v[u - u0][0], &h = v[u - u0][1];
+                const unsigned shift = (unsigned)((uintptr_t)row[u] & 15u);
+                const bool by8 = shift & 8u, by4 = shift & 4u;
+                const uint32_t w[6] = {by8 ? l.z : l.x, by8 ? l.w : l.y, by8 ? h.x : l.z, by8 ? h.y : l.w, by8 ? h.z : h.x, by8 ? h.w : h.y};
+                uint32_t y[5], x[4];
+#pragma unroll
+                for (int e = 0; e < 5; ++e) y[e] = by4 ? w[e + 1] : w[e];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = __funnelshift_r(y[e], y[e + 1], 8 * (shift & 3u));
+                    if (count < 16) x[e] &= count >= 4 * e + 4 ? ~0u : count <= 4 * e ? 0u : ~0u >> (32 - 8 * (count - 4 * e));
+                }
+                if (thread + u * kInt8Fillers < kPieces) put(stage, thread + u * kInt8Fillers, x);
+            }
+        }
+#pragma unroll 1
+        for (unsigned left = ends; left != 0; left &= left - 1) {
+            const int i = thread + (__ffs((int)left) - 1) * kInt8Fillers;
+            int r, rows;
+            const signed char* p = place(P, f0, r0, i >> 3, r, rows) + at;
+            uint32_t byte[16], x[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int b = 0; b < 16; ++b) byte[b] = b < count ? (uint32_t)(unsigned char)__ldg(p + b) : 0u;
+#pragma unroll
+            for (int b = 0; b < 16; ++b) x[b / 4] |= byte[b] << (8 * (b % 4));
+            put(stage, i, x);
+        }
+        fence_async_proxy();  // (the products read shared memory by the other way)
+    }
+};
+template <>
+struct Int8FewFill<0> {};
+
+// Grid: S CTAs (one cluster) per tile; tiles_m and tiles_n count tiles of NR tokens and of 128 channels.  ANY: rows on any boundary, filled by all
+// warps but the one that issues the products.
+template <int NR, bool ANY>
 __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __grid_constant__ Int8Params P, const int S) {
     using F = Int8FewShape<NR>;
     extern __shared__ unsigned char int8_smem[];
@@ -376,15 +471,25 @@ __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __gr
     const int f0 = tile / P.tiles_m * kInt8Part, r0 = tile % P.tiles_m * NR;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < F::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (int s = 0; s < F::kStages; ++s) { mbar_init(full + 8 * s, ANY ? kInt8Fillers / 32 : 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done, 1);
         fence_barrier_init();
     }
-    if (threadIdx.x == 32) {
+    if (!ANY && threadIdx.x == 32) {
         prefetch_map(&P.w);
         prefetch_map(&P.q);
     }
     if (warp == 2) ffn_tmem_alloc<1>(slot, F::kTmemCols);
+    const int steps = (P.K + kInt8BK - 1) / kInt8BK;
+    const int first = (int)((long long)steps * part / S), last = (int)((long long)steps * (part + 1) / S);
+    Int8FewFill<ANY ? NR : 0> fill;
+    if constexpr (ANY) {
+        fill.start(P, f0, r0, (int)threadIdx.x - (warp > 1 ? 32 : 0));
+        if (warp != 1) {
+            fill.fetch(P, first);
+            if (first + 1 < last) fill.fetch(P, first + 1);
+        }
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -393,12 +498,25 @@ __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __gr
     wait_for_previous_kernel();
     let_next_kernel_start();
 
-    const int steps = (P.K + kInt8BK - 1) / kInt8BK;
-    const int first = (int)((long long)steps * part / S), last = (int)((long long)steps * (part + 1) / S);
     FfnWait w{P.gave_up, P.timeout_ns, false};
-    if (warp == 0) {
+    const int fill_to = (int)min((long long)last, (long long)first + P.fills);
+    if (ANY && warp != 1) {
+        int s = 0;
+        uint32_t phase = 0;
+        for (int k = first; k < fill_to; ++k) {
+            ffn_wait(empty + 8 * s, phase ^ 1u, w);
+            w.aborted = __any_sync(0xFFFFFFFFu, w.aborted);
+            if (w.aborted) break;
+            if constexpr (ANY) {
+                if (k + 2 < fill_to) fill.fetch(P, k + 2);
+                fill(P, f0, r0, ring + s * F::kStage, k);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8 * s);
+            if (++s == F::kStages) { s = 0; phase ^= 1u; }
+        }
+    } else if (!ANY && warp == 0) {
         if (lane == 0) {
-            const int fill_to = (int)min((long long)last, (long long)first + P.fills);
             int s = 0;
             uint32_t phase = 0;
             for (int k = first; k < fill_to; ++k) {

@@ -48,15 +48,23 @@ int launch(Int8Params& P, const Bytes& q, const Bytes& w, const Device& dev, cud
     return BMGD_OK;
 }
 
-template <int NR>
+bool tma_ready(const Bytes& m) { return (uintptr_t)m.base % 16 == 0 && m.ld % 16 == 0; }
+
+template <int NR, bool ANY>
 int launch_few(Int8Params& P, const Bytes& q, const Bytes& w, int split, const Device& dev, cudaStream_t s) {
     using F = Int8FewShape<NR>;
-    int rc = make_map(q, NR, &P.q);
-    if (rc == BMGD_OK) rc = make_map(w, kInt8Part, &P.w);
+    int rc = BMGD_OK;
+    if constexpr (ANY) {
+        P.q_rows = static_cast<const signed char*>(q.base); P.ld_q = q.ld;
+        P.w_rows = static_cast<const signed char*>(w.base); P.ld_w = w.ld;
+    } else {
+        rc = make_map(q, NR, &P.q);
+        if (rc == BMGD_OK) rc = make_map(w, kInt8Part, &P.w);
+    }
     if (rc != BMGD_OK) return rc;
     P.tiles_m = (P.M + NR - 1) / NR;
     P.tiles_n = (P.N + kInt8Part - 1) / kInt8Part;
-    auto* fn = int8_few_kernel<NR>;
+    auto* fn = int8_few_kernel<NR, ANY>;
     static std::atomic<unsigned long long> allowed{0};
     rc = allow_smem(fn, F::kSmem, dev, allowed);
     if (rc != BMGD_OK) return rc;
@@ -68,11 +76,11 @@ int launch_few(Int8Params& P, const Bytes& q, const Bytes& w, int split, const D
 }
 
 // Tokens per tile and split of the contraction for the form with exchanged roles: the estimate of the 16-bit contractions, whose
-// stages have the same bytes.
+// stages have the same bytes.  any: stages filled by threads, about 1.2 us each, so that single ones are worth a CTA.
 struct FewChoice {
     int rows, split;
 };
-FewChoice choose_few(const Int8Params& P, const Device& dev) {
+FewChoice choose_few(const Int8Params& P, bool any, const Device& dev) {
     const int steps = (P.K + kInt8BK - 1) / kInt8BK;
     FewChoice best{16, 1};
     double least = 1e30;
@@ -81,9 +89,9 @@ FewChoice choose_few(const Int8Params& P, const Device& dev) {
         const int64_t tiles = (int64_t)((P.M + nr - 1) / nr) * ((P.N + kInt8Part - 1) / kInt8Part), slots = 2 * (int64_t)dev.sms;
         const double stage = 16384 + nr * 128, rows = (double)std::min(nr, P.M);
         for (int split : {1, 2, 3, 4, 8}) {
-            if (split > 1 && (tiles * split > slots || split * 2 > steps)) break;
+            if (split > 1 && (tiles * split > slots || split * (any ? 1 : 2) > steps)) break;
             const double turns = (double)((tiles * split + slots - 1) / slots);
-            const double copies = std::max(turns * ((steps + split - 1) / split) * stage / 80e3, (double)tiles * steps * stage / 24e6);
+            const double copies = std::max(turns * ((steps + split - 1) / split) * (any ? 1.2 : stage / 80e3), (double)tiles * steps * stage / 24e6);
             const double t = copies + turns * rows * (0.015 + 0.006 * (split - 1)) + (split > 1 ? 1.0 : 0.0);
             if (t < least) { least = t; best = FewChoice{nr, split}; }
         }
@@ -91,10 +99,10 @@ FewChoice choose_few(const Int8Params& P, const Device& dev) {
     return best;
 }
 
+constexpr int kSms = 148;               // (the workspace's size follows from it, with or without a device)
 constexpr int kVecBytes = 100 * 1024;  // of tokens in shared memory, for each of two blocks to an SM
 
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
-bool tma_ready(const Bytes& m) { return (uintptr_t)m.base % 16 == 0 && m.ld % 16 == 0; }
 
 // Operands that TMA cannot read are copied, both in one launch.
 int align_operands(Bytes* const (&list)[2], Space* space, bool run, cudaStream_t s) {
@@ -174,9 +182,14 @@ int product(const bmgd_quantized_linear_args* a, Space* space, bool run, const D
                               a->ld_codes, a->ld_weight, a->ld_y, a->outputs, a->inputs, a->type};
         return a->rows == 1 ? launch_vec<1>(V, dev, s) : launch_vec<2>(V, dev, s);
     }
-    Bytes* const operands[2] = {&q, &w};
-    const int rc = align_operands(operands, space, run, s);
-    if (rc != BMGD_OK || !run) return rc;
+    const int64_t small = ((a->rows + 127) / 128) * ((a->outputs + 127ll) / 128);
+    const bool few = a->rows <= 64 || small * 2 < kSms, ready = tma_ready(q) && tma_ready(w);
+    if (!few) {
+        Bytes* const operands[2] = {&q, &w};
+        const int rc = align_operands(operands, space, run, s);
+        if (rc != BMGD_OK) return rc;
+    }
+    if (!run) return BMGD_OK;
     Int8Params P{};
     P.q_scale = a->scale; P.w_scale = a->weight_scale; P.bias = a->bias;
     P.out = a->y; P.ld_out = a->ld_y;
@@ -189,13 +202,12 @@ int product(const bmgd_quantized_linear_args* a, Space* space, bool run, const D
     // Exchanged roles up to 64 tokens, and where tiles of 128 x 128 do not fill half the GPU; otherwise the tiles that take least turns, a turn of
     // 128 x 128, of 256 x 192 and of 256 x 256 for a pair being as 0.30 to 0.33 to 0.38 (microseconds for 128 inputs).  Measured on 4096 -> 11008: 128 tokens
     // 18.0 with exchanged roles, 14.4, 15.6, 17.3 with the three; 256: 23.7, 22.8, 16.0, 17.7; 512: 27.1 with the third, 24.0 with the second; 1024: 44.7, 38.5.
-    const int64_t small = ((a->rows + 127) / 128) * ((a->outputs + 127ll) / 128);
-    if (a->rows <= 64 || small * 2 < dev.sms) {
-        const FewChoice c = choose_few(P, dev);
-        if (c.rows == 16) return launch_few<16>(P, q, w, c.split, dev, s);
-        if (c.rows == 32) return launch_few<32>(P, q, w, c.split, dev, s);
-        if (c.rows == 64) return launch_few<64>(P, q, w, c.split, dev, s);
-        return launch_few<128>(P, q, w, c.split, dev, s);
+    if (few) {
+        const FewChoice c = choose_few(P, !ready, dev);
+        if (c.rows == 16) return ready ? launch_few<16, false>(P, q, w, c.split, dev, s) : launch_few<16, true>(P, q, w, c.split, dev, s);
+        if (c.rows == 32) return ready ? launch_few<32, false>(P, q, w, c.split, dev, s) : launch_few<32, true>(P, q, w, c.split, dev, s);
+        if (c.rows == 64) return ready ? launch_few<64, false>(P, q, w, c.split, dev, s) : launch_few<64, true>(P, q, w, c.split, dev, s);
+        return ready ? launch_few<128, false>(P, q, w, c.split, dev, s) : launch_few<128, true>(P, q, w, c.split, dev, s);
     }
     const int64_t pairs = dev.sms / 2, tall = (a->rows + 255) / 256;
     auto turns = [](int64_t tiles, int64_t units) { return (double)((tiles + units - 1) / units); };

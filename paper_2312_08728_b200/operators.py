@@ -523,11 +523,11 @@ def int8_linear(q: torch.Tensor, q_scale: torch.Tensor, w: torch.Tensor, w_scale
         if n > 0:
             base_q, base_w, work, size = q.data_ptr(), w.data_ptr(), None, 0
             args = _QUANTIZED_LINEAR.pack(n, d, c, _TYPES[dtype], 0, base_q, at_q, base_w, at_w, at_b, y.data_ptr(), ld_q, ld_w, c)
-            if (base_q | base_w | ld_q | ld_w) % 16:  # (rows on 16-byte boundaries need no workspace)
+            if (base_q | base_w | ld_q | ld_w) % 16:  # (rows on 16-byte boundaries need no workspace, few tokens neither)
                 need = ctypes.c_int64()
                 _status(L.bmgd_quantized_linear_workspace_bytes(args, ctypes.byref(need)), "bmgd_quantized_linear_workspace_bytes")
                 size = need.value
-                work = _one_per_row(size, torch.uint8)
+                work = _one_per_row(size, torch.uint8) if size else None
             _status(L.bmgd_quantized_linear(args, work.data_ptr() if work is not None else None, size, _current(device)), "bmgd_quantized_linear")
     _hand(stream, device, (y,))
     return y

@@ -138,6 +138,32 @@ def test_calls_at_once_on_several_streams():
 
 # ---------------------------------------------------------------- waits that run out
 
+@pytest.mark.parametrize("shape", [(1, 1, 1), (1, 15, 3), (3, 17, 129), (2, 130, 5), (16, 127, 128), (29, 1371, 2501), (64, 129, 300), (40, 4099, 1000), (100, 1371, 130), (129, 515, 129),
+                                   (300, 1000, 1000), (500, 77, 600)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("extra,shift", [(0, 1), (1, 0), (2, 2), (3, 3), (16, 7)])
+def test_few_tokens_on_any_boundary(shape, extra, shift):
+    check(*operands(*shape, seed=5, extra=extra, shift=shift, full=True), dtype=torch.float32)
+
+
+def test_one_operand_on_any_boundary():
+    q, qs, w, ws = operands(33, 1360, 700, seed=6)
+    odd = operands(33, 1360, 700, seed=6, extra=3, shift=1)
+    y = check(q, qs, w, ws)
+    odd[0].copy_(q), odd[2].copy_(w)
+    assert torch.equal(check(odd[0], qs, w, ws), y) and torch.equal(check(q, qs, odd[2], ws), y) and torch.equal(check(odd[0], qs, odd[2], ws), y)
+
+
+def test_nothing_beyond_a_row_counts():
+    """What stands in front of, behind and between the rows changes nothing."""
+    jobs = [operands(20, 1371, 400, seed=7, extra=5, shift=3) for _ in range(2)]
+    for t in (jobs[1][0], jobs[1][2]):
+        flat = torch.as_strided(t, (t.storage_offset() + t.shape[0] * t.stride(0),), (1,), 0)
+        kept = t.clone()
+        flat.fill_(-77)
+        t.copy_(kept)
+    assert torch.equal(ops.int8_linear(*jobs[0]), ops.int8_linear(*jobs[1]))
+
+
 def starve(job, fills, dtype=torch.bfloat16, budget_ms=5.0):
     """A product whose kernel fetches `fills` pieces per CTA; the output's memory is zero before."""
     L = binding.load_library()
@@ -152,7 +178,8 @@ def starve(job, fills, dtype=torch.bfloat16, budget_ms=5.0):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("fills", [0, 1, 8])
-@pytest.mark.parametrize("shape", [(3, 2048, 1376), (100, 128, 136), (700, 512, 2700), (2304, 1024, 2816), (2048, 1024, 2048)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("shape", [(3, 2048, 1376), (100, 128, 136), (700, 512, 2700), (2304, 1024, 2816), (2048, 1024, 2048), (3, 2047, 1376), (100, 127, 136)],
+                         ids=lambda s: "x".join(map(str, s)))
 def test_what_was_not_computed_is_nan(shape, fills, dtype):
     job = operands(*shape, seed=2)
     want = ops.int8_linear(*job, dtype=dtype)
@@ -190,7 +217,7 @@ def test_refusals():
     y = ops.int8_linear(q[:0], qs.detach()[:0], w, ws)
     assert y.shape == (0, 8)
     L, need = binding.load_library(), ctypes.c_int64()
-    args = ops._QUANTIZED_LINEAR.pack(4, 32, 8, 1, 0, q.data_ptr() + 1, qs.data_ptr(), w.data_ptr() + 1, ws.data_ptr(), 0, 1 << 20, 32, 32, 8)
+    args = ops._QUANTIZED_LINEAR.pack(4000, 32, 800, 1, 0, q.data_ptr() + 1, qs.data_ptr(), w.data_ptr() + 1, ws.data_ptr(), 0, 1 << 20, 32, 32, 800)
     assert L.bmgd_quantized_linear_workspace_bytes(args, ctypes.byref(need)) == 0 and need.value > 0
     assert L.bmgd_quantized_linear(args, None, 0, None) == binding.ERR_ARG
     assert L.bmgd_quantized_linear(args, 1 << 20, need.value - 1, None) == binding.ERR_CAPACITY

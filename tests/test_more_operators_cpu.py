@@ -113,10 +113,11 @@ def test_quantized_linear_workspace():
     def bytes_of(**kw):
         assert L.bmgd_quantized_linear_workspace_bytes(linear(**kw), ctypes.byref(need)) == 0
         return need.value
-    assert bytes_of() == 0 and bytes_of(rows=500) == 0
-    assert bytes_of(rows=500, ld_codes=65) >= 500 * 64 and bytes_of(ld_weight=65) >= 32 * 64 and bytes_of(weight=2 * PTR + 1) >= 32 * 64
-    assert bytes_of(rows=500, inputs=63, ld_codes=63, ld_weight=63) >= 532 * 64
-    odd = linear(rows=500, ld_codes=65)
+    many = dict(rows=2000, outputs=1000, ld_y=1000)      # (few tokens, or few tiles, are read on any boundary)
+    assert bytes_of() == 0 and bytes_of(rows=500) == 0 and bytes_of(ld_codes=65, ld_weight=65) == 0 and bytes_of(**many) == 0
+    assert bytes_of(**many, ld_codes=65) >= 2000 * 64 and bytes_of(**many, ld_weight=65) >= 1000 * 64 and bytes_of(**many, weight=2 * PTR + 1) >= 1000 * 64
+    assert bytes_of(**many, inputs=63, ld_codes=63, ld_weight=63) >= 3000 * 64
+    odd = linear(**many, ld_codes=65)
     assert L.bmgd_quantized_linear_workspace_bytes(odd, ctypes.byref(need)) == 0
     assert L.bmgd_quantized_linear(odd, None, 1 << 40, None) == binding.ERR_ARG
     assert L.bmgd_quantized_linear(odd, PTR + 16, 1 << 40, None) == binding.ERR_ARG
