@@ -11,6 +11,16 @@ namespace {
 using namespace bmgdk;
 
 int launched() { return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA; }
+// As a dependent of the kernel before it, and letting the next one start beside it: a token's way through a layer is a row of short kernels, and a product brings its
+// weights to L2 meanwhile.
+template <typename P>
+int start(void (*fn)(P), unsigned grid, int threads, const P& params, cudaStream_t s) {
+    cudaLaunchConfig_t lc{};
+    cudaLaunchAttribute at[2];
+    launch_config(&lc, at, dim3(grid), threads, 0, 1, s);
+    if (cudaLaunchKernelEx(&lc, fn, params) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
+    return BMGD_OK;
+}
 int value_bytes(int type) { return type == BMGD_TYPE_F32 ? 4 : 2; }
 bool off(const void* p, int bytes) { return (uintptr_t)p % (unsigned)bytes != 0; }
 // whether rows of that stride in bytes all start on 16-byte boundaries
@@ -43,21 +53,17 @@ template <typename T, bool RES, bool CODES, bool ANY>
 int forward_flow(const NormParams& P, cudaStream_t s) {
     const Threads t = threads_for((P.width + Piece<T>::kValues - 1) / Piece<T>::kValues);
     const unsigned grid = flow_grid(t, P.rows, t.pieces >= 4 ? 512 : 1024);
-    if (t.threads == 32 && t.pieces == 1) norm_flow_kernel<T, 1, true, RES, CODES, ANY><<<grid, 256, 0, s>>>(P);
-    else if (t.threads == 32) norm_flow_kernel<T, 2, true, RES, CODES, ANY><<<grid, 256, 0, s>>>(P);
-    else if (t.pieces == 2) norm_flow_kernel<T, 2, false, RES, CODES, ANY><<<grid, t.threads, 0, s>>>(P);
-    else if (t.pieces == 4) norm_flow_kernel<T, 4, false, RES, CODES, ANY><<<grid, t.threads, 0, s>>>(P);
-    else norm_flow_kernel<T, 8, false, RES, CODES, ANY><<<grid, t.threads, 0, s>>>(P);
-    return launched();
+    if (t.threads == 32 && t.pieces == 1) return start(norm_flow_kernel<T, 1, true, RES, CODES, ANY>, grid, 256, P, s);
+    if (t.threads == 32) return start(norm_flow_kernel<T, 2, true, RES, CODES, ANY>, grid, 256, P, s);
+    if (t.pieces == 2) return start(norm_flow_kernel<T, 2, false, RES, CODES, ANY>, grid, t.threads, P, s);
+    if (t.pieces == 4) return start(norm_flow_kernel<T, 4, false, RES, CODES, ANY>, grid, t.threads, P, s);
+    return start(norm_flow_kernel<T, 8, false, RES, CODES, ANY>, grid, t.threads, P, s);
 }
 // Rows of up to 4096 pieces; longer ones are read more than once.
 template <typename T, bool CODES>
 int forward(const NormParams& P, bool aligned, cudaStream_t s) {
     const int64_t pieces = ((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16;
-    if (pieces > 4096) {
-        norm_long_kernel<T, CODES><<<(unsigned)P.rows, 1024, 0, s>>>(P);
-        return launched();
-    }
+    if (pieces > 4096) return start(norm_long_kernel<T, CODES>, (unsigned)P.rows, 1024, P, s);
     if (aligned) return P.residual ? forward_flow<T, true, CODES, false>(P, s) : forward_flow<T, false, CODES, false>(P, s);
     return P.residual ? forward_flow<T, true, CODES, true>(P, s) : forward_flow<T, false, CODES, true>(P, s);
 }
@@ -166,19 +172,15 @@ int codes_flow(const CodesParams& P, cudaStream_t s) {
         t.threads = (int)((count + t.pieces * 32 - 1) / (t.pieces * 32)) * 32;
     }
     const unsigned grid = flow_grid(t, P.rows, t.pieces == 6 ? 384 : t.pieces == 4 ? 768 : 1024);
-    if (t.threads == 32 && t.pieces == 1) codes_flow_kernel<T, 1, true, GATE, ANY><<<grid, 256, 0, s>>>(P);
-    else if (t.threads == 32) codes_flow_kernel<T, 2, true, GATE, ANY><<<grid, 256, 0, s>>>(P);
-    else if (t.pieces == 2) codes_flow_kernel<T, 2, false, GATE, ANY><<<grid, t.threads, 0, s>>>(P);
-    else if (t.pieces == 4) codes_flow_kernel<T, 4, false, GATE, ANY><<<grid, t.threads, 0, s>>>(P);
-    else codes_flow_kernel<T, 6, false, GATE, ANY><<<grid, t.threads, 0, s>>>(P);
-    return launched();
+    if (t.threads == 32 && t.pieces == 1) return start(codes_flow_kernel<T, 1, true, GATE, ANY>, grid, 256, P, s);
+    if (t.threads == 32) return start(codes_flow_kernel<T, 2, true, GATE, ANY>, grid, 256, P, s);
+    if (t.pieces == 2) return start(codes_flow_kernel<T, 2, false, GATE, ANY>, grid, t.threads, P, s);
+    if (t.pieces == 4) return start(codes_flow_kernel<T, 4, false, GATE, ANY>, grid, t.threads, P, s);
+    return start(codes_flow_kernel<T, 6, false, GATE, ANY>, grid, t.threads, P, s);
 }
 template <typename T>
 int codes(const CodesParams& P, bool aligned, cudaStream_t s) {
-    if (((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16 > 6 * 384) {
-        codes_long_kernel<T><<<(unsigned)P.rows, 1024, 0, s>>>(P);
-        return launched();
-    }
+    if (((int64_t)P.width * (int64_t)sizeof(T) + 15) / 16 > 6 * 384) return start(codes_long_kernel<T>, (unsigned)P.rows, 1024, P, s);
     if (aligned) return P.gate ? codes_flow<T, true, false>(P, s) : codes_flow<T, false, false>(P, s);
     return P.gate ? codes_flow<T, true, true>(P, s) : codes_flow<T, false, true>(P, s);
 }

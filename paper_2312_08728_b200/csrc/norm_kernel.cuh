@@ -166,6 +166,8 @@ struct Place {  // of a block's (a warp's) rows
 
 template <typename T, int NV, bool WARP, bool RES, bool CODES, bool ANY>
 __global__ void __launch_bounds__(WARP ? 256 : 512, NV >= 4 ? 1 : 2) norm_flow_kernel(const __grid_constant__ NormParams P) {
+    wait_for_previous_kernel();
+    let_next_kernel_start();
     constexpr int VE = Piece<T>::kValues;
     constexpr bool kAhead = NV <= 4;  // (registers do not suffice for two rows of eight pieces, nor for their weights)
     typedef typename SquareSum<T>::type Sum;
@@ -288,6 +290,8 @@ __global__ void __launch_bounds__(WARP ? 256 : 512, NV >= 4 ? 1 : 2) norm_flow_k
 // ---- forward, rows of any length: a block of 1024 to a row, which is read again for each of the steps (from L2, mostly)
 template <typename T, bool CODES>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__ NormParams P) {
+    wait_for_previous_kernel();
+    let_next_kernel_start();
     constexpr int VE = Piece<T>::kValues, TH = 1024;
     __shared__ typename SquareSum<T>::type sums[TH / 32];
     __shared__ float tops[TH / 32];
@@ -656,6 +660,8 @@ __device__ __forceinline__ float gated_one(const CodesParams& P, T x, const T* g
 // as norm_flow_kernel
 template <typename T, int NV, bool WARP, bool GATE, bool ANY>
 __global__ void __launch_bounds__(WARP ? 256 : 384, NV == 6 ? 1 : 2) codes_flow_kernel(const __grid_constant__ CodesParams P) {
+    wait_for_previous_kernel();
+    let_next_kernel_start();
     constexpr int VE = Piece<T>::kValues;
     __shared__ __align__(16) float cells[2][32];
     const int tid = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
@@ -711,6 +717,8 @@ __global__ void __launch_bounds__(WARP ? 256 : 384, NV == 6 ? 1 : 2) codes_flow_
 // rows of any length, read twice
 template <typename T>
 __global__ void __launch_bounds__(1024) codes_long_kernel(const __grid_constant__ CodesParams P) {
+    wait_for_previous_kernel();
+    let_next_kernel_start();
     constexpr int VE = Piece<T>::kValues, TH = 1024;
     __shared__ float cells[TH / 32];
     const int tid = threadIdx.x;
