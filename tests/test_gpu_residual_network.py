@@ -199,3 +199,42 @@ def test_refusals():
         net.set_theta(net.get_theta()[:-1])
     net.set_theta(net.get_theta())
     assert normed(torch.ones(1, 8, device="cuda"), None)[0].shape == (1, 8)
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 70])
+def test_a_layer_behind_copies_and_other_streams_in_a_graph(n):
+    """Launches that start beside the end of the one before them wait for whatever stands there: a copy, a memset, two streams that meet."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    d, f = 520, 1000
+    rows = torch.randn(n, d, device="cuda", generator=gen).to(torch.bfloat16)
+    w, parts = torch.rand(d, device="cuda", generator=gen) + 0.5, [torch.zeros(n, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    up = ops.quantize_weight(torch.randn(d, 2 * f, device="cuda", generator=gen))
+    down = ops.quantize_weight(torch.randn(f, d, device="cuda", generator=gen))
+    other = torch.cuda.Stream()
+
+    def layer():
+        here = torch.cuda.current_stream()
+        other.wait_stream(here)
+        with torch.cuda.stream(other):
+            parts[1].zero_()
+            parts[1].add_(rows)
+        parts[0].copy_(rows)
+        here.wait_stream(other)
+        q, s, total = ops.rms_norm_int8(parts[0], w, residual=parts[1])
+        v = ops.int8_linear(q, s, *up)
+        q, s = ops.quantize_rows(v[:, f:], gate=v[:, :f])
+        return ops.int8_linear(q, s, *down), total
+
+    layer()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = layer()
+    for k in range(20):
+        rows.normal_(generator=gen)
+        want = [t.clone() for t in layer()]
+        for t in (*parts, *got):
+            t.zero_()
+        graph.replay()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
