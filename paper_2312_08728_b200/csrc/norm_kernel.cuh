@@ -603,13 +603,13 @@ struct CodesParams {
     long long ld_x, ld_gate, ld_codes, rows;
     int width, act;
 };
-// act(gate) as it is wanted here.  16-bit rows: exponential and reciprocal from the special unit, within a few 2^-23 of the value.  fp32 rows: the exact functions, because
-// their codes are read against values of the same type, and next to a border a code follows every bit.
+// act(gate) as it is wanted here.  SiLU and sigmoid of 16-bit rows: exponential and reciprocal from the special unit, within (8 + 2 |g|) 2^-24 of the value; of fp32 rows the exact
+// functions, because their codes are read against values of the same type, and next to a border a code follows every bit.  GELU: within (16 + 2 g^2) 2^-24 below zero.
 template <typename T, int ACT>
 __device__ __forceinline__ float gate_value(float g) {
     if constexpr (ACT == kActRelu) return g <= 0.f ? 0.f : g;
-    if constexpr (ACT == kActGelu) return g * (0.5f * (1.f + erff(g * 0.70710678118654752f)));
     float s;
+    if constexpr (ACT == kActGelu) return g * gelu_share(g, s);
     if constexpr (sizeof(T) == 4) {
         s = __fdiv_rn(1.f, 1.f + expf(-g));
     } else {
