@@ -29,7 +29,10 @@ __device__ __forceinline__ float gelu_share(float g, float& e) {
 // relu by comparisons alone: -inf gives 0, and NaN, which fails both, stays NaN
 __device__ __forceinline__ float act_value(int act, float g) {
     if (act == kActRelu) return g <= 0.f ? 0.f : g;
-    if (act == kActGelu) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+    if (act == kActGelu) {
+        float e;
+        return g * gelu_share(g, e);
+    }
     const float s = __fdividef(1.f, 1.f + __expf(-g));
     return act == kActSigmoid ? s : g * s;
 }
@@ -38,9 +41,10 @@ __device__ __forceinline__ void act_both(int act, float g, float& value, float& 
         value = g <= 0.f ? 0.f : g;
         slope = g <= 0.f ? 0.f : g > 0.f ? 1.f : g;
     } else if (act == kActGelu) {
-        const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        float e;
+        const float cdf = gelu_share(g, e);
         value = g * cdf;
-        slope = cdf + g * __expf(-0.5f * g * g) * 0.3989422804014327f;
+        slope = cdf + g * e * 0.3989422804014327f;
     } else {
         const float s = __fdividef(1.f, 1.f + __expf(-g));
         if (act == kActSigmoid) { value = s; slope = s * (1.f - s); }
