@@ -117,7 +117,7 @@ def peak_hbm():
 # sources of the operators on device tensors: none of the measured step kernels is made from them
 OPERATOR_SOURCES = {"activation.cuh", "adamw.cu", "adamw_kernel.cuh", "contract.cuh", "dropout.cu", "dropout_kernel.cuh", "ffn_kernel.cuh",
                     "gated_ffn.cu", "int8_kernel.cuh", "int8_linear.cu", "launch.cuh", "logprob.cu", "logprob_kernel.cuh", "norm.cu",
-                    "norm_kernel.cuh", "operator_host.cuh", "pair.cuh", "residual.cu", "residual_kernel.cuh", "values.cuh"}
+                    "norm_kernel.cuh", "operator_host.cuh", "overlap.cuh", "pair.cuh", "residual.cu", "residual_kernel.cuh", "values.cuh"}
 
 
 def kernel_source_hash():

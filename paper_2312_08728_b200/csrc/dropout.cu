@@ -3,6 +3,7 @@
 
 #include "../../include/bmgd.h"
 #include "dropout_kernel.cuh"
+#include "overlap.cuh"
 
 namespace {
 
@@ -19,13 +20,6 @@ int dropout(const DropoutParams& P, cudaStream_t s) {
     return cudaGetLastError() == cudaSuccess ? BMGD_OK : BMGD_ERR_CUDA;
 }
 
-// [rows][width] of strides lp and lq (in bytes w a row): the same memory value for value, or none of it
-bool apart_or_same(const void* p, int64_t lp, const void* q, int64_t lq, int64_t w, int64_t rows) {
-    if (p == q && (lp == lq || rows == 1)) return true;
-    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-    return a >= b + (uintptr_t)((rows - 1) * lq + w) || b >= a + (uintptr_t)((rows - 1) * lp + w);
-}
-
 }  // namespace
 
 extern "C" {
@@ -40,8 +34,8 @@ int bmgd_dropout(const bmgd_dropout_args* a, void* stream) {
     const int64_t eb = a->type == BMGD_TYPE_F32 ? 4 : 2;
     if (!a->x || !a->y || a->ld_x < a->width || a->ld_y < a->width || (a->residual && a->ld_residual < a->width)) return BMGD_ERR_ARG;
     if ((uintptr_t)a->x % eb || (uintptr_t)a->y % eb || (uintptr_t)a->residual % eb || (uintptr_t)a->step % 8) return BMGD_ERR_ARG;
-    if (!apart_or_same(a->y, a->ld_y * eb, a->x, a->ld_x * eb, a->width * eb, a->rows)) return BMGD_ERR_ARG;
-    if (a->residual && !apart_or_same(a->y, a->ld_y * eb, a->residual, a->ld_residual * eb, a->width * eb, a->rows)) return BMGD_ERR_ARG;
+    const Region y{a->y, a->rows, a->width * eb, a->ld_y * eb};
+    if (!same_or_apart(y, {a->x, a->rows, a->width * eb, a->ld_x * eb}) || !same_or_apart(y, {a->residual, a->rows, a->width * eb, a->ld_residual * eb})) return BMGD_ERR_ARG;
     DropoutParams P{};
     P.x = a->x; P.residual = a->residual; P.y = a->y; P.step = reinterpret_cast<const long long*>(a->step);
     P.ld_x = a->ld_x; P.ld_residual = a->ld_residual; P.ld_y = a->ld_y; P.rows = a->rows; P.width = a->width;

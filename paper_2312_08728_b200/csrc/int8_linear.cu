@@ -5,6 +5,7 @@
 #include "../../include/bmgd.h"
 #include "int8_kernel.cuh"
 #include "operator_host.cuh"
+#include "overlap.cuh"
 
 namespace {
 
@@ -133,10 +134,9 @@ int check(const bmgd_quantized_linear_args* a, bool pointers) {
     if (!pointers || a->rows == 0) return BMGD_OK;
     if (!a->codes || !a->scale || !a->weight || !a->weight_scale || !a->y) return BMGD_ERR_ARG;
     if ((uintptr_t)a->scale % 4 || (uintptr_t)a->weight_scale % 4 || (uintptr_t)a->bias % 4 || (uintptr_t)a->y % (a->type == BMGD_TYPE_F32 ? 4 : 2)) return BMGD_ERR_ARG;
-    const uintptr_t y = (uintptr_t)a->y, end = y + (uintptr_t)(((a->rows - 1) * a->ld_y + a->outputs) * (a->type == BMGD_TYPE_F32 ? 4 : 2));
-    const uintptr_t q = (uintptr_t)a->codes, w = (uintptr_t)a->weight;
-    if (q < end && y < q + (uintptr_t)((a->rows - 1) * a->ld_codes + a->inputs)) return BMGD_ERR_ARG;
-    if (w < end && y < w + (uintptr_t)((a->outputs - 1) * a->ld_weight + a->inputs)) return BMGD_ERR_ARG;
+    const int64_t eb = a->type == BMGD_TYPE_F32 ? 4 : 2;
+    const Region y{a->y, a->rows, a->outputs * eb, a->ld_y * eb};
+    if (share_memory(y, {a->codes, a->rows, a->inputs, a->ld_codes}) || share_memory(y, {a->weight, a->outputs, a->inputs, a->ld_weight})) return BMGD_ERR_ARG;
     return BMGD_OK;
 }
 

@@ -3,6 +3,7 @@
 
 #include "../../include/bmgd.h"
 #include "logprob_kernel.cuh"
+#include "overlap.cuh"
 
 namespace {
 
@@ -80,9 +81,7 @@ int bmgd_log_probs_backward(const bmgd_log_probs_args* a, void* stream) {
     const int64_t eb = a->type == BMGD_TYPE_F32 ? 4 : 2;
     if (!a->saved || !a->dlogits || a->ld_dlogits < a->C || (uintptr_t)a->dlogits % eb) return BMGD_ERR_ARG;
     // the gradient may take the logits' place, value for value
-    const uintptr_t z = (uintptr_t)a->logits, d = (uintptr_t)a->dlogits;
-    const bool same = z == d && (a->ld_logits == a->ld_dlogits || a->rows == 1);
-    if (!same && z < d + (uintptr_t)(((a->rows - 1) * a->ld_dlogits + a->C) * eb) && d < z + (uintptr_t)(((a->rows - 1) * a->ld_logits + a->C) * eb)) return BMGD_ERR_ARG;
+    if (!same_or_apart({a->dlogits, a->rows, a->C * eb, a->ld_dlogits * eb}, {a->logits, a->rows, a->C * eb, a->ld_logits * eb})) return BMGD_ERR_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const LogProbParams P = params(a);
     if (a->type == BMGD_TYPE_F32) return backward<float>(P, s);

@@ -5,6 +5,7 @@
 #include "../../include/bmgd.h"
 #include "norm_kernel.cuh"
 #include "operator_host.cuh"
+#include "overlap.cuh"
 
 namespace {
 
@@ -25,11 +26,6 @@ int value_bytes(int type) { return type == BMGD_TYPE_F32 ? 4 : 2; }
 bool off(const void* p, int bytes) { return (uintptr_t)p % (unsigned)bytes != 0; }
 // whether rows of that stride in bytes all start on 16-byte boundaries
 bool on16(const void* p, int64_t stride) { return ((uintptr_t)p | (uintptr_t)stride) % 16 == 0; }
-// whether [rows][width] of stride ld at p and the same of stride lq at q share memory
-bool overlap(const void* p, int64_t ld, int64_t pw, const void* q, int64_t lq, int64_t qw, int64_t rows) {
-    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-    return a < b + (uintptr_t)((rows - 1) * lq + qw) && b < a + (uintptr_t)((rows - 1) * ld + pw);
-}
 
 // Threads of a row of `count` pieces: a warp up to 64 (two each), then two pieces a thread up to 1024, four up to 2048, eight.
 struct Threads {
@@ -157,8 +153,9 @@ int check_backward(const bmgd_rms_norm* a) {
     if (!a->total || !a->dy || !a->dx || !a->rstd) return BMGD_ERR_ARG;
     if (off(a->total, eb) || off(a->dy, eb) || off(a->dx, eb) || off(a->dtotal, eb) || off(a->rstd, 4)) return BMGD_ERR_ARG;
     const int64_t w = (int64_t)a->width * eb;  // a row of dx may be written before another thread has read the same row
-    if (overlap(a->dx, a->ld_dx * eb, w, a->total, a->ld_total * eb, w, a->rows) || overlap(a->dx, a->ld_dx * eb, w, a->dy, a->ld_dy * eb, w, a->rows) ||
-        (a->dtotal && overlap(a->dx, a->ld_dx * eb, w, a->dtotal, a->ld_dtotal * eb, w, a->rows))) return BMGD_ERR_ARG;
+    const Region dx{a->dx, a->rows, w, a->ld_dx * eb};
+    if (share_memory(dx, {a->total, a->rows, w, a->ld_total * eb}) || share_memory(dx, {a->dy, a->rows, w, a->ld_dy * eb}) ||
+        share_memory(dx, {a->dtotal, a->rows, w, a->ld_dtotal * eb})) return BMGD_ERR_ARG;
     return BMGD_OK;
 }
 
@@ -206,14 +203,9 @@ int bmgd_rms_norm_forward(const bmgd_rms_norm* a, void* stream) {
     if (a->y ? a->ld_y < a->width : a->ld_codes < a->width) return BMGD_ERR_ARG;
     if ((a->residual != nullptr) != (a->total != nullptr) || (a->residual && (a->ld_residual < a->width || a->ld_total < a->width))) return BMGD_ERR_ARG;
     // What is written overlaps nothing that is read: rows are read more than once where they are long.
-    const void* const out[2] = {a->total, a->y ? a->y : (const void*)a->codes};
-    const int64_t ld_out[2] = {a->ld_total * eb, a->y ? a->ld_y * eb : a->ld_codes}, w_out[2] = {w, a->y ? w : (int64_t)a->width};
-    for (int k = 0; k < 2; ++k) {
-        if (!out[k]) continue;
-        if (overlap(out[k], ld_out[k], w_out[k], a->x, a->ld_x * eb, w, a->rows)) return BMGD_ERR_ARG;
-        if (a->residual && overlap(out[k], ld_out[k], w_out[k], a->residual, a->ld_residual * eb, w, a->rows)) return BMGD_ERR_ARG;
-    }
-    if (out[0] && overlap(out[0], ld_out[0], w, out[1], ld_out[1], w_out[1], a->rows)) return BMGD_ERR_ARG;
+    const Region x{a->x, a->rows, w, a->ld_x * eb}, r{a->residual, a->rows, w, a->ld_residual * eb}, total{a->total, a->rows, w, a->ld_total * eb},
+        y = a->y ? Region{a->y, a->rows, w, a->ld_y * eb} : Region{a->codes, a->rows, a->width, a->ld_codes};
+    if (share_memory(total, x) || share_memory(total, r) || share_memory(y, x) || share_memory(y, r) || share_memory(total, y)) return BMGD_ERR_ARG;
     NormParams P = shared_params(a);
     P.x = a->x; P.ld_x = a->ld_x;
     P.residual = a->residual; P.ld_residual = a->ld_residual;
@@ -270,8 +262,8 @@ int bmgd_quantize_rows(const bmgd_quantize_rows_args* a, void* stream) {
     if (!a->x || !a->codes || !a->scale || a->ld_x < a->width || a->ld_codes < a->width || (a->gate && a->ld_gate < a->width)) return BMGD_ERR_ARG;
     if (off(a->x, eb) || off(a->gate, eb) || off(a->scale, 4)) return BMGD_ERR_ARG;
     const int64_t w = (int64_t)a->width * eb;
-    if (overlap(a->codes, a->ld_codes, a->width, a->x, a->ld_x * eb, w, a->rows) ||
-        (a->gate && overlap(a->codes, a->ld_codes, a->width, a->gate, a->ld_gate * eb, w, a->rows))) return BMGD_ERR_ARG;
+    const Region q{a->codes, a->rows, a->width, a->ld_codes};
+    if (share_memory(q, {a->x, a->rows, w, a->ld_x * eb}) || share_memory(q, {a->gate, a->rows, w, a->ld_gate * eb})) return BMGD_ERR_ARG;
     const CodesParams P{a->x, a->gate, reinterpret_cast<signed char*>(a->codes), a->scale, a->ld_x, a->ld_gate, a->ld_codes, a->rows, a->width, a->activation};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool aligned = w % 16 == 0 && on16(a->x, a->ld_x * eb) && on16(a->gate, a->gate ? a->ld_gate * eb : 0) && on16(a->codes, a->ld_codes);
@@ -285,8 +277,7 @@ int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_
     if (inputs < 1 || outputs < 1 || inputs > (1 << 24) || outputs > (1 << 24) || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
     if (!dev_w || !dev_codes || !dev_scale || ld_w < outputs || ld_codes < inputs || off(dev_w, value_bytes(type)) || off(dev_scale, 4)) return BMGD_ERR_ARG;
     const int eb = value_bytes(type);
-    const uintptr_t a = (uintptr_t)dev_w, b = (uintptr_t)dev_codes;
-    if (a < b + (uintptr_t)((outputs - 1) * ld_codes + inputs) && b < a + (uintptr_t)(((inputs - 1) * ld_w + outputs) * eb)) return BMGD_ERR_ARG;
+    if (share_memory({dev_codes, outputs, inputs, ld_codes}, {dev_w, inputs, (int64_t)outputs * eb, ld_w * eb})) return BMGD_ERR_ARG;
     signed char* q = reinterpret_cast<signed char*>(dev_codes);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == BMGD_TYPE_F32) return weight_codes<float>(dev_w, ld_w, inputs, outputs, q, ld_codes, dev_scale, s);
