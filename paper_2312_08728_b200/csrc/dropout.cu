@@ -35,6 +35,7 @@ int bmgd_dropout(const bmgd_dropout_args* a, void* stream) {
     if (!a->x || !a->y || a->ld_x < a->width || a->ld_y < a->width || (a->residual && a->ld_residual < a->width)) return BMGD_ERR_ARG;
     if ((uintptr_t)a->x % eb || (uintptr_t)a->y % eb || (uintptr_t)a->residual % eb || (uintptr_t)a->step % 8) return BMGD_ERR_ARG;
     const Region y{a->y, a->rows, a->width * eb, a->ld_y * eb};
+    if (share_memory(y, vector_region(a->step, 8))) return BMGD_ERR_ARG;
     if (!same_or_apart(y, {a->x, a->rows, a->width * eb, a->ld_x * eb}) || !same_or_apart(y, {a->residual, a->rows, a->width * eb, a->ld_residual * eb})) return BMGD_ERR_ARG;
     DropoutParams P{};
     P.x = a->x; P.residual = a->residual; P.y = a->y; P.step = reinterpret_cast<const long long*>(a->step);

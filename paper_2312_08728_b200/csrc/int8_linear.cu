@@ -136,8 +136,8 @@ int check(const bmgd_quantized_linear_args* a, bool pointers) {
     if ((uintptr_t)a->scale % 4 || (uintptr_t)a->weight_scale % 4 || (uintptr_t)a->bias % 4 || (uintptr_t)a->y % (a->type == BMGD_TYPE_F32 ? 4 : 2)) return BMGD_ERR_ARG;
     const int64_t eb = a->type == BMGD_TYPE_F32 ? 4 : 2;
     const Region y{a->y, a->rows, a->outputs * eb, a->ld_y * eb};
-    if (share_memory(y, {a->codes, a->rows, a->inputs, a->ld_codes}) || share_memory(y, {a->weight, a->outputs, a->inputs, a->ld_weight})) return BMGD_ERR_ARG;
-    return BMGD_OK;
+    return writes_apart({y}, {{a->codes, a->rows, a->inputs, a->ld_codes}, {a->weight, a->outputs, a->inputs, a->ld_weight}, vector_region(a->scale, a->rows * 4),
+                              vector_region(a->weight_scale, a->outputs * 4ll), vector_region(a->bias, a->outputs * 4ll)}) ? BMGD_OK : BMGD_ERR_ARG;
 }
 
 // One or two tokens: two blocks to an SM, with as many warps each (8 to 16) as let the channels come out most evenly, 2 x 148 x W of them at a

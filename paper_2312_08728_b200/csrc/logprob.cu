@@ -66,6 +66,9 @@ int bmgd_log_probs(const bmgd_log_probs_args* a, void* stream) {
     if (rc != BMGD_OK) return rc;
     if (a->rows == 0) return BMGD_OK;
     if (a->top > 0 && (!a->top_class || !a->top_logprob)) return BMGD_ERR_ARG;
+    const int64_t eb = a->type == BMGD_TYPE_F32 ? 4 : 2, words = a->rows * 4;
+    if (!writes_apart({vector_region(a->logprob, words), vector_region(a->entropy, words), vector_region(a->saved, words * 3), vector_region(a->top_class, words * a->top),
+                       vector_region(a->top_logprob, words * a->top)}, {{a->logits, a->rows, a->C * eb, a->ld_logits * eb}, vector_region(a->y, words)})) return BMGD_ERR_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const LogProbParams P = params(a);
     const bool top = a->top > 0;
@@ -81,7 +84,10 @@ int bmgd_log_probs_backward(const bmgd_log_probs_args* a, void* stream) {
     const int64_t eb = a->type == BMGD_TYPE_F32 ? 4 : 2;
     if (!a->saved || !a->dlogits || a->ld_dlogits < a->C || (uintptr_t)a->dlogits % eb) return BMGD_ERR_ARG;
     // the gradient may take the logits' place, value for value
+    const int64_t words = a->rows * 4;
     if (!same_or_apart({a->dlogits, a->rows, a->C * eb, a->ld_dlogits * eb}, {a->logits, a->rows, a->C * eb, a->ld_logits * eb})) return BMGD_ERR_ARG;
+    if (!writes_apart({{a->dlogits, a->rows, a->C * eb, a->ld_dlogits * eb}}, {vector_region(a->y, words), vector_region(a->saved, words * 3), vector_region(a->dlogprob, words),
+                       vector_region(a->dentropy, words)})) return BMGD_ERR_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const LogProbParams P = params(a);
     if (a->type == BMGD_TYPE_F32) return backward<float>(P, s);

@@ -126,6 +126,7 @@ int backward_all(const NormParams& P, const BackShape& b, cudaStream_t s) {
     return BMGD_OK;
 }
 
+int64_t weight_bytes(const bmgd_rms_norm* a) { return (int64_t)a->width * (a->weight_type == BMGD_TYPE_F32 ? 4 : value_bytes(a->type)); }
 int check(const bmgd_rms_norm* a) {
     if (!a || a->rows < 0 || a->rows > 0x7FFFFFFFll || a->width < 1 || a->width > (1 << 24) || a->reserved != 0) return BMGD_ERR_ARG;
     if (a->type < BMGD_TYPE_F32 || a->type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
@@ -154,9 +155,9 @@ int check_backward(const bmgd_rms_norm* a) {
     if (off(a->total, eb) || off(a->dy, eb) || off(a->dx, eb) || off(a->dtotal, eb) || off(a->rstd, 4)) return BMGD_ERR_ARG;
     const int64_t w = (int64_t)a->width * eb;  // a row of dx may be written before another thread has read the same row
     const Region dx{a->dx, a->rows, w, a->ld_dx * eb};
-    if (share_memory(dx, {a->total, a->rows, w, a->ld_total * eb}) || share_memory(dx, {a->dy, a->rows, w, a->ld_dy * eb}) ||
-        share_memory(dx, {a->dtotal, a->rows, w, a->ld_dtotal * eb})) return BMGD_ERR_ARG;
-    return BMGD_OK;
+    const int64_t weights = weight_bytes(a);
+    return writes_apart({dx, vector_region(a->dweight, weights)}, {{a->total, a->rows, w, a->ld_total * eb}, {a->dy, a->rows, w, a->ld_dy * eb}, {a->dtotal, a->rows, w, a->ld_dtotal * eb},
+                        vector_region(a->weight, weights), vector_region(a->rstd, a->rows * 4)}) ? BMGD_OK : BMGD_ERR_ARG;
 }
 
 // Up to 384 threads with two, four or six pieces: a row's values are held in fp32, and two blocks of four pieces a thread (85 registers) fit an SM.
@@ -202,10 +203,10 @@ int bmgd_rms_norm_forward(const bmgd_rms_norm* a, void* stream) {
     if ((a->y == nullptr) == (a->codes == nullptr) || (a->codes != nullptr) != (a->scale != nullptr)) return BMGD_ERR_ARG;
     if (a->y ? a->ld_y < a->width : a->ld_codes < a->width) return BMGD_ERR_ARG;
     if ((a->residual != nullptr) != (a->total != nullptr) || (a->residual && (a->ld_residual < a->width || a->ld_total < a->width))) return BMGD_ERR_ARG;
-    // What is written overlaps nothing that is read: rows are read more than once where they are long.
+    // (rows are read more than once where they are long)
     const Region x{a->x, a->rows, w, a->ld_x * eb}, r{a->residual, a->rows, w, a->ld_residual * eb}, total{a->total, a->rows, w, a->ld_total * eb},
         y = a->y ? Region{a->y, a->rows, w, a->ld_y * eb} : Region{a->codes, a->rows, a->width, a->ld_codes};
-    if (share_memory(total, x) || share_memory(total, r) || share_memory(y, x) || share_memory(y, r) || share_memory(total, y)) return BMGD_ERR_ARG;
+    if (!writes_apart({total, y, vector_region(a->scale, a->rows * 4), vector_region(a->rstd, a->rows * 4)}, {x, r, vector_region(a->weight, weight_bytes(a))})) return BMGD_ERR_ARG;
     NormParams P = shared_params(a);
     P.x = a->x; P.ld_x = a->ld_x;
     P.residual = a->residual; P.ld_residual = a->ld_residual;
@@ -263,7 +264,7 @@ int bmgd_quantize_rows(const bmgd_quantize_rows_args* a, void* stream) {
     if (off(a->x, eb) || off(a->gate, eb) || off(a->scale, 4)) return BMGD_ERR_ARG;
     const int64_t w = (int64_t)a->width * eb;
     const Region q{a->codes, a->rows, a->width, a->ld_codes};
-    if (share_memory(q, {a->x, a->rows, w, a->ld_x * eb}) || share_memory(q, {a->gate, a->rows, w, a->ld_gate * eb})) return BMGD_ERR_ARG;
+    if (!writes_apart({q, vector_region(a->scale, a->rows * 4)}, {{a->x, a->rows, w, a->ld_x * eb}, {a->gate, a->rows, w, a->ld_gate * eb}})) return BMGD_ERR_ARG;
     const CodesParams P{a->x, a->gate, reinterpret_cast<signed char*>(a->codes), a->scale, a->ld_x, a->ld_gate, a->ld_codes, a->rows, a->width, a->activation};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool aligned = w % 16 == 0 && on16(a->x, a->ld_x * eb) && on16(a->gate, a->gate ? a->ld_gate * eb : 0) && on16(a->codes, a->ld_codes);
@@ -277,7 +278,7 @@ int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_
     if (inputs < 1 || outputs < 1 || inputs > (1 << 24) || outputs > (1 << 24) || type < BMGD_TYPE_F32 || type > BMGD_TYPE_F16) return BMGD_ERR_ARG;
     if (!dev_w || !dev_codes || !dev_scale || ld_w < outputs || ld_codes < inputs || off(dev_w, value_bytes(type)) || off(dev_scale, 4)) return BMGD_ERR_ARG;
     const int eb = value_bytes(type);
-    if (share_memory({dev_codes, outputs, inputs, ld_codes}, {dev_w, inputs, (int64_t)outputs * eb, ld_w * eb})) return BMGD_ERR_ARG;
+    if (!writes_apart({{dev_codes, outputs, inputs, ld_codes}, vector_region(dev_scale, outputs * 4ll)}, {{dev_w, inputs, (int64_t)outputs * eb, ld_w * eb}})) return BMGD_ERR_ARG;
     signed char* q = reinterpret_cast<signed char*>(dev_codes);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == BMGD_TYPE_F32) return weight_codes<float>(dev_w, ld_w, inputs, outputs, q, ld_codes, dev_scale, s);

@@ -1,6 +1,7 @@
 // Whether two matrices in memory share a byte.  Host side, without CUDA.
 #pragma once
 #include <cstdint>
+#include <initializer_list>
 
 namespace bmgdk {
 
@@ -46,6 +47,16 @@ inline bool share_memory(const Region& x, const Region& y) {
     if (x.rows == 1 && y.rows == 1) return true;
     const wide_int last = y.rows - 1;
     return held_floor_sum(x.rows, ly, lx, a - b + x.width - 1, last) > held_floor_sum(x.rows, ly, lx, a - b - y.width, last);
+}
+// whether what is written shares nothing with what is read, nor with anything else that is written
+inline bool writes_apart(std::initializer_list<Region> written, std::initializer_list<Region> read) {
+    for (const Region* w = written.begin(); w != written.end(); ++w) {
+        for (const Region& r : read)
+            if (share_memory(*w, r)) return false;
+        for (const Region* v = written.begin(); v != w; ++v)
+            if (share_memory(*w, *v)) return false;
+    }
+    return true;
 }
 // the same memory value for value, or none of it
 inline bool same_or_apart(const Region& x, const Region& y) {
