@@ -27,7 +27,7 @@ the two is the caller's (wait_stream or events); the memory of inputs and output
 
 None of them is part of an autograd graph: gradients are outputs like others.  gated_ffn, rms_norm, rms_norm_int8, quantize_rows, int8_linear,
 log_probs and dropout refuse tensors that require gradients where a graph would be recorded (call them under torch.no_grad(), with the
-backward calls beside them).  adamw_step writes parameters and
+backward calls beside them), and dual tensors of forward-mode differentiation.  The other calls take both and give plain results.  adamw_step writes parameters and
 copies in place and tells autograd so: a graph that has saved one of them refuses its backward pass (an update that is replayed from a
 CUDA graph tells it only at its capture).
 """
@@ -41,6 +41,7 @@ from array import array
 from typing import List, Optional, Sequence, Tuple, Union
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 
 from . import binding as _binding
 from .binding import BMGD_OK, BmgdError
@@ -140,6 +141,10 @@ def _no_graph(name: str, *tensors: Optional[torch.Tensor]) -> None:
         for t in tensors:
             if t is not None and t.requires_grad:
                 raise ValueError(f"{name} records no autograd graph: call it under torch.no_grad(), or with detached tensors")
+    if getattr(_forward_ad, "_current_level", 0) >= 0:  # (inside forward_ad.dual_level(); no_grad() does not stop it)
+        for t in tensors:
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError(f"{name} records no autograd graph: call it without tangents, on the primal of a dual tensor")
 
 
 def _vector(t: Optional[torch.Tensor], name: str, size: int, dtype: torch.dtype, device: torch.device) -> int:
