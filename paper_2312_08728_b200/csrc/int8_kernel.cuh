@@ -175,13 +175,13 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_kernel(const __grid_cons
             const int own = (int)threadIdx.x - 128;
             if (own < BN) {
                 const int col = n0 + own;
-                ws[own] = col < P.N ? __ldg(P.w_scale + col) : 0.f;
-                ws[BN + own] = P.bias && col < P.N ? __ldg(P.bias + col) : 0.f;
+                ws[own] = col < P.N ? __ldca(P.w_scale + col) : 0.f;
+                ws[BN + own] = P.bias && col < P.N ? __ldca(P.bias + col) : 0.f;
             }
             asm volatile("bar.sync 1, 256;" ::: "memory");
             const long long row0 = (long long)m0 + rank * 128 + quarter * 32;
             const int rows = (int)max(0ll, min(32ll, P.M - row0));
-            const float qs = lane < rows ? __ldg(P.q_scale + row0 + lane) : 0.f;
+            const float qs = lane < rows ? __ldca(P.q_scale + row0 + lane) : 0.f;
             ffn_wait(acc_full + 8 * acc, acc_phase, w);
             w.aborted = __any_sync(0xFFFFFFFFu, w.aborted);
             if (w.aborted) {  // this warp's part of this tile, and of those that follow, has not been computed: NaN
@@ -324,8 +324,8 @@ __device__ __forceinline__ void int8_few_finish(const Int8Params& P, uint32_t su
     float ws[4], b[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        ws[e] = e < left ? __ldg(P.w_scale + f + e) : 0.f;
-        b[e] = e < left && P.bias ? __ldg(P.bias + f + e) : 0.f;
+        ws[e] = e < left ? __ldca(P.w_scale + f + e) : 0.f;
+        b[e] = e < left && P.bias ? __ldca(P.bias + f + e) : 0.f;
     }
     for (int i0 = part * (kInt8FewThreads / 32) + warp; i0 < some; i0 += step * kRows) {
         int4 y[kRows][SP];
@@ -334,7 +334,7 @@ __device__ __forceinline__ void int8_few_finish(const Int8Params& P, uint32_t su
         for (int r = 0; r < kRows; ++r) {
             if (r > 0 && i0 + r * step >= some) continue;
             const uint32_t at = sums + (uint32_t)(((i0 + r * step) * kInt8Part + lane * 4) * 4);
-            qs[r] = __ldg(P.q_scale + first_row + i0 + r * step);
+            qs[r] = __ldca(P.q_scale + first_row + i0 + r * step);
 #pragma unroll
             for (int c = 0; c < SP; ++c)
                 if (c < S) y[r][c] = ld_cluster_ints(at, c);
@@ -421,7 +421,7 @@ struct Int8FewFill {
             for (int u = u0; u < min(kEach, u0 + kBatch); ++u) {
                 const uint4* two = reinterpret_cast<const uint4*>(row[u] + k * kInt8BK - ((uintptr_t)row[u] & 15u));
 #pragma unroll
-                for (int e = 0; e < 2; ++e) v[u - u0][e] = pieces >> u & 1u ? __ldg(two + e) : make_uint4(0, 0, 0, 0);
+                for (int e = 0; e < 2; ++e) v[u - u0][e] = pieces >> u & 1u ? __ldca(two + e) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int u = u0; u < min(kEach, u0 + kBatch); ++u) {
@@ -447,7 +447,7 @@ struct Int8FewFill {
             const signed char* p = place(P, f0, r0, i >> 3, r, rows) + at;
             uint32_t byte[16], x[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int b = 0; b < 16; ++b) byte[b] = b < count ? (uint32_t)(unsigned char)__ldg(p + b) : 0u;
+            for (int b = 0; b < 16; ++b) byte[b] = b < count ? (uint32_t)(unsigned char)__ldca(p + b) : 0u;
 #pragma unroll
             for (int b = 0; b < 16; ++b) x[b / 4] |= byte[b] << (8 * (b % 4));
             put(stage, i, x);
@@ -671,11 +671,11 @@ __global__ void __launch_bounds__(512, 2) int8_vec_kernel(const __grid_constant_
 #pragma unroll
             for (int m = 0; m < M; ++m) sum[m] += x * reinterpret_cast<const signed char*>(int8_tokens + m * pieces)[c];
         }
-        const float ws = __ldg(P.w_scale + n), bias = P.bias ? __ldg(P.bias + n) : 0.f;
+        const float ws = __ldca(P.w_scale + n), bias = P.bias ? __ldca(P.bias + n) : 0.f;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             const int total = __reduce_add_sync(0xFFFFFFFFu, sum[m]);
-            if (lane == m) int8_store1(P.out, P.type, m * P.ld_out + n, (float)total * __ldg(P.q_scale + m) * ws + bias);
+            if (lane == m) int8_store1(P.out, P.type, m * P.ld_out + n, (float)total * __ldca(P.q_scale + m) * ws + bias);
         }
     }
 }

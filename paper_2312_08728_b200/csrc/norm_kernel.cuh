@@ -60,17 +60,17 @@ __device__ __forceinline__ void load_weights(const void* weight, int f32, int c,
         if (((uintptr_t)p & 15u) == 0) {
 #pragma unroll
             for (int e = 0; e < VE; e += 4) {
-                const float4 v = __ldg(reinterpret_cast<const float4*>(p + e));
+                const float4 v = __ldca(reinterpret_cast<const float4*>(p + e));
                 w[e] = v.x; w[e + 1] = v.y; w[e + 2] = v.z; w[e + 3] = v.w;
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) w[e] = __ldg(p + e);
+            for (int e = 0; e < VE; ++e) w[e] = __ldca(p + e);
         }
     } else {
         const T* p = static_cast<const T*>(weight) + c;
         if (((uintptr_t)p & 15u) == 0) {
-            unpack_piece<T>(__ldg(reinterpret_cast<const uint4*>(p)), w);
+            unpack_piece<T>(__ldca(reinterpret_cast<const uint4*>(p)), w);
         } else {
 #pragma unroll
             for (int e = 0; e < VE; ++e) w[e] = to_f32(p[e]);
@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(1024) norm_back_long_kernel(const __grid_const
 
 // dw from the blocks' sums: 32 columns to a block, 32 threads to a column
 template <typename T>
-__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* __restrict__ part, int blocks, int width, void* __restrict__ dweight, int f32) {
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const float* part, int blocks, int width, void* dweight, int f32) {
     __shared__ float cells[32][33];
     wait_for_previous_kernel();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
