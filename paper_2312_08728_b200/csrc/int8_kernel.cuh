@@ -599,16 +599,33 @@ __global__ void __launch_bounds__(kInt8FewThreads, 2) int8_few_kernel(const __gr
 // ---------------------------------------------------------------- one or two tokens
 // A warp to a channel, its row of weights read in batches of 32 x 4 pieces of 16 bytes, the next batch (or channel) under way while this
 // one is multiplied on the integer dot-product units; the tokens stand in shared memory.  Bound by reading the weights once.  No tensor maps, barriers or
-// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 9.2 us where int8_few_kernel took 11.8 (a launch by itself 2.3,
+// tensor memory to set up, and no split along the contraction: 1 x 4096 -> 11008 8.7 us where int8_few_kernel took 11.8 (a launch by itself 2.3,
 // reading the weights at the copy rate 6.9); in batches of 8 pieces with half as many warps 10.9.  Four tokens took 16.0 that way where int8_few_kernel
 // takes 12.0: each is read from shared memory as often as the weights from memory.
 constexpr int kInt8Vec = 4;
+// Weights that all warps together bring to L2 before they wait for the kernel in front, in lines of 128 bytes: a quarter of L2, so that none is gone again when it is read.  1 x 4096 ->
+// 11008 9.9 us without any, 8.7 with 32 MB, 9.1 with 64 or without a bound (45 MB); 1 x 16384 -> 4096 13.5, 11.6, 13.3; 1 x 65552 -> 11008 117, 117, 119, 127 without a bound (310 MB).
+constexpr long long kInt8Ahead = (32ll << 20) / 128;
+constexpr __host__ __device__ int int8_ahead(long long warps) { return (int)(kInt8Ahead / warps); }
+// of the next row, `left` being a warp's share that is left
+constexpr __host__ __device__ int int8_ahead_lines(int inputs, int left) { return (inputs + 127) / 128 < left ? (inputs + 127) / 128 : left; }
+constexpr bool int8_ahead_holds() {
+    for (int inputs : {1, 127, 128, 129, 4096, 11008, 16000, 65552, 102400})
+        for (int warps : {1, 37, 296 * 8, 296 * 13, 296 * 16}) {
+            long long all = 0;
+            for (int left = int8_ahead(warps), rows = 0; rows < 4 && left > 0; left -= int8_ahead_lines(inputs, left), ++rows) all += warps * (long long)int8_ahead_lines(inputs, left);
+            if (all > kInt8Ahead) return false;
+        }
+    return true;
+}
+static_assert(int8_ahead_holds(), "all warps' lines together stay within the bound");
 struct Int8VecParams {
     const signed char *q, *w;               // rows of w on 16-byte boundaries
     const float *q_scale, *w_scale, *bias;
     void* out;
     long long ld_q, ld_w, ld_out;
     int N, K, type;
+    int ahead;                              // lines of weights that a warp brings to L2 before it waits
 };
 template <int M>
 __global__ void __launch_bounds__(512, 2) int8_vec_kernel(const __grid_constant__ Int8VecParams P) {
@@ -616,9 +633,9 @@ __global__ void __launch_bounds__(512, 2) int8_vec_kernel(const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const int pieces = (P.K + 15) / 16, full = P.K / 16, batches = (full + 32 * kInt8Vec - 1) / (32 * kInt8Vec), step = (int)gridDim.x * warps;
     int n = (int)blockIdx.x * warps + warp;
-    // Weights on their way to L2 while the kernel in front still runs: up to 16 KB a warp, 64 MB in all (9.9 us to 9.2).  It reads nothing.
-    for (int c = n, taken = 0; c < P.N && taken < 16384; c += step, taken += P.K)
-        for (int b = lane * 128; b < P.K; b += 32 * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(P.w + c * P.ld_w + b));
+    // weights on their way to L2 while the kernel in front still runs; it reads nothing
+    for (int c = n, left = P.ahead; c < P.N && left > 0; c += step, left -= int8_ahead_lines(P.K, left))
+        for (int b = lane; b < int8_ahead_lines(P.K, left); b += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(P.w + c * P.ld_w + b * 128));
     wait_for_previous_kernel();
     let_next_kernel_start();
     uint4 v[kInt8Vec];

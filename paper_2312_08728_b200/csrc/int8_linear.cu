@@ -143,7 +143,7 @@ int check(const bmgd_quantized_linear_args* a, bool pointers) {
 // One or two tokens: two blocks to an SM, with as many warps each (8 to 16) as let the channels come out most evenly, 2 x 148 x W of them at a
 // time.  (11008 channels: 13 warps, three each; 4096: 14, one each.)
 template <int M>
-int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
+int launch_vec(Int8VecParams P, const Device& dev, cudaStream_t s) {
     const int blocks = 2 * dev.sms;
     int best = 8;
     if (P.N <= blocks * 8) {
@@ -164,7 +164,9 @@ int launch_vec(const Int8VecParams& P, const Device& dev, cudaStream_t s) {
     }
     cudaLaunchConfig_t lc{};
     cudaLaunchAttribute at[2];
-    launch_config(&lc, at, dim3((unsigned)std::min((P.N + best - 1) / best, blocks)), best * 32, bytes, 1, s);
+    const int grid = std::min((P.N + best - 1) / best, blocks);
+    P.ahead = int8_ahead(grid * best);
+    launch_config(&lc, at, dim3((unsigned)grid), best * 32, bytes, 1, s);
     if (cudaLaunchKernelEx(&lc, fn, P) != cudaSuccess) { cudaGetLastError(); return BMGD_ERR_CUDA; }
     return BMGD_OK;
 }
@@ -179,7 +181,7 @@ int product(const bmgd_quantized_linear_args* a, Space* space, bool run, const D
     if (few_enough(a) && dev.budget_ns == 0) {  // (the others' waits are what a budget is given to test)
         if (!run) return BMGD_OK;
         const Int8VecParams V{reinterpret_cast<const signed char*>(a->codes), reinterpret_cast<const signed char*>(a->weight), a->scale, a->weight_scale, a->bias, a->y,
-                              a->ld_codes, a->ld_weight, a->ld_y, a->outputs, a->inputs, a->type};
+                              a->ld_codes, a->ld_weight, a->ld_y, a->outputs, a->inputs, a->type, 0};
         return a->rows == 1 ? launch_vec<1>(V, dev, s) : launch_vec<2>(V, dev, s);
     }
     const int64_t small = ((a->rows + 127) / 128) * ((a->outputs + 127ll) / 128);
