@@ -382,7 +382,8 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
                     void* dev_scratch, int64_t scratch_bytes, void* stream);
 
 /* Root-mean-square norm of rows with the residual's addition, of one type (all three): with t = x + residual, rounded to the type
- * (t = x without a residual), and s = 1 / sqrt(mean of t^2 + eps),   y = t s weight.  Sums are fp32: values beyond 1.8e19 make s zero.
+ * (t = x without a residual), and s = 1 / sqrt(mean of t^2 + eps),   y = t s weight.  Sums are fp32 (of fp32 rows 64 bits): squares whose
+ * sum (of fp32 rows: whose mean) is beyond 3.4e38 make s zero, and means of squares below 1e-38, where eps is no larger, lose bits.
  * y in the type, or (codes and scale instead) in 8 bits: codes = y * 127 / a to the nearest whole number, scale = a / 127 with a the
  * row's largest magnitude; rows below 2^-120 throughout have codes and scale 0, rows with NaN or Inf codes 0 and scale NaN.
  * Nothing that is written may overlap what is read, or anything else that is written.  Any row strides from `width` on. */
@@ -391,7 +392,7 @@ typedef struct bmgd_rms_norm {
     int32_t width;                       /* 1 to 2^24 */
     int32_t type, weight_type;           /* weight_type: `type` or BMGD_TYPE_F32 */
     int32_t reserved;                    /* must be zero */
-    double eps;                          /* 0 gives NaN for rows of zeros */
+    double eps;                          /* taken in fp32, if it is positive as 2^-149 at least; 0 gives NaN for rows of zeros */
     const void* x;
     const void* residual;                /* NULL: none */
     const void* weight;                  /* [width]; NULL: ones */

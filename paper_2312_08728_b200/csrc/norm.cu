@@ -1,6 +1,7 @@
 // Host side of bmgd_rms_norm_forward, bmgd_rms_norm_backward, bmgd_quantize_rows and bmgd_quantize_weight.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "../../include/bmgd.h"
 #include "norm_kernel.cuh"
@@ -138,7 +139,7 @@ NormParams shared_params(const bmgd_rms_norm* a) {
     NormParams P{};
     P.weight = a->weight;
     P.weight_f32 = a->weight_type == BMGD_TYPE_F32;
-    P.rows = a->rows; P.width = a->width; P.eps = (float)a->eps; P.per_width = 1.f / (float)a->width;
+    P.rows = a->rows; P.width = a->width; P.eps = a->eps > 0.0 ? std::max((float)a->eps, std::numeric_limits<float>::denorm_min()) : 0.f; P.per_width = 1.f / (float)a->width;
     P.rstd = a->rstd;
     P.far = a->rows * a->width * value_bytes(a->type) > kFarBytes;
     return P;
