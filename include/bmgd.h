@@ -384,8 +384,8 @@ int bmgd_adamw_step(const bmgd_adamw_tensor* tensors, int32_t count, const bmgd_
 /* Root-mean-square norm of rows with the residual's addition, of one type (all three): with t = x + residual, rounded to the type
  * (t = x without a residual), and s = 1 / sqrt(mean of t^2 + eps),   y = t s weight.  Sums are fp32 (of fp32 rows 64 bits): squares whose
  * sum (of fp32 rows: whose mean) is beyond 3.4e38 make s zero, and means of squares below 1e-38, where eps is no larger, lose bits.
- * y in the type, or (codes and scale instead) in 8 bits: codes = y * 127 / a to the nearest whole number, scale = a / 127 with a the
- * row's largest magnitude; rows below 2^-120 throughout have codes and scale 0, rows with NaN or Inf codes 0 and scale NaN.
+ * y in the type, or (codes and scale instead) in 8 bits: codes = y ((1 / a) 127) in fp32, rounded to the nearest whole number, scale =
+ * a / 127 with a the row's largest magnitude; rows below 2^-120 throughout have codes and scale 0, rows with NaN or Inf codes 0 and scale NaN.
  * Nothing that is written may overlap what is read, or anything else that is written.  Any row strides from `width` on. */
 typedef struct bmgd_rms_norm {
     int64_t rows;                        /* 0 to 2^31 - 1 */
@@ -432,7 +432,7 @@ int bmgd_quantize_weight(const void* dev_w, int64_t ld_w, int32_t inputs, int32_
                          int64_t ld_codes, float* dev_scale, void* stream);
 
 /* Product in 8-bit integers: y = (codes weight^T) scale_i weight_scale_j + bias_j, codes [rows][inputs], weight
- * [outputs][inputs]; the sums are exact, the rest is fp32, rounded once to `type`.  Operands whose rows do not start on 16-byte
+ * [outputs][inputs]; the sums are exact, the rest is fp32 in this order (a scale beyond 1e29 may leave its range on the way), rounded once to `type`.  Operands whose rows do not start on 16-byte
  * boundaries are copied into the workspace first, unless the tokens or the tiles are few.  y overlaps no operand. */
 typedef struct bmgd_quantized_linear_args {
     int64_t rows;                        /* 0 to 2^31 - 256 */

@@ -15,8 +15,10 @@
 // Alternatives.  The maxima of 32 parts of the row (the threads of equal lane) bound the K-th
 // largest logit from below: at least K of the parts hold a logit at or above the K-th largest of them.  While it reads, a thread leaves the
 // maximum of each of its stretches in shared memory; only stretches that reach the bound are looked at again (a few dozen of a row of independent logits, from L2), what reaches the
-// bound is put aside, and its K largest are ranked by counting.  Rows with more candidates than there is room (thousands of equal logits, a mask that
-// leaves fewer than K) are taken value by value: largest below the last one, with all that equal it.
+// bound is put aside, and its K largest are ranked by counting.  Rows with more candidates than there is room are taken value by value: largest below the last one, with all that equal it.
+// These are rows of thousands of equal logits, or with a mask that leaves fewer than K; rows of 161 to 255 classes in 16-bit types with K above C / 8 (fewer than K of the parts have a logit,
+// so nothing is ruled out); and with K near 32 ordinary ones too: at the lowest of 32 maxima some 130 independent logits are left on average, and often more than 160 (16384 x 4000 with
+// 20 alternatives 78 us, with 32 780; 8191 x 200 16 and 95).
 //
 // A row with NaN or +Inf has NaN for its log probability and entropy; in the order of the alternatives NaN is largest.  A row whose logits are
 // all -Inf has no distribution: log probability and entropy 0, no gradient, alternatives -Inf from class 0 on.
@@ -311,7 +313,7 @@ __device__ __noinline__ RowScore score_careful(const T* z, int C, float m, LogPr
 }
 
 // TH threads to a row (TH = 32: a warp, eight rows to a block), rows taken with the grid's stride: the first pieces of the next row are
-// fetched before this one's sums are joined.  Small blocks with many registers: 8191 x 50257 bf16 took 135 us with 64 threads and 85 registers, 142
+// fetched before this one's sums are joined.  Small blocks with many registers: 8191 x 50257 bf16 took 135 us with 64 threads and 85 registers (by now 132 with 80), 142
 // with 128, 157 with 256; 142 with 64 threads and 64 registers.
 template <typename T, int TH, bool TOP>
 __global__ void __launch_bounds__(TH == 32 ? 256 : TH, TH == 32 ? 3 : TH >= 512 ? 1 : 768 / TH) logprob_kernel(const __grid_constant__ LogProbParams P) {

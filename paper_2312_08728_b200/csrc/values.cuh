@@ -72,7 +72,7 @@ __device__ __forceinline__ uint4 load_piece(const T* p) {
     for (int i = 0; i < Piece<T>::kValues; ++i) t[i] = p[i];
     return w;
 }
-// Results larger than this many bytes are written as data that is not wanted again (the gradient of 8191 x 50257 bf16 logits: 275 us to 255); smaller ones stay
+// Results larger than this many bytes are written as data that is not wanted again (the gradient of 8191 x 50257 bf16 logits: 275 us to 258); smaller ones stay
 // in L2 for the kernel that reads them.
 constexpr long long kFarBytes = 48ll << 20;
 __device__ __forceinline__ void store16(uint4* p, const uint4& w, bool far) {
